@@ -67,6 +67,8 @@ extern "C" {
 #define PDA_DEV_BAD_PAGE 1     /* block_table entry outside [0, num_pages) for a live page     */
 #define PDA_DEV_BAD_SEQ_LEN 2  /* seq_lens[b] > block_table_stride * page_size                 */
 #define PDA_DEV_TIMEOUT 3      /* a bounded wait on an asynchronous copy expired               */
+#define PDA_DEV_NO_PAGES 4     /* paged_build_tables: the free list holds fewer pages than asked */
+#define PDA_DEV_NO_SLOTS 5     /* paged_build_tables: more new tokens than slot_map has room for */
 
 /* KV element types */
 #define PDA_BF16 0
@@ -445,6 +447,144 @@ int pda_debug_wait_timeout(uint32_t polls, int32_t* status, uint64_t* result, pd
  * decode kernels' GB/s are to be read (a copy moves half its bytes as writes and
  * is the lower figure). */
 int pda_debug_read_probe(const void* buf, uint64_t bytes, uint32_t* sink, pda_stream_t stream);
+
+/* ---- Step tables and latent attention ---------------------------------------------
+ *
+ * A latent cache holds, for every token, ONE row shared by all query heads:
+ *     row = [ c (latent_dim elements) | r (rope_dim elements) ]        bf16
+ * c is the compressed vector from which every head's keys and values are projected
+ * (k_nope[h] = Wk[h] c, v[h] = Wv[h] c), r the rotary part of the key, the same for
+ * all heads. (The paper has no counterpart; the calls below are this library's.) The
+ * attention over it has two forms that give the same result:
+ *   expanded  keys [k_nope[h] | r] and values v[h] per head, as the projections leave
+ *             them: latent_prefill_attention, for prompts;
+ *   absorbed  the projections moved to the query and the output (q_latent[h] =
+ *             Wk[h]^T q_nope[h], v-part = Wv[h] out[h]), so that the cached rows
+ *             themselves are keys and values: paged_latent_attention, for decoding.
+ * A step: paged_build_tables -> latent_append -> one of the two. */
+
+/* Element (page, slot, d) of the cache lives at page*page_stride + slot*slot_stride + d,
+ * d < latent_dim + rope_dim. Strides in elements, their byte values multiples of 16.
+ * page_size 1..1024; latent_dim a multiple of 8, 8..1024; rope_dim a multiple of 8,
+ * 0..256. dtype: PDA_BF16. */
+typedef struct pda_latent_desc {
+  int64_t page_stride;
+  int64_t slot_stride;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t latent_dim;
+  int32_t rope_dim;
+  int32_t dtype;
+} pda_latent_desc;
+
+/* The tables of one step, built on the device from request lengths. With P = page_size,
+ * L = seq_lens[b] (length AFTER the step), n = new_lens[b] (tokens of this step, 0..L):
+ *     held = ceil((L - n) / P) pages are in block_table[b] already,
+ *     need = ceil(L / P); entries [held, need) are written with new pages: page k of the
+ *     step, counted in (b, page) order, is free_pages[free_count - 1 - k];
+ *     cu_new[b] = n_0 + ... + n_{b-1}, b = 0 .. batch;
+ *     token t = cu_new[b] + i (i < n) stands at position L - n + i of sequence b:
+ *     positions[t] = L - n + i,
+ *     slot_map[t] = block_table[b][positions[t] / P] * P + positions[t] % P;
+ *     slot_map[t] = positions[t] = -1 for cu_new[batch] <= t < capacity;
+ *     *free_count_out = *free_count - (pages taken).
+ *   free_pages      int32[free_capacity], the free page ids, a stack whose top is at
+ *                   *free_count - 1 (values beyond free_capacity count as free_capacity);
+ *                   read only: to give pages back, write their ids at *free_count onwards
+ *                   and raise it
+ *   free_count_out  may be free_count itself
+ *   slot_map        int32[capacity]; positions int32[capacity] or NULL
+ *   batch           >= 0; page_size 1..1024
+ * A sequence with n < 0, n > L, L < 0 or L > block_table_stride * P gets nothing (n counts as
+ * 0) and *status PDA_DEV_BAD_SEQ_LEN. Where the free list is too short (PDA_DEV_NO_PAGES) or
+ * the tokens are more than capacity (PDA_DEV_NO_SLOTS), no page is taken, the table stays as
+ * it was and every slot_map entry is -1. A page id below 0, or one whose slots pass 2^31 - 1,
+ * gives slot -1 and PDA_DEV_BAD_PAGE. Entries of block_table beyond need are left as they are. */
+int paged_build_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t batch,
+                       int32_t page_size, const int32_t* free_pages, int32_t free_capacity,
+                       const int32_t* free_count, int32_t* free_count_out, int32_t* block_table,
+                       int32_t block_table_stride, int32_t* cu_new, int32_t* slot_map,
+                       int32_t* positions, int32_t capacity, int32_t* status, pda_stream_t stream);
+
+/* Rows of n_tokens new tokens into their slots of the latent cache: for slot_map[t] = s >= 0
+ *     row(s / P, s % P) = [ f(c_new[t]) | rope_new[t] ],
+ *     f(c) = c bytewise (norm_weight NULL), or the root-mean-square norm
+ *     f(c) = bf16(c / sqrt(mean(c^2) + eps) * norm_weight), in 32 bits, rounded once.
+ *   c_new     [n_tokens, latent_dim] bf16, c_stride elements from token to token
+ *   rope_new  [n_tokens, rope_dim] bf16, rope_stride elements from token to token (both may
+ *             be parts of one buffer; NULL with rope_dim 0)
+ *   slot_map  int32[n_tokens]; entries < 0 are skipped, entries beyond the cache are
+ *             skipped with PDA_DEV_BAD_PAGE. Entries >= 0 must be distinct.
+ *   eps       >= 0, finite */
+int latent_append(const void* c_new, int64_t c_stride, const void* rope_new, int64_t rope_stride,
+                  void* cache, const pda_latent_desc* desc, const void* norm_weight, float eps,
+                  const int32_t* slot_map, int32_t n_tokens, int32_t* status,
+                  pda_stream_t stream);
+
+/* Absorbed attention of n_query_tokens tokens per sequence over the paged latent cache. Query
+ * token i of sequence b stands at position L - n + i (L = seq_lens[b], n = n_query_tokens; the
+ * cache holds all L rows) and attends tokens j <= L - n + i:
+ *     out[b,i,h,:] = softmax_j( scale * (q_latent[b,i,h] . c_j + q_rope[b,i,h] . r_j) ) . c_j
+ *   q_latent  [batch, n, num_q_heads, latent_dim] bf16: element (token, head, d) at
+ *             token*ql_token_stride + head*ql_head_stride + d, token = b*n + i
+ *   q_rope    [batch, n, num_q_heads, rope_dim] bf16, likewise (NULL with rope_dim 0)
+ *   out       [batch, n, num_q_heads, latent_dim] bf16, likewise
+ *             (strides: multiples of 8 elements, >= 0; out rows must not overlap)
+ *   block_table, seq_lens  as in paged_decode_attention, with desc's page size
+ *   workspace device memory of pda_latent_workspace_bytes(...) bytes, 256-byte aligned. Need
+ *             not be initialised, holds nothing between calls; calls that can overlap on the
+ *             GPU (graphs replayed side by side included) need separate ones.
+ *   flags     PDA_FLAG_FORCE_GENERIC
+ * Rows whose range is empty (L = 0, or i < n - L) are zero. L < 0 counts as 0. A bad page id or
+ * length zeroes the sequence's rows and sets *status. Every slot holding a live token must be
+ * finite; all other slots, pages and table entries may hold anything.
+ * 1 <= n <= 4096, batch * n <= 65535. The tensor-core kernel (tcgen05) takes latent_dim 128, 256,
+ * 384 or 512 with rope_dim 64 and page sizes 16, 32, 64, 128 and larger powers of two; other
+ * shapes run on a plain kernel. Results do not depend on timing: sums are taken in an order
+ * fixed by the lengths and the number of SMs. */
+int paged_latent_attention(const void* q_latent, int64_t ql_token_stride, int64_t ql_head_stride,
+                           const void* q_rope, int64_t qr_token_stride, int64_t qr_head_stride,
+                           const void* cache, const pda_latent_desc* desc,
+                           const int32_t* block_table, int32_t block_table_stride,
+                           const int32_t* seq_lens, int32_t batch, int32_t num_q_heads,
+                           int32_t n_query_tokens, float scale, void* out,
+                           int64_t out_token_stride, int64_t out_head_stride, void* workspace,
+                           int64_t workspace_bytes, uint32_t flags, int32_t* status,
+                           pda_stream_t stream);
+
+/* Bytes of workspace that paged_latent_attention needs, or PDA_ERR_INVALID_ARG. */
+int64_t pda_latent_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t n_query_tokens,
+                                   int32_t latent_dim);
+
+/* Expanded attention of packed ragged sequences (prompts, or chunks of prompts behind a
+ * context): sequence b has query tokens cu_q[b] .. cu_q[b+1]-1 and key tokens cu_k[b] ..
+ * cu_k[b+1]-1, aligned at their ends: with nq and nk of them, query i attends keys
+ * j <= nk - nq + i:
+ *     out[i,h,:] = softmax_j( scale * (q[i,h,:nope] . k_nope[j,h] + q[i,h,nope:] . k_rope[j]) ) . v[j,h]
+ *   q       [total_q, num_heads, nope_dim + rope_dim] bf16
+ *   k_nope  [total_k, num_heads, nope_dim], v [total_k, num_heads, v_dim] bf16 (may be the two
+ *           parts of one buffer); k_rope [total_k, rope_dim], one for all heads (NULL with
+ *           rope_dim 0)
+ *   out     [total_q, num_heads, v_dim] bf16
+ *           Strides in elements, multiples of 8, >= 0; rows of out must not overlap.
+ *   cu_q, cu_k  device int32[batch + 1], ascending
+ *   max_q   an upper bound of the sequences' query tokens (host: the launch is sized by it)
+ * Rows without any key are zero. Rows of out outside all sequences are left as they were, and
+ * rows of the inputs outside all sequences may hold anything. A sequence whose ranges do not
+ * lie in the arrays or that has more than max_q query tokens is zeroed (as far as its rows
+ * lie within the array and max_q) and sets *status PDA_DEV_BAD_SEQ_LEN.
+ * nope_dim, v_dim: multiples of 8 up to 512; rope_dim a multiple of 8 up to 256; batch and
+ * num_heads <= 65535. Dims 128, 64 and 128 run on the tensor-core kernel (tcgen05),
+ * others and PDA_FLAG_FORCE_GENERIC on a plain kernel. */
+int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                             const void* k_nope, int64_t kn_token_stride, int64_t kn_head_stride,
+                             const void* k_rope, int64_t kr_token_stride, const void* v,
+                             int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu_q,
+                             const int32_t* cu_k, int32_t batch, int32_t num_heads,
+                             int32_t nope_dim, int32_t rope_dim, int32_t v_dim, int32_t max_q,
+                             int32_t total_q, int32_t total_k, float scale, void* out,
+                             int64_t out_token_stride, int64_t out_head_stride, uint32_t flags,
+                             int32_t* status, pda_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -7,6 +7,7 @@ fails, a ``RuntimeError`` is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -19,14 +20,17 @@ PDA_BF16, PDA_FP8_E4M3 = 0, 1
 PDA_FLAG_FORCE_GENERIC = 1
 PDA_FLAG_MQ_MMA_SYNC = 2
 PDA_FLAG_MQ_ONE_UNIT = 4
-DEV_STATUS = {0: "ok", 1: "bad page id", 2: "seq_len exceeds block table", 3: "copy wait timed out"}
+DEV_STATUS = {0: "ok", 1: "bad page id", 2: "seq_len exceeds block table", 3: "copy wait timed out",
+              4: "too few free pages", 5: "too few slot map entries"}
 
 EXPORTS = ["pda_version", "pda_status_string", "pda_max_chunks", "kv_append",
            "paged_decode_attention", "paged_decode_reduce", "paged_decode_step_host",
            "pda_debug_e4m3_decode", "paged_decode_attention_static", "pda_workspace_ints",
            "paged_decode_step", "pda_advance_seq_lens", "paged_window_decode_attention", "kv_append_tokens",
            "paged_verify_attention", "paged_prefix_decode_attention", "kv_append_fp8", "kv_append_tokens_fp8",
-           "pda_set_persistent_threshold", "pda_debug_wait_timeout", "pda_debug_read_probe"]
+           "pda_set_persistent_threshold", "pda_debug_wait_timeout", "pda_debug_read_probe",
+           "paged_build_tables", "latent_append", "paged_latent_attention", "pda_latent_workspace_bytes",
+           "latent_prefill_attention"]
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 
 
@@ -34,6 +38,11 @@ class CacheDesc(C.Structure):
     _fields_ = [("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64),
                 ("num_pages", C.c_int32), ("page_size", C.c_int32), ("num_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class LatentDesc(C.Structure):
+    _fields_ = [("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("num_pages", C.c_int32),
+                ("page_size", C.c_int32), ("latent_dim", C.c_int32), ("rope_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -78,6 +87,15 @@ def lib():
         L.pda_debug_read_probe.argtypes = [vp, C.c_uint64, vp, vp]
         L.paged_decode_attention_static.argtypes = [vp, vp, vp, dp, vp, vp, vp, i32, vp, i32, i32,
                                                     f32, i32, i32, vp, vp, vp]
+        i64, lp = C.c_int64, C.POINTER(LatentDesc)
+        L.paged_build_tables.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp]
+        L.latent_append.argtypes = [vp, i64, vp, i64, vp, lp, vp, f32, vp, i32, vp, vp]
+        L.paged_latent_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, lp, vp, i32, vp, i32, i32, i32, f32,
+                                             vp, i64, i64, vp, i64, u32, vp, vp]
+        L.pda_latent_workspace_bytes.restype = i64
+        L.pda_latent_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.latent_prefill_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, vp, i32, i32,
+                                               i32, i32, i32, i32, i32, i32, f32, vp, i64, i64, u32, vp, vp]
         _lib = L
     return _lib
 
@@ -367,3 +385,187 @@ def kv_append_tokens_fp8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, block
 def set_persistent_threshold(min_units_per_cta: int):
     """Units per resident CTA from which the unsplit fused step uses the persistent kernel (0: always)."""
     _check(lib().pda_set_persistent_threshold(int(min_units_per_cta)), "pda_set_persistent_threshold")
+
+
+_same_context = contextlib.nullcontext()
+
+
+def _device_call(t):
+    """The device the call's tensors live on becomes current for the call (streams, launches)."""
+    return _same_context if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _same_device(*tensors):
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("expected CUDA tensors")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+        dev = t.device
+
+
+def _int32(*tensors):
+    for t in tensors:
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError("expected contiguous int32 tensors")
+
+
+def _bf16_rows(name, t):
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name}: expected bfloat16, got {t.dtype}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+
+
+def latent_desc(cache: torch.Tensor, latent_dim: int) -> LatentDesc:
+    """Descriptor of a ``[num_pages, P, latent_dim + rope_dim]`` bf16 latent cache."""
+    if cache.dim() != 3:
+        raise ValueError("a latent cache is [num_pages, page_size, latent_dim + rope_dim]")
+    _bf16_rows("cache", cache)
+    n, P, W = cache.shape
+    # (a dimension of extent 1 may carry any stride: the one of the dense layout is taken)
+    slot = cache.stride(1) if P > 1 else max(cache.stride(1), W)
+    page = cache.stride(0) if n > 1 else max(cache.stride(0), P * slot)
+    return LatentDesc(page, slot, n, P, int(latent_dim), W - int(latent_dim), PDA_BF16)
+
+
+def _check_table(block_table, batch):
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise ValueError("block_table: expected int32 [batch, pages]")
+    if block_table.shape[1] > 1 and block_table.stride(1) != 1:
+        raise ValueError("block_table: rows must be contiguous")
+    # the row stride is also the row's capacity: a view with a longer stride than its row would be read past it
+    if batch > 1 and block_table.stride(0) != block_table.shape[1]:
+        raise ValueError("block_table: rows must follow one another (pass a contiguous table)")
+    return block_table.shape[1]
+
+
+def paged_build_tables(seq_lens, new_lens, page_size, free_pages, free_count, block_table, cu_new, slot_map,
+                       positions=None, free_count_out=None, status=None, stream=None):
+    """A step's block-table rows, cumulative counts, slot map and positions from request lengths, on the device.
+
+    ``free_count`` int32[1] (updated in place unless ``free_count_out`` is given); ``cu_new`` int32[B + 1];
+    ``slot_map`` and ``positions`` int32[capacity]."""
+    B = seq_lens.shape[0]
+    _int32(seq_lens, new_lens, free_pages, free_count, cu_new, slot_map, positions, free_count_out, status)
+    stride = _check_table(block_table, B)
+    if new_lens.shape[0] != B or cu_new.numel() < B + 1 or (positions is not None and positions.numel() < slot_map.numel()):
+        raise ValueError("new_lens, cu_new or positions too short")
+    _same_device(seq_lens, new_lens, free_pages, free_count, block_table, cu_new, slot_map, positions, free_count_out, status)
+    if free_count_out is None:
+        free_count_out = free_count
+    with _device_call(seq_lens):
+        rc = lib().paged_build_tables(_ptr(seq_lens), _ptr(new_lens), B, int(page_size), _ptr(free_pages), free_pages.numel(),
+                                      _ptr(free_count), _ptr(free_count_out), _ptr(block_table), stride, _ptr(cu_new),
+                                      _ptr(slot_map), _ptr(positions), slot_map.numel(), _ptr(status), _stream(stream))
+    _check(rc, "paged_build_tables")
+
+
+def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, status=None, stream=None):
+    """Rows ``[c_new | rope_new]`` (``[T, R]``, ``[T, Dr]``) into the cache slots ``slot_map``; with ``norm_weight``
+    ``[R]`` the latent's root-mean-square norm on the way."""
+    T, R = c_new.shape
+    desc = latent_desc(cache, R)
+    _bf16_rows("c_new", c_new)
+    _int32(slot_map, status)
+    if desc.rope_dim > 0:
+        _bf16_rows("rope_new", rope_new)
+        if tuple(rope_new.shape) != (T, desc.rope_dim):
+            raise ValueError("rope_new: expected [T, rope_dim]")
+    else:
+        rope_new = None
+    if slot_map.numel() != T:
+        raise ValueError("slot_map: expected one entry per token")
+    if norm_weight is not None:
+        _bf16_rows("norm_weight", norm_weight)
+        if norm_weight.numel() != R:
+            raise ValueError("norm_weight: expected [latent_dim]")
+    _same_device(c_new, rope_new, cache, slot_map, norm_weight, status)
+    with _device_call(cache):
+        rc = lib().latent_append(_ptr(c_new), c_new.stride(0), _ptr(rope_new), 0 if rope_new is None else rope_new.stride(0),
+                                 _ptr(cache), C.byref(desc), _ptr(norm_weight), float(eps), _ptr(slot_map), T, _ptr(status),
+                                 _stream(stream))
+    _check(rc, "latent_append")
+
+
+def latent_workspace(batch, num_q_heads, n_query_tokens, latent_dim, device="cuda"):
+    """Workspace of ``paged_latent_attention`` (uninitialised; one per stream of overlapping calls)."""
+    n = int(lib().pda_latent_workspace_bytes(batch, num_q_heads, n_query_tokens, latent_dim))
+    _check(min(n, 0), "pda_latent_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _token_strides(name, t):
+    """(token stride, head stride) of ``[B, T, H, D]``, tokens numbered ``b*T + t``; ``[B, H, D]`` is ``T = 1``."""
+    B, T, H, _ = t.shape
+    if B > 1 and T > 1 and t.stride(0) != T * t.stride(1):
+        raise ValueError(f"{name}: batch and token dimensions must be evenly strided together")
+    token = t.stride(1) if T > 1 else t.stride(0)
+    return (token if B * T > 1 else 0), (t.stride(2) if H > 1 else 0)
+
+
+def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale, out=None, workspace=None, flags=0,
+                           status=None, stream=None):
+    """Absorbed attention over the paged latent cache: ``q_latent [B,T,H,R]`` (or ``[B,H,R]``), ``q_rope [B,T,H,Dr]``;
+    fills and returns ``out`` like ``q_latent``. Without ``workspace`` one is allocated for the call."""
+    if out is None:
+        out = torch.empty(q_latent.shape, dtype=q_latent.dtype, device=q_latent.device)
+    ql, qr, o = (t if t is None or t.dim() == 4 else t.unsqueeze(1) for t in (q_latent, q_rope, out))
+    B, T, H, R = ql.shape
+    desc = latent_desc(cache, R)
+    for name, t in (("q_latent", ql), ("q_rope", qr), ("out", o)):
+        if t is not None:
+            _bf16_rows(name, t)
+    if desc.rope_dim > 0 and tuple(qr.shape) != (B, T, H, desc.rope_dim):
+        raise ValueError("q_rope: expected [batch, tokens, heads, rope_dim]")
+    if o.shape != ql.shape:
+        raise ValueError("out: expected the shape of q_latent")
+    _int32(seq_lens, status)
+    if seq_lens.numel() != B:
+        raise ValueError("seq_lens: expected one entry per sequence")
+    stride = _check_table(block_table, B)
+    qls, qrs, os_ = _token_strides("q_latent", ql), (0, 0) if desc.rope_dim == 0 else _token_strides("q_rope", qr), _token_strides("out", o)
+    if workspace is None:
+        workspace = latent_workspace(B, H, T, R, device=cache.device)
+    _same_device(ql, qr, o, cache, block_table, seq_lens, workspace, status)
+    with _device_call(cache):
+        rc = lib().paged_latent_attention(
+            _ptr(ql), qls[0], qls[1], None if desc.rope_dim == 0 else _ptr(qr), qrs[0], qrs[1], _ptr(cache), C.byref(desc),
+            _ptr(block_table), stride, _ptr(seq_lens), B, H, T, float(scale), _ptr(o), os_[0], os_[1],
+            _ptr(workspace), workspace.numel() * workspace.element_size(), flags, _ptr(status), _stream(stream))
+    _check(rc, "paged_latent_attention")
+    return out
+
+
+def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out=None, flags=0, status=None, stream=None):
+    """Expanded causal attention over packed sequences: ``q [Tq,H,Dn+Dr]``, ``k_nope [Tk,H,Dn]``, ``k_rope [Tk,Dr]``,
+    ``v [Tk,H,Dv]``, ``cu_q``/``cu_k`` int32[B + 1]; fills and returns ``out [Tq,H,Dv]``."""
+    tq, H, D = q.shape
+    tk, _, dn = k_nope.shape
+    dv, dr = v.shape[2], D - dn
+    if out is None:
+        out = torch.empty((tq, H, dv), dtype=q.dtype, device=q.device)
+    for name, t, shape in (("q", q, (tq, H, D)), ("k_nope", k_nope, (tk, H, dn)), ("v", v, (tk, H, dv)), ("out", out, (tq, H, dv)),
+                           ("k_rope", k_rope if dr else None, (tk, dr))):
+        if t is not None:
+            _bf16_rows(name, t)
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name}: expected {shape}")
+    _int32(cu_q, cu_k, status)
+    if cu_q.numel() != cu_k.numel() or cu_q.numel() < 1:
+        raise ValueError("cu_q and cu_k: expected batch + 1 entries each")
+    _same_device(q, k_nope, k_rope if dr else None, v, out, cu_q, cu_k, status)
+
+    def st(t, i):
+        return t.stride(i) if t.shape[i] > 1 else 0
+
+    with _device_call(q):
+        rc = lib().latent_prefill_attention(
+            _ptr(q), st(q, 0), st(q, 1), _ptr(k_nope), st(k_nope, 0), st(k_nope, 1), _ptr(k_rope) if dr else None,
+            st(k_rope, 0) if dr else 0, _ptr(v), st(v, 0), st(v, 1), _ptr(cu_q), _ptr(cu_k), cu_q.numel() - 1, H, dn, dr, dv,
+            int(max_q), tq, tk, float(scale), _ptr(out), st(out, 0), st(out, 1), flags, _ptr(status), _stream(stream))
+    _check(rc, "latent_prefill_attention")
+    return out

@@ -168,6 +168,8 @@ const char* pda_status_string(int code) {
     case PDA_DEV_BAD_PAGE: return "device: block_table entry out of range";
     case PDA_DEV_BAD_SEQ_LEN: return "device: seq_len exceeds block_table capacity";
     case PDA_DEV_TIMEOUT: return "device: bounded wait on an asynchronous copy expired";
+    case PDA_DEV_NO_PAGES: return "device: fewer free pages than the step needs";
+    case PDA_DEV_NO_SLOTS: return "device: more new tokens than the slot map holds";
     default: return code > 0 ? "cuda error or unknown device status" : "unknown error";
   }
 }

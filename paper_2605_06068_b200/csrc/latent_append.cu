@@ -1,0 +1,82 @@
+// latent_append: the step's rows [c | rope key] into the slots of the latent cache, the latent optionally
+// divided by its root mean square and multiplied by a weight on the way. One warp per token, 16-byte
+// accesses; the row stays in registers between the sum of squares and the store, so the bytes move once.
+#include "latent.cuh"
+
+namespace pda {
+
+namespace {
+
+constexpr int kAppWarps = 4;
+constexpr int kAppMaxVec = 4;  // 16-byte vectors of the latent per lane: latent_dim <= 1024
+
+template <bool kNorm>
+__global__ void __launch_bounds__(kAppWarps * 32) latent_append_kernel(LatentAppendParams p) {
+  const int lane = threadIdx.x & 31;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kAppWarps + (threadIdx.x >> 5);
+  if (t >= p.n_tokens) return;
+  const int slot = p.slot_map[t];
+  const int cv = p.geom.latent_dim / 8, rv = p.geom.rope_dim / 8;
+  const uint4* c = reinterpret_cast<const uint4*>(p.c_new + t * p.c_stride);
+  const uint4* r = reinterpret_cast<const uint4*>(p.rope_new + t * p.rope_stride);
+  uint4 x[kAppMaxVec];
+#pragma unroll
+  for (int i = 0; i < kAppMaxVec; ++i) x[i] = lane + i * 32 < cv ? c[lane + i * 32] : make_uint4(0, 0, 0, 0);
+  const uint4 rope = lane < rv ? r[lane] : make_uint4(0, 0, 0, 0);
+  if (slot < 0) return;  // a padding entry
+  if (slot >= static_cast<int64_t>(p.geom.num_pages) * p.geom.page_size) {
+    if (lane == 0) report(p.status, PDA_DEV_BAD_PAGE);
+    return;
+  }
+  if constexpr (kNorm) {
+    float ss = 0.f;  // 32 bits throughout; padding vectors add zero
+#pragma unroll
+    for (int i = 0; i < kAppMaxVec; ++i) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
+        ss = fmaf(lo, lo, ss);
+        ss = fmaf(hi, hi, ss);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    const float inv = 1.f / sqrtf(ss / static_cast<float>(p.geom.latent_dim) + p.eps);
+    const uint4* wv = reinterpret_cast<const uint4*>(p.norm_weight);
+#pragma unroll
+    for (int i = 0; i < kAppMaxVec; ++i) {
+      if (lane + i * 32 < cv) {
+        const uint4 g = __ldg(wv + lane + i * 32);
+        const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
+        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // one rounding to bf16, at the end
+          const float lo = __uint_as_float(w[e] << 16) * inv * __uint_as_float(gw[e] << 16);
+          const float hi = __uint_as_float(w[e] & 0xffff0000u) * inv * __uint_as_float(gw[e] & 0xffff0000u);
+          const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+          w[e] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  const int page = slot / p.geom.page_size;
+  uint4* dst = reinterpret_cast<uint4*>(p.cache + page * p.geom.page_stride +
+                                        static_cast<int64_t>(slot - page * p.geom.page_size) * p.geom.slot_stride);
+#pragma unroll
+  for (int i = 0; i < kAppMaxVec; ++i)
+    if (lane + i * 32 < cv) dst[lane + i * 32] = x[i];
+  if (lane < rv) dst[cv + lane] = rope;
+}
+
+}  // namespace
+
+cudaError_t launch_latent_append(const LatentAppendParams& p, cudaStream_t stream) {
+  const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(p.n_tokens) + kAppWarps - 1) / kAppWarps);
+  if (p.norm_weight) latent_append_kernel<true><<<blocks, kAppWarps * 32, 0, stream>>>(p);
+  else latent_append_kernel<false><<<blocks, kAppWarps * 32, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace pda

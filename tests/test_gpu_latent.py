@@ -1,0 +1,470 @@
+"""The latent-attention operators and the step tables on the GPU, against plain references in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import latent_util as U
+from paper_2605_06068_b200 import binding as pda
+
+pytestmark = pytest.mark.gpu
+
+GENERIC = pda.PDA_FLAG_FORCE_GENERIC
+
+
+def randn(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale).to(torch.bfloat16)
+
+
+def ints(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+# ---- step tables -----------------------------------------------------------------------------------
+
+def run_tables(L, n, P, pad=0, spare=5, in_place=False, seed=0):
+    L, n = list(map(int, L)), list(map(int, n))
+    g = np.random.default_rng(seed)
+    held = [-(-(a - b) // P) for a, b in zip(L, n)]
+    need = [-(-a // P) for a in L]
+    pool = sum(need) + spare
+    perm = g.permutation(pool).astype(np.int32)
+    table = np.full((len(L), max(need + [0]) + 2), -7, dtype=np.int32)
+    at = 0
+    for b, h in enumerate(held):
+        table[b, :h] = perm[at:at + h]
+        at += h
+    free = perm[at:]
+    cap = sum(n) + pad
+    dt, cu = ints(table), torch.full((len(L) + 1,), -9, dtype=torch.int32, device="cuda")
+    slots, pos = (torch.full((cap,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    cnt, status = ints([len(free)]), ints([0])
+    out = cnt if in_place else ints([-9])
+    pda.paged_build_tables(ints(L), ints(n), P, ints(free), cnt, dt, cu, slots, positions=pos, free_count_out=None if in_place else out,
+                           status=status)
+    rt, rcu, rs, rp, rc = U.tables(L, n, P, free, len(free), table, cap)
+    assert int(status.item()) == 0
+    assert (dt.cpu().numpy() == rt).all() and cu.tolist() == rcu and slots.tolist() == rs and pos.tolist() == rp
+    assert out.item() == rc
+
+
+@pytest.mark.parametrize("P", [1, 16, 24, 64])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_tables_small(P, in_place):
+    run_tables([1, 16, 17, 64, 65, 100, 33, 0], [1, 16, 1, 0, 65, 36, 33, 0], P, pad=3, in_place=in_place)
+    run_tables([1], [1], P, in_place=in_place)
+    run_tables([500], [500], P, in_place=in_place)
+
+
+@pytest.mark.parametrize("B", [31, 1024, 1025, 2500])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_tables_many(B, in_place):
+    g = np.random.default_rng(B)
+    L = g.integers(0, 90, size=B)
+    n = np.where(g.random(B) < 0.3, 1, g.integers(0, 90, size=B))
+    run_tables(L, np.minimum(n, L), 16, pad=int(g.integers(0, 5000)), in_place=in_place, seed=B)
+
+
+def test_tables_refuse_on_the_device():
+    P, free = 16, list(range(100, 110))
+
+    def call(L, n, table=None, count=10, cap=64, freel=free, stride=4):
+        B = len(L)
+        dt = ints(np.full((B, stride), 5) if table is None else table)
+        cu, slots, out, st = ints([0] * (B + 1)), ints([0] * cap), ints([0]), ints([0])
+        pda.paged_build_tables(ints(L), ints(n), P, ints(freel), ints([count]), dt, cu, slots, free_count_out=out, status=st)
+        return dt.cpu().numpy(), cu.tolist(), slots.tolist(), out.item(), st.item()
+
+    # too few pages: nothing is taken
+    t, cu, slots, cnt, st = call([64, 64, 64], [64, 64, 64], cap=200)
+    assert st == 4 and (t == 5).all() and set(slots) == {-1} and cnt == 10 and cu == [0, 64, 128, 192]
+    # a count beyond the list, and below zero
+    assert call([64, 64, 64], [64, 64, 64], count=1000, cap=200)[4] == 4
+    assert call([16], [16], count=-3)[4] == 4
+    # too few slots
+    t, cu, slots, cnt, st = call([20, 20], [20, 20], cap=39)
+    assert st == 5 and (t == 5).all() and set(slots) == {-1} and cnt == 10
+    # lengths that cannot be: the others go ahead
+    for L, n in ((-1, 0), (5, 6), (5, -1), (65, 1)):
+        t, cu, slots, cnt, st = call([3, L, 18], [3, n, 2])
+        assert st == 2 and cu == [0, 3, 3, 5] and cnt == 8
+        assert slots[:5] == [109 * 16, 109 * 16 + 1, 109 * 16 + 2, 108 * 16, 108 * 16 + 1]
+    # page ids that no slot number can hold
+    t, cu, slots, cnt, st = call([17, 3], [1, 1], table=[[5] * 4, [-4] * 4], freel=[2 ** 30] * 10)
+    assert st == 1 and slots[:2] == [-1, -1]
+
+
+def test_tables_empty_batch():
+    cu, slots, out = ints([9]), ints([9, 9]), ints([9])
+    e = torch.empty(0, dtype=torch.int32, device="cuda")
+    pda.paged_build_tables(e, e, 16, ints([1, 2]), ints([2]), torch.empty((0, 4), dtype=torch.int32, device="cuda"), cu, slots, free_count_out=out)
+    assert cu.tolist() == [0] and slots.tolist() == [-1, -1] and out.item() == 2
+
+
+# ---- append ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T", [1, 5, 257])
+@pytest.mark.parametrize("R,Dr,P", [(512, 64, 64), (8, 0, 1), (1024, 256, 16), (264, 8, 5)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_append(T, R, Dr, P, norm):
+    pages = T // P + 3
+    buf = torch.cat([randn(1, T, R) * (torch.rand(T, 1) * 4 + 0.01), randn(2, T, Dr + 8)], dim=1).to(torch.bfloat16)
+    cache = randn(3, pages, P, R + Dr + 16)[:, :, :R + Dr]           # rows with a gap behind them
+    slots = np.random.default_rng(T).permutation(pages * P)[:T].astype(np.int32)
+    slots[T // 2] = -1
+    w = (randn(4, R, scale=0.3) + 1).to(torch.bfloat16)
+    d = torch.empty((pages, P, R + Dr + 16), dtype=torch.bfloat16, device="cuda")[:, :, :R + Dr]
+    d.copy_(cache)
+    dbuf, status = buf.cuda(), ints([0])
+    pda.latent_append(dbuf[:, :R], dbuf[:, R:R + Dr], d, ints(slots), norm_weight=w.cuda() if norm else None, eps=1e-5, status=status)
+    c = buf[:, :R].double()
+    if norm:
+        c = c / torch.sqrt((c * c).mean(1, keepdim=True) + 1e-5) * w.double()
+    ref = cache.clone().double()
+    for t in range(T):
+        if slots[t] >= 0:
+            ref[slots[t] // P, slots[t] % P] = torch.cat([c[t], buf[t, R:R + Dr].double()])
+    got = d.cpu().double()
+    if norm:  # one rounding to bf16 and a few 32-bit ones
+        assert ((got - ref).abs() <= ref.abs() * (U.EPS + 2.0 ** -18)).all()
+        rest = torch.ones(pages * P, dtype=torch.bool)
+        rest[slots[slots >= 0].astype(np.int64)] = False
+        assert torch.equal(got.reshape(pages * P, -1)[rest], ref.reshape(pages * P, -1)[rest])
+        assert torch.equal(got[..., R:], ref[..., R:])
+    else:
+        assert torch.equal(got, ref)
+    assert status.item() == 0
+
+
+def test_append_slot_beyond_the_cache():
+    cache, status = torch.zeros((2, 16, 72), dtype=torch.bfloat16, device="cuda"), ints([0])
+    pda.latent_append(randn(1, 3, 64).cuda(), randn(2, 3, 8).cuda(), cache, ints([32, 31, 2 ** 31 - 1]), status=status)
+    assert status.item() == 1
+    nz = cache.view(32, 72).abs().sum(1) != 0
+    assert nz.tolist() == [False] * 31 + [True]
+
+
+def test_append_all_zero_row_is_zero():
+    cache = torch.ones((1, 16, 72), dtype=torch.bfloat16, device="cuda")
+    z = torch.zeros((1, 64), dtype=torch.bfloat16, device="cuda")
+    pda.latent_append(z, randn(2, 1, 8).cuda(), cache, ints([3]), norm_weight=torch.ones(64, dtype=torch.bfloat16, device="cuda"), eps=1e-6)
+    assert (cache[0, 3, :64] == 0).all() and (cache[0, 2] == 1).all()
+
+
+# ---- absorbed attention ----------------------------------------------------------------------------
+
+def run_absorbed(lens, H, T, R, Dr, P, seed=1, flags=0, layout="plain", scale=None, spread=1.0, **kw):
+    pg = U.Paged(lens, P, R, Dr, seed, spread=spread, **kw)
+    B = len(lens)
+    ql, qr = randn(seed + 1, B, T, H, R), randn(seed + 2, B, T, H, Dr)
+    scale = 1.0 / np.sqrt(192.0) if scale is None else scale
+    if layout == "plain":
+        dql, dqr, out = ql.cuda(), qr.cuda(), torch.full((B, T, H, R), float("nan"), dtype=torch.bfloat16, device="cuda")
+    else:  # heads outermost, as a batched product leaves them; the rotary part a slice
+        dql = ql.permute(2, 0, 1, 3).contiguous().cuda().permute(1, 2, 0, 3)
+        dqr = torch.cat([randn(9, B, T, H, 128), qr], dim=-1).cuda()[..., 128:]
+        out = torch.full((H, B, T, R), float("nan"), dtype=torch.bfloat16, device="cuda").permute(1, 2, 0, 3)
+    ws = pda.latent_workspace(B, H, T, R)
+    ws.fill_(255)
+    got = pda.paged_latent_attention(dql, dqr, pg.cache, pg.dtable, pg.dlens, scale, out=out, workspace=ws, flags=flags, status=pg.status)
+    torch.cuda.synchronize()
+    assert pg.status.item() == 0
+    ref, tol = U.absorbed(ql, qr, pg.host, pg.table, lens, scale, R)
+    U.check(got, ref, tol, f"lens {lens[:6]} H {H} T {T} R {R} P {P}")
+    return pg, dql, dqr, ws, got
+
+
+LENS = [1, 0, 17, 64, 65, 63, 128, 200, 16, 15]
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+@pytest.mark.parametrize("H", [1, 16, 24, 64, 128])
+@pytest.mark.parametrize("P", [16, 64])
+def test_absorbed_lengths(H, P, flags):
+    run_absorbed(LENS, H, 1, 512, 64, P, flags=flags)
+
+
+@pytest.mark.parametrize("R,Dr,P,H", [(128, 64, 16, 8), (256, 64, 32, 33), (384, 64, 128, 16), (512, 64, 256, 65), (512, 64, 8, 16),
+                                      (512, 64, 48, 16), (64, 64, 16, 4), (200, 40, 7, 5), (1024, 0, 16, 3), (8, 8, 1, 2)])
+def test_absorbed_shapes(R, Dr, P, H):
+    run_absorbed([70, 1, 300, 129], H, 1, R, Dr, P, seed=R)
+
+
+@pytest.mark.parametrize("T,H", [(2, 16), (3, 5), (5, 64), (16, 8), (7, 128), (40, 16)])
+@pytest.mark.parametrize("layout", ["plain", "bmm"])
+def test_absorbed_blocks_of_queries(T, H, layout):
+    # among them sequences shorter than the block: query tokens before the first one have nothing to attend
+    run_absorbed([T, T + 1, 1, 0, 64, 63 + T, 130, 300], H, T, 512, 64, 64, seed=T, layout=layout)
+
+
+@pytest.mark.parametrize("lens,H,T", [([4000], 16, 1), ([3000, 1, 2000], 128, 1), ([5000, 4997], 32, 3), ([257] * 30, 64, 1)])
+@pytest.mark.parametrize("P", [16, 64])
+def test_absorbed_split_over_the_tokens(lens, H, T, P):
+    run_absorbed(lens, H, T, 512, 64, P, seed=3)
+
+
+def test_absorbed_many_sequences():
+    g = np.random.default_rng(5)
+    run_absorbed([int(x) for x in g.integers(0, 150, size=700)], 16, 1, 128, 64, 16, seed=5)
+
+
+@pytest.mark.parametrize("spread,scale", [(30.0, 0.07), (1e-3, 0.07), (1.0, 0.0), (8.0, 1.0)])
+def test_absorbed_peaked_and_flat_scores(spread, scale):
+    run_absorbed([700, 65, 1300], 32, 1, 512, 64, 64, seed=6, spread=spread, scale=scale)
+
+
+def test_absorbed_rising_scores():
+    """Every block of tokens raises the running maximum far beyond the last one's, then it falls again."""
+    L, H, R = 1024, 16, 512
+    pg = U.Paged([L], 64, R, 64, 7)
+    ql, qr = randn(8, 1, 1, H, R), randn(9, 1, 1, H, 64)
+    ramp = torch.cat([torch.linspace(-60, 60, L // 2), torch.linspace(60, -60, L // 2)])
+    host = pg.host.clone()
+    for i in range(L // 64):
+        rows = host[int(pg.table[0, i])].float()
+        rows[:, :R] += ramp[i * 64:(i + 1) * 64, None] * ql[0, 0, i % H].float() / 100
+        host[int(pg.table[0, i])] = rows.to(torch.bfloat16)
+    pg.cache.copy_(host)
+    got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 0.07)
+    ref, tol = U.absorbed(ql, qr, host, pg.table, [L], 0.07, R)
+    U.check(got, ref, tol)
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_absorbed_strides_of_the_cache(flags):
+    run_absorbed([100, 33, 64], 16, 1, 512, 64, 16, flags=flags, slot_pad=8, page_pad=24)
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_absorbed_bad_pages_and_lengths(flags):
+    lens = [700, 300, 64, 500, 129]
+    pg = U.Paged(lens, 64, 512, 64, 11)
+    ql, qr = randn(1, 5, 1, 16, 512), randn(2, 5, 1, 16, 64)
+    ref, tol = U.absorbed(ql, qr, pg.host, pg.table, lens, 0.07, 512)
+    for seq, entry, value in ((0, 10, -1), (1, 0, pg.cache.shape[0]), (3, 3, -2 ** 31), (4, 2, 2 ** 31 - 1)):
+        t = pg.dtable.clone()
+        t[seq, entry] = value
+        st = ints([0])
+        got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, t, pg.dlens, 0.07, status=st, flags=flags)
+        assert st.item() == 1
+        r, o = ref.clone(), tol.clone()
+        r[seq], o[seq] = 0, 0
+        U.check(got, r, o, f"bad page in {seq}")
+    for seq, L in ((2, 64 * pg.table.shape[1] + 1), (0, 2 ** 31 - 1), (3, -5)):
+        ls = list(lens)
+        ls[seq] = L
+        st = ints([0])
+        got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, ints(ls), 0.07, status=st, flags=flags)
+        assert st.item() == (2 if L > 0 else 0)
+        r, o = ref.clone(), tol.clone()
+        r[seq], o[seq] = 0, 0
+        U.check(got, r, o, f"length {L}")
+
+
+def test_absorbed_repeats_bit_for_bit_and_other_streams():
+    pg, ql, qr, ws, first = run_absorbed([900, 77, 2500, 64], 32, 1, 512, 64, 64, seed=21)
+    first = first.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        a = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 1.0 / np.sqrt(192.0))
+    b = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 1.0 / np.sqrt(192.0), stream=s, workspace=ws)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(a, first) and torch.equal(b, first)
+
+
+def test_absorbed_far_offsets():
+    """Pages whose offsets pass 2^31 elements."""
+    R, W, P = 512, 576, 64
+    page_stride = 2 ** 28                                    # elements; 10 pages span 5.4 GB
+    n_pages = 10
+    flat = torch.empty((n_pages - 1) * page_stride + P * W, dtype=torch.bfloat16, device="cuda")
+    cache = flat.as_strided((n_pages, P, W), (page_stride, W, 1))
+    host = randn(1, n_pages, P, W)
+    cache.copy_(host)
+    table = np.array([[9, 8, 2, 7, 0], [1, 9, 9, 9, 9]], dtype=np.int32)
+    lens = [300, 50]
+    ql, qr = randn(2, 2, 1, 16, R), randn(3, 2, 1, 16, 64)
+    ref, tol = U.absorbed(ql, qr, host, table, lens, 0.07, R)
+    for flags in (0, GENERIC):
+        got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), cache, ints(table), ints(lens), 0.07, flags=flags)
+        U.check(got, ref, tol)
+    pda.latent_append(randn(4, 1, R).cuda(), randn(5, 1, 64).cuda(), cache, ints([9 * P + 63]))
+    assert torch.equal(cache[9, 63, :R].cpu(), randn(4, 1, R)[0]) and torch.equal(cache[9, 62].cpu(), host[9, 62])
+
+
+# ---- expanded attention ----------------------------------------------------------------------------
+
+def run_expanded(q_lens, k_lens, H, dims=(128, 64, 128), seed=1, flags=0, gap=0, scale=None, max_q=None, spread=1.0):
+    dn, dr, dv = dims
+    cq = [gap + int(x) for x in np.concatenate([[0], np.cumsum(q_lens)])]
+    ck = [gap + int(x) for x in np.concatenate([[0], np.cumsum(k_lens)])]
+    tq, tk = cq[-1] + gap, ck[-1] + gap
+    scale = 1.0 / np.sqrt(dn + dr) if scale is None else scale
+    q, kv, kr = randn(seed, tq, H, dn + dr), randn(seed + 1, tk, H, dn + dv, scale=spread), randn(seed + 2, tk, dr, scale=spread)
+    if gap:
+        for t, n in ((q, tq), (kv, tk), (kr, tk)):          # rows outside the sequences hold anything
+            t[:gap] = float("nan")
+            t[n - gap:] = float("nan")
+    dq, dkv, dkr = q.cuda(), kv.cuda(), kr.cuda()
+    out = torch.full((tq, H, dv), -5.0, dtype=torch.bfloat16, device="cuda")
+    st = ints([0])
+    got = pda.latent_prefill_attention(dq, dkv[..., :dn], dkr, dkv[..., dn:], ints(cq), ints(ck), max_q or max(q_lens), scale,
+                                       out=out, flags=flags, status=st)
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    ref, tol = U.expanded(q, kv[..., :dn], kr, kv[..., dn:], cq, ck, scale)
+    if gap:
+        assert (got[:gap] == -5).all() and (got[tq - gap:] == -5).all()
+    U.check(got[cq[0]:cq[-1]], ref[cq[0]:cq[-1]], tol[cq[0]:cq[-1]], f"q {q_lens[:5]} k {k_lens[:5]} H {H} {dims}")
+    return dq, dkv, dkr, got
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+@pytest.mark.parametrize("lens", [[1], [2, 1, 3], [127, 128, 129], [255, 256, 257, 64], [400, 1, 31]])
+def test_expanded_prompts(lens, flags):
+    run_expanded(lens, lens, 3, flags=flags)
+
+
+@pytest.mark.parametrize("q_lens,k_lens", [([1], [300]), ([5, 128, 1], [600, 128, 129]), ([200, 0, 10], [513, 40, 10]), ([130], [1000]),
+                                           ([300, 7], [17, 0])])
+def test_expanded_behind_a_context(q_lens, k_lens):
+    # the last pair: more query tokens than keys, and none at all: rows without keys are zero
+    run_expanded(q_lens, k_lens, 2, seed=4, gap=0)
+    run_expanded(q_lens, k_lens, 2, seed=5, gap=3, max_q=max(q_lens) + 200)
+
+
+@pytest.mark.parametrize("dims", [(64, 32, 64), (128, 64, 64), (128, 0, 128), (200, 8, 96), (512, 256, 512)])
+def test_expanded_shapes(dims):
+    run_expanded([40, 3], [70, 3], 2, dims=dims, seed=6)
+
+
+@pytest.mark.parametrize("spread,scale", [(30.0, 0.07), (1e-3, 0.07), (1.0, 0.0), (4.0, 1.0)])
+def test_expanded_peaked_and_flat_scores(spread, scale):
+    run_expanded([300], [700], 2, seed=7, spread=spread, scale=scale)
+
+
+def test_expanded_long():
+    run_expanded([1500, 700], [1500, 2100], 2, seed=8)
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_expanded_bad_ranges(flags):
+    tq = tk = 60
+    q, kn, kr, v = randn(1, tq, 2, 192), randn(2, tk, 2, 128), randn(3, tk, 64), randn(4, tk, 2, 128)
+    d = [x.cuda() for x in (q, kn, kr, v)]
+    good_q, good_k = [0, 20, 40, 60], [0, 20, 40, 60]
+    ref, tol = U.expanded(q, kn, kr, v, good_q, good_k, 0.07)
+    for cq, ck, zero, skip in (([0, 20, 40, 61], good_k, [2], []), (good_q, [0, 20, 40, 61], [2], []), (good_q, [0, 20, 10, 60], [1, 2], []),
+                               (good_q, [-3, 20, 40, 60], [0], []), ([-2, 20, 40, 60], good_k, [], [0])):
+        out, st = torch.full((tq, 2, 128), -5.0, dtype=torch.bfloat16, device="cuda"), ints([0])
+        pda.latent_prefill_attention(*d, ints(cq), ints(ck), 20 if cq[-1] == 60 else 21, 0.07, out=out, flags=flags, status=st)
+        assert st.item() == 2
+        r, o, x = ref.clone(), tol.clone(), out.cpu().double()
+        if ck == [0, 20, 10, 60]:        # the last sequence's keys 10 .. 60 are a range of their own
+            rr, oo = U.expanded(q, kn, kr, v, [40, 60], [10, 60], 0.07)
+            r[40:], o[40:] = rr[40:], oo[40:]
+            zero = [1]
+        for b in zero:
+            r[20 * b:20 * b + 20], o[20 * b:20 * b + 20] = 0, 0
+        for b in skip:
+            assert (x[20 * b:20 * b + 20] == -5).all()
+            x[20 * b:20 * b + 20] = r[20 * b:20 * b + 20]
+        U.check(x, r, o, f"{cq} {ck}")
+    # more query tokens than max_q
+    out, st = torch.full((tq, 2, 128), -5.0, dtype=torch.bfloat16, device="cuda"), ints([0])
+    pda.latent_prefill_attention(*d, ints([0, 25, 45, 60]), ints([0, 25, 45, 60]), 20, 0.07, out=out, flags=flags, status=st)
+    assert st.item() == 2 and (out[:20] == 0).all() and (out[20:25] == -5).all() and (out[25:] != -5).any()
+
+
+# ---- together --------------------------------------------------------------------------------------
+
+def test_prompts_then_decoding_steps():
+    """Tables, append and both forms as a layer runs them, against the definition on the stored rows."""
+    B, H, R, Dr, Dn, Dv, P = 4, 16, 512, 64, 128, 128, 16
+    prompts, steps, pool = [37, 1, 160, 64], 4, 64
+    scale = 1.0 / np.sqrt(Dn + Dr)
+    wk, wv = randn(1, H, Dn, R, scale=R ** -0.5).cuda(), randn(2, H, Dv, R, scale=R ** -0.5).cuda()
+    norm_w = (randn(3, R, scale=0.1) + 1).to(torch.bfloat16).cuda()
+    cache = torch.full((pool, P, R + Dr), float("nan"), dtype=torch.bfloat16, device="cuda")
+    table = torch.full((B, 16), -1, dtype=torch.int32, device="cuda")
+    free, count, status = ints(np.random.default_rng(0).permutation(pool)), ints([pool]), ints([0])
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    ws = pda.latent_workspace(B, H, 1, R)
+    for step in range(steps + 1):
+        new = prompts if step == 0 else [1] * B
+        n = sum(new)
+        new_lens, cu, slots, pos = ints(new), ints([0] * (B + 1)), ints([0] * (n + 5)), ints([0] * (n + 5))
+        lens = lens + new_lens
+        pda.paged_build_tables(lens, new_lens, P, free, count, table, cu, slots, positions=pos, status=status)
+        rows = randn(10 + step, n, R + Dr).cuda()
+        pda.latent_append(rows[:, :R], rows[:, R:], cache, slots[:n], norm_weight=norm_w, eps=1e-6, status=status)
+        q = randn(50 + step, n, H, Dn + Dr).cuda()
+        if step == 0:
+            stored = cache.view(-1, R + Dr)[slots[:n].long()]
+            k_nope = torch.einsum("tr,hdr->thd", stored[:, :R].float(), wk.float()).to(torch.bfloat16)
+            v = torch.einsum("tr,hdr->thd", stored[:, :R].float(), wv.float()).to(torch.bfloat16)
+            out = pda.latent_prefill_attention(q, k_nope, stored[:, R:], v, cu, cu, max(new), scale, status=status)
+        else:
+            ql = torch.einsum("thd,hdr->thr", q[..., :Dn].float(), wk.float()).to(torch.bfloat16)
+            o = pda.paged_latent_attention(ql, q[..., Dn:], cache, table, lens, scale, workspace=ws, status=status)
+            out = torch.einsum("thr,hdr->thd", o.float(), wv.float())
+        assert status.item() == 0
+        at, where = 0, table.cpu().numpy()
+        for b, L in enumerate(lens.tolist()):
+            j = np.arange(L)
+            stored = cache[torch.as_tensor(where[b, j // P].astype(np.int64)).cuda(), torch.as_tensor(j % P).cuda()].double()
+            for h in range(H):
+                k = torch.cat([stored[:, :R] @ wk[h].double().T, stored[:, R:]], dim=1)
+                vv = stored[:, :R] @ wv[h].double().T
+                for i in range(new[b]):
+                    live = L - new[b] + i + 1
+                    w = torch.softmax(k[:live] @ q[at + i, h].double() * scale, dim=0)
+                    ref = w @ vv[:live]
+                    # every rounding to bf16 on the way (keys or absorbed query, values or latent output, weights,
+                    # output) is 2^-8 of values near 1: scores move by less than 5 * 2^-8, outputs by a tenth at most
+                    assert float((out[at + i, h].double() - ref).abs().max()) < 0.1, (step, b, h, i)
+            at += new[b]
+    assert count.item() == pool - sum(-(-int(L) // P) for L in lens.tolist())
+
+
+def test_step_in_a_graph():
+    """A whole decode step captured once and replayed while the lengths grow on the device."""
+    B, H, R, Dr, P, steps = 3, 16, 512, 64, 16, 20
+    g = np.random.default_rng(1)
+    start = [30, 1, 100]
+    pg = U.Paged(start, P, R, Dr, 5, pages_extra=12)
+    used = {int(x) for b, L in enumerate(start) for x in pg.table[b, :-(-L // P)]}
+    free = [i for i in range(pg.cache.shape[0]) if i not in used]
+    table = torch.full((B, 12), -1, dtype=torch.int32, device="cuda")
+    table[:, :pg.table.shape[1]] = pg.dtable
+    lens, one, count, status = ints(start), ints([1] * B), ints([len(free)]), ints([0])
+    dfree, cu, slots = ints(free), ints([0] * (B + 1)), ints([0] * B)
+    rows, ql, qr = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((B, R + Dr), (B, 1, H, R), (B, 1, H, Dr)))
+    out, ws = torch.zeros((B, 1, H, R), dtype=torch.bfloat16, device="cuda"), pda.latent_workspace(B, H, 1, R)
+
+    def step():
+        pda.advance_seq_lens(lens)
+        pda.paged_build_tables(lens, one, P, dfree, count, table, cu, slots, status=status)
+        pda.latent_append(rows[:, :R], rows[:, R:], pg.cache, slots, status=status)
+        pda.paged_latent_attention(ql, qr, pg.cache, table, lens, 0.07, out=out, workspace=ws, status=status)
+
+    graph = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(steps):
+        rows.copy_(randn(100 + i, B, R + Dr))
+        hq, hr = randn(200 + i, B, 1, H, R), randn(300 + i, B, 1, H, Dr)
+        ql.copy_(hq)
+        qr.copy_(hr)
+        graph.replay()
+        now = [L + 2 + i for L in start]
+        assert lens.tolist() == now and status.item() == 0
+        ref, tol = U.absorbed(hq, hr, pg.cache.cpu(), table.cpu().numpy(), now, 0.07, R)
+        U.check(out, ref, tol, f"replay {i}")
