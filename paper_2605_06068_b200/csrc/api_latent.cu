@@ -99,6 +99,8 @@ int paged_latent_attention(const void* q_latent, int64_t ql_token_stride, int64_
                       static_cast<__nv_bfloat16*>(out), static_cast<const __nv_bfloat16*>(cache), block_table, seq_lens,
                       status, ql_token_stride, ql_head_stride, qr_token_stride, qr_head_stride, out_token_stride,
                       out_head_stride, g, block_table_stride, batch, num_q_heads, n_query_tokens, scale, workspace};
+  if (!(flags & PDA_FLAG_FORCE_GENERIC) && pda::latent_tc_supports(p))
+    return static_cast<int>(pda::launch_latent_tc(p, static_cast<cudaStream_t>(stream)));
   return static_cast<int>(pda::launch_latent_generic(p, static_cast<cudaStream_t>(stream)));
 }
 

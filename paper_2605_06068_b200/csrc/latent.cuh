@@ -111,6 +111,8 @@ inline int64_t latent_workspace_bytes(int num_q_heads, int n_q, int latent_dim) 
 cudaError_t launch_build_tables(const TablesParams& p, cudaStream_t stream);
 cudaError_t launch_latent_append(const LatentAppendParams& p, cudaStream_t stream);
 cudaError_t launch_latent_generic(const LatentParams& p, cudaStream_t stream);
+bool latent_tc_supports(const LatentParams& p);  // tcgen05 kernel
+cudaError_t launch_latent_tc(const LatentParams& p, cudaStream_t stream);
 cudaError_t launch_latent_prefill_generic(const LatentPrefillParams& p, cudaStream_t stream);
 
 }  // namespace pda

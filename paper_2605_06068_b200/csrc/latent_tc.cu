@@ -1,0 +1,804 @@
+// Absorbed attention over the paged latent cache on tcgen05 + TMEM: up to 64 query rows (query tokens x
+// heads) per CTA against tiles of 64 cached rows, each tile fetched once and used as keys and as values.
+//
+// Both products run transposed, so that the query rows are the N of the instruction and the accumulator
+// fits tensor memory (O of 128 rows x 512 dims in f32 would be all of it):
+//   S^T[64 tokens x N]   = C[64 x (R + 64)] . Q^T      M = 64, A = the tile (K-major), B = Q (K-major)
+//   O^T[128 dims x N] (+)= C^T[128 x 64] . P^T         R / 128 of them, M = 128, A = the tile read
+//                                                      MN-major, B = P (MN-major, written by the softmax)
+// N = 16, 32 or 64, the least that holds the rows (fewer rows: less of the tensor core's time, which for
+// 16 rows stays far below the tile's trip from memory). A tile is 64 tokens because two tiles (2 x 72 KB)
+// next to Q (72 KB at N = 64) are what shared memory holds; they are filled and freed by the 128-byte
+// lines that one O^T instruction group reads, so that the next tile's copies start while P . C runs.
+//
+// Work: the tiles of all sequences form one list, cut into equal spans, one per group of CTAs (the CTAs of
+// a group take the row blocks of the same span at the same time: the tile comes from memory once and
+// from L2 for the others). A sequence that lies in several spans leaves partial results (normalised, with
+// the log2 of their weight) in the workspace, merged by a second kernel; one within a span is
+// written directly. Spans depend on the lengths and the number of SMs only.
+//
+// Softmax: a thread holds 2 tokens x N / 4 query rows. Weights are taken relative to a reference per row
+// that is raised (and O, in tensor memory, rescaled) only when a score passes it by more than 2^8; the
+// decision is one vote per tile, so that in the steady state no maximum crosses lanes. Row sums stay in
+// registers, per token lane, until the end. Weights are rounded to bf16 for the tensor core (they are at
+// most 2^8, and relative to their row's sum the rounding is 2^-8 whatever the reference); sums, scores and
+// O are 32-bit.
+//
+// Warps: 0-3 softmax and output, 4 TMA producer, 5 S issue + TMEM, 6 P . C issue, 7 Q rows. All waits are
+// bounded; on a timeout every role leaves its loop, outstanding copies and products are waited for (with a
+// limit) and tensor memory is released.
+#include <cmath>
+
+#include "latent.cuh"
+#include "tcgen05_ptx.cuh"
+#include "tma_ptx.cuh"
+
+namespace pda {
+
+namespace {
+
+constexpr int kLTok = 64;                       // tokens per tile
+constexpr int kLLineBytes = kLTok * 128;        // one 128-byte line of 64 tokens
+constexpr int kLMaxLines = 9;                   // latent 512 + rope 64
+constexpr int kLStageBytes = kLMaxLines * kLLineBytes;
+constexpr int kLStages = 2;
+constexpr int kLGroups = 5;                     // line groups of a stage: rope, then pairs of latent lines
+constexpr int kLThreads = 256;
+constexpr int kLProducer = 4, kLSIssue = 5, kLPvIssue = 6, kLQLoad = 7;
+constexpr uint32_t kLTmemCols = 512, kLTmemS = 256;  // O^T: R / 128 blocks of N columns from 0; S^T from 256
+constexpr float kLNoMax = -1e30f;               // reference of a row that has seen no score yet
+constexpr float kLRescale = 8.f;                // log2
+constexpr int kLMinSpan = 2;                    // tiles: below this a span costs more than it shortens
+
+template <int N>
+struct LCfg {
+  static constexpr int kQBytes = kLMaxLines * N * 128;
+  static constexpr int kPBytes = kLTok * 128;
+  static constexpr int kBarBytes = 384;
+  // column maxima / sums of the four warps (the first row also inverse sums), rescale factors, row offsets
+  static constexpr int kRowBytes = 4 * N * 4 + N * 4 + N * 4;
+  static constexpr int kSmemBytes = kLStages * kLStageBytes + kQBytes + kPBytes + kRowBytes + kBarBytes + 1024;
+};
+static_assert(LCfg<64>::kSmemBytes <= 232448, "shared memory");
+
+struct LPlan {
+  int32_t row_blocks, per_pass, passes, groups;  // row blocks per sequence; taken at once; rounds; CTA groups
+};
+
+struct LRecord {  // a sequence whose first span is this one and that continues: see latent_merge_kernel
+  int32_t vseq, first_slot, n_seg, pad;
+};
+
+__device__ __forceinline__ int seq_tokens(const LatentParams& p, int b) {
+  const int L = p.seq_lens[b];
+  return L <= 0 || L > static_cast<int64_t>(p.block_table_stride) * p.geom.page_size ? 0 : L;
+}
+__device__ __forceinline__ int seq_tiles(int L) { return L <= 0 ? 1 : (L - 1) / kLTok + 1; }  // (an empty one takes a place too)
+
+// One sequence's part of a CTA's span.
+struct Segment {
+  int b, rb, L;        // sequence, row block (-1: none in this pass), tokens
+  int tile0, n_tiles;  // tiles to attend (cut at what the row block can see)
+  int off, take;       // tiles of the list it stands for
+  int whole;           // tiles of the sequence in the list
+  int vseq;
+};
+
+struct Walk {
+  int vseq, off, rem;
+};
+
+template <int N>
+__device__ __forceinline__ bool next_segment(const LatentParams& p, const LPlan& plan, int r, Walk& w, Segment& s) {
+  if (w.rem <= 0) return false;
+  s.vseq = w.vseq;
+  s.b = w.vseq % p.batch;
+  const int rb = (w.vseq / p.batch) * plan.per_pass + r;
+  s.rb = rb < plan.row_blocks ? rb : -1;
+  s.L = seq_tokens(p, s.b);
+  s.whole = seq_tiles(s.L);
+  s.off = w.off;
+  s.take = min(s.whole - w.off, w.rem);
+  const int last_row = min((rb + 1) * N, p.n_q * p.num_q_heads) - 1;
+  const int see = min(max(s.L - p.n_q + last_row / p.num_q_heads + 1, 0), s.L);  // what its last row can see
+  s.tile0 = w.off;
+  s.n_tiles = s.rb < 0 ? 0 : max(0, min(w.off + s.take, (see + kLTok - 1) / kLTok) - w.off);
+  w.rem -= s.take;
+  w.off = 0;
+  w.vseq += 1;
+  return true;
+}
+
+__device__ __forceinline__ void mma_ss_if(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                          uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred pe, pa;\n\tsetp.ne.b32 pe, %5, 0;\n\tsetp.ne.b32 pa, %4, 0;\n\t"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, pa;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// bf16 x bf16 -> f32, M x N
+__host__ __device__ constexpr uint32_t latent_idesc(int m, int n, bool a_mn, bool b_mn) {
+  return (1u << 4) | (kFmtBf16 << 7) | (kFmtBf16 << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+         (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+__device__ __forceinline__ void tma_load_4d_hint_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot,
+                                                    int line, int page, uint64_t policy) {
+  asm volatile(
+      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %6, 0;\n\t"
+      "@pe cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {0, %3, %4, %5}], [%2], %7;\n\t}"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(slot), "r"(line), "r"(page), "r"(leader), "l"(policy) : "memory");
+}
+__device__ __forceinline__ uint64_t l2_policy_normal() {
+  uint64_t pol;
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+  return pol;
+}
+// 16 lanes x 8 J columns: register 4 j + 0, 1: lane t / 4, columns 8 j + 2 (t % 4) + 0, 1; + 2, 3: lane t / 4 + 8
+template <int J>
+__device__ __forceinline__ void tmem_ld_16x256b(uint32_t taddr, uint32_t (&r)[4 * J]) {
+  if constexpr (J == 2) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+  } else if constexpr (J == 4) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr));
+  } else {
+    static_assert(J == 8);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+  }
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void stsm_x4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool soft_any(bool x) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(static_cast<uint32_t>(x)) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+template <int N>
+__global__ void __launch_bounds__(kLThreads, 1)
+latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ LatentParams p,
+                 const __grid_constant__ LPlan plan) {
+  using C = LCfg<N>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* rows_raw = smem + kLStages * kLStageBytes + C::kQBytes + C::kPBytes;
+  float* wred = reinterpret_cast<float*>(rows_raw);                 // [4][N]
+  float* alpha = wred + 4 * N;                                      // [N]
+  int32_t* row_off = reinterpret_cast<int32_t*>(alpha + N);         // [N] offset of the row in out, in units of 8 elements; -1: none
+  float* inv_l = wred;                                              // [N] (thread n replaces column n of what it has summed)
+  uint64_t* bars = reinterpret_cast<uint64_t*>(rows_raw + C::kRowBytes);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 40);
+  int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
+  int* span = cta_err + 1;                                          // [3] first sequence, tile, tiles
+  int64_t* scan = reinterpret_cast<int64_t*>(wred);                 // (start of the kernel only) [8] warps' sums
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = blockIdx.x / plan.per_pass, r = blockIdx.x % plan.per_pass;
+  const LatentGeom& geo = p.geom;
+  const int m_tiles = geo.latent_dim / 128, n_groups = m_tiles + 1;
+  asm volatile("griddepcontrol.launch_dependents;");
+
+  // a CTA of this launch has met an expired wait: the rest do not start (the output is lost anyway)
+  const LatentWorkspace lay = latent_workspace_layout(p.num_q_heads, p.n_q, geo.latent_dim);
+  uint8_t* ws = static_cast<uint8_t*>(p.workspace);
+  if (p.status != nullptr && __syncthreads_or(*reinterpret_cast<volatile int32_t*>(p.status) == PDA_DEV_TIMEOUT)) {
+    if (r == 0 && tid == 0) reinterpret_cast<LRecord*>(ws + lay.records)[g] = LRecord{-1, 0, 0, 0};  // (nothing to merge)
+    return;
+  }
+
+  const uint32_t ring = smem_u32(smem), q_sm = ring + kLStages * kLStageBytes, p_sm = q_sm + C::kQBytes;
+  const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kLStages * kLGroups;  // [stage][group]
+  const uint32_t bar_s = empty0 + 8 * kLStages * kLGroups, bar_sfree = bar_s + 16, bar_p = bar_sfree + 16, bar_pv = bar_p + 8,
+                 bar_q = bar_pv + 8, bar_qfree = bar_q + 8, bar_ofree = bar_qfree + 8, bar_drain = bar_ofree + 8;
+  if (tid == 0) {
+    for (int i = 0; i < 2 * kLStages * kLGroups; ++i) mbar_init(full0 + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_s + 8 * i, 1);
+      mbar_init(bar_sfree + 8 * i, 4);
+    }
+    mbar_init(bar_p, 4);
+    mbar_init(bar_pv, 1);
+    mbar_init(bar_q, 1);
+    mbar_init(bar_qfree, 1);
+    mbar_init(bar_ofree, 4);
+    mbar_init(bar_drain, 2);
+    *cta_err = 0;
+    span[0] = span[1] = span[2] = 0;
+    fence_mbar_init();
+    fence_proxy_async();
+  }
+  if (warp == kLSIssue) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kLTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // ---- this group's span of the tile list: every thread sums a run of sequences, then the sums are scanned
+  const int per_thread = (p.batch + kLThreads - 1) / kLThreads;
+  const int b0 = min(tid * per_thread, p.batch), b1 = min(b0 + per_thread, p.batch);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += seq_tiles(seq_tokens(p, b));
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) scan[warp] = incl;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  int64_t list = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < kLThreads / 32; ++w) {
+    before += w < warp ? scan[w] : 0;
+    list += scan[w];
+  }
+  before += incl - mine;
+  const int64_t total = list * plan.passes;
+  const int64_t span_tiles = max((total + plan.groups - 1) / plan.groups, static_cast<int64_t>(kLMinSpan));
+  const int64_t start = g * span_tiles, stop = min(start + span_tiles, total);
+  if (start < stop) {
+    const int64_t pass = start / list, in_pass = start - pass * list;
+    if (in_pass >= before && in_pass < before + mine) {  // (one thread)
+      int64_t at = before;
+      for (int b = b0; b < b1; ++b) {
+        const int n = seq_tiles(seq_tokens(p, b));
+        if (in_pass < at + n) {
+          span[0] = static_cast<int>(pass) * p.batch + b;
+          span[1] = static_cast<int>(in_pass - at);
+          span[2] = static_cast<int>(stop - start);
+          break;
+        }
+        at += n;
+      }
+    }
+  }
+  __syncthreads();
+  const uint32_t tmem = *tmem_slot;
+  Walk walk{span[0], span[1], span[2]};
+  Segment s;
+  bool ok = true;
+
+  if (warp == kLProducer) {
+    // ================= TMA producer: lines of the tiles, in the order in which they are read and freed ========
+    const uint32_t leader = elect_one();
+    const int box = min(geo.page_size, kLTok), ept = kLTok / box;  // rows per copy, copies per line of a tile
+    // row blocks of other CTAs read the same tiles: only a tile that is read once is marked to leave L2 first
+    const uint64_t policy = plan.row_blocks == 1 ? l2_policy_evict_first() : l2_policy_normal();
+    int i = 0;  // tiles of this CTA
+    while (ok && next_segment<N>(p, plan, r, walk, s)) {
+      const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
+      const int batch_tiles = 32 / ept;  // tiles whose page ids the lanes hold
+      auto load_ids = [&](int t) -> int {  // lane -> copy (t + lane / ept, lane % ept) of this segment
+        const int tile = t + lane / ept;
+        const int64_t tok = static_cast<int64_t>(s.tile0 + tile) * kLTok + (lane % ept) * box;
+        if (tile >= s.n_tiles || tok >= s.L) return 0;
+        const int v = __ldg(table + tok / geo.page_size);
+        return v < 0 || v >= geo.num_pages ? 0 : v;  // (the softmax warps look for these and drop the segment)
+      };
+      int ids = load_ids(0), ids_next = 0;
+      for (int t = 0; t < s.n_tiles; ++t, ++i) {
+        const int in_batch = t % batch_tiles;
+        if (in_batch == 0) {
+          if (t > 0) ids = ids_next;
+          ids_next = load_ids(t + batch_tiles);
+        }
+        const int st = i & 1;
+        const int tok0 = (s.tile0 + t) * kLTok;
+        const int n_copies = min(ept, (s.L - tok0 + box - 1) / box);
+        for (int gr = 0; gr < n_groups; ++gr) {
+          const uint32_t idx = 8 * (st * kLGroups + gr);
+          if (i >= kLStages) ok = mbar_wait_bounded(empty0 + idx, ((i >> 1) - 1) & 1);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1), n_lines = gr == 0 ? 1 : 2;
+          mbar_expect_tx_if(leader, full0 + idx, n_lines * n_copies * box * 128);
+          for (int c = 0; c < n_copies; ++c) {
+            const int page = __shfl_sync(0xffffffffu, ids, in_batch * ept + c);
+            const int slot = (tok0 + c * box) & (geo.page_size - 1);
+            for (int ln = 0; ln < n_lines; ++ln)
+              tma_load_4d_hint_if(leader, ring + st * kLStageBytes + (line0 + ln) * kLLineBytes + c * box * 128, &map, full0 + idx,
+                                  slot, line0 + ln, page, policy);
+          }
+        }
+        if (!ok) break;
+      }
+    }
+    if (!ok) {  // copies in flight end before the CTA does
+      if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+      for (int k = max(i - 1, 0); k <= i; ++k)
+        for (int gr = 0; gr < n_groups; ++gr) mbar_wait_bounded(full0 + 8 * ((k & 1) * kLGroups + gr), (k >> 1) & 1, 1u << 12);
+    }
+  } else if (warp == kLSIssue) {
+    // ================= S^T(i) = C . Q^T =================
+    constexpr uint32_t idesc = latent_idesc(64, N, false, false);
+    const uint32_t leader = elect_one();
+    const uint32_t u_tmem = __shfl_sync(0xffffffffu, tmem, 0);
+    int i = 0, seg = 0;
+    while (ok && next_segment<N>(p, plan, r, walk, s)) {
+      if (s.n_tiles == 0) continue;
+      ok = mbar_wait_bounded(bar_q, seg & 1);
+      for (int t = 0; ok && t < s.n_tiles; ++t, ++i) {
+        const int st = i & 1;
+        if (i >= 2) ok = mbar_spin_bounded(bar_sfree + 8 * st, ((i >> 1) - 1) & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t d = u_tmem + kLTmemS + st * N;
+        for (int gr = 0; gr < n_groups; ++gr) {
+          ok = mbar_wait_bounded(full0 + 8 * (st * kLGroups + gr), (i >> 1) & 1);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1), n_lines = gr == 0 ? 1 : 2;
+          for (int ln = line0; ln < line0 + n_lines; ++ln) {
+            const uint64_t ad = tc_desc(ring + st * kLStageBytes + ln * kLLineBytes, 16, 1024);
+            const uint64_t bd = tc_desc(q_sm + ln * (N * 128), 16, 1024);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) mma_ss_if(leader, d, ad + 2 * ks, bd + 2 * ks, idesc, (gr | ks) ? 1u : 0u);
+          }
+        }
+        if (!ok) break;
+        tc_commit_if(leader, bar_s + 8 * st);
+        tc_commit_if(leader, empty0 + 8 * (st * kLGroups));  // the rope line is only read here
+        if (t == s.n_tiles - 1) tc_commit_if(leader, bar_qfree);
+      }
+      ++seg;
+    }
+    if (!ok) {
+      if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    }
+    tc_commit_if(leader, bar_drain);
+  } else if (warp == kLPvIssue) {
+    // ================= O^T += C^T . P^T(i) =================
+    constexpr uint32_t idesc = latent_idesc(128, N, true, true);
+    const uint32_t leader = elect_one();
+    const uint32_t u_tmem = __shfl_sync(0xffffffffu, tmem, 0);
+    int i = 0, seg = 0;
+    while (ok && next_segment<N>(p, plan, r, walk, s)) {
+      if (s.n_tiles == 0) continue;
+      if (seg > 0) ok = mbar_wait_bounded(bar_ofree, (seg - 1) & 1);
+      for (int t = 0; ok && t < s.n_tiles; ++t, ++i) {
+        const int st = i & 1;
+        ok = mbar_spin_bounded(bar_p, i & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t bd = tc_desc(p_sm, 16, 1024);
+        for (int m = 0; m < m_tiles; ++m) {
+          const uint64_t ad = tc_desc(ring + st * kLStageBytes + 2 * m * kLLineBytes, kLLineBytes, 1024);
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks)
+            mma_ss_if(leader, u_tmem + m * N, ad + 128 * ks, bd + 128 * ks, idesc, (t > 0 || ks > 0) ? 1u : 0u);
+          tc_commit_if(leader, empty0 + 8 * (st * kLGroups + 1 + m));
+        }
+        tc_commit_if(leader, bar_pv);
+      }
+      ++seg;
+    }
+    if (!ok) {
+      if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    }
+    tc_commit_if(leader, bar_drain);
+  } else if (warp == kLQLoad) {
+    // ================= Q rows of a segment: [line][N rows][128 B], swizzled =================
+    int seg = 0;
+    while (ok && next_segment<N>(p, plan, r, walk, s)) {
+      if (s.n_tiles == 0) continue;
+      if (seg > 0) {
+        ok = mbar_wait_bounded(bar_qfree, (seg - 1) & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+      }
+      const int cv = geo.latent_dim / 8;
+      for (int n = 0; n < N; ++n) {
+        const int row = s.rb * N + n;
+        const bool live = row < p.n_q * p.num_q_heads;
+        const int t = row / p.num_q_heads, h = row - t * p.num_q_heads;
+        const int64_t token = static_cast<int64_t>(s.b) * p.n_q + t;
+        const __nv_bfloat16* ql = live ? p.q_latent + token * p.ql_token_stride + h * p.ql_head_stride : p.q_latent;
+        const __nv_bfloat16* qr = live ? p.q_rope + token * p.qr_token_stride + h * p.qr_head_stride : p.q_rope;
+        for (int c = lane; c < cv + 8; c += 32) {
+          const __nv_bfloat16* src = c < cv ? ql + c * 8 : qr + (c - cv) * 8;
+          cp_async16(q_sm + (c >> 3) * (N * 128) + n * 128 + (((c & 7) ^ (n & 7)) << 4), live ? src : (c < cv ? ql : qr), live ? 16u : 0u);
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_tc(bar_q);
+      ++seg;
+    }
+    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+  } else {
+    // ================= softmax, output =================
+    // After an expired wait a warp goes on without waiting (the four meet at the same named barriers), and
+    // what it writes is zero.
+    constexpr int J = N / 8;  // column blocks of 8; a thread's columns are 8 j + 2 (lane % 4) + {0, 1}
+    const float scale_log2 = p.scale * 1.4426950408889634f;
+    const int tok_a = warp * 16 + (lane >> 2), tok_b = tok_a + 8;  // its tokens within the tile
+    const int col0 = 2 * (lane & 3);
+    const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+    const int rows_total = p.n_q * p.num_q_heads;
+    LRecord rec{-1, 0, 0, 0};
+    int i = 0;
+    bool first_in_span = true;
+    while (next_segment<N>(p, plan, r, walk, s)) {
+      const bool at_start = first_in_span;
+      first_in_span = false;
+      const bool is_first = s.off == 0, is_last = s.off + s.take == s.whole;
+      if (is_first && !is_last)
+        rec = LRecord{s.vseq, 2 * g + (at_start ? 0 : 1), 1 + static_cast<int>((s.whole - s.take + span_tiles - 1) / span_tiles), 0};
+      if (s.rb < 0) continue;
+      const bool partial = !(is_first && is_last);
+      const int slot = 2 * g + (at_start ? 0 : 1);
+      // row addresses; pages and length
+      if (tid < N) {
+        const int row = s.rb * N + tid;
+        const int t = row / p.num_q_heads, h = row - t * p.num_q_heads;
+        row_off[tid] = row < rows_total ? static_cast<int32_t>(((static_cast<int64_t>(s.b) * p.n_q + t) * p.out_token_stride +
+                                                                h * p.out_head_stride) / 8) : -1;
+      }
+      bool bad = false;
+      {
+        const int raw = p.seq_lens[s.b];
+        if (raw > 0 && s.L == 0 && tid == 0) report(p.status, PDA_DEV_BAD_SEQ_LEN);
+        const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
+        const int64_t tok_end = min(static_cast<int64_t>(s.off + s.take) * kLTok, static_cast<int64_t>(s.L));
+        const int pg1 = static_cast<int>((tok_end + geo.page_size - 1) / geo.page_size);
+        for (int k = static_cast<int>(static_cast<int64_t>(s.off) * kLTok / geo.page_size) + tid; k < pg1; k += 128) {
+          const int v = __ldg(table + k);
+          bad |= v < 0 || v >= geo.num_pages;
+        }
+        if (bad) report(p.status, PDA_DEV_BAD_PAGE);
+      }
+      bad = soft_any(bad);
+
+      float m_ref[2 * J], l[2 * J];
+#pragma unroll
+      for (int c = 0; c < 2 * J; ++c) { m_ref[c] = kLNoMax; l[c] = 0.f; }
+      for (int t = 0; t < s.n_tiles; ++t, ++i) {
+        const int st = i & 1;
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * st, (i >> 1) & 1));
+        tc_fence_after();
+        uint32_t sv[4 * J];
+        tmem_ld_16x256b<J>(tmem + kLTmemS + st * N + lane_base, sv);
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_tc(bar_sfree + 8 * st);
+        const int tok0 = (s.tile0 + t) * kLTok;
+        const int valid = s.L - tok0;  // tokens of this tile (may be more than it has)
+        float x[4 * J];
+#pragma unroll
+        for (int c = 0; c < 4 * J; ++c) x[c] = __uint_as_float(sv[c]) * scale_log2;
+        if (tok0 + kLTok > s.L - p.n_q + 1) {  // the end of the sequence, or of what some query token may see
+#pragma unroll
+          for (int c = 0; c < 2 * J; ++c) {
+            const int row = s.rb * N + 8 * (c >> 1) + col0 + (c & 1);
+            const int lim = p.n_q == 1 ? valid : min(valid, valid - p.n_q + row / p.num_q_heads + 1);
+            const int e = 4 * (c >> 1) + (c & 1);
+            if (tok_a >= lim) x[e] = -INFINITY;
+            if (tok_b >= lim) x[e + 2] = -INFINITY;
+          }
+          if (valid < kLTok) {
+            // rows of the tile behind the sequence's end hold anything (pages' tails, an earlier tile): their
+            // weight is 0, and so must be what it multiplies
+            for (int k = tid; k < (kLTok - valid) * (geo.latent_dim / 8); k += 128) {
+              const int row = valid + k / (geo.latent_dim / 8), ch = k % (geo.latent_dim / 8);
+              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};"
+                           ::"r"(ring + st * kLStageBytes + (ch >> 3) * kLLineBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0));
+            }
+          }
+        }
+        bool above = false;
+#pragma unroll
+        for (int c = 0; c < 2 * J; ++c) {
+          const int e = 4 * (c >> 1) + (c & 1);
+          above |= fmaxf(x[e], x[e + 2]) > m_ref[c] + kLRescale;
+        }
+        const bool raise = soft_any(above);
+        if (raise) {
+          float mx[2 * J];
+#pragma unroll
+          for (int c = 0; c < 2 * J; ++c) {
+            const int e = 4 * (c >> 1) + (c & 1);
+            mx[c] = fmaxf(x[e], x[e + 2]);
+          }
+#pragma unroll
+          for (int o = 4; o <= 16; o <<= 1)
+#pragma unroll
+            for (int c = 0; c < 2 * J; ++c) mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], o));
+          if (lane < 4) {
+#pragma unroll
+            for (int c = 0; c < 2 * J; ++c) wred[warp * N + 8 * (c >> 1) + col0 + (c & 1)] = mx[c];
+          }
+          soft_sync();
+#pragma unroll
+          for (int c = 0; c < 2 * J; ++c) {
+            const int col = 8 * (c >> 1) + col0 + (c & 1);
+            const float m_new = fmaxf(fmaxf(fmaxf(wred[col], wred[N + col]), fmaxf(wred[2 * N + col], wred[3 * N + col])), m_ref[c]);
+            const float a = ex2(m_ref[c] - m_new);
+            if (warp == 0 && lane < 4) alpha[col] = a;
+            l[c] *= a;
+            m_ref[c] = m_new;
+          }
+          soft_sync();
+        }
+        // weights (P's buffer and, where the reference rose, O are free once the last product is through)
+        uint32_t pk[2 * J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const float a0 = ex2(x[4 * j] - m_ref[2 * j]), a1 = ex2(x[4 * j + 1] - m_ref[2 * j + 1]);
+          const float b0v = ex2(x[4 * j + 2] - m_ref[2 * j]), b1v = ex2(x[4 * j + 3] - m_ref[2 * j + 1]);
+          l[2 * j] += a0 + b0v;
+          l[2 * j + 1] += a1 + b1v;
+          pk[2 * j] = pack2<false>(a0, a1);
+          pk[2 * j + 1] = pack2<false>(b0v, b1v);
+        }
+        if (i > 0) {
+          if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv, (i - 1) & 1));
+        }
+        if (raise && t > 0) {
+          tc_fence_after();
+          for (int cb = 0; cb < m_tiles * N; cb += 16) {
+            uint32_t ov[16];
+            tmem_ld16(tmem + lane_base + cb, ov);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) ov[k] = __float_as_uint(__uint_as_float(ov[k]) * alpha[(cb + k) % N]);
+            tmem_st16(tmem + lane_base + cb, ov);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+        }
+        {
+          const int mi = lane >> 3, row = warp * 16 + (mi & 1) * 8 + (lane & 7);
+#pragma unroll
+          for (int j = 0; j < J; j += 2)
+            stsm_x4(p_sm + row * 128 + (((j + (mi >> 1)) ^ (row & 7)) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_tc(bar_p);
+      }
+
+      // ---- the segment's result
+      soft_sync();  // (alpha and wred: every warp is past the last tile)
+#pragma unroll
+      for (int o = 4; o <= 16; o <<= 1)
+#pragma unroll
+        for (int c = 0; c < 2 * J; ++c) l[c] += __shfl_xor_sync(0xffffffffu, l[c], o);
+      if (lane < 4) {
+#pragma unroll
+        for (int c = 0; c < 2 * J; ++c) wred[warp * N + 8 * (c >> 1) + col0 + (c & 1)] = l[c];
+      }
+      if (warp == 0 && lane < 4) {
+#pragma unroll
+        for (int c = 0; c < 2 * J; ++c) alpha[8 * (c >> 1) + col0 + (c & 1)] = m_ref[c];
+      }
+      soft_sync();
+      const int64_t part_row0 = (static_cast<int64_t>(slot) * plan.per_pass + r) * N;
+      if (tid < N) {
+        const float sum = (wred[tid] + wred[N + tid]) + (wred[2 * N + tid] + wred[3 * N + tid]);
+        inv_l[tid] = bad || sum == 0.f ? 0.f : 1.f / sum;
+        // (+inf marks a segment with a bad page: the merge then zeroes the row)
+        if (partial) reinterpret_cast<float*>(ws + lay.part_lse)[part_row0 + tid] = bad ? INFINITY : alpha[tid] + __log2f(sum);
+      }
+      soft_sync();
+      if (s.n_tiles > 0) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv, (i - 1) & 1));
+        tc_fence_after();
+      }
+      for (int m = 0; m < m_tiles; ++m) {
+        const int dim = m * 128 + warp * 32 + lane;
+        for (int cb = 0; cb < N; cb += 16) {
+          uint32_t ov[16];
+          tmem_ld16(tmem + lane_base + m * N + cb, ov);
+          tmem_wait_ld();
+          float v[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = s.n_tiles > 0 && ok && !bad ? __uint_as_float(ov[k]) * inv_l[cb + k] : 0.f;
+          if (partial) {
+            float* dst = reinterpret_cast<float*>(ws + lay.part_o) + (part_row0 + cb) * geo.latent_dim + dim;
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              if (row_off[cb + k] >= 0) dst[static_cast<int64_t>(k) * geo.latent_dim] = v[k];
+          } else {
+            // neighbouring lanes swap, so that each stores two dims of one row
+            const bool odd = lane & 1;
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+              const float other = __shfl_xor_sync(0xffffffffu, odd ? v[k] : v[k + 1], 1);
+              const uint32_t w = odd ? pack2<false>(other, v[k + 1]) : pack2<false>(v[k], other);
+              const int64_t off = row_off[cb + k + (odd ? 1 : 0)];
+              if (off >= 0) *reinterpret_cast<uint32_t*>(p.out + 8 * off + (dim & ~1)) = w;
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (s.n_tiles > 0 && lane == 0) mbar_arrive_tc(bar_ofree);
+      soft_sync();  // (row_off and inv_l are free again)
+    }
+    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    if (r == 0 && tid == 0) reinterpret_cast<LRecord*>(ws + lay.records)[g] = rec;
+  }
+
+  // ---- teardown
+  __syncwarp();
+  if (warp == kLPvIssue && !mbar_wait_bounded(bar_drain, 0, 1u << 12) && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0 && *cta_err) report(p.status, *cta_err);
+  if (warp == kLSIssue) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kLTmemCols) : "memory");
+  }
+}
+
+// Rows of the sequences that lie in several spans: one CTA per row of every span boundary's sequence.
+template <int N>
+__global__ void __launch_bounds__(128) latent_merge_kernel(const __grid_constant__ LatentParams p, const __grid_constant__ LPlan plan) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const LatentWorkspace lay = latent_workspace_layout(p.num_q_heads, p.n_q, p.geom.latent_dim);
+  const uint8_t* ws = static_cast<const uint8_t*>(p.workspace);
+  const LRecord rec = reinterpret_cast<const LRecord*>(ws + lay.records)[blockIdx.x];
+  if (rec.vseq < 0) return;
+  const int r = blockIdx.y, n = blockIdx.z, tid = threadIdx.x;
+  const int row = ((rec.vseq / p.batch) * plan.per_pass + r) * N + n, b = rec.vseq % p.batch;
+  if (row >= p.n_q * p.num_q_heads) return;
+  const int t = row / p.num_q_heads, h = row - t * p.num_q_heads;
+  __nv_bfloat16* out = p.out + (static_cast<int64_t>(b) * p.n_q + t) * p.out_token_stride + h * p.out_head_stride;
+  const int R = p.geom.latent_dim;
+  const float* lse = reinterpret_cast<const float*>(ws + lay.part_lse);
+  const float* part = reinterpret_cast<const float*>(ws + lay.part_o);
+  const int g0 = blockIdx.x;
+  auto row_of = [&](int k) -> int64_t {  // slot of the k-th segment: later spans hold theirs in their first slot
+    return (static_cast<int64_t>(k == 0 ? rec.first_slot : 2 * (g0 + k)) * plan.per_pass + r) * N + n;
+  };
+  float M = -INFINITY;
+  for (int k = tid & 31; k < rec.n_seg; k += 32) M = fmaxf(M, lse[row_of(k)]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  const bool dead = M == -INFINITY || M == INFINITY;  // nothing to attend, or a bad page
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float W = 0.f;
+  if (tid * 4 < R && !dead) {
+#pragma unroll 8
+    for (int k = 0; k < rec.n_seg; ++k) {
+      const int64_t at = row_of(k);
+      const float w = ex2(lse[at] - M);
+      const float4 v = *reinterpret_cast<const float4*>(part + at * R + tid * 4);
+      W += w;
+      acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y);
+      acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
+    }
+  }
+  if (tid * 4 < R) {
+    const float inv = dead ? 0.f : 1.f / W;
+    uint2 o;
+    o.x = pack2<false>(acc.x * inv, acc.y * inv);
+    o.y = pack2<false>(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>(out + tid * 4) = o;
+  }
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+  static EncodeFn fn = [] {
+    void* sym = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      sym = nullptr;
+    return reinterpret_cast<EncodeFn>(sym);
+  }();
+  return fn;
+}
+
+// How many row blocks run at once, and how often: the choice that keeps most CTAs busy, for at most 37
+// row blocks at once (four groups of CTAs), fewer rounds first.
+LPlan make_plan(int row_blocks, int ctas) {
+  LPlan best{row_blocks, 1, row_blocks, ctas};
+  double best_eff = -1.0;
+  for (int passes = 1; passes <= row_blocks; ++passes) {
+    const int per = (row_blocks + passes - 1) / passes;
+    if (per > 37 || per > ctas) continue;
+    const int groups = ctas / per;
+    const double eff = static_cast<double>(row_blocks) / (static_cast<double>(passes) * per) * groups * per / ctas;
+    if (eff > best_eff + 0.02) {
+      best_eff = eff;
+      best = LPlan{row_blocks, per, passes, groups};
+    }
+    if (per == 1) break;
+  }
+  return best;
+}
+
+template <int N>
+cudaError_t launch_n(const CUtensorMap& map, const LatentParams& p, int sms, cudaStream_t stream) {
+  const int rows = p.n_q * p.num_q_heads;
+  const LPlan plan = make_plan((rows + N - 1) / N, sms < kLatMaxCtas ? sms : kLatMaxCtas);
+  cudaError_t e = cudaFuncSetAttribute(latent_tc_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, LCfg<N>::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  latent_tc_kernel<N><<<plan.groups * plan.per_pass, kLThreads, LCfg<N>::kSmemBytes, stream>>>(map, p, plan);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  // the merge's CTAs are placed while the attention kernel runs and wait for its end
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(plan.groups, plan.per_pass, N);
+  cfg.blockDim = dim3(128);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, latent_merge_kernel<N>, p, plan);
+}
+
+}  // namespace
+
+bool latent_tc_supports(const LatentParams& p) {
+  const LatentGeom& g = p.geom;
+  if (g.rope_dim != 64 || g.latent_dim % 128 || g.latent_dim > 512 || g.num_pages < 1) return false;
+  if (g.page_size < 16 || (g.page_size & (g.page_size - 1))) return false;
+  // what a tensor map can describe, and 32-bit tile counts
+  if (g.page_stride >= (1ll << 38) || g.slot_stride >= (1ll << 38)) return false;
+  const int64_t last_out = (static_cast<int64_t>(p.batch) * p.n_q - 1) * (p.out_token_stride / 8) + (p.num_q_heads - 1) * (p.out_head_stride / 8);
+  if (last_out > INT32_MAX) return false;
+  const int64_t row_blocks = (static_cast<int64_t>(p.n_q) * p.num_q_heads + kLatMaxRows - 1) / kLatMaxRows;
+  return row_blocks * p.batch <= INT32_MAX / 4;
+}
+
+cudaError_t launch_latent_tc(const LatentParams& p, cudaStream_t stream) {
+  EncodeFn enc = encode_fn();
+  if (!enc) return cudaErrorNotSupported;
+  const LatentGeom& g = p.geom;
+  alignas(64) CUtensorMap map;
+  const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(g.page_size), static_cast<cuuint64_t>((g.latent_dim + g.rope_dim) / 64),
+                              static_cast<cuuint64_t>(g.num_pages)};
+  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(g.slot_stride) * 2, 128, static_cast<cuuint64_t>(g.page_stride) * 2};
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(g.page_size < kLTok ? g.page_size : kLTok), 1, 1};
+  const cuuint32_t step[4] = {1, 1, 1, 1};
+  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16*>(p.cache), dims, strides, box, step,
+          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorNotSupported;
+  int dev = 0, sms = 0;
+  cudaError_t e;
+  if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+  switch (latent_tile_rows(static_cast<int64_t>(p.n_q) * p.num_q_heads)) {
+    case 16: return launch_n<16>(map, p, sms, stream);
+    case 32: return launch_n<32>(map, p, sms, stream);
+    default: return launch_n<64>(map, p, sms, stream);
+  }
+}
+
+}  // namespace pda
