@@ -390,33 +390,49 @@ def set_persistent_threshold(min_units_per_cta: int):
 _same_context = contextlib.nullcontext()
 
 
-def _device_call(t):
+def _device_call(device):
     """The device the call's tensors live on becomes current for the call (streams, launches)."""
-    return _same_context if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+    return _same_context if device == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _raw(stream, device):
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _dp(t):
+    return None if t is None else t.data_ptr()
 
 
 def _same_device(*tensors):
+    """Device index that all given tensors (None is skipped) live on."""
     dev = None
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("expected CUDA tensors")
-        if dev is not None and t.device != dev:
-            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
-        dev = t.device
+        if t is not None:
+            d = t.get_device()
+            if d != dev:
+                if d < 0:
+                    raise ValueError("expected CUDA tensors")
+                if dev is not None:
+                    raise ValueError(f"tensors on different devices: {dev} and {d}")
+                dev = d
+    return dev
+
+
+_I32, _BF16 = torch.int32, torch.bfloat16
 
 
 def _int32(*tensors):
     for t in tensors:
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+        if t is not None and (t.dtype is not _I32 or not t.is_contiguous()):
             raise ValueError("expected contiguous int32 tensors")
 
 
 def _bf16_rows(name, t):
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not _BF16:
         raise TypeError(f"{name}: expected bfloat16, got {t.dtype}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
 
 
@@ -454,13 +470,13 @@ def paged_build_tables(seq_lens, new_lens, page_size, free_pages, free_count, bl
     stride = _check_table(block_table, B)
     if new_lens.shape[0] != B or cu_new.numel() < B + 1 or (positions is not None and positions.numel() < slot_map.numel()):
         raise ValueError("new_lens, cu_new or positions too short")
-    _same_device(seq_lens, new_lens, free_pages, free_count, block_table, cu_new, slot_map, positions, free_count_out, status)
+    dev = _same_device(seq_lens, new_lens, free_pages, free_count, block_table, cu_new, slot_map, positions, free_count_out, status)
     if free_count_out is None:
         free_count_out = free_count
-    with _device_call(seq_lens):
-        rc = lib().paged_build_tables(_ptr(seq_lens), _ptr(new_lens), B, int(page_size), _ptr(free_pages), free_pages.numel(),
-                                      _ptr(free_count), _ptr(free_count_out), _ptr(block_table), stride, _ptr(cu_new),
-                                      _ptr(slot_map), _ptr(positions), slot_map.numel(), _ptr(status), _stream(stream))
+    with _device_call(dev):
+        rc = lib().paged_build_tables(_dp(seq_lens), _dp(new_lens), B, int(page_size), _dp(free_pages), free_pages.numel(),
+                                      _dp(free_count), _dp(free_count_out), _dp(block_table), stride, _dp(cu_new),
+                                      _dp(slot_map), _dp(positions), slot_map.numel(), _dp(status), _raw(stream, dev))
     _check(rc, "paged_build_tables")
 
 
@@ -483,11 +499,11 @@ def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, 
         _bf16_rows("norm_weight", norm_weight)
         if norm_weight.numel() != R:
             raise ValueError("norm_weight: expected [latent_dim]")
-    _same_device(c_new, rope_new, cache, slot_map, norm_weight, status)
-    with _device_call(cache):
-        rc = lib().latent_append(_ptr(c_new), c_new.stride(0), _ptr(rope_new), 0 if rope_new is None else rope_new.stride(0),
-                                 _ptr(cache), C.byref(desc), _ptr(norm_weight), float(eps), _ptr(slot_map), T, _ptr(status),
-                                 _stream(stream))
+    dev = _same_device(c_new, rope_new, cache, slot_map, norm_weight, status)
+    with _device_call(dev):
+        rc = lib().latent_append(_dp(c_new), c_new.stride(0), _dp(rope_new), 0 if rope_new is None else rope_new.stride(0),
+                                 _dp(cache), C.byref(desc), _dp(norm_weight), float(eps), _dp(slot_map), T, _dp(status),
+                                 _raw(stream, dev))
     _check(rc, "latent_append")
 
 
@@ -530,12 +546,12 @@ def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale
     qls, qrs, os_ = _token_strides("q_latent", ql), (0, 0) if desc.rope_dim == 0 else _token_strides("q_rope", qr), _token_strides("out", o)
     if workspace is None:
         workspace = latent_workspace(B, H, T, R, device=cache.device)
-    _same_device(ql, qr, o, cache, block_table, seq_lens, workspace, status)
-    with _device_call(cache):
+    dev = _same_device(ql, qr, o, cache, block_table, seq_lens, workspace, status)
+    with _device_call(dev):
         rc = lib().paged_latent_attention(
-            _ptr(ql), qls[0], qls[1], None if desc.rope_dim == 0 else _ptr(qr), qrs[0], qrs[1], _ptr(cache), C.byref(desc),
-            _ptr(block_table), stride, _ptr(seq_lens), B, H, T, float(scale), _ptr(o), os_[0], os_[1],
-            _ptr(workspace), workspace.numel() * workspace.element_size(), flags, _ptr(status), _stream(stream))
+            _dp(ql), qls[0], qls[1], None if desc.rope_dim == 0 else _dp(qr), qrs[0], qrs[1], _dp(cache), C.byref(desc),
+            _dp(block_table), stride, _dp(seq_lens), B, H, T, float(scale), _dp(o), os_[0], os_[1],
+            _dp(workspace), workspace.numel() * workspace.element_size(), flags, _dp(status), _raw(stream, dev))
     _check(rc, "paged_latent_attention")
     return out
 
@@ -557,15 +573,15 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
     _int32(cu_q, cu_k, status)
     if cu_q.numel() != cu_k.numel() or cu_q.numel() < 1:
         raise ValueError("cu_q and cu_k: expected batch + 1 entries each")
-    _same_device(q, k_nope, k_rope if dr else None, v, out, cu_q, cu_k, status)
+    dev = _same_device(q, k_nope, k_rope if dr else None, v, out, cu_q, cu_k, status)
 
     def st(t, i):
         return t.stride(i) if t.shape[i] > 1 else 0
 
-    with _device_call(q):
+    with _device_call(dev):
         rc = lib().latent_prefill_attention(
-            _ptr(q), st(q, 0), st(q, 1), _ptr(k_nope), st(k_nope, 0), st(k_nope, 1), _ptr(k_rope) if dr else None,
-            st(k_rope, 0) if dr else 0, _ptr(v), st(v, 0), st(v, 1), _ptr(cu_q), _ptr(cu_k), cu_q.numel() - 1, H, dn, dr, dv,
-            int(max_q), tq, tk, float(scale), _ptr(out), st(out, 0), st(out, 1), flags, _ptr(status), _stream(stream))
+            _dp(q), st(q, 0), st(q, 1), _dp(k_nope), st(k_nope, 0), st(k_nope, 1), _dp(k_rope) if dr else None,
+            st(k_rope, 0) if dr else 0, _dp(v), st(v, 0), st(v, 1), _dp(cu_q), _dp(cu_k), cu_q.numel() - 1, H, dn, dr, dv,
+            int(max_q), tq, tk, float(scale), _dp(out), st(out, 0), st(out, 1), flags, _dp(status), _raw(stream, dev))
     _check(rc, "latent_prefill_attention")
     return out

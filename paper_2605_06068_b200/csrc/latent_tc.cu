@@ -48,6 +48,7 @@ constexpr int kLProducer = 4, kLSIssue = 5, kLPvIssue = 6, kLQLoad = 7;
 constexpr uint32_t kLTmemCols = 512, kLTmemS = 256;  // O^T: R / 128 blocks of N columns from 0; S^T from 256
 constexpr float kLNoMax = -1e30f;               // reference of a row that has seen no score yet
 constexpr float kLRescale = 8.f;                // log2
+constexpr int kLAhead = 3;                      // tiles fetched into L2 ahead of their copies
 constexpr int kLMinSpan = 2;                    // tiles: below this a span costs more than it shortens
 
 template <int N>
@@ -63,6 +64,13 @@ static_assert(LCfg<64>::kSmemBytes <= 232448, "shared memory");
 
 struct LPlan {
   int32_t row_blocks, per_pass, passes, groups;  // row blocks per sequence; taken at once; rounds; CTA groups
+  int32_t page_shift;                            // log2 of the page size
+  int32_t q_box;                                 // heads per copy of Q (0: rows by plain copies)
+};
+
+struct LMaps {
+  CUtensorMap line, pair, whole;  // the cache: one line, two lines, all lines of a run of slots
+  CUtensorMap q_latent, q_rope;  // one line of q_box heads of a token
 };
 
 struct LRecord {  // a sequence whose first span is this one and that continues: see latent_merge_kernel
@@ -86,6 +94,7 @@ struct Segment {
 
 struct Walk {
   int vseq, off, rem;
+  int L0;  // tokens of the first sequence; -1 behind it
 };
 
 template <int N>
@@ -95,7 +104,8 @@ __device__ __forceinline__ bool next_segment(const LatentParams& p, const LPlan&
   s.b = w.vseq % p.batch;
   const int rb = (w.vseq / p.batch) * plan.per_pass + r;
   s.rb = rb < plan.row_blocks ? rb : -1;
-  s.L = seq_tokens(p, s.b);
+  s.L = w.L0 >= 0 ? w.L0 : seq_tokens(p, s.b);
+  w.L0 = -1;
   s.whole = seq_tiles(s.L);
   s.off = w.off;
   s.take = min(s.whole - w.off, w.rem);
@@ -116,6 +126,8 @@ __device__ __forceinline__ void mma_ss_if(uint32_t leader, uint32_t d_tmem, uint
       "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, pa;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
+// A value that all lanes hold, said so to the compiler.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 // bf16 x bf16 -> f32, M x N
 __host__ __device__ constexpr uint32_t latent_idesc(int m, int n, bool a_mn, bool b_mn) {
   return (1u << 4) | (kFmtBf16 << 7) | (kFmtBf16 << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
@@ -128,6 +140,20 @@ __device__ __forceinline__ void tma_load_4d_hint_if(uint32_t leader, uint32_t ds
       "@pe cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
       " [%0], [%1, {0, %3, %4, %5}], [%2], %7;\n\t}"
       ::"r"(dst), "l"(map), "r"(bar), "r"(slot), "r"(line), "r"(page), "r"(leader), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int line,
+                                               int head, int token) {
+  asm volatile(
+      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %6, 0;\n\t"
+      "@pe cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {0, %3, %4, %5}], [%2];\n\t}"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(line), "r"(head), "r"(token), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_4d_if(uint32_t leader, const CUtensorMap* map, int slot, int page) {
+  asm volatile(
+      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %3, 0;\n\t"
+      "@pe cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {0, %1, 0, %2}];\n\t}"
+      ::"l"(map), "r"(slot), "r"(page), "r"(leader) : "memory");
 }
 __device__ __forceinline__ uint64_t l2_policy_normal() {
   uint64_t pol;
@@ -181,7 +207,7 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32
 
 template <int N>
 __global__ void __launch_bounds__(kLThreads, 1)
-latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ LatentParams p,
+latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ LatentParams p,
                  const __grid_constant__ LPlan plan) {
   using C = LCfg<N>;
   extern __shared__ uint8_t smem_raw[];
@@ -194,27 +220,26 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   uint64_t* bars = reinterpret_cast<uint64_t*>(rows_raw + C::kRowBytes);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 40);
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
-  int* span = cta_err + 1;                                          // [3] first sequence, tile, tiles
-  int64_t* scan = reinterpret_cast<int64_t*>(wred);                 // (start of the kernel only) [8] warps' sums
+  int* span = cta_err + 1;                                          // [4] first sequence, tile, tiles, its tokens
+  uint32_t* scan = reinterpret_cast<uint32_t*>(wred);               // (start of the kernel only) [8] warps' sums
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = blockIdx.x / plan.per_pass, r = blockIdx.x % plan.per_pass;
   const LatentGeom& geo = p.geom;
   const int m_tiles = geo.latent_dim / 128, n_groups = m_tiles + 1;
-  asm volatile("griddepcontrol.launch_dependents;");
-
-  // a CTA of this launch has met an expired wait: the rest do not start (the output is lost anyway)
-  const LatentWorkspace lay = latent_workspace_layout(p.num_q_heads, p.n_q, geo.latent_dim);
-  uint8_t* ws = static_cast<uint8_t*>(p.workspace);
-  if (p.status != nullptr && __syncthreads_or(*reinterpret_cast<volatile int32_t*>(p.status) == PDA_DEV_TIMEOUT)) {
-    if (r == 0 && tid == 0) reinterpret_cast<LRecord*>(ws + lay.records)[g] = LRecord{-1, 0, 0, 0};  // (nothing to merge)
-    return;
-  }
-
   const uint32_t ring = smem_u32(smem), q_sm = ring + kLStages * kLStageBytes, p_sm = q_sm + C::kQBytes;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kLStages * kLGroups;  // [stage][group]
   const uint32_t bar_s = empty0 + 8 * kLStages * kLGroups, bar_sfree = bar_s + 16, bar_p = bar_sfree + 16, bar_pv = bar_p + 8,
                  bar_q = bar_pv + 8, bar_qfree = bar_q + 8, bar_ofree = bar_qfree + 8, bar_drain = bar_ofree + 8;
+  // (the set-up that reads nothing runs beside the end of the kernel before this one)
+  if (warp == kLProducer && elect_one()) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.line) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.pair) : "memory");
+  }
+  if (warp == kLQLoad && plan.q_box > 0 && elect_one()) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q_latent) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q_rope) : "memory");
+  }
   if (tid == 0) {
     for (int i = 0; i < 2 * kLStages * kLGroups; ++i) mbar_init(full0 + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
@@ -232,45 +257,54 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     fence_mbar_init();
     fence_proxy_async();
   }
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // (tensor memory only now: a kernel before this one may still have had to ask for its own)
   if (warp == kLSIssue) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kLTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // once a CTA of this launch has met an expired wait, the rest find no work (the output is lost anyway)
+  const LatentWorkspace lay = latent_workspace_layout(p.num_q_heads, p.n_q, geo.latent_dim);
+  uint8_t* ws = static_cast<uint8_t*>(p.workspace);
+  const int status_now = p.status != nullptr ? *reinterpret_cast<volatile int32_t*>(p.status) : 0;
   // ---- this group's span of the tile list: every thread sums a run of sequences, then the sums are scanned
   const int per_thread = (p.batch + kLThreads - 1) / kLThreads;
   const int b0 = min(tid * per_thread, p.batch), b1 = min(b0 + per_thread, p.batch);
-  int64_t mine = 0;
+  uint32_t mine = 0;  // (the host has checked that the list fits 32 bits)
   for (int b = b0; b < b1; ++b) mine += seq_tiles(seq_tokens(p, b));
-  int64_t incl = mine;
+  uint32_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+    const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += u;
   }
   if (lane == 31) scan[warp] = incl;
   tc_fence_before();
-  __syncthreads();
+  const bool dead = __syncthreads_or(status_now == PDA_DEV_TIMEOUT);
   tc_fence_after();
-  int64_t list = 0, before = 0;
+  uint32_t list = 0, before = 0;
 #pragma unroll
   for (int w = 0; w < kLThreads / 32; ++w) {
     before += w < warp ? scan[w] : 0;
     list += scan[w];
   }
   before += incl - mine;
-  const int64_t total = list * plan.passes;
-  const int64_t span_tiles = max((total + plan.groups - 1) / plan.groups, static_cast<int64_t>(kLMinSpan));
-  const int64_t start = g * span_tiles, stop = min(start + span_tiles, total);
-  if (start < stop) {
-    const int64_t pass = start / list, in_pass = start - pass * list;
+  const uint32_t total = list * plan.passes;
+  const int span_tiles = max(static_cast<int>((total + plan.groups - 1) / plan.groups), kLMinSpan);
+  const int64_t start = static_cast<int64_t>(g) * span_tiles;
+  if (start < total && !dead) {
+    const uint32_t pass = static_cast<uint32_t>(start) / list, in_pass = static_cast<uint32_t>(start) - pass * list;
     if (in_pass >= before && in_pass < before + mine) {  // (one thread)
-      int64_t at = before;
+      uint32_t at = before;
       for (int b = b0; b < b1; ++b) {
-        const int n = seq_tiles(seq_tokens(p, b));
+        const int L = seq_tokens(p, b);
+        const uint32_t n = seq_tiles(L);
         if (in_pass < at + n) {
+          span[3] = L;
           span[0] = static_cast<int>(pass) * p.batch + b;
           span[1] = static_cast<int>(in_pass - at);
-          span[2] = static_cast<int>(stop - start);
+          span[2] = static_cast<int>(min(static_cast<int64_t>(span_tiles), total - start));
           break;
         }
         at += n;
@@ -279,53 +313,79 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   }
   __syncthreads();
   const uint32_t tmem = *tmem_slot;
-  Walk walk{span[0], span[1], span[2]};
+  Walk walk{span[0], span[1], span[2], span[3]};
   Segment s;
   bool ok = true;
 
   if (warp == kLProducer) {
     // ================= TMA producer: lines of the tiles, in the order in which they are read and freed ========
     const uint32_t leader = elect_one();
-    const int box = min(geo.page_size, kLTok), ept = kLTok / box;  // rows per copy, copies per line of a tile
+    const int box = uniform(min(geo.page_size, kLTok)), ept = kLTok / box;  // rows per copy, copies per line of a tile
     // row blocks of other CTAs read the same tiles: only a tile that is read once is marked to leave L2 first
     const uint64_t policy = plan.row_blocks == 1 ? l2_policy_evict_first() : l2_policy_normal();
-    int i = 0;  // tiles of this CTA
+    const int ahead = r == 0 ? min(kLAhead, 32 / ept) : 0;  // (the row blocks of a span read the same tiles)
+    int i = 0, cur_batch = 0;  // tiles of this CTA
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
+      if (s.n_tiles == 0) continue;
       const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
       const int batch_tiles = 32 / ept;  // tiles whose page ids the lanes hold
       auto load_ids = [&](int t) -> int {  // lane -> copy (t + lane / ept, lane % ept) of this segment
-        const int tile = t + lane / ept;
-        const int64_t tok = static_cast<int64_t>(s.tile0 + tile) * kLTok + (lane % ept) * box;
+        const int tile = t + lane / ept, tok = (s.tile0 + tile) * kLTok + (lane % ept) * box;
         if (tile >= s.n_tiles || tok >= s.L) return 0;
-        const int v = __ldg(table + tok / geo.page_size);
+        const int v = __ldg(table + (tok >> plan.page_shift));
         return v < 0 || v >= geo.num_pages ? 0 : v;  // (the softmax warps look for these and drop the segment)
       };
-      int ids = load_ids(0), ids_next = 0;
+      int ids = load_ids(0), ids_next = load_ids(batch_tiles);
+      // Tiles are fetched into L2 a few ahead of the copies: two stages do not cover the trip to memory.
+      auto prefetch = [&](int t) {  // t within the ids held: this batch or the next
+        const int in_batch = t % batch_tiles, tok0 = (s.tile0 + t) * kLTok;
+        const int n_copies = min(ept, (s.L - tok0 + box - 1) / box);
+        for (int c = 0; c < n_copies; ++c) {
+          const int page = __shfl_sync(0xffffffffu, t / batch_tiles == cur_batch ? ids : ids_next, in_batch * ept + c);
+          tma_prefetch_4d_if(leader, &maps.whole, uniform((tok0 + c * box) & (geo.page_size - 1)), page);
+        }
+      };
+      cur_batch = 0;
       for (int t = 0; t < s.n_tiles; ++t, ++i) {
         const int in_batch = t % batch_tiles;
-        if (in_batch == 0) {
-          if (t > 0) ids = ids_next;
+        if (in_batch == 0 && t > 0) {
+          ids = ids_next;
+          ++cur_batch;
           ids_next = load_ids(t + batch_tiles);
         }
-        const int st = i & 1;
         const int tok0 = (s.tile0 + t) * kLTok;
-        const int n_copies = min(ept, (s.L - tok0 + box - 1) / box);
-        for (int gr = 0; gr < n_groups; ++gr) {
-          const uint32_t idx = 8 * (st * kLGroups + gr);
-          if (i >= kLStages) ok = mbar_wait_bounded(empty0 + idx, ((i >> 1) - 1) & 1);
+        const int n_copies = uniform(min(ept, (s.L - tok0 + box - 1) / box));
+        const uint32_t st = uniform(i & 1), sb = ring + st * kLStageBytes, bars0 = 8 * (st * kLGroups);
+        const uint32_t parity = ((i >> 1) - 1) & 1;
+        const uint32_t line_bytes = n_copies * box * 128;
+        const int slot = uniform(tok0 & (geo.page_size - 1));
+        const int page0 = __shfl_sync(0xffffffffu, ids, in_batch * ept);
+        // rope first: it is freed first (by the S product), then the latent pairs as P . C frees them
+#pragma unroll
+        for (int gr = 0; gr < kLGroups; ++gr) {
+          if (gr >= n_groups) break;
+          if (i >= kLStages) ok = mbar_spin_bounded(empty0 + bars0 + 8 * gr, parity);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1), n_lines = gr == 0 ? 1 : 2;
-          mbar_expect_tx_if(leader, full0 + idx, n_lines * n_copies * box * 128);
-          for (int c = 0; c < n_copies; ++c) {
-            const int page = __shfl_sync(0xffffffffu, ids, in_batch * ept + c);
-            const int slot = (tok0 + c * box) & (geo.page_size - 1);
-            for (int ln = 0; ln < n_lines; ++ln)
-              tma_load_4d_hint_if(leader, ring + st * kLStageBytes + (line0 + ln) * kLLineBytes + c * box * 128, &map, full0 + idx,
-                                  slot, line0 + ln, page, policy);
+          const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1);
+          const uint32_t bar = full0 + bars0 + 8 * gr, dst = sb + line0 * kLLineBytes;
+          mbar_expect_tx_if(leader, bar, gr == 0 ? line_bytes : 2 * line_bytes);
+          // (a copy of 64 rows takes both lines of a group at once; smaller pages go line by line, so that
+          // the rows of a line stay together)
+          if (box == kLTok) {
+            tma_load_4d_hint_if(leader, dst, gr == 0 ? &maps.line : &maps.pair, bar, slot, line0, page0, policy);
+          } else {
+            for (int c = 0; c < n_copies; ++c) {
+              const int page = __shfl_sync(0xffffffffu, ids, in_batch * ept + c);  // (a box is a whole page)
+              tma_load_4d_hint_if(leader, dst + c * box * 128, &maps.line, bar, 0, line0, page, policy);
+              if (gr > 0) tma_load_4d_hint_if(leader, dst + kLLineBytes + c * box * 128, &maps.line, bar, 0, line0 + 1, page, policy);
+            }
           }
         }
         if (!ok) break;
+        // (the first tiles of a segment: once the two that go straight to shared memory are under way)
+        if (t >= 1)
+          for (int k = t == 1 ? 2 : t + ahead; k <= min(t + ahead, s.n_tiles - 1); ++k) prefetch(k);
       }
     }
     if (!ok) {  // copies in flight end before the CTA does
@@ -337,7 +397,6 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     // ================= S^T(i) = C . Q^T =================
     constexpr uint32_t idesc = latent_idesc(64, N, false, false);
     const uint32_t leader = elect_one();
-    const uint32_t u_tmem = __shfl_sync(0xffffffffu, tmem, 0);
     int i = 0, seg = 0;
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
       if (s.n_tiles == 0) continue;
@@ -347,18 +406,23 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         if (i >= 2) ok = mbar_spin_bounded(bar_sfree + 8 * st, ((i >> 1) - 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const uint32_t d = u_tmem + kLTmemS + st * N;
-        for (int gr = 0; gr < n_groups; ++gr) {
-          ok = mbar_wait_bounded(full0 + 8 * (st * kLGroups + gr), (i >> 1) & 1);
+        // (operands warp-uniform by a shuffle, offsets constant: 33 clocks an MMA; computed per thread: 100)
+        const uint32_t d = uniform(tmem + kLTmemS + st * N), sb = uniform(ring + st * kLStageBytes), u_q = uniform(q_sm);
+#pragma unroll
+        for (int gr = 0; gr < kLGroups; ++gr) {
+          if (gr >= n_groups) break;
+          ok = mbar_spin_bounded(full0 + 8 * (st * kLGroups + gr), (i >> 1) & 1);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
-          const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1), n_lines = gr == 0 ? 1 : 2;
-          for (int ln = line0; ln < line0 + n_lines; ++ln) {
-            const uint64_t ad = tc_desc(ring + st * kLStageBytes + ln * kLLineBytes, 16, 1024);
-            const uint64_t bd = tc_desc(q_sm + ln * (N * 128), 16, 1024);
+          const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1);
+          const uint64_t ad = tc_desc(sb + line0 * kLLineBytes, 16, 1024), bd = tc_desc(u_q + line0 * (N * 128), 16, 1024);
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) mma_ss_if(leader, d, ad + 2 * ks, bd + 2 * ks, idesc, (gr | ks) ? 1u : 0u);
+          for (int ks = 0; ks < 4; ++ks) mma_ss_if(leader, d, ad + 2 * ks, bd + 2 * ks, idesc, (ks > 0 || gr > 0) ? 1u : 0u);
+          if (gr > 0) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              mma_ss_if(leader, d, ad + kLLineBytes / 16 + 2 * ks, bd + N * 128 / 16 + 2 * ks, idesc, 1u);
           }
         }
         if (!ok) break;
@@ -376,7 +440,6 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     // ================= O^T += C^T . P^T(i) =================
     constexpr uint32_t idesc = latent_idesc(128, N, true, true);
     const uint32_t leader = elect_one();
-    const uint32_t u_tmem = __shfl_sync(0xffffffffu, tmem, 0);
     int i = 0, seg = 0;
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
       if (s.n_tiles == 0) continue;
@@ -387,13 +450,16 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        const uint64_t bd = tc_desc(p_sm, 16, 1024);
-        for (int m = 0; m < m_tiles; ++m) {
-          const uint64_t ad = tc_desc(ring + st * kLStageBytes + 2 * m * kLLineBytes, kLLineBytes, 1024);
+        const uint64_t bd = tc_desc(uniform(p_sm), 16, 1024);
+        const uint32_t sb = uniform(ring + st * kLStageBytes), d = uniform(tmem), bars0 = uniform(empty0 + 8 * (st * kLGroups + 1));
+        const uint32_t acc = uniform(t > 0 ? 1u : 0u);
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-            mma_ss_if(leader, u_tmem + m * N, ad + 128 * ks, bd + 128 * ks, idesc, (t > 0 || ks > 0) ? 1u : 0u);
-          tc_commit_if(leader, empty0 + 8 * (st * kLGroups + 1 + m));
+        for (int m = 0; m < kLGroups - 1; ++m) {
+          if (m >= m_tiles) break;
+          const uint64_t ad = tc_desc(sb + 2 * m * kLLineBytes, kLLineBytes, 1024);
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) mma_ss_if(leader, d + m * N, ad + 128 * ks, bd + 128 * ks, idesc, ks > 0 ? 1u : acc);
+          tc_commit_if(leader, bars0 + 8 * m);
         }
         tc_commit_if(leader, bar_pv);
       }
@@ -409,9 +475,26 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
       if (s.n_tiles == 0) continue;
       if (seg > 0) {
-        ok = mbar_wait_bounded(bar_qfree, (seg - 1) & 1);
+        ok = mbar_spin_bounded(bar_qfree, (seg - 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
+      }
+      if (plan.q_box > 0) {
+        // runs of q_box heads of one token (one query token: N heads, those beyond the last are zero)
+        const uint32_t leader = elect_one();
+        const int live = min(N, p.n_q * p.num_q_heads - s.rb * N);
+        const int runs = (live + plan.q_box - 1) / plan.q_box, lines = 2 * m_tiles + 1;
+        mbar_expect_tx_if(leader, bar_q, uniform(runs * plan.q_box * lines * 128));
+        for (int k = 0; k < runs; ++k) {
+          const int row = s.rb * N + k * plan.q_box;
+          const int t = uniform(row / p.num_q_heads), h = uniform(row - t * p.num_q_heads);
+          const int token = uniform(s.b * p.n_q + t);
+          const uint32_t dst = uniform(q_sm + k * plan.q_box * 128);
+          for (int ln = 0; ln < lines - 1; ++ln) tma_load_4d_if(leader, dst + ln * (N * 128), &maps.q_latent, bar_q, ln, h, token);
+          tma_load_4d_if(leader, dst + (lines - 1) * (N * 128), &maps.q_rope, bar_q, 0, h, token);
+        }
+        ++seg;
+        continue;
       }
       const int cv = geo.latent_dim / 8;
       for (int n = 0; n < N; ++n) {
@@ -432,7 +515,10 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       if (lane == 0) mbar_arrive_tc(bar_q);
       ++seg;
     }
-    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    if (!ok) {
+      if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+      if (seg > 0) mbar_wait_bounded(bar_q, (seg - 1) & 1, 1u << 12);
+    }
   } else {
     // ================= softmax, output =================
     // After an expired wait a warp goes on without waiting (the four meet at the same named barriers), and
@@ -451,7 +537,7 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       first_in_span = false;
       const bool is_first = s.off == 0, is_last = s.off + s.take == s.whole;
       if (is_first && !is_last)
-        rec = LRecord{s.vseq, 2 * g + (at_start ? 0 : 1), 1 + static_cast<int>((s.whole - s.take + span_tiles - 1) / span_tiles), 0};
+        rec = LRecord{s.vseq, 2 * g + (at_start ? 0 : 1), 1 + (s.whole - s.take - 1) / span_tiles + 1, 0};
       if (s.rb < 0) continue;
       const bool partial = !(is_first && is_last);
       const int slot = 2 * g + (at_start ? 0 : 1);
@@ -468,8 +554,8 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         if (raw > 0 && s.L == 0 && tid == 0) report(p.status, PDA_DEV_BAD_SEQ_LEN);
         const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
         const int64_t tok_end = min(static_cast<int64_t>(s.off + s.take) * kLTok, static_cast<int64_t>(s.L));
-        const int pg1 = static_cast<int>((tok_end + geo.page_size - 1) / geo.page_size);
-        for (int k = static_cast<int>(static_cast<int64_t>(s.off) * kLTok / geo.page_size) + tid; k < pg1; k += 128) {
+        const int pg1 = static_cast<int>((tok_end + geo.page_size - 1) >> plan.page_shift);
+        for (int k = static_cast<int>((static_cast<int64_t>(s.off) * kLTok) >> plan.page_shift) + tid; k < pg1; k += 128) {
           const int v = __ldg(table + k);
           bad |= v < 0 || v >= geo.num_pages;
         }
@@ -569,7 +655,13 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             tmem_ld16(tmem + lane_base + cb, ov);
             tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) ov[k] = __float_as_uint(__uint_as_float(ov[k]) * alpha[(cb + k) % N]);
+            for (int k = 0; k < 16; k += 4) {
+              const float4 a = *reinterpret_cast<const float4*>(alpha + (cb & (N - 1)) + k);
+              ov[k] = __float_as_uint(__uint_as_float(ov[k]) * a.x);
+              ov[k + 1] = __float_as_uint(__uint_as_float(ov[k + 1]) * a.y);
+              ov[k + 2] = __float_as_uint(__uint_as_float(ov[k + 2]) * a.z);
+              ov[k + 3] = __float_as_uint(__uint_as_float(ov[k + 3]) * a.w);
+            }
             tmem_st16(tmem + lane_base + cb, ov);
           }
           tmem_wait_st();
@@ -620,13 +712,21 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           tmem_ld16(tmem + lane_base + m * N + cb, ov);
           tmem_wait_ld();
           float v[16];
+          int32_t off[16];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = s.n_tiles > 0 && ok && !bad ? __uint_as_float(ov[k]) * inv_l[cb + k] : 0.f;
+          for (int k = 0; k < 16; k += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(inv_l + cb + k);
+            const int4 o = *reinterpret_cast<const int4*>(row_off + cb + k);
+            v[k] = f.x; v[k + 1] = f.y; v[k + 2] = f.z; v[k + 3] = f.w;
+            off[k] = o.x; off[k + 1] = o.y; off[k + 2] = o.z; off[k + 3] = o.w;
+          }
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = s.n_tiles > 0 && ok && !bad ? __uint_as_float(ov[k]) * v[k] : 0.f;
           if (partial) {
             float* dst = reinterpret_cast<float*>(ws + lay.part_o) + (part_row0 + cb) * geo.latent_dim + dim;
 #pragma unroll
             for (int k = 0; k < 16; ++k)
-              if (row_off[cb + k] >= 0) dst[static_cast<int64_t>(k) * geo.latent_dim] = v[k];
+              if (off[k] >= 0) dst[k * geo.latent_dim] = v[k];
           } else {
             // neighbouring lanes swap, so that each stores two dims of one row
             const bool odd = lane & 1;
@@ -634,8 +734,8 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             for (int k = 0; k < 16; k += 2) {
               const float other = __shfl_xor_sync(0xffffffffu, odd ? v[k] : v[k + 1], 1);
               const uint32_t w = odd ? pack2<false>(other, v[k + 1]) : pack2<false>(v[k], other);
-              const int64_t off = row_off[cb + k + (odd ? 1 : 0)];
-              if (off >= 0) *reinterpret_cast<uint32_t*>(p.out + 8 * off + (dim & ~1)) = w;
+              const int64_t to = odd ? off[k + 1] : off[k];
+              if (to >= 0) *reinterpret_cast<uint32_t*>(p.out + 8 * to + (dim & ~1)) = w;
             }
           }
         }
@@ -661,50 +761,84 @@ latent_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   }
 }
 
-// Rows of the sequences that lie in several spans: one CTA per row of every span boundary's sequence.
-template <int N>
-__global__ void __launch_bounds__(128) latent_merge_kernel(const __grid_constant__ LatentParams p, const __grid_constant__ LPlan plan) {
+// Rows of the sequences that lie in several spans. Grid: (span, row block, rows). kWide: a CTA per row, its
+// warps sharing the row's segments (few sequences, each over many spans); else a warp per row (many
+// sequences over two or three spans: a quarter of the CTAs).
+constexpr int kMergeWarps = 4;
+template <int N, bool kWide>
+__global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __grid_constant__ LatentParams p,
+                                                                        const __grid_constant__ LPlan plan) {
+  __shared__ float4 acc_sh[kWide ? kMergeWarps - 1 : 1][kWide ? 128 : 1];
+  __shared__ float w_sh[kMergeWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const LatentWorkspace lay = latent_workspace_layout(p.num_q_heads, p.n_q, p.geom.latent_dim);
   const uint8_t* ws = static_cast<const uint8_t*>(p.workspace);
   const LRecord rec = reinterpret_cast<const LRecord*>(ws + lay.records)[blockIdx.x];
   if (rec.vseq < 0) return;
-  const int r = blockIdx.y, n = blockIdx.z, tid = threadIdx.x;
+  const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = kWide ? blockIdx.z : blockIdx.z * kMergeWarps + warp;
   const int row = ((rec.vseq / p.batch) * plan.per_pass + r) * N + n, b = rec.vseq % p.batch;
-  if (row >= p.n_q * p.num_q_heads) return;
+  if (row >= p.n_q * p.num_q_heads) return;  // (kWide: the whole CTA)
   const int t = row / p.num_q_heads, h = row - t * p.num_q_heads;
   __nv_bfloat16* out = p.out + (static_cast<int64_t>(b) * p.n_q + t) * p.out_token_stride + h * p.out_head_stride;
-  const int R = p.geom.latent_dim;
+  const int vecs = p.geom.latent_dim / 4;  // 16-byte vectors of a partial row, a multiple of 32
   const float* lse = reinterpret_cast<const float*>(ws + lay.part_lse);
-  const float* part = reinterpret_cast<const float*>(ws + lay.part_o);
+  const float4* part = reinterpret_cast<const float4*>(ws + lay.part_o);
   const int g0 = blockIdx.x;
-  auto row_of = [&](int k) -> int64_t {  // slot of the k-th segment: later spans hold theirs in their first slot
+  auto row_of = [&](int k) -> int64_t {  // row of the k-th segment: later spans hold theirs in their first slot
     return (static_cast<int64_t>(k == 0 ? rec.first_slot : 2 * (g0 + k)) * plan.per_pass + r) * N + n;
   };
   float M = -INFINITY;
-  for (int k = tid & 31; k < rec.n_seg; k += 32) M = fmaxf(M, lse[row_of(k)]);
+  for (int k = lane; k < rec.n_seg; k += 32) M = fmaxf(M, lse[row_of(k)]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   const bool dead = M == -INFINITY || M == INFINITY;  // nothing to attend, or a bad page
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 acc[4];
+#pragma unroll
+  for (int v = 0; v < 4; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
   float W = 0.f;
-  if (tid * 4 < R && !dead) {
-#pragma unroll 8
-    for (int k = 0; k < rec.n_seg; ++k) {
+  if (!dead) {
+#pragma unroll 4
+    for (int k = kWide ? warp : 0; k < rec.n_seg; k += kWide ? kMergeWarps : 1) {
       const int64_t at = row_of(k);
       const float w = ex2(lse[at] - M);
-      const float4 v = *reinterpret_cast<const float4*>(part + at * R + tid * 4);
       W += w;
-      acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y);
-      acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        if (v * 32 < vecs) {
+          const float4 x = part[at * vecs + v * 32 + lane];
+          acc[v].x = fmaf(w, x.x, acc[v].x); acc[v].y = fmaf(w, x.y, acc[v].y);
+          acc[v].z = fmaf(w, x.z, acc[v].z); acc[v].w = fmaf(w, x.w, acc[v].w);
+        }
+      }
     }
   }
-  if (tid * 4 < R) {
-    const float inv = dead ? 0.f : 1.f / W;
-    uint2 o;
-    o.x = pack2<false>(acc.x * inv, acc.y * inv);
-    o.y = pack2<false>(acc.z * inv, acc.w * inv);
-    *reinterpret_cast<uint2*>(out + tid * 4) = o;
+  if constexpr (kWide) {  // warp 0 adds the warps' sums, in their order
+    if (warp > 0) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc_sh[warp - 1][v * 32 + lane] = acc[v];
+      if (lane == 0) w_sh[warp] = W;
+    }
+    __syncthreads();
+    if (warp > 0) return;
+    for (int u = 1; u < kMergeWarps; ++u) {
+      W += w_sh[u];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float4 x = acc_sh[u - 1][v * 32 + lane];
+        acc[v].x += x.x; acc[v].y += x.y; acc[v].z += x.z; acc[v].w += x.w;
+      }
+    }
+  }
+  const float inv = dead ? 0.f : 1.f / W;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    if (v * 32 < vecs) {
+      uint2 o;
+      o.x = pack2<false>(acc[v].x * inv, acc[v].y * inv);
+      o.y = pack2<false>(acc[v].z * inv, acc[v].w * inv);
+      *reinterpret_cast<uint2*>(out + 4 * (v * 32 + lane)) = o;
+    }
   }
 }
 
@@ -725,7 +859,7 @@ EncodeFn encode_fn() {
 // How many row blocks run at once, and how often: the choice that keeps most CTAs busy, for at most 37
 // row blocks at once (four groups of CTAs), fewer rounds first.
 LPlan make_plan(int row_blocks, int ctas) {
-  LPlan best{row_blocks, 1, row_blocks, ctas};
+  LPlan best{row_blocks, 1, row_blocks, ctas, 0, 0};
   double best_eff = -1.0;
   for (int passes = 1; passes <= row_blocks; ++passes) {
     const int per = (row_blocks + passes - 1) / passes;
@@ -734,32 +868,84 @@ LPlan make_plan(int row_blocks, int ctas) {
     const double eff = static_cast<double>(row_blocks) / (static_cast<double>(passes) * per) * groups * per / ctas;
     if (eff > best_eff + 0.02) {
       best_eff = eff;
-      best = LPlan{row_blocks, per, passes, groups};
+      best = LPlan{row_blocks, per, passes, groups, 0, 0};
     }
     if (per == 1) break;
   }
   return best;
 }
 
+// Map of [pages][lines of 128 bytes][rows][64 elements], box [1][box_lines][box_rows][64].
+bool encode_map(EncodeFn enc, CUtensorMap* map, const void* base, int64_t lines, int64_t rows, int64_t outer, int64_t row_stride,
+                int64_t outer_stride, int box_lines, int box_rows, bool lines_inner) {
+  const cuuint64_t rs = static_cast<cuuint64_t>(row_stride) * 2, os = static_cast<cuuint64_t>(outer_stride) * 2;
+  const cuuint64_t nl = lines, nr = rows, no = outer;
+  const cuuint64_t dims[4] = {64, lines_inner ? nl : nr, lines_inner ? nr : nl, no};
+  const cuuint64_t strides[3] = {lines_inner ? 128 : rs, lines_inner ? rs : 128, os};
+  const cuuint32_t bl = box_lines, br = box_rows;
+  const cuuint32_t box[4] = {64, lines_inner ? bl : br, lines_inner ? br : bl, 1};
+  const cuuint32_t step[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Heads per copy of Q: all N rows at once for one query token, else the largest run of heads that divides
+// both a token's heads and a row block and keeps the swizzle's 8-row period; 0 where there is none, or where
+// the strides are not a tensor map's.
+int q_box_of(const LatentParams& p, int N) {
+  const auto fits = [](int64_t stride, int64_t extent) { return extent == 1 || (stride > 0 && stride < (1ll << 38)); };
+  const int64_t tokens = static_cast<int64_t>(p.batch) * p.n_q;
+  if (!fits(p.ql_token_stride, tokens) || !fits(p.qr_token_stride, tokens) || !fits(p.ql_head_stride, p.num_q_heads) ||
+      !fits(p.qr_head_stride, p.num_q_heads))
+    return 0;
+  if (p.n_q == 1) return N;
+  for (int box = N; box >= 8; box /= 2)
+    if (p.num_q_heads % box == 0) return box;
+  return 0;
+}
+
+// Launch attributes: the kernel may be placed while the one before it on the stream ends (both kernels here
+// wait for that one's end before they read anything).
+struct OverlapConfig {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  OverlapConfig(dim3 grid, int threads, int smem, cudaStream_t stream) {
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+  }
+};
+
 template <int N>
-cudaError_t launch_n(const CUtensorMap& map, const LatentParams& p, int sms, cudaStream_t stream) {
+cudaError_t launch_n(EncodeFn enc, LMaps& maps, const LatentParams& p, int sms, cudaStream_t stream) {
   const int rows = p.n_q * p.num_q_heads;
-  const LPlan plan = make_plan((rows + N - 1) / N, sms < kLatMaxCtas ? sms : kLatMaxCtas);
+  LPlan plan = make_plan((rows + N - 1) / N, sms < kLatMaxCtas ? sms : kLatMaxCtas);
+  plan.page_shift = __builtin_ctz(p.geom.page_size);
+  plan.q_box = q_box_of(p, N);
+  if (plan.q_box > 0) {
+    const int64_t tokens = static_cast<int64_t>(p.batch) * p.n_q;
+    const auto some = [](int64_t stride, int64_t extent) { return extent == 1 ? int64_t{64} : stride; };  // (never stepped)
+    if (!encode_map(enc, &maps.q_latent, p.q_latent, p.geom.latent_dim / 64, p.num_q_heads, tokens,
+                    some(p.ql_head_stride, p.num_q_heads), some(p.ql_token_stride, tokens), 1, plan.q_box, true) ||
+        !encode_map(enc, &maps.q_rope, p.q_rope, 1, p.num_q_heads, tokens, some(p.qr_head_stride, p.num_q_heads),
+                    some(p.qr_token_stride, tokens), 1, plan.q_box, true))
+      return cudaErrorNotSupported;
+  }
   cudaError_t e = cudaFuncSetAttribute(latent_tc_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, LCfg<N>::kSmemBytes);
   if (e != cudaSuccess) return e;
-  latent_tc_kernel<N><<<plan.groups * plan.per_pass, kLThreads, LCfg<N>::kSmemBytes, stream>>>(map, p, plan);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  // the merge's CTAs are placed while the attention kernel runs and wait for its end
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(plan.groups, plan.per_pass, N);
-  cfg.blockDim = dim3(128);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, latent_merge_kernel<N>, p, plan);
+  OverlapConfig attention(dim3(plan.groups * plan.per_pass), kLThreads, LCfg<N>::kSmemBytes, stream);
+  if ((e = cudaLaunchKernelEx(&attention.cfg, latent_tc_kernel<N>, maps, p, plan)) != cudaSuccess) return e;
+  // (the spans cut at most groups - 1 sequences: with few sequences those have many segments each)
+  const bool wide = static_cast<int64_t>(p.batch) * plan.passes * 4 <= plan.groups;
+  OverlapConfig merge(dim3(plan.groups, plan.per_pass, wide ? N : N / kMergeWarps), kMergeWarps * 32, 0, stream);
+  return wide ? cudaLaunchKernelEx(&merge.cfg, latent_merge_kernel<N, true>, p, plan)
+              : cudaLaunchKernelEx(&merge.cfg, latent_merge_kernel<N, false>, p, plan);
 }
 
 }  // namespace
@@ -773,31 +959,29 @@ bool latent_tc_supports(const LatentParams& p) {
   const int64_t last_out = (static_cast<int64_t>(p.batch) * p.n_q - 1) * (p.out_token_stride / 8) + (p.num_q_heads - 1) * (p.out_head_stride / 8);
   if (last_out > INT32_MAX) return false;
   const int64_t row_blocks = (static_cast<int64_t>(p.n_q) * p.num_q_heads + kLatMaxRows - 1) / kLatMaxRows;
-  return row_blocks * p.batch <= INT32_MAX / 4;
+  // (rounds x sequences, and the tiles of all of them, are counted in 32 bits)
+  const int64_t tiles = (static_cast<int64_t>(p.block_table_stride) * g.page_size + kLTok - 1) / kLTok + 1;
+  return tiles <= INT32_MAX / (4 * row_blocks * p.batch);
 }
 
 cudaError_t launch_latent_tc(const LatentParams& p, cudaStream_t stream) {
   EncodeFn enc = encode_fn();
   if (!enc) return cudaErrorNotSupported;
   const LatentGeom& g = p.geom;
-  alignas(64) CUtensorMap map;
-  const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(g.page_size), static_cast<cuuint64_t>((g.latent_dim + g.rope_dim) / 64),
-                              static_cast<cuuint64_t>(g.num_pages)};
-  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(g.slot_stride) * 2, 128, static_cast<cuuint64_t>(g.page_stride) * 2};
-  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(g.page_size < kLTok ? g.page_size : kLTok), 1, 1};
-  const cuuint32_t step[4] = {1, 1, 1, 1};
-  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16*>(p.cache), dims, strides, box, step,
-          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  LMaps maps{};
+  const int box = g.page_size < kLTok ? g.page_size : kLTok, lines = (g.latent_dim + g.rope_dim) / 64;
+  if (!encode_map(enc, &maps.line, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, 1, box, false) ||
+      !encode_map(enc, &maps.pair, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, 2, box, false) ||
+      !encode_map(enc, &maps.whole, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, lines, box, false))
     return cudaErrorNotSupported;
   int dev = 0, sms = 0;
   cudaError_t e;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   switch (latent_tile_rows(static_cast<int64_t>(p.n_q) * p.num_q_heads)) {
-    case 16: return launch_n<16>(map, p, sms, stream);
-    case 32: return launch_n<32>(map, p, sms, stream);
-    default: return launch_n<64>(map, p, sms, stream);
+    case 16: return launch_n<16>(enc, maps, p, sms, stream);
+    case 32: return launch_n<32>(enc, maps, p, sms, stream);
+    default: return launch_n<64>(enc, maps, p, sms, stream);
   }
 }
 
