@@ -17,14 +17,14 @@
 // the log2 of their weight) in the workspace, merged by a second kernel; one within a span is
 // written directly. Spans depend on the lengths and the number of SMs only.
 //
-// Softmax: a thread holds 2 tokens x N / 4 query rows. Weights are taken relative to a reference per row
+// Softmax: a thread holds 2 tokens x N / 8 query rows. Weights are taken relative to a reference per row
 // that is raised (and O, in tensor memory, rescaled) only when a score passes it by more than 2^8; the
 // decision is one vote per tile, so that in the steady state no maximum crosses lanes. Row sums stay in
 // registers, per token lane, until the end. Weights are rounded to bf16 for the tensor core (they are at
 // most 2^8, and relative to their row's sum the rounding is 2^-8 whatever the reference); sums, scores and
 // O are 32-bit.
 //
-// Warps: 0-3 softmax and output, 4 TMA producer, 5 S issue + TMEM, 6 P . C issue, 7 Q rows. All waits are
+// Warps: 0-7 softmax and output, 8 and 12 TMA producers, 9 S issue + TMEM, 10 P . C issue, 11 Q rows. All waits are
 // bounded; on a timeout every role leaves its loop, outstanding copies and products are waited for (with a
 // limit) and tensor memory is released.
 #include <cmath>
@@ -43,24 +43,25 @@ constexpr int kLMaxLines = 9;                   // latent 512 + rope 64
 constexpr int kLStageBytes = kLMaxLines * kLLineBytes;
 constexpr int kLStages = 2;
 constexpr int kLGroups = 5;                     // line groups of a stage: rope, then pairs of latent lines
-constexpr int kLThreads = 256;
-constexpr int kLProducer = 4, kLSIssue = 5, kLPvIssue = 6, kLQLoad = 7;
+constexpr int kLSoftWarps = 8, kLSoft = kLSoftWarps * 32;  // two warps per 32 lanes of tensor memory, half the columns each
+constexpr int kLThreads = kLSoft + 160;
+constexpr int kLProducer = 8, kLSIssue = 9, kLPvIssue = 10, kLQLoad = 11, kLProducer2 = 12;
 constexpr uint32_t kLTmemCols = 512, kLTmemS = 256;  // O^T: R / 128 blocks of N columns from 0; S^T from 256
 constexpr float kLNoMax = -1e30f;               // reference of a row that has seen no score yet
 constexpr float kLRescale = 8.f;                // log2
-constexpr int kLAhead = 3;                      // tiles fetched into L2 ahead of their copies
 constexpr int kLMinSpan = 2;                    // tiles: below this a span costs more than it shortens
 
 template <int N>
 struct LCfg {
   static constexpr int kQBytes = kLMaxLines * N * 128;
+  static constexpr int kQBufs = N <= 32 ? 2 : 1;  // what fits: with two, the next segment's rows arrive during this one
   static constexpr int kPBytes = kLTok * 128;
   static constexpr int kBarBytes = 384;
-  // column maxima / sums of the four warps (the first row also inverse sums), rescale factors, row offsets
+  // column maxima / sums of the four token quarters (the first row also inverse sums), rescale factors, row offsets
   static constexpr int kRowBytes = 4 * N * 4 + N * 4 + N * 4;
-  static constexpr int kSmemBytes = kLStages * kLStageBytes + kQBytes + kPBytes + kRowBytes + kBarBytes + 1024;
+  static constexpr int kSmemBytes = kLStages * kLStageBytes + kQBufs * kQBytes + kPBytes + kRowBytes + kBarBytes + 1024;
 };
-static_assert(LCfg<64>::kSmemBytes <= 232448, "shared memory");
+static_assert(LCfg<64>::kSmemBytes <= 232448 && LCfg<32>::kSmemBytes <= 232448, "shared memory");
 
 struct LPlan {
   int32_t row_blocks, per_pass, passes, groups;  // row blocks per sequence; taken at once; rounds; CTA groups
@@ -69,7 +70,7 @@ struct LPlan {
 };
 
 struct LMaps {
-  CUtensorMap line, pair, whole;  // the cache: one line, two lines, all lines of a run of slots
+  CUtensorMap line, pair;        // the cache: one line, two lines of a run of slots
   CUtensorMap q_latent, q_rope;  // one line of q_box heads of a token
 };
 
@@ -149,12 +150,6 @@ __device__ __forceinline__ void tma_load_4d_if(uint32_t leader, uint32_t dst, co
       " [%0], [%1, {0, %3, %4, %5}], [%2];\n\t}"
       ::"r"(dst), "l"(map), "r"(bar), "r"(line), "r"(head), "r"(token), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void tma_prefetch_4d_if(uint32_t leader, const CUtensorMap* map, int slot, int page) {
-  asm volatile(
-      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %3, 0;\n\t"
-      "@pe cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {0, %1, 0, %2}];\n\t}"
-      ::"l"(map), "r"(slot), "r"(page), "r"(leader) : "memory");
-}
 __device__ __forceinline__ uint64_t l2_policy_normal() {
   uint64_t pol;
   asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
@@ -163,25 +158,18 @@ __device__ __forceinline__ uint64_t l2_policy_normal() {
 // 16 lanes x 8 J columns: register 4 j + 0, 1: lane t / 4, columns 8 j + 2 (t % 4) + 0, 1; + 2, 3: lane t / 4 + 8
 template <int J>
 __device__ __forceinline__ void tmem_ld_16x256b(uint32_t taddr, uint32_t (&r)[4 * J]) {
-  if constexpr (J == 2) {
+  if constexpr (J == 1) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
+  } else if constexpr (J == 2) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
-  } else if constexpr (J == 4) {
+  } else {
+    static_assert(J == 4);
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
                    "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
-  } else {
-    static_assert(J == 8);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
   }
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -194,10 +182,13 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 __device__ __forceinline__ void stsm_x4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void stsm_x2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x2.shared.b16 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ bool soft_any(bool x) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                : "=r"(r) : "r"(static_cast<uint32_t>(x)) : "memory");
   return r != 0;
 }
@@ -212,7 +203,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   using C = LCfg<N>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* rows_raw = smem + kLStages * kLStageBytes + C::kQBytes + C::kPBytes;
+  uint8_t* rows_raw = smem + kLStages * kLStageBytes + C::kQBufs * C::kQBytes + C::kPBytes;
   float* wred = reinterpret_cast<float*>(rows_raw);                 // [4][N]
   float* alpha = wred + 4 * N;                                      // [N]
   int32_t* row_off = reinterpret_cast<int32_t*>(alpha + N);         // [N] offset of the row in out, in units of 8 elements; -1: none
@@ -221,16 +212,16 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 40);
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   int* span = cta_err + 1;                                          // [4] first sequence, tile, tiles, its tokens
-  uint32_t* scan = reinterpret_cast<uint32_t*>(wred);               // (start of the kernel only) [8] warps' sums
+  uint32_t* scan = reinterpret_cast<uint32_t*>(wred);               // (start of the kernel only) warps' sums
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = blockIdx.x / plan.per_pass, r = blockIdx.x % plan.per_pass;
   const LatentGeom& geo = p.geom;
   const int m_tiles = geo.latent_dim / 128, n_groups = m_tiles + 1;
-  const uint32_t ring = smem_u32(smem), q_sm = ring + kLStages * kLStageBytes, p_sm = q_sm + C::kQBytes;
+  const uint32_t ring = smem_u32(smem), q_sm = ring + kLStages * kLStageBytes, p_sm = q_sm + C::kQBufs * C::kQBytes;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kLStages * kLGroups;  // [stage][group]
   const uint32_t bar_s = empty0 + 8 * kLStages * kLGroups, bar_sfree = bar_s + 16, bar_p = bar_sfree + 16, bar_pv = bar_p + 8,
-                 bar_q = bar_pv + 8, bar_qfree = bar_q + 8, bar_ofree = bar_qfree + 8, bar_drain = bar_ofree + 8;
+                 bar_q = bar_pv + 8, bar_qfree = bar_q + 16, bar_ofree = bar_qfree + 16, bar_drain = bar_ofree + 8;
   // (the set-up that reads nothing runs beside the end of the kernel before this one)
   if (warp == kLProducer && elect_one()) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.line) : "memory");
@@ -241,16 +232,19 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q_rope) : "memory");
   }
   if (tid == 0) {
-    for (int i = 0; i < 2 * kLStages * kLGroups; ++i) mbar_init(full0 + 8 * i, 1);
+    for (int i = 0; i < kLStages * kLGroups; ++i) {
+      mbar_init(full0 + 8 * i, geo.page_size < kLTok ? 2 : 1);  // (one arrival per producer warp)
+      mbar_init(empty0 + 8 * i, 1);
+    }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_s + 8 * i, 1);
-      mbar_init(bar_sfree + 8 * i, 4);
+      mbar_init(bar_sfree + 8 * i, kLSoftWarps);
+      mbar_init(bar_q + 8 * i, 1);      // Q buffer i
+      mbar_init(bar_qfree + 8 * i, 1);
     }
-    mbar_init(bar_p, 4);
+    mbar_init(bar_p, kLSoftWarps);
     mbar_init(bar_pv, 1);
-    mbar_init(bar_q, 1);
-    mbar_init(bar_qfree, 1);
-    mbar_init(bar_ofree, 4);
+    mbar_init(bar_ofree, kLSoftWarps);
     mbar_init(bar_drain, 2);
     *cta_err = 0;
     span[0] = span[1] = span[2] = 0;
@@ -317,14 +311,16 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   Segment s;
   bool ok = true;
 
-  if (warp == kLProducer) {
+  if (warp == kLProducer || (warp == kLProducer2 && geo.page_size < kLTok)) {
     // ================= TMA producer: lines of the tiles, in the order in which they are read and freed ========
+    // (pages smaller than a tile: two warps share the copies, even and odd pages; one warp issues its 36
+    // copies a tile no faster than one in 75 clocks, which was 4400 clocks a tile against 2700 from memory)
+    const int odd = warp == kLProducer2 ? 1 : 0;
     const uint32_t leader = elect_one();
     const int box = uniform(min(geo.page_size, kLTok)), ept = kLTok / box;  // rows per copy, copies per line of a tile
     // row blocks of other CTAs read the same tiles: only a tile that is read once is marked to leave L2 first
     const uint64_t policy = plan.row_blocks == 1 ? l2_policy_evict_first() : l2_policy_normal();
-    const int ahead = r == 0 ? min(kLAhead, 32 / ept) : 0;  // (the row blocks of a span read the same tiles)
-    int i = 0, cur_batch = 0;  // tiles of this CTA
+    int i = 0;  // tiles of this CTA
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
       if (s.n_tiles == 0) continue;
       const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
@@ -336,30 +332,21 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         return v < 0 || v >= geo.num_pages ? 0 : v;  // (the softmax warps look for these and drop the segment)
       };
       int ids = load_ids(0), ids_next = load_ids(batch_tiles);
-      // Tiles are fetched into L2 a few ahead of the copies: two stages do not cover the trip to memory.
-      auto prefetch = [&](int t) {  // t within the ids held: this batch or the next
-        const int in_batch = t % batch_tiles, tok0 = (s.tile0 + t) * kLTok;
-        const int n_copies = min(ept, (s.L - tok0 + box - 1) / box);
-        for (int c = 0; c < n_copies; ++c) {
-          const int page = __shfl_sync(0xffffffffu, t / batch_tiles == cur_batch ? ids : ids_next, in_batch * ept + c);
-          tma_prefetch_4d_if(leader, &maps.whole, uniform((tok0 + c * box) & (geo.page_size - 1)), page);
-        }
-      };
-      cur_batch = 0;
       for (int t = 0; t < s.n_tiles; ++t, ++i) {
         const int in_batch = t % batch_tiles;
         if (in_batch == 0 && t > 0) {
           ids = ids_next;
-          ++cur_batch;
           ids_next = load_ids(t + batch_tiles);
         }
         const int tok0 = (s.tile0 + t) * kLTok;
         const int n_copies = uniform(min(ept, (s.L - tok0 + box - 1) / box));
         const uint32_t st = uniform(i & 1), sb = ring + st * kLStageBytes, bars0 = 8 * (st * kLGroups);
         const uint32_t parity = ((i >> 1) - 1) & 1;
-        const uint32_t line_bytes = n_copies * box * 128;
+        const uint32_t my_bytes = uniform((ept == 1 ? n_copies : (n_copies + 1 - odd) / 2) * box * 128);
         const int slot = uniform(tok0 & (geo.page_size - 1));
-        const int page0 = __shfl_sync(0xffffffffu, ids, in_batch * ept);
+        int pages[2];  // of this warp's copies (a box of fewer than 64 rows is a whole page)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) pages[k] = __shfl_sync(0xffffffffu, ids, (in_batch * ept + 2 * k + odd) & 31);
         // rope first: it is freed first (by the S product), then the latent pairs as P . C frees them
 #pragma unroll
         for (int gr = 0; gr < kLGroups; ++gr) {
@@ -369,23 +356,22 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
           if (!ok) break;
           const int line0 = gr == 0 ? 2 * m_tiles : 2 * (gr - 1);
           const uint32_t bar = full0 + bars0 + 8 * gr, dst = sb + line0 * kLLineBytes;
-          mbar_expect_tx_if(leader, bar, gr == 0 ? line_bytes : 2 * line_bytes);
+          mbar_expect_tx_if(leader, bar, gr == 0 ? my_bytes : 2 * my_bytes);
           // (a copy of 64 rows takes both lines of a group at once; smaller pages go line by line, so that
           // the rows of a line stay together)
           if (box == kLTok) {
-            tma_load_4d_hint_if(leader, dst, gr == 0 ? &maps.line : &maps.pair, bar, slot, line0, page0, policy);
+            tma_load_4d_hint_if(leader, dst, gr == 0 ? &maps.line : &maps.pair, bar, slot, line0, pages[0], policy);
           } else {
-            for (int c = 0; c < n_copies; ++c) {
-              const int page = __shfl_sync(0xffffffffu, ids, in_batch * ept + c);  // (a box is a whole page)
-              tma_load_4d_hint_if(leader, dst + c * box * 128, &maps.line, bar, 0, line0, page, policy);
-              if (gr > 0) tma_load_4d_hint_if(leader, dst + kLLineBytes + c * box * 128, &maps.line, bar, 0, line0 + 1, page, policy);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int c = 2 * k + odd;
+              if (c >= n_copies) break;
+              tma_load_4d_hint_if(leader, dst + c * box * 128, &maps.line, bar, 0, line0, pages[k], policy);
+              if (gr > 0) tma_load_4d_hint_if(leader, dst + kLLineBytes + c * box * 128, &maps.line, bar, 0, line0 + 1, pages[k], policy);
             }
           }
         }
         if (!ok) break;
-        // (the first tiles of a segment: once the two that go straight to shared memory are under way)
-        if (t >= 1)
-          for (int k = t == 1 ? 2 : t + ahead; k <= min(t + ahead, s.n_tiles - 1); ++k) prefetch(k);
       }
     }
     if (!ok) {  // copies in flight end before the CTA does
@@ -400,14 +386,16 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
     int i = 0, seg = 0;
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
       if (s.n_tiles == 0) continue;
-      ok = mbar_wait_bounded(bar_q, seg & 1);
+      // (segment seg is the (seg / bufs)-th in its buffer)
+      const int qb = seg % C::kQBufs;
+      ok = mbar_spin_bounded(bar_q + 8 * qb, (seg / C::kQBufs) & 1);
       for (int t = 0; ok && t < s.n_tiles; ++t, ++i) {
         const int st = i & 1;
         if (i >= 2) ok = mbar_spin_bounded(bar_sfree + 8 * st, ((i >> 1) - 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         // (operands warp-uniform by a shuffle, offsets constant: 33 clocks an MMA; computed per thread: 100)
-        const uint32_t d = uniform(tmem + kLTmemS + st * N), sb = uniform(ring + st * kLStageBytes), u_q = uniform(q_sm);
+        const uint32_t d = uniform(tmem + kLTmemS + st * N), sb = uniform(ring + st * kLStageBytes), u_q = uniform(q_sm + qb * C::kQBytes);
 #pragma unroll
         for (int gr = 0; gr < kLGroups; ++gr) {
           if (gr >= n_groups) break;
@@ -428,7 +416,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         if (!ok) break;
         tc_commit_if(leader, bar_s + 8 * st);
         tc_commit_if(leader, empty0 + 8 * (st * kLGroups));  // the rope line is only read here
-        if (t == s.n_tiles - 1) tc_commit_if(leader, bar_qfree);
+        if (t == s.n_tiles - 1) tc_commit_if(leader, bar_qfree + 8 * qb);
       }
       ++seg;
     }
@@ -474,8 +462,10 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
     int seg = 0;
     while (ok && next_segment<N>(p, plan, r, walk, s)) {
       if (s.n_tiles == 0) continue;
-      if (seg > 0) {
-        ok = mbar_spin_bounded(bar_qfree, (seg - 1) & 1);
+      const int qb = seg % C::kQBufs;
+      const uint32_t bar_qb = uniform(bar_q + 8 * qb), q_to = uniform(q_sm + qb * C::kQBytes);
+      if (seg >= C::kQBufs) {
+        ok = mbar_spin_bounded(bar_qfree + 8 * qb, (seg / C::kQBufs - 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
       }
@@ -484,14 +474,14 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         const uint32_t leader = elect_one();
         const int live = min(N, p.n_q * p.num_q_heads - s.rb * N);
         const int runs = (live + plan.q_box - 1) / plan.q_box, lines = 2 * m_tiles + 1;
-        mbar_expect_tx_if(leader, bar_q, uniform(runs * plan.q_box * lines * 128));
+        mbar_expect_tx_if(leader, bar_qb, uniform(runs * plan.q_box * lines * 128));
         for (int k = 0; k < runs; ++k) {
           const int row = s.rb * N + k * plan.q_box;
           const int t = uniform(row / p.num_q_heads), h = uniform(row - t * p.num_q_heads);
           const int token = uniform(s.b * p.n_q + t);
-          const uint32_t dst = uniform(q_sm + k * plan.q_box * 128);
-          for (int ln = 0; ln < lines - 1; ++ln) tma_load_4d_if(leader, dst + ln * (N * 128), &maps.q_latent, bar_q, ln, h, token);
-          tma_load_4d_if(leader, dst + (lines - 1) * (N * 128), &maps.q_rope, bar_q, 0, h, token);
+          const uint32_t dst = uniform(q_to + k * plan.q_box * 128);
+          for (int ln = 0; ln < lines - 1; ++ln) tma_load_4d_if(leader, dst + ln * (N * 128), &maps.q_latent, bar_qb, ln, h, token);
+          tma_load_4d_if(leader, dst + (lines - 1) * (N * 128), &maps.q_rope, bar_qb, 0, h, token);
         }
         ++seg;
         continue;
@@ -506,28 +496,30 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         const __nv_bfloat16* qr = live ? p.q_rope + token * p.qr_token_stride + h * p.qr_head_stride : p.q_rope;
         for (int c = lane; c < cv + 8; c += 32) {
           const __nv_bfloat16* src = c < cv ? ql + c * 8 : qr + (c - cv) * 8;
-          cp_async16(q_sm + (c >> 3) * (N * 128) + n * 128 + (((c & 7) ^ (n & 7)) << 4), live ? src : (c < cv ? ql : qr), live ? 16u : 0u);
+          cp_async16(q_to + (c >> 3) * (N * 128) + n * 128 + (((c & 7) ^ (n & 7)) << 4), live ? src : (c < cv ? ql : qr), live ? 16u : 0u);
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive_tc(bar_q);
+      if (lane == 0) mbar_arrive_tc(bar_qb);
       ++seg;
     }
     if (!ok) {
       if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-      if (seg > 0) mbar_wait_bounded(bar_q, (seg - 1) & 1, 1u << 12);
+      for (int k = max(seg - C::kQBufs, 0); k < seg; ++k)
+        mbar_wait_bounded(bar_q + 8 * (k % C::kQBufs), (k / C::kQBufs) & 1, 1u << 12);
     }
-  } else {
+  } else if (warp < kLSoftWarps) {
     // ================= softmax, output =================
-    // After an expired wait a warp goes on without waiting (the four meet at the same named barriers), and
+    // After an expired wait a warp goes on without waiting (all eight meet at the same named barriers), and
     // what it writes is zero.
-    constexpr int J = N / 8;  // column blocks of 8; a thread's columns are 8 j + 2 (lane % 4) + {0, 1}
+    constexpr int J = N / 16;  // column blocks of 8 of this warp; a thread's columns are col0 + 8 j + {0, 1}
+    const int quad = warp & 3, half = warp >> 2;
     const float scale_log2 = p.scale * 1.4426950408889634f;
-    const int tok_a = warp * 16 + (lane >> 2), tok_b = tok_a + 8;  // its tokens within the tile
-    const int col0 = 2 * (lane & 3);
-    const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+    const int tok_a = quad * 16 + (lane >> 2), tok_b = tok_a + 8;  // its tokens within the tile
+    const int col0 = half * (N / 2) + 2 * (lane & 3);
+    const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
     const int rows_total = p.n_q * p.num_q_heads;
     LRecord rec{-1, 0, 0, 0};
     int i = 0;
@@ -555,7 +547,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
         const int64_t tok_end = min(static_cast<int64_t>(s.off + s.take) * kLTok, static_cast<int64_t>(s.L));
         const int pg1 = static_cast<int>((tok_end + geo.page_size - 1) >> plan.page_shift);
-        for (int k = static_cast<int>((static_cast<int64_t>(s.off) * kLTok) >> plan.page_shift) + tid; k < pg1; k += 128) {
+        for (int k = static_cast<int>((static_cast<int64_t>(s.off) * kLTok) >> plan.page_shift) + tid; k < pg1; k += kLSoft) {
           const int v = __ldg(table + k);
           bad |= v < 0 || v >= geo.num_pages;
         }
@@ -571,7 +563,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * st, (i >> 1) & 1));
         tc_fence_after();
         uint32_t sv[4 * J];
-        tmem_ld_16x256b<J>(tmem + kLTmemS + st * N + lane_base, sv);
+        tmem_ld_16x256b<J>(tmem + kLTmemS + st * N + half * (N / 2) + lane_base, sv);
         tmem_wait_ld();
         tc_fence_before();
         __syncwarp();
@@ -593,7 +585,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
           if (valid < kLTok) {
             // rows of the tile behind the sequence's end hold anything (pages' tails, an earlier tile): their
             // weight is 0, and so must be what it multiplies
-            for (int k = tid; k < (kLTok - valid) * (geo.latent_dim / 8); k += 128) {
+            for (int k = tid; k < (kLTok - valid) * (geo.latent_dim / 8); k += kLSoft) {
               const int row = valid + k / (geo.latent_dim / 8), ch = k % (geo.latent_dim / 8);
               asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};"
                            ::"r"(ring + st * kLStageBytes + (ch >> 3) * kLLineBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0));
@@ -620,7 +612,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
             for (int c = 0; c < 2 * J; ++c) mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], o));
           if (lane < 4) {
 #pragma unroll
-            for (int c = 0; c < 2 * J; ++c) wred[warp * N + 8 * (c >> 1) + col0 + (c & 1)] = mx[c];
+            for (int c = 0; c < 2 * J; ++c) wred[quad * N + 8 * (c >> 1) + col0 + (c & 1)] = mx[c];
           }
           soft_sync();
 #pragma unroll
@@ -628,7 +620,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
             const int col = 8 * (c >> 1) + col0 + (c & 1);
             const float m_new = fmaxf(fmaxf(fmaxf(wred[col], wred[N + col]), fmaxf(wred[2 * N + col], wred[3 * N + col])), m_ref[c]);
             const float a = ex2(m_ref[c] - m_new);
-            if (warp == 0 && lane < 4) alpha[col] = a;
+            if (quad == 0 && lane < 4) alpha[col] = a;
             l[c] *= a;
             m_ref[c] = m_new;
           }
@@ -650,7 +642,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         }
         if (raise && t > 0) {
           tc_fence_after();
-          for (int cb = 0; cb < m_tiles * N; cb += 16) {
+          for (int cb = half * 16; cb < m_tiles * N; cb += 32) {
             uint32_t ov[16];
             tmem_ld16(tmem + lane_base + cb, ov);
             tmem_wait_ld();
@@ -668,10 +660,14 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
           tc_fence_before();
         }
         {
-          const int mi = lane >> 3, row = warp * 16 + (mi & 1) * 8 + (lane & 7);
+          const int mi = lane >> 3, row = quad * 16 + (mi & 1) * 8 + (lane & 7), ch = half * J;
+          if constexpr (J == 1) {
+            stsm_x2(p_sm + row * 128 + ((ch ^ (row & 7)) << 4), pk[0], pk[1]);
+          } else {
 #pragma unroll
-          for (int j = 0; j < J; j += 2)
-            stsm_x4(p_sm + row * 128 + (((j + (mi >> 1)) ^ (row & 7)) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
+            for (int j = 0; j < J; j += 2)
+              stsm_x4(p_sm + row * 128 + (((ch + j + (mi >> 1)) ^ (row & 7)) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
+          }
         }
         fence_proxy_async();
         __syncwarp();
@@ -686,9 +682,9 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         for (int c = 0; c < 2 * J; ++c) l[c] += __shfl_xor_sync(0xffffffffu, l[c], o);
       if (lane < 4) {
 #pragma unroll
-        for (int c = 0; c < 2 * J; ++c) wred[warp * N + 8 * (c >> 1) + col0 + (c & 1)] = l[c];
+        for (int c = 0; c < 2 * J; ++c) wred[quad * N + 8 * (c >> 1) + col0 + (c & 1)] = l[c];
       }
-      if (warp == 0 && lane < 4) {
+      if (quad == 0 && lane < 4) {
 #pragma unroll
         for (int c = 0; c < 2 * J; ++c) alpha[8 * (c >> 1) + col0 + (c & 1)] = m_ref[c];
       }
@@ -705,12 +701,11 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv, (i - 1) & 1));
         tc_fence_after();
       }
-      for (int m = 0; m < m_tiles; ++m) {
-        const int dim = m * 128 + warp * 32 + lane;
-        for (int cb = 0; cb < N; cb += 16) {
+      for (int x0 = half * 16; x0 < m_tiles * N; x0 += 32) {  // 16 columns at a time, the two warps of 32 lanes in turn
+        const int m = x0 / N, cb = x0 % N, dim = m * 128 + quad * 32 + lane;
+        {
           uint32_t ov[16];
-          tmem_ld16(tmem + lane_base + m * N + cb, ov);
-          tmem_wait_ld();
+          tmem_ld16(tmem + lane_base + x0, ov);
           float v[16];
           int32_t off[16];
 #pragma unroll
@@ -720,6 +715,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
             v[k] = f.x; v[k + 1] = f.y; v[k + 2] = f.z; v[k + 3] = f.w;
             off[k] = o.x; off[k + 1] = o.y; off[k + 2] = o.z; off[k + 3] = o.w;
           }
+          tmem_wait_ld();
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = s.n_tiles > 0 && ok && !bad ? __uint_as_float(ov[k]) * v[k] : 0.f;
           if (partial) {
@@ -971,8 +967,7 @@ cudaError_t launch_latent_tc(const LatentParams& p, cudaStream_t stream) {
   LMaps maps{};
   const int box = g.page_size < kLTok ? g.page_size : kLTok, lines = (g.latent_dim + g.rope_dim) / 64;
   if (!encode_map(enc, &maps.line, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, 1, box, false) ||
-      !encode_map(enc, &maps.pair, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, 2, box, false) ||
-      !encode_map(enc, &maps.whole, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, lines, box, false))
+      !encode_map(enc, &maps.pair, p.cache, lines, g.page_size, g.num_pages, g.slot_stride, g.page_stride, 2, box, false))
     return cudaErrorNotSupported;
   int dev = 0, sms = 0;
   cudaError_t e;
