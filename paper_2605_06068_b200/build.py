@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libpda.so")
 SOURCES = ["api.cu", "kv_append.cu", "reduce.cu", "attention_generic.cu", "attention_tma.cu", "attention_persist.cu", "attention_mq.cu", "attention_mq_tc.cu", "attention_mq_tcp.cu", "attention_mq_tc8p.cu",
-           "static_scratch.cu", "debug.cu", "api_latent.cu", "tables.cu", "latent_append.cu", "latent_generic.cu", "latent_tc.cu"]
+           "static_scratch.cu", "debug.cu", "api_latent.cu", "tables.cu", "latent_append.cu", "latent_generic.cu", "latent_tc.cu", "latent_prefill_tc.cu"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -131,6 +131,8 @@ int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_he
                              kn_token_stride, kn_head_stride, kr_token_stride, v_token_stride, v_head_stride,
                              out_token_stride, out_head_stride, batch, num_heads, nope_dim, rope_dim, v_dim, max_q, total_q,
                              total_k, scale};
+  if (!(flags & PDA_FLAG_FORCE_GENERIC) && pda::latent_prefill_tc_supports(p))
+    return static_cast<int>(pda::launch_latent_prefill_tc(p, static_cast<cudaStream_t>(stream)));
   return static_cast<int>(pda::launch_latent_prefill_generic(p, static_cast<cudaStream_t>(stream)));
 }
 

@@ -114,5 +114,7 @@ cudaError_t launch_latent_generic(const LatentParams& p, cudaStream_t stream);
 bool latent_tc_supports(const LatentParams& p);  // tcgen05 kernel
 cudaError_t launch_latent_tc(const LatentParams& p, cudaStream_t stream);
 cudaError_t launch_latent_prefill_generic(const LatentPrefillParams& p, cudaStream_t stream);
+bool latent_prefill_tc_supports(const LatentPrefillParams& p);  // tcgen05 kernel
+cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t stream);
 
 }  // namespace pda

@@ -30,6 +30,7 @@
 #include <cmath>
 
 #include "latent.cuh"
+#include "latent_ptx.cuh"
 #include "tcgen05_ptx.cuh"
 #include "tma_ptx.cuh"
 
@@ -120,20 +121,6 @@ __device__ __forceinline__ bool next_segment(const LatentParams& p, const LPlan&
   return true;
 }
 
-__device__ __forceinline__ void mma_ss_if(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
-                                          uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred pe, pa;\n\tsetp.ne.b32 pe, %5, 0;\n\tsetp.ne.b32 pa, %4, 0;\n\t"
-      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, pa;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
-}
-// A value that all lanes hold, said so to the compiler.
-__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
-// bf16 x bf16 -> f32, M x N
-__host__ __device__ constexpr uint32_t latent_idesc(int m, int n, bool a_mn, bool b_mn) {
-  return (1u << 4) | (kFmtBf16 << 7) | (kFmtBf16 << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-         (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
-}
 __device__ __forceinline__ void tma_load_4d_hint_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot,
                                                     int line, int page, uint64_t policy) {
   asm volatile(
@@ -141,14 +128,6 @@ __device__ __forceinline__ void tma_load_4d_hint_if(uint32_t leader, uint32_t ds
       "@pe cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
       " [%0], [%1, {0, %3, %4, %5}], [%2], %7;\n\t}"
       ::"r"(dst), "l"(map), "r"(bar), "r"(slot), "r"(line), "r"(page), "r"(leader), "l"(policy) : "memory");
-}
-__device__ __forceinline__ void tma_load_4d_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int line,
-                                               int head, int token) {
-  asm volatile(
-      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %6, 0;\n\t"
-      "@pe cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {0, %3, %4, %5}], [%2];\n\t}"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(line), "r"(head), "r"(token), "r"(leader) : "memory");
 }
 __device__ __forceinline__ uint64_t l2_policy_normal() {
   uint64_t pol;
@@ -838,20 +817,6 @@ __global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __
   }
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encode_fn() {
-  static EncodeFn fn = [] {
-    void* sym = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
-      sym = nullptr;
-    return reinterpret_cast<EncodeFn>(sym);
-  }();
-  return fn;
-}
-
 // How many row blocks run at once, and how often: the choice that keeps most CTAs busy, for at most 37
 // row blocks at once (four groups of CTAs), fewer rounds first.
 LPlan make_plan(int row_blocks, int ctas) {
@@ -961,7 +926,7 @@ bool latent_tc_supports(const LatentParams& p) {
 }
 
 cudaError_t launch_latent_tc(const LatentParams& p, cudaStream_t stream) {
-  EncodeFn enc = encode_fn();
+  EncodeFn enc = tensor_map_encoder();
   if (!enc) return cudaErrorNotSupported;
   const LatentGeom& g = p.geom;
   LMaps maps{};
