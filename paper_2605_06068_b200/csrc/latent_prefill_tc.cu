@@ -1,22 +1,27 @@
 // Expanded attention (keys [k_nope per head | k_rope shared], values per head; packed ragged sequences,
 // causal from the end) on tcgen05 + TMEM, dims 128 + 64 and 128.
 //
-// A CTA takes 256 query rows of one head as two halves of 128 (TMEM lane = row) and walks over the keys
-// 128 at a time:
-//   S[w] = Q[w] . K^T    12 MMAs M128 N128 K16, Q and K in shared memory (2 lines of k_nope, 1 of k_rope:
+// A pair of CTAs (a cluster of two SMs, tcgen05 cta_group::2) takes 512 query rows of one head as two halves
+// of 256, 128 rows of each in either CTA (TMEM lane = row), and walks over the keys 128 at a time:
+//   S[w] = Q[w] . K^T    12 MMAs M256 N128 K16; of K each CTA holds 64 keys (2 lines of k_nope, 1 of k_rope:
 //                        the shared part is copied from its one array, never concatenated in memory)
-//   O[w] += P[w] . V     2 x 8 MMAs M128 N64 K16, P (bf16) in tensor memory over the S it came from
-// S[0], S[1], O[0], O[1] fill the 512 columns. The tensor core alternates between the halves (PV of one,
-// the next S of the same, then the other's), so that one half's softmax runs under the other's products:
-// 1300 clocks of products per half and tile against 1024 of exponentials. That is the bound: 2 x 320 x
-// 128 x 256 operations per 2600 clocks.
-// K and V lines (128 keys x 128 bytes = 16 KB) go through a ring of 8 in the order in which they are used
-// and freed: 3 of K(j), 2 of V(j), ...
+//   O[w] += P[w] . V     8 MMAs M256 N128 K16; P (bf16) in tensor memory over the S it came from, of V each
+//                        CTA holds 64 of the 128 dims
+// Every MMA reads both CTAs' shares of B, so a CTA copies 40 KB a tile for 256 rows instead of 80: Q takes
+// 96 KB, and with 80 KB a tile the ring was so short (1.6 tiles) that products waited for copies; with
+// the pair it holds three tiles, and half the bytes come from L2.
+// S[0], S[1], O[0], O[1] fill the 512 columns. The halves stay in opposite phase, one's softmax under the other's
+// products: 1300 clocks of products per half and tile against 1024 of exponentials, of which every kFPolyOf-th
+// pair is taken by a polynomial on the FMA units.
 // The softmax takes weights relative to a reference per row that is raised (and O rescaled in tensor memory)
 // only when the row's maximum passes it by more than 2^8; row sums are kept by the row's thread, of the
 // 32-bit weights; the rounding of the weights to bf16 is 2^-8 of each.
 // Blocks at the end of the longest prompts have the most keys and start first.
-// Warps: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 MMA issue + TMEM. All waits are bounded.
+// Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the
+// pair's first CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are
+// bounded.
+#include <type_traits>
+
 #include "latent.cuh"
 #include "latent_ptx.cuh"
 #include "tcgen05_ptx.cuh"
@@ -26,191 +31,336 @@ namespace pda {
 
 namespace {
 
-constexpr int kFRows = 256, kFKeys = 128;
-constexpr int kFLine = kFKeys * 128;         // 16 KB: one 128-byte line of 128 rows
-constexpr int kFQLines = 3, kFKLines = 3, kFVLines = 2, kFUnits = kFKLines + kFVLines;
-constexpr int kFSlots = 8;
-constexpr int kFThreads = 384, kFProducer = 8, kFMma = 9;
-constexpr int kFSmemBytes = 2 * kFQLines * kFLine + kFSlots * kFLine + 512 + 1024;
+constexpr int kFRows = 512, kFHalf = 256, kFKeys = 128;  // query rows of a pair of CTAs, of a half; keys per tile
+constexpr int kFQLines = 3;
+constexpr int kFQLine = 128 * 128;                        // one 128-byte line of the CTA's 128 rows of a half
+constexpr int kFKLine = 64 * 128, kFKBytes = 3 * kFKLine;  // of its 64 keys
+constexpr int kFVBytes = kFKeys * 128;                    // its line (64 dims) of all keys
+constexpr int kFStages = 3;                               // tiles
+constexpr int kFSoftWarps = 8, kFThreads = (kFSoftWarps + 4) * 32, kFProducer = 8, kFMma = 9, kFRelay = 11;  // (9, 10: one per half)
+constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 512 + 1024;
 static_assert(kFSmemBytes <= 232448, "shared memory");
-// 384 threads start with 168 registers; the control warps keep 72 and the softmax warps take 208
-constexpr uint32_t kFRegsSoftmax = 208, kFRegsControl = 72;
+// 384 threads start with 168 registers (64512 in all); the control warps keep 104 and the softmax warps take 200
+constexpr uint32_t kFRegsSoftmax = 200, kFRegsControl = 104;
+static_assert(kFSoftWarps * 32 * kFRegsSoftmax + 128 * kFRegsControl <= kFThreads * 168, "registers");
 constexpr uint32_t kFTmemCols = 512, kFTmemO = 256;  // S[w] at 128 w, P[w] over its first 64 columns, O[w] at 256 + 128 w
 constexpr float kFNoMax = -1e30f;
 constexpr float kFRescale = 8.f;
+constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
+
+// 2^x for two x <= 2^7 on the FMA units, so that the exponentials are not bound by the special-function unit
+// alone: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the
+// polynomial of degree 3 whose largest relative error over [-1/2, 1/2] is least (7.5e-5, found by Remez
+// exchange; a weight's rounding to bf16 is 3.9e-3), n added to the exponent. x below -126 gives 2^-126.
+__device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
+  auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
+  float x0, x1;
+  f32x2_split(x, x0, x1);
+  x = f32x2(__float_as_uint(fmaxf(x0, -126.f)), __float_as_uint(fmaxf(x1, -126.f)));
+  const uint64_t t = add_f32x2(x, both(12582912.f));
+  const uint64_t f = add_f32x2(x, fma_f32x2(t, both(-1.f), both(12582912.f)));
+  uint64_t y = fma_f32x2(f, both(0.0551716691f), both(0.242611122f));
+  y = fma_f32x2(y, f, both(0.693260985f));
+  y = fma_f32x2(y, f, both(0.999928074f));
+  float t0, t1;
+  f32x2_split(t, t0, t1);
+  f32x2_split(y, w0, w1);
+  w0 = __uint_as_float(__float_as_uint(w0) + (__float_as_uint(t0) << 23));
+  w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
+}
 
 struct FMaps {
   CUtensorMap q, k_nope, k_rope, v;
 };
 
-__global__ void __launch_bounds__(kFThreads, 1)
+// ---- the pair: instructions of cta_group::2 and barriers in the other CTA ----
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {  // bar: an address of in_cta
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// The same where only tensor memory has been written, which the tcgen05 fences order.
+__device__ __forceinline__ void arrive_cluster_tc(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_spin_cluster(uint32_t bar, uint32_t parity) {  // for arrivals from either CTA
+  for (uint32_t i = 0; i < kTestSpinLimit; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A copy into this CTA whose bytes count for a barrier of either CTA of the pair.
+__device__ __forceinline__ void tma_load_4d_pair_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int c1, int c2,
+                                                    int c3) {
+  asm volatile(
+      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %6, 0;\n\t"
+      "@pe cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {0, %3, %4, %5}], [%2];\n\t}"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c1), "r"(c2), "r"(c3), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void mma2_ss_if(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred pe, pa;\n\tsetp.ne.b32 pe, %5, 0;\n\tsetp.ne.b32 pa, %4, 0;\n\t"
+      "@pe tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, pa;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void mma2_ts_if(uint32_t leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred pe, pa;\n\tsetp.ne.b32 pe, %5, 0;\n\tsetp.ne.b32 pa, %4, 0;\n\t"
+      "@pe tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, pa;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// Arrival at the barrier at this offset in both CTAs once this thread's products so far are through.
+__device__ __forceinline__ void commit2_if(uint32_t leader, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred pe;\n\t.reg .b16 m;\n\tsetp.ne.b32 pe, %1, 0;\n\tmov.b16 m, 3;\n\t"
+      "@pe tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
+      ::"r"(bar), "r"(leader) : "memory");
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFThreads, 1)
 latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_constant__ LatentPrefillParams p, int q_blocks) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (2 * kFQLines + kFSlots) * kFLine);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 32);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes));
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 40);
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x & 1;  // in the pair
 
   // late blocks first (all heads and sequences of a block index together)
   const int per_block = p.num_heads * p.batch;
-  const int qb = q_blocks - 1 - static_cast<int>(blockIdx.x / per_block);
-  const int b = static_cast<int>(blockIdx.x % per_block) / p.num_heads, h = static_cast<int>(blockIdx.x % per_block) % p.num_heads;
+  const int pair = blockIdx.x >> 1;
+  const int qb = q_blocks - 1 - pair / per_block;
+  const int b = (pair % per_block) / p.num_heads, h = (pair % per_block) % p.num_heads;
   const PrefillSpan sp = prefill_span(p, b);
   const int row0 = qb * kFRows;
-  if (row0 >= sp.nq) return;
-  // keys that the last row of half w can see, in tiles
+  if (row0 >= sp.nq) return;  // (both CTAs)
+  // keys that the last row of half w can see, in tiles (of either CTA: the pair walks together)
   int n_tiles[2];
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    const int first = row0 + 128 * w, last = min(first + 127, sp.nq - 1);
+    const int first = row0 + kFHalf * w, last = min(first + kFHalf - 1, sp.nq - 1);
     const int see = first >= sp.nq ? 0 : min(max(sp.nk - sp.nq_all + last + 1, 0), sp.nk);
     n_tiles[w] = (see + kFKeys - 1) / kFKeys;
   }
   const int n_max = max(n_tiles[0], n_tiles[1]);
-  // (a CTA of this launch has met an expired wait: nothing more is attended)
-  const bool dead = p.status != nullptr && *reinterpret_cast<volatile int32_t*>(p.status) == PDA_DEV_TIMEOUT;
+  bool ok = true;
 
-  const uint32_t q_sm = smem_u32(smem), ring = q_sm + 2 * kFQLines * kFLine;
-  const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kFSlots, bar_q = empty0 + 8 * kFSlots;  // Q half w
-  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 16, bar_drain = bar_pv + 16;
+  const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + 2 * kFQLines * kFQLine, v_sm = k_sm + kFStages * kFKBytes;
+  // Barriers, at the same place in both CTAs. Of the pair's first CTA: full_k (both CTAs' copies), v_ready, bar_q,
+  // bar_p, bar_turn. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s, bar_pv.
+  const uint32_t full_k = smem_u32(bars), empty_k = full_k + 8 * kFStages, full_v = empty_k + 8 * kFStages,
+                 empty_v = full_v + 8 * kFStages, v_ready = empty_v + 8 * kFStages, bar_q = v_ready + 8 * kFStages;
+  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 16, bar_turn = bar_pv + 16, bar_drain = bar_turn + 16, bar_never = bar_drain + 8;
   if (tid == 0) {
-    for (int i = 0; i < 2 * kFSlots; ++i) mbar_init(full0 + 8 * i, 1);
+    for (int i = 0; i < kFStages; ++i) {
+      mbar_init(full_k + 8 * i, 1);
+      mbar_init(empty_k + 8 * i, 2);
+      mbar_init(full_v + 8 * i, 1);
+      mbar_init(empty_v + 8 * i, 2);
+      mbar_init(v_ready + 8 * i, 2);
+    }
     for (int w = 0; w < 2; ++w) {
       mbar_init(bar_q + 8 * w, 1);
       mbar_init(bar_s + 8 * w, 1);
-      mbar_init(bar_p + 8 * w, 4);
+      mbar_init(bar_p + 8 * w, 8);  // four warps of each CTA
       mbar_init(bar_pv + 8 * w, 1);
+      mbar_init(bar_turn + 8 * w, 1);
     }
-    mbar_init(bar_drain, 1);
+    mbar_init(bar_drain, 2);
+    mbar_init(bar_never, 1);
     *cta_err = 0;
     fence_mbar_init();
     fence_proxy_async();
   }
   if (warp == kFMma) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kFTmemCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kFTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
-  const bool skip = __syncthreads_or(dead) || n_max == 0;
+  __syncthreads();
+  cluster_sync();
   tc_fence_after();
+  const bool skip = n_max == 0;
   const uint32_t tmem = *tmem_slot;
-  bool ok = true;
 
-  if (warp >= 8) {
+  // ================= products of half w =================
+  // A warp for each half, which prepares its next products while the other's are being issued (one warp for
+  // both spent as long between the products as on them), taking turns: so the halves stay in opposite phase.
+  // (Without turns the products interleave, both halves run their softmax at the same time and the tensor core
+  // waits.)
+  auto issue_role = [&](auto half) {
+    constexpr int w = decltype(half)::value;
+    constexpr uint32_t idesc_s = latent_idesc(256, kFKeys, false, false), idesc_o = latent_idesc(256, 128, false, true);
+    const uint32_t leader = elect_one();
+    const uint32_t u_q = uniform(q_sm + w * kFQLines * kFQLine), u_k = uniform(k_sm), u_v = uniform(v_sm), u_tmem = uniform(tmem);
+    const uint32_t u_ek = uniform(empty_k), u_ev = uniform(empty_v);
+    const int n = uniform(n_tiles[w]), n_all = uniform(n_max);
+    const uint32_t d_s = u_tmem + 128 * w, d_o = u_tmem + kFTmemO + 128 * w;
+    auto wait = [&](uint32_t bar, int phase) {
+      if (ok) ok = __all_sync(0xffffffffu, mbar_spin_cluster(bar, phase & 1));
+    };
+    auto give_back = [&](uint32_t bar) {  // a tile's part that this half does not read, in both CTAs
+      if (ok && lane < 2) arrive_cluster(in_cta(bar, lane));
+      __syncwarp();
+    };
+    auto s_product = [&](uint32_t k_addr) {
+      const uint64_t q0 = tc_desc(u_q, 16, 1024), k0 = tc_desc(k_addr, 16, 1024);
+#pragma unroll
+      for (int ln = 0; ln < kFQLines; ++ln)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          mma2_ss_if(leader, d_s, q0 + ln * (kFQLine / 16) + 2 * ks, k0 + ln * (kFKLine / 16) + 2 * ks, idesc_s, (ln > 0 || ks > 0) ? 1u : 0u);
+      commit2_if(leader, bar_s + 8 * w);
+    };
+    if (n > 0) {
+      wait(bar_q + 8 * w, 0);
+      wait(full_k, 0);
+      if (ok) {
+        tc_fence_after();
+        s_product(u_k);
+        commit2_if(leader, u_ek);
+      }
+    } else {
+      wait(full_k, 0);
+      give_back(empty_k);
+    }
+    for (int j = 0; ok && j < n_all; ++j) {
+      const int sv = j % kFStages, sk = (j + 1) % kFStages, rv = j / kFStages, rk = (j + 1) / kFStages;
+      // turn j: half 0 after half 1's turn j - 1, half 1 after half 0's turn j
+      const auto my_turn = [&]() {
+        if (w == 1) wait(bar_turn + 8, j);
+        else if (j > 0) wait(bar_turn, j - 1);
+      };
+      const auto pass_turn = [&]() {
+        if (lane == 0) mbar_arrive_tc(bar_turn + 8 * (w ^ 1));
+      };
+      wait(v_ready + 8 * sv, rv);
+      if (j + 1 < n_all) wait(full_k + 8 * sk, rk);
+      if (j < n) {
+        const uint64_t v0 = tc_desc(uniform(u_v + sv * kFVBytes), 16, 1024);
+        const uint32_t k_addr = uniform(u_k + sk * kFKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
+        const uint32_t acc = uniform(j > 0 ? 1u : 0u);
+        wait(bar_p + 8 * w, j);
+        my_turn();
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
+        commit2_if(leader, bar_pv + 8 * w);
+        commit2_if(leader, ev);
+        if (j + 1 < n) {
+          // S(j + 1) takes the place of P(j): the tensor core works a thread's products off in order
+          s_product(k_addr);
+          pass_turn();
+          commit2_if(leader, ek);
+        } else {
+          pass_turn();
+          if (j + 1 < n_all) give_back(empty_k + 8 * sk);
+        }
+      } else {
+        my_turn();
+        pass_turn();
+        give_back(empty_v + 8 * sv);
+        if (j + 1 < n_all) give_back(empty_k + 8 * sk);
+      }
+    }
+    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    asm volatile(
+        "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %1, 0;\n\t"
+        "@pe tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar_drain), "r"(leader) : "memory");
+    __syncwarp();
+    if (!mbar_wait_bounded(bar_drain, 0, 1u << 12) && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+  };
+
+  if (warp >= kFSoftWarps) {
     reg_alloc_dec<kFRegsControl>();
     if (warp == kFProducer && !skip) {
-      // ================= TMA producer =================
-      const uint32_t leader = elect_one();
-      const uint32_t u_q = uniform(q_sm), u_ring = uniform(ring), u_h = uniform(h);
-      const int token0 = uniform(sp.q0 + row0), key0 = uniform(sp.k0);
-      int armed = 0;
+      // ================= TMA producer: this CTA's rows of Q, keys of K, dims of V =================
+      const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
+      const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
+      const int token0 = uniform(sp.q0 + row0 + 128 * rank), key0 = uniform(sp.k0), u_h = uniform(h);
+      const uint32_t to_q = uniform(in_cta(bar_q, 0)), to_k = uniform(in_cta(full_k, 0));
       auto load_q = [&](int w) {
-        mbar_expect_tx_if(leader, bar_q + 8 * w, kFQLines * kFLine);
+        mbar_expect_tx_if(first, bar_q + 8 * w, 2 * kFQLines * kFQLine);
 #pragma unroll
         for (int ln = 0; ln < kFQLines; ++ln)
-          tma_load_4d_if(leader, u_q + (w * kFQLines + ln) * kFLine, &maps.q, bar_q + 8 * w, ln, u_h, token0 + 128 * w);
+          tma_load_4d_pair_if(leader, u_q + (w * kFQLines + ln) * kFQLine, &maps.q, to_q + 8 * w, ln, u_h, token0 + kFHalf * w);
       };
       if (n_tiles[0] > 0) load_q(0);
-      int slot = 0;
-      uint32_t round = 0;
+      int armed_k = 0, armed_v = 0;
       for (int j = 0; ok && j < n_max; ++j) {
-#pragma unroll
-        for (int u = 0; u < kFUnits; ++u) {
-          if (round > 0) ok = mbar_wait_bounded(empty0 + 8 * slot, (round - 1) & 1);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          const uint32_t bar = uniform(full0 + 8 * slot), dst = uniform(u_ring + slot * kFLine);
-          const int key = key0 + j * kFKeys;
-          mbar_expect_tx_if(leader, bar, kFLine);
-          if (u < 2) tma_load_4d_if(leader, dst, &maps.k_nope, bar, u, u_h, key);
-          else if (u == 2) tma_load_4d_if(leader, dst, &maps.k_rope, bar, 0, 0, key);
-          else tma_load_4d_if(leader, dst, &maps.v, bar, u - 3, u_h, key);
-          ++armed;
-          if (++slot == kFSlots) { slot = 0; ++round; }
-          if (j == 0 && u == 2 && n_tiles[1] > 0) load_q(1);
-        }
+        const int st = uniform(j % kFStages), round = j / kFStages;
+        if (round > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(empty_k + 8 * st, (round - 1) & 1));
+        if (!ok) break;
+        mbar_expect_tx_if(first, full_k + 8 * st, 2 * kFKBytes);
+        const int key = key0 + j * kFKeys, my_key = key + 64 * rank;
+        const uint32_t kd = u_k + st * kFKBytes;
+        tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k + 8 * st, 0, u_h, my_key);
+        tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k + 8 * st, 1, u_h, my_key);
+        tma_load_4d_pair_if(leader, kd + 2 * kFKLine, &maps.k_rope, to_k + 8 * st, 0, 0, my_key);
+        ++armed_k;
+        if (j == 0 && n_tiles[1] > 0) load_q(1);
+        if (round > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(empty_v + 8 * st, (round - 1) & 1));
+        if (!ok) break;
+        mbar_expect_tx_if(leader, full_v + 8 * st, kFVBytes);
+        tma_load_4d_if(leader, u_v + st * kFVBytes, &maps.v, full_v + 8 * st, rank, u_h, key);
+        ++armed_v;
       }
-      if (!ok) {  // copies in flight end before the CTA does
+      if (!ok) {  // copies in flight end before the CTA does (K's and Q's count in the first CTA: given time here)
         if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-        for (int u = max(armed - kFSlots, 0); u < armed; ++u) mbar_wait_bounded(full0 + 8 * (u % kFSlots), (u / kFSlots) & 1, 1u << 12);
-        for (int w = 0; w < 2; ++w)
-          if (n_tiles[w] > 0 && (w == 0 || armed > 2)) mbar_wait_bounded(bar_q + 8 * w, 0, 1u << 12);
+        for (int j = max(armed_v - kFStages, 0); j < armed_v; ++j) mbar_wait_bounded(full_v + 8 * (j % kFStages), (j / kFStages) & 1, 1u << 12);
+        for (int k = 0; k < 64; ++k) mbar_wait_bounded(bar_never, 0, 1);  // (4 us a poll)
       }
-    } else if (warp == kFMma && !skip) {
-      // ================= products =================
-      constexpr uint32_t idesc_s = latent_idesc(128, kFKeys, false, false), idesc_o = latent_idesc(128, 64, false, true);
-      const uint32_t leader = elect_one();
-      const uint32_t u_q = uniform(q_sm), u_ring = uniform(ring), u_tmem = uniform(tmem);
-      auto wait_unit = [&](int u) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(full0 + 8 * (u % kFSlots), (u / kFSlots) & 1));
-      };
-      auto s_product = [&](int w, int j) {
-#pragma unroll
-        for (int ln = 0; ln < kFKLines; ++ln) {
-          const int u = j * kFUnits + ln;
-          wait_unit(u);
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t ad = tc_desc(uniform(u_q + (w * kFQLines + ln) * kFLine), 16, 1024);
-          const uint64_t bd = tc_desc(uniform(u_ring + (u % kFSlots) * kFLine), 16, 1024);
-          const uint32_t d = uniform(u_tmem + 128 * w);
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks) mma_ss_if(leader, d, ad + 2 * ks, bd + 2 * ks, idesc_s, (ln > 0 || ks > 0) ? 1u : 0u);
-        }
-        tc_commit_if(leader, uniform(bar_s + 8 * w));
-      };
-      auto o_product = [&](int w, int j) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_p + 8 * w, j & 1));
-        const uint32_t acc = uniform(j > 0 ? 1u : 0u);
-#pragma unroll
-        for (int ln = 0; ln < kFVLines; ++ln) {
-          const int u = j * kFUnits + kFKLines + ln;
-          wait_unit(u);
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t bd = tc_desc(uniform(u_ring + (u % kFSlots) * kFLine), 16, 1024);
-          const uint32_t pa = uniform(u_tmem + 128 * w), d = uniform(u_tmem + kFTmemO + 128 * w + 64 * ln);
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) tc_mma_ts_if<false>(leader, d, pa + 8 * ks, bd + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
-        }
-        tc_commit_if(leader, uniform(bar_pv + 8 * w));
-      };
-      auto release = [&](int j, int first, int n) {
-        for (int k = 0; k < n; ++k) tc_commit_if(leader, uniform(empty0 + 8 * ((j * kFUnits + first + k) % kFSlots)));
-      };
-      for (int w = 0; w < 2; ++w) {
-        if (n_tiles[w] == 0) continue;
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar_q + 8 * w, 0));
-        if (ok) s_product(w, 0);
-      }
-      if (ok) release(0, 0, kFKLines);
+    } else if (warp == kFRelay && !skip) {
+      // ================= V tiles: cleared behind the sequence's end, then handed to the first CTA =================
+      const uint32_t to = in_cta(v_ready, 0);
       for (int j = 0; ok && j < n_max; ++j) {
-        for (int w = 0; ok && w < 2; ++w) {
-          // S(j + 1) takes the place of P(j): the tensor core works its products off in order
-          if (j < n_tiles[w]) o_product(w, j);
-          if (!ok) break;
-          if (w == 1) release(j, kFKLines, kFVLines);
-          if (j + 1 < n_tiles[w]) s_product(w, j + 1);
+        const int st = j % kFStages;
+        ok = __all_sync(0xffffffffu, mbar_spin_bounded(full_v + 8 * st, (j / kFStages) & 1));
+        if (!ok) break;
+        const int valid = sp.nk - j * kFKeys;
+        if (valid < kFKeys) {
+          // (keys behind the end have weight 0, but what they hold may be anything)
+          for (int k = lane; k < (kFKeys - valid) * 8; k += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * kFVBytes + valid * 128 + k * 16), "r"(0));
+          fence_proxy_async();
         }
-        if (ok && j + 1 < n_max) release(j + 1, 0, kFKLines);
+        __syncwarp();
+        if (lane == 0) arrive_cluster(to + 8 * st);
       }
       if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-      tc_commit_if(leader, bar_drain);
-      __syncwarp();
-      if (!mbar_wait_bounded(bar_drain, 0, 1u << 12) && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    } else if (warp == kFMma && rank == 0 && !skip) {
+      issue_role(std::integral_constant<int, 0>{});
+    } else if (warp == kFMma + 1 && rank == 0 && !skip) {
+      issue_role(std::integral_constant<int, 1>{});
     }
   } else {
     reg_alloc_inc<kFRegsSoftmax>();
     // ================= softmax and output: thread = row =================
     const int w = warp >> 2, t = tid & 127;
-    const int row = row0 + 128 * w + t;                       // query token of the sequence
+    const int row = row0 + kFHalf * w + 128 * rank + t;       // query token of the sequence
     const int lim = min(sp.nk, sp.nk - sp.nq_all + row + 1);  // keys it sees
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t my_s = tmem + 128 * w + lane_base, my_o = tmem + kFTmemO + 128 * w + lane_base;
     const float scale_log2 = p.scale * 1.4426950408889634f;
     const uint64_t scale2 = f32x2(__float_as_uint(scale_log2), __float_as_uint(scale_log2));
-    const int n = skip ? 0 : n_tiles[w];
+    const int n = n_tiles[w];
+    const uint32_t to_p = in_cta(bar_p + 8 * w, 0);
     float m_ref = kFNoMax, l = 0.f;
     for (int j = 0; j < n; ++j) {
       if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * w, j & 1));
@@ -221,26 +371,13 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       for (int c = 0; c < 4; ++c) tmem_ld32(my_s + 32 * c, sv[c]);
       tmem_wait_ld();
       const int vis = lim - j * kFKeys;  // visible columns of this row
-      if (__any_sync(0xffffffffu, vis < kFKeys)) {
+      const bool edge = __any_sync(0xffffffffu, vis < kFKeys);
+      if (edge) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (c * 32 + e >= vis) sv[c][e] = 0xff800000u;  // -inf
-        const int valid = sp.nk - j * kFKeys;
-        if (valid < kFKeys && (w == 0 || j >= n_tiles[0])) {
-          // keys behind the sequence's end have weight 0, but their values may be anything: cleared (the halves
-          // share V; the other half's product with it is issued after this one's)
-          for (int ln = 0; ln < kFVLines; ++ln) {
-            const int u = j * kFUnits + kFKLines + ln;
-            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(full0 + 8 * (u % kFSlots), (u / kFSlots) & 1));
-            if (!ok) break;
-            for (int k = t; k < (kFKeys - valid) * 8; k += 128)
-              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(ring + (u % kFSlots) * kFLine + valid * 128 + k * 16), "r"(0));
-          }
-          fence_proxy_async();
-          if (!ok) break;
-        }
       }
       float mx[4];
 #pragma unroll
@@ -271,26 +408,36 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       }
       const uint64_t ref2 = f32x2(__float_as_uint(-m_ref), __float_as_uint(-m_ref));
       uint64_t sum2[2] = {0ull, 0ull};
+      auto weights = [&](auto poly) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t pk[16];
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          float x0, x1;
-          f32x2_split(fma_f32x2(f32x2(sv[c][e], sv[c][e + 1]), scale2, ref2), x0, x1);
-          const float w0 = ex2(x0), w1 = ex2(x1);
-          sum2[(e >> 1) & 1] = add_f32x2(sum2[(e >> 1) & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
-          pk[e >> 1] = pack2<false>(w0, w1);
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t x = fma_f32x2(f32x2(sv[c][2 * e], sv[c][2 * e + 1]), scale2, ref2);
+            float w0, w1;
+            if (decltype(poly)::value && e % kFPolyOf == kFPolyOf - 1) {
+              exp2_pair(x, w0, w1);
+            } else {
+              f32x2_split(x, w0, w1);
+              w0 = ex2(w0);
+              w1 = ex2(w1);
+            }
+            sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
+            pk[e] = pack2<false>(w0, w1);
+          }
+          tmem_st16(my_s + 16 * c, pk);
         }
-        tmem_st16(my_s + 16 * c, pk);
-      }
+      };
+      if (edge) weights(std::false_type{});  // (weights of hidden keys are exactly zero)
+      else weights(std::true_type{});
       float s0, s1;
       f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
       l += s0 + s1;
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_tc(bar_p + 8 * w);
+      if (lane == 0) arrive_cluster_tc(to_p);
     }
     // ---- output
     if (n > 0) {
@@ -298,7 +445,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
       tc_fence_after();
     }
-    if (row0 + 128 * w + (warp & 3) * 32 < sp.nq) {  // (warp-uniform)
+    if (row0 + kFHalf * w + 128 * rank + (warp & 3) * 32 < sp.nq) {  // (warp-uniform)
       const float inv = n == 0 || !ok || l == 0.f ? 0.f : 1.f / l;
       __nv_bfloat16* out = p.out + (static_cast<int64_t>(sp.q0) + row) * p.out_token_stride + h * p.out_head_stride;
 #pragma unroll 1
@@ -320,24 +467,25 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     }
   }
 
-  // ---- teardown
+  // ---- teardown: neither CTA leaves while the other may still reach its barriers or tensor memory
   tc_fence_before();
   __syncthreads();
   if (tid == 0 && *cta_err) report(p.status, *cta_err);
+  cluster_sync();
   if (warp == kFMma) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kFTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kFTmemCols) : "memory");
   }
 }
 
-// [tokens][heads][lines][64]: a copy takes one line of 128 tokens of one head
+// [tokens][heads][lines][64]: a copy takes one line of box_tokens tokens of one head
 bool encode_rows(EncodeFn enc, CUtensorMap* map, const void* base, int64_t dim, int64_t heads, int64_t tokens, int64_t head_stride,
-                 int64_t token_stride) {
+                 int64_t token_stride, int box_tokens) {
   const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(dim / 64), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
   // (a dimension of extent 1 is never stepped over)
   const cuuint64_t strides[3] = {128, heads == 1 ? 128 : static_cast<cuuint64_t>(head_stride) * 2,
                                  tokens == 1 ? 128 : static_cast<cuuint64_t>(token_stride) * 2};
-  const cuuint32_t box[4] = {64, 1, 1, kFKeys};
+  const cuuint32_t box[4] = {64, 1, 1, static_cast<cuuint32_t>(box_tokens)};
   const cuuint32_t step[4] = {1, 1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -354,23 +502,23 @@ bool latent_prefill_tc_supports(const LatentPrefillParams& p) {
       !fits(p.v_head_stride, p.num_heads))
     return false;
   // (row and key numbers are counted in 32 bits, up to one block behind the last)
-  if (p.total_q > INT32_MAX - 512 || p.total_k > INT32_MAX - 512) return false;
-  return static_cast<int64_t>((p.max_q + kFRows - 1) / kFRows) * p.num_heads * p.batch <= INT32_MAX;
+  if (p.total_q > INT32_MAX - 1024 || p.total_k > INT32_MAX - 1024) return false;
+  return static_cast<int64_t>((p.max_q + kFRows - 1) / kFRows) * p.num_heads * p.batch <= INT32_MAX / 2;
 }
 
 cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t stream) {
   EncodeFn enc = tensor_map_encoder();
   if (!enc) return cudaErrorNotSupported;
   FMaps maps{};
-  if (!encode_rows(enc, &maps.q, p.q, 192, p.num_heads, p.total_q, p.q_head_stride, p.q_token_stride) ||
-      !encode_rows(enc, &maps.k_nope, p.k_nope, 128, p.num_heads, p.total_k, p.kn_head_stride, p.kn_token_stride) ||
-      !encode_rows(enc, &maps.k_rope, p.k_rope, 64, 1, p.total_k, 0, p.kr_token_stride) ||
-      !encode_rows(enc, &maps.v, p.v, 128, p.num_heads, p.total_k, p.v_head_stride, p.v_token_stride))
+  if (!encode_rows(enc, &maps.q, p.q, 192, p.num_heads, p.total_q, p.q_head_stride, p.q_token_stride, 128) ||
+      !encode_rows(enc, &maps.k_nope, p.k_nope, 128, p.num_heads, p.total_k, p.kn_head_stride, p.kn_token_stride, 64) ||
+      !encode_rows(enc, &maps.k_rope, p.k_rope, 64, 1, p.total_k, 0, p.kr_token_stride, 64) ||
+      !encode_rows(enc, &maps.v, p.v, 128, p.num_heads, p.total_k, p.v_head_stride, p.v_token_stride, kFKeys))
     return cudaErrorNotSupported;
   cudaError_t e = cudaFuncSetAttribute(latent_prefill_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFSmemBytes);
   if (e != cudaSuccess) return e;
   const int q_blocks = (p.max_q + kFRows - 1) / kFRows;
-  latent_prefill_tc_kernel<<<q_blocks * p.num_heads * p.batch, kFThreads, kFSmemBytes, stream>>>(maps, p, q_blocks);
+  latent_prefill_tc_kernel<<<2 * q_blocks * p.num_heads * p.batch, kFThreads, kFSmemBytes, stream>>>(maps, p, q_blocks);
   return cudaGetLastError();
 }
 
