@@ -46,7 +46,7 @@ static_assert(kFSoftWarps * 32 * kFRegsSoftmax + 128 * kFRegsControl <= kFThread
 constexpr uint32_t kFTmemCols = 512, kFTmemO = 256;  // S[w] at 128 w, P[w] over its first 64 columns, O[w] at 256 + 128 w
 constexpr float kFNoMax = -1e30f;
 constexpr float kFRescale = 8.f;
-constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
+constexpr int kFPolyOf = 3;  // every third pair of exponentials by polynomial (prompt of 8192, 32 heads: 585 us; none 601, every second 626)
 
 // 2^x for two x <= 2^7 on the FMA units, so that the exponentials are not bound by the special-function unit
 // alone: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the
@@ -165,7 +165,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
   // bar_p, bar_turn. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s, bar_pv.
   const uint32_t full_k = smem_u32(bars), empty_k = full_k + 8 * kFStages, full_v = empty_k + 8 * kFStages,
                  empty_v = full_v + 8 * kFStages, v_ready = empty_v + 8 * kFStages, bar_q = v_ready + 8 * kFStages;
-  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 16, bar_turn = bar_pv + 16, bar_drain = bar_turn + 16, bar_never = bar_drain + 8;
+  // (bar_p and bar_pv: [half w][keys 0..63, 64..127 of the tile])
+  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_drain = bar_turn + 16, bar_never = bar_drain + 8;
   if (tid == 0) {
     for (int i = 0; i < kFStages; ++i) {
       mbar_init(full_k + 8 * i, 1);
@@ -177,8 +178,10 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     for (int w = 0; w < 2; ++w) {
       mbar_init(bar_q + 8 * w, 1);
       mbar_init(bar_s + 8 * w, 1);
-      mbar_init(bar_p + 8 * w, 8);  // four warps of each CTA
-      mbar_init(bar_pv + 8 * w, 1);
+      for (int k = 0; k < 2; ++k) {
+        mbar_init(bar_p + 16 * w + 8 * k, 8);  // four warps of each CTA
+        mbar_init(bar_pv + 16 * w + 8 * k, 1);
+      }
       mbar_init(bar_turn + 8 * w, 1);
     }
     mbar_init(bar_drain, 2);
@@ -242,38 +245,47 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     for (int j = 0; ok && j < n_all; ++j) {
       const int sv = j % kFStages, sk = (j + 1) % kFStages, rv = j / kFStages, rk = (j + 1) / kFStages;
       // turn j: half 0 after half 1's turn j - 1, half 1 after half 0's turn j
-      const auto my_turn = [&]() {
-        if (w == 1) wait(bar_turn + 8, j);
-        else if (j > 0) wait(bar_turn, j - 1);
-      };
+      const uint32_t turn_bar = w == 1 || j > 0 ? bar_turn + 8 * w : 0u;
+      const int turn_phase = w == 1 ? j : j - 1;
       const auto pass_turn = [&]() {
         if (lane == 0) mbar_arrive_tc(bar_turn + 8 * (w ^ 1));
       };
       wait(v_ready + 8 * sv, rv);
-      if (j + 1 < n_all) wait(full_k + 8 * sk, rk);
       if (j < n) {
         const uint64_t v0 = tc_desc(uniform(u_v + sv * kFVBytes), 16, 1024);
         const uint32_t k_addr = uniform(u_k + sk * kFKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
         const uint32_t acc = uniform(j > 0 ? 1u : 0u);
-        wait(bar_p + 8 * w, j);
-        my_turn();
+        // the tile's first 64 keys as soon as their weights are there, under the softmax of the other 64
+        wait(bar_p + 16 * w, j);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
-        commit2_if(leader, bar_pv + 8 * w);
-        commit2_if(leader, ev);
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
+        commit2_if(leader, bar_pv + 16 * w);
+        if (j + 1 < n_all) wait(full_k + 8 * sk, rk);
+        {  // the other weights and the turn, looked for at once by different lanes
+          const bool second = (lane & 1) && turn_bar != 0u;
+          wait(second ? turn_bar : bar_p + 16 * w + 8, second ? turn_phase : j);
+        }
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 4; ks < 8; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, 1u);
+        commit2_if(leader, bar_pv + 16 * w + 8);
         if (j + 1 < n) {
           // S(j + 1) takes the place of P(j): the tensor core works a thread's products off in order
           s_product(k_addr);
           pass_turn();
+          commit2_if(leader, ev);
           commit2_if(leader, ek);
         } else {
           pass_turn();
+          commit2_if(leader, ev);
           if (j + 1 < n_all) give_back(empty_k + 8 * sk);
         }
       } else {
-        my_turn();
+        if (j + 1 < n_all) wait(full_k + 8 * sk, rk);
+        if (turn_bar != 0u) wait(turn_bar, turn_phase);
         pass_turn();
         give_back(empty_v + 8 * sv);
         if (j + 1 < n_all) give_back(empty_k + 8 * sk);
@@ -360,61 +372,40 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     const float scale_log2 = p.scale * 1.4426950408889634f;
     const uint64_t scale2 = f32x2(__float_as_uint(scale_log2), __float_as_uint(scale_log2));
     const int n = n_tiles[w];
-    const uint32_t to_p = in_cta(bar_p + 8 * w, 0);
+    const uint32_t to_p = in_cta(bar_p + 16 * w, 0);
     float m_ref = kFNoMax, l = 0.f;
     for (int j = 0; j < n; ++j) {
       if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * w, j & 1));
       if (!ok) break;
       tc_fence_after();
-      uint32_t sv[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(my_s + 32 * c, sv[c]);
-      tmem_wait_ld();
       const int vis = lim - j * kFKeys;  // visible columns of this row
       const bool edge = __any_sync(0xffffffffu, vis < kFKeys);
-      if (edge) {
+      // 64 keys at a time; the first half's products start while the second half is here
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+      for (int k = 0; k < 2; ++k) {
+        uint32_t sv[64];
+        tmem_ld32(my_s + 64 * k, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+        tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+        tmem_wait_ld();
+        if (edge) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (c * 32 + e >= vis) sv[c][e] = 0xff800000u;  // -inf
-      }
-      float mx[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        mx[c] = fmaxf(__uint_as_float(sv[c][0]), __uint_as_float(sv[c][1]));
-#pragma unroll
-        for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
-      }
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2;
-      if (__any_sync(0xffffffffu, top > m_ref + kFRescale)) {
-        const float m_new = fmaxf(m_ref, top), a = ex2(m_ref - m_new);
-        m_ref = m_new;
-        l *= a;
-        if (j > 0) {
-          if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 8 * w, (j - 1) & 1));
-          if (!ok) break;
-          tc_fence_after();
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            uint32_t ov[32];
-            tmem_ld32(my_o + 32 * c, ov);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
-            tmem_st32(my_o + 32 * c, ov);
-          }
+          for (int e = 0; e < 64; ++e)
+            if (64 * k + e >= vis) sv[e] = 0xff800000u;  // -inf
         }
-      }
-      const uint64_t ref2 = f32x2(__float_as_uint(-m_ref), __float_as_uint(-m_ref));
-      uint64_t sum2[2] = {0ull, 0ull};
-      auto weights = [&](auto poly) {
+        // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
+        // reference by so much that the reference is raised and the weights are taken again.
+        uint32_t pk[32];
+        float part;
+        const float neg_inf = -INFINITY;
+        float top = neg_inf;
+        auto weights = [&](auto poly, auto with_max) {
+          const uint64_t ref2 = f32x2(__float_as_uint(-m_ref), __float_as_uint(-m_ref));
+          uint64_t sum2[2] = {0ull, 0ull};
+          float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint64_t x = fma_f32x2(f32x2(sv[c][2 * e], sv[c][2 * e + 1]), scale2, ref2);
+          for (int e = 0; e < 32; ++e) {
+            const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), scale2, ref2);
+            if (decltype(with_max)::value) mx[e & 1] = max3(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
             float w0, w1;
             if (decltype(poly)::value && e % kFPolyOf == kFPolyOf - 1) {
               exp2_pair(x, w0, w1);
@@ -426,22 +417,47 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
             pk[e] = pack2<false>(w0, w1);
           }
-          tmem_st16(my_s + 16 * c, pk);
+          float s0, s1;
+          f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
+          part = s0 + s1;
+          if (decltype(with_max)::value) top = fmaxf(mx[0], mx[1]) * scale_log2;
+        };
+        constexpr std::true_type yes{};
+        constexpr std::false_type no{};
+        if (edge) weights(no, yes);  // (weights of hidden keys are exactly zero)
+        else weights(yes, yes);
+        if (__any_sync(0xffffffffu, top > m_ref + kFRescale)) {
+          const float m_new = fmaxf(m_ref, top), a = ex2(m_ref - m_new);
+          m_ref = m_new;
+          l *= a;
+          if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first half of this one
+            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? j - 1 : j) & 1));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              uint32_t ov[32];
+              tmem_ld32(my_o + 32 * c, ov);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
+              tmem_st32(my_o + 32 * c, ov);
+            }
+          }
+          weights(no, no);
         }
-      };
-      if (edge) weights(std::false_type{});  // (weights of hidden keys are exactly zero)
-      else weights(std::true_type{});
-      float s0, s1;
-      f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
-      l += s0 + s1;
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_cluster_tc(to_p);
+        l += part;
+        tmem_st32(my_s + 32 * k, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cluster_tc(to_p + 8 * k);
+      }
+      if (!ok) break;
     }
     // ---- output
     if (n > 0) {
-      if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 8 * w, (n - 1) & 1));
+      if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (n - 1) & 1));
       if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
       tc_fence_after();
     }
