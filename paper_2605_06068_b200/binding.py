@@ -442,21 +442,24 @@ def latent_desc(cache: torch.Tensor, latent_dim: int) -> LatentDesc:
         raise ValueError("a latent cache is [num_pages, page_size, latent_dim + rope_dim]")
     _bf16_rows("cache", cache)
     n, P, W = cache.shape
+    page, slot, _ = cache.stride()
     # (a dimension of extent 1 may carry any stride: the one of the dense layout is taken)
-    slot = cache.stride(1) if P > 1 else max(cache.stride(1), W)
-    page = cache.stride(0) if n > 1 else max(cache.stride(0), P * slot)
-    return LatentDesc(page, slot, n, P, int(latent_dim), W - int(latent_dim), PDA_BF16)
+    if P == 1:
+        slot = max(slot, W)
+    if n <= 1:
+        page = max(page, P * slot)
+    return LatentDesc(page, slot, n, P, latent_dim, W - latent_dim, PDA_BF16)
 
 
 def _check_table(block_table, batch):
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != batch:
+    """Entries per row. The row stride is also the row's capacity: a view whose stride is longer than its row would be
+    read past it, so rows must follow one another."""
+    if block_table.dtype is not _I32 or block_table.dim() != 2 or block_table.shape[0] != batch:
         raise ValueError("block_table: expected int32 [batch, pages]")
-    if block_table.shape[1] > 1 and block_table.stride(1) != 1:
-        raise ValueError("block_table: rows must be contiguous")
-    # the row stride is also the row's capacity: a view with a longer stride than its row would be read past it
-    if batch > 1 and block_table.stride(0) != block_table.shape[1]:
+    n = block_table.shape[1]
+    if not block_table.is_contiguous():
         raise ValueError("block_table: rows must follow one another (pass a contiguous table)")
-    return block_table.shape[1]
+    return n
 
 
 def paged_build_tables(seq_lens, new_lens, page_size, free_pages, free_count, block_table, cu_new, slot_map,
@@ -465,10 +468,10 @@ def paged_build_tables(seq_lens, new_lens, page_size, free_pages, free_count, bl
 
     ``free_count`` int32[1] (updated in place unless ``free_count_out`` is given); ``cu_new`` int32[B + 1];
     ``slot_map`` and ``positions`` int32[capacity]."""
-    B = seq_lens.shape[0]
+    B = seq_lens.numel()
     _int32(seq_lens, new_lens, free_pages, free_count, cu_new, slot_map, positions, free_count_out, status)
     stride = _check_table(block_table, B)
-    if new_lens.shape[0] != B or cu_new.numel() < B + 1 or (positions is not None and positions.numel() < slot_map.numel()):
+    if new_lens.numel() != B or cu_new.numel() < B + 1 or (positions is not None and positions.numel() < slot_map.numel()):
         raise ValueError("new_lens, cu_new or positions too short")
     dev = _same_device(seq_lens, new_lens, free_pages, free_count, block_table, cu_new, slot_map, positions, free_count_out, status)
     if free_count_out is None:
@@ -514,45 +517,59 @@ def latent_workspace(batch, num_q_heads, n_query_tokens, latent_dim, device="cud
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _token_strides(name, t):
-    """(token stride, head stride) of ``[B, T, H, D]``, tokens numbered ``b*T + t``; ``[B, H, D]`` is ``T = 1``."""
-    B, T, H, _ = t.shape
-    if B > 1 and T > 1 and t.stride(0) != T * t.stride(1):
-        raise ValueError(f"{name}: batch and token dimensions must be evenly strided together")
-    token = t.stride(1) if T > 1 else t.stride(0)
-    return (token if B * T > 1 else 0), (t.stride(2) if H > 1 else 0)
+def _token_strides(name, t, B, T, H):
+    """(token stride, head stride) of ``[B, T, H, D]`` (or ``[B, H, D]``: ``T = 1``), tokens numbered ``b*T + t``."""
+    if t.dim() == 3:
+        token, head, _ = t.stride()
+    else:
+        batch, token, head, _ = t.stride()
+        if T == 1:
+            token = batch
+        elif B > 1 and batch != T * token:
+            raise ValueError(f"{name}: batch and token dimensions must be evenly strided together")
+    return (token if B * T > 1 else 0), (head if H > 1 else 0)
 
 
 def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale, out=None, workspace=None, flags=0,
                            status=None, stream=None):
     """Absorbed attention over the paged latent cache: ``q_latent [B,T,H,R]`` (or ``[B,H,R]``), ``q_rope [B,T,H,Dr]``;
     fills and returns ``out`` like ``q_latent``. Without ``workspace`` one is allocated for the call."""
+    shape = q_latent.shape
+    if len(shape) == 4:
+        B, T, H, R = shape
+    else:
+        (B, H, R), T = shape, 1
     if out is None:
-        out = torch.empty(q_latent.shape, dtype=q_latent.dtype, device=q_latent.device)
-    ql, qr, o = (t if t is None or t.dim() == 4 else t.unsqueeze(1) for t in (q_latent, q_rope, out))
-    B, T, H, R = ql.shape
-    desc = latent_desc(cache, R)
-    for name, t in (("q_latent", ql), ("q_rope", qr), ("out", o)):
-        if t is not None:
-            _bf16_rows(name, t)
-    if desc.rope_dim > 0 and tuple(qr.shape) != (B, T, H, desc.rope_dim):
-        raise ValueError("q_rope: expected [batch, tokens, heads, rope_dim]")
-    if o.shape != ql.shape:
+        out = torch.empty(shape, dtype=q_latent.dtype, device=q_latent.device)
+    elif out.shape != shape:
         raise ValueError("out: expected the shape of q_latent")
+    desc = latent_desc(cache, R)
+    rope = desc.rope_dim
+    _bf16_rows("q_latent", q_latent)
+    _bf16_rows("out", out)
+    if rope > 0:
+        _bf16_rows("q_rope", q_rope)
+        if q_rope.shape[:-1] != shape[:-1] or q_rope.shape[-1] != rope:
+            raise ValueError("q_rope: expected [batch, tokens, heads, rope_dim]")
+        qr_token, qr_head = _token_strides("q_rope", q_rope, B, T, H)
+    else:
+        q_rope, qr_token, qr_head = None, 0, 0
+    ql_token, ql_head = _token_strides("q_latent", q_latent, B, T, H)
+    out_token, out_head = _token_strides("out", out, B, T, H)
     _int32(seq_lens, status)
     if seq_lens.numel() != B:
         raise ValueError("seq_lens: expected one entry per sequence")
     stride = _check_table(block_table, B)
-    qls, qrs, os_ = _token_strides("q_latent", ql), (0, 0) if desc.rope_dim == 0 else _token_strides("q_rope", qr), _token_strides("out", o)
     if workspace is None:
         workspace = latent_workspace(B, H, T, R, device=cache.device)
-    dev = _same_device(ql, qr, o, cache, block_table, seq_lens, workspace, status)
+    dev = _same_device(q_latent, q_rope, out, cache, block_table, seq_lens, workspace, status)
     with _device_call(dev):
         rc = lib().paged_latent_attention(
-            _dp(ql), qls[0], qls[1], None if desc.rope_dim == 0 else _dp(qr), qrs[0], qrs[1], _dp(cache), C.byref(desc),
-            _dp(block_table), stride, _dp(seq_lens), B, H, T, float(scale), _dp(o), os_[0], os_[1],
-            _dp(workspace), workspace.numel() * workspace.element_size(), flags, _dp(status), _raw(stream, dev))
-    _check(rc, "paged_latent_attention")
+            q_latent.data_ptr(), ql_token, ql_head, _dp(q_rope), qr_token, qr_head, cache.data_ptr(), C.byref(desc),
+            block_table.data_ptr(), stride, seq_lens.data_ptr(), B, H, T, scale, out.data_ptr(), out_token, out_head,
+            workspace.data_ptr(), workspace.nbytes, flags, _dp(status), _raw(stream, dev))
+    if rc:
+        _check(rc, "paged_latent_attention")
     return out
 
 

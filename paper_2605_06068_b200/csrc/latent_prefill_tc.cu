@@ -16,10 +16,12 @@
 // The softmax takes weights relative to a reference per row that is raised (and O rescaled in tensor memory)
 // only when the row's maximum passes it by more than 2^8; row sums are kept by the row's thread, of the
 // 32-bit weights; the rounding of the weights to bf16 is 2^-8 of each.
-// Blocks at the end of the longest prompts have the most keys and start first.
+// Each pair of CTAs works through several row blocks, those with the most keys first and dealt to and fro; the
+// producer runs on into the next block's Q, K and V while the last one's output is written.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the
 // pair's first CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are
 // bounded.
+#include <algorithm>
 #include <type_traits>
 
 #include "latent.cuh"
@@ -38,15 +40,18 @@ constexpr int kFKLine = 64 * 128, kFKBytes = 3 * kFKLine;  // of its 64 keys
 constexpr int kFVBytes = kFKeys * 128;                    // its line (64 dims) of all keys
 constexpr int kFStages = 3;                               // tiles
 constexpr int kFSoftWarps = 8, kFThreads = (kFSoftWarps + 4) * 32, kFProducer = 8, kFMma = 9, kFRelay = 11;  // (9, 10: one per half)
-constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 512 + 1024;
+constexpr int kFOutBytes = 1024;                          // per softmax warp: 8 rows of 64 dims on their way out
+constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 2048 + kFSoftWarps * kFOutBytes + 1024;
 static_assert(kFSmemBytes <= 232448, "shared memory");
 // 384 threads start with 168 registers (64512 in all); the control warps keep 104 and the softmax warps take 200
 constexpr uint32_t kFRegsSoftmax = 200, kFRegsControl = 104;
 static_assert(kFSoftWarps * 32 * kFRegsSoftmax + 128 * kFRegsControl <= kFThreads * 168, "registers");
 constexpr uint32_t kFTmemCols = 512, kFTmemO = 256;  // S[w] at 128 w, P[w] over its first 64 columns, O[w] at 256 + 128 w
+constexpr int kFUnitSlots = 4;                            // units the producer may be ahead
+constexpr int kFMaxList = 128;                            // row blocks that are sorted by their work
 constexpr float kFNoMax = -1e30f;
 constexpr float kFRescale = 8.f;
-constexpr int kFPolyOf = 3;  // every third pair of exponentials by polynomial (prompt of 8192, 32 heads: 585 us; none 601, every second 626)
+constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
 
 // 2^x for two x <= 2^7 on the FMA units, so that the exponentials are not bound by the special-function unit
 // alone: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the
@@ -69,6 +74,15 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
   w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
 }
 
+// One row block of one head, as the producer hands it to the other warps of its CTA. row0 < 0: no more.
+struct FUnit {
+  int row0, h, q0, nq, nq_all, k0, nk, n0, n1;
+};
+struct FPlan {
+  int q_blocks;  // blocks of max_q
+  int listed;    // the row blocks of all sequences are few enough to be listed and sorted in shared memory
+};
+
 struct FMaps {
   CUtensorMap q, k_nope, k_rope, v;
 };
@@ -82,7 +96,7 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {  // bar: an address of in_cta
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// The same where only tensor memory has been written, which the tcgen05 fences order.
+// The same where nothing has been written, or only tensor memory, which the tcgen05 fences order.
 __device__ __forceinline__ void arrive_cluster_tc(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -132,41 +146,32 @@ __device__ __forceinline__ void commit2_if(uint32_t leader, uint32_t bar) {
 }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFThreads, 1)
-latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_constant__ LatentPrefillParams p, int q_blocks) {
+latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_constant__ LatentPrefillParams p,
+                         const __grid_constant__ FPlan plan) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes));
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 40);
+  FUnit* units = reinterpret_cast<FUnit*>(bars + 48);               // [kFUnitSlots]
+  uint32_t* list = reinterpret_cast<uint32_t*>(units + kFUnitSlots);  // [kFMaxList] sequence and block, most work first
+  uint32_t* work = list + kFMaxList;                                // [kFMaxList] (start of the kernel only)
+  uint32_t* scan = work + kFMaxList;                                // [5] sequences' blocks, by warp; their sum
+  uint32_t* tmem_slot = scan + 5;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
+  static_assert(48 * 8 + kFUnitSlots * sizeof(FUnit) + 2 * kFMaxList * 4 + 7 * 4 <= 2048, "shared memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1;  // in the pair
-
-  // late blocks first (all heads and sequences of a block index together)
-  const int per_block = p.num_heads * p.batch;
-  const int pair = blockIdx.x >> 1;
-  const int qb = q_blocks - 1 - pair / per_block;
-  const int b = (pair % per_block) / p.num_heads, h = (pair % per_block) % p.num_heads;
-  const PrefillSpan sp = prefill_span(p, b);
-  const int row0 = qb * kFRows;
-  if (row0 >= sp.nq) return;  // (both CTAs)
-  // keys that the last row of half w can see, in tiles (of either CTA: the pair walks together)
-  int n_tiles[2];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const int first = row0 + kFHalf * w, last = min(first + kFHalf - 1, sp.nq - 1);
-    const int see = first >= sp.nq ? 0 : min(max(sp.nk - sp.nq_all + last + 1, 0), sp.nk);
-    n_tiles[w] = (see + kFKeys - 1) / kFKeys;
-  }
-  const int n_max = max(n_tiles[0], n_tiles[1]);
+  const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   bool ok = true;
 
   const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + 2 * kFQLines * kFQLine, v_sm = k_sm + kFStages * kFKBytes;
   // Barriers, at the same place in both CTAs. Of the pair's first CTA: full_k (both CTAs' copies), v_ready, bar_q,
-  // bar_p, bar_turn. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s, bar_pv.
+  // bar_p, bar_turn, bar_ofree. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s,
+  // bar_pv, bar_qfree, the unit slots'. bar_p and bar_pv: [half w][keys 0..63, 64..127 of the tile].
   const uint32_t full_k = smem_u32(bars), empty_k = full_k + 8 * kFStages, full_v = empty_k + 8 * kFStages,
                  empty_v = full_v + 8 * kFStages, v_ready = empty_v + 8 * kFStages, bar_q = v_ready + 8 * kFStages;
-  // (bar_p and bar_pv: [half w][keys 0..63, 64..127 of the tile])
-  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_drain = bar_turn + 16, bar_never = bar_drain + 8;
+  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_qfree = bar_turn + 16,
+                 bar_ofree = bar_qfree + 16, unit_full = bar_ofree + 16, unit_empty = unit_full + 8 * kFUnitSlots,
+                 bar_drain = unit_empty + 8 * kFUnitSlots, bar_never = bar_drain + 8;
   if (tid == 0) {
     for (int i = 0; i < kFStages; ++i) {
       mbar_init(full_k + 8 * i, 1);
@@ -183,6 +188,12 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         mbar_init(bar_pv + 16 * w + 8 * k, 1);
       }
       mbar_init(bar_turn + 8 * w, 1);
+      mbar_init(bar_qfree + 8 * w, 1);
+      mbar_init(bar_ofree + 8 * w, 8);
+    }
+    for (int i = 0; i < kFUnitSlots; ++i) {
+      mbar_init(unit_full + 8 * i, 1);
+      mbar_init(unit_empty + 8 * i, kFSoftWarps + 1 + (rank == 0 ? 2 : 0));  // softmax, relay, product warps
     }
     mbar_init(bar_drain, 2);
     mbar_init(bar_never, 1);
@@ -190,16 +201,77 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     fence_mbar_init();
     fence_proxy_async();
   }
+  if (warp == kFProducer && elect_one()) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k_nope) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k_rope) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
+  }
   if (warp == kFMma) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kFTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  // ---- the row blocks that there are, those with the most keys first (every CTA for itself, all alike)
+  int my_blocks = 0;
+  PrefillSpan mine{0, 0, 0, 0, 0};
+  if (plan.listed && tid < kFMaxList && tid < p.batch) {
+    mine = prefill_span(p, tid);
+    my_blocks = (mine.nq + kFRows - 1) / kFRows;
+  }
+  int incl = my_blocks;
+  if (plan.listed && tid < kFMaxList) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    if (lane == 31) scan[warp] = incl;
+  }
   tc_fence_before();
+  __syncthreads();
+  int n_blocks = 0;
+  uint32_t my_work = 0, my_entry = 0;
+  if (plan.listed) {
+    int before = incl - my_blocks;
+    for (int i = 0; i < kFMaxList / 32; ++i) {
+      before += i < warp ? scan[i] : 0;
+      n_blocks += scan[i];
+    }
+    // (ascending offsets give at most as many as the host has allowed for; others are reported)
+    if (n_blocks > kFMaxList) {
+      report(p.status, PDA_DEV_BAD_SEQ_LEN);
+      n_blocks = kFMaxList;
+    }
+    for (int k = 0; k < my_blocks && before + k < kFMaxList; ++k) {
+      const int last = min((k + 1) * kFRows, mine.nq) - 1;
+      work[before + k] = min(max(mine.nk - mine.nq_all + last + 1, 0), mine.nk);
+      list[before + k] = tid | (k << 7);
+    }
+    __syncthreads();
+    int place = 0;
+    if (tid < n_blocks) {
+      my_work = work[tid];
+      my_entry = list[tid];
+      for (int i = 0; i < n_blocks; ++i) place += work[i] > my_work || (work[i] == my_work && i < tid);
+    }
+    __syncthreads();
+    if (tid < n_blocks) list[place] = my_entry;
+  }
   __syncthreads();
   cluster_sync();
   tc_fence_after();
-  const bool skip = n_max == 0;
   const uint32_t tmem = *tmem_slot;
+
+  // Unit number k of this CTA, for the warps that are told by the producer.
+  auto next_unit = [&](int k, FUnit& un) {
+    const int slot = k % kFUnitSlots;
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(unit_full + 8 * slot, (k / kFUnitSlots) & 1));
+    if (!ok) return false;
+    un = units[slot];
+    __syncwarp();
+    if (lane == 0) mbar_arrive_tc(unit_empty + 8 * slot);
+    return un.row0 >= 0;
+  };
 
   // ================= products of half w =================
   // A warp for each half, which prepares its next products while the other's are being issued (one warp for
@@ -212,14 +284,9 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     const uint32_t leader = elect_one();
     const uint32_t u_q = uniform(q_sm + w * kFQLines * kFQLine), u_k = uniform(k_sm), u_v = uniform(v_sm), u_tmem = uniform(tmem);
     const uint32_t u_ek = uniform(empty_k), u_ev = uniform(empty_v);
-    const int n = uniform(n_tiles[w]), n_all = uniform(n_max);
     const uint32_t d_s = u_tmem + 128 * w, d_o = u_tmem + kFTmemO + 128 * w;
     auto wait = [&](uint32_t bar, int phase) {
       if (ok) ok = __all_sync(0xffffffffu, mbar_spin_cluster(bar, phase & 1));
-    };
-    auto give_back = [&](uint32_t bar) {  // a tile's part that this half does not read, in both CTAs
-      if (ok && lane < 2) arrive_cluster(in_cta(bar, lane));
-      __syncwarp();
     };
     auto s_product = [&](uint32_t k_addr) {
       const uint64_t q0 = tc_desc(u_q, 16, 1024), k0 = tc_desc(k_addr, 16, 1024);
@@ -230,66 +297,75 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
           mma2_ss_if(leader, d_s, q0 + ln * (kFQLine / 16) + 2 * ks, k0 + ln * (kFKLine / 16) + 2 * ks, idesc_s, (ln > 0 || ks > 0) ? 1u : 0u);
       commit2_if(leader, bar_s + 8 * w);
     };
-    if (n > 0) {
-      wait(bar_q + 8 * w, 0);
-      wait(full_k, 0);
-      if (ok) {
-        tc_fence_after();
-        s_product(u_k);
-        commit2_if(leader, u_ek);
-      }
-    } else {
-      wait(full_k, 0);
-      give_back(empty_k);
-    }
-    for (int j = 0; ok && j < n_all; ++j) {
-      const int sv = j % kFStages, sk = (j + 1) % kFStages, rv = j / kFStages, rk = (j + 1) / kFStages;
-      // turn j: half 0 after half 1's turn j - 1, half 1 after half 0's turn j
-      const uint32_t turn_bar = w == 1 || j > 0 ? bar_turn + 8 * w : 0u;
-      const int turn_phase = w == 1 ? j : j - 1;
-      const auto pass_turn = [&]() {
-        if (lane == 0) mbar_arrive_tc(bar_turn + 8 * (w ^ 1));
+    FUnit un;
+    // Before this unit: tiles of the pair; of this half; units of this half; tiles on which the halves take turns.
+    int t0 = 0, mine = 0, done = 0, turns = 0;
+    for (int k = 0; next_unit(k, un); ++k) {
+      const int n = uniform(w == 0 ? un.n0 : un.n1), n_other = uniform(w == 0 ? un.n1 : un.n0);
+      // Both halves give a tile back. The one that does not read it does so as soon as it is there (not before: a
+      // half that did not follow every phase of a barrier could not tell the phases apart) and goes on, to the next
+      // unit where this was the last tile.
+      auto hand_on = [&](uint32_t full, uint32_t empty, int phase) {
+        wait(full, phase);
+        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty, lane));
+        __syncwarp();
       };
-      wait(v_ready + 8 * sv, rv);
-      if (j < n) {
+      if (n > 0) {  // S(0): its place is free, the tensor core works a thread's products off in order
+        const int sk = t0 % kFStages;
+        wait(bar_q + 8 * w, done);
+        wait(full_k + 8 * sk, t0 / kFStages);
+        if (!ok) break;
+        tc_fence_after();
+        s_product(uniform(u_k + sk * kFKBytes));
+        if (n == 1) commit2_if(leader, bar_qfree + 8 * w);
+        commit2_if(leader, uniform(u_ek + 8 * sk));
+      }
+      for (int j = 0; j < n; ++j) {
+        const int t = t0 + j, sv = t % kFStages, sk = (t + 1) % kFStages;
+        // turn i: half 0 after half 1's turn i - 1, half 1 after half 0's turn i
+        const bool taking_turns = j < n_other;
+        const int turn = turns + j;
+        const uint32_t turn_bar = taking_turns && (w == 1 || turn > 0) ? bar_turn + 8 * w : 0u;
+        const int turn_phase = w == 1 ? turn : turn - 1;
+        wait(v_ready + 8 * sv, t / kFStages);
         const uint64_t v0 = tc_desc(uniform(u_v + sv * kFVBytes), 16, 1024);
         const uint32_t k_addr = uniform(u_k + sk * kFKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
         const uint32_t acc = uniform(j > 0 ? 1u : 0u);
+        if (j == 0 && done > 0) wait(bar_ofree + 8 * w, done - 1);  // the last unit's output has been read
         // the tile's first 64 keys as soon as their weights are there, under the softmax of the other 64
-        wait(bar_p + 16 * w, j);
+        wait(bar_p + 16 * w, mine + j);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
         commit2_if(leader, bar_pv + 16 * w);
-        if (j + 1 < n_all) wait(full_k + 8 * sk, rk);
+        if (j + 1 < n) wait(full_k + 8 * sk, (t + 1) / kFStages);
         {  // the other weights and the turn, looked for at once by different lanes
           const bool second = (lane & 1) && turn_bar != 0u;
-          wait(second ? turn_bar : bar_p + 16 * w + 8, second ? turn_phase : j);
+          wait(second ? turn_bar : bar_p + 16 * w + 8, second ? turn_phase : mine + j);
         }
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int ks = 4; ks < 8; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, 1u);
         commit2_if(leader, bar_pv + 16 * w + 8);
-        if (j + 1 < n) {
-          // S(j + 1) takes the place of P(j): the tensor core works a thread's products off in order
-          s_product(k_addr);
-          pass_turn();
-          commit2_if(leader, ev);
-          commit2_if(leader, ek);
-        } else {
-          pass_turn();
-          commit2_if(leader, ev);
-          if (j + 1 < n_all) give_back(empty_k + 8 * sk);
-        }
-      } else {
-        if (j + 1 < n_all) wait(full_k + 8 * sk, rk);
-        if (turn_bar != 0u) wait(turn_bar, turn_phase);
-        pass_turn();
-        give_back(empty_v + 8 * sv);
-        if (j + 1 < n_all) give_back(empty_k + 8 * sk);
+        // S(j + 1) takes the place of P(j): the tensor core works a thread's products off in order
+        if (j + 1 < n) s_product(k_addr);
+        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * (w ^ 1));
+        if (j + 2 == n) commit2_if(leader, bar_qfree + 8 * w);
+        commit2_if(leader, ev);
+        if (j + 1 < n) commit2_if(leader, ek);
       }
+      for (int t = t0 + n; ok && t < t0 + n_other; ++t) {
+        const int st = t % kFStages;
+        hand_on(full_k + 8 * st, empty_k + 8 * st, t / kFStages);
+        hand_on(v_ready + 8 * st, empty_v + 8 * st, t / kFStages);
+      }
+      if (!ok) break;
+      t0 += max(n, n_other);
+      turns += min(n, n_other);
+      mine += n;
+      if (n > 0) ++done;
     }
     if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
     asm volatile(
@@ -301,186 +377,290 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
 
   if (warp >= kFSoftWarps) {
     reg_alloc_dec<kFRegsControl>();
-    if (warp == kFProducer && !skip) {
-      // ================= TMA producer: this CTA's rows of Q, keys of K, dims of V =================
+    if (warp == kFProducer) {
+      // ================= units, and TMA: this CTA's rows of Q, keys of K, dims of V =================
       const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
       const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
-      const int token0 = uniform(sp.q0 + row0 + 128 * rank), key0 = uniform(sp.k0), u_h = uniform(h);
       const uint32_t to_q = uniform(in_cta(bar_q, 0)), to_k = uniform(in_cta(full_k, 0));
-      auto load_q = [&](int w) {
-        mbar_expect_tx_if(first, bar_q + 8 * w, 2 * kFQLines * kFQLine);
+      const int64_t n_units = static_cast<int64_t>(plan.listed ? n_blocks : plan.q_blocks * p.batch) * p.num_heads;
+      int64_t round = 0;
+      // The pair's next unit: every pairs-th of the order, to and fro, so that each pair gets early (long) and late
+      // (short) ones. Unlisted blocks may be empty: 32 at a time are looked at.
+      auto find_unit = [&](FUnit& un) {
+        while (true) {
+          const int64_t r = round + lane, at = r * pairs + (r & 1 ? pairs - 1 - pair : pair);
+          int qb = 0, b = 0, h = 0;
+          PrefillSpan sp{0, 0, 0, 0, 0};
+          if (at < n_units) {
+            if (plan.listed) {
+              const uint32_t e = list[at / p.num_heads];
+              h = static_cast<int>(at % p.num_heads);
+              b = e & 127;
+              qb = e >> 7;
+            } else {
+              const int64_t in_block = at % (static_cast<int64_t>(p.batch) * p.num_heads);
+              qb = plan.q_blocks - 1 - static_cast<int>(at / (static_cast<int64_t>(p.batch) * p.num_heads));
+              b = static_cast<int>(in_block / p.num_heads);
+              h = static_cast<int>(in_block % p.num_heads);
+            }
+            sp = prefill_span(p, b);
+          }
+          const uint32_t have = __ballot_sync(0xffffffffu, qb * kFRows < sp.nq);
+          if (have == 0) {
+            // (r grows with the lane, and so does `at` from one pair of rounds to the next)
+            if (round * pairs >= n_units) return false;
+            round += 32;
+            continue;
+          }
+          const int src = __ffs(have) - 1;
+          round += src + 1;
+          // keys that the last row of half w can see, in tiles (of either CTA: the pair walks together)
+          int n[2];
 #pragma unroll
-        for (int ln = 0; ln < kFQLines; ++ln)
-          tma_load_4d_pair_if(leader, u_q + (w * kFQLines + ln) * kFQLine, &maps.q, to_q + 8 * w, ln, u_h, token0 + kFHalf * w);
+          for (int w = 0; w < 2; ++w) {
+            const int from = qb * kFRows + kFHalf * w, last = min(from + kFHalf - 1, sp.nq - 1);
+            const int see = from >= sp.nq ? 0 : min(max(sp.nk - sp.nq_all + last + 1, 0), sp.nk);
+            n[w] = (see + kFKeys - 1) / kFKeys;
+          }
+          auto from_lane = [&](int v) { return __shfl_sync(0xffffffffu, v, src); };
+          un = FUnit{from_lane(qb * kFRows), from_lane(h), from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.nq_all),
+                     from_lane(sp.k0), from_lane(sp.nk), from_lane(n[0]), from_lane(n[1])};
+          return true;
+        }
       };
-      if (n_tiles[0] > 0) load_q(0);
-      int armed_k = 0, armed_v = 0;
-      for (int j = 0; ok && j < n_max; ++j) {
-        const int st = uniform(j % kFStages), round = j / kFStages;
-        if (round > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(empty_k + 8 * st, (round - 1) & 1));
+      int t = 0, done[2] = {0, 0};  // tiles so far; units of each half so far
+      for (int k = 0;; ++k) {
+        FUnit un;
+        const bool more = find_unit(un);
+        if (!more) un.row0 = -1;
+        const int slot = k % kFUnitSlots;
+        if (k >= kFUnitSlots) ok = __all_sync(0xffffffffu, mbar_wait_bounded(unit_empty + 8 * slot, (k / kFUnitSlots - 1) & 1));
         if (!ok) break;
-        mbar_expect_tx_if(first, full_k + 8 * st, 2 * kFKBytes);
-        const int key = key0 + j * kFKeys, my_key = key + 64 * rank;
-        const uint32_t kd = u_k + st * kFKBytes;
-        tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k + 8 * st, 0, u_h, my_key);
-        tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k + 8 * st, 1, u_h, my_key);
-        tma_load_4d_pair_if(leader, kd + 2 * kFKLine, &maps.k_rope, to_k + 8 * st, 0, 0, my_key);
-        ++armed_k;
-        if (j == 0 && n_tiles[1] > 0) load_q(1);
-        if (round > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(empty_v + 8 * st, (round - 1) & 1));
-        if (!ok) break;
-        mbar_expect_tx_if(leader, full_v + 8 * st, kFVBytes);
-        tma_load_4d_if(leader, u_v + st * kFVBytes, &maps.v, full_v + 8 * st, rank, u_h, key);
-        ++armed_v;
-      }
-      if (!ok) {  // copies in flight end before the CTA does (K's and Q's count in the first CTA: given time here)
-        if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-        for (int j = max(armed_v - kFStages, 0); j < armed_v; ++j) mbar_wait_bounded(full_v + 8 * (j % kFStages), (j / kFStages) & 1, 1u << 12);
-        for (int k = 0; k < 64; ++k) mbar_wait_bounded(bar_never, 0, 1);  // (4 us a poll)
-      }
-    } else if (warp == kFRelay && !skip) {
-      // ================= V tiles: cleared behind the sequence's end, then handed to the first CTA =================
-      const uint32_t to = in_cta(v_ready, 0);
-      for (int j = 0; ok && j < n_max; ++j) {
-        const int st = j % kFStages;
-        ok = __all_sync(0xffffffffu, mbar_spin_bounded(full_v + 8 * st, (j / kFStages) & 1));
-        if (!ok) break;
-        const int valid = sp.nk - j * kFKeys;
-        if (valid < kFKeys) {
-          // (keys behind the end have weight 0, but what they hold may be anything)
-          for (int k = lane; k < (kFKeys - valid) * 8; k += 32)
-            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * kFVBytes + valid * 128 + k * 16), "r"(0));
-          fence_proxy_async();
+        if (lane == 0) {
+          units[slot] = un;
+          mbar_arrive_tc(unit_full + 8 * slot);
         }
         __syncwarp();
-        if (lane == 0) arrive_cluster(to + 8 * st);
+        if (!more) break;
+        const int token0 = uniform(un.q0 + un.row0 + 128 * rank), key0 = un.k0, u_h = uniform(un.h);
+        const int n_all = max(un.n0, un.n1);
+        auto load_q = [&](int w) {
+          if (ok && done[w] > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_qfree + 8 * w, (done[w] - 1) & 1));
+          if (!ok) return;
+          mbar_expect_tx_if(first, bar_q + 8 * w, 2 * kFQLines * kFQLine);
+#pragma unroll
+          for (int ln = 0; ln < kFQLines; ++ln)
+            tma_load_4d_pair_if(leader, u_q + (w * kFQLines + ln) * kFQLine, &maps.q, to_q + 8 * w, ln, u_h, token0 + kFHalf * w);
+          ++done[w];
+        };
+        if (un.n0 > 0) load_q(0);
+        for (int j = 0; ok && j < n_all; ++j, ++t) {
+          const int st = uniform(t % kFStages), rnd = t / kFStages;
+          if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_k + 8 * st, (rnd - 1) & 1));
+          if (!ok) break;
+          mbar_expect_tx_if(first, full_k + 8 * st, 2 * kFKBytes);
+          const int key = uniform(key0 + j * kFKeys), my_key = key + 64 * rank;
+          const uint32_t kd = u_k + st * kFKBytes;
+          tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k + 8 * st, 0, u_h, my_key);
+          tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k + 8 * st, 1, u_h, my_key);
+          tma_load_4d_pair_if(leader, kd + 2 * kFKLine, &maps.k_rope, to_k + 8 * st, 0, 0, my_key);
+          if (j == 0 && un.n1 > 0) load_q(1);
+          if (ok && rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_v + 8 * st, (rnd - 1) & 1));
+          if (!ok) break;
+          mbar_expect_tx_if(leader, full_v + 8 * st, kFVBytes);
+          tma_load_4d_if(leader, u_v + st * kFVBytes, &maps.v, full_v + 8 * st, rank, u_h, key);
+        }
+        if (!ok) break;
+      }
+      if (!ok) {  // copies in flight end before the CTA does: they are given time (a millisecond; a copy takes microseconds)
+        if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+        for (int k = 0; k < 256; ++k) mbar_wait_bounded(bar_never, 0, 1);  // (4 us a poll)
+      }
+    } else if (warp == kFRelay) {
+      // ================= V tiles: cleared behind the sequence's end, then handed to the first CTA =================
+      const uint32_t to = in_cta(v_ready, 0);
+      FUnit un;
+      int t = 0;
+      for (int k = 0; next_unit(k, un); ++k) {
+        const int n_all = max(un.n0, un.n1);
+        for (int j = 0; ok && j < n_all; ++j, ++t) {
+          const int st = t % kFStages;
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_v + 8 * st, (t / kFStages) & 1));
+          if (!ok) break;
+          const int valid = un.nk - j * kFKeys;
+          if (valid < kFKeys) {
+            // (keys behind the end have weight 0, but what they hold may be anything)
+            for (int i = lane; i < (kFKeys - valid) * 8; i += 32)
+              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * kFVBytes + valid * 128 + i * 16), "r"(0));
+            fence_proxy_async();
+          }
+          __syncwarp();
+          if (lane == 0) {
+            if (valid < kFKeys) arrive_cluster(to + 8 * st);  // (with what has been written before it)
+            else arrive_cluster_tc(to + 8 * st);
+          }
+        }
+        if (!ok) break;
       }
       if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-    } else if (warp == kFMma && rank == 0 && !skip) {
+    } else if (warp == kFMma && rank == 0) {
       issue_role(std::integral_constant<int, 0>{});
-    } else if (warp == kFMma + 1 && rank == 0 && !skip) {
+    } else if (warp == kFMma + 1 && rank == 0) {
       issue_role(std::integral_constant<int, 1>{});
     }
   } else {
     reg_alloc_inc<kFRegsSoftmax>();
     // ================= softmax and output: thread = row =================
-    const int w = warp >> 2, t = tid & 127;
-    const int row = row0 + kFHalf * w + 128 * rank + t;       // query token of the sequence
-    const int lim = min(sp.nk, sp.nk - sp.nq_all + row + 1);  // keys it sees
+    const int w = warp >> 2;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t my_s = tmem + 128 * w + lane_base, my_o = tmem + kFTmemO + 128 * w + lane_base;
     const float scale_log2 = p.scale * 1.4426950408889634f;
     const uint64_t scale2 = f32x2(__float_as_uint(scale_log2), __float_as_uint(scale_log2));
-    const int n = n_tiles[w];
-    const uint32_t to_p = in_cta(bar_p + 16 * w, 0);
-    float m_ref = kFNoMax, l = 0.f;
-    for (int j = 0; j < n; ++j) {
-      if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * w, j & 1));
-      if (!ok) break;
-      tc_fence_after();
-      const int vis = lim - j * kFKeys;  // visible columns of this row
-      const bool edge = __any_sync(0xffffffffu, vis < kFKeys);
-      // 64 keys at a time; the first half's products start while the second half is here
+    const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
+    const uint32_t stage = smem_u32(smem) + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 2048 + warp * kFOutBytes;
+    const float neg_inf = -INFINITY;
+    FUnit un;
+    int t = 0;  // tiles of this half so far
+    for (int unit = 0; next_unit(unit, un); ++unit) {
+      const int row = un.row0 + kFHalf * w + 128 * rank + (tid & 127);  // query token of the sequence
+      const int lim = min(un.nk, un.nk - un.nq_all + row + 1);          // keys it sees
+      const int n = w == 0 ? un.n0 : un.n1;
+      float m_ref = kFNoMax, l = 0.f;
+      for (int j = 0; j < n; ++j, ++t) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * w, t & 1));
+        if (!ok) break;
+        tc_fence_after();
+        const int vis = lim - j * kFKeys;  // visible columns of this row
+        const bool edge = __any_sync(0xffffffffu, vis < kFKeys);
+        // 64 keys at a time; the first run's products start while the second run is here
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint32_t sv[64];
-        tmem_ld32(my_s + 64 * k, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
-        tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-        tmem_wait_ld();
-        if (edge) {
+        for (int k = 0; k < 2; ++k) {
+          uint32_t sv[64];
+          tmem_ld32(my_s + 64 * k, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+          tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+          tmem_wait_ld();
+          if (edge) {
 #pragma unroll
-          for (int e = 0; e < 64; ++e)
-            if (64 * k + e >= vis) sv[e] = 0xff800000u;  // -inf
-        }
-        // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
-        // reference by so much that the reference is raised and the weights are taken again.
-        uint32_t pk[32];
-        float part;
-        const float neg_inf = -INFINITY;
-        float top = neg_inf;
-        auto weights = [&](auto poly, auto with_max) {
-          const uint64_t ref2 = f32x2(__float_as_uint(-m_ref), __float_as_uint(-m_ref));
-          uint64_t sum2[2] = {0ull, 0ull};
-          float mx[2] = {neg_inf, neg_inf};
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), scale2, ref2);
-            if (decltype(with_max)::value) mx[e & 1] = max3(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
-            float w0, w1;
-            if (decltype(poly)::value && e % kFPolyOf == kFPolyOf - 1) {
-              exp2_pair(x, w0, w1);
-            } else {
-              f32x2_split(x, w0, w1);
-              w0 = ex2(w0);
-              w1 = ex2(w1);
-            }
-            sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
-            pk[e] = pack2<false>(w0, w1);
+            for (int e = 0; e < 64; ++e)
+              if (64 * k + e >= vis) sv[e] = 0xff800000u;  // -inf
           }
-          float s0, s1;
-          f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
-          part = s0 + s1;
-          if (decltype(with_max)::value) top = fmaxf(mx[0], mx[1]) * scale_log2;
-        };
-        constexpr std::true_type yes{};
-        constexpr std::false_type no{};
-        if (edge) weights(no, yes);  // (weights of hidden keys are exactly zero)
-        else weights(yes, yes);
-        if (__any_sync(0xffffffffu, top > m_ref + kFRescale)) {
-          const float m_new = fmaxf(m_ref, top), a = ex2(m_ref - m_new);
-          m_ref = m_new;
-          l *= a;
-          if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first half of this one
-            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? j - 1 : j) & 1));
-            if (!ok) break;
-            tc_fence_after();
+          if (k == 0 && j == 0) {  // the first reference: the maximum of the first 64 scores
+            float mx[2] = {neg_inf, neg_inf};
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+            m_ref = fmaxf(kFNoMax, fmaxf(mx[0], mx[1]) * scale_log2);
+          }
+          // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
+          // reference by so much that the reference is raised and the weights are taken again.
+          uint32_t pk[32];
+          float part;
+          float top;
+          auto weights = [&](auto poly) {
+            const uint64_t ref2 = f32x2(__float_as_uint(-m_ref), __float_as_uint(-m_ref));
+            uint64_t sum2[2] = {0ull, 0ull};
+            float mx[2] = {neg_inf, neg_inf};
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), scale2, ref2);
+              mx[e & 1] = max3(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
+              float w0, w1;
+              if (decltype(poly)::value && e % kFPolyOf == kFPolyOf - 1) {
+                exp2_pair(x, w0, w1);
+              } else {
+                f32x2_split(x, w0, w1);
+                w0 = ex2(w0);
+                w1 = ex2(w1);
+              }
+              sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
+              pk[e] = pack2<false>(w0, w1);
+            }
+            float s0, s1;
+            f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
+            part = s0 + s1;
+            top = fmaxf(mx[0], mx[1]) * scale_log2;
+          };
+          while (true) {
+            if (edge) weights(std::false_type{});  // (weights of hidden keys are exactly zero)
+            else weights(std::true_type{});
+            if (!__any_sync(0xffffffffu, top > m_ref + kFRescale)) break;
+            const float m_new = fmaxf(m_ref, top), a = ex2(m_ref - m_new);
+            m_ref = m_new;
+            l *= a;
+            if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first run of this one
+              if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              uint32_t ov[32];
-              tmem_ld32(my_o + 32 * c, ov);
-              tmem_wait_ld();
+              for (int c = 0; c < 8; ++c) {
+                uint32_t ov[16];
+                tmem_ld16(my_o + 16 * c, ov);
+                tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
-              tmem_st32(my_o + 32 * c, ov);
+                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
+                tmem_st16(my_o + 16 * c, ov);
+              }
             }
           }
-          weights(no, no);
+          if (!ok) break;
+          l += part;
+          tmem_st32(my_s + 32 * k, pk);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cluster_tc(to_p + 8 * k);
         }
-        l += part;
-        tmem_st32(my_s + 32 * k, pk);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_cluster_tc(to_p + 8 * k);
+        if (!ok) break;
+      }
+      // ---- output
+      if (n > 0) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (t - 1) & 1));
+        tc_fence_after();
+      }
+      const bool rows_here = un.row0 + kFHalf * w + 128 * rank + (warp & 3) * 32 < un.nq;  // (warp-uniform)
+      const bool some = n > 0 && ok && l != 0.f;
+      const float inv = 1.f / l;
+      __nv_bfloat16* out = p.out + (static_cast<int64_t>(un.q0) + row - lane) * p.out_token_stride + un.h * p.out_head_stride;  // the warp's first row
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        uint32_t ov[64];
+        tmem_ld32(my_o + 64 * half, *reinterpret_cast<uint32_t(*)[32]>(&ov[0]));
+        tmem_ld32(my_o + 64 * half + 32, *reinterpret_cast<uint32_t(*)[32]>(&ov[32]));
+        tmem_wait_ld();
+        if (half == 1 && n > 0) {  // O is in registers: the next unit's products may write it
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cluster_tc(to_ofree);
+        }
+        if (rows_here) {
+          // Rows are stored 128 bytes at a time, 4 rows to an instruction, by way of shared memory, 8 rows at a time
+          // (each thread storing its own row, 32 rows to an instruction, took 3300 clocks).
+#pragma unroll
+          for (int e = 0; e < 64; e += 2)
+            ov[e >> 1] = some ? pack2<false>(__uint_as_float(ov[e]) * inv, __uint_as_float(ov[e + 1]) * inv) : 0u;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            if ((lane >> 3) == g) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (lane & 7) * 128 + ((c ^ (lane & 7)) << 4)),
+                             "r"(ov[4 * c]), "r"(ov[4 * c + 1]), "r"(ov[4 * c + 2]), "r"(ov[4 * c + 3]) : "memory");
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int r = 4 * i + (lane >> 3), c = lane & 7;  // of the 8 rows
+              uint4 x;
+              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                           : "r"(stage + r * 128 + ((c ^ r) << 4)) : "memory");
+              if (row - lane + 8 * g + r < un.nq) *reinterpret_cast<uint4*>(out + (8 * g + r) * p.out_token_stride + 64 * half + 8 * c) = x;
+            }
+            __syncwarp();
+          }
+        }
       }
       if (!ok) break;
     }
-    // ---- output
-    if (n > 0) {
-      if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (n - 1) & 1));
-      if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-      tc_fence_after();
-    }
-    if (row0 + kFHalf * w + 128 * rank + (warp & 3) * 32 < sp.nq) {  // (warp-uniform)
-      const float inv = n == 0 || !ok || l == 0.f ? 0.f : 1.f / l;
-      __nv_bfloat16* out = p.out + (static_cast<int64_t>(sp.q0) + row) * p.out_token_stride + h * p.out_head_stride;
-#pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        uint32_t ov[32];
-        tmem_ld32(my_o + 32 * c, ov);
-        tmem_wait_ld();
-        if (row < sp.nq) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint32_t o[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              o[k] = inv == 0.f ? 0u : pack2<false>(__uint_as_float(ov[e + 2 * k]) * inv, __uint_as_float(ov[e + 2 * k + 1]) * inv);
-            *reinterpret_cast<uint4*>(out + 32 * c + e) = make_uint4(o[0], o[1], o[2], o[3]);
-          }
-        }
-      }
-    }
+    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
   }
 
   // ---- teardown: neither CTA leaves while the other may still reach its barriers or tensor memory
@@ -519,7 +699,7 @@ bool latent_prefill_tc_supports(const LatentPrefillParams& p) {
     return false;
   // (row and key numbers are counted in 32 bits, up to one block behind the last)
   if (p.total_q > INT32_MAX - 1024 || p.total_k > INT32_MAX - 1024) return false;
-  return static_cast<int64_t>((p.max_q + kFRows - 1) / kFRows) * p.num_heads * p.batch <= INT32_MAX / 2;
+  return static_cast<int64_t>((p.max_q + kFRows - 1) / kFRows) * p.batch <= INT32_MAX;
 }
 
 cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t stream) {
@@ -533,8 +713,16 @@ cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t 
     return cudaErrorNotSupported;
   cudaError_t e = cudaFuncSetAttribute(latent_prefill_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFSmemBytes);
   if (e != cudaSuccess) return e;
+  // One pair of CTAs per two SMs at most; the row blocks of all sequences are at most one a sequence and one for
+  // every kFRows query tokens.
+  int dev = 0, sms = 0;
+  if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   const int q_blocks = (p.max_q + kFRows - 1) / kFRows;
-  latent_prefill_tc_kernel<<<2 * q_blocks * p.num_heads * p.batch, kFThreads, kFSmemBytes, stream>>>(maps, p, q_blocks);
+  const int64_t most = std::min(static_cast<int64_t>(p.batch) + p.total_q / kFRows, static_cast<int64_t>(p.batch) * q_blocks);
+  const FPlan plan{q_blocks, most <= kFMaxList ? 1 : 0};
+  const int64_t pairs = std::min(most * p.num_heads, static_cast<int64_t>(std::max(sms / 2, 1)));
+  latent_prefill_tc_kernel<<<static_cast<unsigned>(2 * pairs), kFThreads, kFSmemBytes, stream>>>(maps, p, plan);
   return cudaGetLastError();
 }
 
