@@ -53,15 +53,26 @@ constexpr float kFNoMax = -1e30f;
 constexpr float kFRescale = 8.f;
 constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 // 2^x for two x <= 2^7 on the FMA units, so that the exponentials are not bound by the special-function unit
 // alone: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the
 // polynomial of degree 3 whose largest relative error over [-1/2, 1/2] is least (7.5e-5, found by Remez
-// exchange; a weight's rounding to bf16 is 3.9e-3), n added to the exponent. x below -126 gives 2^-126.
+// exchange; a weight's rounding to bf16 is 3.9e-3), times 2^n built from its exponent. x below -126 gives 2^-126, a NaN
+// a NaN.
 __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
   auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
   float x0, x1;
   f32x2_split(x, x0, x1);
-  x = f32x2(__float_as_uint(fmaxf(x0, -126.f)), __float_as_uint(fmaxf(x1, -126.f)));
+  x = f32x2(__float_as_uint(max_nan(x0, -126.f)), __float_as_uint(max_nan(x1, -126.f)));
   const uint64_t t = add_f32x2(x, both(12582912.f));
   const uint64_t f = add_f32x2(x, fma_f32x2(t, both(-1.f), both(12582912.f)));
   uint64_t y = fma_f32x2(f, both(0.0551716691f), both(0.242611122f));
@@ -69,9 +80,8 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
   y = fma_f32x2(y, f, both(0.999928074f));
   float t0, t1;
   f32x2_split(t, t0, t1);
-  f32x2_split(y, w0, w1);
-  w0 = __uint_as_float(__float_as_uint(w0) + (__float_as_uint(t0) << 23));
-  w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
+  // (times 2^n, not added to the exponent field: so a NaN stays one)
+  f32x2_split(mul_f32x2(y, f32x2((__float_as_uint(t0) << 23) + 0x3f800000u, (__float_as_uint(t1) << 23) + 0x3f800000u)), w0, w1);
 }
 
 // One row block of one head, as the producer hands it to the other warps of its CTA. row0 < 0: no more.

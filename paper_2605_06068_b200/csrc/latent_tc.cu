@@ -757,10 +757,16 @@ __global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __
     return (static_cast<int64_t>(k == 0 ? rec.first_slot : 2 * (g0 + k)) * plan.per_pass + r) * N + n;
   };
   float M = -INFINITY;
-  for (int k = lane; k < rec.n_seg; k += 32) M = fmaxf(M, lse[row_of(k)]);
+  bool nan = false;  // (a maximum passes over a NaN: the row is one, not empty)
+  for (int k = lane; k < rec.n_seg; k += 32) {
+    const float x = lse[row_of(k)];
+    nan |= x != x;
+    M = fmaxf(M, x);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  const bool dead = M == -INFINITY || M == INFINITY;  // nothing to attend, or a bad page
+  nan = __any_sync(0xffffffffu, nan);
+  const bool dead = M == INFINITY || (M == -INFINITY && !nan);  // a bad page, or nothing to attend
   float4 acc[4];
 #pragma unroll
   for (int v = 0; v < 4; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);

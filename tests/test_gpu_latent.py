@@ -230,6 +230,45 @@ def test_absorbed_rising_scores():
     U.check(got, ref, tol)
 
 
+def test_absorbed_more_row_blocks_than_run_at_once():
+    run_absorbed([100, 70, 1, 230], 64, 100, 128, 64, 64, seed=31)         # 100 row blocks of 64: several rounds
+    run_absorbed([500], 128, 40, 512, 64, 16, seed=32)
+
+
+def test_absorbed_one_query_for_all_heads():
+    """Query strides of zero (a broadcast over the heads), and a head count that no copy of several heads fits."""
+    pg = U.Paged([130, 64], 64, 512, 64, 41)
+    for T, H in ((1, 12), (3, 7)):
+        ql, qr = randn(42, 2, T, 1, 512), randn(43, 2, T, 1, 64)
+        got = pda.paged_latent_attention(ql.cuda().expand(2, T, H, 512), qr.cuda().expand(2, T, H, 64), pg.cache, pg.dtable, pg.dlens, 0.07,
+                                         out=torch.empty((2, T, H, 512), dtype=torch.bfloat16, device="cuda"))
+        ref, tol = U.absorbed(ql.expand(2, T, H, 512), qr.expand(2, T, H, 64), pg.host, pg.table, [130, 64], 0.07, 512)
+        U.check(got, ref, tol)
+
+
+@pytest.mark.parametrize("lens", [[300, 90], [64, 50], [100, 4000]])
+def test_absorbed_nan_in_one_query_stays_there(lens):
+    pg = U.Paged(lens, 64, 512, 64, 44)
+    ql, qr = randn(45, 2, 1, 16, 512), randn(46, 2, 1, 16, 64)
+    ref, tol = U.absorbed(ql, qr, pg.host, pg.table, lens, 0.07, 512)
+    ql[1, 0, 3, 100] = float("nan")
+    got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 0.07).cpu()
+    assert torch.isnan(got[1, 0, 3]).all()
+    got[1, 0, 3], ref[1, 0, 3] = 0, 0
+    U.check(got, ref, tol)
+
+
+def test_absorbed_workspace_reuse_across_shapes():
+    """One workspace for calls of different shapes in a row: nothing in it outlives a call."""
+    ws = pda.latent_workspace(64, 128, 1, 512)
+    for i, (lens, H) in enumerate((([3000, 10], 128), ([900] * 40, 64), ([1] * 64, 128), ([5000], 128))):
+        pg = U.Paged(lens, 64, 512, 64, 50 + i)
+        ql, qr = randn(60 + i, len(lens), 1, H, 512), randn(70 + i, len(lens), 1, H, 64)
+        got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 0.07, workspace=ws)
+        ref, tol = U.absorbed(ql, qr, pg.host, pg.table, lens, 0.07, 512)
+        U.check(got, ref, tol, str(i))
+
+
 @pytest.mark.parametrize("flags", [0, GENERIC])
 def test_absorbed_strides_of_the_cache(flags):
     run_absorbed([100, 33, 64], 16, 1, 512, 64, 16, flags=flags, slot_pad=8, page_pad=24)
@@ -347,6 +386,85 @@ def test_expanded_peaked_and_flat_scores(spread, scale):
 
 def test_expanded_long():
     run_expanded([1500, 700], [1500, 2100], 2, seed=8)
+
+
+def test_expanded_many_sequences():
+    g = np.random.default_rng(3)
+    n = [int(x) for x in g.integers(0, 40, size=200)]                        # more than are sorted
+    run_expanded(n, [x + int(y) for x, y in zip(n, g.integers(0, 60, size=200))], 2, seed=11)
+    run_expanded([200] * 100, [200] * 100, 1, seed=12)                       # as many tokens as make more blocks than that
+    run_expanded([1] * 127 + [513], [30] * 127 + [600], 1, seed=13)
+
+
+def test_expanded_many_heads():
+    run_expanded([300, 1, 77, 520, 128], [300, 50, 77, 700, 128], 40, seed=14)   # several row blocks per pair of CTAs
+
+
+def test_expanded_unequal_halves():
+    """The two halves of a row block with 0, 1, 2 and many tiles of difference, in a row."""
+    run_expanded([600, 256, 257, 130, 512, 385], [300, 2000, 257, 1500, 100, 385], 30, seed=15)
+
+
+def test_expanded_huge_values_behind_the_mask():
+    """Later tokens' values near the largest number must not reach earlier rows."""
+    nq = 200
+    q, kv, kr = randn(1, nq, 2, 192), randn(2, nq, 2, 256), randn(3, nq, 64)
+    kv[150:, :, 128:] = 3e38
+    args = [x.cuda() for x in (q, kv, kr)]
+    for flags in (0, GENERIC):
+        got = pda.latent_prefill_attention(args[0], args[1][..., :128], args[2], args[1][..., 128:], ints([0, nq]), ints([0, nq]), nq, 0.07, flags=flags)
+        ref, tol = U.expanded(q[:150], kv[:150, :, :128], kr[:150], kv[:150, :, 128:], [0, 150], [0, 150], 0.07)
+        U.check(got[:150], ref, tol)
+
+
+@pytest.mark.parametrize("token", [0, 5, 67, 130])
+def test_expanded_nan_reaches_the_rows_that_see_it(token):
+    nq = 300
+    q, kv, kr = randn(1, nq, 2, 192), randn(2, nq, 2, 256), randn(3, nq, 64)
+    ref, tol = U.expanded(q, kv[..., :128], kr, kv[..., 128:], [0, nq], [0, nq], 0.07)
+    kv[token, 1, 17] = float("nan")
+    args = [x.cuda() for x in (q, kv, kr)]
+    for flags in (0, GENERIC):
+        got = pda.latent_prefill_attention(args[0], args[1][..., :128], args[2], args[1][..., 128:], ints([0, nq]), ints([0, nq]), nq, 0.07, flags=flags).cpu()
+        assert torch.isnan(got[token:, 1]).all()
+        U.check(got[:, 0], ref[:, 0], tol[:, 0])
+        if token:
+            U.check(got[:token, 1], ref[:token, 1], tol[:token, 1])
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_expanded_strides(flags):
+    """Queries a part of wider rows, keys, values and output with the heads outermost."""
+    lens, H = [70, 200], 3
+    T = sum(lens)
+    q, kn, kr, v = randn(1, T, H, 192), randn(2, T, H, 128), randn(3, T, 64), randn(4, T, H, 128)
+    dq = torch.cat([q, randn(5, T, H, 64)], dim=-1).cuda()[..., :192]
+    heads_out = lambda t: t.permute(1, 0, 2).contiguous().cuda().permute(1, 0, 2)
+    dkr = torch.cat([randn(6, T, 512), kr], dim=-1).cuda()[:, 512:]
+    out = torch.full((H, T, 128), -5.0, dtype=torch.bfloat16, device="cuda").permute(1, 0, 2)
+    cu = [0, 70, 270]
+    got = pda.latent_prefill_attention(dq, heads_out(kn), dkr, heads_out(v), ints(cu), ints(cu), 200, 0.07, out=out, flags=flags)
+    ref, tol = U.expanded(q, kn, kr, v, cu, cu, 0.07)
+    U.check(got, ref, tol)
+
+
+def test_expanded_repeats_bit_for_bit_in_a_graph_and_on_other_streams():
+    dq, dkv, dkr, first = run_expanded([300, 40, 700], [300, 90, 900], 8, seed=16)
+    cq, ck = ints([0, 300, 340, 1040]), ints([0, 300, 390, 1290])
+    call = lambda out, **kw: pda.latent_prefill_attention(dq, dkv[..., :128], dkr, dkv[..., 128:], cq, ck, 700, 1.0 / np.sqrt(192.0), out=out, **kw)
+    s, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [torch.zeros_like(first) for _ in range(3)]
+    torch.cuda.synchronize()
+    call(outs[0], stream=s)
+    call(outs[1], stream=s2)                        # two at once
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[2])
+    graph.replay()
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o, first)
 
 
 @pytest.mark.parametrize("flags", [0, GENERIC])
