@@ -581,24 +581,37 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
     dv, dr = v.shape[2], D - dn
     if out is None:
         out = torch.empty((tq, H, dv), dtype=q.dtype, device=q.device)
-    for name, t, shape in (("q", q, (tq, H, D)), ("k_nope", k_nope, (tk, H, dn)), ("v", v, (tk, H, dv)), ("out", out, (tq, H, dv)),
-                           ("k_rope", k_rope if dr else None, (tk, dr))):
-        if t is not None:
-            _bf16_rows(name, t)
-            if tuple(t.shape) != shape:
-                raise ValueError(f"{name}: expected {shape}")
+    _bf16_rows("q", q)
+    _bf16_rows("k_nope", k_nope)
+    _bf16_rows("v", v)
+    _bf16_rows("out", out)
+    if k_nope.shape[1] != H or v.shape[:2] != k_nope.shape[:2]:
+        raise ValueError("k_nope and v: expected [key tokens, heads, dim]")
+    if out.shape != (tq, H, dv):
+        raise ValueError("out: expected [query tokens, heads, value dim]")
+    kr_token = 0
+    if dr:
+        _bf16_rows("k_rope", k_rope)
+        if k_rope.shape != (tk, dr):
+            raise ValueError("k_rope: expected [key tokens, rope_dim]")
+        kr_token = k_rope.stride(0) if tk > 1 else 0
+    else:
+        k_rope = None
     _int32(cu_q, cu_k, status)
-    if cu_q.numel() != cu_k.numel() or cu_q.numel() < 1:
+    n = cu_q.numel()
+    if n != cu_k.numel() or n < 1:
         raise ValueError("cu_q and cu_k: expected batch + 1 entries each")
-    dev = _same_device(q, k_nope, k_rope if dr else None, v, out, cu_q, cu_k, status)
+    dev = _same_device(q, k_nope, k_rope, v, out, cu_q, cu_k, status)
 
-    def st(t, i):
-        return t.stride(i) if t.shape[i] > 1 else 0
+    def st(t, tokens):  # (a dimension of extent 1 may carry any stride)
+        token, head, _ = t.stride()
+        return token if tokens > 1 else 0, head if H > 1 else 0
 
     with _device_call(dev):
         rc = lib().latent_prefill_attention(
-            _dp(q), st(q, 0), st(q, 1), _dp(k_nope), st(k_nope, 0), st(k_nope, 1), _dp(k_rope) if dr else None,
-            st(k_rope, 0) if dr else 0, _dp(v), st(v, 0), st(v, 1), _dp(cu_q), _dp(cu_k), cu_q.numel() - 1, H, dn, dr, dv,
-            int(max_q), tq, tk, float(scale), _dp(out), st(out, 0), st(out, 1), flags, _dp(status), _raw(stream, dev))
-    _check(rc, "latent_prefill_attention")
+            q.data_ptr(), *st(q, tq), k_nope.data_ptr(), *st(k_nope, tk), _dp(k_rope), kr_token, v.data_ptr(), *st(v, tk),
+            cu_q.data_ptr(), cu_k.data_ptr(), n - 1, H, dn, dr, dv, int(max_q), tq, tk, scale, out.data_ptr(), *st(out, tq),
+            flags, _dp(status), _raw(stream, dev))
+    if rc:
+        _check(rc, "latent_prefill_attention")
     return out

@@ -1,6 +1,6 @@
 // paged_build_tables: block-table rows, slot map, positions and cumulative token counts of one step.
 // Integer work on a few hundred lengths, so the time is launch and latency: one launch, in which every CTA
-// scans all lengths by itself (1024 at a time, one per thread) and then writes its own share of the new
+// scans all lengths by itself (256 or 1024 at a time, one per thread) and then writes its own share of the new
 // pages and of the tokens. Nothing is handed from CTA to CTA: a page id is taken from the free list (or,
 // for pages that were there before, from the table's untouched part), never read back from what another
 // CTA writes. The order of pages and tokens is that of the scan, so results do not depend on timing.
@@ -10,8 +10,7 @@ namespace pda {
 
 namespace {
 
-constexpr int kTabThreads = 1024;       // sequences per scan step
-constexpr int kTabTokensPerCta = 2048;  // token entries a CTA writes
+constexpr int kTabTokensPerThread = 2;  // token entries a CTA writes
 
 struct SeqStep {
   int held, take, start, n;  // pages before, pages taken, position of the first new token, new tokens
@@ -34,28 +33,28 @@ __device__ __forceinline__ SeqStep load_step(const TablesParams& p, int b) {
   return s;
 }
 
-// Exclusive scan of two counters over the CTA; `tot` receives the sums. scratch: 2 x 32.
-__device__ __forceinline__ void block_scan2(int64_t a, int64_t b, int64_t& ea, int64_t& eb, int64_t& tot_a, int64_t& tot_b,
-                                            int64_t (*scratch)[32]) {
+// Exclusive scan of two counters over the CTA of kWarps warps; `tot` receives the sums.
+template <int kWarps, class Acc>
+__device__ __forceinline__ void block_scan2(Acc a, Acc b, Acc& ea, Acc& eb, Acc& tot_a, Acc& tot_b, Acc (*scratch)[kWarps]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t ia = a, ib = b;
+  Acc ia = a, ib = b;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t ua = __shfl_up_sync(0xffffffffu, ia, o), ub = __shfl_up_sync(0xffffffffu, ib, o);
+    const Acc ua = __shfl_up_sync(0xffffffffu, ia, o), ub = __shfl_up_sync(0xffffffffu, ib, o);
     if (lane >= o) { ia += ua; ib += ub; }
   }
   __syncthreads();  // (scratch may still be read by the previous step)
   if (lane == 31) { scratch[0][warp] = ia; scratch[1][warp] = ib; }
   __syncthreads();
-  int64_t wa = scratch[0][lane], wb = scratch[1][lane];
+  Acc wa = lane < kWarps ? scratch[0][lane] : 0, wb = lane < kWarps ? scratch[1][lane] : 0;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t ua = __shfl_up_sync(0xffffffffu, wa, o), ub = __shfl_up_sync(0xffffffffu, wb, o);
+  for (int o = 1; o < kWarps; o <<= 1) {
+    const Acc ua = __shfl_up_sync(0xffffffffu, wa, o), ub = __shfl_up_sync(0xffffffffu, wb, o);
     if (lane >= o) { wa += ua; wb += ub; }
   }
-  tot_a = __shfl_sync(0xffffffffu, wa, 31);
-  tot_b = __shfl_sync(0xffffffffu, wb, 31);
-  const int64_t ba = __shfl_sync(0xffffffffu, wa, (warp + 31) & 31), bb = __shfl_sync(0xffffffffu, wb, (warp + 31) & 31);
+  tot_a = __shfl_sync(0xffffffffu, wa, kWarps - 1);
+  tot_b = __shfl_sync(0xffffffffu, wb, kWarps - 1);
+  const Acc ba = __shfl_sync(0xffffffffu, wa, (warp + 31) & 31), bb = __shfl_sync(0xffffffffu, wb, (warp + 31) & 31);
   ea = ia - a + (warp ? ba : 0);
   eb = ib - b + (warp ? bb : 0);
 }
@@ -77,9 +76,12 @@ __device__ __forceinline__ int find(const int32_t* a, int n, int x) {
 
 // write_count: this launch stores free_count_out (it is another address than free_count, or no other CTA
 // reads free_count). count_only: nothing but free_count_out is written.
+// kThreads: sequences per scan step. Acc: 32 bits where no sum of lengths can pass them.
+template <int kTabThreads, class Acc>
 __global__ void __launch_bounds__(kTabThreads)
 build_tables_kernel(TablesParams p, bool write_count, bool count_only) {
-  __shared__ int64_t scratch[2][32];
+  constexpr int kTabTokensPerCta = kTabTokensPerThread * kTabThreads;
+  __shared__ Acc scratch[2][kTabThreads / 32];
   __shared__ int32_t cu_s[kTabThreads + 1], tk_s[kTabThreads + 1], start_s[kTabThreads], held_s[kTabThreads];
   const int tid = threadIdx.x;
   const int count = p.free_count[0];
@@ -87,13 +89,14 @@ build_tables_kernel(TablesParams p, bool write_count, bool count_only) {
 
   // totals first: either every page that the step needs can be had, or none is taken
   SeqStep s{};
-  int64_t en = 0, et = 0, tot_n = 0, tot_t = 0;
+  Acc en = 0, et = 0;
+  int64_t tot_n = 0, tot_t = 0;
   bool any_bad = false;
   for (int b0 = 0; b0 < p.batch; b0 += kTabThreads) {
     s = load_step(p, b0 + tid);
     any_bad |= s.bad;
-    int64_t cn, ct;
-    block_scan2(s.n, s.take, en, et, cn, ct, scratch);
+    Acc cn, ct;
+    block_scan2<kTabThreads / 32, Acc>(s.n, s.take, en, et, cn, ct, scratch);
     tot_n += cn;
     tot_t += ct;
   }
@@ -114,7 +117,10 @@ build_tables_kernel(TablesParams p, bool write_count, bool count_only) {
     int64_t cn = tot_n, ct = tot_t;
     if (p.batch > kTabThreads) {
       s = load_step(p, b0 + tid);
-      block_scan2(s.n, s.take, en, et, cn, ct, scratch);
+      Acc sum_n, sum_t;
+      block_scan2<kTabThreads / 32, Acc>(s.n, s.take, en, et, sum_n, sum_t, scratch);
+      cn = sum_n;
+      ct = sum_t;
     }
     if (blockIdx.x == 0 && b0 + tid < p.batch) {
       p.cu_new[b0 + tid] = clamp_i32(base_n + en);
@@ -166,15 +172,26 @@ build_tables_kernel(TablesParams p, bool write_count, bool count_only) {
 
 }  // namespace
 
-cudaError_t launch_build_tables(const TablesParams& p, cudaStream_t stream) {
-  int64_t ctas = (static_cast<int64_t>(p.capacity) + kTabTokensPerCta - 1) / kTabTokensPerCta;
+namespace {
+template <int kThreads, class Acc>
+cudaError_t launch(const TablesParams& p, cudaStream_t stream) {
+  constexpr int kTokens = kTabTokensPerThread * kThreads;
+  int64_t ctas = (static_cast<int64_t>(p.capacity) + kTokens - 1) / kTokens;
   if (ctas < 1) ctas = 1;
   // In place (free_count_out == free_count) with several CTAs: the new count is stored by a second launch,
   // after every CTA of the first has read the old one.
   const bool in_place = p.free_count == p.free_count_out && ctas > 1;
-  build_tables_kernel<<<static_cast<unsigned>(ctas), kTabThreads, 0, stream>>>(p, !in_place, false);
-  if (in_place) build_tables_kernel<<<1, kTabThreads, 0, stream>>>(p, true, true);
+  build_tables_kernel<kThreads, Acc><<<static_cast<unsigned>(ctas), kThreads, 0, stream>>>(p, !in_place, false);
+  if (in_place) build_tables_kernel<kThreads, Acc><<<1, kThreads, 0, stream>>>(p, true, true);
   return cudaGetLastError();
+}
+}  // namespace
+
+// Up to 256 sequences fit a CTA of 256 threads, whose scan has two levels of 8 instead of 32.
+cudaError_t launch_build_tables(const TablesParams& p, cudaStream_t stream) {
+  const bool small_sums = static_cast<int64_t>(p.batch) * p.block_table_stride <= INT32_MAX / p.page_size;
+  if (p.batch <= 256) return small_sums ? launch<256, int32_t>(p, stream) : launch<256, int64_t>(p, stream);
+  return small_sums ? launch<1024, int32_t>(p, stream) : launch<1024, int64_t>(p, stream);
 }
 
 }  // namespace pda
