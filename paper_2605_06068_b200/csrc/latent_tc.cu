@@ -50,7 +50,6 @@ constexpr int kLProducer = 8, kLSIssue = 9, kLPvIssue = 10, kLQLoad = 11, kLProd
 constexpr uint32_t kLTmemCols = 512, kLTmemS = 256;  // O^T: R / 128 blocks of N columns from 0; S^T from 256
 constexpr float kLNoMax = -1e30f;               // reference of a row that has seen no score yet
 constexpr float kLRescale = 8.f;                // log2
-constexpr int kLMinSpan = 2;                    // tiles: below this a span costs more than it shortens
 
 template <int N>
 struct LCfg {
@@ -67,6 +66,7 @@ static_assert(LCfg<64>::kSmemBytes <= 232448 && LCfg<32>::kSmemBytes <= 232448, 
 struct LPlan {
   int32_t row_blocks, per_pass, passes, groups;  // row blocks per sequence; taken at once; rounds; CTA groups
   int32_t page_shift;                            // log2 of the page size
+  int32_t by_sequence;                           // records are indexed by sequence (there are fewer than groups)
   int32_t q_box;                                 // heads per copy of Q (0: rows by plain copies)
 };
 
@@ -75,8 +75,10 @@ struct LMaps {
   CUtensorMap q_latent, q_rope;  // one line of q_box heads of a token
 };
 
-struct LRecord {  // a sequence whose first span is this one and that continues: see latent_merge_kernel
-  int32_t vseq, first_slot, n_seg, pad;
+// A sequence that continues behind its first span: see latent_merge_kernel. One per group (the sequence that
+// leaves its span), or one per sequence where those are fewer. vseq < 0: none.
+struct LRecord {
+  int32_t vseq, first_slot, n_seg, group;
 };
 
 __device__ __forceinline__ int seq_tokens(const LatentParams& p, int b) {
@@ -257,7 +259,12 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   }
   before += incl - mine;
   const uint32_t total = list * plan.passes;
-  const int span_tiles = max(static_cast<int>((total + plan.groups - 1) / plan.groups), kLMinSpan);
+  // Equal spans, but of at least two tiles where sequences have at most two (a merge costs more than a tile: 100
+  // tokens 10.2 instead of 11.4 us) or more than 32 (so many parts of one sequence cost more to merge: 8000 tokens,
+  // 16 heads 16.7 instead of 20.0 us); in between single tiles are faster (8 x 700 tokens, 32 heads: 14.0, else 18.3 us).
+  const uint32_t sequences = static_cast<uint32_t>(p.batch);
+  const int span_tiles = max(static_cast<int>((total + plan.groups - 1) / plan.groups),
+                             list <= 2 * sequences || list > 32 * sequences ? 2 : 1);
   const int64_t start = static_cast<int64_t>(g) * span_tiles;
   if (start < total && !dead) {
     const uint32_t pass = static_cast<uint32_t>(start) / list, in_pass = static_cast<uint32_t>(start) - pass * list;
@@ -494,14 +501,18 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
     const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
     const int rows_total = p.n_q * p.num_q_heads;
     LRecord rec{-1, 0, 0, 0};
+    LRecord* records = reinterpret_cast<LRecord*>(ws + lay.records);
     int i = 0;
     bool first_in_span = true;
     while (next_segment<N>(p, plan, r, walk, s)) {
       const bool at_start = first_in_span;
       first_in_span = false;
       const bool is_first = s.off == 0, is_last = s.off + s.take == s.whole;
-      if (is_first && !is_last)
-        rec = LRecord{s.vseq, 2 * g + (at_start ? 0 : 1), 1 + (s.whole - s.take - 1) / span_tiles + 1, 0};
+      if (is_first) {
+        const LRecord now{is_last ? -1 : s.vseq, 2 * g + (at_start ? 0 : 1), 1 + (s.whole - s.take - 1) / span_tiles + 1, g};
+        if (!is_last) rec = now;
+        if (plan.by_sequence && r == 0 && tid == 0) records[s.vseq] = now;
+      }
       if (s.rb < 0) continue;
       const bool partial = !(is_first && is_last);
       const int slot = 2 * g + (at_start ? 0 : 1);
@@ -714,7 +725,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
       soft_sync();  // (row_off and inv_l are free again)
     }
     if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-    if (r == 0 && tid == 0) reinterpret_cast<LRecord*>(ws + lay.records)[g] = rec;
+    if (r == 0 && tid == 0 && (!plan.by_sequence || (dead && g < p.batch * plan.passes))) records[g] = rec;
   }
 
   // ---- teardown
@@ -729,13 +740,14 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   }
 }
 
-// Rows of the sequences that lie in several spans. Grid: (span, row block, rows). kWide: a CTA per row, its
+// Rows of the sequences that lie in several spans. Grid: (record, row block, rows). kWide: a CTA per row, its
 // warps sharing the row's segments (few sequences, each over many spans); else a warp per row (many
 // sequences over two or three spans: a quarter of the CTAs).
-constexpr int kMergeWarps = 4;
+constexpr int kMergeRows = 4, kMergeWideWarps = 8;
 template <int N, bool kWide>
-__global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __grid_constant__ LatentParams p,
+__global__ void __launch_bounds__(kWide ? kMergeWideWarps * 32 : kMergeRows * 32) latent_merge_kernel(const __grid_constant__ LatentParams p,
                                                                         const __grid_constant__ LPlan plan) {
+  constexpr int kMergeWarps = kWide ? kMergeWideWarps : kMergeRows;
   __shared__ float4 acc_sh[kWide ? kMergeWarps - 1 : 1][kWide ? 128 : 1];
   __shared__ float w_sh[kMergeWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -752,16 +764,29 @@ __global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __
   const int vecs = p.geom.latent_dim / 4;  // 16-byte vectors of a partial row, a multiple of 32
   const float* lse = reinterpret_cast<const float*>(ws + lay.part_lse);
   const float4* part = reinterpret_cast<const float4*>(ws + lay.part_o);
-  const int g0 = blockIdx.x;
+  const int g0 = rec.group;
   auto row_of = [&](int k) -> int64_t {  // row of the k-th segment: later spans hold theirs in their first slot
     return (static_cast<int64_t>(k == 0 ? rec.first_slot : 2 * (g0 + k)) * plan.per_pass + r) * N + n;
   };
-  float M = -INFINITY;
-  bool nan = false;  // (a maximum passes over a NaN: the row is one, not empty)
+  // The first segments' rows are asked for before the weights are known: the trips to L2 are what this kernel
+  // spends its time on.
+  constexpr int kStep = kWide ? kMergeWarps : 1, kAhead = 2;
+  const int k0 = kWide ? warp : 0;
+  float4 x[kAhead][4];
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) {
+    const int k = k0 + a * kStep;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      if (k < rec.n_seg && v * 32 < vecs) x[a][v] = part[row_of(k) * vecs + v * 32 + lane];
+  }
+  float M = -INFINITY, mine = -INFINITY;  // (mine: the lane-th segment's)
+  bool nan = false;                       // (a maximum passes over a NaN: the row is one, not empty)
   for (int k = lane; k < rec.n_seg; k += 32) {
-    const float x = lse[row_of(k)];
-    nan |= x != x;
-    M = fmaxf(M, x);
+    const float y = lse[row_of(k)];
+    if (k == lane) mine = y;
+    nan |= y != y;
+    M = fmaxf(M, y);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
@@ -771,20 +796,28 @@ __global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __
 #pragma unroll
   for (int v = 0; v < 4; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
   float W = 0.f;
-  if (!dead) {
-#pragma unroll 4
-    for (int k = kWide ? warp : 0; k < rec.n_seg; k += kWide ? kMergeWarps : 1) {
-      const int64_t at = row_of(k);
-      const float w = ex2(lse[at] - M);
-      W += w;
+  auto add = [&](float w, const float4 (&y)[4]) {
+    W += w;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (v * 32 < vecs) {
-          const float4 x = part[at * vecs + v * 32 + lane];
-          acc[v].x = fmaf(w, x.x, acc[v].x); acc[v].y = fmaf(w, x.y, acc[v].y);
-          acc[v].z = fmaf(w, x.z, acc[v].z); acc[v].w = fmaf(w, x.w, acc[v].w);
-        }
+    for (int v = 0; v < 4; ++v) {
+      if (v * 32 < vecs) {
+        acc[v].x = fmaf(w, y[v].x, acc[v].x); acc[v].y = fmaf(w, y[v].y, acc[v].y);
+        acc[v].z = fmaf(w, y[v].z, acc[v].z); acc[v].w = fmaf(w, y[v].w, acc[v].w);
       }
+    }
+  };
+  if (!dead) {  // (the whole warp)
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+      if (k0 + a * kStep < rec.n_seg) add(ex2(__shfl_sync(0xffffffffu, mine, k0 + a * kStep) - M), x[a]);
+#pragma unroll 4
+    for (int k = k0 + kAhead * kStep; k < rec.n_seg; k += kStep) {
+      const int64_t at = row_of(k);
+      float4 y[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (v * 32 < vecs) y[v] = part[at * vecs + v * 32 + lane];
+      add(ex2(lse[at] - M), y);
     }
   }
   if constexpr (kWide) {  // warp 0 adds the warps' sums, in their order
@@ -819,7 +852,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) latent_merge_kernel(const __
 // How many row blocks run at once, and how often: the choice that keeps most CTAs busy, for at most 37
 // row blocks at once (four groups of CTAs), fewer rounds first.
 LPlan make_plan(int row_blocks, int ctas) {
-  LPlan best{row_blocks, 1, row_blocks, ctas, 0, 0};
+  LPlan best{row_blocks, 1, row_blocks, ctas, 0, 0, 0};
   double best_eff = -1.0;
   for (int passes = 1; passes <= row_blocks; ++passes) {
     const int per = (row_blocks + passes - 1) / passes;
@@ -828,7 +861,7 @@ LPlan make_plan(int row_blocks, int ctas) {
     const double eff = static_cast<double>(row_blocks) / (static_cast<double>(passes) * per) * groups * per / ctas;
     if (eff > best_eff + 0.02) {
       best_eff = eff;
-      best = LPlan{row_blocks, per, passes, groups, 0, 0};
+      best = LPlan{row_blocks, per, passes, groups, 0, 0, 0};
     }
     if (per == 1) break;
   }
@@ -886,6 +919,7 @@ template <int N>
 cudaError_t launch_n(EncodeFn enc, LMaps& maps, const LatentParams& p, int sms, cudaStream_t stream) {
   const int rows = p.n_q * p.num_q_heads;
   LPlan plan = make_plan((rows + N - 1) / N, sms < kLatMaxCtas ? sms : kLatMaxCtas);
+  plan.by_sequence = static_cast<int64_t>(p.batch) * plan.passes <= plan.groups;
   plan.page_shift = __builtin_ctz(p.geom.page_size);
   plan.q_box = q_box_of(p, N);
   if (plan.q_box > 0) {
@@ -902,8 +936,9 @@ cudaError_t launch_n(EncodeFn enc, LMaps& maps, const LatentParams& p, int sms, 
   OverlapConfig attention(dim3(plan.groups * plan.per_pass), kLThreads, LCfg<N>::kSmemBytes, stream);
   if ((e = cudaLaunchKernelEx(&attention.cfg, latent_tc_kernel<N>, maps, p, plan)) != cudaSuccess) return e;
   // (the spans cut at most groups - 1 sequences: with few sequences those have many segments each)
-  const bool wide = static_cast<int64_t>(p.batch) * plan.passes * 4 <= plan.groups;
-  OverlapConfig merge(dim3(plan.groups, plan.per_pass, wide ? N : N / kMergeWarps), kMergeWarps * 32, 0, stream);
+  const int64_t sequences = static_cast<int64_t>(p.batch) * plan.passes;
+  const bool wide = sequences * 4 <= plan.groups;
+  OverlapConfig merge(dim3(plan.by_sequence ? static_cast<unsigned>(sequences) : plan.groups, plan.per_pass, wide ? N : N / kMergeRows), 32 * (wide ? kMergeWideWarps : kMergeRows), 0, stream);
   return wide ? cudaLaunchKernelEx(&merge.cfg, latent_merge_kernel<N, true>, p, plan)
               : cudaLaunchKernelEx(&merge.cfg, latent_merge_kernel<N, false>, p, plan);
 }
