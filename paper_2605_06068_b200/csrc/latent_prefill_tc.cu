@@ -18,6 +18,9 @@
 // 32-bit weights; the rounding of the weights to bf16 is 2^-8 of each.
 // Each pair of CTAs works through several row blocks, those with the most keys first and dealt to and fro; the
 // producer runs on into the next block's Q, K and V while the last one's output is written.
+// Measured (B200): a prompt of 8192 tokens with 32 heads 0.66 ms, 1.04 PFLOP/s, 3800 clocks a tile: a half's chain of
+// S, weights (2100), P . V and the next S, of which the other half covers the most; the clock is held at 1.58 GHz
+// by the power cap. 24 prompts of 1..700 tokens with 16 heads: 80 us.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the
 // pair's first CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are
 // bounded.

@@ -24,6 +24,11 @@
 // most 2^8, and relative to their row's sum the rounding is 2^-8 whatever the reference); sums, scores and
 // O are 32-bit.
 //
+// Measured (B200, 512 + 64, pages of 64): 64 sequences of 512..4096 tokens, 16 heads, 41 us a call in a graph (floor from
+// HBM 27), the tiles in the middle at 5.9 TB/s; 128 such sequences with 128 heads 150 us, 2900 clocks a tile,
+// of which the MMAs keep shared memory busy for 2000 (they read A for 64 columns only: 33 clocks an MMA of S, 49 of O) and the
+// tile's arrival for 600: with 64 rows that is the bound, with 16 or 32 it is HBM.
+//
 // Warps: 0-7 softmax and output, 8 and 12 TMA producers, 9 S issue + TMEM, 10 P . C issue, 11 Q rows. All waits are
 // bounded; on a timeout every role leaves its loop, outstanding copies and products are waited for (with a
 // limit) and tensor memory is released.
