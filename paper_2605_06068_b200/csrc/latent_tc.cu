@@ -458,6 +458,17 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         const uint32_t leader = elect_one();
         const int live = min(N, p.n_q * p.num_q_heads - s.rb * N);
         const int runs = (live + plan.q_box - 1) / plan.q_box, lines = 2 * m_tiles + 1;
+        if (runs * plan.q_box < N) {
+          // rows that there are not are zero: what an earlier segment left there would have its say in when the
+          // references are raised, and so in the other rows' rounding
+          const int first = runs * plan.q_box;
+          for (int k = lane; k < lines * (N - first) * 8; k += 32) {
+            const int ln = k / ((N - first) * 8), at = k - ln * (N - first) * 8;
+            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(q_to + ln * (N * 128) + first * 128 + at * 16), "r"(0) : "memory");
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
         mbar_expect_tx_if(leader, bar_qb, uniform(runs * plan.q_box * lines * 128));
         for (int k = 0; k < runs; ++k) {
           const int row = s.rb * N + k * plan.q_box;

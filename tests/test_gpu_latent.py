@@ -300,6 +300,19 @@ def test_absorbed_bad_pages_and_lengths(flags):
         U.check(got, r, o, f"length {L}")
 
 
+def test_absorbed_rows_that_are_not_there_do_not_matter():
+    """112 rows in two blocks of 64: what earlier segments left behind the last row must not change the others'
+    rounding. (Many sequences per CTA, the same call over and over between calls that leave other things behind.)"""
+    lens = [int(x) for x in np.random.default_rng(4).integers(0, 1500, size=17)]
+    pg, ql, qr, ws, first = run_absorbed(lens, 16, 7, 512, 64, 32, seed=61)
+    first = first.clone()
+    other, oql, oqr, ows, _ = run_absorbed([900] * 40, 64, 1, 512, 64, 64, seed=62, spread=20.0)
+    for _ in range(10):
+        pda.paged_latent_attention(oql, oqr, other.cache, other.dtable, other.dlens, 0.3, workspace=ows)
+        got = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 1.0 / np.sqrt(192.0), workspace=ws)
+        assert torch.equal(got, first)
+
+
 def test_absorbed_repeats_bit_for_bit_and_other_streams():
     pg, ql, qr, ws, first = run_absorbed([900, 77, 2500, 64], 32, 1, 512, 64, 64, seed=21)
     first = first.clone()
