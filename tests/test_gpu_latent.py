@@ -65,6 +65,23 @@ def test_tables_many(B, in_place):
     run_tables(L, np.minimum(n, L), 16, pad=int(g.integers(0, 5000)), in_place=in_place, seed=B)
 
 
+def test_tables_sums_beyond_32_bits_of_room():
+    """A table whose rows have room for more tokens than 32 bits count (the sums are then kept in 64)."""
+    B, stride = 40, 1 << 22
+    table = torch.full((B, stride), -7, dtype=torch.int32, device="cuda")
+    L, n = [5 + b for b in range(B)], [1 + b % 3 for b in range(B)]
+    free = list(range(500, 600))
+    held = [-(-(a - b) // 16) for a, b in zip(L, n)]
+    host = np.full((B, 8), -7, dtype=np.int32)
+    for b in range(B):
+        host[b, :held[b]] = 3 * b + np.arange(held[b])
+    table[:, :8] = ints(host)
+    cu, slots, cnt = ints([0] * (B + 1)), ints([0] * (sum(n) + 2)), ints([100])
+    pda.paged_build_tables(ints(L), ints(n), 16, ints(free), cnt, table, cu, slots)
+    rt, rcu, rs, _, rc = U.tables(L, n, 16, free, 100, host, sum(n) + 2)
+    assert (table[:, :8].cpu().numpy() == rt).all() and cu.tolist() == rcu and slots.tolist() == rs and cnt.item() == rc
+
+
 def test_tables_refuse_on_the_device():
     P, free = 16, list(range(100, 110))
 
@@ -599,3 +616,54 @@ def test_step_in_a_graph():
         assert lens.tolist() == now and status.item() == 0
         ref, tol = U.absorbed(hq, hr, pg.cache.cpu(), table.cpu().numpy(), now, 0.07, R)
         U.check(out, ref, tol, f"replay {i}")
+
+
+def test_calls_on_several_streams_at_once():
+    """Both forms, the append and the tables on four streams at the same time, each with buffers of its own."""
+    jobs = []
+    for i, (lens, H) in enumerate((([2000, 5, 700], 128), ([300] * 50, 16), ([9000], 32))):
+        pg = U.Paged(lens, 64, 512, 64, 80 + i)
+        ql, qr = randn(83 + i, len(lens), 1, H, 512).cuda(), randn(86 + i, len(lens), 1, H, 64).cuda()
+        ws, out = pda.latent_workspace(len(lens), H, 1, 512), torch.zeros_like(ql)
+        jobs.append((lambda s, pg=pg, ql=ql, qr=qr, ws=ws, out=out: pda.paged_latent_attention(
+            ql, qr, pg.cache, pg.dtable, pg.dlens, 0.07, out=out, workspace=ws, stream=s), out))
+    q, kv, kr = randn(90, 900, 16, 192).cuda(), randn(91, 900, 16, 256).cuda(), randn(92, 900, 64).cuda()
+    cu, out = ints([0, 600, 900]), torch.zeros((900, 16, 128), dtype=torch.bfloat16, device="cuda")
+    jobs.append((lambda s: pda.latent_prefill_attention(q, kv[..., :128], kr, kv[..., 128:], cu, cu, 600, 0.07, out=out, stream=s), out))
+    want = []
+    for call, o in jobs:
+        call(None)
+        torch.cuda.synchronize()
+        want.append(o.clone())
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(15):
+        for (_, o), s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                o.zero_()
+        for (call, _), s in zip(jobs, streams):
+            call(s)
+    torch.cuda.synchronize()
+    for (_, o), w in zip(jobs, want):
+        assert torch.equal(o, w)
+
+
+def test_two_graphs_replayed_side_by_side():
+    """Two captured calls with a workspace each, replayed on two streams."""
+    pg, ql, qr, ws, first = run_absorbed([3000, 100], 64, 1, 512, 64, 64, seed=95)
+    first = first.clone()
+    graphs, outs = [], []
+    for _ in range(2):
+        w, o, g = pda.latent_workspace(2, 64, 1, 512), torch.zeros_like(first), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 1.0 / np.sqrt(192.0), out=o, workspace=w)
+        graphs.append((g, w))
+        outs.append(o)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for (g, _), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o, first)
