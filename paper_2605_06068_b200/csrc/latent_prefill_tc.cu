@@ -43,8 +43,7 @@ constexpr int kFKLine = 64 * 128, kFKBytes = 3 * kFKLine;  // of its 64 keys
 constexpr int kFVBytes = kFKeys * 128;                    // its line (64 dims) of all keys
 constexpr int kFStages = 3;                               // tiles
 constexpr int kFSoftWarps = 8, kFThreads = (kFSoftWarps + 4) * 32, kFProducer = 8, kFMma = 9, kFRelay = 11;  // (9, 10: one per half)
-constexpr int kFOutBytes = 1024;                          // per softmax warp: 8 rows of 64 dims on their way out
-constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 2048 + kFSoftWarps * kFOutBytes + 1024;
+constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 2048 + 1024;
 static_assert(kFSmemBytes <= 232448, "shared memory");
 // 384 threads start with 168 registers (64512 in all); the control warps keep 104 and the softmax warps take 200
 constexpr uint32_t kFRegsSoftmax = 200, kFRegsControl = 104;
@@ -56,26 +55,21 @@ constexpr float kFNoMax = -1e30f;
 constexpr float kFRescale = 8.f;
 constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
 
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {  // NaN if any is
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
 }
 // 2^x for two x <= 2^7 on the FMA units, so that the exponentials are not bound by the special-function unit
 // alone: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the
 // polynomial of degree 3 whose largest relative error over [-1/2, 1/2] is least (7.5e-5, found by Remez
-// exchange; a weight's rounding to bf16 is 3.9e-3), times 2^n built from its exponent. x below -126 gives 2^-126, a NaN
-// a NaN.
+// exchange; a weight's rounding to bf16 is 3.9e-3), n added to the exponent. x below -126 gives 2^-126, and so
+// does a NaN: that is looked for in the scores' maximum.
 __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
   auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
   float x0, x1;
   f32x2_split(x, x0, x1);
-  x = f32x2(__float_as_uint(max_nan(x0, -126.f)), __float_as_uint(max_nan(x1, -126.f)));
+  x = f32x2(__float_as_uint(fmaxf(x0, -126.f)), __float_as_uint(fmaxf(x1, -126.f)));
   const uint64_t t = add_f32x2(x, both(12582912.f));
   const uint64_t f = add_f32x2(x, fma_f32x2(t, both(-1.f), both(12582912.f)));
   uint64_t y = fma_f32x2(f, both(0.0551716691f), both(0.242611122f));
@@ -83,14 +77,24 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
   y = fma_f32x2(y, f, both(0.999928074f));
   float t0, t1;
   f32x2_split(t, t0, t1);
-  // (times 2^n, not added to the exponent field: so a NaN stays one)
-  f32x2_split(mul_f32x2(y, f32x2((__float_as_uint(t0) << 23) + 0x3f800000u, (__float_as_uint(t1) << 23) + 0x3f800000u)), w0, w1);
+  f32x2_split(y, w0, w1);
+  w0 = __uint_as_float(__float_as_uint(w0) + (__float_as_uint(t0) << 23));
+  w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
 }
 
 // One row block of one head, as the producer hands it to the other warps of its CTA. row0 < 0: no more.
+// dual: the block has at most kFHalf rows, and the second half takes the same rows of the next head (with tiles of its
+// own: the pair's tiles are then this head's and that head's by turns).
 struct FUnit {
-  int row0, h, q0, nq, nq_all, k0, nk, n0, n1;
+  int row0, h, q0, nq, nq_all, k0, nk, n0, n1, dual;
+  __device__ int first_row(int w) const { return row0 + (dual ? 0 : kFHalf * w); }
+  __device__ int head(int w) const { return h + (dual ? w : 0); }
+  __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
 };
+constexpr uint32_t kFSmallBlock = 1u << 30;  // (in a list entry) at most kFHalf rows
+__device__ __forceinline__ int units_of(uint32_t entry, int num_heads, bool by_two) {
+  return by_two && (entry & kFSmallBlock) ? (num_heads + 1) / 2 : num_heads;
+}
 struct FPlan {
   int q_blocks;  // blocks of max_q
   int listed;    // the row blocks of all sequences are few enough to be listed and sorted in shared memory
@@ -166,7 +170,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes));
   FUnit* units = reinterpret_cast<FUnit*>(bars + 48);               // [kFUnitSlots]
   uint32_t* list = reinterpret_cast<uint32_t*>(units + kFUnitSlots);  // [kFMaxList] sequence and block, most work first
-  uint32_t* work = list + kFMaxList;                                // [kFMaxList] (start of the kernel only)
+  uint32_t* work = list + kFMaxList;                                // [kFMaxList] keys, then units of the entries before
   uint32_t* scan = work + kFMaxList;                                // [5] sequences' blocks, by warp; their sum
   uint32_t* tmem_slot = scan + 5;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
@@ -244,6 +248,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
   __syncthreads();
   int n_blocks = 0;
   uint32_t my_work = 0, my_entry = 0;
+  bool by_two = true;  // heads two by two on small blocks
   if (plan.listed) {
     int before = incl - my_blocks;
     for (int i = 0; i < kFMaxList / 32; ++i) {
@@ -255,10 +260,13 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       report(p.status, PDA_DEV_BAD_SEQ_LEN);
       n_blocks = kFMaxList;
     }
+    // ... unless there is a pair of CTAs for each head of each block (then half as many units are no gain: 4 chunks of 24
+    // tokens behind 2000..4000, 16 heads, 65 us one by one, 79 by two; 64 prompts of 200 tokens 102 and 73)
+    by_two = static_cast<int64_t>(n_blocks) * p.num_heads > pairs;
     for (int k = 0; k < my_blocks && before + k < kFMaxList; ++k) {
       const int last = min((k + 1) * kFRows, mine.nq) - 1;
       work[before + k] = min(max(mine.nk - mine.nq_all + last + 1, 0), mine.nk);
-      list[before + k] = tid | (k << 7);
+      list[before + k] = tid | (k << 7) | (mine.nq - k * kFRows <= kFHalf ? kFSmallBlock : 0u);
     }
     __syncthreads();
     int place = 0;
@@ -269,6 +277,11 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     }
     __syncthreads();
     if (tid < n_blocks) list[place] = my_entry;
+    __syncthreads();
+    uint32_t units_before = 0;
+    if (tid < n_blocks)
+      for (int i = 0; i < tid; ++i) units_before += units_of(list[i], p.num_heads, by_two);
+    if (tid < n_blocks) work[tid] = units_before;
   }
   __syncthreads();
   cluster_sync();
@@ -315,31 +328,37 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     int t0 = 0, mine = 0, done = 0, turns = 0;
     for (int k = 0; next_unit(k, un); ++k) {
       const int n = uniform(w == 0 ? un.n0 : un.n1), n_other = uniform(w == 0 ? un.n1 : un.n0);
+      const int dual = uniform(un.dual);
+      const int step = dual ? 2 : 1, own = dual ? w : 0, other = 1 - w;  // this half's tiles: t0 + step * j + own
       // Both halves give a tile back. The one that does not read it does so as soon as it is there (not before: a
       // half that did not follow every phase of a barrier could not tell the phases apart) and goes on, to the next
       // unit where this was the last tile.
-      auto hand_on = [&](uint32_t full, uint32_t empty, int phase) {
-        wait(full, phase);
-        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty, lane));
+      auto hand_on = [&](uint32_t full, uint32_t empty, int t) {
+        const int st = t % kFStages;
+        wait(full + 8 * st, t / kFStages);
+        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty + 8 * st, lane));
         __syncwarp();
       };
+      if (dual && w == 1 && n > 0) hand_on(full_k, empty_k, t0);  // (dual: both halves have n tiles, or none)
       if (n > 0) {  // S(0): its place is free, the tensor core works a thread's products off in order
-        const int sk = t0 % kFStages;
+        const int t = t0 + own, sk = t % kFStages;
         wait(bar_q + 8 * w, done);
-        wait(full_k + 8 * sk, t0 / kFStages);
+        wait(full_k + 8 * sk, t / kFStages);
         if (!ok) break;
         tc_fence_after();
         s_product(uniform(u_k + sk * kFKBytes));
         if (n == 1) commit2_if(leader, bar_qfree + 8 * w);
         commit2_if(leader, uniform(u_ek + 8 * sk));
       }
+      if (dual && w == 0 && n > 0) hand_on(full_k, empty_k, t0 + 1);
       for (int j = 0; j < n; ++j) {
-        const int t = t0 + j, sv = t % kFStages, sk = (t + 1) % kFStages;
+        const int t = t0 + step * j + own, tn = t + step, sv = t % kFStages, sk = tn % kFStages;
         // turn i: half 0 after half 1's turn i - 1, half 1 after half 0's turn i
         const bool taking_turns = j < n_other;
         const int turn = turns + j;
         const uint32_t turn_bar = taking_turns && (w == 1 || turn > 0) ? bar_turn + 8 * w : 0u;
         const int turn_phase = w == 1 ? turn : turn - 1;
+        if (dual && w == 1) hand_on(v_ready, empty_v, t - 1);
         wait(v_ready + 8 * sv, t / kFStages);
         const uint64_t v0 = tc_desc(uniform(u_v + sv * kFVBytes), 16, 1024);
         const uint32_t k_addr = uniform(u_k + sk * kFKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
@@ -352,7 +371,10 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
         commit2_if(leader, bar_pv + 16 * w);
-        if (j + 1 < n) wait(full_k + 8 * sk, (t + 1) / kFStages);
+        if (j + 1 < n) {
+          if (dual && w == 1) hand_on(full_k, empty_k, tn - 1);
+          wait(full_k + 8 * sk, tn / kFStages);
+        }
         {  // the other weights and the turn, looked for at once by different lanes
           const bool second = (lane & 1) && turn_bar != 0u;
           wait(second ? turn_bar : bar_p + 16 * w + 8, second ? turn_phase : mine + j);
@@ -364,18 +386,22 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         commit2_if(leader, bar_pv + 16 * w + 8);
         // S(j + 1) takes the place of P(j): the tensor core works a thread's products off in order
         if (j + 1 < n) s_product(k_addr);
-        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * (w ^ 1));
+        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * other);
         if (j + 2 == n) commit2_if(leader, bar_qfree + 8 * w);
         commit2_if(leader, ev);
         if (j + 1 < n) commit2_if(leader, ek);
+        if (dual && w == 0) {
+          hand_on(v_ready, empty_v, t + 1);
+          if (j + 1 < n) hand_on(full_k, empty_k, tn + 1);
+        }
       }
-      for (int t = t0 + n; ok && t < t0 + n_other; ++t) {
-        const int st = t % kFStages;
-        hand_on(full_k + 8 * st, empty_k + 8 * st, t / kFStages);
-        hand_on(v_ready + 8 * st, empty_v + 8 * st, t / kFStages);
-      }
+      if (!dual)
+        for (int t = t0 + n; ok && t < t0 + n_other; ++t) {
+          hand_on(full_k, empty_k, t);
+          hand_on(v_ready, empty_v, t);
+        }
       if (!ok) break;
-      t0 += max(n, n_other);
+      t0 += dual ? n + n_other : max(n, n_other);
       turns += min(n, n_other);
       mine += n;
       if (n > 0) ++done;
@@ -395,7 +421,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
       const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
       const uint32_t to_q = uniform(in_cta(bar_q, 0)), to_k = uniform(in_cta(full_k, 0));
-      const int64_t n_units = static_cast<int64_t>(plan.listed ? n_blocks : plan.q_blocks * p.batch) * p.num_heads;
+      const int64_t n_units = !plan.listed ? static_cast<int64_t>(plan.q_blocks) * p.batch * p.num_heads
+                              : n_blocks == 0 ? 0 : static_cast<int64_t>(work[n_blocks - 1]) + units_of(list[n_blocks - 1], p.num_heads, by_two);
       int64_t round = 0;
       // The pair's next unit: every pairs-th of the order, to and fro, so that each pair gets early (long) and late
       // (short) ones. Unlisted blocks may be empty: 32 at a time are looked at.
@@ -406,10 +433,15 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
           PrefillSpan sp{0, 0, 0, 0, 0};
           if (at < n_units) {
             if (plan.listed) {
-              const uint32_t e = list[at / p.num_heads];
-              h = static_cast<int>(at % p.num_heads);
+              int lo = 0, hi = n_blocks;  // work[lo] <= at < work[hi]
+              while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (work[mid] <= at) lo = mid; else hi = mid;
+              }
+              const uint32_t e = list[lo];
+              h = static_cast<int>(at - work[lo]);
               b = e & 127;
-              qb = e >> 7;
+              qb = (e & (kFSmallBlock - 1)) >> 7;
             } else {
               const int64_t in_block = at % (static_cast<int64_t>(p.batch) * p.num_heads);
               qb = plan.q_blocks - 1 - static_cast<int>(at / (static_cast<int64_t>(p.batch) * p.num_heads));
@@ -418,7 +450,9 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             }
             sp = prefill_span(p, b);
           }
-          const uint32_t have = __ballot_sync(0xffffffffu, qb * kFRows < sp.nq);
+          const bool small = by_two && sp.nq - qb * kFRows <= kFHalf;  // heads two by two
+          if (small) h *= 2;
+          const uint32_t have = __ballot_sync(0xffffffffu, qb * kFRows < sp.nq && h < p.num_heads);
           if (have == 0) {
             // (r grows with the lane, and so does `at` from one pair of rounds to the next)
             if (round * pairs >= n_units) return false;
@@ -436,8 +470,10 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             n[w] = (see + kFKeys - 1) / kFKeys;
           }
           auto from_lane = [&](int v) { return __shfl_sync(0xffffffffu, v, src); };
-          un = FUnit{from_lane(qb * kFRows), from_lane(h), from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.nq_all),
-                     from_lane(sp.k0), from_lane(sp.nk), from_lane(n[0]), from_lane(n[1])};
+          const bool dual = small && h + 1 < p.num_heads;
+          if (dual) n[1] = n[0];
+          un = FUnit{from_lane(qb * kFRows), from_lane(h), from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.nq_all), from_lane(sp.k0),
+                     from_lane(sp.nk), from_lane(n[0]), from_lane(n[1]), from_lane(dual)};
           return true;
         }
       };
@@ -455,19 +491,20 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         }
         __syncwarp();
         if (!more) break;
-        const int token0 = uniform(un.q0 + un.row0 + 128 * rank), key0 = un.k0, u_h = uniform(un.h);
-        const int n_all = max(un.n0, un.n1);
+        const int key0 = un.k0, n_all = un.tiles();
         auto load_q = [&](int w) {
           if (ok && done[w] > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_qfree + 8 * w, (done[w] - 1) & 1));
           if (!ok) return;
+          const int head = uniform(un.head(w)), token = uniform(un.q0 + un.first_row(w) + 128 * rank);
           mbar_expect_tx_if(first, bar_q + 8 * w, 2 * kFQLines * kFQLine);
 #pragma unroll
           for (int ln = 0; ln < kFQLines; ++ln)
-            tma_load_4d_pair_if(leader, u_q + (w * kFQLines + ln) * kFQLine, &maps.q, to_q + 8 * w, ln, u_h, token0 + kFHalf * w);
+            tma_load_4d_pair_if(leader, u_q + (w * kFQLines + ln) * kFQLine, &maps.q, to_q + 8 * w, ln, head, token);
           ++done[w];
         };
         if (un.n0 > 0) load_q(0);
-        for (int j = 0; ok && j < n_all; ++j, ++t) {
+        for (int i = 0; ok && i < n_all; ++i, ++t) {
+          const int j = un.dual ? i >> 1 : i, u_h = uniform(un.head(i & 1));
           const int st = uniform(t % kFStages), rnd = t / kFStages;
           if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_k + 8 * st, (rnd - 1) & 1));
           if (!ok) break;
@@ -477,7 +514,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
           tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k + 8 * st, 0, u_h, my_key);
           tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k + 8 * st, 1, u_h, my_key);
           tma_load_4d_pair_if(leader, kd + 2 * kFKLine, &maps.k_rope, to_k + 8 * st, 0, 0, my_key);
-          if (j == 0 && un.n1 > 0) load_q(1);
+          if (i == 0 && un.n1 > 0) load_q(1);
           if (ok && rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_v + 8 * st, (rnd - 1) & 1));
           if (!ok) break;
           mbar_expect_tx_if(leader, full_v + 8 * st, kFVBytes);
@@ -495,16 +532,16 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       FUnit un;
       int t = 0;
       for (int k = 0; next_unit(k, un); ++k) {
-        const int n_all = max(un.n0, un.n1);
-        for (int j = 0; ok && j < n_all; ++j, ++t) {
-          const int st = t % kFStages;
+        const int n_all = un.tiles();
+        for (int i = 0; ok && i < n_all; ++i, ++t) {
+          const int j = un.dual ? i >> 1 : i, st = t % kFStages;
           ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_v + 8 * st, (t / kFStages) & 1));
           if (!ok) break;
           const int valid = un.nk - j * kFKeys;
           if (valid < kFKeys) {
             // (keys behind the end have weight 0, but what they hold may be anything)
-            for (int i = lane; i < (kFKeys - valid) * 8; i += 32)
-              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * kFVBytes + valid * 128 + i * 16), "r"(0));
+            for (int c = lane; c < (kFKeys - valid) * 8; c += 32)
+              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * kFVBytes + valid * 128 + c * 16), "r"(0));
             fence_proxy_async();
           }
           __syncwarp();
@@ -530,13 +567,12 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     const float scale_log2 = p.scale * 1.4426950408889634f;
     const uint64_t scale2 = f32x2(__float_as_uint(scale_log2), __float_as_uint(scale_log2));
     const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
-    const uint32_t stage = smem_u32(smem) + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 2048 + warp * kFOutBytes;
     const float neg_inf = -INFINITY;
     FUnit un;
     int t = 0;  // tiles of this half so far
     for (int unit = 0; next_unit(unit, un); ++unit) {
-      const int row = un.row0 + kFHalf * w + 128 * rank + (tid & 127);  // query token of the sequence
-      const int lim = min(un.nk, un.nk - un.nq_all + row + 1);          // keys it sees
+      const int row = un.first_row(w) + 128 * rank + (tid & 127);  // query token of the sequence
+      const int lim = min(un.nk, un.nk - un.nq_all + row + 1);     // keys it sees
       const int n = w == 0 ? un.n0 : un.n1;
       float m_ref = kFNoMax, l = 0.f;
       for (int j = 0; j < n; ++j, ++t) {
@@ -575,7 +611,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), scale2, ref2);
-              mx[e & 1] = max3(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
+              mx[e & 1] = max3_nan(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
               float w0, w1;
               if (decltype(poly)::value && e % kFPolyOf == kFPolyOf - 1) {
                 exp2_pair(x, w0, w1);
@@ -590,7 +626,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             float s0, s1;
             f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
             part = s0 + s1;
-            top = fmaxf(mx[0], mx[1]) * scale_log2;
+            top = max3_nan(mx[0], mx[0], mx[1]) * scale_log2;
+            if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
           };
           while (true) {
             if (edge) weights(std::false_type{});  // (weights of hidden keys are exactly zero)
@@ -629,45 +666,37 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (t - 1) & 1));
         tc_fence_after();
       }
-      const bool rows_here = un.row0 + kFHalf * w + 128 * rank + (warp & 3) * 32 < un.nq;  // (warp-uniform)
+      // (warp-uniform; the second half of a block with at most kFHalf rows has none, unless they are the next head's)
+      const bool rows_here = un.first_row(w) + 128 * rank + (warp & 3) * 32 < un.nq;
       const bool some = n > 0 && ok && l != 0.f;
       const float inv = 1.f / l;
-      __nv_bfloat16* out = p.out + (static_cast<int64_t>(un.q0) + row - lane) * p.out_token_stride + un.h * p.out_head_stride;  // the warp's first row
+      __nv_bfloat16* out = p.out + (static_cast<int64_t>(un.q0) + row) * p.out_token_stride + un.head(w) * p.out_head_stride;
+      // A thread stores its own row, 32 bytes (a whole sector) at a time where the rows' alignment allows it.
+      const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0 && p.out_token_stride % 16 == 0 && p.out_head_stride % 16 == 0;
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        uint32_t ov[64];
-        tmem_ld32(my_o + 64 * half, *reinterpret_cast<uint32_t(*)[32]>(&ov[0]));
-        tmem_ld32(my_o + 64 * half + 32, *reinterpret_cast<uint32_t(*)[32]>(&ov[32]));
+      for (int c = 0; c < 4; ++c) {
+        uint32_t ov[32];
+        tmem_ld32(my_o + 32 * c, ov);
         tmem_wait_ld();
-        if (half == 1 && n > 0) {  // O is in registers: the next unit's products may write it
+        if (c == 3 && n > 0) {  // O is in registers: the next unit's products may write it
           tc_fence_before();
           __syncwarp();
           if (lane == 0) arrive_cluster_tc(to_ofree);
         }
-        if (rows_here) {
-          // Rows are stored 128 bytes at a time, 4 rows to an instruction, by way of shared memory, 8 rows at a time
-          // (each thread storing its own row, 32 rows to an instruction, took 3300 clocks).
+        if (rows_here && row < un.nq) {
 #pragma unroll
-          for (int e = 0; e < 64; e += 2)
+          for (int e = 0; e < 32; e += 2)
             ov[e >> 1] = some ? pack2<false>(__uint_as_float(ov[e]) * inv, __uint_as_float(ov[e + 1]) * inv) : 0u;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            if ((lane >> 3) == g) {
-#pragma unroll
-              for (int c = 0; c < 8; ++c)
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + (lane & 7) * 128 + ((c ^ (lane & 7)) << 4)),
-                             "r"(ov[4 * c]), "r"(ov[4 * c + 1]), "r"(ov[4 * c + 2]), "r"(ov[4 * c + 3]) : "memory");
+          for (int k = 0; k < 16; k += 8) {
+            __nv_bfloat16* dst = out + 32 * c + 2 * k;
+            if (wide) {
+              asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(ov[k]), "r"(ov[k + 1]), "r"(ov[k + 2]),
+                           "r"(ov[k + 3]), "r"(ov[k + 4]), "r"(ov[k + 5]), "r"(ov[k + 6]), "r"(ov[k + 7]) : "memory");
+            } else {
+              reinterpret_cast<uint4*>(dst)[0] = make_uint4(ov[k], ov[k + 1], ov[k + 2], ov[k + 3]);
+              reinterpret_cast<uint4*>(dst)[1] = make_uint4(ov[k + 4], ov[k + 5], ov[k + 6], ov[k + 7]);
             }
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int r = 4 * i + (lane >> 3), c = lane & 7;  // of the 8 rows
-              uint4 x;
-              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
-                           : "r"(stage + r * 128 + ((c ^ r) << 4)) : "memory");
-              if (row - lane + 8 * g + r < un.nq) *reinterpret_cast<uint4*>(out + (8 * g + r) * p.out_token_stride + 64 * half + 8 * c) = x;
-            }
-            __syncwarp();
           }
         }
       }
