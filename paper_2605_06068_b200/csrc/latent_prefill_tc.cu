@@ -18,9 +18,13 @@
 // 32-bit weights; the rounding of the weights to bf16 is 2^-8 of each.
 // Each pair of CTAs works through several row blocks, those with the most keys first and dealt to and fro; the
 // producer runs on into the next block's Q, K and V while the last one's output is written.
-// Measured (B200): a prompt of 8192 tokens with 32 heads 0.66 ms, 1.04 PFLOP/s, 3800 clocks a tile: a half's chain of
-// S, weights (2100), P . V and the next S, of which the other half covers the most; the clock is held at 1.58 GHz
-// by the power cap. 24 prompts of 1..700 tokens with 16 heads: 80 us.
+// A block of at most 256 rows would leave the second half idle. It gets the same rows of the next head instead (64
+// prompts of 200 tokens with 16 heads 102 -> 73 us), or, where there is a pair of CTAs for each block and head
+// already, the later part of the same head's keys (4 chunks of 24 tokens behind 2000..4000, 16 heads: 66 us with one
+// half, 79 with two heads, 47 with half of the keys each).
+// Measured (B200): a prompt of 8192 tokens with 32 heads 0.68 ms, 1.01 PFLOP/s (0.64 replayed from a graph), 3800
+// clocks a tile: a half's chain of S, weights (2100), P . V and the next S, of which the other half covers the most;
+// the clock is held at 1.58 GHz by the power cap. 24 prompts of 1..700 tokens with 16 heads: 77 us.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the
 // pair's first CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are
 // bounded.
@@ -43,7 +47,8 @@ constexpr int kFKLine = 64 * 128, kFKBytes = 3 * kFKLine;  // of its 64 keys
 constexpr int kFVBytes = kFKeys * 128;                    // its line (64 dims) of all keys
 constexpr int kFStages = 3;                               // tiles
 constexpr int kFSoftWarps = 8, kFThreads = (kFSoftWarps + 4) * 32, kFProducer = 8, kFMma = 9, kFRelay = 11;  // (9, 10: one per half)
-constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + 2048 + 1024;
+constexpr int kFBookBytes = 3 * 1024;  // barriers, units, the list of row blocks, the second half's sums
+constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + kFBookBytes + 1024;
 static_assert(kFSmemBytes <= 232448, "shared memory");
 // 384 threads start with 168 registers (64512 in all); the control warps keep 104 and the softmax warps take 200
 constexpr uint32_t kFRegsSoftmax = 200, kFRegsControl = 104;
@@ -83,13 +88,19 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
 }
 
 // One row block of one head, as the producer hands it to the other warps of its CTA. row0 < 0: no more.
-// dual: the block has at most kFHalf rows, and the second half takes the same rows of the next head (with tiles of its
-// own: the pair's tiles are then this head's and that head's by turns).
+// dual: the block has at most kFHalf rows and both halves take the same ones, with tiles of their own by turns (first
+// half's, second half's, ...; as many for both): kTwoHeads: the second half's are the next head's; kSplitKeys: the
+// second half's are the later n1 tiles of the same head, and the first half's warps merge the two results.
+enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
 struct FUnit {
   int row0, h, q0, nq, nq_all, k0, nk, n0, n1, dual;
   __device__ int first_row(int w) const { return row0 + (dual ? 0 : kFHalf * w); }
-  __device__ int head(int w) const { return h + (dual ? w : 0); }
+  __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
   __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
+  // The pair's i-th tile: whose half's (where that matters), and which 128 keys.
+  __device__ int half_of(int i) const { return i & 1; }
+  __device__ int keys_of(int i) const { return dual ? key_tile(i & 1, i >> 1) : i; }
+  __device__ int key_tile(int w, int j) const { return dual == kSplitKeys && w ? n0 + j : j; }
 };
 constexpr uint32_t kFSmallBlock = 1u << 30;  // (in a list entry) at most kFHalf rows
 __device__ __forceinline__ int units_of(uint32_t entry, int num_heads, bool by_two) {
@@ -168,13 +179,14 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes));
-  FUnit* units = reinterpret_cast<FUnit*>(bars + 48);               // [kFUnitSlots]
+  FUnit* units = reinterpret_cast<FUnit*>(bars + 56);               // [kFUnitSlots]
   uint32_t* list = reinterpret_cast<uint32_t*>(units + kFUnitSlots);  // [kFMaxList] sequence and block, most work first
   uint32_t* work = list + kFMaxList;                                // [kFMaxList] keys, then units of the entries before
   uint32_t* scan = work + kFMaxList;                                // [5] sequences' blocks, by warp; their sum
-  uint32_t* tmem_slot = scan + 5;
+  uint32_t* tmem_slot = scan + 6;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
-  static_assert(48 * 8 + kFUnitSlots * sizeof(FUnit) + 2 * kFMaxList * 4 + 7 * 4 <= 2048, "shared memory");
+  float* merge_sh = reinterpret_cast<float*>(cta_err + 1);          // [128][2]
+  static_assert(56 * 8 + kFUnitSlots * sizeof(FUnit) + 2 * kFMaxList * 4 + 8 * 4 + 1024 <= kFBookBytes, "shared memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1;  // in the pair
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
@@ -188,7 +200,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
                  empty_v = full_v + 8 * kFStages, v_ready = empty_v + 8 * kFStages, bar_q = v_ready + 8 * kFStages;
   const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_qfree = bar_turn + 16,
                  bar_ofree = bar_qfree + 16, unit_full = bar_ofree + 16, unit_empty = unit_full + 8 * kFUnitSlots,
-                 bar_drain = unit_empty + 8 * kFUnitSlots, bar_never = bar_drain + 8;
+                 bar_drain = unit_empty + 8 * kFUnitSlots, bar_never = bar_drain + 8, bar_merge = bar_never + 8;
   if (tid == 0) {
     for (int i = 0; i < kFStages; ++i) {
       mbar_init(full_k + 8 * i, 1);
@@ -214,6 +226,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     }
     mbar_init(bar_drain, 2);
     mbar_init(bar_never, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(bar_merge + 8 * i, 1);
     *cta_err = 0;
     fence_mbar_init();
     fence_proxy_async();
@@ -260,8 +273,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       report(p.status, PDA_DEV_BAD_SEQ_LEN);
       n_blocks = kFMaxList;
     }
-    // ... unless there is a pair of CTAs for each head of each block (then half as many units are no gain: 4 chunks of 24
-    // tokens behind 2000..4000, 16 heads, 65 us one by one, 79 by two; 64 prompts of 200 tokens 102 and 73)
+    // ... unless there is a pair of CTAs for each head of each block: half as many units are no gain then
     by_two = static_cast<int64_t>(n_blocks) * p.num_heads > pairs;
     for (int k = 0; k < my_blocks && before + k < kFMaxList; ++k) {
       const int last = min((k + 1) * kFRows, mine.nq) - 1;
@@ -294,9 +306,11 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(unit_full + 8 * slot, (k / kFUnitSlots) & 1));
     if (!ok) return false;
     un = units[slot];
-    __syncwarp();
-    if (lane == 0) mbar_arrive_tc(unit_empty + 8 * slot);
     return un.row0 >= 0;
+  };
+  auto free_unit = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive_tc(unit_empty + 8 * (k % kFUnitSlots));
   };
 
   // ================= products of half w =================
@@ -327,6 +341,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     // Before this unit: tiles of the pair; of this half; units of this half; tiles on which the halves take turns.
     int t0 = 0, mine = 0, done = 0, turns = 0;
     for (int k = 0; next_unit(k, un); ++k) {
+      free_unit(k);
       const int n = uniform(w == 0 ? un.n0 : un.n1), n_other = uniform(w == 0 ? un.n1 : un.n0);
       const int dual = uniform(un.dual);
       const int step = dual ? 2 : 1, own = dual ? w : 0, other = 1 - w;  // this half's tiles: t0 + step * j + own
@@ -470,8 +485,14 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             n[w] = (see + kFKeys - 1) / kFKeys;
           }
           auto from_lane = [&](int v) { return __shfl_sync(0xffffffffu, v, src); };
-          const bool dual = small && h + 1 < p.num_heads;
-          if (dual) n[1] = n[0];
+          int dual = kOneHead;
+          if (small && h + 1 < p.num_heads) {
+            dual = kTwoHeads;
+            n[1] = n[0];
+          } else if (!by_two && n[0] > 1 && n[1] == 0) {  // (the second half has no rows, and pairs are not short)
+            dual = kSplitKeys;
+            n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last visible key)
+          }
           un = FUnit{from_lane(qb * kFRows), from_lane(h), from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.nq_all), from_lane(sp.k0),
                      from_lane(sp.nk), from_lane(n[0]), from_lane(n[1]), from_lane(dual)};
           return true;
@@ -504,12 +525,12 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         };
         if (un.n0 > 0) load_q(0);
         for (int i = 0; ok && i < n_all; ++i, ++t) {
-          const int j = un.dual ? i >> 1 : i, u_h = uniform(un.head(i & 1));
+          const int u_h = uniform(un.head(un.half_of(i)));
           const int st = uniform(t % kFStages), rnd = t / kFStages;
           if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_k + 8 * st, (rnd - 1) & 1));
           if (!ok) break;
           mbar_expect_tx_if(first, full_k + 8 * st, 2 * kFKBytes);
-          const int key = uniform(key0 + j * kFKeys), my_key = key + 64 * rank;
+          const int key = uniform(key0 + un.keys_of(i) * kFKeys), my_key = key + 64 * rank;
           const uint32_t kd = u_k + st * kFKBytes;
           tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k + 8 * st, 0, u_h, my_key);
           tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k + 8 * st, 1, u_h, my_key);
@@ -532,12 +553,13 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       FUnit un;
       int t = 0;
       for (int k = 0; next_unit(k, un); ++k) {
+        free_unit(k);
         const int n_all = un.tiles();
         for (int i = 0; ok && i < n_all; ++i, ++t) {
-          const int j = un.dual ? i >> 1 : i, st = t % kFStages;
+          const int st = t % kFStages;
           ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_v + 8 * st, (t / kFStages) & 1));
           if (!ok) break;
-          const int valid = un.nk - j * kFKeys;
+          const int valid = max(un.nk - un.keys_of(i) * kFKeys, 0);
           if (valid < kFKeys) {
             // (keys behind the end have weight 0, but what they hold may be anything)
             for (int c = lane; c < (kFKeys - valid) * 8; c += 32)
@@ -568,18 +590,21 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     const uint64_t scale2 = f32x2(__float_as_uint(scale_log2), __float_as_uint(scale_log2));
     const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
     const float neg_inf = -INFINITY;
-    FUnit un;
-    int t = 0;  // tiles of this half so far
-    for (int unit = 0; next_unit(unit, un); ++unit) {
-      const int row = un.first_row(w) + 128 * rank + (tid & 127);  // query token of the sequence
-      const int lim = min(un.nk, un.nk - un.nq_all + row + 1);     // keys it sees
-      const int n = w == 0 ? un.n0 : un.n1;
+    int t = 0, merges = 0;  // tiles of this half, merges with the second half so far
+    for (int unit = 0;; ++unit) {
+      int n, seen;  // tiles; columns that this thread's row sees, from the half's first tile on
+      {
+        FUnit un;
+        if (!next_unit(unit, un)) break;
+        n = w == 0 ? un.n0 : un.n1;
+        seen = min(un.nk, un.nk - un.nq_all + un.first_row(w) + 128 * rank + (tid & 127) + 1) - un.key_tile(w, 0) * kFKeys;
+      }
       float m_ref = kFNoMax, l = 0.f;
       for (int j = 0; j < n; ++j, ++t) {
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * w, t & 1));
         if (!ok) break;
         tc_fence_after();
-        const int vis = lim - j * kFKeys;  // visible columns of this row
+        const int vis = seen - j * kFKeys;  // visible columns of this row
         const bool edge = __any_sync(0xffffffffu, vis < kFKeys);
         // 64 keys at a time; the first run's products start while the second run is here
 #pragma unroll
@@ -666,8 +691,44 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (t - 1) & 1));
         tc_fence_after();
       }
+      const FUnit un = units[unit % kFUnitSlots];  // (read again: it takes registers that the loop above needs)
+      free_unit(unit);
+      const int row = un.first_row(w) + 128 * rank + (tid & 127);  // query token of the sequence
+      const bool split = un.dual == kSplitKeys;
+      float* sums = merge_sh + 2 * (tid & 127);  // the row's reference and sum from the second half
+      if (split && w == 1) {  // the first half's warp of the same rows takes it from here
+        *reinterpret_cast<float2*>(sums) = make_float2(m_ref, l);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_tc(bar_merge + 8 * (warp & 3));
+        if (!ok) break;
+        continue;
+      }
       // (warp-uniform; the second half of a block with at most kFHalf rows has none, unless they are the next head's)
       const bool rows_here = un.first_row(w) + 128 * rank + (warp & 3) * 32 < un.nq;
+      if (split) {  // O and the sum of both halves, in the first half's place
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_merge + 8 * (warp & 3), merges & 1));
+        tc_fence_after();
+        ++merges;
+        const float2 other = *reinterpret_cast<const float2*>(sums);
+        const float m = fmaxf(m_ref, other.x);
+        const float mul = ex2(m_ref - m), mul_other = ex2(other.x - m);
+        l = l * mul + other.y * mul_other;
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c) {
+          uint32_t ov[16], o2[16];
+          tmem_ld16(my_o + 16 * c, ov);
+          tmem_ld16(my_o + 128 + 16 * c, o2);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(fmaf(__uint_as_float(o2[e]), mul_other, __uint_as_float(ov[e]) * mul));
+          tmem_st16(my_o + 16 * c, ov);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cluster_tc(to_ofree + 8);  // (the second half's O has been read)
+      }
       const bool some = n > 0 && ok && l != 0.f;
       const float inv = 1.f / l;
       __nv_bfloat16* out = p.out + (static_cast<int64_t>(un.q0) + row) * p.out_token_stride + un.head(w) * p.out_head_stride;

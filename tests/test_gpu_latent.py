@@ -435,6 +435,15 @@ def test_expanded_unequal_halves():
     run_expanded([600, 256, 257, 130, 512, 385], [300, 2000, 257, 1500, 100, 385], 30, seed=15)
 
 
+@pytest.mark.parametrize("q_lens,k_lens", [([1], [129]), ([256], [256]), ([24, 17], [4000, 2049]), ([129, 200], [900, 385]),
+                                           ([700, 768], [3000, 768]), ([250, 256], [200, 130]), ([100], [60]), ([30, 0, 256], [1300, 500, 641])])
+@pytest.mark.parametrize("spread", [1.0, 30.0])
+def test_expanded_few_rows_behind_a_long_context(q_lens, k_lens, spread):
+    """Row blocks of at most 256 rows, with room for each: odd and even numbers of tiles, rows that see the first few
+    keys or none, the last block of a longer prompt; with a spread of 30 a row's weight lies on one key."""
+    run_expanded(q_lens, k_lens, 3, seed=17, spread=spread)
+
+
 def test_expanded_huge_values_behind_the_mask():
     """Later tokens' values near the largest number must not reach earlier rows."""
     nq = 200
