@@ -489,7 +489,8 @@ typedef struct pda_latent_desc {
  *     slot_map[t] = positions[t] = -1 for cu_new[batch] <= t < capacity;
  *     *free_count_out = *free_count - (pages taken).
  *   free_pages      int32[free_capacity], the free page ids, a stack whose top is at
- *                   *free_count - 1 (values beyond free_capacity count as free_capacity);
+ *                   *free_count - 1 (values beyond free_capacity count as free_capacity,
+ *                   negative ones as 0, for *free_count_out too);
  *                   read only: to give pages back, write their ids at *free_count onwards
  *                   and raise it
  *   free_count_out  may be free_count itself

@@ -85,8 +85,7 @@ build_tables_kernel(TablesParams p, bool write_count, bool count_only) {
   __shared__ Acc scratch[2][kTabThreads / 32];
   __shared__ int32_t cu_s[kTabThreads + 1], tk_s[kTabThreads + 1], start_s[kTabThreads], held_s[kTabThreads];
   const int tid = threadIdx.x;
-  const int count = p.free_count[0];
-  const int avail = min(max(count, 0), p.free_capacity);
+  const int avail = min(max(p.free_count[0], 0), p.free_capacity);
 
   // totals first: either every page that the step needs can be had, or none is taken
   SeqStep s{};
@@ -108,7 +107,7 @@ build_tables_kernel(TablesParams p, bool write_count, bool count_only) {
     if (tid == 0 && !pages_ok) report(p.status, PDA_DEV_NO_PAGES);
     if (tid == 0 && !slots_ok) report(p.status, PDA_DEV_NO_SLOTS);
   }
-  if (blockIdx.x == 0 && write_count && tid == 0) p.free_count_out[0] = ok ? count - static_cast<int>(tot_t) : count;
+  if (blockIdx.x == 0 && write_count && tid == 0) p.free_count_out[0] = ok ? avail - static_cast<int>(tot_t) : avail;
   if (count_only) return;
 
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTabTokensPerCta;
