@@ -125,6 +125,7 @@ int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_he
   if (!aligned16(q) || !aligned16(k_nope) || !aligned16(k_rope) || !aligned16(v) || !aligned16(out) || !aligned4(cu_q) ||
       !aligned4(cu_k) || !aligned4(status))
     return PDA_ERR_MISALIGNED;
+  if (max_q > total_q) max_q = total_q;  // (no sequence has more)
   pda::LatentPrefillParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(k_nope),
                              static_cast<const __nv_bfloat16*>(k_rope), static_cast<const __nv_bfloat16*>(v),
                              static_cast<__nv_bfloat16*>(out), cu_q, cu_k, status, q_token_stride, q_head_stride,

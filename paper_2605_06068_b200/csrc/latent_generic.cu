@@ -110,19 +110,33 @@ __global__ void __launch_bounds__(kGenThreads) latent_generic_kernel(LatentParam
 __global__ void __launch_bounds__(kGenThreads) latent_prefill_generic_kernel(LatentPrefillParams p) {
   extern __shared__ float q_sh[];
   __shared__ float p_sh[kGenBlock], red_sh[kGenThreads / 32];
-  const int i = blockIdx.x / p.num_heads, h = blockIdx.x % p.num_heads, b = blockIdx.y;
-  PrefillSpan sp = prefill_span(p, b);
-  if (i >= sp.nq) return;
-  const int64_t token = static_cast<int64_t>(sp.q0) + i;
-  const int n = max(sp.nk - sp.nq_all + i + 1, 0) * (sp.nk > 0);
-  for (int d = threadIdx.x; d < p.nope_dim + p.rope_dim; d += kGenThreads)
-    q_sh[d] = __bfloat162float(p.q[token * p.q_token_stride + h * p.q_head_stride + d]);
-  const int64_t k0 = sp.k0;
-  auto kn = [&](int j) { return p.k_nope + (k0 + j) * p.kn_token_stride + h * p.kn_head_stride; };
-  auto kr = [&](int j) { return p.k_rope + (k0 + j) * p.kr_token_stride; };
-  auto v = [&](int j) { return p.v + (k0 + j) * p.v_token_stride + h * p.v_head_stride; };
-  attend_row(q_sh, p.nope_dim, p.rope_dim, p.v_dim, n, p.scale, kn, kr, v,
-             p.out + token * p.out_token_stride + h * p.out_head_stride, p_sh, red_sh);
+  // (every sequence's ranges are looked at, those without rows among them)
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * kGenThreads + threadIdx.x; b < p.batch;
+       b += static_cast<int64_t>(gridDim.x) * kGenThreads)
+    prefill_span(p, static_cast<int>(b));
+  const int64_t units = static_cast<int64_t>(p.total_q) * p.num_heads;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t token = unit / p.num_heads;
+    const int h = static_cast<int>(unit % p.num_heads);
+    int b = 0;  // the last sequence that does not start behind the token
+    for (int hi = p.batch; hi - b > 1;) {
+      const int mid = (b + hi) >> 1;
+      if (p.cu_q[mid] <= token) b = mid; else hi = mid;
+    }
+    const PrefillSpan sp = prefill_span(p, b);
+    if (token < sp.q0 || token - sp.q0 >= sp.nq) continue;
+    const int i = static_cast<int>(token - sp.q0);
+    __syncthreads();  // (q_sh may still be read for the last row)
+    const int n = max(sp.nk - sp.nq_all + i + 1, 0) * (sp.nk > 0);
+    for (int d = threadIdx.x; d < p.nope_dim + p.rope_dim; d += kGenThreads)
+      q_sh[d] = __bfloat162float(p.q[token * p.q_token_stride + h * p.q_head_stride + d]);
+    const int64_t k0 = sp.k0;
+    auto kn = [&](int j) { return p.k_nope + (k0 + j) * p.kn_token_stride + h * p.kn_head_stride; };
+    auto kr = [&](int j) { return p.k_rope + (k0 + j) * p.kr_token_stride; };
+    auto v = [&](int j) { return p.v + (k0 + j) * p.v_token_stride + h * p.v_head_stride; };
+    attend_row(q_sh, p.nope_dim, p.rope_dim, p.v_dim, n, p.scale, kn, kr, v,
+               p.out + token * p.out_token_stride + h * p.out_head_stride, p_sh, red_sh);
+  }
 }
 
 }  // namespace
@@ -135,9 +149,9 @@ cudaError_t launch_latent_generic(const LatentParams& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_latent_prefill_generic(const LatentPrefillParams& p, cudaStream_t stream) {
-  const int64_t x = static_cast<int64_t>(p.max_q) * p.num_heads;
-  if (x > INT32_MAX) return cudaErrorInvalidValue;
-  latent_prefill_generic_kernel<<<dim3(static_cast<unsigned>(x), p.batch), kGenThreads, (p.nope_dim + p.rope_dim) * 4, stream>>>(p);
+  const int64_t units = static_cast<int64_t>(p.total_q) * p.num_heads;
+  const unsigned ctas = static_cast<unsigned>(units < INT32_MAX ? units : INT32_MAX);
+  latent_prefill_generic_kernel<<<ctas, kGenThreads, (p.nope_dim + p.rope_dim) * 4, stream>>>(p);
   return cudaGetLastError();
 }
 

@@ -109,6 +109,7 @@ __device__ __forceinline__ int units_of(uint32_t entry, int num_heads, bool by_t
 struct FPlan {
   int q_blocks;  // blocks of max_q
   int listed;    // the row blocks of all sequences are few enough to be listed and sorted in shared memory
+  int64_t slots;  // > 0: row blocks are looked for at this many places (below), not at each of q_blocks of each sequence
 };
 
 struct FMaps {
@@ -436,7 +437,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
       const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
       const uint32_t to_q = uniform(in_cta(bar_q, 0)), to_k = uniform(in_cta(full_k, 0));
-      const int64_t n_units = !plan.listed ? static_cast<int64_t>(plan.q_blocks) * p.batch * p.num_heads
+      const int64_t n_units = plan.slots > 0 ? plan.slots * p.num_heads
+                              : !plan.listed ? static_cast<int64_t>(plan.q_blocks) * p.batch * p.num_heads
                               : n_blocks == 0 ? 0 : static_cast<int64_t>(work[n_blocks - 1]) + units_of(list[n_blocks - 1], p.num_heads, by_two);
       int64_t round = 0;
       // The pair's next unit: every pairs-th of the order, to and fro, so that each pair gets early (long) and late
@@ -457,13 +459,26 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
               h = static_cast<int>(at - work[lo]);
               b = e & 127;
               qb = (e & (kFSmallBlock - 1)) >> 7;
+            } else if (plan.slots > 0) {
+              // Sequence b's blocks stand from place cu_q[b] / kFRows + b on: the next sequence's come behind them,
+              // and all places are one a sequence and one for every kFRows tokens.
+              h = static_cast<int>(at % p.num_heads);
+              const int64_t place = plan.slots - 1 - at / p.num_heads;
+              int hi = p.batch;  // the last sequence whose first place is not behind this one
+              while (hi - b > 1) {
+                const int mid = (b + hi) >> 1;
+                if (p.cu_q[mid] / kFRows + static_cast<int64_t>(mid) <= place) b = mid; else hi = mid;
+              }
+              const int64_t in_seq = place - (p.cu_q[b] / kFRows + static_cast<int64_t>(b));
+              qb = in_seq < 0 || in_seq >= plan.q_blocks ? plan.q_blocks : static_cast<int>(in_seq);
             } else {
               const int64_t in_block = at % (static_cast<int64_t>(p.batch) * p.num_heads);
               qb = plan.q_blocks - 1 - static_cast<int>(at / (static_cast<int64_t>(p.batch) * p.num_heads));
               b = static_cast<int>(in_block / p.num_heads);
               h = static_cast<int>(in_block % p.num_heads);
             }
-            sp = prefill_span(p, b);
+            if (qb < plan.q_blocks) sp = prefill_span(p, b);
+            else qb = 0;  // (no such block: sp has no rows)
           }
           const bool small = by_two && sp.nq - qb * kFRows <= kFHalf;  // heads two by two
           if (small) h *= 2;
@@ -579,6 +594,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       issue_role(std::integral_constant<int, 0>{});
     } else if (warp == kFMma + 1 && rank == 0) {
       issue_role(std::integral_constant<int, 1>{});
+    } else if (warp == kFMma && pair == 0 && plan.slots > 0) {
+      for (int b = lane; b < p.batch; b += 32) prefill_span(p, b);  // (reports sequences that no place leads to)
     }
   } else {
     reg_alloc_inc<kFRegsSoftmax>();
@@ -823,7 +840,11 @@ cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t 
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   const int q_blocks = (p.max_q + kFRows - 1) / kFRows;
   const int64_t most = std::min(static_cast<int64_t>(p.batch) + p.total_q / kFRows, static_cast<int64_t>(p.batch) * q_blocks);
-  const FPlan plan{q_blocks, most <= kFMaxList ? 1 : 0};
+  // Not listed, the sequences' last possible blocks come first (their keys are the most). Where the sequences differ so
+  // much that most of these places would be empty, the places are counted by the tokens instead.
+  const int64_t places = static_cast<int64_t>(p.batch) + p.total_q / kFRows;
+  const int listed = most <= kFMaxList ? 1 : 0;
+  const FPlan plan{q_blocks, listed, !listed && static_cast<int64_t>(p.batch) * q_blocks > 4 * places ? places : 0};
   const int64_t pairs = std::min(most * p.num_heads, static_cast<int64_t>(std::max(sms / 2, 1)));
   latent_prefill_tc_kernel<<<static_cast<unsigned>(2 * pairs), kFThreads, kFSmemBytes, stream>>>(maps, p, plan);
   return cudaGetLastError();

@@ -111,6 +111,24 @@ def test_tables_refuse_on_the_device():
     assert st == 1 and slots[:2] == [-1, -1]
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_tables_count_beyond_the_list(in_place):
+    """A count beyond the list counts as the list's length from then on: no page is handed out twice."""
+    free = list(range(100, 110))
+    count, taken = ints([1000]), []
+    for left in (7, 4, 1):
+        cu, slots, table = ints([0, 0, 0]), ints([0] * 1500), ints(np.zeros((2, 8)))
+        out = count if in_place else ints([0])
+        pda.paged_build_tables(ints([17, 3]), ints([17, 3]), 16, ints(free), count, table, cu, slots, free_count_out=out)
+        taken += table[0, :2].tolist() + table[1, :1].tolist()
+        assert out.item() == left
+        count = out
+    assert taken == free[:0:-1]
+    count, cu, slots, st = ints([-5]), ints([0, 0]), ints([0]), ints([0])
+    pda.paged_build_tables(ints([1]), ints([1]), 16, ints(free), count, ints(np.zeros((1, 8))), cu, slots, status=st)
+    assert count.item() == 0 and st.item() == 4
+
+
 def test_tables_empty_batch():
     cu, slots, out = ints([9]), ints([9, 9]), ints([9])
     e = torch.empty(0, dtype=torch.int32, device="cuda")
@@ -442,6 +460,54 @@ def test_expanded_few_rows_behind_a_long_context(q_lens, k_lens, spread):
     """Row blocks of at most 256 rows, with room for each: odd and even numbers of tiles, rows that see the first few
     keys or none, the last block of a longer prompt; with a spread of 30 a row's weight lies on one key."""
     run_expanded(q_lens, k_lens, 3, seed=17, spread=spread)
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_expanded_loose_bound_of_the_query_tokens(flags):
+    """max_q far above what the sequences have, with few and with many of them."""
+    most = (2 ** 31 - 1) // 2
+    run_expanded([5, 130, 1], [70, 130, 9], 2, seed=18, max_q=most, flags=flags)
+    run_expanded([3, 0, 1, 40] * 50, [9, 5, 1, 60] * 50, 2, seed=19, max_q=most, flags=flags)
+
+
+@pytest.mark.parametrize("long_at", [0, 77, 149])
+@pytest.mark.parametrize("gap", [0, 700])
+def test_expanded_one_long_among_many_short(long_at, gap):
+    """More sequences than are listed, one of which has many row blocks."""
+    g = np.random.default_rng(long_at)
+    n = [int(x) for x in g.integers(0, 20, size=150)]
+    n[long_at] = 2600
+    run_expanded(n, [x + int(y) for x, y in zip(n, g.integers(0, 200, size=150))], 3, seed=20, gap=gap)
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_expanded_bad_ranges_among_many(flags):
+    """Sequences whose ranges are bad are reported and zeroed, also those without rows; the others are as they should be."""
+    B, H = 150, 2
+    n = [3] * B
+    n[70] = 2600
+    cq = [int(x) for x in np.concatenate([[0], np.cumsum(n)])]
+    T = cq[-1]
+    q, kn, kr, v = randn(1, T, H, 192), randn(2, T, H, 128), randn(3, T, 64), randn(4, T, H, 128)
+    ref, tol = U.expanded(q, kn, kr, v, cq, cq, 0.07)
+    d = [x.cuda() for x in (q, kn, kr, v)]
+
+    def call(cq, ck, max_q):
+        out, st = torch.full((T, H, 128), -5.0, dtype=torch.bfloat16, device="cuda"), ints([0])
+        pda.latent_prefill_attention(*d, ints(cq), ints(ck), max_q, 0.07, out=out, flags=flags, status=st)
+        return out.cpu().double(), st.item()
+
+    x, st = call(cq, cq[:-1] + [T + 1], 2600)                # the last one's keys pass the array
+    assert st == 2 and (x[T - 3:] == 0).all()
+    U.check(x[:T - 3], ref[:T - 3], tol[:T - 3], "the others")
+    x, st = call(cq, cq, 1000)                               # one has more rows than max_q: so many are zeroed
+    a, b = cq[70], cq[71]
+    assert st == 2 and (x[a:a + 1000] == 0).all() and (x[a + 1000:b] == -5).all()
+    U.check(x[:a], ref[:a], tol[:a], "before")
+    U.check(x[b:], ref[b:], tol[b:], "behind")
+    no_rows = cq[:100] + [cq[100]] * 2 + cq[102:]            # sequence 100 has no rows, and keys out of range
+    x, st = call(no_rows, [0] * 100 + [5, 0] + [0] * (B - 101), 2600)
+    assert st == 2
 
 
 def test_expanded_huge_values_behind_the_mask():
