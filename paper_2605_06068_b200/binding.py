@@ -401,6 +401,13 @@ def _raw(stream, device):
     return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """A buffer of the stream that the call runs on: allocated on another one, the allocator would give its memory
+    away, or take it from work still queued there, without waiting for the call."""
+    with _same_context if stream is None else torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _dp(t):
     return None if t is None else t.data_ptr()
 
@@ -510,11 +517,11 @@ def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, 
     _check(rc, "latent_append")
 
 
-def latent_workspace(batch, num_q_heads, n_query_tokens, latent_dim, device="cuda"):
+def latent_workspace(batch, num_q_heads, n_query_tokens, latent_dim, device="cuda", stream=None):
     """Workspace of ``paged_latent_attention`` (uninitialised; one per stream of overlapping calls)."""
     n = int(lib().pda_latent_workspace_bytes(batch, num_q_heads, n_query_tokens, latent_dim))
     _check(min(n, 0), "pda_latent_workspace_bytes")
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return _empty(n, torch.uint8, device, stream)
 
 
 def _token_strides(name, t, B, T, H):
@@ -540,7 +547,7 @@ def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale
     else:
         (B, H, R), T = shape, 1
     if out is None:
-        out = torch.empty(shape, dtype=q_latent.dtype, device=q_latent.device)
+        out = _empty(shape, q_latent.dtype, q_latent.device, stream)
     elif out.shape != shape:
         raise ValueError("out: expected the shape of q_latent")
     desc = latent_desc(cache, R)
@@ -561,7 +568,7 @@ def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale
         raise ValueError("seq_lens: expected one entry per sequence")
     stride = _check_table(block_table, B)
     if workspace is None:
-        workspace = latent_workspace(B, H, T, R, device=cache.device)
+        workspace = latent_workspace(B, H, T, R, device=cache.device, stream=stream)
     dev = _same_device(q_latent, q_rope, out, cache, block_table, seq_lens, workspace, status)
     with _device_call(dev):
         rc = lib().paged_latent_attention(
@@ -580,7 +587,7 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
     tk, _, dn = k_nope.shape
     dv, dr = v.shape[2], D - dn
     if out is None:
-        out = torch.empty((tq, H, dv), dtype=q.dtype, device=q.device)
+        out = _empty((tq, H, dv), q.dtype, q.device, stream)
     _bf16_rows("q", q)
     _bf16_rows("k_nope", k_nope)
     _bf16_rows("v", v)
@@ -610,7 +617,7 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
     with _device_call(dev):
         rc = lib().latent_prefill_attention(
             q.data_ptr(), *st(q, tq), k_nope.data_ptr(), *st(k_nope, tk), _dp(k_rope), kr_token, v.data_ptr(), *st(v, tk),
-            cu_q.data_ptr(), cu_k.data_ptr(), n - 1, H, dn, dr, dv, int(max_q), tq, tk, scale, out.data_ptr(), *st(out, tq),
+            cu_q.data_ptr(), cu_k.data_ptr(), n - 1, H, dn, dr, dv, min(int(max_q), tq), tq, tk, scale, out.data_ptr(), *st(out, tq),
             flags, _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "latent_prefill_attention")

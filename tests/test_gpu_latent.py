@@ -693,6 +693,34 @@ def test_step_in_a_graph():
         U.check(out, ref, tol, f"replay {i}")
 
 
+def test_buffers_of_a_call_belong_to_its_stream(monkeypatch):
+    """What a call on another stream allocates is not handed out on the current one while the call may still run."""
+    import paper_2605_06068_b200.binding as binding
+    real, seen = binding.lib(), {}
+
+    class Recorder:
+        def __getattr__(self, name):
+            f = getattr(real, name)
+
+            def call(*args):
+                seen[name] = args
+                return f(*args)
+            return call if name == "paged_latent_attention" else f
+
+    monkeypatch.setattr(binding, "lib", lambda: Recorder())
+    pg = U.Paged([700, 40], 64, 512, 64, 50)
+    ql, qr = randn(51, 2, 16, 512).cuda(), randn(52, 2, 16, 64).cuda()
+    s = torch.cuda.Stream()
+    first = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 0.07)
+    torch.cuda.synchronize()
+    out = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 0.07, stream=s)
+    at, size = seen["paged_latent_attention"][18], seen["paged_latent_attention"][19]
+    held = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(4)]   # of the current stream
+    assert at not in [x.data_ptr() for x in held]
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+
+
 def test_calls_on_several_streams_at_once():
     """Both forms, the append and the tables on four streams at the same time, each with buffers of its own."""
     jobs = []
