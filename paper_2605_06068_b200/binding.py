@@ -8,6 +8,7 @@ fails, a ``RuntimeError`` is raised.
 from __future__ import annotations
 
 import contextlib
+import functools
 import ctypes as C
 import os
 
@@ -437,25 +438,37 @@ def _int32(*tensors):
 
 
 def _bf16_rows(name, t):
+    """The strides of a bf16 tensor whose last dimension is contiguous."""
     if t.dtype is not _BF16:
         raise TypeError(f"{name}: expected bfloat16, got {t.dtype}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    strides = t.stride()
+    if strides[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
+    return strides
 
 
 def latent_desc(cache: torch.Tensor, latent_dim: int) -> LatentDesc:
     """Descriptor of a ``[num_pages, P, latent_dim + rope_dim]`` bf16 latent cache."""
+    return LatentDesc.from_buffer_copy(_desc_of(cache, latent_dim))
+
+
+def _desc_of(cache, latent_dim):
+    """The same, shared by calls with equal layouts (not to be written to)."""
     if cache.dim() != 3:
         raise ValueError("a latent cache is [num_pages, page_size, latent_dim + rope_dim]")
-    _bf16_rows("cache", cache)
+    page, slot, _ = _bf16_rows("cache", cache)
     n, P, W = cache.shape
-    page, slot, _ = cache.stride()
     # (a dimension of extent 1 may carry any stride: the one of the dense layout is taken)
     if P == 1:
         slot = max(slot, W)
     if n <= 1:
         page = max(page, P * slot)
-    return LatentDesc(page, slot, n, P, latent_dim, W - latent_dim, PDA_BF16)
+    return _latent_desc(page, slot, n, P, latent_dim, W - latent_dim)
+
+
+@functools.lru_cache(maxsize=64)
+def _latent_desc(page_stride, slot_stride, num_pages, page_size, latent_dim, rope_dim):
+    return LatentDesc(page_stride, slot_stride, num_pages, page_size, latent_dim, rope_dim, PDA_BF16)
 
 
 def _check_table(block_table, batch):
@@ -484,9 +497,10 @@ def paged_build_tables(seq_lens, new_lens, page_size, free_pages, free_count, bl
     if free_count_out is None:
         free_count_out = free_count
     with _device_call(dev):
-        rc = lib().paged_build_tables(_dp(seq_lens), _dp(new_lens), B, int(page_size), _dp(free_pages), free_pages.numel(),
-                                      _dp(free_count), _dp(free_count_out), _dp(block_table), stride, _dp(cu_new),
-                                      _dp(slot_map), _dp(positions), slot_map.numel(), _dp(status), _raw(stream, dev))
+        rc = lib().paged_build_tables(seq_lens.data_ptr(), new_lens.data_ptr(), B, int(page_size), free_pages.data_ptr(),
+                                      free_pages.numel(), free_count.data_ptr(), free_count_out.data_ptr(),
+                                      block_table.data_ptr(), stride, cu_new.data_ptr(), slot_map.data_ptr(),
+                                      _dp(positions), slot_map.numel(), _dp(status), _raw(stream, dev))
     _check(rc, "paged_build_tables")
 
 
@@ -494,13 +508,15 @@ def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, 
     """Rows ``[c_new | rope_new]`` (``[T, R]``, ``[T, Dr]``) into the cache slots ``slot_map``; with ``norm_weight``
     ``[R]`` the latent's root-mean-square norm on the way."""
     T, R = c_new.shape
-    desc = latent_desc(cache, R)
-    _bf16_rows("c_new", c_new)
+    desc = _desc_of(cache, R)
+    c_stride, rope_stride = _bf16_rows("c_new", c_new)[0], 0
     _int32(slot_map, status)
-    if desc.rope_dim > 0:
-        _bf16_rows("rope_new", rope_new)
-        if tuple(rope_new.shape) != (T, desc.rope_dim):
+    rope = desc.rope_dim
+    if rope > 0:
+        rope_strides = _bf16_rows("rope_new", rope_new)
+        if rope_new.shape != (T, rope):
             raise ValueError("rope_new: expected [T, rope_dim]")
+        rope_stride = rope_strides[0]
     else:
         rope_new = None
     if slot_map.numel() != T:
@@ -511,9 +527,8 @@ def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, 
             raise ValueError("norm_weight: expected [latent_dim]")
     dev = _same_device(c_new, rope_new, cache, slot_map, norm_weight, status)
     with _device_call(dev):
-        rc = lib().latent_append(_dp(c_new), c_new.stride(0), _dp(rope_new), 0 if rope_new is None else rope_new.stride(0),
-                                 _dp(cache), C.byref(desc), _dp(norm_weight), float(eps), _dp(slot_map), T, _dp(status),
-                                 _raw(stream, dev))
+        rc = lib().latent_append(c_new.data_ptr(), c_stride, _dp(rope_new), rope_stride, cache.data_ptr(), C.byref(desc),
+                                 _dp(norm_weight), float(eps), slot_map.data_ptr(), T, _dp(status), _raw(stream, dev))
     _check(rc, "latent_append")
 
 
@@ -526,10 +541,11 @@ def latent_workspace(batch, num_q_heads, n_query_tokens, latent_dim, device="cud
 
 def _token_strides(name, t, B, T, H):
     """(token stride, head stride) of ``[B, T, H, D]`` (or ``[B, H, D]``: ``T = 1``), tokens numbered ``b*T + t``."""
-    if t.dim() == 3:
-        token, head, _ = t.stride()
+    strides = _bf16_rows(name, t)
+    if len(strides) == 3:
+        token, head, _ = strides
     else:
-        batch, token, head, _ = t.stride()
+        batch, token, head, _ = strides
         if T == 1:
             token = batch
         elif B > 1 and batch != T * token:
@@ -550,13 +566,10 @@ def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale
         out = _empty(shape, q_latent.dtype, q_latent.device, stream)
     elif out.shape != shape:
         raise ValueError("out: expected the shape of q_latent")
-    desc = latent_desc(cache, R)
+    desc = _desc_of(cache, R)
     rope = desc.rope_dim
-    _bf16_rows("q_latent", q_latent)
-    _bf16_rows("out", out)
     if rope > 0:
-        _bf16_rows("q_rope", q_rope)
-        if q_rope.shape[:-1] != shape[:-1] or q_rope.shape[-1] != rope:
+        if q_rope.shape != ((B, T, H, rope) if len(shape) == 4 else (B, H, rope)):
             raise ValueError("q_rope: expected [batch, tokens, heads, rope_dim]")
         qr_token, qr_head = _token_strides("q_rope", q_rope, B, T, H)
     else:
@@ -584,24 +597,21 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
     """Expanded causal attention over packed sequences: ``q [Tq,H,Dn+Dr]``, ``k_nope [Tk,H,Dn]``, ``k_rope [Tk,Dr]``,
     ``v [Tk,H,Dv]``, ``cu_q``/``cu_k`` int32[B + 1]; fills and returns ``out [Tq,H,Dv]``."""
     tq, H, D = q.shape
-    tk, _, dn = k_nope.shape
+    tk, kh, dn = k_nope.shape
     dv, dr = v.shape[2], D - dn
     if out is None:
         out = _empty((tq, H, dv), q.dtype, q.device, stream)
-    _bf16_rows("q", q)
-    _bf16_rows("k_nope", k_nope)
-    _bf16_rows("v", v)
-    _bf16_rows("out", out)
-    if k_nope.shape[1] != H or v.shape[:2] != k_nope.shape[:2]:
+    strides = _bf16_rows("q", q), _bf16_rows("k_nope", k_nope), _bf16_rows("v", v), _bf16_rows("out", out)
+    if kh != H or v.shape != (tk, H, dv):
         raise ValueError("k_nope and v: expected [key tokens, heads, dim]")
     if out.shape != (tq, H, dv):
         raise ValueError("out: expected [query tokens, heads, value dim]")
     kr_token = 0
     if dr:
-        _bf16_rows("k_rope", k_rope)
+        rope_strides = _bf16_rows("k_rope", k_rope)
         if k_rope.shape != (tk, dr):
             raise ValueError("k_rope: expected [key tokens, rope_dim]")
-        kr_token = k_rope.stride(0) if tk > 1 else 0
+        kr_token = rope_strides[0] if tk > 1 else 0
     else:
         k_rope = None
     _int32(cu_q, cu_k, status)
@@ -610,14 +620,18 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
         raise ValueError("cu_q and cu_k: expected batch + 1 entries each")
     dev = _same_device(q, k_nope, k_rope, v, out, cu_q, cu_k, status)
 
-    def st(t, tokens):  # (a dimension of extent 1 may carry any stride)
-        token, head, _ = t.stride()
-        return token if tokens > 1 else 0, head if H > 1 else 0
-
+    # (a dimension of extent 1 may carry any stride)
+    (qt, qh, _), (kt, kh, _), (vt, vh, _), (ot, oh, _) = strides
+    if H == 1:
+        qh = kh = vh = oh = 0
+    if tq <= 1:
+        qt = ot = 0
+    if tk <= 1:
+        kt = vt = 0
     with _device_call(dev):
         rc = lib().latent_prefill_attention(
-            q.data_ptr(), *st(q, tq), k_nope.data_ptr(), *st(k_nope, tk), _dp(k_rope), kr_token, v.data_ptr(), *st(v, tk),
-            cu_q.data_ptr(), cu_k.data_ptr(), n - 1, H, dn, dr, dv, min(int(max_q), tq), tq, tk, scale, out.data_ptr(), *st(out, tq),
+            q.data_ptr(), qt, qh, k_nope.data_ptr(), kt, kh, _dp(k_rope), kr_token, v.data_ptr(), vt, vh,
+            cu_q.data_ptr(), cu_k.data_ptr(), n - 1, H, dn, dr, dv, min(int(max_q), tq), tq, tk, scale, out.data_ptr(), ot, oh,
             flags, _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "latent_prefill_attention")
