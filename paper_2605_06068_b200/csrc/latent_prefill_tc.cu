@@ -10,9 +10,14 @@
 // Every MMA reads both CTAs' shares of B, so a CTA copies 40 KB a tile for 256 rows instead of 80: Q takes
 // 96 KB, and with 80 KB a tile the ring was so short (1.6 tiles) that products waited for copies; with
 // the pair it holds three tiles, and half the bytes come from L2.
-// S[0], S[1], O[0], O[1] fill the 512 columns. The halves stay in opposite phase, one's softmax under the other's
-// products: 1300 clocks of products per half and tile against 1024 of exponentials, of which every kFPolyOf-th
-// pair is taken by a polynomial on the FMA units.
+// S[0], S[1], O[0], O[1] fill the 512 columns, P lies over the S it comes from, and a thread's softmax takes 64 keys at
+// a time. Two forms of the kernel (the launch chooses, with figures there):
+//   S at once     S of the next tile follows the second 64 keys' P . V; the halves take turns, one's softmax under the
+//                 other's products: 1300 clocks of products per half and tile against 1024 of exponentials.
+//   S in two runs 64 keys each (32 of either CTA's), each taken again as soon as its own P . V is through, so a half has
+//                 scores of the next tile before its softmax is done with this one, and nobody takes turns: 10 % more
+//                 clocks of products, which read A for 64 columns only.
+// Of the exponentials every kFPolyOf-th pair is taken by a polynomial on the FMA units.
 // The softmax takes weights relative to a reference per row that is raised (and O rescaled in tensor memory)
 // only when the row's maximum passes it by more than 2^8; row sums are kept by the row's thread, of the
 // 32-bit weights; the rounding of the weights to bf16 is 2^-8 of each.
@@ -22,9 +27,9 @@
 // prompts of 200 tokens with 16 heads 102 -> 73 us), or, where there is a pair of CTAs for each block and head
 // already, the later part of the same head's keys (4 chunks of 24 tokens behind 2000..4000, 16 heads: 66 us with one
 // half, 79 with two heads, 47 with half of the keys each).
-// Measured (B200): a prompt of 8192 tokens with 32 heads 0.68 ms, 1.01 PFLOP/s (0.64 replayed from a graph), 3800
-// clocks a tile: a half's chain of S, weights (2100), P . V and the next S, of which the other half covers the most;
-// the clock is held at 1.58 GHz by the power cap. 24 prompts of 1..700 tokens with 16 heads: 77 us.
+// Measured (B200): a prompt of 8192 tokens with 32 heads 0.62 ms, 1.1 PFLOP/s; the clock is held near 1.6 GHz by the
+// power cap. 24 prompts of 1..700 tokens with 16 heads: 76 us, of which a block of 200 rows and its two tiles a half
+// take 7 us: copies of 256 KB a CTA (4000 to 5000 clocks from asking to use), two softmaxes and the output in a row.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the
 // pair's first CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are
 // bounded.
@@ -47,7 +52,7 @@ constexpr int kFKLine = 64 * 128, kFKBytes = 3 * kFKLine;  // of its 64 keys
 constexpr int kFVBytes = kFKeys * 128;                    // its line (64 dims) of all keys
 constexpr int kFStages = 3;                               // tiles
 constexpr int kFSoftWarps = 8, kFThreads = (kFSoftWarps + 4) * 32, kFProducer = 8, kFMma = 9, kFRelay = 11;  // (9, 10: one per half)
-constexpr int kFBookBytes = 3 * 1024;  // barriers, units, the list of row blocks, the second half's sums
+constexpr int kFBookBytes = 5 * 1024;  // barriers, units, the list of row blocks, the second half's sums
 constexpr int kFSmemBytes = 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes) + kFBookBytes + 1024;
 static_assert(kFSmemBytes <= 232448, "shared memory");
 // 384 threads start with 168 registers (64512 in all); the control warps keep 104 and the softmax warps take 200
@@ -93,7 +98,7 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
 // second half's are the later n1 tiles of the same head, and the first half's warps merge the two results.
 enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
 struct FUnit {
-  int row0, h, q0, nq, nq_all, k0, nk, n0, n1, dual;
+  int row0, h, q0, nq, k0, nk, n0, n1, dual;
   __device__ int first_row(int w) const { return row0 + (dual ? 0 : kFHalf * w); }
   __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
   __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
@@ -174,20 +179,23 @@ __device__ __forceinline__ void commit2_if(uint32_t leader, uint32_t bar) {
       ::"r"(bar), "r"(leader) : "memory");
 }
 
+template <bool kRuns>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFThreads, 1)
 latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_constant__ LatentPrefillParams p,
                          const __grid_constant__ FPlan plan) {
+  constexpr uint32_t kRunP = kRuns ? 64 : 32;  // columns from the first run's weights to the second's
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + 2 * kFQLines * kFQLine + kFStages * (kFKBytes + kFVBytes));
-  FUnit* units = reinterpret_cast<FUnit*>(bars + 56);               // [kFUnitSlots]
+  FUnit* units = reinterpret_cast<FUnit*>(bars + 68);               // [kFUnitSlots]
   uint32_t* list = reinterpret_cast<uint32_t*>(units + kFUnitSlots);  // [kFMaxList] sequence and block, most work first
   uint32_t* work = list + kFMaxList;                                // [kFMaxList] keys, then units of the entries before
   uint32_t* scan = work + kFMaxList;                                // [5] sequences' blocks, by warp; their sum
   uint32_t* tmem_slot = scan + 6;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   float* merge_sh = reinterpret_cast<float*>(cta_err + 1);          // [128][2]
-  static_assert(56 * 8 + kFUnitSlots * sizeof(FUnit) + 2 * kFMaxList * 4 + 8 * 4 + 1024 <= kFBookBytes, "shared memory");
+  int4* spans = reinterpret_cast<int4*>(reinterpret_cast<uint8_t*>(bars) + kFBookBytes - kFMaxList * 16);  // listed sequences' q0, nq, k0, nk
+  static_assert(68 * 8 + kFUnitSlots * sizeof(FUnit) + 2 * kFMaxList * 4 + 8 * 4 + 1024 + kFMaxList * 16 <= kFBookBytes, "shared memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1;  // in the pair
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
@@ -196,24 +204,27 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
   const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + 2 * kFQLines * kFQLine, v_sm = k_sm + kFStages * kFKBytes;
   // Barriers, at the same place in both CTAs. Of the pair's first CTA: full_k (both CTAs' copies), v_ready, bar_q,
   // bar_p, bar_turn, bar_ofree. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s,
-  // bar_pv, bar_qfree, the unit slots'. bar_p and bar_pv: [half w][keys 0..63, 64..127 of the tile].
-  const uint32_t full_k = smem_u32(bars), empty_k = full_k + 8 * kFStages, full_v = empty_k + 8 * kFStages,
-                 empty_v = full_v + 8 * kFStages, v_ready = empty_v + 8 * kFStages, bar_q = v_ready + 8 * kFStages;
-  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 16, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_qfree = bar_turn + 16,
+  // bar_pv, bar_qfree, the unit slots'. bar_s, bar_p and bar_pv: [half w][run of
+  // 64 keys] (bar_s with S at once: the first only).
+  const uint32_t full_k = smem_u32(bars), empty_k = full_k + 24 * kFStages, full_v = empty_k + 8 * kFStages,
+                 empty_v = full_v + 8 * kFStages, v_ready = empty_v + 8 * kFStages, bar_q = v_ready + 24 * kFStages;
+  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 32, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_qfree = bar_turn + 16,
                  bar_ofree = bar_qfree + 16, unit_full = bar_ofree + 16, unit_empty = unit_full + 8 * kFUnitSlots,
                  bar_drain = unit_empty + 8 * kFUnitSlots, bar_never = bar_drain + 8, bar_merge = bar_never + 8;
   if (tid == 0) {
     for (int i = 0; i < kFStages; ++i) {
-      mbar_init(full_k + 8 * i, 1);
+      for (int set = 0; set < 3; ++set) {
+        mbar_init(full_k + 8 * (kFStages * set + i), 1);
+        mbar_init(v_ready + 8 * (kFStages * set + i), 2);
+      }
       mbar_init(empty_k + 8 * i, 2);
       mbar_init(full_v + 8 * i, 1);
       mbar_init(empty_v + 8 * i, 2);
-      mbar_init(v_ready + 8 * i, 2);
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(bar_q + 8 * w, 1);
-      mbar_init(bar_s + 8 * w, 1);
       for (int k = 0; k < 2; ++k) {
+        mbar_init(bar_s + 16 * w + 8 * k, 1);
         mbar_init(bar_p + 16 * w + 8 * k, 8);  // four warps of each CTA
         mbar_init(bar_pv + 16 * w + 8 * k, 1);
       }
@@ -248,6 +259,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
   if (plan.listed && tid < kFMaxList && tid < p.batch) {
     mine = prefill_span(p, tid);
     my_blocks = (mine.nq + kFRows - 1) / kFRows;
+    spans[tid] = make_int4(mine.q0, mine.nq, mine.k0, mine.nk);
   }
   int incl = my_blocks;
   if (plan.listed && tid < kFMaxList) {
@@ -291,9 +303,19 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     __syncthreads();
     if (tid < n_blocks) list[place] = my_entry;
     __syncthreads();
-    uint32_t units_before = 0;
-    if (tid < n_blocks)
-      for (int i = 0; i < tid; ++i) units_before += units_of(list[i], p.num_heads, by_two);
+    uint32_t units = tid < n_blocks ? units_of(list[tid], p.num_heads, by_two) : 0;
+    const uint32_t my_units = units;
+    if (tid < kFMaxList) {
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, units, o);
+        if (lane >= o) units += u;
+      }
+      if (lane == 31) scan[warp] = units;
+    }
+    __syncthreads();
+    uint32_t units_before = units - my_units;
+    for (int i = 0; i < kFMaxList / 32; ++i) units_before += i < warp ? scan[i] : 0;
     if (tid < n_blocks) work[tid] = units_before;
   }
   __syncthreads();
@@ -314,14 +336,20 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     if (lane == 0) mbar_arrive_tc(unit_empty + 8 * (k % kFUnitSlots));
   };
 
+  // The barrier of a tile, from full_k or v_ready: both halves' tiles, the first half's and the second half's (dual
+  // blocks) are counted each for themselves, so that who waits for a set's barriers follows all their phases. (Three
+  // tiles of a set are in the ring at most: a barrier's next use comes behind its last one's wait.)
+  auto tile_bar = [&](uint32_t first, int set, int count) { return first + 8 * (kFStages * set + count % kFStages); };
+
   // ================= products of half w =================
-  // A warp for each half, which prepares its next products while the other's are being issued (one warp for
-  // both spent as long between the products as on them), taking turns: so the halves stay in opposite phase.
-  // (Without turns the products interleave, both halves run their softmax at the same time and the tensor core
-  // waits.)
+  // A warp for each half, which prepares its next products while the other's are being issued (one warp for both
+  // spent as long between the products as on them). Where S is taken at once, they take turns: so the halves stay in
+  // opposite phase (without, both ran their softmax at the same time and the tensor core waited: 0.89 ms instead of 0.61
+  // for the 8192-token prompt).
   auto issue_role = [&](auto half) {
     constexpr int w = decltype(half)::value;
-    constexpr uint32_t idesc_s = latent_idesc(256, kFKeys, false, false), idesc_o = latent_idesc(256, 128, false, true);
+    constexpr uint32_t idesc_s = latent_idesc(256, kFKeys, false, false), idesc_run = latent_idesc(256, kFKeys / 2, false, false),
+                       idesc_o = latent_idesc(256, 128, false, true);
     const uint32_t leader = elect_one();
     const uint32_t u_q = uniform(q_sm + w * kFQLines * kFQLine), u_k = uniform(k_sm), u_v = uniform(v_sm), u_tmem = uniform(tmem);
     const uint32_t u_ek = uniform(empty_k), u_ev = uniform(empty_v);
@@ -329,67 +357,75 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     auto wait = [&](uint32_t bar, int phase) {
       if (ok) ok = __all_sync(0xffffffffu, mbar_spin_cluster(bar, phase & 1));
     };
-    auto s_product = [&](uint32_t k_addr) {
-      const uint64_t q0 = tc_desc(u_q, 16, 1024), k0 = tc_desc(k_addr, 16, 1024);
+    // S of a tile at once, or of run k of two: of each CTA's 64 keys those from 32 k on
+    auto s_product = [&](uint32_t k_addr, int k, uint32_t idesc) {
+      const uint64_t q0 = tc_desc(u_q, 16, 1024), k0 = tc_desc(k_addr, 16, 1024) + 256 * k;
 #pragma unroll
       for (int ln = 0; ln < kFQLines; ++ln)
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
-          mma2_ss_if(leader, d_s, q0 + ln * (kFQLine / 16) + 2 * ks, k0 + ln * (kFKLine / 16) + 2 * ks, idesc_s, (ln > 0 || ks > 0) ? 1u : 0u);
-      commit2_if(leader, bar_s + 8 * w);
+          mma2_ss_if(leader, d_s + 64 * k, q0 + ln * (kFQLine / 16) + 2 * ks, k0 + ln * (kFKLine / 16) + 2 * ks, idesc, (ln > 0 || ks > 0) ? 1u : 0u);
+      commit2_if(leader, bar_s + 16 * w + 8 * k);
     };
     FUnit un;
     // Before this unit: tiles of the pair; of this half; units of this half; tiles on which the halves take turns.
     int t0 = 0, mine = 0, done = 0, turns = 0;
+    int counts[2] = {0, 0};  // tiles of blocks of two halves; of dual ones, this half's
     for (int k = 0; next_unit(k, un); ++k) {
       free_unit(k);
       const int n = uniform(w == 0 ? un.n0 : un.n1), n_other = uniform(w == 0 ? un.n1 : un.n0);
       const int dual = uniform(un.dual);
-      const int step = dual ? 2 : 1, own = dual ? w : 0, other = 1 - w;  // this half's tiles: t0 + step * j + own
-      // Both halves give a tile back. The one that does not read it does so as soon as it is there (not before: a
-      // half that did not follow every phase of a barrier could not tell the phases apart) and goes on, to the next
-      // unit where this was the last tile.
-      auto hand_on = [&](uint32_t full, uint32_t empty, int t) {
-        const int st = t % kFStages;
-        wait(full + 8 * st, t / kFStages);
-        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty + 8 * st, lane));
+      const int step = dual ? 2 : 1, own = dual ? w : 0;  // this half's tiles: t0 + step * j + own
+      const int set = dual ? 1 + w : 0, c0 = counts[dual ? 1 : 0];  // this unit's tiles on the set's barriers: c0 + j
+      // Both halves give a tile of a block of two halves back. The one that does not read it does so as soon as it is
+      // there (see tile_bar) and goes on, to the next unit where this was the last tile.
+      auto hand_on = [&](uint32_t full, uint32_t empty, int j) {
+        wait(tile_bar(full, 0, c0 + j), (c0 + j) / kFStages);
+        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty + 8 * ((t0 + j) % kFStages), lane));
         __syncwarp();
       };
-      if (dual && w == 1 && n > 0) hand_on(full_k, empty_k, t0);  // (dual: both halves have n tiles, or none)
+      // (a tile of a dual block is given back twice by its half)
+      auto give_back = [&](uint32_t bar) {
+        commit2_if(leader, bar);
+        if (dual) commit2_if(leader, bar);
+      };
       if (n > 0) {  // S(0): its place is free, the tensor core works a thread's products off in order
         const int t = t0 + own, sk = t % kFStages;
         wait(bar_q + 8 * w, done);
-        wait(full_k + 8 * sk, t / kFStages);
+        wait(tile_bar(full_k, set, c0), c0 / kFStages);
         if (!ok) break;
         tc_fence_after();
-        s_product(uniform(u_k + sk * kFKBytes));
+        const uint32_t k_addr = uniform(u_k + sk * kFKBytes);
+        s_product(k_addr, 0, kRuns ? idesc_run : idesc_s);
+        if constexpr (kRuns) s_product(k_addr, 1, idesc_run);
         if (n == 1) commit2_if(leader, bar_qfree + 8 * w);
-        commit2_if(leader, uniform(u_ek + 8 * sk));
+        give_back(uniform(u_ek + 8 * sk));
       }
-      if (dual && w == 0 && n > 0) hand_on(full_k, empty_k, t0 + 1);
       for (int j = 0; j < n; ++j) {
         const int t = t0 + step * j + own, tn = t + step, sv = t % kFStages, sk = tn % kFStages;
-        // turn i: half 0 after half 1's turn i - 1, half 1 after half 0's turn i
-        const bool taking_turns = j < n_other;
-        const int turn = turns + j;
-        const uint32_t turn_bar = taking_turns && (w == 1 || turn > 0) ? bar_turn + 8 * w : 0u;
-        const int turn_phase = w == 1 ? turn : turn - 1;
-        if (dual && w == 1) hand_on(v_ready, empty_v, t - 1);
-        wait(v_ready + 8 * sv, t / kFStages);
+        wait(tile_bar(v_ready, set, c0 + j), (c0 + j) / kFStages);
         const uint64_t v0 = tc_desc(uniform(u_v + sv * kFVBytes), 16, 1024);
         const uint32_t k_addr = uniform(u_k + sk * kFKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
         const uint32_t acc = uniform(j > 0 ? 1u : 0u);
         if (j == 0 && done > 0) wait(bar_ofree + 8 * w, done - 1);  // the last unit's output has been read
-        // the tile's first 64 keys as soon as their weights are there, under the softmax of the other 64
+        // turn i: half 0 after half 1's turn i - 1, half 1 after half 0's turn i
+        const bool taking_turns = !kRuns && j < n_other;
+        const int turn = turns + j;
+        const uint32_t turn_bar = taking_turns && (w == 1 || turn > 0) ? bar_turn + 8 * w : 0u;
+        const int turn_phase = w == 1 ? turn : turn - 1;
+        // (a run's keys: 64 k .. 64 k + 63 of the tile; in two runs 32 k .. 32 k + 31 and the same from 64 on)
+        const uint64_t v_lo = v0 + (kRuns ? 256u : 512u), v_hi = v0 + (kRuns ? 256u : 0u);
         wait(bar_p + 16 * w, mine + j);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, (ks < 2 ? v0 : v_hi) + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
         commit2_if(leader, bar_pv + 16 * w);
-        if (j + 1 < n) {
-          if (dual && w == 1) hand_on(full_k, empty_k, tn - 1);
-          wait(full_k + 8 * sk, tn / kFStages);
+        if (j + 1 < n) wait(tile_bar(full_k, set, c0 + j + 1), (c0 + j + 1) / kFStages);
+        if (kRuns && j + 1 < n) {
+          if (!ok) break;
+          tc_fence_after();
+          s_product(k_addr, 0, idesc_run);  // over these weights: the tensor core works a thread's products off in order
         }
         {  // the other weights and the turn, looked for at once by different lanes
           const bool second = (lane & 1) && turn_bar != 0u;
@@ -398,27 +434,23 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int ks = 4; ks < 8; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + 128 * ks, idesc_o, 1u);
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + kRunP + 8 * ks, (ks < 2 ? v_lo : v_lo + v_hi - v0) + 128 * ks, idesc_o, 1u);
         commit2_if(leader, bar_pv + 16 * w + 8);
-        // S(j + 1) takes the place of P(j): the tensor core works a thread's products off in order
-        if (j + 1 < n) s_product(k_addr);
-        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * other);
+        if (j + 1 < n) s_product(k_addr, kRuns ? 1 : 0, kRuns ? idesc_run : idesc_s);
+        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * (1 - w));
         if (j + 2 == n) commit2_if(leader, bar_qfree + 8 * w);
-        commit2_if(leader, ev);
-        if (j + 1 < n) commit2_if(leader, ek);
-        if (dual && w == 0) {
-          hand_on(v_ready, empty_v, t + 1);
-          if (j + 1 < n) hand_on(full_k, empty_k, tn + 1);
-        }
+        give_back(ev);
+        if (j + 1 < n) give_back(ek);
       }
       if (!dual)
-        for (int t = t0 + n; ok && t < t0 + n_other; ++t) {
-          hand_on(full_k, empty_k, t);
-          hand_on(v_ready, empty_v, t);
+        for (int j = n; ok && j < n_other; ++j) {
+          hand_on(full_k, empty_k, j);
+          hand_on(v_ready, empty_v, j);
         }
       if (!ok) break;
       t0 += dual ? n + n_other : max(n, n_other);
-      turns += min(n, n_other);
+      if (dual) counts[1] += n; else counts[0] += max(n, n_other);
+      if (!kRuns) turns += min(n, n_other);
       mine += n;
       if (n > 0) ++done;
     }
@@ -436,30 +468,55 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       // ================= units, and TMA: this CTA's rows of Q, keys of K, dims of V =================
       const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
       const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
-      const uint32_t to_q = uniform(in_cta(bar_q, 0)), to_k = uniform(in_cta(full_k, 0));
+      const uint32_t to_q = uniform(in_cta(bar_q, 0));
       const int64_t n_units = plan.slots > 0 ? plan.slots * p.num_heads
                               : !plan.listed ? static_cast<int64_t>(plan.q_blocks) * p.batch * p.num_heads
                               : n_blocks == 0 ? 0 : static_cast<int64_t>(work[n_blocks - 1]) + units_of(list[n_blocks - 1], p.num_heads, by_two);
       int64_t round = 0;
+      auto make_unit = [&](FUnit& un, int qb, int h, int4 span) {
+        const int nq = span.y, nk = span.w;
+        // keys that the last row of half w can see, in tiles (of either CTA: the pair walks together)
+        int n[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int from = qb * kFRows + kFHalf * w, last = min(from + kFHalf - 1, nq - 1);
+          const int see = from >= nq ? 0 : min(max(nk - nq + last + 1, 0), nk);
+          n[w] = (see + kFKeys - 1) / kFKeys;
+        }
+        int dual = kOneHead;
+        if (by_two && nq - qb * kFRows <= kFHalf && h + 1 < p.num_heads) {
+          dual = kTwoHeads;
+          n[1] = n[0];
+        } else if (!by_two && n[0] > 1 && n[1] == 0) {  // (the second half has no rows, and pairs are not short)
+          dual = kSplitKeys;
+          n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last visible key)
+        }
+        un = FUnit{qb * kFRows, h, span.x, nq, span.z, nk, n[0], n[1], dual};
+      };
       // The pair's next unit: every pairs-th of the order, to and fro, so that each pair gets early (long) and late
       // (short) ones. Unlisted blocks may be empty: 32 at a time are looked at.
       auto find_unit = [&](FUnit& un) {
+        if (plan.listed) {
+          while (round * pairs < n_units) {
+            const int r = static_cast<int>(round++), at = r * pairs + (r & 1 ? pairs - 1 - pair : pair);
+            if (at >= n_units) continue;
+            int entry = -1;  // the last one whose units start at or before this one
+#pragma unroll
+            for (int i = 0; i < kFMaxList; i += 32)
+              entry += __popc(__ballot_sync(0xffffffffu, i + lane < n_blocks && work[i + lane] <= static_cast<uint32_t>(at)));
+            const uint32_t e = list[entry];
+            const int h = at - static_cast<int>(work[entry]);
+            make_unit(un, (e & (kFSmallBlock - 1)) >> 7, by_two && (e & kFSmallBlock) ? 2 * h : h, spans[e & 127]);
+            return true;
+          }
+          return false;
+        }
         while (true) {
           const int64_t r = round + lane, at = r * pairs + (r & 1 ? pairs - 1 - pair : pair);
           int qb = 0, b = 0, h = 0;
           PrefillSpan sp{0, 0, 0, 0, 0};
           if (at < n_units) {
-            if (plan.listed) {
-              int lo = 0, hi = n_blocks;  // work[lo] <= at < work[hi]
-              while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (work[mid] <= at) lo = mid; else hi = mid;
-              }
-              const uint32_t e = list[lo];
-              h = static_cast<int>(at - work[lo]);
-              b = e & 127;
-              qb = (e & (kFSmallBlock - 1)) >> 7;
-            } else if (plan.slots > 0) {
+            if (plan.slots > 0) {
               // Sequence b's blocks stand from place cu_q[b] / kFRows + b on: the next sequence's come behind them,
               // and all places are one a sequence and one for every kFRows tokens.
               h = static_cast<int>(at % p.num_heads);
@@ -491,29 +548,13 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
           }
           const int src = __ffs(have) - 1;
           round += src + 1;
-          // keys that the last row of half w can see, in tiles (of either CTA: the pair walks together)
-          int n[2];
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const int from = qb * kFRows + kFHalf * w, last = min(from + kFHalf - 1, sp.nq - 1);
-            const int see = from >= sp.nq ? 0 : min(max(sp.nk - sp.nq_all + last + 1, 0), sp.nk);
-            n[w] = (see + kFKeys - 1) / kFKeys;
-          }
           auto from_lane = [&](int v) { return __shfl_sync(0xffffffffu, v, src); };
-          int dual = kOneHead;
-          if (small && h + 1 < p.num_heads) {
-            dual = kTwoHeads;
-            n[1] = n[0];
-          } else if (!by_two && n[0] > 1 && n[1] == 0) {  // (the second half has no rows, and pairs are not short)
-            dual = kSplitKeys;
-            n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last visible key)
-          }
-          un = FUnit{from_lane(qb * kFRows), from_lane(h), from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.nq_all), from_lane(sp.k0),
-                     from_lane(sp.nk), from_lane(n[0]), from_lane(n[1]), from_lane(dual)};
+          make_unit(un, from_lane(qb), from_lane(h), make_int4(from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.k0), from_lane(sp.nk)));
           return true;
         }
       };
       int t = 0, done[2] = {0, 0};  // tiles so far; units of each half so far
+      int counts[3] = {0, 0, 0};    // tiles so far by set of barriers
       for (int k = 0;; ++k) {
         FUnit un;
         const bool more = find_unit(un);
@@ -544,12 +585,16 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
           const int st = uniform(t % kFStages), rnd = t / kFStages;
           if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_k + 8 * st, (rnd - 1) & 1));
           if (!ok) break;
-          mbar_expect_tx_if(first, full_k + 8 * st, 2 * kFKBytes);
+          const int set = un.dual ? 1 + (i & 1) : 0;
+          const int count = set == 0 ? counts[0] : set == 1 ? counts[1] : counts[2];
+          const uint32_t bar = uniform(tile_bar(full_k, set, count)), to_k = uniform(in_cta(bar, 0));
+          if (set == 0) ++counts[0]; else if (set == 1) ++counts[1]; else ++counts[2];
+          mbar_expect_tx_if(first, bar, 2 * kFKBytes);
           const int key = uniform(key0 + un.keys_of(i) * kFKeys), my_key = key + 64 * rank;
           const uint32_t kd = u_k + st * kFKBytes;
-          tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k + 8 * st, 0, u_h, my_key);
-          tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k + 8 * st, 1, u_h, my_key);
-          tma_load_4d_pair_if(leader, kd + 2 * kFKLine, &maps.k_rope, to_k + 8 * st, 0, 0, my_key);
+          tma_load_4d_pair_if(leader, kd, &maps.k_nope, to_k, 0, u_h, my_key);
+          tma_load_4d_pair_if(leader, kd + kFKLine, &maps.k_nope, to_k, 1, u_h, my_key);
+          tma_load_4d_pair_if(leader, kd + 2 * kFKLine, &maps.k_rope, to_k, 0, 0, my_key);
           if (i == 0 && un.n1 > 0) load_q(1);
           if (ok && rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_v + 8 * st, (rnd - 1) & 1));
           if (!ok) break;
@@ -564,7 +609,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
       }
     } else if (warp == kFRelay) {
       // ================= V tiles: cleared behind the sequence's end, then handed to the first CTA =================
-      const uint32_t to = in_cta(v_ready, 0);
+      int counts[3] = {0, 0, 0};  // tiles so far by set of barriers
       FUnit un;
       int t = 0;
       for (int k = 0; next_unit(k, un); ++k) {
@@ -581,10 +626,14 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
               asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * kFVBytes + valid * 128 + c * 16), "r"(0));
             fence_proxy_async();
           }
+          const int set = un.dual ? 1 + (i & 1) : 0;
+          const int count = set == 0 ? counts[0] : set == 1 ? counts[1] : counts[2];
+          const uint32_t to = in_cta(tile_bar(v_ready, set, count), 0);
+          if (set == 0) ++counts[0]; else if (set == 1) ++counts[1]; else ++counts[2];
           __syncwarp();
           if (lane == 0) {
-            if (valid < kFKeys) arrive_cluster(to + 8 * st);  // (with what has been written before it)
-            else arrive_cluster_tc(to + 8 * st);
+            if (valid < kFKeys) arrive_cluster(to);  // (with what has been written before it)
+            else arrive_cluster_tc(to);
           }
         }
         if (!ok) break;
@@ -614,26 +663,33 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         FUnit un;
         if (!next_unit(unit, un)) break;
         n = w == 0 ? un.n0 : un.n1;
-        seen = min(un.nk, un.nk - un.nq_all + un.first_row(w) + 128 * rank + (tid & 127) + 1) - un.key_tile(w, 0) * kFKeys;
+        const int row = un.first_row(w) + 128 * rank + (tid & 127);
+        // (a warp without any row sees nothing; one with some goes by the mask, so as not to take the slower way)
+        seen = row - lane < un.nq ? min(un.nk, un.nk - un.nq + row + 1) - un.key_tile(w, 0) * kFKeys : 0;
       }
       float m_ref = kFNoMax, l = 0.f;
-      for (int j = 0; j < n; ++j, ++t) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 8 * w, t & 1));
-        if (!ok) break;
-        tc_fence_after();
+      // One tile; masked: some row of the warp does not see all of it.
+      auto tile = [&](auto masked, int j) {
+        constexpr bool kMasked = decltype(masked)::value;
         const int vis = seen - j * kFKeys;  // visible columns of this row
-        const bool edge = __any_sync(0xffffffffu, vis < kFKeys);
         // 64 keys at a time; the first run's products start while the second run is here
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
+          if (kRuns || k == 0) {
+            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 16 * w + 8 * k, t & 1));
+            if (!ok) return;
+            tc_fence_after();
+          }
           uint32_t sv[64];
           tmem_ld32(my_s + 64 * k, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
           tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
           tmem_wait_ld();
-          if (edge) {
+          // keys of the run's columns: 64 k + e, or 32 k + e, from the 32nd on 32 k + 32 + e
+          const int vis_lo = vis - (kRuns ? 32 * k : 64 * k), vis_hi = vis - (kRuns ? 32 * k + 32 : 64 * k);
+          if (kMasked) {
 #pragma unroll
             for (int e = 0; e < 64; ++e)
-              if (64 * k + e >= vis) sv[e] = 0xff800000u;  // -inf
+              if (e >= (e < 32 ? vis_lo : vis_hi)) sv[e] = 0xff800000u;  // -inf
           }
           if (k == 0 && j == 0) {  // the first reference: the maximum of the first 64 scores
             float mx[2] = {neg_inf, neg_inf};
@@ -672,8 +728,13 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
           };
           while (true) {
-            if (edge) weights(std::false_type{});  // (weights of hidden keys are exactly zero)
-            else weights(std::true_type{});
+            if (kMasked && __all_sync(0xffffffffu, vis_lo <= 0)) {  // no row of the warp sees any of these
+#pragma unroll
+              for (int e = 0; e < 32; ++e) pk[e] = 0;
+              part = 0.f;
+              break;
+            }
+            weights(std::bool_constant<!kMasked>{});  // (weights of hidden keys are exactly zero)
             if (!__any_sync(0xffffffffu, top > m_ref + kFRescale)) break;
             const float m_new = fmaxf(m_ref, top), a = ex2(m_ref - m_new);
             m_ref = m_new;
@@ -693,16 +754,19 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
               }
             }
           }
-          if (!ok) break;
+          if (!ok) return;
           l += part;
-          tmem_st32(my_s + 32 * k, pk);
+          tmem_st32(my_s + kRunP * k, pk);
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) arrive_cluster_tc(to_p + 8 * k);
         }
-        if (!ok) break;
-      }
+      };
+      // (the tiles that every row of the warp sees come first)
+      const int n_full = min(n, __reduce_min_sync(0xffffffffu, max(seen, 0)) / kFKeys);
+      for (int j = 0; ok && j < n_full; ++j, ++t) tile(std::false_type{}, j);
+      for (int j = n_full; ok && j < n; ++j, ++t) tile(std::true_type{}, j);
       // ---- output
       if (n > 0) {
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (t - 1) & 1));
@@ -831,11 +895,10 @@ cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t 
       !encode_rows(enc, &maps.k_rope, p.k_rope, 64, 1, p.total_k, 0, p.kr_token_stride, 64) ||
       !encode_rows(enc, &maps.v, p.v, 128, p.num_heads, p.total_k, p.v_head_stride, p.v_token_stride, kFKeys))
     return cudaErrorNotSupported;
-  cudaError_t e = cudaFuncSetAttribute(latent_prefill_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFSmemBytes);
-  if (e != cudaSuccess) return e;
   // One pair of CTAs per two SMs at most; the row blocks of all sequences are at most one a sequence and one for
   // every kFRows query tokens.
   int dev = 0, sms = 0;
+  cudaError_t e;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
   const int q_blocks = (p.max_q + kFRows - 1) / kFRows;
@@ -846,7 +909,17 @@ cudaError_t launch_latent_prefill_tc(const LatentPrefillParams& p, cudaStream_t 
   const int listed = most <= kFMaxList ? 1 : 0;
   const FPlan plan{q_blocks, listed, !listed && static_cast<int64_t>(p.batch) * q_blocks > 4 * places ? places : 0};
   const int64_t pairs = std::min(most * p.num_heads, static_cast<int64_t>(std::max(sms / 2, 1)));
-  latent_prefill_tc_kernel<<<static_cast<unsigned>(2 * pairs), kFThreads, kFSmemBytes, stream>>>(maps, p, plan);
+  // S in two runs where the units have many tiles: very many keys a sequence and rows enough for both halves, or fewer
+  // units than pairs of CTAs (then the chain of one half is what is left, not power or copies). Both ways measured (at
+  // once, in two runs): a prompt of 8192, 32 heads 625 and 613 us; chunks of 500..1024 behind 1000..16384, 16 heads
+  // 170 and 165; 7 chunks of 8..408 behind 1500..3000, 4 heads 62 and 52; but prompts of 1..700, 16 heads 75 and 78;
+  // chunks of 700 behind 1500..3000, 16 heads 178 and 188; 40 chunks of 24 behind 2000..4000, 16 heads 316 and 339.
+  // (By what the call's totals say, not by max_q: the result does not depend on how loose a bound that is.)
+  const bool runs = places * p.num_heads <= sms / 2 ? p.total_k >= 1024ll * p.batch
+                                                    : p.total_k >= 4096ll * p.batch && p.total_q >= static_cast<int64_t>(kFHalf) * p.batch;
+  const auto kernel = runs ? latent_prefill_tc_kernel<true> : latent_prefill_tc_kernel<false>;
+  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFSmemBytes)) != cudaSuccess) return e;
+  kernel<<<static_cast<unsigned>(2 * pairs), kFThreads, kFSmemBytes, stream>>>(maps, p, plan);
   return cudaGetLastError();
 }
 

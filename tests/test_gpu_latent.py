@@ -470,6 +470,11 @@ def test_expanded_loose_bound_of_the_query_tokens(flags):
     run_expanded([3, 0, 1, 40] * 50, [9, 5, 1, 60] * 50, 2, seed=19, max_q=most, flags=flags)
 
 
+def test_expanded_result_does_not_depend_on_the_bound():
+    outs = [run_expanded([130, 300, 70] * 6, [1200, 2300, 900] * 6, 3, seed=22, max_q=m)[3] for m in (300, 513, 10000)]
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
 @pytest.mark.parametrize("long_at", [0, 77, 149])
 @pytest.mark.parametrize("gap", [0, 700])
 def test_expanded_one_long_among_many_short(long_at, gap):
@@ -508,6 +513,26 @@ def test_expanded_bad_ranges_among_many(flags):
     no_rows = cq[:100] + [cq[100]] * 2 + cq[102:]            # sequence 100 has no rows, and keys out of range
     x, st = call(no_rows, [0] * 100 + [5, 0] + [0] * (B - 101), 2600)
     assert st == 2
+
+
+@pytest.mark.parametrize("q_lens,k_lens,H", [([700, 300, 513], [5000, 4300, 4700], 41), ([8192], [8192], 6), ([257], [20000], 1),
+                                             ([600, 40, 1100], [1500, 1024, 1100], 2), ([300] * 3, [12500, 130, 300], 30)])
+@pytest.mark.parametrize("spread", [1.0, 20.0])
+def test_expanded_many_keys(q_lens, k_lens, H, spread):
+    """Long contexts, with several row blocks per pair of CTAs and with fewer than there are."""
+    run_expanded(q_lens, k_lens, H, seed=21, spread=spread)
+
+
+@pytest.mark.parametrize("token", [0, 31, 33, 70, 100, 2000, 4130])
+def test_expanded_nan_among_many_keys(token):
+    """A NaN in one key reaches the rows that see it and no other."""
+    nq, nk, H = 600, 4200, 2
+    q, kv, kr = randn(1, nq, H, 192), randn(2, nk, H, 256), randn(3, nk, 64)
+    kv[token, 1, 5] = float("nan")
+    out = pda.latent_prefill_attention(q.cuda(), kv[..., :128].cuda(), kr.cuda(), kv[..., 128:].cuda(), ints([0, nq]), ints([0, nk]), nq, 0.07)
+    nan = out.float().isnan().any(-1).cpu()
+    sees = torch.arange(nq) + nk - nq >= token
+    assert not nan[:, 0].any() and (nan[:, 1] == sees).all()
 
 
 def test_expanded_huge_values_behind_the_mask():
