@@ -24,9 +24,9 @@
 // Each pair of CTAs works through several row blocks, those with the most keys first and dealt to and fro; the
 // producer runs on into the next block's Q, K and V while the last one's output is written.
 // A block of at most 256 rows would leave the second half idle. It gets the same rows of the next head instead (64
-// prompts of 200 tokens with 16 heads 102 -> 73 us), or, where there is a pair of CTAs for each block and head
+// prompts of 200 tokens with 16 heads: 102 us one head at a time, 83 two), or, where there is a pair of CTAs for each block and head
 // already, the later part of the same head's keys (4 chunks of 24 tokens behind 2000..4000, 16 heads: 66 us with one
-// half, 79 with two heads, 47 with half of the keys each).
+// half, 79 with two heads, 49 with half of the keys each).
 // Measured (B200): a prompt of 8192 tokens with 32 heads 0.62 ms, 1.1 PFLOP/s; the clock is held near 1.6 GHz by the
 // power cap. 24 prompts of 1..700 tokens with 16 heads: 76 us, of which a block of 200 rows and its two tiles a half
 // take 7 us: copies of 256 KB a CTA (4000 to 5000 clocks from asking to use), two softmaxes and the output in a row.
