@@ -81,7 +81,8 @@ struct LMaps {
 };
 
 // A sequence that continues behind its first span: see latent_merge_kernel. One per group (the sequence that
-// leaves its span), or one per sequence where those are fewer. vseq < 0: none.
+// leaves its span), or one per sequence where those are fewer. vseq < 0: none. Every record is written by every
+// call, after an expired wait too and whatever *status holds: the merge takes them for addresses.
 struct LRecord {
   int32_t vseq, first_slot, n_seg, group;
 };
@@ -237,10 +238,8 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kLTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // once a CTA of this launch has met an expired wait, the rest find no work (the output is lost anyway)
   const LatentWorkspace lay = latent_workspace_layout(p.num_q_heads, p.n_q, geo.latent_dim);
   uint8_t* ws = static_cast<uint8_t*>(p.workspace);
-  const int status_now = p.status != nullptr ? *reinterpret_cast<volatile int32_t*>(p.status) : 0;
   // ---- this group's span of the tile list: every thread sums a run of sequences, then the sums are scanned
   const int per_thread = (p.batch + kLThreads - 1) / kLThreads;
   const int b0 = min(tid * per_thread, p.batch), b1 = min(b0 + per_thread, p.batch);
@@ -254,7 +253,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   }
   if (lane == 31) scan[warp] = incl;
   tc_fence_before();
-  const bool dead = __syncthreads_or(status_now == PDA_DEV_TIMEOUT);
+  __syncthreads();
   tc_fence_after();
   uint32_t list = 0, before = 0;
 #pragma unroll
@@ -271,7 +270,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
   const int span_tiles = max(static_cast<int>((total + plan.groups - 1) / plan.groups),
                              list <= 2 * sequences || list > 32 * sequences ? 2 : 1);
   const int64_t start = static_cast<int64_t>(g) * span_tiles;
-  if (start < total && !dead) {
+  if (start < total) {
     const uint32_t pass = static_cast<uint32_t>(start) / list, in_pass = static_cast<uint32_t>(start) - pass * list;
     if (in_pass >= before && in_pass < before + mine) {  // (one thread)
       uint32_t at = before;
@@ -741,7 +740,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
       soft_sync();  // (row_off and inv_l are free again)
     }
     if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
-    if (r == 0 && tid == 0 && (!plan.by_sequence || (dead && g < p.batch * plan.passes))) records[g] = rec;
+    if (r == 0 && tid == 0 && !plan.by_sequence) records[g] = rec;
   }
 
   // ---- teardown
