@@ -659,6 +659,9 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     int t = 0, merges = 0;  // tiles of this half, merges with the second half so far
     for (int unit = 0;; ++unit) {
       int n, seen;  // tiles; columns that this thread's row sees, from the half's first tile on
+      // The row's reference. A row behind the sequence's last is another sequence's, or anything: its reference is
+      // infinite, so that it never asks for the warp's to be raised and has no say in the other rows' rounding.
+      float m_ref;
       {
         FUnit un;
         if (!next_unit(unit, un)) break;
@@ -666,8 +669,9 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         const int row = un.first_row(w) + 128 * rank + (tid & 127);
         // (a warp without any row sees nothing; one with some goes by the mask, so as not to take the slower way)
         seen = row - lane < un.nq ? min(un.nk, un.nk - un.nq + row + 1) - un.key_tile(w, 0) * kFKeys : 0;
+        m_ref = row < un.nq ? kFNoMax : INFINITY;
       }
-      float m_ref = kFNoMax, l = 0.f;
+      float l = 0.f;
       // One tile; masked: some row of the warp does not see all of it.
       auto tile = [&](auto masked, int j) {
         constexpr bool kMasked = decltype(masked)::value;
@@ -695,7 +699,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
             for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-            m_ref = fmaxf(kFNoMax, fmaxf(mx[0], mx[1]) * scale_log2);
+            m_ref = fmaxf(m_ref, fmaxf(mx[0], mx[1]) * scale_log2);
           }
           // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
           // reference by so much that the reference is raised and the weights are taken again.

@@ -36,3 +36,54 @@ def test_absorbed_with_a_status_word_that_holds_an_expired_wait(lens):
     ref, tol = U.absorbed(ql, qr, pg.host, pg.table, lens, 0.07, 512)
     U.check(out, ref, tol)
     assert st.item() == 3
+
+
+# ---- memory behind a sequence ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("q_lens,k_lens,H", [([40], [1000], 3),             # the keys of a small block split over the halves
+                                             ([77], [77], 4), ([150, 9] * 40, [150, 300] * 40, 4),   # two heads at once
+                                             ([530], [4600], 2),            # S in two runs
+                                             ([300, 513], [700, 513], 60)])  # several row blocks per pair of CTAs
+def test_expanded_bits_do_not_depend_on_the_queries_behind(q_lens, k_lens, H):
+    """The rows that share a warp with a sequence's last ones are the next sequence's or anything: with other (finite,
+    large) values there, the same bits. The keys' size grows, so that such a row's scores pass its first ones again
+    and again."""
+    B = len(q_lens)
+    cq = [int(x) for x in np.concatenate([[0], np.cumsum(np.asarray(q_lens) + 50)])]    # 50 rows of nobody's behind each
+    ck = [int(x) for x in np.concatenate([[0], np.cumsum(k_lens)])]
+    q, kv, kr = randn(1, cq[-1], H, 192), randn(2, ck[-1], H, 256), randn(3, ck[-1], 64)
+    for b in range(B):
+        kv[ck[b]:ck[b + 1], :, :128] *= torch.linspace(0.2, 2, k_lens[b])[:, None, None]
+    dkv, dkr = kv.cuda(), kr.cuda()
+    outs = []
+    for spread in (0.0, 1.0, 30.0):
+        d = q.clone()
+        out = torch.zeros((cq[-1], H, 128), dtype=torch.bfloat16, device="cuda")
+        for b in range(B):
+            end = cq[b] + q_lens[b]
+            d[end:end + 50] = randn(100 + b, 50, H, 192) * spread
+        dq = d.cuda()
+        for b in range(0, B, 10):   # one call cannot leave rows between sequences out: a call for every tenth, at its place
+            pda.latent_prefill_attention(dq[cq[b]:], dkv[..., :128], dkr, dkv[..., 128:], ints([0, q_lens[b]]), ints(ck[b:b + 2]),
+                                         q_lens[b], 0.07, out=out[cq[b]:])
+        outs.append(out)
+        # all sequences in one call, their queries packed: behind each but the last stand the next one's
+        packed = torch.cat([d[cq[b]:cq[b] + q_lens[b]] for b in range(B)] + [d[cq[-1] - 50:]]).cuda()
+        cu = [int(x) for x in np.concatenate([[0], np.cumsum(q_lens)])]
+        outs.append(pda.latent_prefill_attention(packed, dkv[..., :128], dkr, dkv[..., 128:], ints(cu), ints(ck), max(q_lens), 0.07,
+                                                 out=torch.zeros((cu[-1] + 50, H, 128), dtype=torch.bfloat16, device="cuda")))
+    for a, b in ((0, 2), (0, 4), (1, 3), (1, 5)):
+        assert torch.equal(outs[a], outs[b])
+
+
+def test_expanded_bits_do_not_depend_on_the_next_sequence():
+    """The same first sequence before two different second ones."""
+    n, k, H = [70, 33], [900, 60], 3
+    q, kv, kr = randn(4, sum(n), H, 192), randn(5, sum(k), H, 256), randn(6, sum(k), 64)
+    kv[:900, :, :128] *= torch.linspace(0.2, 2, 900)[:, None, None]
+    outs = []
+    for spread in (1.0, 40.0):
+        q[70:] = randn(7, 33, H, 192) * spread
+        outs.append(pda.latent_prefill_attention(q.cuda(), kv[..., :128].cuda(), kr.cuda(), kv[..., 128:].cuda(), ints([0, 70, 103]),
+                                                 ints([0, 900, 960]), 70, 0.07)[:70])
+    assert torch.equal(outs[0], outs[1])
