@@ -1,6 +1,8 @@
 // The plain kernels of the two latent-attention forms, for shapes outside the tensor-core kernels: one CTA
 // per query row, scores by a warp per token, the running maximum and sum of the softmax over blocks of
 // tokens, everything in 32 bits. Bound by reading every row once per query row.
+#include <cfloat>
+
 #include "latent.cuh"
 
 namespace pda {
@@ -34,7 +36,8 @@ __device__ __forceinline__ void attend_row(const float* q_sh, int da, int db, in
   float acc[kGenMaxDims];
 #pragma unroll
   for (int e = 0; e < kGenMaxDims; ++e) acc[e] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  // (the maximum starts at the lowest finite number, so that scores of -inf get a weight of 0 and not inf - inf)
+  float m = -FLT_MAX, l = 0.f;
   for (int j0 = 0; j0 < n; j0 += kGenBlock) {
     const int nb = min(kGenBlock, n - j0);
     __syncthreads();
@@ -51,7 +54,7 @@ __device__ __forceinline__ void attend_row(const float* q_sh, int da, int db, in
     __syncthreads();
     const float bm = block_reduce(tid < nb ? p_sh[tid] : -INFINITY, true, red_sh);
     const float m_new = fmaxf(m, bm);
-    const float keep = m == -INFINITY ? 0.f : expf(m - m_new);
+    const float keep = expf(m - m_new);
     const float w = tid < nb ? expf(p_sh[tid] - m_new) : 0.f;
     l = l * keep + block_reduce(w, false, red_sh);
     if (tid < nb) p_sh[tid] = w;
@@ -67,7 +70,7 @@ __device__ __forceinline__ void attend_row(const float* q_sh, int da, int db, in
     }
     m = m_new;
   }
-  const float inv = n > 0 ? 1.f / l : 0.f;
+  const float inv = n > 0 ? 1.f / l : 0.f;  // (all scores -inf: 0 * inf, a NaN)
 #pragma unroll
   for (int e = 0; e < kGenMaxDims; ++e)
     if (tid + e * kGenThreads < dv) out[tid + e * kGenThreads] = __float2bfloat16(n > 0 ? acc[e] * inv : 0.f);

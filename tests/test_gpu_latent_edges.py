@@ -87,3 +87,146 @@ def test_expanded_bits_do_not_depend_on_the_next_sequence():
         outs.append(pda.latent_prefill_attention(q.cuda(), kv[..., :128].cuda(), kr.cuda(), kv[..., 128:].cuda(), ints([0, 70, 103]),
                                                  ints([0, 900, 960]), 70, 0.07)[:70])
     assert torch.equal(outs[0], outs[1])
+
+
+# ---- scores at the ends of the range ---------------------------------------------------------------
+# Scores made of powers of two are exact in 32 bits whatever their size, so that of a row's error bound (latent_util)
+# all but the scores' part remains: the output's rounding 2^-8 |out|, the weights' 2 * 2^-8 A (theirs and their sum's),
+# the 32-bit sums' L 2^-24 A, and the exponential's 2^-12 A (a polynomial's 7.5e-5 of every fourth pair is 2^-13.7).
+
+def attend_exact(q, k, v, scale, n_keys):
+    ref = U.attend(q, k, v, scale, n_keys)[0]
+    A = U.attend(q, k, v.abs(), scale, n_keys)[0]
+    return ref, 1.01 * (U.EPS * ref.abs() + (2 * U.EPS + k.shape[0] * 2.0 ** -24 + 2.0 ** -12) * A)
+
+
+def levels(kind, n):
+    """Scores of n tokens in units of the largest size, as a rotary key's one element."""
+    c = torch.ones(n)
+    if kind == "down":         # the first tokens weigh, those from the 64th on not
+        c[min(64, n - 1):] = 2
+        return -c
+    if kind == "up":           # the reference rises by far, from below to above zero
+        return torch.where(torch.arange(n) < n // 2, -1.0, 1.0)
+    if kind == "late":         # the first 130 far below the rest
+        c[:min(130, n - 1)] = 4
+        return -c
+    return c if kind == "plus" else -c
+
+
+KINDS = ["minus", "plus", "down", "up", "late"]
+
+
+def run_levels_absorbed(kind, log2_size, flags, lens=(700, 3000, 5, 64), H=16, T=1, R=512, P=64):
+    """Scores of +-2^log2_size (times 1, 2 or 4): all of it from one rotary element, the latent part of the query zero."""
+    pg = U.Paged(list(lens), P, R, 64, 9)
+    half = log2_size // 2
+    host = pg.host.clone()
+    for b, L in enumerate(lens):
+        c = levels(kind, L) * 2.0 ** half
+        j = np.arange(L)
+        rows = host[torch.as_tensor(pg.table[b][j // P].astype(np.int64)), torch.as_tensor(j % P)]
+        rows[:, R:] = 0
+        rows[:, R] = c.to(torch.bfloat16)
+        host[torch.as_tensor(pg.table[b][j // P].astype(np.int64)), torch.as_tensor(j % P)] = rows
+    pg.cache.copy_(host)
+    B = len(lens)
+    ql, qr = torch.zeros((B, T, H, R), dtype=torch.bfloat16), torch.zeros((B, T, H, 64), dtype=torch.bfloat16)
+    qr[..., 0] = 2.0 ** (log2_size - half - 3)
+    got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 8.0, flags=flags, status=pg.status).cpu()
+    assert pg.status.item() == 0
+    for b, L in enumerate(lens):
+        j = np.arange(L)
+        rows = host[torch.as_tensor(pg.table[b][j // P].astype(np.int64)), torch.as_tensor(j % P)]
+        n_keys = (torch.arange(T) + (L - T + 1)).clamp(min=0)
+        ref, tol = attend_exact(torch.cat([ql[b, :, 0], qr[b, :, 0]], dim=-1), rows, rows[:, :R], 8.0, n_keys)
+        for h in range(H):
+            U.check(got[b, :, h], ref, tol, f"{kind} 2^{log2_size} sequence {b} head {h}")
+
+
+def run_levels_expanded(kind, log2_size, flags, q_lens=(70, 530, 3), k_lens=(1000, 700, 300), H=2):
+    half = log2_size // 2
+    cq, ck = ([int(x) for x in np.concatenate([[0], np.cumsum(n)])] for n in (q_lens, k_lens))
+    q, kr = torch.zeros((cq[-1], H, 192), dtype=torch.bfloat16), torch.zeros((ck[-1], 64), dtype=torch.bfloat16)
+    kn, v = torch.zeros((ck[-1], H, 128), dtype=torch.bfloat16), randn(1, ck[-1], H, 128)
+    q[..., 128] = 2.0 ** (log2_size - half - 3)
+    for b, n in enumerate(k_lens):
+        kr[ck[b]:ck[b + 1], 0] = (levels(kind, n) * 2.0 ** half).to(torch.bfloat16)
+    st = ints([0])
+    got = pda.latent_prefill_attention(q.cuda(), kn.cuda(), kr.cuda(), v.cuda(), ints(cq), ints(ck), max(q_lens), 8.0, flags=flags, status=st).cpu()
+    assert st.item() == 0
+    for b in range(len(q_lens)):
+        n_keys = (torch.arange(q_lens[b]) + k_lens[b] - q_lens[b] + 1).clamp(min=0)
+        for h in range(H):
+            ref, tol = attend_exact(q[cq[b]:cq[b + 1], h], torch.cat([kn[ck[b]:ck[b + 1], h], kr[ck[b]:ck[b + 1]]], dim=1),
+                                    v[ck[b]:ck[b + 1], h], 8.0, n_keys)
+            U.check(got[cq[b]:cq[b + 1], h], ref, tol, f"{kind} 2^{log2_size} sequence {b} head {h}")
+
+
+
+
+def minus_infinity_absorbed(marked, flags, H=16, R=512):
+    """(out, rows) of one sequence whose marked tokens' scores pass the lowest 32-bit number."""
+    n = len(marked)
+    pg = U.Paged([n], 64, R, 64, 12)
+    host = pg.host.clone()
+    j = np.arange(n)
+    at = torch.as_tensor(pg.table[0][j // 64].astype(np.int64)), torch.as_tensor(j % 64)
+    rows = host[at]
+    rows[:, R:] = 0
+    rows[:, R] = torch.where(marked, -2.0 ** 100, 0.0).to(torch.bfloat16)
+    host[at] = rows
+    pg.cache.copy_(host)
+    ql, qr = torch.zeros((1, 1, H, R), dtype=torch.bfloat16), torch.zeros((1, 1, H, 64), dtype=torch.bfloat16)
+    qr[..., 0] = 2.0 ** 100
+    return pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 0.5, flags=flags).cpu()[0, 0], rows
+
+
+def minus_infinity_expanded(marked, nq, flags, H=2):
+    n = len(marked)
+    q, kn = torch.zeros((nq, H, 192), dtype=torch.bfloat16), torch.zeros((n, H, 128), dtype=torch.bfloat16)
+    kr, v = torch.zeros((n, 64), dtype=torch.bfloat16), randn(2, n, H, 128)
+    kr[:, 0] = torch.where(marked, -2.0 ** 100, 0.0).to(torch.bfloat16)
+    q[..., 128] = 2.0 ** 100
+    out = pda.latent_prefill_attention(q.cuda(), kn.cuda(), kr.cuda(), v.cuda(), ints([0, nq]), ints([0, n]), nq, 0.5, flags=flags).cpu()
+    return out, q, torch.cat([kn[:, 0], kr], dim=1), v
+
+
+def marks(kind, n):
+    m = torch.zeros(n, dtype=torch.bool)
+    if kind == "first":
+        m[:200] = True
+    elif kind == "most":
+        m[:] = True
+        m[n // 2] = False
+    elif kind == "last":
+        m[n // 3:] = True
+    return m
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [20, 28, 40, 101])
+def test_plain_kernels_far_scores(kind, size):
+    run_levels_absorbed(kind, size, GENERIC)
+    run_levels_expanded(kind, size, GENERIC)
+
+
+@pytest.mark.parametrize("kind", ["first", "most", "last"])
+def test_plain_kernels_scores_below_the_range(kind):
+    """Scores of -inf weigh nothing beside finite ones, wherever they stand."""
+    n, nq = 700, 90
+    marked = marks(kind, n)
+    got, rows = minus_infinity_absorbed(marked, GENERIC)
+    ref, tol = attend_exact(torch.zeros(1, 1), torch.zeros(int((~marked).sum()), 1), rows[~marked, :512], 1.0, (~marked).sum()[None])
+    for h in range(got.shape[0]):
+        U.check(got[h:h + 1], ref, tol)
+    got, q, k, v = minus_infinity_expanded(marked, nq, GENERIC)
+    for h in range(2):
+        ref, tol = attend_exact(q[:, h], k, v[:, h], 0.5, torch.arange(nq) + n - nq + 1)
+        U.check(got[:, h], ref, tol)
+
+
+def test_plain_kernels_only_scores_below_the_range():
+    """A row without any finite score has no softmax."""
+    assert minus_infinity_absorbed(torch.ones(300, dtype=torch.bool), GENERIC)[0].isnan().all()
+    assert minus_infinity_expanded(torch.ones(300, dtype=torch.bool), 40, GENERIC)[0].isnan().all()
