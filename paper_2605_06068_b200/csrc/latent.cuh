@@ -93,14 +93,14 @@ constexpr int kLatMaxRows = 64;    // query rows per CTA
 // Rows are padded to the tile a launch uses: 16, 32 or 64.
 __host__ __device__ constexpr int latent_tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : kLatMaxRows; }
 struct LatentWorkspace {           // byte offsets
-  int64_t part_o, part_lse, records, bytes;
+  int64_t part_o, part_w, records, bytes;
 };
 __host__ __device__ inline LatentWorkspace latent_workspace_layout(int num_q_heads, int n_q, int latent_dim) {
   const int64_t rows = 2ll * kLatMaxCtas * latent_tile_rows(static_cast<int64_t>(num_q_heads) * n_q);
   LatentWorkspace w;
   w.part_o = 0;
-  w.part_lse = rows * latent_dim * 4;
-  w.records = (w.part_lse + rows * 4 + 255) / 256 * 256;
+  w.part_w = rows * latent_dim * 4;  // float2: reference and sum of the weights
+  w.records = (w.part_w + rows * 8 + 255) / 256 * 256;
   w.bytes = w.records + (kLatMaxCtas * 16 + 255) / 256 * 256;
   return w;
 }

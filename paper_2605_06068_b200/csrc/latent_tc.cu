@@ -14,8 +14,8 @@
 // Work: the tiles of all sequences form one list, cut into equal spans, one per group of CTAs (the CTAs of
 // a group take the row blocks of the same span at the same time: the tile comes from memory once and
 // from L2 for the others). A sequence that lies in several spans leaves partial results (normalised, with
-// the log2 of their weight) in the workspace, merged by a second kernel; one within a span is
-// written directly. Spans depend on the lengths and the number of SMs only.
+// the reference and the sum of their weights: their logarithm in one number would lose the sum next to a large
+// reference) in the workspace, merged by a second kernel; one within a span is written directly. Spans depend on the lengths and the number of SMs only.
 //
 // Softmax: a thread holds 2 tokens x N / 8 query rows. Weights are taken relative to a reference per row
 // that is raised (and O, in tensor memory, rescaled) only when a score passes it by more than 2^8; the
@@ -32,6 +32,7 @@
 // Warps: 0-7 softmax and output, 8 and 12 TMA producers, 9 S issue + TMEM, 10 P . C issue, 11 Q rows. All waits are
 // bounded; on a timeout every role leaves its loop, outstanding copies and products are waited for (with a
 // limit) and tensor memory is released.
+#include <cfloat>
 #include <cmath>
 
 #include "latent.cuh"
@@ -53,7 +54,7 @@ constexpr int kLSoftWarps = 8, kLSoft = kLSoftWarps * 32;  // two warps per 32 l
 constexpr int kLThreads = kLSoft + 160;
 constexpr int kLProducer = 8, kLSIssue = 9, kLPvIssue = 10, kLQLoad = 11, kLProducer2 = 12;
 constexpr uint32_t kLTmemCols = 512, kLTmemS = 256;  // O^T: R / 128 blocks of N columns from 0; S^T from 256
-constexpr float kLNoMax = -1e30f;               // reference of a row that has seen no score yet
+constexpr float kLNoMax = -FLT_MAX;             // reference of a row that has seen no finite score yet: the lowest it can be
 constexpr float kLRescale = 8.f;                // log2
 
 template <int N>
@@ -690,9 +691,12 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
       const int64_t part_row0 = (static_cast<int64_t>(slot) * plan.per_pass + r) * N;
       if (tid < N) {
         const float sum = (wred[tid] + wred[N + tid]) + (wred[2 * N + tid] + wred[3 * N + tid]);
-        inv_l[tid] = bad || sum == 0.f ? 0.f : 1.f / sum;
-        // (+inf marks a segment with a bad page: the merge then zeroes the row)
-        if (partial) reinterpret_cast<float*>(ws + lay.part_lse)[part_row0 + tid] = bad ? INFINITY : alpha[tid] + __log2f(sum);
+        // A sum of zero: the row sees no token of this segment, or none that scores more than -inf. If that is all it has,
+        // the first gives zeros and the second (0 * inf) NaN, which of a part the merge finds out.
+        const bool sees = s.L - p.n_q + (s.rb * N + tid) / p.num_q_heads + 1 > 0;
+        inv_l[tid] = bad || (sum == 0.f && (partial || !sees)) ? 0.f : 1.f / sum;
+        // (a sum below zero marks a segment with a bad page: the merge then zeroes the row)
+        if (partial) reinterpret_cast<float2*>(ws + lay.part_w)[part_row0 + tid] = make_float2(alpha[tid], bad ? -1.f : sum);
       }
       soft_sync();
       if (s.n_tiles > 0) {
@@ -777,7 +781,8 @@ __global__ void __launch_bounds__(kWide ? kMergeWideWarps * 32 : kMergeRows * 32
   const int t = row / p.num_q_heads, h = row - t * p.num_q_heads;
   __nv_bfloat16* out = p.out + (static_cast<int64_t>(b) * p.n_q + t) * p.out_token_stride + h * p.out_head_stride;
   const int vecs = p.geom.latent_dim / 4;  // 16-byte vectors of a partial row, a multiple of 32
-  const float* lse = reinterpret_cast<const float*>(ws + lay.part_lse);
+  const bool sees = seq_tokens(p, b) - p.n_q + t + 1 > 0;
+  const float2* wt = reinterpret_cast<const float2*>(ws + lay.part_w);
   const float4* part = reinterpret_cast<const float4*>(ws + lay.part_o);
   const int g0 = rec.group;
   auto row_of = [&](int k) -> int64_t {  // row of the k-th segment: later spans hold theirs in their first slot
@@ -795,18 +800,19 @@ __global__ void __launch_bounds__(kWide ? kMergeWideWarps * 32 : kMergeRows * 32
     for (int v = 0; v < 4; ++v)
       if (k < rec.n_seg && v * 32 < vecs) x[a][v] = part[row_of(k) * vecs + v * 32 + lane];
   }
-  float M = -INFINITY, mine = -INFINITY;  // (mine: the lane-th segment's)
-  bool nan = false;                       // (a maximum passes over a NaN: the row is one, not empty)
+  float M = kLNoMax;
+  float2 mine = make_float2(kLNoMax, 0.f);  // the lane-th segment's reference and sum
+  bool bad = false;                         // a bad page in some segment
   for (int k = lane; k < rec.n_seg; k += 32) {
-    const float y = lse[row_of(k)];
+    const float2 y = wt[row_of(k)];
     if (k == lane) mine = y;
-    nan |= y != y;
-    M = fmaxf(M, y);
+    bad |= y.y < 0.f;
+    M = fmaxf(M, y.x);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  nan = __any_sync(0xffffffffu, nan);
-  const bool dead = M == INFINITY || (M == -INFINITY && !nan);  // a bad page, or nothing to attend
+  bad = __any_sync(0xffffffffu, bad);
+  const float w_mine = ex2(mine.x - M) * mine.y;
   float4 acc[4];
 #pragma unroll
   for (int v = 0; v < 4; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -821,10 +827,10 @@ __global__ void __launch_bounds__(kWide ? kMergeWideWarps * 32 : kMergeRows * 32
       }
     }
   };
-  if (!dead) {  // (the whole warp)
+  if (!bad) {  // (the whole warp)
 #pragma unroll
     for (int a = 0; a < kAhead; ++a)
-      if (k0 + a * kStep < rec.n_seg) add(ex2(__shfl_sync(0xffffffffu, mine, k0 + a * kStep) - M), x[a]);
+      if (k0 + a * kStep < rec.n_seg) add(__shfl_sync(0xffffffffu, w_mine, k0 + a * kStep), x[a]);
 #pragma unroll 4
     for (int k = k0 + kAhead * kStep; k < rec.n_seg; k += kStep) {
       const int64_t at = row_of(k);
@@ -832,7 +838,8 @@ __global__ void __launch_bounds__(kWide ? kMergeWideWarps * 32 : kMergeRows * 32
 #pragma unroll
       for (int v = 0; v < 4; ++v)
         if (v * 32 < vecs) y[v] = part[at * vecs + v * 32 + lane];
-      add(ex2(lse[at] - M), y);
+      const float2 f = wt[at];
+      add(ex2(f.x - M) * f.y, y);
     }
   }
   if constexpr (kWide) {  // warp 0 adds the warps' sums, in their order
@@ -852,7 +859,7 @@ __global__ void __launch_bounds__(kWide ? kMergeWideWarps * 32 : kMergeRows * 32
       }
     }
   }
-  const float inv = dead ? 0.f : 1.f / W;
+  const float inv = bad || (W == 0.f && !sees) ? 0.f : 1.f / W;  // (no finite score among what it sees: 0 * inf, a NaN)
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     if (v * 32 < vecs) {

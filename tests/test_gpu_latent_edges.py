@@ -230,3 +230,52 @@ def test_plain_kernels_only_scores_below_the_range():
     """A row without any finite score has no softmax."""
     assert minus_infinity_absorbed(torch.ones(300, dtype=torch.bool), GENERIC)[0].isnan().all()
     assert minus_infinity_expanded(torch.ones(300, dtype=torch.bool), 40, GENERIC)[0].isnan().all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [20, 27, 28, 31, 40, 101])
+def test_absorbed_far_scores(kind, size):
+    run_levels_absorbed(kind, size, 0)
+    run_levels_absorbed(kind, size, 0, lens=(200, 66, 1, 2000), H=24, T=5)
+
+
+def test_absorbed_far_scores_split_unevenly():
+    """Equal scores far from zero over many spans, each with its own number of tokens: every token weighs the same."""
+    for size in (24, 60, 101):
+        run_levels_absorbed("minus", size, 0, lens=(4000, 1, 999), H=16)
+        run_levels_absorbed("plus", size, 0, lens=(9000,), H=64)
+
+
+@pytest.mark.parametrize("n", [100, 700, 5000])
+@pytest.mark.parametrize("kind", ["first", "most", "last"])
+def test_absorbed_scores_below_the_range(kind, n):
+    marked = marks(kind, n) if n > 200 else torch.arange(n) % 3 == 0
+    got, rows = minus_infinity_absorbed(marked, 0)
+    ref, tol = attend_exact(torch.zeros(1, 1), torch.zeros(int((~marked).sum()), 1), rows[~marked, :512], 1.0, (~marked).sum()[None])
+    for h in range(got.shape[0]):
+        U.check(got[h:h + 1], ref, tol)
+
+
+@pytest.mark.parametrize("n", [1, 60, 300, 5000])
+def test_absorbed_only_scores_below_the_range(n):
+    """A row without any finite score has no softmax: NaN, and not the zeros of a row that sees nothing."""
+    assert minus_infinity_absorbed(torch.ones(n, dtype=torch.bool), 0)[0].isnan().all()
+
+
+@pytest.mark.parametrize("lens", [[2, 1], [900, 2], [3000]])
+@pytest.mark.parametrize("flags", [0, GENERIC])
+def test_absorbed_infinite_query(lens, flags):
+    """-inf scores throughout for one row, +inf for another, next to rows that see nothing and ordinary ones."""
+    T, H = 4, 16
+    pg = U.Paged(lens, 64, 512, 64, 14)
+    host = pg.host.clone()
+    host[..., 512:] = host[..., 512:].abs()
+    pg.cache.copy_(host)
+    ql, qr = randn(15, len(lens), T, H, 512), randn(16, len(lens), T, H, 64)
+    ref, tol = U.absorbed(ql, qr, host, pg.table, lens, 0.07, 512)
+    qr[:, 3, 2, 7], qr[:, 3, 9, 7] = float("-inf"), float("inf")
+    got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 0.07, flags=flags).cpu()
+    for h in (2, 9):
+        assert got[:, 3, h].isnan().all()
+        got[:, 3, h], ref[:, 3, h] = 0, 0
+    U.check(got, ref, tol)
