@@ -34,6 +34,7 @@
 // pair's first CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are
 // bounded.
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "latent.cuh"
@@ -61,7 +62,7 @@ static_assert(kFSoftWarps * 32 * kFRegsSoftmax + 128 * kFRegsControl <= kFThread
 constexpr uint32_t kFTmemCols = 512, kFTmemO = 256;  // S[w] at 128 w, P[w] over its first 64 columns, O[w] at 256 + 128 w
 constexpr int kFUnitSlots = 4;                            // units the producer may be ahead
 constexpr int kFMaxList = 128;                            // row blocks that are sorted by their work
-constexpr float kFNoMax = -1e30f;
+constexpr float kFNoMax = -FLT_MAX;  // reference of a row that has seen no finite score yet: the lowest it can be
 constexpr float kFRescale = 8.f;
 constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
 
@@ -91,6 +92,21 @@ __device__ __forceinline__ void exp2_pair(uint64_t x, float& w0, float& w1) {
   w0 = __uint_as_float(__float_as_uint(w0) + (__float_as_uint(t0) << 23));
   w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
 }
+
+// A row's weights are 2^(c s - c r), s its scores and r its reference as they come from the product, by one fused
+// multiply-add with c r rounded: off by half a step of c r, the same for all of the row, so it cancels in the quotient. c is
+// scale * log2(e) as long as |c r| < 2^28, where that is at most 2^8. Beyond, scores that differ at all differ by 16 and
+// more there, so that only the largest one weighs anything in 32 bits, and by any c that is large enough: then c is a
+// power of two with 2^31 <= |c r| < 2^32, c r is exact, and other scores are 2^7 and more away.
+__device__ __forceinline__ float score_factor(float r, float scale_log2) {
+  if (fabsf(r * scale_log2) < 268435456.f) return scale_log2;
+  const uint32_t exponent = (__float_as_uint(r) >> 23) & 255u;
+  return __uint_as_float(min(127u + 31u + 127u - min(exponent, 254u), 254u) << 23);
+}
+// What weights and sums taken at reference `from` are multiplied by to be those at a reference `to` >= from whose factor is c
+// (each product rounded by itself, as the weights have it). Where either reference is far, the two are equal or the products
+// are 16 or more apart, with any factor: then next to `to` what was taken at `from` is as good as nothing.
+__device__ __forceinline__ float rescale(float from, float to, float c) { return ex2(__fmul_rn(from, c) - __fmul_rn(to, c)); }
 
 // One row block of one head, as the producer hands it to the other warps of its CTA. row0 < 0: no more.
 // dual: the block has at most kFHalf rows and both halves take the same ones, with tiles of their own by turns (first
@@ -653,15 +669,15 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t my_s = tmem + 128 * w + lane_base, my_o = tmem + kFTmemO + 128 * w + lane_base;
     const float scale_log2 = p.scale * 1.4426950408889634f;
-    const uint64_t scale2 = f32x2(__float_as_uint(scale_log2), __float_as_uint(scale_log2));
     const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
     const float neg_inf = -INFINITY;
     int t = 0, merges = 0;  // tiles of this half, merges with the second half so far
     for (int unit = 0;; ++unit) {
       int n, seen;  // tiles; columns that this thread's row sees, from the half's first tile on
-      // The row's reference. A row behind the sequence's last is another sequence's, or anything: its reference is
-      // infinite, so that it never asks for the warp's to be raised and has no say in the other rows' rounding.
-      float m_ref;
+      // The row's reference, a score as it comes from the product, and the factor that goes with it. A row behind the
+      // sequence's last is another sequence's, or anything: its reference is infinite, so that it never asks for the
+      // warp's to be raised and has no say in the other rows' rounding.
+      float m_ref, c_ref;
       {
         FUnit un;
         if (!next_unit(unit, un)) break;
@@ -671,6 +687,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         seen = row - lane < un.nq ? min(un.nk, un.nk - un.nq + row + 1) - un.key_tile(w, 0) * kFKeys : 0;
         m_ref = row < un.nq ? kFNoMax : INFINITY;
       }
+      c_ref = score_factor(m_ref, scale_log2);
       float l = 0.f;
       // One tile; masked: some row of the warp does not see all of it.
       auto tile = [&](auto masked, int j) {
@@ -699,7 +716,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
             for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-            m_ref = fmaxf(m_ref, fmaxf(mx[0], mx[1]) * scale_log2);
+            m_ref = fmaxf(m_ref, fmaxf(mx[0], mx[1]));
+            c_ref = score_factor(m_ref, scale_log2);
           }
           // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
           // reference by so much that the reference is raised and the weights are taken again.
@@ -707,12 +725,14 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
           float part;
           float top;
           auto weights = [&](auto poly) {
-            const uint64_t ref2 = f32x2(__float_as_uint(-m_ref), __float_as_uint(-m_ref));
+            const float minus_ref = -__fmul_rn(m_ref, c_ref);
+            const uint64_t ref2 = f32x2(__float_as_uint(minus_ref), __float_as_uint(minus_ref));
+            const uint64_t c2 = f32x2(__float_as_uint(c_ref), __float_as_uint(c_ref));
             uint64_t sum2[2] = {0ull, 0ull};
             float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), scale2, ref2);
+              const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), c2, ref2);
               mx[e & 1] = max3_nan(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
               float w0, w1;
               if (decltype(poly)::value && e % kFPolyOf == kFPolyOf - 1) {
@@ -728,7 +748,7 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
             float s0, s1;
             f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
             part = s0 + s1;
-            top = max3_nan(mx[0], mx[0], mx[1]) * scale_log2;
+            top = max3_nan(mx[0], mx[0], mx[1]);
             if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
           };
           while (true) {
@@ -739,9 +759,11 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
               break;
             }
             weights(std::bool_constant<!kMasked>{});  // (weights of hidden keys are exactly zero)
-            if (!__any_sync(0xffffffffu, top > m_ref + kFRescale)) break;
-            const float m_new = fmaxf(m_ref, top), a = ex2(m_ref - m_new);
+            if (!__any_sync(0xffffffffu, top * c_ref > m_ref * c_ref + kFRescale)) break;
+            const float m_new = fmaxf(m_ref, top), c_new = score_factor(m_new, scale_log2);
+            const float a = rescale(m_ref, m_new, c_new);
             m_ref = m_new;
+            c_ref = c_new;
             l *= a;
             if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first run of this one
               if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
@@ -797,7 +819,8 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         ++merges;
         const float2 other = *reinterpret_cast<const float2*>(sums);
         const float m = fmaxf(m_ref, other.x);
-        const float mul = ex2(m_ref - m), mul_other = ex2(other.x - m);
+        const float c_new = score_factor(m, scale_log2);
+        const float mul = rescale(m_ref, m, c_new), mul_other = rescale(other.x, m, c_new);
         l = l * mul + other.y * mul_other;
 #pragma unroll 1
         for (int c = 0; c < 8; ++c) {
@@ -814,8 +837,10 @@ latent_prefill_tc_kernel(const __grid_constant__ FMaps maps, const __grid_consta
         __syncwarp();
         if (lane == 0) arrive_cluster_tc(to_ofree + 8);  // (the second half's O has been read)
       }
-      const bool some = n > 0 && ok && l != 0.f;
-      const float inv = 1.f / l;
+      // A row that sees keys has a score at its reference, of weight 1 or (c r rounded) a little less, unless none of them is
+      // finite: then it has no softmax and is NaN. (The polynomial gives such scores 2^-126.)
+      const bool some = n > 0 && ok && un.nk - un.nq + row >= 0;
+      const float inv = 1.f / (l < 5.4210109e-20f ? NAN : l);  // 2^-64
       __nv_bfloat16* out = p.out + (static_cast<int64_t>(un.q0) + row) * p.out_token_stride + un.head(w) * p.out_head_stride;
       // A thread stores its own row, 32 bytes (a whole sector) at a time where the rows' alignment allows it.
       const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0 && p.out_token_stride % 16 == 0 && p.out_head_stride % 16 == 0;

@@ -123,7 +123,7 @@ def run_levels_absorbed(kind, log2_size, flags, lens=(700, 3000, 5, 64), H=16, T
     half = log2_size // 2
     host = pg.host.clone()
     for b, L in enumerate(lens):
-        c = levels(kind, L) * 2.0 ** half
+        c = levels(kind, L) * 2.0 ** half * 165 / 128
         j = np.arange(L)
         rows = host[torch.as_tensor(pg.table[b][j // P].astype(np.int64)), torch.as_tensor(j % P)]
         rows[:, R:] = 0
@@ -132,7 +132,7 @@ def run_levels_absorbed(kind, log2_size, flags, lens=(700, 3000, 5, 64), H=16, T
     pg.cache.copy_(host)
     B = len(lens)
     ql, qr = torch.zeros((B, T, H, R), dtype=torch.bfloat16), torch.zeros((B, T, H, 64), dtype=torch.bfloat16)
-    qr[..., 0] = 2.0 ** (log2_size - half - 3)
+    qr[..., 0] = 2.0 ** (log2_size - half - 3) * 141 / 128      # (the products are exact in 32 bits, and not times log2(e))
     got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 8.0, flags=flags, status=pg.status).cpu()
     assert pg.status.item() == 0
     for b, L in enumerate(lens):
@@ -149,9 +149,10 @@ def run_levels_expanded(kind, log2_size, flags, q_lens=(70, 530, 3), k_lens=(100
     cq, ck = ([int(x) for x in np.concatenate([[0], np.cumsum(n)])] for n in (q_lens, k_lens))
     q, kr = torch.zeros((cq[-1], H, 192), dtype=torch.bfloat16), torch.zeros((ck[-1], 64), dtype=torch.bfloat16)
     kn, v = torch.zeros((ck[-1], H, 128), dtype=torch.bfloat16), randn(1, ck[-1], H, 128)
-    q[..., 128] = 2.0 ** (log2_size - half - 3)
+    # (141 * 165 / 2^14: exact in 32 bits, and not when multiplied by log2(e))
+    q[..., 128] = 2.0 ** (log2_size - half - 3) * 141 / 128
     for b, n in enumerate(k_lens):
-        kr[ck[b]:ck[b + 1], 0] = (levels(kind, n) * 2.0 ** half).to(torch.bfloat16)
+        kr[ck[b]:ck[b + 1], 0] = (levels(kind, n) * 2.0 ** half * 165 / 128).to(torch.bfloat16)
     st = ints([0])
     got = pda.latent_prefill_attention(q.cuda(), kn.cuda(), kr.cuda(), v.cuda(), ints(cq), ints(ck), max(q_lens), 8.0, flags=flags, status=st).cpu()
     assert st.item() == 0
@@ -278,4 +279,63 @@ def test_absorbed_infinite_query(lens, flags):
     for h in (2, 9):
         assert got[:, 3, h].isnan().all()
         got[:, 3, h], ref[:, 3, h] = 0, 0
+    U.check(got, ref, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [20, 27, 28, 29, 31, 40, 101])
+def test_expanded_far_scores(kind, size):
+    run_levels_expanded(kind, size, 0)                                              # one of them with its keys split over the halves
+    run_levels_expanded(kind, size, 0, q_lens=(90, 200), k_lens=(4000, 129), H=60)  # two heads at once
+    run_levels_expanded(kind, size, 0, q_lens=(300,), k_lens=(5000,), H=2)          # S in two runs
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -120, 2.0 ** -60, 2.0 ** 60, 2.0 ** 120])
+def test_expanded_far_scales(scale):
+    """Scores so small that only their scale makes them count, and the other way round."""
+    n, H = 900, 2
+    q, kr, v = torch.zeros((n, H, 192), dtype=torch.bfloat16), torch.zeros((n, 64), dtype=torch.bfloat16), randn(1, n, H, 128)
+    kn = torch.zeros((n, H, 128), dtype=torch.bfloat16)
+    half = -int(np.log2(scale)) // 2
+    q[..., 128] = 2.0 ** half
+    kr[:, 0] = (torch.arange(n) % 4 - 2).to(torch.bfloat16) * 2.0 ** half      # scores -2, -1, 0 and 1 times 1
+    for flags in (0, GENERIC):
+        got = pda.latent_prefill_attention(q.cuda(), kn.cuda(), kr.cuda(), v.cuda(), ints([0, n]), ints([0, n]), n, scale, flags=flags).cpu()
+        for h in range(H):
+            ref, tol = attend_exact(q[:, h], torch.cat([kn[:, h], kr], dim=1), v[:, h], scale, torch.arange(n) + 1)
+            U.check(got[:, h], ref, tol)
+
+
+@pytest.mark.parametrize("kind", ["first", "most", "last"])
+@pytest.mark.parametrize("n,nq", [(700, 90), (5000, 300), (900, 900)])
+def test_expanded_scores_below_the_range(kind, n, nq):
+    marked = marks(kind, n)
+    marked[0] = False                   # (each row sees one that is not)
+    got, q, k, v = minus_infinity_expanded(marked, nq, 0)
+    for h in range(2):
+        ref, tol = attend_exact(q[:, h], k, v[:, h], 0.5, torch.arange(nq) + n - nq + 1)
+        U.check(got[:, h], ref, tol)
+
+
+@pytest.mark.parametrize("n,nq", [(1, 1), (300, 40), (300, 300), (2000, 70), (5000, 300), (30, 60)])
+def test_expanded_only_scores_below_the_range(n, nq):
+    """NaN where a row sees keys, zeros where it sees none."""
+    got = minus_infinity_expanded(torch.ones(n, dtype=torch.bool), nq, 0)[0]
+    sees = torch.arange(nq) + n - nq >= 0
+    assert got[sees].isnan().all() and (got[~sees] == 0).all()
+
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+@pytest.mark.parametrize("n,nq", [(1000, 70), (4500, 600), (300, 300)])
+def test_expanded_infinite_query(n, nq, flags):
+    """-inf scores throughout for one row, +inf for another; the others are as they should be."""
+    H, a, b = 2, nq // 3, nq - 1
+    q, kv, kr = randn(1, nq, H, 192), randn(2, n, H, 256), randn(3, n, 64).abs()
+    ref, tol = U.expanded(q, kv[..., :128], kr, kv[..., 128:], [0, nq], [0, n], 0.07)
+    q[a, 1, 130], q[b, 1, 140] = float("-inf"), float("inf")
+    got = pda.latent_prefill_attention(q.cuda(), kv[..., :128].cuda(), kr.cuda(), kv[..., 128:].cuda(), ints([0, nq]), ints([0, n]), nq, 0.07,
+                                       flags=flags).cpu()
+    for i in (a, b):
+        assert got[i, 1].isnan().all()
+        got[i, 1], ref[i, 1] = 0, 0
     U.check(got, ref, tol)
