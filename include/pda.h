@@ -39,8 +39,11 @@
  *   - Return value: 0 = PDA_OK; < 0 = PDA_ERR_* detected on the host before
  *     anything was enqueued; > 0 = the cudaError_t of a failed launch.
  *   - `status` (optional, device int32, caller-zeroed): problems found on the
- *     device are recorded with atomicMax(status, PDA_DEV_*). The affected unit's
- *     output is zero-filled; no out-of-bounds access is ever made.
+ *     device are recorded as PDA_DEV_*: the largest code stays, PDA_DEV_TIMEOUT
+ *     above all others. The affected unit's output is zero-filled; no out-of-bounds
+ *     access is ever made. Calls may share one word; while it holds
+ *     PDA_DEV_TIMEOUT, the verification and prefix calls do not start their
+ *     attention (their output is not to be used), the others work as ever.
  *   - bf16 = upper half of an IEEE binary32. e4m3 = OCP FP8 E4M3 (bias 7, max
  *     finite 448, no infinities, S.1111.111 = NaN).
  */
@@ -62,7 +65,7 @@ extern "C" {
 #define PDA_ERR_MISALIGNED (-3)   /* a pointer or stride breaks the 16-byte alignment rule     */
 #define PDA_ERR_TOO_LARGE (-4)    /* size beyond a documented fixed maximum                    */
 
-/* device-side status codes (atomicMax into *status) */
+/* device-side status codes (in *status the largest stays, PDA_DEV_TIMEOUT above all) */
 #define PDA_DEV_OK 0
 #define PDA_DEV_BAD_PAGE 1     /* block_table entry outside [0, num_pages) for a live page     */
 #define PDA_DEV_BAD_SEQ_LEN 2  /* seq_lens[b] > block_table_stride * page_size                 */
@@ -433,7 +436,7 @@ int pda_debug_e4m3_decode(float* out256, pda_stream_t stream);
  * poll: 1.05 s) and 2^24 (21.9 ns per poll: 0.37 s).
  * Nothing faults and nothing waits without a limit; the context stays usable.
  *   polls   1 .. 2^20
- *   status  device int32: receives atomicMax(PDA_DEV_TIMEOUT)
+ *   status  device int32: receives PDA_DEV_TIMEOUT
  *   result  device uint64[3] or NULL: nanoseconds spent in the suspended and in the
  *           spinning wait, and a mask of the waits that wrongly reported completion
  *           (must be 0). */

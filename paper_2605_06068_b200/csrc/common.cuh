@@ -60,8 +60,20 @@ struct MqParams {
   int32_t n_chunks_grid;  // chunk CTAs launched per (sequence, head) when split
 };
 
+// The largest code stays in *status, but an expired wait, whose number is not the largest, above all others: it voids
+// more than the others do, and kernels look for it before they start.
 __device__ __forceinline__ void report(int32_t* status, int code) {
-  if (status != nullptr) atomicMax(status, code);
+  if (status == nullptr) return;
+  if (code == PDA_DEV_TIMEOUT) {
+    atomicExch(status, code);
+    return;
+  }
+  int now = *reinterpret_cast<volatile int32_t*>(status);
+  while (now != PDA_DEV_TIMEOUT && now < code) {
+    const int seen = atomicCAS(status, now, code);
+    if (seen == now) break;
+    now = seen;
+  }
 }
 
 __device__ __forceinline__ float bf16_bits_to_float(uint16_t bits) {

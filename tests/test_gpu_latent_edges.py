@@ -38,6 +38,28 @@ def test_absorbed_with_a_status_word_that_holds_an_expired_wait(lens):
     assert st.item() == 3
 
 
+def test_an_expired_wait_stands_above_all_other_codes():
+    """One status word for all calls of a step: a wait that expires after other trouble is seen, and stays."""
+    def tables(st, count, cap):
+        pda.paged_build_tables(ints([64]), ints([64]), 16, ints(range(10)), ints([count]), ints(np.zeros((1, 8))), ints([0, 0]),
+                               ints([0] * max(cap, 1))[:cap], status=st)
+
+    for before in (0, 1, 2, 4, 5):
+        st = ints([before])
+        pda.debug_wait_timeout(1, st)
+        assert st.item() == 3
+        tables(st, 1, 64)                        # too few pages
+        tables(st, 10, 63)                       # too few slots
+        assert st.item() == 3
+    st = ints([1])
+    tables(st, 1, 64)
+    assert st.item() == 4
+    tables(st, 10, 63)
+    assert st.item() == 5
+    tables(st, 1, 64)
+    assert st.item() == 5
+
+
 # ---- memory behind a sequence ----------------------------------------------------------------------
 
 @pytest.mark.parametrize("q_lens,k_lens,H", [([40], [1000], 3),             # the keys of a small block split over the halves
