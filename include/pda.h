@@ -578,7 +578,7 @@ int64_t pda_latent_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t n
  * lie in the arrays or that has more than max_q query tokens is zeroed (as far as its rows
  * lie within the array and max_q) and sets *status PDA_DEV_BAD_SEQ_LEN.
  * nope_dim, v_dim: multiples of 8 up to 512; rope_dim a multiple of 8 up to 256; batch and
- * num_heads <= 65535. Dims 128, 64 and 128 run on the tensor-core kernel (tcgen05),
+ * num_heads <= 65535; the smaller of max_q and total_q times num_heads < 2^31. Dims 128, 64 and 128 run on the tensor-core kernel (tcgen05),
  * others and PDA_FLAG_FORCE_GENERIC on a plain kernel. */
 int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride,
                              const void* k_nope, int64_t kn_token_stride, int64_t kn_head_stride,

@@ -114,6 +114,7 @@ int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_he
   if (batch < 0 || num_heads <= 0 || nope_dim <= 0 || rope_dim < 0 || v_dim <= 0 || max_q < 0 || total_q < 0 || total_k < 0)
     return PDA_ERR_INVALID_ARG;
   if (flags & ~PDA_FLAG_FORCE_GENERIC) return PDA_ERR_INVALID_ARG;
+  if (max_q > total_q) max_q = total_q;  // (no sequence has more)
   if (nope_dim % 8 || nope_dim > 512 || rope_dim % 8 || rope_dim > 256 || v_dim % 8 || v_dim > 512) return PDA_ERR_UNSUPPORTED;
   if (batch > 65535 || num_heads > 65535 || static_cast<int64_t>(max_q) * num_heads > INT32_MAX) return PDA_ERR_TOO_LARGE;
   if (batch == 0 || max_q == 0 || total_q == 0) return PDA_OK;
@@ -125,7 +126,6 @@ int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_he
   if (!aligned16(q) || !aligned16(k_nope) || !aligned16(k_rope) || !aligned16(v) || !aligned16(out) || !aligned4(cu_q) ||
       !aligned4(cu_k) || !aligned4(status))
     return PDA_ERR_MISALIGNED;
-  if (max_q > total_q) max_q = total_q;  // (no sequence has more)
   pda::LatentPrefillParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(k_nope),
                              static_cast<const __nv_bfloat16*>(k_rope), static_cast<const __nv_bfloat16*>(v),
                              static_cast<__nv_bfloat16*>(out), cu_q, cu_k, status, q_token_stride, q_head_stride,

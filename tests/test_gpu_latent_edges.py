@@ -361,3 +361,21 @@ def test_expanded_infinite_query(n, nq, flags):
         assert got[i, 1].isnan().all()
         got[i, 1], ref[i, 1] = 0, 0
     U.check(got, ref, tol)
+
+
+# ---- bounds and strides that mean nothing ----------------------------------------------------------
+
+@pytest.mark.parametrize("flags", [0, GENERIC])
+@pytest.mark.parametrize("max_q", [60, 61, 2 ** 30, 2 ** 31 - 1])
+def test_expanded_any_bound_of_the_query_tokens_in_c(max_q, flags):
+    """The C call takes any bound, however loose, whatever the number of heads."""
+    T, H = 60, 5
+    q, kv, kr = randn(1, T, H, 192).cuda(), randn(2, T, H, 256).cuda(), randn(3, T, 64).cuda()
+    out, st, cu = torch.zeros((T, H, 128), dtype=torch.bfloat16, device="cuda"), ints([0]), ints([0, T])
+    rc = pda.lib().latent_prefill_attention(q.data_ptr(), H * 192, 192, kv.data_ptr(), H * 256, 256, kr.data_ptr(), 64,
+                                            kv[..., 128:].data_ptr(), H * 256, 256, cu.data_ptr(), cu.data_ptr(), 1, H, 128, 64, 128, max_q, T, T,
+                                            0.07, out.data_ptr(), H * 128, 128, flags, st.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    ref, tol = U.expanded(q.cpu(), kv[..., :128].cpu(), kr.cpu(), kv[..., 128:].cpu(), [0, T], [0, T], 0.07)
+    U.check(out, ref, tol)
+    assert st.item() == 0
