@@ -509,14 +509,15 @@ def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, 
     ``[R]`` the latent's root-mean-square norm on the way."""
     T, R = c_new.shape
     desc = _desc_of(cache, R)
-    c_stride, rope_stride = _bf16_rows("c_new", c_new)[0], 0
+    # (a dimension of extent 1 may carry any stride)
+    c_stride, rope_stride = _bf16_rows("c_new", c_new)[0] if T > 1 else 0, 0
     _int32(slot_map, status)
     rope = desc.rope_dim
     if rope > 0:
         rope_strides = _bf16_rows("rope_new", rope_new)
         if rope_new.shape != (T, rope):
             raise ValueError("rope_new: expected [T, rope_dim]")
-        rope_stride = rope_strides[0]
+        rope_stride = rope_strides[0] if T > 1 else 0
     else:
         rope_new = None
     if slot_map.numel() != T:

@@ -379,3 +379,11 @@ def test_expanded_any_bound_of_the_query_tokens_in_c(max_q, flags):
     ref, tol = U.expanded(q.cpu(), kv[..., :128].cpu(), kr.cpu(), kv[..., 128:].cpu(), [0, T], [0, T], 0.07)
     U.check(out, ref, tol)
     assert st.item() == 0
+
+
+def test_append_one_row_of_any_stride():
+    """A tensor of one row may carry any stride between rows, as one cut out of a wider buffer does."""
+    buf, rope = randn(1, 601).cuda(), randn(2, 99).cuda()
+    cache = torch.zeros((2, 16, 576), dtype=torch.bfloat16, device="cuda")
+    pda.latent_append(buf.as_strided((1, 512), (601, 1)), rope.as_strided((1, 64), (99, 1)), cache, ints([17]))
+    assert torch.equal(cache[1, 1], torch.cat([buf[:512], rope[:64]])) and int((cache.view(32, 576) != 0).any(1).sum()) == 1
