@@ -524,8 +524,8 @@ def latent_append(c_new, rope_new, cache, slot_map, norm_weight=None, eps=1e-6, 
         raise ValueError("slot_map: expected one entry per token")
     if norm_weight is not None:
         _bf16_rows("norm_weight", norm_weight)
-        if norm_weight.numel() != R:
-            raise ValueError("norm_weight: expected [latent_dim]")
+        if norm_weight.numel() != R or not norm_weight.is_contiguous():
+            raise ValueError("norm_weight: expected [latent_dim], contiguous")
     dev = _same_device(c_new, rope_new, cache, slot_map, norm_weight, status)
     with _device_call(dev):
         rc = lib().latent_append(c_new.data_ptr(), c_stride, _dp(rope_new), rope_stride, cache.data_ptr(), C.byref(desc),
