@@ -583,6 +583,8 @@ def paged_latent_attention(q_latent, q_rope, cache, block_table, seq_lens, scale
     stride = _check_table(block_table, B)
     if workspace is None:
         workspace = latent_workspace(B, H, T, R, device=cache.device, stream=stream)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace: must be contiguous")
     dev = _same_device(q_latent, q_rope, out, cache, block_table, seq_lens, workspace, status)
     with _device_call(dev):
         rc = lib().paged_latent_attention(

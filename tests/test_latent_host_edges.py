@@ -24,3 +24,11 @@ def test_append_takes_a_weight_of_any_shape_without_gaps():
     for weight in (bf(512), bf(1, 512), bf(2, 256), bf(4, 512)[1]):
         with pytest.raises(ValueError, match="CUDA"):        # (past all checks that a CPU tensor can fail)
             pda.latent_append(bf(2, 512), bf(2, 64), bf(3, 16, 576), i32(2), norm_weight=weight)
+
+
+@pytest.mark.parametrize("make", [lambda n: torch.zeros(1, dtype=torch.uint8).expand(n), lambda n: torch.zeros(2 * n, dtype=torch.uint8)[::2]])
+def test_attention_refuses_a_workspace_with_gaps(make):
+    """Its bytes are counted, and written one behind the other: an expanded or sliced tensor does not own so many."""
+    n = 64 << 20
+    with pytest.raises(ValueError, match="workspace"):
+        pda.paged_latent_attention(bf(2, 4, 512), bf(2, 4, 64), bf(3, 16, 576), i32(2, 4), i32(2), 0.1, workspace=make(n))
