@@ -123,7 +123,7 @@ __device__ __forceinline__ bool next_segment(const LatentParams& p, const LPlan&
   const int last_row = min((rb + 1) * N, p.n_q * p.num_q_heads) - 1;
   const int see = min(max(s.L - p.n_q + last_row / p.num_q_heads + 1, 0), s.L);  // what its last row can see
   s.tile0 = w.off;
-  s.n_tiles = s.rb < 0 ? 0 : max(0, min(w.off + s.take, (see + kLTok - 1) / kLTok) - w.off);
+  s.n_tiles = s.rb < 0 || see == 0 ? 0 : max(0, min(w.off + s.take, seq_tiles(see)) - w.off);
   w.rem -= s.take;
   w.off = 0;
   w.vseq += 1;
@@ -310,8 +310,11 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
       const int32_t* table = p.block_table + static_cast<int64_t>(s.b) * p.block_table_stride;
       const int batch_tiles = 32 / ept;  // tiles whose page ids the lanes hold
       auto load_ids = [&](int t) -> int {  // lane -> copy (t + lane / ept, lane % ept) of this segment
-        const int tile = t + lane / ept, tok = (s.tile0 + tile) * kLTok + (lane % ept) * box;
-        if (tile >= s.n_tiles || tok >= s.L) return 0;
+        const int tile = t + lane / ept;
+        if (tile >= s.n_tiles) return 0;
+        const int tok0 = (s.tile0 + tile) * kLTok;  // (lengths go up to 2^31 - 1: nothing is added up beyond them)
+        if ((lane % ept) * box >= s.L - tok0) return 0;
+        const int tok = tok0 + (lane % ept) * box;
         const int v = __ldg(table + (tok >> plan.page_shift));
         return v < 0 || v >= geo.num_pages ? 0 : v;  // (the softmax warps look for these and drop the segment)
       };
@@ -323,7 +326,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
           ids_next = load_ids(t + batch_tiles);
         }
         const int tok0 = (s.tile0 + t) * kLTok;
-        const int n_copies = uniform(min(ept, (s.L - tok0 + box - 1) / box));
+        const int n_copies = uniform((min(kLTok, s.L - tok0) + box - 1) / box);
         const uint32_t st = uniform(i & 1), sb = ring + st * kLStageBytes, bars0 = 8 * (st * kLGroups);
         const uint32_t parity = ((i >> 1) - 1) & 1;
         const uint32_t my_bytes = uniform((ept == 1 ? n_copies : (n_copies + 1 - odd) / 2) * box * 128);
@@ -572,7 +575,7 @@ latent_tc_kernel(const __grid_constant__ LMaps maps, const __grid_constant__ Lat
         float x[4 * J];
 #pragma unroll
         for (int c = 0; c < 4 * J; ++c) x[c] = __uint_as_float(sv[c]) * scale_log2;
-        if (tok0 + kLTok > s.L - p.n_q + 1) {  // the end of the sequence, or of what some query token may see
+        if (valid < kLTok + p.n_q - 1) {  // the end of the sequence, or of what some query token may see
 #pragma unroll
           for (int c = 0; c < 2 * J; ++c) {
             const int row = s.rb * N + 8 * (c >> 1) + col0 + (c & 1);

@@ -387,3 +387,27 @@ def test_append_one_row_of_any_stride():
     cache = torch.zeros((2, 16, 576), dtype=torch.bfloat16, device="cuda")
     pda.latent_append(buf.as_strided((1, 512), (601, 1)), rope.as_strided((1, 64), (99, 1)), cache, ints([17]))
     assert torch.equal(cache[1, 1], torch.cat([buf[:512], rope[:64]])) and int((cache.view(32, 576) != 0).any(1).sum()) == 1
+
+
+# ---- the longest sequences -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,H,short", [(1, 16, 1), (3, 8, 62), (1, 16, 0)])
+def test_absorbed_longest_sequence(T, H, short):
+    """Just below 2^31 tokens: the same page over and over, the last one its own. Every slot behind the end is NaN."""
+    P, R, n = 1024, 128, 2 ** 21
+    L = 2 ** 31 - 1 - short
+    host = torch.stack([randn(1, P, R + 64), randn(2, P, R + 64)])
+    host[1, P - 1 - short:] = float("nan")
+    table = torch.zeros((1, n), dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    ql, qr, st = randn(3, 1, T, H, R), randn(4, 1, T, H, 64), ints([0])
+    got = pda.paged_latent_attention(ql.cuda(), qr.cuda(), host.cuda(), table, ints([L]), 0.07, status=st)
+    assert st.item() == 0
+    # Each row of the first page stands there 2^21 - 1 times; the last page's share of 2^-21 is less than what the bound
+    # allows for 1024 keys' roundings. A CTA adds up its 226719 tiles of 64 tokens in 32 bits: four products a tile into the
+    # output sum, each off by at most a step of it (2^-23: whether the tensor core rounds or cuts off is not known), and one
+    # addition a tile into a weights' sum, off by half a step.
+    q = torch.cat([ql[0], qr[0]], dim=-1).reshape(T * H, -1)
+    ref, tol = U.attend(q, host[0], host[0][:, :R], 0.07, torch.full((T * H,), P))
+    A = U.attend(q, host[0], host[0][:, :R].abs(), 0.07, torch.full((T * H,), P))[0]
+    U.check(got.reshape(T * H, R), ref, tol + 226719 * (4 * 2.0 ** -23 + 2.0 ** -24) * A)
