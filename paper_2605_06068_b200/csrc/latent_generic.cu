@@ -38,8 +38,8 @@ __device__ __forceinline__ void attend_row(const float* q_sh, int da, int db, in
   for (int e = 0; e < kGenMaxDims; ++e) acc[e] = 0.f;
   // (the maximum starts at the lowest finite number, so that scores of -inf get a weight of 0 and not inf - inf)
   float m = -FLT_MAX, l = 0.f;
-  for (int j0 = 0; j0 < n; j0 += kGenBlock) {
-    const int nb = min(kGenBlock, n - j0);
+  for (int j0 = 0, nb; j0 < n; j0 += nb) {  // (n goes up to 2^31 - 1, and j0 no further)
+    nb = min(kGenBlock, n - j0);
     __syncthreads();
     for (int j = warp; j < nb; j += kGenThreads / 32) {
       const __nv_bfloat16* ka = key_a(j0 + j);
