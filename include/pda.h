@@ -502,7 +502,7 @@ typedef struct pda_latent_desc {
  * A sequence with n < 0, n > L, L < 0 or L > block_table_stride * P gets nothing (n counts as
  * 0) and *status PDA_DEV_BAD_SEQ_LEN. Where the free list is too short (PDA_DEV_NO_PAGES) or
  * the tokens are more than capacity (PDA_DEV_NO_SLOTS), no page is taken, the table stays as
- * it was and every slot_map entry is -1. A page id below 0, or one whose slots pass 2^31 - 1,
+ * it was and every slot_map and positions entry is -1 (cu_new counts all the same). A page id below 0, or one whose slots pass 2^31 - 1,
  * gives slot -1 and PDA_DEV_BAD_PAGE. Entries of block_table beyond need are left as they are. */
 int paged_build_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t batch,
                        int32_t page_size, const int32_t* free_pages, int32_t free_capacity,
@@ -544,8 +544,9 @@ int latent_append(const void* c_new, int64_t c_stride, const void* rope_new, int
  * finite; all other slots, pages and table entries may hold anything.
  * 1 <= n <= 4096, batch * n <= 65535. The tensor-core kernel (tcgen05) takes latent_dim 128, 256,
  * 384 or 512 with rope_dim 64 and page sizes 16, 32, 64, 128 and larger powers of two; other
- * shapes run on a plain kernel. Results do not depend on timing: sums are taken in an order
- * fixed by the lengths and the number of SMs. */
+ * shapes run on a plain kernel, which takes a CTA per query row. Scores are held in 32 bits: a row
+ * with a NaN or +inf among those it sees, or with none above -inf, is NaN. Results do not depend on
+ * timing: sums are taken in an order fixed by the lengths and the number of SMs. */
 int paged_latent_attention(const void* q_latent, int64_t ql_token_stride, int64_t ql_head_stride,
                            const void* q_rope, int64_t qr_token_stride, int64_t qr_head_stride,
                            const void* cache, const pda_latent_desc* desc,
@@ -574,12 +575,19 @@ int64_t pda_latent_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t n
  *   cu_q, cu_k  device int32[batch + 1], ascending
  *   max_q   an upper bound of the sequences' query tokens (host: the launch is sized by it)
  * Rows without any key are zero. Rows of out outside all sequences are left as they were, and
- * rows of the inputs outside all sequences may hold anything. A sequence whose ranges do not
- * lie in the arrays or that has more than max_q query tokens is zeroed (as far as its rows
- * lie within the array and max_q) and sets *status PDA_DEV_BAD_SEQ_LEN.
+ * rows of the inputs outside all sequences may hold anything: neither what stands there nor what
+ * stands in other sequences changes a bit of a sequence's result (the lengths may: they decide how
+ * the work is cut). Within a sequence q and the keys may hold anything (a row with a NaN or +inf
+ * among the scores it sees, or with none above -inf, is NaN, and no other row is), but every value
+ * v must be finite: on the tensor-core kernel an infinity or NaN in v makes earlier rows NaN too,
+ * whose weight for it is 0. Scores are held in 32 bits. A sequence whose ranges do not lie in the
+ * arrays or that has more than max_q query tokens is zeroed (as far as its rows lie within the
+ * array and max_q) and sets *status PDA_DEV_BAD_SEQ_LEN.
  * nope_dim, v_dim: multiples of 8 up to 512; rope_dim a multiple of 8 up to 256; batch and
- * num_heads <= 65535; the smaller of max_q and total_q times num_heads < 2^31. Dims 128, 64 and 128 run on the tensor-core kernel (tcgen05),
- * others and PDA_FLAG_FORCE_GENERIC on a plain kernel. */
+ * num_heads <= 65535; the smaller of max_q and total_q times num_heads < 2^31. Dims 128, 64 and
+ * 128 run on the tensor-core kernel (tcgen05); other dims, a scale that is not above 0 and finite,
+ * token or head strides of 0 (a broadcast) in an extent above 1 and PDA_FLAG_FORCE_GENERIC on a
+ * plain kernel, which takes a CTA per query row and head. */
 int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride,
                              const void* k_nope, int64_t kn_token_stride, int64_t kn_head_stride,
                              const void* k_rope, int64_t kr_token_stride, const void* v,
