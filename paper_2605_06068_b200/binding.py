@@ -447,13 +447,9 @@ def _bf16_rows(name, t):
     return strides
 
 
-def latent_desc(cache: torch.Tensor, latent_dim: int) -> LatentDesc:
-    """Descriptor of a ``[num_pages, P, latent_dim + rope_dim]`` bf16 latent cache."""
-    return LatentDesc.from_buffer_copy(_desc_of(cache, latent_dim))
-
-
 def _desc_of(cache, latent_dim):
-    """The same, shared by calls with equal layouts (not to be written to)."""
+    """Descriptor of a ``[num_pages, P, latent_dim + rope_dim]`` bf16 latent cache, shared by calls with equal layouts
+    (not to be written to)."""
     if cache.dim() != 3:
         raise ValueError("a latent cache is [num_pages, page_size, latent_dim + rope_dim]")
     page, slot, _ = _bf16_rows("cache", cache)
