@@ -389,6 +389,54 @@ def test_append_one_row_of_any_stride():
     assert torch.equal(cache[1, 1], torch.cat([buf[:512], rope[:64]])) and int((cache.view(32, 576) != 0).any(1).sum()) == 1
 
 
+@pytest.mark.parametrize("offset,pad", [(8, 0), (0, 8), (8, 24), (16, 0)])
+@pytest.mark.parametrize("lens", [[70, 200, 1], [600]])
+def test_expanded_output_aligned_to_16_bytes_only(offset, pad, lens):
+    """Rows that begin at 16 but not at 32 bytes: by their base, by the tokens' or heads' stride."""
+    H, T = 3, sum(lens)
+    cu = [int(x) for x in np.concatenate([[0], np.cumsum(lens)])]
+    q, kv, kr = randn(1, T, H, 192), randn(2, T, H, 256), randn(3, T, 64)
+    buf = torch.full((offset + T * H * (128 + pad) + 64,), -5.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[offset:].as_strided((T, H, 128), (H * (128 + pad), 128 + pad, 1))
+    pda.latent_prefill_attention(q.cuda(), kv[..., :128].cuda(), kr.cuda(), kv[..., 128:].cuda(), ints(cu), ints(cu), max(lens), 0.07, out=out)
+    ref, tol = U.expanded(q, kv[..., :128], kr, kv[..., 128:], cu, cu, 0.07)
+    U.check(out, ref, tol)
+    out.fill_(-5.0)
+    assert (buf == -5).all()                        # nothing between the rows, before or behind them
+
+
+@pytest.mark.parametrize("lens", [[700, 3, 64], [4000], [60] * 200])
+def test_absorbed_output_between_other_things(lens):
+    """Rows at 16 bytes' alignment with gaps, written directly and by the merge."""
+    B, H, R = len(lens), 5, 512
+    pg = U.Paged(lens, 64, R, 64, 31)
+    ql, qr = randn(32, B, 1, H, R), randn(33, B, 1, H, 64)
+    buf = torch.full((8 + B * H * (R + 8) + 64,), -5.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[8:].as_strided((B, 1, H, R), (H * (R + 8), H * (R + 8), R + 8, 1))
+    pda.paged_latent_attention(ql.cuda(), qr.cuda(), pg.cache, pg.dtable, pg.dlens, 0.07, out=out, status=pg.status)
+    ref, tol = U.absorbed(ql, qr, pg.host, pg.table, lens, 0.07, R)
+    U.check(out, ref, tol)
+    out.fill_(-5.0)
+    assert (buf == -5).all() and pg.status.item() == 0
+
+
+def test_calls_captured_without_a_workspace_of_their_own():
+    """Buffers that captured calls allocate are the graph's: replays between other calls give the same."""
+    pg = U.Paged([3000, 70, 1], 64, 512, 64, 34)
+    ql, qr = randn(35, 3, 1, 16, 512).cuda(), randn(36, 3, 1, 16, 64).cuda()
+    want = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 0.07).clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = pda.paged_latent_attention(ql, qr, pg.cache, pg.dtable, pg.dlens, 0.07)
+    for _ in range(5):
+        other = pda.paged_latent_attention(-ql, qr, pg.cache, pg.dtable, pg.dlens, 0.3)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    assert not torch.equal(other, want)
+
+
 # ---- the longest sequences -------------------------------------------------------------------------
 
 @pytest.mark.parametrize("T,H,short", [(1, 16, 1), (3, 8, 62), (1, 16, 0)])
