@@ -24,8 +24,8 @@
 // most 2^8, and relative to their row's sum the rounding is 2^-8 whatever the reference); sums, scores and
 // O are 32-bit.
 //
-// Measured (B200, 512 + 64, pages of 64): 64 sequences of 512..4096 tokens, 16 heads, 41 us a call in a graph (floor from
-// HBM 27), the tiles in the middle at 5.9 TB/s; 128 such sequences with 128 heads 150 us, 2900 clocks a tile,
+// Measured (B200, 512 + 64, pages of 64): 64 sequences of 512..4096 tokens, 16 heads, 43 us a call (floor from HBM 27);
+// 128 such sequences with 128 heads 166 us a call, 151 in a graph, 2900 clocks a tile,
 // of which the MMAs keep shared memory busy for 2000 (they read A for 64 columns only: 33 clocks an MMA of S, 49 of O) and the
 // tile's arrival for 600: with 64 rows that is the bound, with 16 or 32 it is HBM.
 //
