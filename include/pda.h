@@ -598,6 +598,138 @@ int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_he
                              int64_t out_token_stride, int64_t out_head_stride, uint32_t flags,
                              int32_t* status, pda_stream_t stream);
 
+/* ---- Rotated keys into the paged cache, and attention with shaped scores ------------
+ *
+ * The layer's step around the paged key/value cache of grouped-query attention: what lies
+ * between the projection and the cache (rope_kv_append), and attention over the cache for
+ * prompts (paged_prefill_attention) and for one token per sequence
+ * (paged_biased_decode_attention), whose scores may be capped, biased by distance and
+ * masked. (The paper has no counterpart; the calls below are this library's.)
+ * A step: paged_build_tables -> rope_kv_append -> one of the two. */
+
+/* From product to score, for query head h at position p and key j:
+ *     s = scale * (q . k_j)
+ *     s = softcap * tanh(s / softcap)          if softcap > 0
+ *     s = s - slopes[h] * |p - j|              if slopes
+ * in 32 bits, and the softmax is over the keys that the token sees. window > 0: among them only
+ * j > p - window. scale finite, softcap finite and >= 0, slopes finite. */
+typedef struct pda_score_desc {
+  float scale;
+  float softcap;        /* 0: none */
+  const float* slopes;  /* device fp32[num_q_heads], or NULL */
+  int32_t window;       /* 0: none */
+} pda_score_desc;
+
+/* A step's queries, keys and values as the projection leaves them: for every token t with slot
+ * slot_map[t] = s >= 0
+ *     q_out[t,h]  = R_t(N(q[t,h], q_norm))     bf16
+ *     key row     = R_t(N(k[t,g], k_norm))     into k_cache, page s / 16, slot s % 16, head g
+ *     value row   = v[t,g]                     into v_cache
+ *   N(x, w)   x / sqrt(mean(x^2) + eps) * w over the head's head_dim elements; x where w is NULL
+ *   R_t       rotation of the first rot_dim elements; the others stay. Frequency f of
+ *             rot_dim / 2 turns the pair (x_f, x_{f + rot_dim/2}), or with `interleaved`
+ *             (x_{2f}, x_{2f+1}), by the angle whose cosine and sine are
+ *             cos_sin[p][f] and cos_sin[p][rot_dim/2 + f], p = positions[axis(f)][t]:
+ *                 (a, b) -> (a cos - b sin, b cos + a sin)
+ *   all of it in 32 bits, rounded once. q_norm, k_norm: bf16[head_dim].
+ *   bf16 caches: rows rounded to bf16. e4m3 caches: the rule of kv_append_tokens_fp8, on the 32-bit
+ *   rows: a row in slot 0 sets its page's scale, amax * 2 / 448 (1 for a row of zeros), the others take the
+ *   stored one; a page that the call opens must have its rows of this call one behind the other in
+ *   the token array, in the order of their slots (as paged_build_tables lays them out).
+ *   q, k, v     [n_tokens, heads, head_dim] bf16 (may be parts of one buffer)
+ *   q_out       likewise; may be q itself
+ *               (strides in elements, multiples of 8, >= 0; rows of q_out must not overlap)
+ *   positions   int32[num_axes][n_tokens], positions_stride elements from axis to axis;
+ *               num_axes 1..4. NULL with rot_dim 0
+ *   freq_axis   HOST uint8[rot_dim / 2], the axis of each frequency, read during the call; NULL: axis 0
+ *   cos_sin     fp32 [table_len][rot_dim], contiguous, 16-byte aligned; NULL with rot_dim 0
+ *   rot_dim     0..head_dim, a multiple of 16
+ *   slot_map    int32[n_tokens]. A token with an entry < 0 is left out altogether (its row of q_out stays
+ *               as it was). An entry beyond the cache: no cache row, PDA_DEV_BAD_PAGE. Entries >= 0
+ *               must be distinct.
+ * A token with a position outside [0, table_len) among the axes that its frequencies use gets a row of
+ * zeros in q_out, no cache row, and PDA_DEV_BAD_SEQ_LEN. desc is that of both caches. */
+int rope_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k,
+                   int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                   int64_t v_token_stride, int64_t v_head_stride, const int32_t* positions,
+                   int64_t positions_stride, int32_t num_axes, const uint8_t* freq_axis,
+                   const float* cos_sin, int32_t table_len, int32_t rot_dim, int32_t interleaved,
+                   const void* q_norm, const void* k_norm, float eps, const int32_t* slot_map,
+                   int32_t n_tokens, int32_t num_q_heads, void* q_out, int64_t qo_token_stride,
+                   int64_t qo_head_stride, void* k_cache, void* v_cache,
+                   const pda_cache_desc* desc, float* k_scale, float* v_scale, int32_t* status,
+                   pda_stream_t stream);
+
+/* Attention of packed ragged sequences (prompts, or chunks of prompts behind a context) over the
+ * paged cache: sequence b has query tokens cu_q[b] .. cu_q[b+1]-1, the last nq of the seq_lens[b] = L
+ * tokens whose keys and values the cache holds. Its i-th query token stands at position
+ * p = L - nq + i and sees the keys lo <= j < hi,
+ *     hi = max(p + 1, min(prefix_lens[b], L)),  lo = max(0, p - window + 1, first_keys[t]);
+ *     out[t,h,:] = softmax_{lo <= j < hi}( score ) . V_j[g,:]       (score: pda_score_desc)
+ *   q, out       [total_q, num_q_heads, head_dim] bf16. Strides in elements, multiples of 8,
+ *                >= 0; rows of out must not overlap
+ *   cu_q         int32[batch + 1], ascending
+ *   max_q        an upper bound of the sequences' query tokens (host: the launch is sized by it)
+ *   prefix_lens  int32[batch], tokens at the start that every query token sees, or NULL
+ *   first_keys   int32[total_q], the first key that a query token sees (its document's start), or NULL
+ *   k_scale .. seq_lens  as in paged_decode_attention
+ *   workspace    device memory of pda_prefill_workspace_bytes bytes, 256-byte aligned, or NULL. With it,
+ *                sequences of few query tokens and many keys are cut along the keys. Need not be
+ *                initialised, holds nothing between calls; calls that can overlap on the GPU
+ *                (graphs replayed side by side included) need separate ones.
+ *   flags        PDA_FLAG_FORCE_GENERIC
+ * Rows that see nothing (p < 0, lo >= hi) are zero. Rows of out outside all sequences are left as they
+ * were, and rows of q outside all sequences may hold anything. Slots that hold no token < L, unused pages
+ * and table entries of pages that no token sees may hold anything; the values of all tokens < L in
+ * pages that are seen must be finite. A row with a NaN or +inf among the scores it sees is NaN;
+ * one with none above -inf is NaN or zero. L < 0 counts as 0. A sequence whose query range does not
+ * lie in the arrays, that has more than max_q query tokens or more than block_table_stride * 16 tokens
+ * is zeroed (as far as its rows lie within the array and max_q) with PDA_DEV_BAD_SEQ_LEN; rows for
+ * which a page id outside the cache is read are zero, with PDA_DEV_BAD_PAGE.
+ * batch and num_q_heads <= 65535; the smaller of max_q and total_q times num_q_heads < 2^31. Groups of up
+ * to 128 query heads with head_dim 64 and 128 run on the tensor-core kernel (tcgen05; e4m3: head_dim 128);
+ * other head_dims, caches without pages, token or head strides of 0 in an extent above 1 and
+ * PDA_FLAG_FORCE_GENERIC on a plain kernel, which takes a warp per query row. */
+int paged_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                            const void* k_cache, const void* v_cache, const pda_cache_desc* desc,
+                            const float* k_scale, const float* v_scale, const int32_t* block_table,
+                            int32_t block_table_stride, const int32_t* seq_lens,
+                            const int32_t* cu_q, int32_t batch, int32_t num_q_heads, int32_t max_q,
+                            int32_t total_q, const pda_score_desc* score,
+                            const int32_t* prefix_lens, const int32_t* first_keys, void* out,
+                            int64_t out_token_stride, int64_t out_head_stride, void* workspace,
+                            int64_t workspace_bytes, uint32_t flags, int32_t* status,
+                            pda_stream_t stream);
+
+/* Bytes of workspace that paged_prefill_attention uses, or PDA_ERR_INVALID_ARG. */
+int64_t pda_prefill_workspace_bytes(int32_t num_q_heads, int32_t head_dim);
+
+/* The same for one token per sequence: query b stands at position p = seq_lens[b] - 1 and sees the
+ * keys max(0, p - window + 1, first_keys[b]) <= j <= p.
+ *   q, out       [batch, num_q_heads, head_dim] bf16, contiguous
+ *   first_keys   int32[batch] or NULL
+ *   chunk_tokens 0: one unit per (sequence, kv head); > 0 (a multiple of 16): split into chunks as in
+ *                paged_decode_attention, with part_o, part_lse and max_chunks as there; they are scratch,
+ *                and the merge runs inside this call
+ *   workspace    (chunk_tokens > 0) int32[pda_workspace_ints(batch, num_kv_heads * ceil(group / 8))] as in
+ *                paged_decode_step: zeroed by the caller once, left zeroed, one per stream of overlapping
+ *                calls. NULL: the merge is a launch of its own
+ *   flags        PDA_FLAG_FORCE_GENERIC
+ * `out` is always written: zeros where nothing is seen (an empty sequence). What is not seen may hold
+ * anything, in pages that are read too. NaN and infinite scores, lengths and page ids as in
+ * paged_prefill_attention. bf16 with head_dim 64, 128 and 256 and e4m3 with head_dim 128 run on the TMA +
+ * tensor-core kernel (there |q| must stay below 65504 for e4m3), groups above 8 heads as several units; other
+ * shapes on a plain kernel, which does not split. */
+int paged_biased_decode_attention(const void* q, const void* k_cache, const void* v_cache,
+                                  const pda_cache_desc* desc, const float* k_scale,
+                                  const float* v_scale, const int32_t* block_table,
+                                  int32_t block_table_stride, const int32_t* seq_lens,
+                                  int32_t batch, int32_t num_q_heads, const pda_score_desc* score,
+                                  const int32_t* first_keys, int32_t chunk_tokens, void* out,
+                                  float* part_o, float* part_lse, int32_t max_chunks,
+                                  int32_t* workspace, uint32_t flags, int32_t* status,
+                                  pda_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,7 +31,8 @@ EXPORTS = ["pda_version", "pda_status_string", "pda_max_chunks", "kv_append",
            "paged_verify_attention", "paged_prefix_decode_attention", "kv_append_fp8", "kv_append_tokens_fp8",
            "pda_set_persistent_threshold", "pda_debug_wait_timeout", "pda_debug_read_probe",
            "paged_build_tables", "latent_append", "paged_latent_attention", "pda_latent_workspace_bytes",
-           "latent_prefill_attention"]
+           "latent_prefill_attention", "rope_kv_append", "paged_prefill_attention", "pda_prefill_workspace_bytes",
+           "paged_biased_decode_attention"]
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 
 
@@ -44,6 +45,10 @@ class CacheDesc(C.Structure):
 class LatentDesc(C.Structure):
     _fields_ = [("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("num_pages", C.c_int32),
                 ("page_size", C.c_int32), ("latent_dim", C.c_int32), ("rope_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ScoreDesc(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p), ("window", C.c_int32)]
 
 
 _lib = None
@@ -97,6 +102,15 @@ def lib():
         L.pda_latent_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.latent_prefill_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, vp, i32, i32,
                                                i32, i32, i32, i32, i32, i32, f32, vp, i64, i64, u32, vp, vp]
+        sp = C.POINTER(ScoreDesc)
+        L.rope_kv_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i32, vp, vp, i32, i32, i32, vp, vp, f32, vp,
+                                     i32, i32, vp, i64, i64, vp, vp, dp, vp, vp, vp, vp]
+        L.paged_prefill_attention.argtypes = [vp, i64, i64, vp, vp, dp, vp, vp, vp, i32, vp, vp, i32, i32, i32, i32, sp, vp, vp, vp,
+                                              i64, i64, vp, i64, u32, vp, vp]
+        L.pda_prefill_workspace_bytes.restype = i64
+        L.pda_prefill_workspace_bytes.argtypes = [i32, i32]
+        L.paged_biased_decode_attention.argtypes = [vp, vp, vp, dp, vp, vp, vp, i32, vp, i32, i32, sp, vp, i32, vp, vp, vp, i32, vp,
+                                                    u32, vp, vp]
         _lib = L
     return _lib
 
@@ -634,4 +648,218 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
             flags, _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "latent_prefill_attention")
+    return out
+
+
+@functools.lru_cache(maxsize=64)
+def _kv_desc(page_stride, head_stride, slot_stride, num_pages, num_kv_heads, page_size, head_dim, dtype):
+    return CacheDesc(page_stride, head_stride, slot_stride, num_pages, page_size, num_kv_heads, head_dim, dtype)
+
+
+def _paged_caches(k_cache, v_cache, k_scale, v_scale):
+    """Descriptor of the two ``[num_pages, Hkv, 16, D]`` caches (not to be written to); e4m3 ones have a scale per page and
+    head."""
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or v_cache.dtype is not k_cache.dtype:
+        raise ValueError("k_cache and v_cache: expected two [pages, kv heads, page size, head_dim] tensors of one type")
+    n, heads, P, D = k_cache.shape
+    strides = []
+    for cache in (k_cache, v_cache):
+        page, head, slot, last = cache.stride()
+        if last != 1 and D > 1:
+            raise ValueError("k_cache, v_cache: the last dimension must be contiguous")
+        # (a dimension of extent 1 may carry any stride: a dense one is taken)
+        if P == 1:
+            slot = D
+        if heads == 1:
+            head = P * slot
+        if n <= 1:
+            page = max(heads * head, P * slot)
+        strides.append((page, head, slot))
+    if strides[0] != strides[1]:
+        raise ValueError("k_cache and v_cache: expected the same strides")
+    if k_cache.dtype is _BF16:
+        dtype = PDA_BF16
+    elif k_cache.dtype in (torch.uint8, torch.float8_e4m3fn):
+        dtype = PDA_FP8_E4M3
+        for scale in (k_scale, v_scale):
+            if scale is None or scale.dtype is not torch.float32 or scale.shape != (n, heads) or not scale.is_contiguous():
+                raise ValueError("k_scale and v_scale: expected contiguous float32 [pages, kv heads] for e4m3 caches")
+    else:
+        raise TypeError(f"unsupported cache dtype {k_cache.dtype}")
+    return _kv_desc(*strides[0], n, heads, P, D, dtype)
+
+
+def _head_rows(name, t, n, D):
+    """(token stride, head stride, heads) of bf16 rows ``[n, heads, D]``."""
+    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != D:
+        raise ValueError(f"{name}: expected [{n}, heads, {D}]")
+    token, head, _ = _bf16_rows(name, t)
+    heads = t.shape[1]
+    return (token if n > 1 else 0), (head if heads > 1 else 0), heads
+
+
+@functools.lru_cache(maxsize=64)
+def _axis_bytes(freq_axis):
+    return bytes(freq_axis)
+
+
+def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_norm=None, k_norm=None, eps=1e-6, interleaved=False,
+                   freq_axis=None, out=None, k_scale=None, v_scale=None, status=None, stream=None):
+    """A step's queries, keys and values ``[T, heads, D]`` as the projection leaves them: root-mean-square norm of each query
+    and key head (``q_norm``, ``k_norm`` ``[D]``), rotation by ``positions``, queries to ``out`` (``q`` itself may be given), keys
+    and values into the cache slots ``slot_map``.
+
+    ``cos_sin`` float32 ``[positions, rot_dim]``: cosines, then sines, of each position's ``rot_dim / 2`` angles; None: no
+    rotation. ``positions`` int32 ``[T]``, or ``[axes, T]`` with ``freq_axis``, the axis of each of the ``rot_dim / 2``
+    frequencies (a sequence of ints on the host). e4m3 caches take ``k_scale``/``v_scale`` ``[pages, Hkv]``, which are updated."""
+    T, Hq, D = q.shape
+    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale)
+    if desc.head_dim != D:
+        raise ValueError("q and the caches differ in head_dim")
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    q_token, q_head, _ = _head_rows("q", q, T, D)
+    k_token, k_head, k_heads = _head_rows("k", k, T, D)
+    v_token, v_head, v_heads = _head_rows("v", v, T, D)
+    o_token, o_head, o_heads = _head_rows("out", out, T, D)
+    if k_heads != desc.num_kv_heads or v_heads != desc.num_kv_heads or o_heads != Hq:
+        raise ValueError("k, v or out: wrong number of heads")
+    _int32(slot_map, status)
+    if slot_map.numel() != T:
+        raise ValueError("slot_map: expected one entry per token")
+    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is not None and (w.dtype is not _BF16 or w.numel() != D or not w.is_contiguous()):
+            raise ValueError(f"{name}: expected contiguous bfloat16 [head_dim]")
+    rot = table = pos_stride = 0
+    axes, axis = 1, None
+    if cos_sin is not None:
+        if cos_sin.dim() != 2 or cos_sin.dtype is not torch.float32 or not cos_sin.is_contiguous():
+            raise ValueError("cos_sin: expected contiguous float32 [positions, rot_dim]")
+        table, rot = cos_sin.shape
+        if positions.dtype is not _I32 or positions.dim() > 2 or positions.shape[-1] != T or (T > 1 and positions.stride(-1) != 1):
+            raise ValueError("positions: expected int32 [T] or [axes, T]")
+        if positions.dim() == 2:
+            axes = positions.shape[0]
+            pos_stride = positions.stride(0) if axes > 1 else T
+            if freq_axis is None and axes > 1:
+                raise ValueError("freq_axis: needed for positions of several axes")
+        if freq_axis is not None:
+            axis = _axis_bytes(tuple(freq_axis))
+            if len(axis) != rot // 2 or (len(axis) and max(axis) >= axes):
+                raise ValueError("freq_axis: expected an axis for each of the rot_dim / 2 frequencies")
+    else:
+        positions = None
+    dev = _same_device(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_norm, k_norm, out, k_scale, v_scale, status)
+    with _device_call(dev):
+        rc = lib().rope_kv_append(
+            q.data_ptr(), q_token, q_head, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, _dp(positions), pos_stride,
+            axes, axis, _dp(cos_sin), table, rot, int(interleaved), _dp(q_norm), _dp(k_norm), eps, slot_map.data_ptr(), T, Hq,
+            out.data_ptr(), o_token, o_head, k_cache.data_ptr(), v_cache.data_ptr(), C.byref(desc), _dp(k_scale), _dp(v_scale),
+            _dp(status), _raw(stream, dev))
+    if rc:
+        _check(rc, "rope_kv_append")
+    return out
+
+
+def _score_desc(scale, softcap, slopes, window, num_q_heads):
+    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.numel() != num_q_heads or not slopes.is_contiguous()):
+        raise ValueError("slopes: expected contiguous float32 [query heads]")
+    return ScoreDesc(scale, softcap, _dp(slopes), window)
+
+
+def prefill_workspace(num_q_heads, head_dim, device="cuda", stream=None):
+    """Workspace of ``paged_prefill_attention`` (uninitialised; one per stream of overlapping calls)."""
+    n = int(lib().pda_prefill_workspace_bytes(num_q_heads, head_dim))
+    _check(min(n, 0), "pda_prefill_workspace_bytes")
+    return _empty(n, torch.uint8, device, stream)
+
+
+def paged_prefill_attention(q, k_cache, v_cache, block_table, seq_lens, cu_q, max_q, scale, softcap=0.0, slopes=None, window=0,
+                            prefix_lens=None, first_keys=None, out=None, k_scale=None, v_scale=None, workspace=None, flags=0,
+                            status=None, stream=None):
+    """Attention of packed ragged prompts (or chunks behind a context) ``q [Tq,Hq,D]`` over the paged cache, the query tokens
+    ``cu_q`` int32[B + 1] of each sequence being the last of its ``seq_lens`` tokens; fills and returns ``out``. Scores are
+    capped by ``softcap``, biased by ``slopes`` [Hq] times the distance and masked by ``window``, ``prefix_lens`` [B] and
+    ``first_keys`` [Tq]. Without ``workspace`` one is allocated for the call."""
+    Tq, Hq, D = q.shape
+    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale)
+    if desc.head_dim != D:
+        raise ValueError("q and the caches differ in head_dim")
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    q_token, q_head, _ = _head_rows("q", q, Tq, D)
+    o_token, o_head, o_heads = _head_rows("out", out, Tq, D)
+    if o_heads != Hq:
+        raise ValueError("out: expected the shape of q")
+    _int32(seq_lens, cu_q, prefix_lens, first_keys, status)
+    B = seq_lens.numel()
+    if cu_q.numel() != B + 1:
+        raise ValueError("cu_q: expected batch + 1 entries")
+    if prefix_lens is not None and prefix_lens.numel() != B:
+        raise ValueError("prefix_lens: expected one entry per sequence")
+    if first_keys is not None and first_keys.numel() != Tq:
+        raise ValueError("first_keys: expected one entry per query token")
+    stride = _check_table(block_table, B)
+    score = _score_desc(scale, softcap, slopes, window, Hq)
+    if workspace is None:
+        workspace = prefill_workspace(Hq, D, device=q.device, stream=stream)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace: must be contiguous")
+    dev = _same_device(q, k_cache, v_cache, block_table, seq_lens, cu_q, slopes, prefix_lens, first_keys, out, k_scale, v_scale,
+                       workspace, status)
+    with _device_call(dev):
+        rc = lib().paged_prefill_attention(
+            q.data_ptr(), q_token, q_head, k_cache.data_ptr(), v_cache.data_ptr(), C.byref(desc), _dp(k_scale), _dp(v_scale),
+            block_table.data_ptr(), stride, seq_lens.data_ptr(), cu_q.data_ptr(), B, Hq, min(int(max_q), Tq), Tq, C.byref(score),
+            _dp(prefix_lens), _dp(first_keys), out.data_ptr(), o_token, o_head, workspace.data_ptr(), workspace.nbytes, flags,
+            _dp(status), _raw(stream, dev))
+    if rc:
+        _check(rc, "paged_prefill_attention")
+    return out
+
+
+def paged_biased_decode_attention(q, k_cache, v_cache, block_table, seq_lens, scale, softcap=0.0, slopes=None, window=0,
+                                  first_keys=None, chunk_tokens=0, out=None, part_o=None, part_lse=None, workspace=None, k_scale=None,
+                                  v_scale=None, flags=0, status=None, stream=None):
+    """``paged_decode_attention`` with scores that are capped by ``softcap``, biased by ``slopes`` [Hq] times the distance and
+    masked by ``window`` and ``first_keys`` [B]; ``q [B,Hq,D]``. ``chunk_tokens > 0`` splits the tokens (``part_o``, ``part_lse``
+    as there; ``workspace`` as in ``paged_decode_step``). Always fills and returns ``out``."""
+    B, Hq, D = q.shape
+    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale)
+    if desc.head_dim != D:
+        raise ValueError("q and the caches differ in head_dim")
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    for name, t in (("q", q), ("out", out)):
+        if t.dtype is not _BF16 or t.shape != (B, Hq, D) or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous bfloat16 [batch, heads, head_dim]")
+    _int32(seq_lens, first_keys, status)
+    if seq_lens.numel() != B or (first_keys is not None and first_keys.numel() != B):
+        raise ValueError("seq_lens and first_keys: expected one entry per sequence")
+    stride = _check_table(block_table, B)
+    mc = 0
+    if chunk_tokens:
+        if part_o is None or part_lse is None:
+            raise ValueError("part_o and part_lse: needed with chunk_tokens")
+        mc = part_lse.shape[-1]
+        if part_o.shape != (B, Hq, mc, D) or part_lse.shape != (B, Hq, mc):
+            raise ValueError("part_o, part_lse: expected [batch, heads, chunks, head_dim] and [batch, heads, chunks]")
+        for t in (part_o, part_lse):
+            if t.dtype is not torch.float32 or not t.is_contiguous():
+                raise ValueError("part_o, part_lse: expected contiguous float32")
+        if workspace is not None:
+            _int32(workspace)
+            parts = -(-(Hq // max(desc.num_kv_heads, 1)) // 8)
+            if workspace.numel() < workspace_ints(B, desc.num_kv_heads * parts):
+                raise ValueError("workspace: too small")
+    score = _score_desc(scale, softcap, slopes, window, Hq)
+    dev = _same_device(q, k_cache, v_cache, block_table, seq_lens, slopes, first_keys, out, part_o, part_lse, workspace, k_scale,
+                       v_scale, status)
+    with _device_call(dev):
+        rc = lib().paged_biased_decode_attention(
+            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), C.byref(desc), _dp(k_scale), _dp(v_scale), block_table.data_ptr(),
+            stride, seq_lens.data_ptr(), B, Hq, C.byref(score), _dp(first_keys), chunk_tokens, out.data_ptr(), _dp(part_o),
+            _dp(part_lse), mc, _dp(workspace), flags, _dp(status), _raw(stream, dev))
+    if rc:
+        _check(rc, "paged_biased_decode_attention")
     return out

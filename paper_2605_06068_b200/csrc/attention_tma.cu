@@ -30,9 +30,11 @@
 // PDA_DEV_TIMEOUT, waits (bounded) for its copies in flight and zero-fills its
 // output. TMA copies never use multicast.
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "decode_tile.cuh"
+#include "shaped.cuh"
 #include "tma_ptx.cuh"
 
 namespace pda {
@@ -58,10 +60,22 @@ struct Cfg {
   static_assert(kMergeBytes <= kWarpRing, "merge buffer reuses the warp's ring");
 };
 
-template <int D, bool kFp8, int kStages, int kWarps>
+// What the shaped form of the kernel has beyond StepParams: the scores' shape, the first key that each sequence's token sees,
+// and the units that a kv head's group is cut into (8 query heads each).
+struct NoShape {
+  static constexpr bool kShaped = false;
+};
+struct DecodeShape {
+  static constexpr bool kShaped = true;
+  ScoreParams score;
+  const int32_t* first_keys;  // may be nullptr
+  int32_t parts;
+};
+
+template <int D, bool kFp8, int kStages, int kWarps, class Shape>
 __global__ void __launch_bounds__(kWarps * 32)
 attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
-                     const __grid_constant__ CUtensorMap v_map, StepParams sp, int longest_first) {
+                     const __grid_constant__ CUtensorMap v_map, StepParams sp, int longest_first, Shape shape) {
   using C = Cfg<D, kFp8, kStages, kWarps>;
   const AttnParams& p = sp.a;
   extern __shared__ uint8_t smem_raw[];
@@ -71,7 +85,12 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gid = lane >> 2, tq = lane & 3;
-  const int c = blockIdx.x, g = blockIdx.y;
+  const int c = blockIdx.x;
+  int g = blockIdx.y, part = 0;
+  if constexpr (Shape::kShaped) {
+    part = g % shape.parts;
+    g /= shape.parts;
+  }
   int b = blockIdx.z;
   int L_ranked = -1;  // the unit's length when the ranking below has it at hand (saves a trip to memory)
   if (longest_first) {  // (the host: unsplit, 2 .. kMaxLptBatch sequences, few units per resident CTA)
@@ -156,9 +175,9 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
     L_ranked = cta_err[3];
     __syncthreads();  // lens aliases the ring: done with it before any copy lands
   }
-  const int G = p.group;
+  const int G = Shape::kShaped ? min(p.group - 8 * part, 8) : p.group;
   const bool split = p.chunk_tokens > 0;
-  const int64_t row0 = static_cast<int64_t>(b) * p.num_q_heads + static_cast<int64_t>(g) * G;
+  const int64_t row0 = static_cast<int64_t>(b) * p.num_q_heads + static_cast<int64_t>(g) * p.group + 8 * part;
 
   // fused step: this launch also writes `out` (merging split-KV partials through the
   // workspace's per-unit chunk counters) and applies the append
@@ -177,7 +196,10 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   const int nch = split ? min((L - p.first_token + p.chunk_tokens - 1) / p.chunk_tokens,
                               p.max_chunks - p.chunk_slot0) : 1;
   // first attended token of this unit: the chunk start, raised by the sliding window
-  const int lo = (p.window > 0 && L - p.window > t0) ? L - p.window : t0;
+  int lo = (p.window > 0 && L - p.window > t0) ? L - p.window : t0;
+  if constexpr (Shape::kShaped) {
+    if (shape.first_keys != nullptr) lo = max(lo, shape.first_keys[b]);
+  }
   int err = 0;
   if (static_cast<int64_t>(L) > static_cast<int64_t>(p.block_table_stride) * kPageSize ||
       (split && static_cast<int64_t>(L - p.first_token) >
@@ -260,7 +282,17 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   uint32_t qf[C::kKSteps][2];
   load_q_fragments<D, kFp8>(p.q + row0 * D, G, gid, tq, qf);
 
-  const float scale_log2 = p.scale * 1.4426950408889634f;
+  float scale_log2 = p.scale * 1.4426950408889634f;
+  using Scores = std::conditional_t<Shape::kShaped, ShapedScores, PlainScores>;
+  Scores scores;
+  if constexpr (Shape::kShaped) {
+    scale_log2 = shape.score.mul;
+    scores.cap = shape.score.cap;
+    const float* slopes = shape.score.slopes;
+    const int head = g * p.group + 8 * part + 2 * tq;
+    scores.slope0 = slopes != nullptr && 2 * tq < G ? slopes[head] * kLog2e : 0.f;
+    scores.slope1 = slopes != nullptr && 2 * tq + 1 < G ? slopes[head + 1] * kLog2e : 0.f;
+  }
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // heads 2tq, 2tq+1
   float o[C::kKSteps][4];
 #pragma unroll
@@ -302,7 +334,8 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
       }
       __syncwarp();
     }
-    decode_tile<D, kFp8>(kt, vt, n_valid, n_skip, scale_log2 * ksc, vsc, qf, m0, m1, l0, l1, o, lane);
+    if constexpr (Shape::kShaped) scores.dist = static_cast<float>(L - 1 - tok0);
+    decode_tile<D, kFp8, Scores>(kt, vt, n_valid, n_skip, scale_log2 * ksc, vsc, qf, m0, m1, l0, l1, o, lane, scores);
 
     // ---- hand the stage back: every lane has consumed its fragments
     __syncwarp();
@@ -335,6 +368,10 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   for (int off = 4; off < 32; off <<= 1) {
     l0 += __shfl_xor_sync(0xffffffffu, l0, off);
     l1 += __shfl_xor_sync(0xffffffffu, l1, off);
+  }
+  if constexpr (Shape::kShaped) {  // a NaN among the row's weights is above all of them, so that it gets through the merges
+    if (l0 != l0) m0 = INFINITY;
+    if (l1 != l1) m1 = INFINITY;
   }
   float* mo = reinterpret_cast<float*>(smem + warp * C::kWarpRing);
   float* mm = mo + 8 * C::kOStride;  // m[8] then l[8]
@@ -382,12 +419,12 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
         if (wgt != 0.f) acc = fmaf(wo[h * C::kOStride + d], wgt, acc);
       }
     }
-    const bool live = !dev_err && lsum > 0.f;
+    const bool live = !dev_err && (Shape::kShaped ? lsum != 0.f : lsum > 0.f);
     const float val = live ? acc / lsum : 0.f;
     if (split && !(fuse && nch == 1)) {
       const int64_t pr = (row0 + h) * p.max_chunks + p.chunk_slot0 + c;
       p.part_o[pr * D + d] = val;
-      if (d == 0) p.part_lse[pr] = live ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
+      if (d == 0) p.part_lse[pr] = live ? (Shape::kShaped && M == INFINITY ? INFINITY : (M + __log2f(lsum)) * kLn2) : -INFINITY;
     } else {
       p.out[(row0 + h) * D + d] = __float2bfloat16_rn(val);
     }
@@ -396,7 +433,8 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   if (fuse && split && nch > 1) {
     // ---- fused reduce: publish this chunk, count it in; the unit's last chunk merges them all.
     // No CTA waits for another one: whoever arrives last finds every partial already visible.
-    int* counter = sp.workspace + 2 + b * p.geom.num_kv_heads + g;
+    int* counter = sp.workspace + 2 + (Shape::kShaped ? b * static_cast<int>(gridDim.y) + static_cast<int>(blockIdx.y)
+                                                      : b * p.geom.num_kv_heads + g);
     __threadfence();
     __syncthreads();
     if (tid == 0) cta_err[1] = (atomicAdd(counter, 1) == nch - 1) ? 1 : 0;
@@ -474,8 +512,8 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
 
 // ---- host side ---------------------------------------------------------------------------
 
-template <int D, bool kFp8, int kStages, int kWarps>
-cudaError_t launch(const StepParams& sp, cudaStream_t stream) {
+template <int D, bool kFp8, int kStages, int kWarps, class Shape = NoShape>
+cudaError_t launch(const StepParams& sp, cudaStream_t stream, const Shape& shape = Shape{}) {
   using C = Cfg<D, kFp8, kStages, kWarps>;
   const AttnParams& p = sp.a;
   alignas(64) CUtensorMap k_map, v_map;
@@ -485,11 +523,13 @@ cudaError_t launch(const StepParams& sp, cudaStream_t stream) {
       !make_cache_tensor_map(&v_map, p.v_cache, p.geom.page_stride, p.geom.head_stride, p.geom.slot_stride,
                              p.geom.num_pages, p.geom.num_kv_heads, p.geom.head_dim, eb))
     return cudaErrorNotSupported;
-  auto kern = attention_tma_kernel<D, kFp8, kStages, kWarps>;
+  auto kern = attention_tma_kernel<D, kFp8, kStages, kWarps, Shape>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
   if (e != cudaSuccess) return e;
   const unsigned chunks = p.chunk_tokens > 0 ? static_cast<unsigned>(p.max_chunks - p.chunk_slot0) : 1u;
-  dim3 grid(chunks, p.geom.num_kv_heads, p.batch);
+  int parts = 1;
+  if constexpr (Shape::kShaped) parts = shape.parts;
+  dim3 grid(chunks, p.geom.num_kv_heads * parts, p.batch);
   int longest_first = 0;
   if (p.chunk_tokens == 0 && p.batch > 1 && p.batch <= kMaxLptBatch) {
     static std::atomic<int> resident_per_sm{0};  // of this instance of the kernel (the same on every device of a process)
@@ -501,9 +541,9 @@ cudaError_t launch(const StepParams& sp, cudaStream_t stream) {
     int dev = 0, sms = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    longest_first = static_cast<int64_t>(p.batch) * p.geom.num_kv_heads <= 4ll * sms * per_sm;
+    longest_first = static_cast<int64_t>(p.batch) * grid.y <= 4ll * sms * per_sm;
   }
-  kern<<<grid, kWarps * 32, C::kSmemBytes, stream>>>(k_map, v_map, sp, longest_first);
+  kern<<<grid, kWarps * 32, C::kSmemBytes, stream>>>(k_map, v_map, sp, longest_first, shape);
   return cudaGetLastError();
 }
 
@@ -566,6 +606,21 @@ cudaError_t launch_step_tma(const StepParams& sp, cudaStream_t stream) {
     return launch<64, false, 3, 4>(sp, stream);
   }
   return launch<128, true, 3, 4>(sp, stream);
+}
+
+bool biased_decode_tma_supports(const AttnParams& p) {
+  if (p.geom.num_pages < 1 || static_cast<int64_t>(p.geom.num_kv_heads) * ((p.group + 7) / 8) > 65535) return false;
+  if (p.geom.dtype == PDA_BF16) return p.geom.head_dim == 64 || p.geom.head_dim == 128 || p.geom.head_dim == 256;
+  return p.geom.head_dim == 128;
+}
+
+cudaError_t launch_biased_decode_tma(const StepParams& sp, const ScoreParams& score, const int32_t* first_keys, cudaStream_t stream) {
+  const AttnParams& p = sp.a;
+  const DecodeShape shape{score, first_keys, (p.group + 7) / 8};
+  if (p.geom.dtype != PDA_BF16) return launch<128, true, 3, 4>(sp, stream, shape);
+  if (p.geom.head_dim == 256) return launch<256, false, 3, 4>(sp, stream, shape);
+  if (p.geom.head_dim == 128) return launch<128, false, 3, 4>(sp, stream, shape);
+  return launch<64, false, 3, 4>(sp, stream, shape);
 }
 
 cudaError_t launch_attention_tma(const AttnParams& p, cudaStream_t stream) {

@@ -10,6 +10,9 @@
 
 #include <cuda_bf16.h>
 
+#include <cfloat>
+
+#include "shaped.cuh"
 #include "tma_ptx.cuh"
 
 namespace pda {
@@ -40,15 +43,30 @@ __device__ __forceinline__ void load_q_fragments(const __nv_bfloat16* q_rows, in
   }
 }
 
+// Shapes of the scores that a tile's products go through on their way to the softmax. PlainScores: none.
+struct PlainScores {
+  static constexpr bool kShaped = false;
+};
+// Capped (cap = C > 0, see ScoreParams) and biased by the distance: token `row` of the tile is `dist - row` before the query;
+// slopes times log2(e) of this thread's heads.
+struct ShapedScores {
+  static constexpr bool kShaped = true;
+  float cap, slope0, slope1, dist;
+  __device__ __forceinline__ float operator()(float y, float slope, int row) const {
+    if (cap > 0.f) y = fmaf(-2.f * cap, rcp_approx(ex2(y) + 1.f), cap);
+    return fmaf(-slope, dist - static_cast<float>(row), y);
+  }
+};
+
 // One page tile. kt / vt: shared-memory addresses of the landed K and V tiles (128-byte
 // swizzled lines); rows [n_skip, n_valid) of the tile are attended; sc = scale * log2(e)
 // (* k_scale for e4m3), vsc = v_scale (1 for bf16). (m, l) are this thread's running maxima and
 // partial sums for heads 2tq and 2tq+1; o is the O^T accumulator fragment. Warp-collective.
-template <int D, bool kFp8>
+template <int D, bool kFp8, class Scores = PlainScores>
 __device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_valid, int n_skip, float sc,
                                             float vsc, const uint32_t (&qf)[D / 16][2], float& m0,
                                             float& m1, float& l0, float& l1, float (&o)[D / 16][4],
-                                            int lane) {
+                                            int lane, const Scores& shape = Scores{}) {
   constexpr int kKSteps = D / 16;
   constexpr int kRowBytes = D * (kFp8 ? 1 : 2);
   constexpr int kPageSize = 16;
@@ -97,6 +115,12 @@ __device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_vali
     }
     float s0 = (sa[0] + sb[0]) * sc, s1 = (sa[1] + sb[1]) * sc;   // token gid,   heads 2tq, 2tq+1
     float s2 = (sa[2] + sb[2]) * sc, s3 = (sa[3] + sb[3]) * sc;   // token gid+8
+    if constexpr (Scores::kShaped) {
+      s0 = shape(s0, shape.slope0, gid);
+      s1 = shape(s1, shape.slope1, gid);
+      s2 = shape(s2, shape.slope0, gid + 8);
+      s3 = shape(s3, shape.slope1, gid + 8);
+    }
     if (n_valid < kPageSize || n_skip > 0) {
       if (gid >= n_valid || gid < n_skip) { s0 = -INFINITY; s1 = -INFINITY; }
       if (gid + 8 >= n_valid || gid + 8 < n_skip) { s2 = -INFINITY; s3 = -INFINITY; }
@@ -109,7 +133,11 @@ __device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_vali
       mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
       mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
     }
-    const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);   // finite: every tile has an attended row
+    float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);   // finite: every tile has an attended row
+    if constexpr (Scores::kShaped) {  // (scores may be infinite here: none above -inf so far weigh nothing)
+      mn0 = mn0 == -INFINITY ? -FLT_MAX : mn0;
+      mn1 = mn1 == -INFINITY ? -FLT_MAX : mn1;
+    }
     const float al0 = ex2(m0 - mn0), al1 = ex2(m1 - mn1);     // ex2(-inf) = 0 on the first tile
     m0 = mn0; m1 = mn1;
     const float p0 = ex2(s0 - mn0), p1 = ex2(s1 - mn1), p2 = ex2(s2 - mn0), p3 = ex2(s3 - mn1);
