@@ -39,6 +39,7 @@
 
 #include "latent.cuh"
 #include "latent_ptx.cuh"
+#include "pair_ptx.cuh"
 #include "tcgen05_ptx.cuh"
 #include "tma_ptx.cuh"
 
@@ -66,11 +67,6 @@ constexpr float kFNoMax = -FLT_MAX;  // reference of a row that has seen no fini
 constexpr float kFRescale = 8.f;
 constexpr int kFPolyOf = 4;  // every fourth pair of exponentials by polynomial
 
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {  // NaN if any is
-  float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 // 2^x for two x <= 2^7 on the FMA units, so that the exponentials are not bound by the special-function unit
 // alone: x = n + f with n the nearest integer (by adding 1.5 * 2^23, whose low bits then hold n), 2^f by the
 // polynomial of degree 3 whose largest relative error over [-1/2, 1/2] is least (7.5e-5, found by Remez
@@ -136,64 +132,6 @@ struct FPlan {
 struct FMaps {
   CUtensorMap q, k_nope, k_rope, v;
 };
-
-// ---- the pair: instructions of cta_group::2 and barriers in the other CTA ----
-__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void arrive_cluster(uint32_t bar) {  // bar: an address of in_cta
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// The same where nothing has been written, or only tensor memory, which the tcgen05 fences order.
-__device__ __forceinline__ void arrive_cluster_tc(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_spin_cluster(uint32_t bar, uint32_t parity) {  // for arrivals from either CTA
-  for (uint32_t i = 0; i < kTestSpinLimit; ++i) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return true;
-  }
-  return false;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// A copy into this CTA whose bytes count for a barrier of either CTA of the pair.
-__device__ __forceinline__ void tma_load_4d_pair_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int c1, int c2,
-                                                    int c3) {
-  asm volatile(
-      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %6, 0;\n\t"
-      "@pe cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {0, %3, %4, %5}], [%2];\n\t}"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(c1), "r"(c2), "r"(c3), "r"(leader) : "memory");
-}
-__device__ __forceinline__ void mma2_ss_if(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                           uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred pe, pa;\n\tsetp.ne.b32 pe, %5, 0;\n\tsetp.ne.b32 pa, %4, 0;\n\t"
-      "@pe tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, pa;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
-}
-__device__ __forceinline__ void mma2_ts_if(uint32_t leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                           uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred pe, pa;\n\tsetp.ne.b32 pe, %5, 0;\n\tsetp.ne.b32 pa, %4, 0;\n\t"
-      "@pe tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, pa;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
-}
-// Arrival at the barrier at this offset in both CTAs once this thread's products so far are through.
-__device__ __forceinline__ void commit2_if(uint32_t leader, uint32_t bar) {
-  asm volatile(
-      "{\n\t.reg .pred pe;\n\t.reg .b16 m;\n\tsetp.ne.b32 pe, %1, 0;\n\tmov.b16 m, 3;\n\t"
-      "@pe tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
-      ::"r"(bar), "r"(leader) : "memory");
-}
 
 template <bool kRuns>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFThreads, 1)

@@ -1,6 +1,90 @@
-#include "shaped.cuh"
+// Launch of the tcgen05 prompt kernel over the paged cache (prefill_tc.cuh).
+#include "prefill_tc.cuh"
+
 namespace pda {
-bool prefill_tc_supports(const PrefillParams&) { return false; }
-cudaError_t launch_prefill_tc(const PrefillParams&, cudaStream_t) { return cudaErrorNotSupported; }
-int64_t prefill_workspace_bytes(int head_dim) { return 256; }
+
+namespace {
+
+// [tokens][heads][lines][64]: a copy takes one line of the group's heads of as many tokens as fill 128 rows
+bool encode_q(CUtensorMap* map, const PrefillParams& p, int tile_rows) {
+  EncodeFn enc = tensor_map_encoder();
+  if (!enc) return false;
+  const cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(p.geom.head_dim / 64), static_cast<cuuint64_t>(p.num_q_heads), static_cast<cuuint64_t>(p.total_q)};
+  // (a dimension of extent 1 is never stepped over)
+  const cuuint64_t strides[3] = {128, p.num_q_heads == 1 ? 128 : static_cast<cuuint64_t>(p.q_head_stride) * 2,
+                                 p.total_q == 1 ? 128 : static_cast<cuuint64_t>(p.q_token_stride) * 2};
+  const cuuint32_t box[4] = {64, 1, static_cast<cuuint32_t>(p.group), static_cast<cuuint32_t>(tile_rows)};
+  const cuuint32_t step[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int kShape>
+cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const PrefillPlan& plan, bool runs, int pairs, cudaStream_t stream) {
+  const auto kernel = runs ? prefill_tc_kernel<D, kShape, true> : prefill_tc_kernel<D, kShape, false>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GCfg<D>::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  kernel<<<static_cast<unsigned>(2 * pairs), kGThreads, GCfg<D>::kSmemBytes, stream>>>(maps, p, plan);
+  if ((e = cudaGetLastError()) != cudaSuccess || !plan.cut) return e;
+  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone ? plan.scale_log2 : 1.f);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool prefill_tc_supports(const PrefillParams& p) {
+  if (p.geom.dtype != PDA_BF16 || (p.geom.head_dim != 64 && p.geom.head_dim != 128)) return false;
+  if (p.group > 128 || p.geom.num_pages < 1 || p.geom.num_pages == INT32_MAX) return false;
+  const auto fits = [](int64_t stride, int64_t extent) { return extent == 1 || (stride > 0 && stride < (1ll << 38)); };
+  if (!fits(p.q_token_stride, p.total_q) || !fits(p.q_head_stride, p.num_q_heads)) return false;
+  // (row numbers are counted in 32 bits, up to one block behind the last)
+  if (p.total_q > INT32_MAX - 1024) return false;
+  const int block_rows = 4 * (128 / p.group);
+  return static_cast<int64_t>((p.max_q + block_rows - 1) / block_rows) * p.batch <= INT32_MAX;
+}
+
+int64_t prefill_workspace_bytes(int head_dim) {
+  return head_dim == 64 || head_dim == 128 ? prefill_records_at(head_dim) + kPreMaxPairs * static_cast<int64_t>(sizeof(PrefillRecord)) : 256;
+}
+
+cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
+  const int tile_rows = 128 / p.group, block_rows = 4 * tile_rows, heads = p.geom.num_kv_heads;
+  PrefillMaps maps{};
+  const CacheGeom& g = p.geom;
+  if (!encode_q(&maps.q, p, tile_rows) ||
+      !make_cache_tensor_map(&maps.k, p.k_cache, g.page_stride, g.head_stride, g.slot_stride, g.num_pages, heads, g.head_dim, 2, 1) ||
+      !make_cache_tensor_map(&maps.v, p.v_cache, g.page_stride, g.head_stride, g.slot_stride, g.num_pages, heads, g.head_dim, 2, 1))
+    return cudaErrorNotSupported;
+  // One pair of CTAs per two SMs at most; the row blocks of all sequences are at most one a sequence and one for
+  // every block_rows query tokens.
+  int dev = 0, sms = 0;
+  cudaError_t e;
+  if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+  const int all_pairs = std::max(sms / 2, 1);
+  const int q_blocks = (p.max_q + block_rows - 1) / block_rows;
+  const int64_t places = static_cast<int64_t>(p.batch) + p.total_q / block_rows;
+  const int64_t most = std::min(places, static_cast<int64_t>(p.batch) * q_blocks);
+  const int listed = most <= kGMaxList ? 1 : 0;
+  int64_t pairs = std::min(most * heads, static_cast<int64_t>(all_pairs));
+  // Blocks are cut along the keys where that gives each at least two pairs.
+  const int cut = listed && p.workspace != nullptr && 2 * most * heads <= std::min(all_pairs, kPreMaxPairs) ? 1 : 0;
+  if (cut) pairs = std::min(all_pairs, kPreMaxPairs);
+  const bool runs = true;
+  // (unshaped scores are scaled behind the maximum, which needs a factor above 0)
+  const int shape = (p.score.cap > 0.f ? kShapeCap : 0) | (p.score.slopes != nullptr || (p.score.cap == 0.f && !(p.score.mul > 0.f)) ? kShapeBias : 0);
+  const PrefillPlan plan{q_blocks, tile_rows, listed, listed ? 0 : places, cut, p.score.mul};
+  const int n = static_cast<int>(pairs);
+  if (g.head_dim == 128) {
+    if (shape == kShapeNone) return launch<128, kShapeNone>(p, maps, plan, runs, n, stream);
+    if (shape == kShapeCap) return launch<128, kShapeCap>(p, maps, plan, runs, n, stream);
+    if (shape == kShapeBias) return launch<128, kShapeBias>(p, maps, plan, runs, n, stream);
+    return launch<128, kShapeCap | kShapeBias>(p, maps, plan, runs, n, stream);
+  }
+  if (shape == kShapeNone) return launch<64, kShapeNone>(p, maps, plan, runs, n, stream);
+  if (shape == kShapeCap) return launch<64, kShapeCap>(p, maps, plan, runs, n, stream);
+  if (shape == kShapeBias) return launch<64, kShapeBias>(p, maps, plan, runs, n, stream);
+  return launch<64, kShapeCap | kShapeBias>(p, maps, plan, runs, n, stream);
+}
+
 }  // namespace pda

@@ -1,0 +1,1080 @@
+// Attention of packed ragged prompts over the paged cache on tcgen05 + TMEM, with shaped scores.
+//
+// The query rows of a kv head are (token, head of the group): 128 / group tokens fill the 128 rows (TMEM lanes) of a CTA, so
+// that a key tile serves the whole group. A pair of CTAs (a cluster of two SMs, tcgen05 cta_group::2) takes a block of four
+// times as many tokens as two halves of 256 rows, 128 of each in either CTA, and walks over the keys 128 at a time (8 pages):
+//   S[w] = Q[w] . K^T    M256 N128; of K each CTA holds 64 keys (4 pages)
+//   O[w] += P[w] . V     M256 N128; P (bf16) in tensor memory over the S it came from; of V each CTA holds 64 of the 128 dims
+//                        (head_dim 64: both hold all 64, and O comes out twice; the exponentials bound that case)
+// S[0], S[1], O[0], O[1] fill the 512 TMEM columns. A thread is a row's softmax and takes 64 keys at a time.
+// The softmax takes weights relative to a reference per row that is raised (and O rescaled in tensor memory) only when
+// the row's maximum passes it by more than 2^8; row sums are kept by the row's thread, of the 32-bit weights.
+// Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the pair's first
+// CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are bounded.
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+#include "pair_ptx.cuh"
+#include "shaped.cuh"
+#include "tcgen05_ptx.cuh"
+#include "tma_ptx.cuh"
+
+namespace pda {
+
+// What a launch decides for all CTAs.
+struct PrefillPlan {
+  int q_blocks;   // blocks of max_q
+  int tile_rows;  // query tokens of 128 rows
+  int listed;     // the row blocks of all sequences are few enough to be listed and sorted in shared memory
+  int64_t slots;  // (not listed) row blocks are looked for at this many places
+  int cut;        // few units: blocks are cut along the keys, so that every pair has a part
+  float scale_log2;
+};
+struct PrefillMaps {
+  CUtensorMap q, k, v;
+};
+// Workspace of a cut launch: per pair of CTAs one part's 512 rows of sums (fp32), references and sums, and a record.
+struct PrefillRecord {
+  int parts, row0, h, q0, nq, pad[3];  // parts of the row block that start here (0: none starts here)
+};
+constexpr int kPreMaxPairs = 74;       // a device with more SMs uses this many where blocks are cut
+constexpr int kPreRows = 512;
+__host__ __device__ constexpr int64_t prefill_part_bytes(int head_dim) { return static_cast<int64_t>(kPreRows) * head_dim * 4; }
+__host__ __device__ constexpr int64_t prefill_sums_at(int head_dim) { return kPreMaxPairs * prefill_part_bytes(head_dim); }
+__host__ __device__ constexpr int64_t prefill_records_at(int head_dim) { return prefill_sums_at(head_dim) + kPreMaxPairs * kPreRows * 8; }
+
+namespace {
+
+constexpr int kGKeys = 128;  // keys per tile
+constexpr int kGQLine = 128 * 128, kGKLine = 64 * 128;
+constexpr int kGSoftWarps = 8, kGThreads = (kGSoftWarps + 4) * 32, kGProducer = 8, kGMma = 9, kGRelay = 11;
+constexpr int kGBookBytes = 5 * 1024;
+constexpr uint32_t kGRegsSoftmax = 200, kGRegsControl = 104;  // 384 threads start with 168 (64512 in all)
+static_assert(kGSoftWarps * 32 * kGRegsSoftmax + 128 * kGRegsControl <= kGThreads * 168, "registers");
+constexpr uint32_t kGTmemCols = 512, kGTmemO = 256;
+constexpr int kGUnitSlots = 4;   // units the producer may be ahead
+constexpr int kGMaxList = 128;   // row blocks that are sorted by their work
+constexpr float kGNoMax = -FLT_MAX;
+constexpr float kGRescale = 8.f;
+constexpr int kGPolyOf = 4;      // every fourth pair of exponentials by polynomial
+constexpr int kGMinTiles = 4;    // of a part
+
+// How scores are shaped (bits): capped; biased by distance.
+enum : int { kShapeNone = 0, kShapeCap = 1, kShapeBias = 2 };
+
+template <int D>
+struct GCfg {
+  static constexpr int kLines = D / 64;
+  static constexpr int kStages = D == 128 ? 4 : 6;
+  static constexpr int kKBytes = kLines * kGKLine;  // of its 64 keys
+  static constexpr int kVBytes = kGKeys * 128;      // its line (64 dims) of all keys
+  static constexpr int kQBytes = kLines * kGQLine;  // of a half
+  static constexpr int kRing = 2 * kQBytes;
+  static constexpr int kBook = kRing + kStages * (kKBytes + kVBytes);
+  static constexpr int kBars = 9 * kStages + 36;
+  static constexpr int kSmemBytes = kBook + kGBookBytes + 1024;
+  static_assert(kSmemBytes <= 232448, "shared memory");
+};
+
+// 2^x for two x <= 2^7 on the FMA units: x = n + f with n the nearest integer, 2^f by the polynomial of degree 3 whose
+// largest relative error over [-1/2, 1/2] is least (7.5e-5, by Remez exchange; a weight's rounding to bf16 is 3.9e-3),
+// n added to the exponent. x below -126 gives 2^-126, and so does a NaN: that is looked for in the scores' maximum.
+__device__ __forceinline__ void exp2_two(uint64_t x, float& w0, float& w1) {
+  auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
+  float x0, x1;
+  f32x2_split(x, x0, x1);
+  x = f32x2(__float_as_uint(fmaxf(x0, -126.f)), __float_as_uint(fmaxf(x1, -126.f)));
+  const uint64_t t = add_f32x2(x, both(12582912.f));  // 1.5 * 2^23
+  const uint64_t f = add_f32x2(x, fma_f32x2(t, both(-1.f), both(12582912.f)));
+  uint64_t y = fma_f32x2(f, both(0.0551716691f), both(0.242611122f));
+  y = fma_f32x2(y, f, both(0.693260985f));
+  y = fma_f32x2(y, f, both(0.999928074f));
+  float t0, t1;
+  f32x2_split(t, t0, t1);
+  f32x2_split(y, w0, w1);
+  w0 = __uint_as_float(__float_as_uint(w0) + (__float_as_uint(t0) << 23));
+  w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Scores that are not shaped stay as they come from the product: weights are 2^(c s - c r), s the scores and r the
+// reference, by one fused multiply-add with c r rounded: off by half a step of c r, the same for all of the row, so it
+// cancels in the quotient. c is the scale as long as |c r| < 2^28, where that is at most 2^8. Beyond, scores that differ at
+// all differ by 16 and more there, so that only the largest one weighs anything in 32 bits, and by any c that is large enough:
+// then c is a power of two with 2^31 <= |c r| < 2^32, c r is exact, and other scores are 2^7 and more away.
+// Shaped scores are in the exponent's units already: c is 1 (far ones again a power of two).
+__device__ __forceinline__ float score_factor(float r, float scale_log2) {
+  if (fabsf(r * scale_log2) < 268435456.f) return scale_log2;
+  const uint32_t exponent = (__float_as_uint(r) >> 23) & 255u;
+  return __uint_as_float(min(127u + 31u + 127u - min(exponent, 254u), 254u) << 23);
+}
+// What weights and sums taken at reference `from` are multiplied by to be those at a reference `to` >= from whose factor is c.
+__device__ __forceinline__ float rescale(float from, float to, float c) { return ex2(__fmul_rn(from, c) - __fmul_rn(to, c)); }
+
+// One row block of one kv head (or a part of its keys), as the producer hands it to the other warps of its CTA. row0 < 0: no
+// more. Rows are counted in query tokens of the sequence. dual: the block fits one half and both halves take the same
+// rows, with tiles of their own by turns: kTwoHeads: the second half's are the next head's; kSplitKeys: the second half's are
+// the later n1 tiles of the same head, and the first half's warps merge the two results.
+enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
+struct GUnit {
+  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace
+  __device__ int first_row(int w, int half_rows) const { return row0 + (dual ? 0 : half_rows * w); }
+  __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
+  __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
+  // The pair's i-th tile: whose half's (where that matters), and which 128 keys from tile0 on.
+  __device__ int half_of(int i) const { return i & 1; }
+  __device__ int keys_of(int i) const { return dual ? key_tile(i & 1, i >> 1) : i; }
+  __device__ int key_tile(int w, int j) const { return dual == kSplitKeys && w ? n0 + j : j; }
+};
+constexpr uint32_t kGSmallBlock = 1u << 30;  // (in a list entry) fits one half
+__device__ __forceinline__ int units_of(uint32_t entry, int heads, bool by_two) {
+  return by_two && (entry & kGSmallBlock) ? (heads + 1) / 2 : heads;
+}
+
+// A page's line into this CTA, its bytes counted at a barrier of either CTA of the pair. A page number at or beyond the
+// cache's is read as zeros.
+__device__ __forceinline__ void tma_load_page_pair_if(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int line, int head,
+                                                      int page) {
+  asm volatile(
+      "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %6, 0;\n\t"
+      "@pe cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {0, 0, %3, %4, %5}], [%2];\n\t}"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(line), "r"(head), "r"(page), "r"(leader) : "memory");
+}
+
+template <int D, int kShape, bool kRuns>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGThreads, 1)
+prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constant__ PrefillParams p,
+                  const __grid_constant__ PrefillPlan plan) {
+  using C = GCfg<D>;
+  constexpr int kStages = C::kStages;
+  constexpr bool kZ = kShape != kShapeNone;        // scores are shaped before the softmax
+  constexpr uint32_t kRunP = kRuns ? 64 : 32;      // columns from the first run's weights to the second's
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBook);
+  GUnit* units = reinterpret_cast<GUnit*>(bars + C::kBars);         // [kGUnitSlots]
+  uint32_t* list = reinterpret_cast<uint32_t*>(units + kGUnitSlots);  // [kGMaxList] sequence and block, most work first
+  uint32_t* work = list + kGMaxList;                                // [kGMaxList] tiles, then units of the entries before
+  uint32_t* scan = work + kGMaxList;                                // [4] by warp
+  uint32_t* tmem_slot = scan + 5;
+  int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
+  uint32_t* target_sh = reinterpret_cast<uint32_t*>(cta_err + 1);   // tiles of a part
+  float* merge_sh = reinterpret_cast<float*>(target_sh + 1);        // [128][2]
+  int4* spans = reinterpret_cast<int4*>(reinterpret_cast<uint8_t*>(bars) + kGBookBytes - kGMaxList * 16);  // listed sequences' q0, nq, L
+  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + 8 * 4 + 1024 + kGMaxList * 16 <= kGBookBytes, "shared memory");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x & 1;  // in the pair
+  const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+  const int half_rows = 2 * plan.tile_rows, block_rows = 4 * plan.tile_rows;  // in query tokens
+  const int heads = p.geom.num_kv_heads;
+  bool ok = true;
+
+  const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + C::kRing, v_sm = k_sm + kStages * C::kKBytes;
+  // Barriers, at the same place in both CTAs. Of the pair's first CTA: full_k (both CTAs' copies), v_ready, bar_q,
+  // bar_p, bar_turn, bar_ofree. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s,
+  // bar_pv, bar_qfree, the unit slots'. bar_s, bar_p and bar_pv: [half w][run of
+  // 64 keys] (bar_s with S at once: the first only).
+  const uint32_t full_k = smem_u32(bars), empty_k = full_k + 24 * kStages, full_v = empty_k + 8 * kStages,
+                 empty_v = full_v + 8 * kStages, v_ready = empty_v + 8 * kStages, bar_q = v_ready + 24 * kStages;
+  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 32, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_qfree = bar_turn + 16,
+                 bar_ofree = bar_qfree + 16, unit_full = bar_ofree + 16, unit_empty = unit_full + 8 * kGUnitSlots,
+                 bar_drain = unit_empty + 8 * kGUnitSlots, bar_never = bar_drain + 8, bar_merge = bar_never + 8;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      for (int set = 0; set < 3; ++set) {
+        mbar_init(full_k + 8 * (kStages * set + i), 1);
+        mbar_init(v_ready + 8 * (kStages * set + i), 2);
+      }
+      mbar_init(empty_k + 8 * i, 2);
+      mbar_init(full_v + 8 * i, 1);
+      mbar_init(empty_v + 8 * i, 2);
+    }
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(bar_q + 8 * w, 1);
+      for (int k = 0; k < 2; ++k) {
+        mbar_init(bar_s + 16 * w + 8 * k, 1);
+        mbar_init(bar_p + 16 * w + 8 * k, 8);  // four warps of each CTA
+        mbar_init(bar_pv + 16 * w + 8 * k, 1);
+      }
+      mbar_init(bar_turn + 8 * w, 1);
+      mbar_init(bar_qfree + 8 * w, 1);
+      mbar_init(bar_ofree + 8 * w, 8);
+    }
+    for (int i = 0; i < kGUnitSlots; ++i) {
+      mbar_init(unit_full + 8 * i, 1);
+      mbar_init(unit_empty + 8 * i, kGSoftWarps + 1 + (rank == 0 ? 2 : 0));  // softmax, relay, product warps
+    }
+    mbar_init(bar_drain, 2);
+    mbar_init(bar_never, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(bar_merge + 8 * i, 1);
+    *cta_err = 0;
+    *target_sh = 1u << 30;
+    fence_mbar_init();
+    fence_proxy_async();
+  }
+  if (warp == kGProducer && elect_one()) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
+  }
+  if (warp == kGMma) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kGTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  // The keys that the query tokens `row0` .. `last` of a sequence can see at most: none before `lo`, none from `hi` on.
+  // (lo by the first token and the window alone; documents that start later narrow it further)
+  auto key_range = [&](int row0, int last, int nq, int L, int prefix, int& lo, int& hi) {
+    const int first_pos = L - nq + row0, last_pos = L - nq + last;
+    hi = last_pos < 0 ? 0 : max(last_pos + 1, min(prefix, L));
+    lo = p.score.window > 0 ? max(first_pos - p.score.window + 1, 0) : 0;
+  };
+  auto prefix_of = [&](int b) { return p.prefix_lens != nullptr ? p.prefix_lens[b] : 0; };
+
+  // ---- the row blocks that there are, those with the most keys first (every CTA for itself, all alike)
+  int my_blocks = 0, my_prefix = 0;
+  SeqSpan mine{0, 0, 0};
+  if (plan.listed && tid < kGMaxList && tid < p.batch) {
+    mine = seq_span(p, tid);
+    my_blocks = (mine.nq + block_rows - 1) / block_rows;
+    my_prefix = prefix_of(tid);
+    spans[tid] = make_int4(mine.q0, mine.nq, mine.L, my_prefix);
+  }
+  int incl = my_blocks;
+  if (plan.listed && tid < kGMaxList) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    if (lane == 31) scan[warp] = incl;
+  }
+  tc_fence_before();
+  __syncthreads();
+  int n_blocks = 0;
+  uint32_t my_work = 0, my_entry = 0;
+  bool by_two = true;  // heads two by two on small blocks
+  if (plan.listed) {
+    int before = incl - my_blocks;
+    for (int i = 0; i < kGMaxList / 32; ++i) {
+      before += i < warp ? scan[i] : 0;
+      n_blocks += scan[i];
+    }
+    // (ascending offsets give at most as many as the host has allowed for; others are reported)
+    if (n_blocks > kGMaxList) {
+      report(p.status, PDA_DEV_BAD_SEQ_LEN);
+      n_blocks = kGMaxList;
+    }
+    // ... unless there is a pair of CTAs for each head of each block: half as many units are no gain then
+    by_two = !plan.cut && static_cast<int64_t>(n_blocks) * heads > pairs;
+    for (int k = 0; k < my_blocks && before + k < kGMaxList; ++k) {
+      int lo, hi;
+      key_range(k * block_rows, min((k + 1) * block_rows, mine.nq) - 1, mine.nq, mine.L, my_prefix, lo, hi);
+      if (p.first_keys != nullptr) lo = max(lo, p.first_keys[mine.q0 + k * block_rows]);
+      work[before + k] = hi > lo ? (hi + kGKeys - 1) / kGKeys - lo / kGKeys : 0;
+      list[before + k] = tid | (k << 7) | (mine.nq - k * block_rows <= half_rows ? kGSmallBlock : 0u);
+    }
+    __syncthreads();
+    int place = 0;
+    if (tid < n_blocks) {
+      my_work = work[tid];
+      my_entry = list[tid];
+      for (int i = 0; i < n_blocks; ++i) place += work[i] > my_work || (work[i] == my_work && i < tid);
+    }
+    // Few units: the fewest tiles a part with which all parts find a pair each.
+    if (plan.cut && warp == 0) {
+      uint32_t below = kGMinTiles - 1, t = work[0];  // (below: too small, or not wanted)
+      for (int i = lane; i < n_blocks; i += 32) t = max(t, work[i]);
+      t = max(__reduce_max_sync(0xffffffffu, t), static_cast<uint32_t>(kGMinTiles));
+      while (t - below > 1) {
+        const uint32_t mid = (t + below) >> 1;
+        uint32_t parts = 0;
+        for (int i = lane; i < n_blocks; i += 32) parts += max((work[i] + mid - 1) / mid, 1u);
+        if (static_cast<int64_t>(__reduce_add_sync(0xffffffffu, parts)) * heads <= pairs) t = mid; else below = mid;
+      }
+      if (lane == 0) *target_sh = t;
+    }
+    __syncthreads();
+    if (tid < n_blocks) {
+      list[place] = my_entry;
+      work[place] = my_work;
+    }
+    __syncthreads();
+    uint32_t units = 0;
+    if (tid < n_blocks) units = plan.cut ? heads * max((work[tid] + *target_sh - 1) / *target_sh, 1u) : units_of(list[tid], heads, by_two);
+    const uint32_t my_units = units;
+    if (tid < kGMaxList) {
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, units, o);
+        if (lane >= o) units += u;
+      }
+      if (lane == 31) scan[warp] = units;
+    }
+    __syncthreads();
+    uint32_t units_before = units - my_units;
+    for (int i = 0; i < kGMaxList / 32; ++i) units_before += i < warp ? scan[i] : 0;
+    if (tid < n_blocks) work[tid] = units_before;
+    if (tid == 0) scan[4] = scan[0] + scan[1] + scan[2] + scan[3];
+    static_assert(kGMaxList == 128, "four warps' sums");
+  }
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  // Unit number k of this CTA, for the warps that are told by the producer.
+  auto next_unit = [&](int k, GUnit& un) {
+    const int slot = k % kGUnitSlots;
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(unit_full + 8 * slot, (k / kGUnitSlots) & 1));
+    if (!ok) return false;
+    un = units[slot];
+    return un.row0 >= 0;
+  };
+  auto free_unit = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive_tc(unit_empty + 8 * (k % kGUnitSlots));
+  };
+
+  // The barrier of a tile, from full_k or v_ready: both halves' tiles, the first half's and the second half's (dual
+  // blocks) are counted each for themselves, so that who waits for a set's barriers follows all their phases. (kStages
+  // tiles of a set are in the ring at most: a barrier's next use comes behind its last one's wait.)
+  auto tile_bar = [&](uint32_t first, int set, int count) { return first + 8 * (kStages * set + count % kStages); };
+
+  // ================= products of half w =================
+  // A warp for each half, which prepares its next products while the other's are being issued. Where S is taken at once, they
+  // take turns, so that the halves stay in opposite phase.
+  auto issue_role = [&](auto half) {
+    constexpr int w = decltype(half)::value;
+    constexpr uint32_t idesc_s = latent_idesc(256, kGKeys, false, false), idesc_run = latent_idesc(256, kGKeys / 2, false, false),
+                       idesc_o = latent_idesc(256, 128, false, true);
+    const uint32_t leader = elect_one();
+    const uint32_t u_q = uniform(q_sm + w * C::kQBytes), u_k = uniform(k_sm), u_v = uniform(v_sm), u_tmem = uniform(tmem);
+    const uint32_t u_ek = uniform(empty_k), u_ev = uniform(empty_v);
+    const uint32_t d_s = u_tmem + 128 * w, d_o = u_tmem + kGTmemO + 128 * w;
+    auto wait = [&](uint32_t bar, int phase) {
+      if (ok) ok = __all_sync(0xffffffffu, mbar_spin_cluster(bar, phase & 1));
+    };
+    // S of a tile at once, or of run k of two: of each CTA's 64 keys those from 32 k on
+    auto s_product = [&](uint32_t k_addr, int k, uint32_t idesc) {
+      const uint64_t q0 = tc_desc(u_q, 16, 1024), k0 = tc_desc(k_addr, 16, 1024) + 256 * k;
+#pragma unroll
+      for (int ln = 0; ln < C::kLines; ++ln)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          mma2_ss_if(leader, d_s + 64 * k, q0 + ln * (kGQLine / 16) + 2 * ks, k0 + ln * (kGKLine / 16) + 2 * ks, idesc, (ln > 0 || ks > 0) ? 1u : 0u);
+      commit2_if(leader, bar_s + 16 * w + 8 * k);
+    };
+    GUnit un;
+    // Before this unit: tiles of the pair; of this half; units of this half; tiles on which the halves take turns.
+    int t0 = 0, mine = 0, done = 0, turns = 0;
+    int counts[2] = {0, 0};  // tiles of blocks of two halves; of dual ones, this half's
+    for (int k = 0; next_unit(k, un); ++k) {
+      free_unit(k);
+      const int n = uniform(w == 0 ? un.n0 : un.n1), n_other = uniform(w == 0 ? un.n1 : un.n0);
+      const int dual = uniform(un.dual);
+      const int step = dual ? 2 : 1, own = dual ? w : 0;  // this half's tiles: t0 + step * j + own
+      const int set = dual ? 1 + w : 0, c0 = counts[dual ? 1 : 0];  // this unit's tiles on the set's barriers: c0 + j
+      // Both halves give a tile of a block of two halves back. The one that does not read it does so as soon as it is
+      // there (see tile_bar) and goes on, to the next unit where this was the last tile.
+      auto hand_on = [&](uint32_t full, uint32_t empty, int j) {
+        wait(tile_bar(full, 0, c0 + j), (c0 + j) / kStages);
+        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty + 8 * ((t0 + j) % kStages), lane));
+        __syncwarp();
+      };
+      // (a tile of a dual block is given back twice by its half)
+      auto give_back = [&](uint32_t bar) {
+        commit2_if(leader, bar);
+        if (dual) commit2_if(leader, bar);
+      };
+      if (n > 0) {  // S(0): its place is free, the tensor core works a thread's products off in order
+        const int t = t0 + own, sk = t % kStages;
+        wait(bar_q + 8 * w, done);
+        wait(tile_bar(full_k, set, c0), c0 / kStages);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t k_addr = uniform(u_k + sk * C::kKBytes);
+        s_product(k_addr, 0, kRuns ? idesc_run : idesc_s);
+        if constexpr (kRuns) s_product(k_addr, 1, idesc_run);
+        if (n == 1) commit2_if(leader, bar_qfree + 8 * w);
+        give_back(uniform(u_ek + 8 * sk));
+      }
+      for (int j = 0; j < n; ++j) {
+        const int t = t0 + step * j + own, tn = t + step, sv = t % kStages, sk = tn % kStages;
+        wait(tile_bar(v_ready, set, c0 + j), (c0 + j) / kStages);
+        const uint64_t v0 = tc_desc(uniform(u_v + sv * C::kVBytes), 16, 1024);
+        const uint32_t k_addr = uniform(u_k + sk * C::kKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
+        const uint32_t acc = uniform(j > 0 ? 1u : 0u);
+        if (j == 0 && done > 0) wait(bar_ofree + 8 * w, done - 1);  // the last unit's output has been read
+        // turn i: half 0 after half 1's turn i - 1, half 1 after half 0's turn i
+        const bool taking_turns = !kRuns && j < n_other;
+        const int turn = turns + j;
+        const uint32_t turn_bar = taking_turns && (w == 1 || turn > 0) ? bar_turn + 8 * w : 0u;
+        const int turn_phase = w == 1 ? turn : turn - 1;
+        // (a run's keys: 64 k .. 64 k + 63 of the tile; in two runs 32 k .. 32 k + 31 and the same from 64 on)
+        const uint64_t v_lo = v0 + (kRuns ? 256u : 512u), v_hi = v0 + (kRuns ? 256u : 0u);
+        wait(bar_p + 16 * w, mine + j);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, (ks < 2 ? v0 : v_hi) + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
+        commit2_if(leader, bar_pv + 16 * w);
+        if (j + 1 < n) wait(tile_bar(full_k, set, c0 + j + 1), (c0 + j + 1) / kStages);
+        if (kRuns && j + 1 < n) {
+          if (!ok) break;
+          tc_fence_after();
+          s_product(k_addr, 0, idesc_run);  // over these weights: the tensor core works a thread's products off in order
+        }
+        {  // the other weights and the turn, looked for at once by different lanes
+          const bool second = (lane & 1) && turn_bar != 0u;
+          wait(second ? turn_bar : bar_p + 16 * w + 8, second ? turn_phase : mine + j);
+        }
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + kRunP + 8 * ks, (ks < 2 ? v_lo : v_lo + v_hi - v0) + 128 * ks, idesc_o, 1u);
+        commit2_if(leader, bar_pv + 16 * w + 8);
+        if (j + 1 < n) s_product(k_addr, kRuns ? 1 : 0, kRuns ? idesc_run : idesc_s);
+        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * (1 - w));
+        if (j + 2 == n) commit2_if(leader, bar_qfree + 8 * w);
+        give_back(ev);
+        if (j + 1 < n) give_back(ek);
+      }
+      if (!dual)
+        for (int j = n; ok && j < n_other; ++j) {
+          hand_on(full_k, empty_k, j);
+          hand_on(v_ready, empty_v, j);
+        }
+      if (!ok) break;
+      t0 += dual ? n + n_other : max(n, n_other);
+      if (dual) counts[1] += n; else counts[0] += max(n, n_other);
+      if (!kRuns) turns += min(n, n_other);
+      mine += n;
+      if (n > 0) ++done;
+    }
+    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    asm volatile(
+        "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %1, 0;\n\t"
+        "@pe tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar_drain), "r"(leader) : "memory");
+    __syncwarp();
+    if (!mbar_wait_bounded(bar_drain, 0, 1u << 12) && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+  };
+
+  if (warp >= kGSoftWarps) {
+    reg_alloc_dec<kGRegsControl>();
+    if (warp == kGProducer) {
+      // ================= units, and TMA: this CTA's rows of Q, pages of K, dims of V =================
+      const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
+      const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
+      const uint32_t to_q = uniform(in_cta(bar_q, 0));
+      const int64_t n_units = !plan.listed ? plan.slots * heads
+                              : n_blocks == 0 ? 0 : static_cast<int64_t>(scan[4]);
+      int64_t round = 0;
+      // b: the unit's sequence. part of parts: of the tiles.
+      int b_now = 0, lo_now = 0, hi_now = 0;  // the unit's sequence and keys
+      int my_parts = 0;                       // (cut) of the row block whose first part this pair has
+      auto make_unit = [&](GUnit& un, int qb, int h, int b, int4 span, int part, int parts, int slot) {
+        const int nq = span.y, L = span.z, row0 = qb * block_rows;
+        const int rows = min(block_rows, nq - row0);
+        int lo, hi;
+        key_range(row0, row0 + rows - 1, nq, L, span.w, lo, hi);
+        if (p.first_keys != nullptr) {  // documents: the first key that any of the rows sees
+          int first_key = INT_MAX;
+          for (int i = lane; i < rows; i += 32) first_key = min(first_key, p.first_keys[span.x + row0 + i]);
+          lo = max(lo, __reduce_min_sync(0xffffffffu, first_key));
+        }
+        int n[2], tile0 = lo / kGKeys, key_end = hi;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int from = row0 + half_rows * w, last = min(from + half_rows, nq) - 1;
+          int lo_w, hi_w = 0;
+          if (from < nq) key_range(from, last, nq, L, span.w, lo_w, hi_w);
+          n[w] = hi_w > lo ? (hi_w + kGKeys - 1) / kGKeys - tile0 : 0;
+        }
+        if (parts > 1) {  // (both halves' tiles within this part of the block's)
+          const int all = max(n[0], n[1]);
+          const int from = static_cast<int>(static_cast<int64_t>(all) * part / parts), to = static_cast<int>(static_cast<int64_t>(all) * (part + 1) / parts);
+          n[0] = min(max(n[0] - from, 0), to - from);
+          n[1] = min(max(n[1] - from, 0), to - from);
+          tile0 += from;
+          key_end = static_cast<int>(min(static_cast<int64_t>(hi), (static_cast<int64_t>(tile0) + to - from) * kGKeys));
+        }
+        int dual = kOneHead;
+        if (by_two && rows <= half_rows && h + 1 < heads) {
+          dual = kTwoHeads;
+          n[1] = n[0];
+        } else if (!by_two && n[0] > 1 && rows <= half_rows) {  // (the second half has no rows, and pairs are not short)
+          dual = kSplitKeys;
+          n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last key)
+        }
+        un = GUnit{row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0};
+        b_now = b;
+        lo_now = lo;
+        hi_now = key_end;
+      };
+      // The pair's next unit: every pairs-th of the order, to and fro, so that each pair gets early (long) and late
+      // (short) ones. Unlisted blocks may be empty: 32 at a time are looked at.
+      auto find_unit = [&](GUnit& un) {
+        if (plan.listed) {
+          while (round * pairs < n_units) {
+            const int r = static_cast<int>(round++), at = r * pairs + (r & 1 ? pairs - 1 - pair : pair);
+            if (at >= n_units) continue;
+            int entry = -1;  // the last one whose units start at or before this one
+#pragma unroll
+            for (int i = 0; i < kGMaxList; i += 32)
+              entry += __popc(__ballot_sync(0xffffffffu, i + lane < n_blocks && work[i + lane] <= static_cast<uint32_t>(at)));
+            const uint32_t e = list[entry];
+            const int units = static_cast<int>(entry + 1 < n_blocks ? work[entry + 1] : n_units) - static_cast<int>(work[entry]);
+            const int in_entry = at - static_cast<int>(work[entry]);
+            const int parts = plan.cut ? units / heads : 1;
+            const int h = in_entry / parts;
+            make_unit(un, (e & (kGSmallBlock - 1)) >> 7, by_two && (e & kGSmallBlock) ? 2 * h : h, e & 127, spans[e & 127], in_entry % parts, parts, at);
+            if (plan.cut && in_entry % parts == 0 && parts > 1) my_parts = parts;
+            return true;
+          }
+          return false;
+        }
+        while (true) {
+          const int64_t r = round + lane, at = r * pairs + (r & 1 ? pairs - 1 - pair : pair);
+          int qb = 0, b = 0, h = 0;
+          SeqSpan sp{0, 0, 0};
+          if (at < n_units) {
+            // Sequence b's blocks stand from place cu_q[b] / block_rows + b on: the next sequence's come behind them,
+            // and all places are one a sequence and one for every block_rows tokens.
+            h = static_cast<int>(at % heads);
+            const int64_t place = plan.slots - 1 - at / heads;
+            int hi = p.batch;  // the last sequence whose first place is not behind this one
+            while (hi - b > 1) {
+              const int mid = (b + hi) >> 1;
+              if (p.cu_q[mid] / block_rows + static_cast<int64_t>(mid) <= place) b = mid; else hi = mid;
+            }
+            const int64_t in_seq = place - (p.cu_q[b] / block_rows + static_cast<int64_t>(b));
+            qb = in_seq < 0 || in_seq >= plan.q_blocks ? plan.q_blocks : static_cast<int>(in_seq);
+            if (qb < plan.q_blocks) sp = seq_span(p, b);
+            else qb = 0;  // (no such block: sp has no rows)
+          }
+          const bool small = sp.nq - qb * block_rows <= half_rows;  // heads two by two
+          if (small) h *= 2;
+          const uint32_t have = __ballot_sync(0xffffffffu, qb * block_rows < sp.nq && h < heads);
+          if (have == 0) {
+            // (r grows with the lane, and so does `at` from one pair of rounds to the next)
+            if (round * pairs >= n_units) return false;
+            round += 32;
+            continue;
+          }
+          const int src = __ffs(have) - 1;
+          round += src + 1;
+          auto from_lane = [&](int v) { return __shfl_sync(0xffffffffu, v, src); };
+          const int b_src = from_lane(b);
+          make_unit(un, from_lane(qb), from_lane(h), b_src, make_int4(from_lane(sp.q0), from_lane(sp.nq), from_lane(sp.L), prefix_of(b_src)), 0, 1, -1);
+          return true;
+        }
+      };
+      int t = 0, done[2] = {0, 0};  // tiles so far; units of each half so far
+      int counts[3] = {0, 0, 0};    // tiles so far by set of barriers
+      for (int k = 0;; ++k) {
+        GUnit un;
+        const bool more = find_unit(un);
+        if (!more) un.row0 = -1;
+        if (plan.cut && k == 0 && rank == 0 && lane == 0)  // what the merge finds at this pair's place (it has one unit at most)
+          reinterpret_cast<PrefillRecord*>(static_cast<uint8_t*>(p.workspace) + prefill_records_at(D))[pair] =
+              PrefillRecord{my_parts, un.row0, more ? un.h : 0, more ? un.q0 : 0, more ? un.nq : 0, {0, 0, 0}};
+        const int slot = k % kGUnitSlots;
+        if (k >= kGUnitSlots) ok = __all_sync(0xffffffffu, mbar_wait_bounded(unit_empty + 8 * slot, (k / kGUnitSlots - 1) & 1));
+        if (!ok) break;
+        if (lane == 0) {
+          units[slot] = un;
+          mbar_arrive_tc(unit_full + 8 * slot);
+        }
+        __syncwarp();
+        if (!more) break;
+        // Page numbers, four tiles (32 pages) at a time: of the first half's tiles (or all) and of the second half's where they
+        // are others. Pages that no row sees are not looked at and read as zeros, like a page number beyond the cache.
+        const int32_t* table = p.block_table + static_cast<int64_t>(b_now) * p.block_table_stride;
+        const int tile0 = un.tile0;
+        auto load_pages = [&](int first_tile) {
+          const int64_t page = (static_cast<int64_t>(tile0) + first_tile) * 8 + lane;
+          int id = p.geom.num_pages;
+          bool bad = false;
+          if (page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now) {
+            const int v = table[page];
+            bad = v < 0 || v >= p.geom.num_pages;
+            if (!bad) id = v;
+          }
+          if (bad) {
+            reinterpret_cast<volatile GUnit*>(units)[slot].bad = 1;
+            __threadfence_block();
+            report(p.status, PDA_DEV_BAD_PAGE);
+          }
+          __syncwarp();
+          return id;
+        };
+        const bool two_streams = un.dual == kSplitKeys;
+        int pages0 = load_pages(0), next0 = un.tiles() > 4 ? load_pages(4) : 0;
+        int pages1 = two_streams ? load_pages(un.n0) : 0, next1 = two_streams && un.n1 > 4 ? load_pages(un.n0 + 4) : 0;
+        const int n_all = un.tiles();
+        auto load_q = [&](int w) {
+          if (ok && done[w] > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_qfree + 8 * w, (done[w] - 1) & 1));
+          if (!ok) return;
+          const int head = uniform(un.head(w) * p.group), token = uniform(un.q0 + un.first_row(w, half_rows) + plan.tile_rows * rank);
+          mbar_expect_tx_if(first, bar_q + 8 * w, 2 * C::kLines * plan.tile_rows * p.group * 128);
+#pragma unroll
+          for (int ln = 0; ln < C::kLines; ++ln)
+            tma_load_4d_pair_if(leader, u_q + w * C::kQBytes + ln * kGQLine, &maps.q, to_q + 8 * w, ln, head, token);
+          ++done[w];
+        };
+        if (un.n0 > 0) load_q(0);
+        for (int i = 0; ok && i < n_all; ++i, ++t) {
+          const int u_h = uniform(un.head(un.half_of(i)));
+          const int st = uniform(t % kStages), rnd = t / kStages;
+          // this tile's pages in lanes 8 j .. 8 j + 7 of `ids`
+          const int j = un.dual ? i >> 1 : i;
+          const bool other = two_streams && (i & 1);
+          if ((j & 3) == 0 && j > 0 && !(un.dual == kTwoHeads && (i & 1))) {
+            if (other) {
+              pages1 = next1;
+              if (j + 4 < un.n1) next1 = load_pages(un.n0 + j + 4);
+            } else {
+              pages0 = next0;
+              if (j + 4 < (un.dual ? un.n0 : n_all)) next0 = load_pages(j + 4);
+            }
+          }
+          const int ids = other ? pages1 : pages0;
+          if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_k + 8 * st, (rnd - 1) & 1));
+          if (!ok) break;
+          const int set = un.dual ? 1 + (i & 1) : 0;
+          const int count = set == 0 ? counts[0] : set == 1 ? counts[1] : counts[2];
+          const uint32_t bar = uniform(tile_bar(full_k, set, count)), to_k = uniform(in_cta(bar, 0));
+          if (set == 0) ++counts[0]; else if (set == 1) ++counts[1]; else ++counts[2];
+          mbar_expect_tx_if(first, bar, 2 * C::kKBytes);
+          const uint32_t kd = u_k + st * C::kKBytes;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int page = __shfl_sync(0xffffffffu, ids, (j & 3) * 8 + 4 * rank + g);
+#pragma unroll
+            for (int ln = 0; ln < C::kLines; ++ln)
+              tma_load_page_pair_if(leader, kd + ln * kGKLine + g * 2048, &maps.k, to_k, ln, u_h, page);
+          }
+          if (i == 0 && un.n1 > 0) load_q(1);
+          if (ok && rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_v + 8 * st, (rnd - 1) & 1));
+          if (!ok) break;
+          mbar_expect_tx_if(leader, full_v + 8 * st, C::kVBytes);
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            const int page = __shfl_sync(0xffffffffu, ids, (j & 3) * 8 + g);
+            tma_load_5d_if(leader, u_v + st * C::kVBytes + g * 2048, &maps.v, full_v + 8 * st, D == 128 ? rank : 0, u_h, page);
+          }
+        }
+        if (!ok) break;
+      }
+      if (!ok) {  // copies in flight end before the CTA does: they are given time (a millisecond; a copy takes microseconds)
+        if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+        for (int k = 0; k < 256; ++k) mbar_wait_bounded(bar_never, 0, 1);  // (4 us a poll)
+      }
+    } else if (warp == kGRelay) {
+      // ================= V tiles: cleared behind the sequence's end, then handed to the first CTA =================
+      int counts[3] = {0, 0, 0};  // tiles so far by set of barriers
+      GUnit un;
+      int t = 0;
+      for (int k = 0; next_unit(k, un); ++k) {
+        free_unit(k);
+        const int n_all = un.tiles();
+        for (int i = 0; ok && i < n_all; ++i, ++t) {
+          const int st = t % kStages;
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_v + 8 * st, (t / kStages) & 1));
+          if (!ok) break;
+          const int64_t valid = un.L - (static_cast<int64_t>(un.tile0) + un.keys_of(i)) * kGKeys;
+          const bool partly = valid > 0 && valid < kGKeys;  // (pages behind the end have been read as zeros)
+          if (partly) {
+            // (keys behind the end have weight 0, but what they hold may be anything)
+            for (int c = lane; c < (kGKeys - static_cast<int>(valid)) * 8; c += 32)
+              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_sm + st * C::kVBytes + static_cast<int>(valid) * 128 + c * 16), "r"(0));
+            fence_proxy_async();
+          }
+          const int set = un.dual ? 1 + (i & 1) : 0;
+          const int count = set == 0 ? counts[0] : set == 1 ? counts[1] : counts[2];
+          const uint32_t to = in_cta(tile_bar(v_ready, set, count), 0);
+          if (set == 0) ++counts[0]; else if (set == 1) ++counts[1]; else ++counts[2];
+          __syncwarp();
+          if (lane == 0) {
+            if (partly) arrive_cluster(to);  // (with what has been written before it)
+            else arrive_cluster_tc(to);
+          }
+        }
+        if (!ok) break;
+      }
+      if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    } else if (warp == kGMma && rank == 0) {
+      issue_role(std::integral_constant<int, 0>{});
+    } else if (warp == kGMma + 1 && rank == 0) {
+      issue_role(std::integral_constant<int, 1>{});
+    } else if (warp == kGMma && pair == 0 && !plan.listed) {
+      for (int b = lane; b < p.batch; b += 32) seq_span(p, b);  // (reports sequences that no place leads to)
+    }
+  } else {
+    reg_alloc_inc<kGRegsSoftmax>();
+    // ================= softmax and output: thread = row =================
+    const int w = warp >> 2;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t my_s = tmem + 128 * w + lane_base, my_o = tmem + kGTmemO + 128 * w + lane_base;
+    const float scale_log2 = kZ ? 1.f : plan.scale_log2;
+    const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
+    const float neg_inf = -INFINITY;
+    // this thread's row of a unit: query token row_token (from the half's first of this CTA), head row_head of the group
+    const int row_token = (tid & 127) / p.group, row_head = (tid & 127) % p.group;
+    const bool row_used = row_token < plan.tile_rows;  // (a group that does not divide 128 leaves rows over)
+    int t = 0, merges = 0;  // tiles of this half, merges with the second half so far
+    for (int unit = 0;; ++unit) {
+      int n, lo, hi;  // tiles; keys that this thread's row sees, from the half's first tile on
+      int full_from, full_to;  // keys that all of the warp's rows see
+      // The row's reference and the factor that goes with it. A row that does not exist is another sequence's, or anything:
+      // its reference is infinite, so that it never asks for the warp's to be raised and has no say in the other rows' rounding.
+      float m_ref, c_ref;
+      float slope = 0.f;  // (biased) per key
+      int key0_pos = 0;   // the half's first key minus the row's position
+      {
+        GUnit un;
+        if (!next_unit(unit, un)) break;
+        n = w == 0 ? un.n0 : un.n1;
+        const int row = un.first_row(w, half_rows) + plan.tile_rows * rank + row_token, pos = un.L - un.nq + row;
+        const bool exists = row_used && row < un.nq;
+        lo = hi = 0;
+        if (exists) visible_keys(pos, un.L, p.score.window, p.first_keys != nullptr ? p.first_keys[un.q0 + row] : 0, un.prefix, lo, hi);
+        const int64_t key0 = (static_cast<int64_t>(un.tile0) + un.key_tile(w, 0)) * kGKeys;
+        const auto from_key0 = [&](int key) { return static_cast<int>(max(min(key - key0, static_cast<int64_t>(1 << 30)), static_cast<int64_t>(-(1 << 30)))); };
+        lo = from_key0(lo);
+        hi = from_key0(min(hi, un.key_end));
+        // (biased: keys behind the token itself go the way of masked tiles, which takes the distance's absolute value)
+        const int full_hi = (kShape & kShapeBias) && exists ? min(hi, from_key0(pos + 1)) : hi;
+        full_from = __reduce_max_sync(0xffffffffu, exists ? lo : -(1 << 30));
+        full_to = __reduce_min_sync(0xffffffffu, exists ? full_hi : 1 << 30);
+        if (!__any_sync(0xffffffffu, exists)) full_to = -(1 << 30);  // (a warp without any row sees nothing)
+        m_ref = exists ? kGNoMax : INFINITY;
+        if constexpr ((kShape & kShapeBias) != 0) {
+          slope = exists && p.score.slopes != nullptr ? p.score.slopes[un.head(w) * p.group + row_head] * kLog2e : 0.f;
+          key0_pos = static_cast<int>(key0 - pos);
+        }
+      }
+      c_ref = score_factor(m_ref, scale_log2);
+      float l = 0.f;
+      // One tile; masked: some row of the warp does not see all of it.
+      auto tile = [&](auto masked, int j) {
+        constexpr bool kMasked = decltype(masked)::value;
+        // 64 keys at a time; the first run's products start while the second run is here
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (kRuns || k == 0) {
+            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 16 * w + 8 * k, t & 1));
+            if (!ok) return;
+            tc_fence_after();
+          }
+          uint32_t sv[64];
+          tmem_ld32(my_s + 64 * k, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+          tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+          tmem_wait_ld();
+          // keys of the run's columns: 64 k + e, or 32 k + e, from the 32nd on 32 k + 32 + e
+          const int first_lo = j * kGKeys + (kRuns ? 32 * k : 64 * k), first_hi = j * kGKeys + (kRuns ? 32 * k + 32 : 64 * k);
+          if constexpr (kZ) {
+            auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
+            const uint64_t mul2 = both(p.score.mul);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {  // 16 keys
+              // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
+              const uint64_t base2 = (kShape & kShapeBias) ? both(slope * static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g)) : 0ull;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int e = 16 * g + 2 * i;
+                [[maybe_unused]] uint64_t bias2 = 0ull;
+                if constexpr ((kShape & kShapeBias) != 0) {
+                  bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), base2);
+                  if (kMasked) {  // -slope |distance|
+                    float b0, b1;
+                    f32x2_split(bias2, b0, b1);
+                    bias2 = f32x2(__float_as_uint(copysignf(b0, -slope)), __float_as_uint(copysignf(b1, -slope)));
+                  }
+                }
+                uint64_t z = f32x2(sv[e], sv[e + 1]);
+                if constexpr ((kShape & kShapeCap) != 0) {
+                  float y0, y1;
+                  f32x2_split(mul_f32x2(z, mul2), y0, y1);
+                  z = f32x2(__float_as_uint(rcp_approx(ex2(y0) + 1.f)), __float_as_uint(rcp_approx(ex2(y1) + 1.f)));
+                  z = fma_f32x2(z, both(-2.f * p.score.cap), both(p.score.cap));
+                  if constexpr ((kShape & kShapeBias) != 0) z = add_f32x2(z, bias2);
+                } else {
+                  z = fma_f32x2(z, mul2, bias2);
+                }
+                float z0, z1;
+                f32x2_split(z, z0, z1);
+                sv[e] = __float_as_uint(z0);
+                sv[e + 1] = __float_as_uint(z1);
+              }
+            }
+          }
+          if (kMasked) {
+            const int hi_lo = hi - first_lo, hi_hi = hi - first_hi, lo_lo = lo - first_lo, lo_hi = lo - first_hi;
+#pragma unroll
+            for (int e = 0; e < 64; ++e)
+              if (e >= (e < 32 ? hi_lo : hi_hi) || e < (e < 32 ? lo_lo : lo_hi)) sv[e] = 0xff800000u;  // -inf
+          }
+          if (k == 0 && j == 0) {  // the first reference: the maximum of the first 64 scores
+            float mx[2] = {neg_inf, neg_inf};
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+            m_ref = fmaxf(m_ref, fmaxf(mx[0], mx[1]));
+            c_ref = score_factor(m_ref, scale_log2);
+          }
+          // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
+          // reference by so much that the reference is raised and the weights are taken again.
+          uint32_t pk[32];
+          float part;
+          float top;
+          auto weights = [&](auto poly) {
+            const float minus_ref = -__fmul_rn(m_ref, c_ref);
+            const uint64_t ref2 = f32x2(__float_as_uint(minus_ref), __float_as_uint(minus_ref));
+            const uint64_t c2 = f32x2(__float_as_uint(c_ref), __float_as_uint(c_ref));
+            uint64_t sum2[2] = {0ull, 0ull};
+            float mx[2] = {neg_inf, neg_inf};
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), c2, ref2);
+              mx[e & 1] = max3_nan(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
+              float w0, w1;
+              if (decltype(poly)::value && e % kGPolyOf == kGPolyOf - 1) {
+                exp2_two(x, w0, w1);
+              } else {
+                f32x2_split(x, w0, w1);
+                w0 = ex2(w0);
+                w1 = ex2(w1);
+              }
+              sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
+              pk[e] = pack2<false>(w0, w1);
+            }
+            float s0, s1;
+            f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
+            part = s0 + s1;
+            top = max3_nan(mx[0], mx[0], mx[1]);
+            if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
+          };
+          while (true) {
+            if (kMasked && __all_sync(0xffffffffu, hi <= first_lo || lo >= first_hi + 64)) {  // no row of the warp sees any of these
+#pragma unroll
+              for (int e = 0; e < 32; ++e) pk[e] = 0;
+              part = 0.f;
+              break;
+            }
+            weights(std::bool_constant<!kMasked>{});  // (weights of hidden keys are exactly zero)
+            const bool raise = top * c_ref > m_ref * c_ref + kGRescale;
+            if (!__any_sync(0xffffffffu, raise)) break;
+            // (only the rows that ask for it: a row's rounding does not depend on its neighbours' scores)
+            const float m_new = raise ? top : m_ref, c_new = score_factor(m_new, scale_log2);
+            const float a = rescale(m_ref, m_new, c_new);
+            m_ref = m_new;
+            c_ref = c_new;
+            l *= a;
+            if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first run of this one
+              if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D / 16; ++c) {
+                uint32_t ov[16];
+                tmem_ld16(my_o + 16 * c, ov);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
+                tmem_st16(my_o + 16 * c, ov);
+              }
+            }
+          }
+          if (!ok) return;
+          l += part;
+          tmem_st32(my_s + kRunP * k, pk);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cluster_tc(to_p + 8 * k);
+        }
+      };
+      for (int j = 0; ok && j < n; ++j, ++t) {
+        if (full_from <= j * kGKeys && full_to >= (j + 1) * kGKeys) tile(std::false_type{}, j);
+        else tile(std::true_type{}, j);
+      }
+      // ---- output
+      if (n > 0) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (t - 1) & 1));
+        tc_fence_after();
+      }
+      GUnit un = units[unit % kGUnitSlots];  // (read again: it takes registers that the loop above needs)
+      un.bad = reinterpret_cast<volatile GUnit*>(units)[unit % kGUnitSlots].bad;
+      free_unit(unit);
+      const int row = un.first_row(w, half_rows) + plan.tile_rows * rank + row_token;  // query token of the sequence
+      const bool exists = row_used && row < un.nq;
+      const bool split = un.dual == kSplitKeys;
+      float* sums = merge_sh + 2 * (tid & 127);  // the row's reference and sum from the second half
+      if (split && w == 1) {  // the first half's warp of the same rows takes it from here
+        *reinterpret_cast<float2*>(sums) = make_float2(m_ref, l);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_tc(bar_merge + 8 * (warp & 3));
+        if (!ok) break;
+        continue;
+      }
+      if (split) {  // O and the sum of both halves, in the first half's place
+        if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_merge + 8 * (warp & 3), merges & 1));
+        tc_fence_after();
+        ++merges;
+        const float2 other = *reinterpret_cast<const float2*>(sums);
+        const float m = fmaxf(m_ref, other.x);
+        const float c_new = score_factor(m, scale_log2);
+        const float mul = rescale(m_ref, m, c_new), mul_other = rescale(other.x, m, c_new);
+        m_ref = m;
+        l = l * mul + other.y * mul_other;
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t ov[16], o2[16];
+          tmem_ld16(my_o + 16 * c, ov);
+          tmem_ld16(my_o + 128 + 16 * c, o2);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(fmaf(__uint_as_float(o2[e]), mul_other, __uint_as_float(ov[e]) * mul));
+          tmem_st16(my_o + 16 * c, ov);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cluster_tc(to_ofree + 8);  // (the second half's O has been read)
+      }
+      // A row that sees keys has a score at its reference, of weight 1 or (c r rounded) a little less, unless none of them is
+      // finite: then it has no softmax and is NaN. (The polynomial gives such scores 2^-126.) Rows that see nothing are zero.
+      bool some = n > 0 && ok && exists && !un.bad;
+      if (some) {
+        int see_lo, see_hi;
+        visible_keys(un.L - un.nq + row, un.L, p.score.window, p.first_keys != nullptr ? p.first_keys[un.q0 + row] : 0, un.prefix, see_lo, see_hi);
+        some = see_lo < see_hi;
+      }
+      const bool partial = un.slot >= 0;
+      float inv = 1.f / (l < 5.4210109e-20f ? NAN : l);  // 2^-64
+      float* part_o = nullptr;
+      if (partial) {  // sums go to the workspace as they are, for the merge
+        const int64_t at = static_cast<int64_t>(un.slot) * kPreRows + (2 * w + rank) * 128 + (tid & 127);
+        part_o = static_cast<float*>(p.workspace) + at * D;
+        float2* ws = reinterpret_cast<float2*>(static_cast<uint8_t*>(p.workspace) + prefill_sums_at(D)) + at;
+        // (no tile here, or no page: nothing. A bad page anywhere makes the row zero: marked by a negative sum)
+        if (exists) *ws = un.bad ? make_float2(INFINITY, -1.f) : n > 0 ? make_float2(m_ref, l) : make_float2(kGNoMax, 0.f);
+        some = n > 0 && ok && !un.bad;
+        inv = 1.f;
+      }
+      __nv_bfloat16* out = p.out + (static_cast<int64_t>(un.q0) + row) * p.out_token_stride + (un.head(w) * p.group + row_head) * p.out_head_stride;
+      // A thread stores its own row, 32 bytes (a whole sector) at a time where the rows' alignment allows it.
+      const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0 && p.out_token_stride % 16 == 0 && p.out_head_stride % 16 == 0;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t ov[32];
+        tmem_ld32(my_o + 32 * c, ov);
+        tmem_wait_ld();
+        if (c == D / 32 - 1 && n > 0) {  // O is in registers: the next unit's products may write it
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cluster_tc(to_ofree);
+        }
+        if (exists && partial) {
+          if (some) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+              asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(part_o + 32 * c + k), "r"(ov[k]), "r"(ov[k + 1]), "r"(ov[k + 2]),
+                           "r"(ov[k + 3]), "r"(ov[k + 4]), "r"(ov[k + 5]), "r"(ov[k + 6]), "r"(ov[k + 7]) : "memory");
+          }
+        } else if (exists) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 2)
+            ov[e >> 1] = some ? pack2<false>(__uint_as_float(ov[e]) * inv, __uint_as_float(ov[e + 1]) * inv) : 0u;
+#pragma unroll
+          for (int k = 0; k < 16; k += 8) {
+            __nv_bfloat16* dst = out + 32 * c + 2 * k;
+            if (wide) {
+              asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(ov[k]), "r"(ov[k + 1]), "r"(ov[k + 2]),
+                           "r"(ov[k + 3]), "r"(ov[k + 4]), "r"(ov[k + 5]), "r"(ov[k + 6]), "r"(ov[k + 7]) : "memory");
+            } else {
+              reinterpret_cast<uint4*>(dst)[0] = make_uint4(ov[k], ov[k + 1], ov[k + 2], ov[k + 3]);
+              reinterpret_cast<uint4*>(dst)[1] = make_uint4(ov[k + 4], ov[k + 5], ov[k + 6], ov[k + 7]);
+            }
+          }
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+    }
+    if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+  }
+
+  // ---- teardown: neither CTA leaves while the other may still reach its barriers or tensor memory
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0 && *cta_err) report(p.status, *cta_err);
+  cluster_sync();
+  if (warp == kGMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kGTmemCols) : "memory");
+  }
+}
+
+// Joins the parts of row blocks that were cut along the keys. A warp per row; a lane owns D / 32 columns.
+template <int D>
+__global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ PrefillPlan plan, float scale_log2) {
+  constexpr int kCols = D / 32;
+  const uint8_t* ws = static_cast<const uint8_t*>(p.workspace);
+  const PrefillRecord rec = reinterpret_cast<const PrefillRecord*>(ws + prefill_records_at(D))[blockIdx.x];
+  const int lane = threadIdx.x & 31;
+  for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); rec.parts > 0 && r < kPreRows; r += gridDim.y * 8) {
+    const int quarter = r >> 7, in_tile = r & 127, token = in_tile / p.group, head = in_tile % p.group;
+    const int row = rec.row0 + quarter * plan.tile_rows + token;
+    if (token >= plan.tile_rows || row >= rec.nq) continue;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kPreRows + r;
+    const float2* sums = reinterpret_cast<const float2*>(ws + prefill_sums_at(D)) + at;
+    float m = kGNoMax;
+    bool bad = false;
+    for (int k = lane; k < rec.parts; k += 32) {
+      const float2 s = sums[static_cast<int64_t>(k) * kPreRows];
+      m = fmaxf(m, s.y != 0.f ? s.x : kGNoMax);
+      bad |= s.y < 0.f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    bad = __any_sync(0xffffffffu, bad);
+    const float c = score_factor(m, scale_log2);
+    float acc[kCols], l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < rec.parts; ++k) {
+      const float2 s = sums[static_cast<int64_t>(k) * kPreRows];
+      if (bad || s.y == 0.f) continue;  // (nothing of this row in that part)
+      const float mul = rescale(s.x, m, c);
+      const float* o = reinterpret_cast<const float*>(ws) + (at + static_cast<int64_t>(k) * kPreRows) * D + kCols * lane;
+      l = fmaf(s.y, mul, l);
+      if constexpr (kCols == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(o);
+        acc[0] = fmaf(v.x, mul, acc[0]), acc[1] = fmaf(v.y, mul, acc[1]), acc[2] = fmaf(v.z, mul, acc[2]), acc[3] = fmaf(v.w, mul, acc[3]);
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(o);
+        acc[0] = fmaf(v.x, mul, acc[0]), acc[1] = fmaf(v.y, mul, acc[1]);
+      }
+    }
+    const bool zero = bad || l == 0.f;
+    const float inv = 1.f / (l < 5.4210109e-20f ? NAN : l);
+    uint32_t packed[kCols / 2];
+#pragma unroll
+    for (int i = 0; i < kCols; i += 2) packed[i / 2] = zero ? 0u : pack2<false>(acc[i] * inv, acc[i + 1] * inv);
+    __nv_bfloat16* out = p.out + (static_cast<int64_t>(rec.q0) + row) * p.out_token_stride + (rec.h * p.group + head) * p.out_head_stride + kCols * lane;
+    if constexpr (kCols == 4) *reinterpret_cast<uint2*>(out) = make_uint2(packed[0], packed[1]);
+    else *reinterpret_cast<uint32_t*>(out) = packed[0];
+  }
+}
+
+}  // namespace
+}  // namespace pda

@@ -44,12 +44,13 @@ struct PrefillParams {
 
 // What sequence b asks for: its query tokens q0 .. q0 + nq - 1 are the last of its L tokens. A sequence whose ranges do
 // not fit is reported and has no keys; of its rows, those that lie in the array (up to max_q) are zeroed.
+constexpr int32_t kMaxTokens = 1 << 30;  // of a sequence with packed queries: keys are counted in 32 bits from anywhere
 struct SeqSpan {
   int32_t q0, nq, L;
 };
 __device__ __forceinline__ SeqSpan seq_span(const PrefillParams& p, int b) {
   const int L = max(p.seq_lens[b], 0);
-  const bool fits = static_cast<int64_t>(L) <= static_cast<int64_t>(p.block_table_stride) * kPageSize;
+  const bool fits = static_cast<int64_t>(L) <= static_cast<int64_t>(p.block_table_stride) * kPageSize && (L <= kMaxTokens || p.cu_q == nullptr);
   if (p.cu_q == nullptr) {
     if (!fits) report(p.status, PDA_DEV_BAD_SEQ_LEN);
     return {b, 1, fits ? L : 0};
