@@ -1,4 +1,7 @@
 // Launch of the tcgen05 prompt kernel over the paged cache (prefill_tc.cuh).
+#include <cmath>
+#include <cstring>
+
 #include "prefill_tc.cuh"
 
 namespace pda {
@@ -19,6 +22,31 @@ bool encode_q(CUtensorMap* map, const PrefillParams& p, int tile_rows) {
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The polynomials of the cap in the product s: C tanh(u s), u = mul / (2 log2 e). Where u is so far from 1 that powers of u or
+// of s could leave 32 bits' range, all go the other way.
+void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
+  // tanh(x) by odd polynomials whose largest error over the range is least (linear programming over 4000 points):
+  // 5.3e-6 for |x| <= 1/2, 2.8e-6 for |x| <= 1
+  static const double c5[3] = {0.9999248385429382, -0.33085504174232483, 0.11254137754440308};
+  static const double c9[5] = {0.9999684691429138, -0.33265823125839233, 0.12922066450119019, -0.04329986125230789, 0.008365885354578495};
+  const double u = static_cast<double>(score.mul) / (2.0 * 1.4426950408889634);
+  const auto twice = [](double v) {
+    const float f = static_cast<float>(v);
+    uint32_t bits;
+    memcpy(&bits, &f, 4);
+    return static_cast<uint64_t>(bits) << 32 | bits;
+  };
+  const bool usable = std::abs(u) >= 1.0 / 4096 && std::abs(u) <= 4096 && score.cap <= 4096.f && score.cap >= 1.f / 4096;
+  plan->limit[0] = usable ? static_cast<float>(0.5 / std::abs(u)) : -1.f;
+  plan->limit[1] = usable ? static_cast<float>(1.0 / std::abs(u)) : -1.f;
+  plan->ref = shape == kShapeCap ? std::max(score.cap - kGFixedTop, 0.f) : 0.f;
+  double power = u * score.cap;
+  for (int i = 0; i < 5; ++i, power *= u * u) {
+    if (i < 3) plan->poly5[i] = twice(usable ? c5[i] * power : 0.0);
+    plan->poly9[i] = twice(usable ? c9[i] * power : 0.0);
+  }
+}
+
 template <int D, int kShape>
 cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const PrefillPlan& plan, bool runs, int pairs, cudaStream_t stream) {
   const auto kernel = runs ? prefill_tc_kernel<D, kShape, true> : prefill_tc_kernel<D, kShape, false>;
@@ -26,7 +54,8 @@ cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const Prefil
   if (e != cudaSuccess) return e;
   kernel<<<static_cast<unsigned>(2 * pairs), kGThreads, GCfg<D>::kSmemBytes, stream>>>(maps, p, plan);
   if ((e = cudaGetLastError()) != cudaSuccess || !plan.cut) return e;
-  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone ? plan.scale_log2 : 1.f);
+  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone ? plan.scale_log2 : 1.f,
+                                                                                       kShape == kShapeCap ? 0.f : 5.4210109e-20f);
   return cudaGetLastError();
 }
 
@@ -71,9 +100,13 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   const int cut = listed && p.workspace != nullptr && 2 * most * heads <= std::min(all_pairs, kPreMaxPairs) ? 1 : 0;
   if (cut) pairs = std::min(all_pairs, kPreMaxPairs);
   const bool runs = true;
-  // (unshaped scores are scaled behind the maximum, which needs a factor above 0)
-  const int shape = (p.score.cap > 0.f ? kShapeCap : 0) | (p.score.slopes != nullptr || (p.score.cap == 0.f && !(p.score.mul > 0.f)) ? kShapeBias : 0);
-  const PrefillPlan plan{q_blocks, tile_rows, listed, listed ? 0 : places, cut, p.score.mul};
+  // Scores that are only capped have a fixed reference, if the cap allows it; otherwise the bias's form takes them, with slopes of
+  // 0, and so it does scores that are not shaped if their factor is not above 0 (they are scaled behind the maximum).
+  const float cap = p.score.cap;
+  const int shape = (cap > 0.f ? kShapeCap : 0) |
+                    (p.score.slopes != nullptr || cap > kGFixedCap || (cap == 0.f && !(p.score.mul > 0.f)) ? kShapeBias : 0);
+  PrefillPlan plan{q_blocks, tile_rows, listed, listed ? 0 : places, cut, p.score.mul};
+  if (cap > 0.f) set_cap(p.score, shape, &plan);
   const int n = static_cast<int>(pairs);
   if (g.head_dim == 128) {
     if (shape == kShapeNone) return launch<128, kShapeNone>(p, maps, plan, runs, n, stream);

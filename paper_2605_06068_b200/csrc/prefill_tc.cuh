@@ -8,7 +8,7 @@
 //                        (head_dim 64: both hold all 64, and O comes out twice; the exponentials bound that case)
 // S[0], S[1], O[0], O[1] fill the 512 TMEM columns. A thread is a row's softmax and takes 64 keys at a time.
 // The softmax takes weights relative to a reference per row that is raised (and O rescaled in tensor memory) only when
-// the row's maximum passes it by more than 2^8; row sums are kept by the row's thread, of the 32-bit weights.
+// the row's maximum passes it by more than 2^32; row sums are kept by the row's thread, of the 32-bit weights.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the pair's first
 // CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are bounded.
 #include <algorithm>
@@ -30,6 +30,10 @@ struct PrefillPlan {
   int64_t slots;  // (not listed) row blocks are looked for at this many places
   int cut;        // few units: blocks are cut along the keys, so that every pair has a part
   float scale_log2;
+  // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): of degree 5 for
+  // |s| <= limit[0], of degree 9 for |s| <= limit[1]; minus the fixed reference (capped only), or 0.
+  float limit[2], ref;
+  uint64_t poly5[3], poly9[5];
 };
 struct PrefillMaps {
   CUtensorMap q, k, v;
@@ -56,9 +60,15 @@ constexpr uint32_t kGTmemCols = 512, kGTmemO = 256;
 constexpr int kGUnitSlots = 4;   // units the producer may be ahead
 constexpr int kGMaxList = 128;   // row blocks that are sorted by their work
 constexpr float kGNoMax = -FLT_MAX;
-constexpr float kGRescale = 8.f;
+// A row's reference is raised once a score passes it by 2^32: weights and their sums are floating-point numbers of 8 exponent
+// bits, whose precision does not depend on their size, and 32 leaves values up to 2^64 room. With 2^8 (scores of +-15: a warp
+// raises on half of its tiles) a prompt of 8192 tokens took 934 us instead of 570.
+constexpr float kGRescale = 32.f;
 constexpr int kGPolyOf = 4;      // every fourth pair of exponentials by polynomial
 constexpr int kGMinTiles = 4;    // of a part
+// Capped scores that are not biased lie within [-C, C] (ScoreParams): they need no maximum. Their weights are taken relative
+// to a reference fixed at max(C - 60, 0), which keeps them and their sums within 2^-120 .. 2^60 for C <= 90 (a cap up to 62).
+constexpr float kGFixedTop = 60.f, kGFixedCap = 90.f;
 
 // How scores are shaped (bits): capped; biased by distance.
 enum : int { kShapeNone = 0, kShapeCap = 1, kShapeBias = 2 };
@@ -122,7 +132,7 @@ __device__ __forceinline__ float rescale(float from, float to, float c) { return
 // the later n1 tiles of the same head, and the first half's warps merge the two results.
 enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
 struct GUnit {
-  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace
+  int b, row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace
   __device__ int first_row(int w, int half_rows) const { return row0 + (dual ? 0 : half_rows * w); }
   __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
   __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
@@ -154,6 +164,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   using C = GCfg<D>;
   constexpr int kStages = C::kStages;
   constexpr bool kZ = kShape != kShapeNone;        // scores are shaped before the softmax
+  constexpr bool kFixed = kShape == kShapeCap;     // ... and lie within bounds: the reference is fixed
   constexpr uint32_t kRunP = kRuns ? 64 : 32;      // columns from the first run's weights to the second's
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -512,7 +523,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           dual = kSplitKeys;
           n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last key)
         }
-        un = GUnit{row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0};
+        un = GUnit{b, row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0};
         b_now = b;
         lo_now = lo;
         hi_now = key_end;
@@ -754,10 +765,34 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         full_from = __reduce_max_sync(0xffffffffu, exists ? lo : -(1 << 30));
         full_to = __reduce_min_sync(0xffffffffu, exists ? full_hi : 1 << 30);
         if (!__any_sync(0xffffffffu, exists)) full_to = -(1 << 30);  // (a warp without any row sees nothing)
-        m_ref = exists ? kGNoMax : INFINITY;
+        m_ref = kFixed ? plan.ref : exists ? kGNoMax : INFINITY;
         if constexpr ((kShape & kShapeBias) != 0) {
           slope = exists && p.score.slopes != nullptr ? p.score.slopes[un.head(w) * p.group + row_head] * kLog2e : 0.f;
           key0_pos = static_cast<int>(key0 - pos);
+          // A bias has the scores rise from tile to tile, up to the token's own key: its score, which no distance lowers, is
+          // taken here as the first reference. (The row's maximum is no lower, and rarely is it much higher.)
+          if (exists && n > 0 && pos >= 0 && lo <= -key0_pos) {
+            const int page = p.block_table[static_cast<int64_t>(un.b) * p.block_table_stride + pos / kPageSize];
+            if (page >= 0 && page < p.geom.num_pages) {
+              const uint4* q = reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(un.q0) + row) * p.q_token_stride + (un.head(w) * p.group + row_head) * p.q_head_stride);
+              const uint4* key = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_cache) + page * p.geom.page_stride +
+                                                                un.head(w) * p.geom.head_stride + (pos % kPageSize) * p.geom.slot_stride);
+              float dot = 0.f;
+#pragma unroll 4
+              for (int c = 0; c < D / 8; ++c) {
+                const uint4 a = q[c], b = key[c];
+                const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  dot = fmaf(__uint_as_float(aw[e] << 16), __uint_as_float(bw[e] << 16), dot);
+                  dot = fmaf(__uint_as_float(aw[e] & 0xffff0000u), __uint_as_float(bw[e] & 0xffff0000u), dot);
+                }
+              }
+              dot *= p.score.mul;
+              if constexpr ((kShape & kShapeCap) != 0) dot = fmaf(-2.f * p.score.cap, rcp_approx(ex2(dot) + 1.f), p.score.cap);
+              if (fabsf(dot) < 3.0e38f) m_ref = dot;
+            }
+          }
         }
       }
       c_ref = score_factor(m_ref, scale_log2);
@@ -779,49 +814,80 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           tmem_wait_ld();
           // keys of the run's columns: 64 k + e, or 32 k + e, from the 32nd on 32 k + 32 + e
           const int first_lo = j * kGKeys + (kRuns ? 32 * k : 64 * k), first_hi = j * kGKeys + (kRuns ? 32 * k + 32 : 64 * k);
-          if constexpr (kZ) {
-            auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
-            const uint64_t mul2 = both(p.score.mul);
+          // (columns of the run that this row sees: from lo_lo and before hi_lo of the first 32, lo_hi and hi_hi of the others)
+          const int hi_lo = hi - first_lo, hi_hi = hi - first_hi, lo_lo = lo - first_lo, lo_hi = lo - first_hi;
+          auto hidden = [&](int e) { return e >= (e < 32 ? hi_lo : hi_hi) || e < (e < 32 ? lo_lo : lo_hi); };
+          auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
+          auto put = [&](int e, uint64_t z) {
+            float z0, z1;
+            f32x2_split(z, z0, z1);
+            sv[e] = __float_as_uint(z0);
+            sv[e + 1] = __float_as_uint(z1);
+          };
+          if constexpr ((kShape & kShapeCap) != 0) {
+            // The cap, minus the reference where that is fixed. The hyperbolic tangent goes by the row's largest product among the
+            // 64: small ones by a polynomial (|y| <= 1/2: degree 5; |y| <= 1: degree 9), of the form whose largest error is least
+            // (2^-17.5 and 2^-18.5, of 1), others, and infinities and NaN, by exponential and reciprocal: three
+            // results of the special-function unit a score with the weight's, which bound the kernel.
+            if (kMasked) {
+#pragma unroll
+              for (int e = 0; e < 64; ++e) sv[e] = hidden(e) ? 0u : sv[e];
+            }
+            float mx[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3_nan(mx[(e >> 1) & 1], fabsf(__uint_as_float(sv[e])), fabsf(__uint_as_float(sv[e + 1])));
+            const float far = max3_nan(mx[0], mx[1], mx[1]);
+            const float ref = kFixed ? plan.ref : 0.f;
+            const uint64_t minus_ref = both(-ref);
+            if (far <= plan.limit[0]) {
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                const uint64_t x = f32x2(sv[e], sv[e + 1]), t2 = mul_f32x2(x, x);
+                uint64_t y = fma_f32x2(t2, plan.poly5[2], plan.poly5[1]);
+                y = fma_f32x2(t2, y, plan.poly5[0]);
+                put(e, kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y));
+              }
+            } else if (far <= plan.limit[1]) {
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                const uint64_t x = f32x2(sv[e], sv[e + 1]), t2 = mul_f32x2(x, x);
+                uint64_t y = fma_f32x2(t2, plan.poly9[4], plan.poly9[3]);
+                y = fma_f32x2(t2, y, plan.poly9[2]);
+                y = fma_f32x2(t2, y, plan.poly9[1]);
+                y = fma_f32x2(t2, y, plan.poly9[0]);
+                put(e, kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y));
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 64; ++e)
+                sv[e] = __float_as_uint(fmaf(-2.f * p.score.cap, rcp_approx(ex2(__uint_as_float(sv[e]) * p.score.mul) + 1.f), p.score.cap - ref));
+            }
+          }
+          if constexpr ((kShape & kShapeBias) != 0) {
+            const uint64_t mul2 = both((kShape & kShapeCap) ? 1.f : p.score.mul), slope2 = both(slope);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {  // 16 keys
               // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
-              const uint64_t base2 = (kShape & kShapeBias) ? both(slope * static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g)) : 0ull;
+              const uint64_t base2 = both(slope * static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g));
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const int e = 16 * g + 2 * i;
-                [[maybe_unused]] uint64_t bias2 = 0ull;
-                if constexpr ((kShape & kShapeBias) != 0) {
-                  bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), base2);
-                  if (kMasked) {  // -slope |distance|
-                    float b0, b1;
-                    f32x2_split(bias2, b0, b1);
-                    bias2 = f32x2(__float_as_uint(copysignf(b0, -slope)), __float_as_uint(copysignf(b1, -slope)));
-                  }
+                uint64_t bias2 = fma_f32x2(slope2, f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), base2);
+                if (kMasked) {  // -slope |distance|
+                  float b0, b1;
+                  f32x2_split(bias2, b0, b1);
+                  bias2 = f32x2(__float_as_uint(copysignf(b0, -slope)), __float_as_uint(copysignf(b1, -slope)));
                 }
-                uint64_t z = f32x2(sv[e], sv[e + 1]);
-                if constexpr ((kShape & kShapeCap) != 0) {
-                  float y0, y1;
-                  f32x2_split(mul_f32x2(z, mul2), y0, y1);
-                  z = f32x2(__float_as_uint(rcp_approx(ex2(y0) + 1.f)), __float_as_uint(rcp_approx(ex2(y1) + 1.f)));
-                  z = fma_f32x2(z, both(-2.f * p.score.cap), both(p.score.cap));
-                  if constexpr ((kShape & kShapeBias) != 0) z = add_f32x2(z, bias2);
-                } else {
-                  z = fma_f32x2(z, mul2, bias2);
-                }
-                float z0, z1;
-                f32x2_split(z, z0, z1);
-                sv[e] = __float_as_uint(z0);
-                sv[e + 1] = __float_as_uint(z1);
+                put(e, fma_f32x2(f32x2(sv[e], sv[e + 1]), mul2, bias2));
               }
             }
           }
           if (kMasked) {
-            const int hi_lo = hi - first_lo, hi_hi = hi - first_hi, lo_lo = lo - first_lo, lo_hi = lo - first_hi;
 #pragma unroll
             for (int e = 0; e < 64; ++e)
-              if (e >= (e < 32 ? hi_lo : hi_hi) || e < (e < 32 ? lo_lo : lo_hi)) sv[e] = 0xff800000u;  // -inf
+              if (hidden(e)) sv[e] = 0xff800000u;  // -inf
           }
-          if (k == 0 && j == 0) {  // the first reference: the maximum of the first 64 scores
+          if (!kFixed && k == 0 && j == 0) {  // the first reference: the maximum of the first 64 scores
             float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
             for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
@@ -833,6 +899,18 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           uint32_t pk[32];
           float part;
           float top;
+          auto fixed_weights = [&] {
+            uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float w0 = ex2(__uint_as_float(sv[2 * e])), w1 = ex2(__uint_as_float(sv[2 * e + 1]));
+              sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
+              pk[e] = pack2<false>(w0, w1);
+            }
+            float s0, s1;
+            f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
+            part = s0 + s1;
+          };
           auto weights = [&](auto poly) {
             const float minus_ref = -__fmul_rn(m_ref, c_ref);
             const uint64_t ref2 = f32x2(__float_as_uint(minus_ref), __float_as_uint(minus_ref));
@@ -865,6 +943,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
 #pragma unroll
               for (int e = 0; e < 32; ++e) pk[e] = 0;
               part = 0.f;
+              break;
+            }
+            if constexpr (kFixed) {
+              fixed_weights();
               break;
             }
             weights(std::bool_constant<!kMasked>{});  // (weights of hidden keys are exactly zero)
@@ -958,7 +1040,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         some = see_lo < see_hi;
       }
       const bool partial = un.slot >= 0;
-      float inv = 1.f / (l < 5.4210109e-20f ? NAN : l);  // 2^-64
+      float inv = 1.f / (!kFixed && l < 5.4210109e-20f ? NAN : l);  // 2^-64
       float* part_o = nullptr;
       if (partial) {  // sums go to the workspace as they are, for the merge
         const int64_t at = static_cast<int64_t>(un.slot) * kPreRows + (2 * w + rank) * 128 + (tid & 127);
@@ -1025,7 +1107,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
 
 // Joins the parts of row blocks that were cut along the keys. A warp per row; a lane owns D / 32 columns.
 template <int D>
-__global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ PrefillPlan plan, float scale_log2) {
+__global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ PrefillPlan plan, float scale_log2, float least) {
   constexpr int kCols = D / 32;
   const uint8_t* ws = static_cast<const uint8_t*>(p.workspace);
   const PrefillRecord rec = reinterpret_cast<const PrefillRecord*>(ws + prefill_records_at(D))[blockIdx.x];
@@ -1066,7 +1148,7 @@ __global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constan
       }
     }
     const bool zero = bad || l == 0.f;
-    const float inv = 1.f / (l < 5.4210109e-20f ? NAN : l);
+    const float inv = 1.f / (l < least ? NAN : l);
     uint32_t packed[kCols / 2];
 #pragma unroll
     for (int i = 0; i < kCols; i += 2) packed[i / 2] = zero ? 0u : pack2<false>(acc[i] * inv, acc[i + 1] * inv);
