@@ -106,6 +106,7 @@ __device__ __forceinline__ void exp2_two(uint64_t x, float& w0, float& w1) {
   w0 = __uint_as_float(__float_as_uint(w0) + (__float_as_uint(t0) << 23));
   w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
 }
+__device__ __forceinline__ uint32_t bits_before(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -800,8 +801,9 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       // One tile; masked: some row of the warp does not see all of it.
       auto tile = [&](auto masked, int j) {
         constexpr bool kMasked = decltype(masked)::value;
-        // 64 keys at a time; the first run's products start while the second run is here
-#pragma unroll
+        // 64 keys at a time; the first run's products start while the second run is here. (Not unrolled: both runs' code, masked and
+        // not, was more than the instruction caches held: a third of all stalls were for instructions.)
+#pragma unroll 1
         for (int k = 0; k < 2; ++k) {
           if (kRuns || k == 0) {
             if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 16 * w + 8 * k, t & 1));
@@ -814,9 +816,13 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           tmem_wait_ld();
           // keys of the run's columns: 64 k + e, or 32 k + e, from the 32nd on 32 k + 32 + e
           const int first_lo = j * kGKeys + (kRuns ? 32 * k : 64 * k), first_hi = j * kGKeys + (kRuns ? 32 * k + 32 : 64 * k);
-          // (columns of the run that this row sees: from lo_lo and before hi_lo of the first 32, lo_hi and hi_hi of the others)
-          const int hi_lo = hi - first_lo, hi_hi = hi - first_hi, lo_lo = lo - first_lo, lo_hi = lo - first_hi;
-          auto hidden = [&](int e) { return e >= (e < 32 ? hi_lo : hi_hi) || e < (e < 32 ? lo_lo : lo_hi); };
+          // (columns of the run that this row sees, a bit each)
+          [[maybe_unused]] uint32_t seen[2];
+          if (kMasked) {
+            seen[0] = bits_before(hi - first_lo) & ~bits_before(lo - first_lo);
+            seen[1] = bits_before(hi - first_hi - 32) & ~bits_before(lo - first_hi - 32);
+          }
+          auto hidden = [&](int e) { return (seen[e >> 5] & (1u << (e & 31))) == 0u; };
           auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
           auto put = [&](int e, uint64_t z) {
             float z0, z1;
