@@ -118,7 +118,7 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
 // cancels in the quotient. c is the scale as long as |c r| < 2^28, where that is at most 2^8. Beyond, scores that differ at
 // all differ by 16 and more there, so that only the largest one weighs anything in 32 bits, and by any c that is large enough:
 // then c is a power of two with 2^31 <= |c r| < 2^32, c r is exact, and other scores are 2^7 and more away.
-// Shaped scores are in the exponent's units already: c is 1 (far ones again a power of two).
+// Biased scores are in the exponent's units already: c is 1 (far ones again a power of two).
 __device__ __forceinline__ float score_factor(float r, float scale_log2) {
   if (fabsf(r * scale_log2) < 268435456.f) return scale_log2;
   const uint32_t exponent = (__float_as_uint(r) >> 23) & 255u;
@@ -165,6 +165,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   using C = GCfg<D>;
   constexpr int kStages = C::kStages;
   constexpr bool kZ = kShape != kShapeNone;        // scores are shaped before the softmax
+  constexpr bool kCap = (kShape & kShapeCap) != 0, kBias = (kShape & kShapeBias) != 0;
   constexpr bool kFixed = kShape == kShapeCap;     // ... and lie within bounds: the reference is fixed
   constexpr uint32_t kRunP = kRuns ? 64 : 32;      // columns from the first run's weights to the second's
   extern __shared__ uint8_t smem_raw[];
@@ -762,12 +763,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         lo = from_key0(lo);
         hi = from_key0(min(hi, un.key_end));
         // (biased: keys behind the token itself go the way of masked tiles, which takes the distance's absolute value)
-        const int full_hi = (kShape & kShapeBias) && exists ? min(hi, from_key0(pos + 1)) : hi;
+        const int full_hi = kBias && exists ? min(hi, from_key0(pos + 1)) : hi;
         full_from = __reduce_max_sync(0xffffffffu, exists ? lo : -(1 << 30));
         full_to = __reduce_min_sync(0xffffffffu, exists ? full_hi : 1 << 30);
         if (!__any_sync(0xffffffffu, exists)) full_to = -(1 << 30);  // (a warp without any row sees nothing)
         m_ref = kFixed ? plan.ref : exists ? kGNoMax : INFINITY;
-        if constexpr ((kShape & kShapeBias) != 0) {
+        if constexpr (kBias) {
           slope = exists && p.score.slopes != nullptr ? p.score.slopes[un.head(w) * p.group + row_head] * kLog2e : 0.f;
           key0_pos = static_cast<int>(key0 - pos);
           // A bias has the scores rise from tile to tile, up to the token's own key: its score, which no distance lowers, is
@@ -779,7 +780,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               const uint4* key = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_cache) + page * p.geom.page_stride +
                                                                 un.head(w) * p.geom.head_stride + (pos % kPageSize) * p.geom.slot_stride);
               float dot = 0.f;
-#pragma unroll 4
+#pragma unroll 8
               for (int c = 0; c < D / 8; ++c) {
                 const uint4 a = q[c], b = key[c];
                 const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
@@ -790,7 +791,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 }
               }
               dot *= p.score.mul;
-              if constexpr ((kShape & kShapeCap) != 0) dot = fmaf(-2.f * p.score.cap, rcp_approx(ex2(dot) + 1.f), p.score.cap);
+              if constexpr (kCap) dot = fmaf(-2.f * p.score.cap, rcp_approx(ex2(dot) + 1.f), p.score.cap);
               if (fabsf(dot) < 3.0e38f) m_ref = dot;
             }
           }
@@ -824,158 +825,186 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           }
           auto hidden = [&](int e) { return (seen[e >> 5] & (1u << (e & 31))) == 0u; };
           auto both = [](float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); };
-          auto put = [&](int e, uint64_t z) {
-            float z0, z1;
-            f32x2_split(z, z0, z1);
-            sv[e] = __float_as_uint(z0);
-            sv[e + 1] = __float_as_uint(z1);
-          };
-          if constexpr ((kShape & kShapeCap) != 0) {
-            // The cap, minus the reference where that is fixed. The hyperbolic tangent goes by the row's largest product among the
-            // 64: small ones by a polynomial (|y| <= 1/2: degree 5; |y| <= 1: degree 9), of the form whose largest error is least
-            // (2^-17.5 and 2^-18.5, of 1), others, and infinities and NaN, by exponential and reciprocal: three
-            // results of the special-function unit a score with the weight's, which bound the kernel.
-            if (kMasked) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e) sv[e] = hidden(e) ? 0u : sv[e];
-            }
-            float mx[2] = {0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3_nan(mx[(e >> 1) & 1], fabsf(__uint_as_float(sv[e])), fabsf(__uint_as_float(sv[e + 1])));
-            const float far = max3_nan(mx[0], mx[1], mx[1]);
-            const float ref = kFixed ? plan.ref : 0.f;
-            const uint64_t minus_ref = both(-ref);
-            if (far <= plan.limit[0]) {
-#pragma unroll
-              for (int e = 0; e < 64; e += 2) {
-                const uint64_t x = f32x2(sv[e], sv[e + 1]), t2 = mul_f32x2(x, x);
-                uint64_t y = fma_f32x2(t2, plan.poly5[2], plan.poly5[1]);
-                y = fma_f32x2(t2, y, plan.poly5[0]);
-                put(e, kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y));
-              }
-            } else if (far <= plan.limit[1]) {
-#pragma unroll
-              for (int e = 0; e < 64; e += 2) {
-                const uint64_t x = f32x2(sv[e], sv[e + 1]), t2 = mul_f32x2(x, x);
-                uint64_t y = fma_f32x2(t2, plan.poly9[4], plan.poly9[3]);
-                y = fma_f32x2(t2, y, plan.poly9[2]);
-                y = fma_f32x2(t2, y, plan.poly9[1]);
-                y = fma_f32x2(t2, y, plan.poly9[0]);
-                put(e, kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y));
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 64; ++e)
-                sv[e] = __float_as_uint(fmaf(-2.f * p.score.cap, rcp_approx(ex2(__uint_as_float(sv[e]) * p.score.mul) + 1.f), p.score.cap - ref));
-            }
-          }
-          if constexpr ((kShape & kShapeBias) != 0) {
-            const uint64_t mul2 = both((kShape & kShapeCap) ? 1.f : p.score.mul), slope2 = both(slope);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {  // 16 keys
-              // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
-              const uint64_t base2 = both(slope * static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g));
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int e = 16 * g + 2 * i;
-                uint64_t bias2 = fma_f32x2(slope2, f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), base2);
-                if (kMasked) {  // -slope |distance|
-                  float b0, b1;
-                  f32x2_split(bias2, b0, b1);
-                  bias2 = f32x2(__float_as_uint(copysignf(b0, -slope)), __float_as_uint(copysignf(b1, -slope)));
-                }
-                put(e, fma_f32x2(f32x2(sv[e], sv[e + 1]), mul2, bias2));
-              }
-            }
-          }
-          if (kMasked) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e)
-              if (hidden(e)) sv[e] = 0xff800000u;  // -inf
-          }
-          if (!kFixed && k == 0 && j == 0) {  // the first reference: the maximum of the first 64 scores
-            float mx[2] = {neg_inf, neg_inf};
-#pragma unroll
-            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-            m_ref = fmaxf(m_ref, fmaxf(mx[0], mx[1]));
-            c_ref = score_factor(m_ref, scale_log2);
-          }
-          // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
-          // reference by so much that the reference is raised and the weights are taken again.
+          auto two = [&](int e) { return f32x2(sv[2 * e], sv[2 * e + 1]); };
           uint32_t pk[32];
-          float part;
-          float top;
-          auto fixed_weights = [&] {
-            uint64_t sum2[2] = {0ull, 0ull};
+          float part = 0.f;
+          if (kMasked && __all_sync(0xffffffffu, hi <= first_lo || lo >= first_hi + 64)) {  // no row of the warp sees any of these
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float w0 = ex2(__uint_as_float(sv[2 * e])), w1 = ex2(__uint_as_float(sv[2 * e + 1]));
-              sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
-              pk[e] = pack2<false>(w0, w1);
-            }
-            float s0, s1;
-            f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
-            part = s0 + s1;
-          };
-          auto weights = [&](auto poly) {
-            const float minus_ref = -__fmul_rn(m_ref, c_ref);
-            const uint64_t ref2 = f32x2(__float_as_uint(minus_ref), __float_as_uint(minus_ref));
-            const uint64_t c2 = f32x2(__float_as_uint(c_ref), __float_as_uint(c_ref));
-            uint64_t sum2[2] = {0ull, 0ull};
-            float mx[2] = {neg_inf, neg_inf};
+            for (int e = 0; e < 32; ++e) pk[e] = 0;
+          } else {
+            if constexpr (kCap) {
+              // The hyperbolic tangent of the cap goes by the row's largest product among the 64: small ones by a polynomial
+              // (|y| <= 1/2: degree 5; |y| <= 1: degree 9), of the form whose largest error is least (2^-17.5 and 2^-18.5, of
+              // 1), others, and infinities and NaN, by exponential and reciprocal: three results of the special-function unit a
+              // score with the weight's. Where the reference is fixed, the weights are taken right behind it.
+              if (kMasked) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const uint64_t x = fma_f32x2(f32x2(sv[2 * e], sv[2 * e + 1]), c2, ref2);
-              mx[e & 1] = max3_nan(mx[e & 1], __uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]));
-              float w0, w1;
-              if (decltype(poly)::value && e % kGPolyOf == kGPolyOf - 1) {
-                exp2_two(x, w0, w1);
-              } else {
-                f32x2_split(x, w0, w1);
-                w0 = ex2(w0);
-                w1 = ex2(w1);
+                for (int e = 0; e < 64; ++e) sv[e] = hidden(e) ? 0u : sv[e];
               }
-              sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
-              pk[e] = pack2<false>(w0, w1);
-            }
-            float s0, s1;
-            f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
-            part = s0 + s1;
-            top = max3_nan(mx[0], mx[0], mx[1]);
-            if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
-          };
-          while (true) {
-            if (kMasked && __all_sync(0xffffffffu, hi <= first_lo || lo >= first_hi + 64)) {  // no row of the warp sees any of these
+              float mx[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int e = 0; e < 32; ++e) pk[e] = 0;
-              part = 0.f;
-              break;
+              for (int e = 0; e < 32; ++e) mx[e & 3] = max3_nan(mx[e & 3], fabsf(__uint_as_float(sv[2 * e])), fabsf(__uint_as_float(sv[2 * e + 1])));
+              const float far = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]);
+              const uint64_t minus_ref = both(-plan.ref);
+              uint64_t sum2[2] = {0ull, 0ull};
+              auto capped = [&](auto shape) {  // (shape: of a pair of products)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  float z0, z1;
+                  f32x2_split(shape(two(e)), z0, z1);
+                  if constexpr (kFixed) {
+                    float w0 = ex2(z0), w1 = ex2(z1);
+                    if (kMasked) {
+                      w0 = hidden(2 * e) ? 0.f : w0;
+                      w1 = hidden(2 * e + 1) ? 0.f : w1;
+                    }
+                    sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
+                    pk[e] = pack2<false>(w0, w1);
+                  } else {
+                    sv[2 * e] = __float_as_uint(z0);
+                    sv[2 * e + 1] = __float_as_uint(z1);
+                  }
+                }
+              };
+              if (!kMasked && far <= plan.limit[0]) {
+                capped([&](uint64_t x) {
+                  const uint64_t t2 = mul_f32x2(x, x);
+                  const uint64_t y = fma_f32x2(t2, fma_f32x2(t2, plan.poly5[2], plan.poly5[1]), plan.poly5[0]);
+                  return kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y);
+                });
+              } else if (far <= plan.limit[1]) {
+                capped([&](uint64_t x) {
+                  const uint64_t t2 = mul_f32x2(x, x);
+                  uint64_t y = fma_f32x2(t2, plan.poly9[4], plan.poly9[3]);
+                  y = fma_f32x2(t2, y, plan.poly9[2]);
+                  y = fma_f32x2(t2, y, plan.poly9[1]);
+                  y = fma_f32x2(t2, y, plan.poly9[0]);
+                  return kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y);
+                });
+              } else {
+                capped([&](uint64_t x) {
+                  float y0, y1;
+                  f32x2_split(mul_f32x2(x, both(p.score.mul)), y0, y1);
+                  const uint64_t r = f32x2(__float_as_uint(rcp_approx(ex2(y0) + 1.f)), __float_as_uint(rcp_approx(ex2(y1) + 1.f)));
+                  return fma_f32x2(r, both(-2.f * p.score.cap), both(p.score.cap - plan.ref));
+                });
+              }
+              if constexpr (kFixed) {
+                float s0, s1;
+                f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
+                part = s0 + s1;
+              }
             }
-            if constexpr (kFixed) {
-              fixed_weights();
-              break;
+            // What the weights' exponents are made of: of scores that are not biased x = c s - c r; of biased ones
+            // x = mul s + (slope (j - p) - r), a constant for the first of 16 keys and slope times 0 .. 15 (keys behind the token
+            // itself, of a prefix: less twice the bias).
+            const auto exponent = [&](int e, float minus_ref) {
+              if constexpr (kBias) {
+                const int g = e >> 3, i = e & 7;
+                // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
+                const float base = fmaf(slope, static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g), minus_ref);
+                const uint64_t bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(base));
+                return kCap ? add_f32x2(two(e), bias2) : fma_f32x2(two(e), both(p.score.mul), bias2);
+              } else {
+                return fma_f32x2(two(e), both(c_ref), both(minus_ref));
+              }
+            };
+            if constexpr (kBias) {
+              if (kMasked && p.prefix_lens != nullptr) {
+                const int own_lo = -key0_pos - first_lo, own_hi = -key0_pos - first_hi;
+                const float twice = kCap ? -2.f * slope : p.score.mul != 0.f ? -2.f * slope / p.score.mul : 0.f;
+#pragma unroll
+                for (int e = 0; e < 64; ++e) {
+                  const int behind = e - (e < 32 ? own_lo : own_hi);
+                  if (behind > 0) sv[e] = __float_as_uint(fmaf(twice, static_cast<float>(behind), __uint_as_float(sv[e])));
+                }
+              }
             }
-            weights(std::bool_constant<!kMasked>{});  // (weights of hidden keys are exactly zero)
-            const bool raise = top * c_ref > m_ref * c_ref + kGRescale;
-            if (!__any_sync(0xffffffffu, raise)) break;
-            // (only the rows that ask for it: a row's rounding does not depend on its neighbours' scores)
-            const float m_new = raise ? top : m_ref, c_new = score_factor(m_new, scale_log2);
-            const float a = rescale(m_ref, m_new, c_new);
-            m_ref = m_new;
-            c_ref = c_new;
-            l *= a;
-            if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first run of this one
-              if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
-              if (!ok) break;
-              tc_fence_after();
+            if constexpr (!kFixed) {
+              if (kMasked && !kBias) {
+#pragma unroll
+                for (int e = 0; e < 64; ++e)
+                  if (hidden(e)) sv[e] = 0xff800000u;  // -inf
+              }
+              const auto visible_exponent = [&](int e, float minus_ref) {
+                uint64_t x = exponent(e, minus_ref);
+                if (kMasked && kBias) {
+                  float x0, x1;
+                  f32x2_split(x, x0, x1);
+                  x = f32x2(hidden(2 * e) ? 0xff800000u : __float_as_uint(x0), hidden(2 * e + 1) ? 0xff800000u : __float_as_uint(x1));
+                }
+                return x;
+              };
+              // The first reference, where there is none yet: the maximum of these 64 scores.
+              if (kBias ? __any_sync(0xffffffffu, m_ref == kGNoMax) : (k == 0 && j == 0)) {
+                float mx[2] = {neg_inf, neg_inf};
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  float z0, z1;
+                  f32x2_split(kBias ? visible_exponent(e, 0.f) : two(e), z0, z1);
+                  mx[e & 1] = max3(mx[e & 1], z0, z1);
+                }
+                const float first = fmaxf(mx[0], mx[1]);
+                if (kBias) m_ref = m_ref == kGNoMax && first > neg_inf ? first : m_ref;
+                else m_ref = fmaxf(m_ref, first);
+                if (!kBias) c_ref = score_factor(m_ref, scale_log2);
+              }
+              // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
+              // reference by so much that the reference is raised and the weights are taken again.
+              float top;  // of the scores; of biased ones, of the exponents
+              while (true) {
+                const float minus_ref = kBias ? -m_ref : -__fmul_rn(m_ref, c_ref);
+                uint64_t sum2[2] = {0ull, 0ull};
+                float mx[2] = {neg_inf, neg_inf};
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  const uint64_t x = visible_exponent(e, minus_ref);
+                  float w0, w1;
+                  f32x2_split(kBias ? x : two(e), w0, w1);
+                  mx[e & 1] = max3_nan(mx[e & 1], w0, w1);
+                  if (!kMasked && e % kGPolyOf == kGPolyOf - 1) {  // (weights of hidden keys are exactly zero, the polynomial's are not)
+                    exp2_two(x, w0, w1);
+                  } else {
+                    f32x2_split(x, w0, w1);
+                    w0 = ex2(w0);
+                    w1 = ex2(w1);
+                  }
+                  sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
+                  pk[e] = pack2<false>(w0, w1);
+                }
+                float s0, s1;
+                f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
+                part = s0 + s1;
+                top = max3_nan(mx[0], mx[0], mx[1]);
+                if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
+                const bool raise = kBias ? top > kGRescale : top * c_ref > m_ref * c_ref + kGRescale;
+                if (!__any_sync(0xffffffffu, raise)) break;
+                // (only the rows that ask for it: a row's rounding does not depend on its neighbours' scores)
+                const float m_new = !raise ? m_ref : kBias ? m_ref + top : top;
+                float a;
+                if (kBias) {
+                  a = raise ? ex2(m_ref - m_new) : 1.f;
+                } else {
+                  const float c_new = score_factor(m_new, scale_log2);
+                  a = rescale(m_ref, m_new, c_new);
+                  c_ref = c_new;
+                }
+                m_ref = m_new;
+                l *= a;
+                if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first run of this one
+                  if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
+                  if (!ok) break;
+                  tc_fence_after();
 #pragma unroll 1
-              for (int c = 0; c < D / 16; ++c) {
-                uint32_t ov[16];
-                tmem_ld16(my_o + 16 * c, ov);
-                tmem_wait_ld();
+                  for (int c = 0; c < D / 16; ++c) {
+                    uint32_t ov[16];
+                    tmem_ld16(my_o + 16 * c, ov);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
-                tmem_st16(my_o + 16 * c, ov);
+                    for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
+                    tmem_st16(my_o + 16 * c, ov);
+                  }
+                }
               }
             }
           }
