@@ -47,22 +47,45 @@ void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
   }
 }
 
-template <int D, int kShape>
-cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const PrefillPlan& plan, bool runs, int pairs, cudaStream_t stream) {
-  const auto kernel = runs ? prefill_tc_kernel<D, kShape, true> : prefill_tc_kernel<D, kShape, false>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GCfg<D>::kSmemBytes);
+template <int D, bool kFp8, int kShape>
+cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const PrefillPlan& plan, int pairs, cudaStream_t stream) {
+  using C = GCfg<D, kFp8>;
+  const auto kernel = prefill_tc_kernel<D, kShape, kFp8>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
   if (e != cudaSuccess) return e;
-  kernel<<<static_cast<unsigned>(2 * pairs), kGThreads, GCfg<D>::kSmemBytes, stream>>>(maps, p, plan);
+  kernel<<<static_cast<unsigned>(2 * pairs), C::kThreads, C::kSmemBytes, stream>>>(maps, p, plan);
   if ((e = cudaGetLastError()) != cudaSuccess || !plan.cut) return e;
   prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone ? plan.scale_log2 : 1.f,
                                                                                        kShape == kShapeCap ? 0.f : 5.4210109e-20f);
   return cudaGetLastError();
 }
 
+template <int D, bool kFp8>
+cudaError_t launch_shape(const PrefillParams& p, const PrefillMaps& maps, const PrefillPlan& plan, int shape, int pairs, cudaStream_t stream) {
+  if (shape == kShapeNone) return launch<D, kFp8, kShapeNone>(p, maps, plan, pairs, stream);
+  if (shape == kShapeCap) return launch<D, kFp8, kShapeCap>(p, maps, plan, pairs, stream);
+  if (shape == kShapeBias) return launch<D, kFp8, kShapeBias>(p, maps, plan, pairs, stream);
+  return launch<D, kFp8, kShapeCap | kShapeBias>(p, maps, plan, pairs, stream);
+}
+
+// e4m3 pages, dims (byte of the line, slot, line, head, page): rows of K whole (a line of 128 bytes), of V in two lines of 64, one
+// for each CTA of a pair; not swizzled, as they are read by threads that convert them.
+bool encode_bytes(CUtensorMap* map, const void* base, const CacheGeom& g, int line_bytes) {
+  EncodeFn enc = tensor_map_encoder();
+  if (!enc) return false;
+  const cuuint64_t line = static_cast<cuuint64_t>(line_bytes), lines = static_cast<cuuint64_t>(g.head_dim) / line;
+  const cuuint64_t dims[5] = {line, static_cast<cuuint64_t>(kPageSize), lines, static_cast<cuuint64_t>(g.num_kv_heads), static_cast<cuuint64_t>(g.num_pages)};
+  const cuuint64_t strides[4] = {static_cast<cuuint64_t>(g.slot_stride), line, static_cast<cuuint64_t>(g.head_stride), static_cast<cuuint64_t>(g.page_stride)};
+  const cuuint32_t box[5] = {static_cast<cuuint32_t>(line), kPageSize, 1, 1, 1};
+  const cuuint32_t step[5] = {1, 1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 bool prefill_tc_supports(const PrefillParams& p) {
-  if (p.geom.dtype != PDA_BF16 || (p.geom.head_dim != 64 && p.geom.head_dim != 128)) return false;
+  if (p.geom.head_dim != 128 && (p.geom.head_dim != 64 || p.geom.dtype != PDA_BF16)) return false;
   if (p.group > 128 || p.geom.num_pages < 1 || p.geom.num_pages == INT32_MAX) return false;
   const auto fits = [](int64_t stride, int64_t extent) { return extent == 1 || (stride > 0 && stride < (1ll << 38)); };
   if (!fits(p.q_token_stride, p.total_q) || !fits(p.q_head_stride, p.num_q_heads)) return false;
@@ -80,9 +103,12 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   const int tile_rows = 128 / p.group, block_rows = 4 * tile_rows, heads = p.geom.num_kv_heads;
   PrefillMaps maps{};
   const CacheGeom& g = p.geom;
-  if (!encode_q(&maps.q, p, tile_rows) ||
-      !make_cache_tensor_map(&maps.k, p.k_cache, g.page_stride, g.head_stride, g.slot_stride, g.num_pages, heads, g.head_dim, 2, 1) ||
-      !make_cache_tensor_map(&maps.v, p.v_cache, g.page_stride, g.head_stride, g.slot_stride, g.num_pages, heads, g.head_dim, 2, 1))
+  const bool fp8 = g.dtype == PDA_FP8_E4M3;
+  const auto encode_cache = [&](CUtensorMap* map, const void* base, int line_bytes) {
+    return fp8 ? encode_bytes(map, base, g, line_bytes)
+               : make_cache_tensor_map(map, base, g.page_stride, g.head_stride, g.slot_stride, g.num_pages, heads, g.head_dim, 2, 1);
+  };
+  if (!encode_q(&maps.q, p, tile_rows) || !encode_cache(&maps.k, p.k_cache, 128) || !encode_cache(&maps.v, p.v_cache, 64))
     return cudaErrorNotSupported;
   // One pair of CTAs per two SMs at most; the row blocks of all sequences are at most one a sequence and one for
   // every block_rows query tokens.
@@ -99,7 +125,6 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   // Blocks are cut along the keys where that gives each at least two pairs.
   const int cut = listed && p.workspace != nullptr && 2 * most * heads <= std::min(all_pairs, kPreMaxPairs) ? 1 : 0;
   if (cut) pairs = std::min(all_pairs, kPreMaxPairs);
-  const bool runs = true;
   // Scores that are only capped have a fixed reference, if the cap allows it; otherwise the bias's form takes them, with slopes of
   // 0, and so it does scores that are not shaped if their factor is not above 0 (they are scaled behind the maximum).
   const float cap = p.score.cap;
@@ -108,16 +133,9 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   PrefillPlan plan{q_blocks, tile_rows, listed, listed ? 0 : places, cut, p.score.mul};
   if (cap > 0.f) set_cap(p.score, shape, &plan);
   const int n = static_cast<int>(pairs);
-  if (g.head_dim == 128) {
-    if (shape == kShapeNone) return launch<128, kShapeNone>(p, maps, plan, runs, n, stream);
-    if (shape == kShapeCap) return launch<128, kShapeCap>(p, maps, plan, runs, n, stream);
-    if (shape == kShapeBias) return launch<128, kShapeBias>(p, maps, plan, runs, n, stream);
-    return launch<128, kShapeCap | kShapeBias>(p, maps, plan, runs, n, stream);
-  }
-  if (shape == kShapeNone) return launch<64, kShapeNone>(p, maps, plan, runs, n, stream);
-  if (shape == kShapeCap) return launch<64, kShapeCap>(p, maps, plan, runs, n, stream);
-  if (shape == kShapeBias) return launch<64, kShapeBias>(p, maps, plan, runs, n, stream);
-  return launch<64, kShapeCap | kShapeBias>(p, maps, plan, runs, n, stream);
+  if (fp8) return launch_shape<128, true>(p, maps, plan, shape, n, stream);
+  if (g.head_dim == 128) return launch_shape<128, false>(p, maps, plan, shape, n, stream);
+  return launch_shape<64, false>(p, maps, plan, shape, n, stream);
 }
 
 }  // namespace pda

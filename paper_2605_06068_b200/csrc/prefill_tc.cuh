@@ -52,10 +52,9 @@ namespace {
 
 constexpr int kGKeys = 128;  // keys per tile
 constexpr int kGQLine = 128 * 128, kGKLine = 64 * 128;
-constexpr int kGSoftWarps = 8, kGThreads = (kGSoftWarps + 4) * 32, kGProducer = 8, kGMma = 9, kGRelay = 11;
-constexpr int kGBookBytes = 5 * 1024;
-constexpr uint32_t kGRegsSoftmax = 200, kGRegsControl = 104;  // 384 threads start with 168 (64512 in all)
-static_assert(kGSoftWarps * 32 * kGRegsSoftmax + 128 * kGRegsControl <= kGThreads * 168, "registers");
+constexpr int kGSoftWarps = 8, kGProducer = 8, kGMma = 9, kGRelay = 11, kGConvert = 12;
+constexpr int kGScaleSlots = 8;  // tiles whose page scales are kept (e4m3): more than both rings hold together
+constexpr int kGBookBytes = 6 * 1024;
 constexpr uint32_t kGTmemCols = 512, kGTmemO = 256;
 constexpr int kGUnitSlots = 4;   // units the producer may be ahead
 constexpr int kGMaxList = 128;   // row blocks that are sorted by their work
@@ -73,16 +72,25 @@ constexpr float kGFixedTop = 60.f, kGFixedCap = 90.f;
 // How scores are shaped (bits): capped; biased by distance.
 enum : int { kShapeNone = 0, kShapeCap = 1, kShapeBias = 2 };
 
-template <int D>
+// e4m3 caches: tiles land in a ring of bytes and are converted to bf16 (exactly) by a warpgroup of their own; the page scales
+// go through the softmax.
+template <int D, bool kFp8>
 struct GCfg {
   static constexpr int kLines = D / 64;
-  static constexpr int kStages = D == 128 ? 4 : 6;
+  static constexpr int kStages = kFp8 ? 3 : D == 128 ? 4 : 6;
+  static constexpr int kRaw = kFp8 ? 3 : 0;         // tiles as bytes
+  static constexpr int kRawBytes = 64 * 128;        // K: 64 keys; V: 64 dims of 128 keys
+  static constexpr int kThreads = (kGSoftWarps + 4 + (kFp8 ? 4 : 0)) * 32;
+  // 384 threads start with 168 registers (64512 in all), 512 with 128 (65536)
+  static constexpr uint32_t kRegsSoftmax = kFp8 ? 184 : 200, kRegsControl = kFp8 ? 72 : 104;
+  static_assert(kGSoftWarps * 32 * kRegsSoftmax + (kThreads - kGSoftWarps * 32) * kRegsControl <= kThreads * (kFp8 ? 128 : 168), "registers");
   static constexpr int kKBytes = kLines * kGKLine;  // of its 64 keys
   static constexpr int kVBytes = kGKeys * 128;      // its line (64 dims) of all keys
   static constexpr int kQBytes = kLines * kGQLine;  // of a half
   static constexpr int kRing = 2 * kQBytes;
-  static constexpr int kBook = kRing + kStages * (kKBytes + kVBytes);
-  static constexpr int kBars = 9 * kStages + 36;
+  static constexpr int kRawAt = kRing + kStages * (kKBytes + kVBytes);
+  static constexpr int kBook = kRawAt + kRaw * 2 * kRawBytes;
+  static constexpr int kBars = 9 * kStages + 32 + 4 * kRaw + kGScaleSlots;
   static constexpr int kSmemBytes = kBook + kGBookBytes + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory");
 };
@@ -158,16 +166,15 @@ __device__ __forceinline__ void tma_load_page_pair_if(uint32_t leader, uint32_t 
       ::"r"(dst), "l"(map), "r"(bar), "r"(line), "r"(head), "r"(page), "r"(leader) : "memory");
 }
 
-template <int D, int kShape, bool kRuns>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGThreads, 1)
+template <int D, int kShape, bool kFp8>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GCfg<D, kFp8>::kThreads, 1)
 prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constant__ PrefillParams p,
                   const __grid_constant__ PrefillPlan plan) {
-  using C = GCfg<D>;
+  using C = GCfg<D, kFp8>;
   constexpr int kStages = C::kStages;
   constexpr bool kZ = kShape != kShapeNone;        // scores are shaped before the softmax
   constexpr bool kCap = (kShape & kShapeCap) != 0, kBias = (kShape & kShapeBias) != 0;
   constexpr bool kFixed = kShape == kShapeCap;     // ... and lie within bounds: the reference is fixed
-  constexpr uint32_t kRunP = kRuns ? 64 : 32;      // columns from the first run's weights to the second's
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBook);
@@ -179,8 +186,9 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   uint32_t* target_sh = reinterpret_cast<uint32_t*>(cta_err + 1);   // tiles of a part
   float* merge_sh = reinterpret_cast<float*>(target_sh + 1);        // [128][2]
+  float* scales_sh = merge_sh + 256;                                // (e4m3) [kGScaleSlots][8 pages][K, V]
   int4* spans = reinterpret_cast<int4*>(reinterpret_cast<uint8_t*>(bars) + kGBookBytes - kGMaxList * 16);  // listed sequences' q0, nq, L
-  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + 8 * 4 + 1024 + kGMaxList * 16 <= kGBookBytes, "shared memory");
+  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + 8 * 4 + 1024 + (kFp8 ? kGScaleSlots * 64 : 0) + kGMaxList * 16 <= kGBookBytes, "shared memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1;  // in the pair
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
@@ -190,19 +198,21 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
 
   const uint32_t q_sm = smem_u32(smem), k_sm = q_sm + C::kRing, v_sm = k_sm + kStages * C::kKBytes;
   // Barriers, at the same place in both CTAs. Of the pair's first CTA: full_k (both CTAs' copies), v_ready, bar_q,
-  // bar_p, bar_turn, bar_ofree. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s,
+  // bar_p, bar_ofree. In each: empty_k, empty_v (both halves' products), full_v (its own copy), bar_s,
   // bar_pv, bar_qfree, the unit slots'. bar_s, bar_p and bar_pv: [half w][run of
-  // 64 keys] (bar_s with S at once: the first only).
+  // 64 keys].
   const uint32_t full_k = smem_u32(bars), empty_k = full_k + 24 * kStages, full_v = empty_k + 8 * kStages,
                  empty_v = full_v + 8 * kStages, v_ready = empty_v + 8 * kStages, bar_q = v_ready + 24 * kStages;
-  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 32, bar_pv = bar_p + 32, bar_turn = bar_pv + 32, bar_qfree = bar_turn + 16,
+  const uint32_t bar_s = bar_q + 16, bar_p = bar_s + 32, bar_pv = bar_p + 32, bar_qfree = bar_pv + 32,
                  bar_ofree = bar_qfree + 16, unit_full = bar_ofree + 16, unit_empty = unit_full + 8 * kGUnitSlots,
-                 bar_drain = unit_empty + 8 * kGUnitSlots, bar_never = bar_drain + 8, bar_merge = bar_never + 8;
+                 bar_drain = unit_empty + 8 * kGUnitSlots, bar_never = bar_drain + 8, bar_merge = bar_never + 8,
+                 raw_full = bar_merge + 32, raw_empty = raw_full + 16 * C::kRaw, scale_full = raw_empty + 16 * C::kRaw;
+  // (e4m3: raw_full and raw_empty [K, V][raw stage], scale_full [scale slot])
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
       for (int set = 0; set < 3; ++set) {
-        mbar_init(full_k + 8 * (kStages * set + i), 1);
-        mbar_init(v_ready + 8 * (kStages * set + i), 2);
+        mbar_init(full_k + 8 * (kStages * set + i), kFp8 ? 8 : 1);  // (e4m3: four converting warps of each CTA)
+        mbar_init(v_ready + 8 * (kStages * set + i), kFp8 ? 8 : 2);
       }
       mbar_init(empty_k + 8 * i, 2);
       mbar_init(full_v + 8 * i, 1);
@@ -215,14 +225,18 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         mbar_init(bar_p + 16 * w + 8 * k, 8);  // four warps of each CTA
         mbar_init(bar_pv + 16 * w + 8 * k, 1);
       }
-      mbar_init(bar_turn + 8 * w, 1);
       mbar_init(bar_qfree + 8 * w, 1);
       mbar_init(bar_ofree + 8 * w, 8);
     }
     for (int i = 0; i < kGUnitSlots; ++i) {
       mbar_init(unit_full + 8 * i, 1);
-      mbar_init(unit_empty + 8 * i, kGSoftWarps + 1 + (rank == 0 ? 2 : 0));  // softmax, relay, product warps
+      mbar_init(unit_empty + 8 * i, kGSoftWarps + (kFp8 ? 4 : 1) + (rank == 0 ? 2 : 0));  // softmax, relay or converting, product warps
     }
+    for (int i = 0; i < 2 * C::kRaw; ++i) {
+      mbar_init(raw_full + 8 * i, 1);
+      mbar_init(raw_empty + 8 * i, 4);
+    }
+    for (int i = 0; kFp8 && i < kGScaleSlots; ++i) mbar_init(scale_full + 8 * i, 1);
     mbar_init(bar_drain, 2);
     mbar_init(bar_never, 1);
     for (int i = 0; i < 4; ++i) mbar_init(bar_merge + 8 * i, 1);
@@ -360,12 +374,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   auto tile_bar = [&](uint32_t first, int set, int count) { return first + 8 * (kStages * set + count % kStages); };
 
   // ================= products of half w =================
-  // A warp for each half, which prepares its next products while the other's are being issued. Where S is taken at once, they
-  // take turns, so that the halves stay in opposite phase.
+  // A warp for each half, which prepares its next products while the other's are being issued. S comes in two runs of 64 keys
+  // (32 of either CTA's), each taken again as soon as its own P . V is through, so that a half has scores of the next tile before
+  // its softmax is done with this one. (S of 128 keys at once, the halves taking turns: 498 us instead of 454 for 8192 tokens.)
   auto issue_role = [&](auto half) {
     constexpr int w = decltype(half)::value;
-    constexpr uint32_t idesc_s = latent_idesc(256, kGKeys, false, false), idesc_run = latent_idesc(256, kGKeys / 2, false, false),
-                       idesc_o = latent_idesc(256, 128, false, true);
+    constexpr uint32_t idesc_s = latent_idesc(256, kGKeys / 2, false, false), idesc_o = latent_idesc(256, 128, false, true);
     const uint32_t leader = elect_one();
     const uint32_t u_q = uniform(q_sm + w * C::kQBytes), u_k = uniform(k_sm), u_v = uniform(v_sm), u_tmem = uniform(tmem);
     const uint32_t u_ek = uniform(empty_k), u_ev = uniform(empty_v);
@@ -373,19 +387,19 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     auto wait = [&](uint32_t bar, int phase) {
       if (ok) ok = __all_sync(0xffffffffu, mbar_spin_cluster(bar, phase & 1));
     };
-    // S of a tile at once, or of run k of two: of each CTA's 64 keys those from 32 k on
-    auto s_product = [&](uint32_t k_addr, int k, uint32_t idesc) {
+    // S of run k of a tile: of each CTA's 64 keys those from 32 k on
+    auto s_product = [&](uint32_t k_addr, int k) {
       const uint64_t q0 = tc_desc(u_q, 16, 1024), k0 = tc_desc(k_addr, 16, 1024) + 256 * k;
 #pragma unroll
       for (int ln = 0; ln < C::kLines; ++ln)
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
-          mma2_ss_if(leader, d_s + 64 * k, q0 + ln * (kGQLine / 16) + 2 * ks, k0 + ln * (kGKLine / 16) + 2 * ks, idesc, (ln > 0 || ks > 0) ? 1u : 0u);
+          mma2_ss_if(leader, d_s + 64 * k, q0 + ln * (kGQLine / 16) + 2 * ks, k0 + ln * (kGKLine / 16) + 2 * ks, idesc_s, (ln > 0 || ks > 0) ? 1u : 0u);
       commit2_if(leader, bar_s + 16 * w + 8 * k);
     };
     GUnit un;
-    // Before this unit: tiles of the pair; of this half; units of this half; tiles on which the halves take turns.
-    int t0 = 0, mine = 0, done = 0, turns = 0;
+    // Before this unit: tiles of the pair; of this half; units of this half.
+    int t0 = 0, mine = 0, done = 0;
     int counts[2] = {0, 0};  // tiles of blocks of two halves; of dual ones, this half's
     for (int k = 0; next_unit(k, un); ++k) {
       free_unit(k);
@@ -412,8 +426,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         if (!ok) break;
         tc_fence_after();
         const uint32_t k_addr = uniform(u_k + sk * C::kKBytes);
-        s_product(k_addr, 0, kRuns ? idesc_run : idesc_s);
-        if constexpr (kRuns) s_product(k_addr, 1, idesc_run);
+        s_product(k_addr, 0);
+        s_product(k_addr, 1);
         if (n == 1) commit2_if(leader, bar_qfree + 8 * w);
         give_back(uniform(u_ek + 8 * sk));
       }
@@ -424,36 +438,26 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         const uint32_t k_addr = uniform(u_k + sk * C::kKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
         const uint32_t acc = uniform(j > 0 ? 1u : 0u);
         if (j == 0 && done > 0) wait(bar_ofree + 8 * w, done - 1);  // the last unit's output has been read
-        // turn i: half 0 after half 1's turn i - 1, half 1 after half 0's turn i
-        const bool taking_turns = !kRuns && j < n_other;
-        const int turn = turns + j;
-        const uint32_t turn_bar = taking_turns && (w == 1 || turn > 0) ? bar_turn + 8 * w : 0u;
-        const int turn_phase = w == 1 ? turn : turn - 1;
-        // (a run's keys: 64 k .. 64 k + 63 of the tile; in two runs 32 k .. 32 k + 31 and the same from 64 on)
-        const uint64_t v_lo = v0 + (kRuns ? 256u : 512u), v_hi = v0 + (kRuns ? 256u : 0u);
+        // (run 0: keys 0 .. 31 and 64 .. 95 of the tile; run 1: 32 .. 63 and 96 .. 127)
         wait(bar_p + 16 * w, mine + j);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, (ks < 2 ? v0 : v_hi) + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 8 * ks, v0 + (ks < 2 ? 0 : 256) + 128 * ks, idesc_o, ks > 0 ? 1u : acc);
         commit2_if(leader, bar_pv + 16 * w);
         if (j + 1 < n) wait(tile_bar(full_k, set, c0 + j + 1), (c0 + j + 1) / kStages);
-        if (kRuns && j + 1 < n) {
+        if (j + 1 < n) {
           if (!ok) break;
           tc_fence_after();
-          s_product(k_addr, 0, idesc_run);  // over these weights: the tensor core works a thread's products off in order
+          s_product(k_addr, 0);  // over these weights: the tensor core works a thread's products off in order
         }
-        {  // the other weights and the turn, looked for at once by different lanes
-          const bool second = (lane & 1) && turn_bar != 0u;
-          wait(second ? turn_bar : bar_p + 16 * w + 8, second ? turn_phase : mine + j);
-        }
+        wait(bar_p + 16 * w + 8, mine + j);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + kRunP + 8 * ks, (ks < 2 ? v_lo : v_lo + v_hi - v0) + 128 * ks, idesc_o, 1u);
+        for (int ks = 0; ks < 4; ++ks) mma2_ts_if(leader, d_o, d_s + 64 + 8 * ks, v0 + (ks < 2 ? 256 : 512) + 128 * ks, idesc_o, 1u);
         commit2_if(leader, bar_pv + 16 * w + 8);
-        if (j + 1 < n) s_product(k_addr, kRuns ? 1 : 0, kRuns ? idesc_run : idesc_s);
-        if (taking_turns && lane == 0) mbar_arrive_tc(bar_turn + 8 * (1 - w));
+        if (j + 1 < n) s_product(k_addr, 1);
         if (j + 2 == n) commit2_if(leader, bar_qfree + 8 * w);
         give_back(ev);
         if (j + 1 < n) give_back(ek);
@@ -466,7 +470,6 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       if (!ok) break;
       t0 += dual ? n + n_other : max(n, n_other);
       if (dual) counts[1] += n; else counts[0] += max(n, n_other);
-      if (!kRuns) turns += min(n, n_other);
       mine += n;
       if (n > 0) ++done;
     }
@@ -479,7 +482,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   };
 
   if (warp >= kGSoftWarps) {
-    reg_alloc_dec<kGRegsControl>();
+    reg_alloc_dec<C::kRegsControl>();
     if (warp == kGProducer) {
       // ================= units, and TMA: this CTA's rows of Q, pages of K, dims of V =================
       const uint32_t leader = elect_one(), first = leader & (rank == 0 ? 1u : 0u);  // (the first CTA expects both CTAs' bytes)
@@ -610,14 +613,24 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         // are others. Pages that no row sees are not looked at and read as zeros, like a page number beyond the cache.
         const int32_t* table = p.block_table + static_cast<int64_t>(b_now) * p.block_table_stride;
         const int tile0 = un.tile0;
-        auto load_pages = [&](int first_tile) {
+        struct Pages {
+          int id;
+          float ks, vs;  // (e4m3) the page's scales
+        };
+        auto load_pages = [&](int first_tile, int head) {
           const int64_t page = (static_cast<int64_t>(tile0) + first_tile) * 8 + lane;
-          int id = p.geom.num_pages;
+          Pages r{p.geom.num_pages, 0.f, 0.f};
           bool bad = false;
           if (page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now) {
             const int v = table[page];
             bad = v < 0 || v >= p.geom.num_pages;
-            if (!bad) id = v;
+            if (!bad) {
+              r.id = v;
+              if constexpr (kFp8) {
+                r.ks = p.k_scale[static_cast<int64_t>(v) * heads + head];
+                r.vs = p.v_scale[static_cast<int64_t>(v) * heads + head];
+              }
+            }
           }
           if (bad) {
             reinterpret_cast<volatile GUnit*>(units)[slot].bad = 1;
@@ -625,11 +638,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
             report(p.status, PDA_DEV_BAD_PAGE);
           }
           __syncwarp();
-          return id;
+          return r;
         };
-        const bool two_streams = un.dual == kSplitKeys;
-        int pages0 = load_pages(0), next0 = un.tiles() > 4 ? load_pages(4) : 0;
-        int pages1 = two_streams ? load_pages(un.n0) : 0, next1 = two_streams && un.n1 > 4 ? load_pages(un.n0 + 4) : 0;
+        // (of the second half where it has tiles of its own: other keys, or the same of the next head)
+        const int from1 = un.dual == kSplitKeys ? un.n0 : 0, head1 = un.head(1);
+        Pages now0 = load_pages(0, un.h), next0 = un.tiles() > 4 ? load_pages(4, un.h) : now0;
+        Pages now1 = un.dual ? load_pages(from1, head1) : now0, next1 = un.dual && un.n1 > 4 ? load_pages(from1 + 4, head1) : now0;
         const int n_all = un.tiles();
         auto load_q = [&](int w) {
           if (ok && done[w] > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_qfree + 8 * w, (done[w] - 1) & 1));
@@ -647,17 +661,40 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           const int st = uniform(t % kStages), rnd = t / kStages;
           // this tile's pages in lanes 8 j .. 8 j + 7 of `ids`
           const int j = un.dual ? i >> 1 : i;
-          const bool other = two_streams && (i & 1);
-          if ((j & 3) == 0 && j > 0 && !(un.dual == kTwoHeads && (i & 1))) {
+          const bool other = un.dual && (i & 1);
+          if ((j & 3) == 0 && j > 0) {
             if (other) {
-              pages1 = next1;
-              if (j + 4 < un.n1) next1 = load_pages(un.n0 + j + 4);
+              now1 = next1;
+              if (j + 4 < un.n1) next1 = load_pages(from1 + j + 4, head1);
             } else {
-              pages0 = next0;
-              if (j + 4 < (un.dual ? un.n0 : n_all)) next0 = load_pages(j + 4);
+              now0 = next0;
+              if (j + 4 < (un.dual ? un.n0 : n_all)) next0 = load_pages(j + 4, un.h);
             }
           }
-          const int ids = other ? pages1 : pages0;
+          const int ids = other ? now1.id : now0.id;
+          if constexpr (kFp8) {
+            const int rs = uniform(t % C::kRaw), used = t / C::kRaw;
+            if (used > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(raw_empty + 8 * rs, (used - 1) & 1));
+            if (!ok) break;
+            // (the scales' place is free: the tile that had it is kGScaleSlots back, more than the tiles in both rings)
+            if ((lane >> 3) == (j & 3))
+              reinterpret_cast<float2*>(scales_sh)[(t % kGScaleSlots) * 8 + (lane & 7)] = other ? make_float2(now1.ks, now1.vs) : make_float2(now0.ks, now0.vs);
+            __syncwarp();
+            if (lane == 0) mbar_arrive_tc(scale_full + 8 * (t % kGScaleSlots));
+            const uint32_t kd = uniform(smem_u32(smem) + C::kRawAt + rs * 2 * C::kRawBytes), vd = kd + C::kRawBytes;
+            mbar_expect_tx_if(leader, raw_full + 8 * rs, C::kRawBytes);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              tma_load_5d_if(leader, kd + g * 2048, &maps.k, raw_full + 8 * rs, 0, u_h, __shfl_sync(0xffffffffu, ids, (j & 3) * 8 + 4 * rank + g));
+            if (i == 0 && un.n1 > 0) load_q(1);
+            if (ok && used > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(raw_empty + 8 * (C::kRaw + rs), (used - 1) & 1));
+            if (!ok) break;
+            mbar_expect_tx_if(leader, raw_full + 8 * (C::kRaw + rs), C::kRawBytes);
+#pragma unroll
+            for (int g = 0; g < 8; ++g)  // (of V the line is the CTA's 64 dims)
+              tma_load_5d_if(leader, vd + g * 1024, &maps.v, raw_full + 8 * (C::kRaw + rs), rank, u_h, __shfl_sync(0xffffffffu, ids, (j & 3) * 8 + g));
+            continue;
+          }
           if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_k + 8 * st, (rnd - 1) & 1));
           if (!ok) break;
           const int set = un.dual ? 1 + (i & 1) : 0;
@@ -689,7 +726,73 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         if (lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
         for (int k = 0; k < 256; ++k) mbar_wait_bounded(bar_never, 0, 1);  // (4 us a poll)
       }
-    } else if (warp == kGRelay) {
+    } else if (kFp8 && warp >= kGConvert) {
+      // ================= e4m3 tiles to bf16, in the layout of the copies of bf16 tiles =================
+      // A thread takes 16 bytes of a row at a time and stores two 16-byte chunks. V rows behind the sequence's end are zero.
+      const int me = tid - kGConvert * 32;
+      auto convert = [&](uint32_t src, uint32_t dst0, uint32_t dst1, bool zero) {
+        uint32_t r[4], o[8];
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(src));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint32_t h[2];
+          e4m3x4_to_f16x2x2(r[e], h[0], h[1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+            o[2 * e + i] = zero ? 0u : pack2<false>(f.x, f.y);
+          }
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+      };
+      auto swizzled = [](uint32_t line, int row, int chunk) { return line + row * 128 + ((chunk ^ (row & 7)) << 4); };
+      int counts[3] = {0, 0, 0};  // tiles so far by set of barriers
+      GUnit un;
+      int t = 0;
+      for (int k = 0; next_unit(k, un); ++k) {
+        free_unit(k);
+        const int n_all = un.tiles();
+        for (int i = 0; ok && i < n_all; ++i, ++t) {
+          const int st = t % kStages, rnd = t / kStages, rs = t % (kFp8 ? C::kRaw : 1), used = t / (kFp8 ? C::kRaw : 1);
+          const int set = un.dual ? 1 + (i & 1) : 0;
+          const int count = set == 0 ? counts[0] : set == 1 ? counts[1] : counts[2];
+          if (set == 0) ++counts[0]; else if (set == 1) ++counts[1]; else ++counts[2];
+          const int64_t valid = un.L - (static_cast<int64_t>(un.tile0) + un.keys_of(i)) * kGKeys;
+          const uint32_t raw = smem_u32(smem) + C::kRawAt + rs * 2 * C::kRawBytes;
+#pragma unroll 1
+          for (int v = 0; v < 2; ++v) {  // K, then V
+            if (rnd > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded((v ? empty_v : empty_k) + 8 * st, (rnd - 1) & 1));
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(raw_full + 8 * (v * C::kRaw + rs), used & 1));
+            if (!ok) break;
+            if (v == 0) {
+              const uint32_t to = k_sm + st * C::kKBytes;
+#pragma unroll
+              for (int x = me; x < 512; x += 128) {
+                const int row = x >> 3, c = x & 7;
+                convert(raw + x * 16, swizzled(to + (c >> 2) * kGKLine, row, 2 * (c & 3)), swizzled(to + (c >> 2) * kGKLine, row, 2 * (c & 3) + 1), false);
+              }
+            } else {
+              const uint32_t to = v_sm + st * C::kVBytes;
+#pragma unroll
+              for (int x = me; x < 512; x += 128) {
+                const int row = x >> 2, c = x & 3;
+                convert(raw + C::kRawBytes + x * 16, swizzled(to, row, 2 * c), swizzled(to, row, 2 * c + 1), row >= valid);
+              }
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              arrive_cluster(in_cta(tile_bar(v ? v_ready : full_k, set, count), 0));
+              mbar_arrive_tc(raw_empty + 8 * (v * C::kRaw + rs));
+            }
+            __syncwarp();
+          }
+        }
+        if (!ok) break;
+      }
+      if (!ok && lane == 0) atomicMax(cta_err, PDA_DEV_TIMEOUT);
+    } else if (!kFp8 && warp == kGRelay) {
       // ================= V tiles: cleared behind the sequence's end, then handed to the first CTA =================
       int counts[3] = {0, 0, 0};  // tiles so far by set of barriers
       GUnit un;
@@ -730,7 +833,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       for (int b = lane; b < p.batch; b += 32) seq_span(p, b);  // (reports sequences that no place leads to)
     }
   } else {
-    reg_alloc_inc<kGRegsSoftmax>();
+    reg_alloc_inc<C::kRegsSoftmax>();
     // ================= softmax and output: thread = row =================
     const int w = warp >> 2;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -742,7 +845,9 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     const int row_token = (tid & 127) / p.group, row_head = (tid & 127) % p.group;
     const bool row_used = row_token < plan.tile_rows;  // (a group that does not divide 128 leaves rows over)
     int t = 0, merges = 0;  // tiles of this half, merges with the second half so far
+    int pair_t = 0;         // (e4m3) tiles of the pair before this unit
     for (int unit = 0;; ++unit) {
+      int step, own;  // (e4m3) the pair's tiles of this half: pair_t + step j + own
       int n, lo, hi;  // tiles; keys that this thread's row sees, from the half's first tile on
       int full_from, full_to;  // keys that all of the warp's rows see
       // The row's reference and the factor that goes with it. A row that does not exist is another sequence's, or anything:
@@ -754,6 +859,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         GUnit un;
         if (!next_unit(unit, un)) break;
         n = w == 0 ? un.n0 : un.n1;
+        step = un.dual ? 2 : 1;
+        own = un.dual ? w : 0;
         const int row = un.first_row(w, half_rows) + plan.tile_rows * rank + row_token, pos = un.L - un.nq + row;
         const bool exists = row_used && row < un.nq;
         lo = hi = 0;
@@ -777,17 +884,32 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
             const int page = p.block_table[static_cast<int64_t>(un.b) * p.block_table_stride + pos / kPageSize];
             if (page >= 0 && page < p.geom.num_pages) {
               const uint4* q = reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(un.q0) + row) * p.q_token_stride + (un.head(w) * p.group + row_head) * p.q_head_stride);
-              const uint4* key = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_cache) + page * p.geom.page_stride +
-                                                                un.head(w) * p.geom.head_stride + (pos % kPageSize) * p.geom.slot_stride);
+              const int64_t key_at = page * p.geom.page_stride + un.head(w) * p.geom.head_stride + (pos % kPageSize) * p.geom.slot_stride;
               float dot = 0.f;
+              auto add = [&](uint32_t a, float b0, float b1) {
+                dot = fmaf(__uint_as_float(a << 16), b0, dot);
+                dot = fmaf(__uint_as_float(a & 0xffff0000u), b1, dot);
+              };
+              if constexpr (kFp8) {
+                const uint2* key = reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.k_cache) + key_at);
 #pragma unroll 8
-              for (int c = 0; c < D / 8; ++c) {
-                const uint4 a = q[c], b = key[c];
-                const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+                for (int c = 0; c < D / 8; ++c) {
+                  const uint4 a = q[c];
+                  const uint2 b = key[c];
+                  const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[2] = {b.x, b.y};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  dot = fmaf(__uint_as_float(aw[e] << 16), __uint_as_float(bw[e] << 16), dot);
-                  dot = fmaf(__uint_as_float(aw[e] & 0xffff0000u), __uint_as_float(bw[e] & 0xffff0000u), dot);
+                  for (int e = 0; e < 4; ++e)
+                    add(aw[e], e4m3_to_float(static_cast<uint8_t>(bw[e >> 1] >> (16 * (e & 1)))), e4m3_to_float(static_cast<uint8_t>(bw[e >> 1] >> (16 * (e & 1) + 8))));
+                }
+                dot *= p.k_scale[static_cast<int64_t>(page) * heads + un.head(w)];
+              } else {
+                const uint4* key = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_cache) + key_at);
+#pragma unroll 8
+                for (int c = 0; c < D / 8; ++c) {
+                  const uint4 a = q[c], b = key[c];
+                  const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) add(aw[e], __uint_as_float(bw[e] << 16), __uint_as_float(bw[e] & 0xffff0000u));
                 }
               }
               dot *= p.score.mul;
@@ -806,17 +928,15 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         // not, was more than the instruction caches held: a third of all stalls were for instructions.)
 #pragma unroll 1
         for (int k = 0; k < 2; ++k) {
-          if (kRuns || k == 0) {
-            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 16 * w + 8 * k, t & 1));
-            if (!ok) return;
-            tc_fence_after();
-          }
+          if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_s + 16 * w + 8 * k, t & 1));
+          if (!ok) return;
+          tc_fence_after();
           uint32_t sv[64];
           tmem_ld32(my_s + 64 * k, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
           tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
           tmem_wait_ld();
-          // keys of the run's columns: 64 k + e, or 32 k + e, from the 32nd on 32 k + 32 + e
-          const int first_lo = j * kGKeys + (kRuns ? 32 * k : 64 * k), first_hi = j * kGKeys + (kRuns ? 32 * k + 32 : 64 * k);
+          // keys of the run's columns: 32 k + e, from the 32nd on 32 k + 32 + e
+          const int first_lo = j * kGKeys + 32 * k, first_hi = first_lo + 32;
           // (columns of the run that this row sees, a bit each)
           [[maybe_unused]] uint32_t seen[2];
           if (kMasked) {
@@ -828,6 +948,26 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           auto two = [&](int e) { return f32x2(sv[2 * e], sv[2 * e + 1]); };
           uint32_t pk[32];
           float part = 0.f;
+          [[maybe_unused]] const float2* scales = nullptr;  // of the run's four pages
+          if constexpr (kFp8) {
+            const int pt = pair_t + step * j + own;
+            if (k == 0) {
+              if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(scale_full + 8 * (pt % kGScaleSlots), (pt / kGScaleSlots) & 1));
+              if (!ok) return;
+            }
+            scales = reinterpret_cast<const float2*>(scales_sh) + (pt % kGScaleSlots) * 8 + 2 * k;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float s0, s1;
+              f32x2_split(mul_f32x2(two(e), both(scales[(e >> 4) * 4 + ((e >> 3) & 1)].x)), s0, s1);
+              sv[2 * e] = __float_as_uint(s0);
+              sv[2 * e + 1] = __float_as_uint(s1);
+            }
+          }
+          auto pack = [&](int e, float w0, float w1) {  // (values' page scales go with the weights)
+            if constexpr (kFp8) f32x2_split(mul_f32x2(f32x2(__float_as_uint(w0), __float_as_uint(w1)), both(scales[(e >> 4) * 4 + ((e >> 3) & 1)].y)), w0, w1);
+            return pack2<false>(w0, w1);
+          };
           if (kMasked && __all_sync(0xffffffffu, hi <= first_lo || lo >= first_hi + 64)) {  // no row of the warp sees any of these
 #pragma unroll
             for (int e = 0; e < 32; ++e) pk[e] = 0;
@@ -846,7 +986,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               for (int e = 0; e < 32; ++e) mx[e & 3] = max3_nan(mx[e & 3], fabsf(__uint_as_float(sv[2 * e])), fabsf(__uint_as_float(sv[2 * e + 1])));
               const float far = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]);
               const uint64_t minus_ref = both(-plan.ref);
-              uint64_t sum2[2] = {0ull, 0ull};
+              [[maybe_unused]] uint64_t sum2[2] = {0ull, 0ull};
               auto capped = [&](auto shape) {  // (shape: of a pair of products)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
@@ -859,7 +999,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                       w1 = hidden(2 * e + 1) ? 0.f : w1;
                     }
                     sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
-                    pk[e] = pack2<false>(w0, w1);
+                    pk[e] = pack(e, w0, w1);
                   } else {
                     sv[2 * e] = __float_as_uint(z0);
                     sv[2 * e + 1] = __float_as_uint(z1);
@@ -970,7 +1110,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                     w1 = ex2(w1);
                   }
                   sum2[e & 1] = add_f32x2(sum2[e & 1], f32x2(__float_as_uint(w0), __float_as_uint(w1)));
-                  pk[e] = pack2<false>(w0, w1);
+                  pk[e] = pack(e, w0, w1);
                 }
                 float s0, s1;
                 f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
@@ -1010,7 +1150,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           }
           if (!ok) return;
           l += part;
-          tmem_st32(my_s + kRunP * k, pk);
+          tmem_st32(my_s + 64 * k, pk);
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -1022,6 +1162,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         else tile(std::true_type{}, j);
       }
       // ---- output
+      if constexpr (kFp8) pair_t += units[unit % kGUnitSlots].tiles();
       if (n > 0) {
         if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8, (t - 1) & 1));
         tc_fence_after();
