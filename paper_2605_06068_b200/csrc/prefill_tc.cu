@@ -68,12 +68,12 @@ cudaError_t launch_shape(const PrefillParams& p, const PrefillMaps& maps, const 
   return launch<D, kFp8, kShapeCap | kShapeBias>(p, maps, plan, pairs, stream);
 }
 
-// e4m3 pages, dims (byte of the line, slot, line, head, page): rows of K whole (a line of 128 bytes), of V in two lines of 64, one
-// for each CTA of a pair; not swizzled, as they are read by threads that convert them.
-bool encode_bytes(CUtensorMap* map, const void* base, const CacheGeom& g, int line_bytes) {
+// e4m3 pages, dims (byte of the line, slot, line, head, page), in lines of 64 bytes: not swizzled, as threads read them that convert
+// them to lines of 64 bf16.
+bool encode_bytes(CUtensorMap* map, const void* base, const CacheGeom& g) {
   EncodeFn enc = tensor_map_encoder();
   if (!enc) return false;
-  const cuuint64_t line = static_cast<cuuint64_t>(line_bytes), lines = static_cast<cuuint64_t>(g.head_dim) / line;
+  const cuuint64_t line = 64, lines = static_cast<cuuint64_t>(g.head_dim) / line;
   const cuuint64_t dims[5] = {line, static_cast<cuuint64_t>(kPageSize), lines, static_cast<cuuint64_t>(g.num_kv_heads), static_cast<cuuint64_t>(g.num_pages)};
   const cuuint64_t strides[4] = {static_cast<cuuint64_t>(g.slot_stride), line, static_cast<cuuint64_t>(g.head_stride), static_cast<cuuint64_t>(g.page_stride)};
   const cuuint32_t box[5] = {static_cast<cuuint32_t>(line), kPageSize, 1, 1, 1};
@@ -104,11 +104,11 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   PrefillMaps maps{};
   const CacheGeom& g = p.geom;
   const bool fp8 = g.dtype == PDA_FP8_E4M3;
-  const auto encode_cache = [&](CUtensorMap* map, const void* base, int line_bytes) {
-    return fp8 ? encode_bytes(map, base, g, line_bytes)
+  const auto encode_cache = [&](CUtensorMap* map, const void* base) {
+    return fp8 ? encode_bytes(map, base, g)
                : make_cache_tensor_map(map, base, g.page_stride, g.head_stride, g.slot_stride, g.num_pages, heads, g.head_dim, 2, 1);
   };
-  if (!encode_q(&maps.q, p, tile_rows) || !encode_cache(&maps.k, p.k_cache, 128) || !encode_cache(&maps.v, p.v_cache, 64))
+  if (!encode_q(&maps.q, p, tile_rows) || !encode_cache(&maps.k, p.k_cache) || !encode_cache(&maps.v, p.v_cache))
     return cudaErrorNotSupported;
   // One pair of CTAs per two SMs at most; the row blocks of all sequences are at most one a sequence and one for
   // every block_rows query tokens.
