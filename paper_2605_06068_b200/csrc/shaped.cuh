@@ -91,7 +91,7 @@ struct RopeAppendParams {
   CacheGeom geom;
   float eps;
   int32_t n_tokens, num_q_heads, table_len, rot_dim, num_axes, axes_used;  // axes_used: bit a for axis a
-  uint8_t freq_axis[128];
+  alignas(4) uint8_t freq_axis[128];
 };
 
 cudaError_t launch_rope_append(const RopeAppendParams& p, bool interleaved, cudaStream_t stream);
