@@ -638,7 +638,8 @@ typedef struct pda_score_desc {
  *   the token array, in the order of their slots (as paged_build_tables lays them out).
  *   q, k, v     [n_tokens, heads, head_dim] bf16 (may be parts of one buffer)
  *   q_out       likewise; may be q itself
- *               (strides in elements, multiples of 8, >= 0; rows of q_out must not overlap)
+ *               (strides in elements, multiples of 8, >= 0, from head to head below 2^31, the caches'
+ *               included; rows of q_out must not overlap)
  *   positions   int32[num_axes][n_tokens], positions_stride elements from axis to axis;
  *               num_axes 1..4. NULL with rot_dim 0
  *   freq_axis   HOST uint8[rot_dim / 2], the axis of each frequency, read during the call; NULL: axis 0

@@ -56,6 +56,9 @@ int rope_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride,
   const int64_t strides[] = {q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride, qo_token_stride, qo_head_stride};
   for (int64_t s : strides)
     if (int rc = check_stride(s)) return rc;
+  // (rows of a token are found by 32-bit strides)
+  if (q_head_stride > INT32_MAX || k_head_stride > INT32_MAX || v_head_stride > INT32_MAX || qo_head_stride > INT32_MAX || g.head_stride > INT32_MAX)
+    return PDA_ERR_TOO_LARGE;
   const void* rows[] = {q, k, v, q_out, k_cache, v_cache, q_norm, k_norm, rot_dim > 0 ? cos_sin : nullptr};
   for (const void* r : rows)
     if (!aligned16(r)) return PDA_ERR_MISALIGNED;
@@ -86,6 +89,7 @@ int rope_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride,
   p.positions_stride = positions_stride;
   p.geom = g;
   p.eps = eps;
+  p.inv_dim = 1.f / static_cast<float>(g.head_dim);
   p.n_tokens = n_tokens;
   p.num_q_heads = num_q_heads;
   p.table_len = table_len;

@@ -3,14 +3,15 @@
 //
 // A head's row lies across D / 16 lanes, each with two 16-byte vectors: for the rotation of halves the vectors i and
 // i + rot/16, whose elements are each other's partners, so that it needs no exchange between lanes; the elements that are not
-// rotated as neighbouring vectors. A warp takes kRows rows of one token at a time for each of its segments: the
-// token's cosines and sines are read once for all of them. The rows are asked for first, before anything that they wait for
-// is known (slot, position, then angles). The norm's sum goes over the segment by shuffles. All of it is held in 32 bits and
-// rounded once.
+// rotated as neighbouring vectors. A warp takes kRows rows of one token and one kind at a time for each of its segments
+// (queries; or keys and the same heads' values, which are copied): the token's cosines and sines times the norm's weights are
+// made once for all of them, and a row's address is one multiply-add. The rows are asked for first, before anything that they
+// wait for is known (slot, position, then angles). All of it is held in 32 bits and rounded once.
 // e4m3 caches: keys and values go another way, since a row's scale is that of its page's first row. A warp takes one head's
 // keys, or values, of kRows tokens a segment one behind the other; of them the first rows of pages give the others their
 // scale by shuffles, and only a page that begins before the warp's tokens has its first row read once more.
 #include "shaped.cuh"
+#include "tcgen05_ptx.cuh"
 #include "tma_ptx.cuh"
 
 namespace pda {
@@ -18,34 +19,44 @@ namespace pda {
 namespace {
 
 constexpr int kRopeWarps = 4;
-constexpr int kRows = 4;  // rows of each segment of a warp
+constexpr int kRows = 4;  // rows of each segment of a warp, even
 
-struct Row {
-  float a[8], b[8];
+// 16 elements of a row as pairs of floats: words 0 .. 3 of the lane's first vector, then those of the second.
+struct Pairs {
+  uint64_t x[8];
 };
-__device__ __forceinline__ void unpack(const uint4& u, float (&x)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ Pairs unpack(const uint4& a, const uint4& b) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  Pairs r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[2 * e] = __uint_as_float(w[e] << 16);
-    x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-  }
+  for (int e = 0; e < 8; ++e) r.x[e] = f32x2(w[e] << 16, w[e] & 0xffff0000u);
+  return r;
 }
-__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-  return make_uint4(pack2<false>(x[0], x[1]), pack2<false>(x[2], x[3]), pack2<false>(x[4], x[5]), pack2<false>(x[6], x[7]));
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
 }
-__device__ __forceinline__ uint2 pack_e4m3(const float (&x)[8], float scale) {
+__device__ __forceinline__ uint64_t both(float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); }
+__device__ __forceinline__ uint32_t to_bf16(uint64_t v) {
+  float lo, hi;
+  f32x2_split(v, lo, hi);
+  return pack2<false>(lo, hi);
+}
+__device__ __forceinline__ uint2 to_e4m3(const uint64_t* v, float scale) {  // four pairs
   uint32_t h[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
+    float lo, hi;
+    f32x2_split(v[e], lo, hi);
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(__fdiv_rn(x[2 * e + 1], scale)), "f"(__fdiv_rn(x[2 * e], scale)));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(__fdiv_rn(hi, scale)), "f"(__fdiv_rn(lo, scale)));
     h[e] = r;
   }
   return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
 }
 
-// What a lane has to do with a row: its two vectors, and their cosines and sines.
+// What a lane has to do with a row: its two vectors, and what they are multiplied by.
 template <int kLanes, bool kPairs>
 struct Lane {
   int i, ca, cb;        // lane of the segment; its vectors of a row
@@ -99,69 +110,84 @@ struct Lane {
       }
     }
   }
-  // Norm (weight: nullptr for rows that have none) and rotation (turned) of a row by its whole segment. any_norm: the same in
-  // all lanes of the warp.
-  __device__ __forceinline__ void turn(const RopeAppendParams& p, Row& x, bool any_norm, const __nv_bfloat16* weight, bool turned,
-                                       const float (&c)[8], const float (&s)[8]) const {
-    if (any_norm) {
-      float ss = 0.f;
+  // Norm and rotation are y = (x A + x' B) / rms: x' the partner (of halves the other vector's element, of pairs the word's
+  // other half), A = cos w, B = -+ sin w' with w, w' the weights of x and x'. They are the same for all of a token's rows of a kind.
+  struct Factors {
+    uint64_t a[8], b[8];
+  };
+  __device__ __forceinline__ Factors factors(const __nv_bfloat16* weight, const float (&c)[8], const float (&s)[8]) const {
+    Pairs w;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], ss));
+    for (int e = 0; e < 8; ++e) w.x[e] = both(1.f);
+    if (weight != nullptr && mine)
+      w = unpack(__ldg(reinterpret_cast<const uint4*>(weight) + ca), __ldg(reinterpret_cast<const uint4*>(weight) + cb));
+    Factors f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (kPairs) {
+        float w0, w1;
+        f32x2_split(w.x[e], w0, w1);
+        f.a[e] = mul2(w.x[e], both(c[e]));
+        f.b[e] = f32x2(__float_as_uint(-s[e] * w1), __float_as_uint(s[e] * w0));
+      } else {
+        const int k = 2 * (e & 3);
+        const uint64_t c2 = f32x2(__float_as_uint(c[k]), __float_as_uint(c[k + 1]));
+        const uint64_t s2 = f32x2(__float_as_uint(s[k]), __float_as_uint(s[k + 1])), minus_s2 = f32x2(__float_as_uint(-s[k]), __float_as_uint(-s[k + 1]));
+        f.a[e] = mul2(w.x[e], c2);
+        f.b[e] = mul2(w.x[e ^ 4], e < 4 ? minus_s2 : s2);
+      }
+    }
+    return f;
+  }
+  // A row by its whole segment (normed: the same in all lanes of the warp).
+  __device__ __forceinline__ Pairs turn(const RopeAppendParams& p, const Pairs& x, bool normed, const Factors& f) const {
+    float inv = 1.f;
+    if (normed) {
+      uint64_t s2[2] = {0ull, 0ull};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s2[e & 1] = fma_f32x2(x.x[e], x.x[e], s2[e & 1]);
+      float s0, s1;
+      f32x2_split(add_f32x2(s2[0], s2[1]), s0, s1);
+      float ss = s0 + s1;
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (weight != nullptr && mine) {
-        const float inv = 1.f / sqrtf(ss / static_cast<float>(p.geom.head_dim) + p.eps);
-        float wa[8], wb[8];
-        unpack(__ldg(reinterpret_cast<const uint4*>(weight) + ca), wa);
-        unpack(__ldg(reinterpret_cast<const uint4*>(weight) + cb), wb);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x.a[e] = x.a[e] * inv * wa[e];
-          x.b[e] = x.b[e] * inv * wb[e];
-        }
-      }
+      inv = rsqrtf(fmaf(ss, p.inv_dim, p.eps));
     }
-    if (turned && rotated) {
+    Pairs y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint64_t partner = x.x[e ^ 4];
       if constexpr (kPairs) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a0 = x.a[2 * e], a1 = x.a[2 * e + 1], b0 = x.b[2 * e], b1 = x.b[2 * e + 1];
-          x.a[2 * e] = fmaf(a0, c[e], -(a1 * s[e]));
-          x.a[2 * e + 1] = fmaf(a1, c[e], a0 * s[e]);
-          x.b[2 * e] = fmaf(b0, c[4 + e], -(b1 * s[4 + e]));
-          x.b[2 * e + 1] = fmaf(b1, c[4 + e], b0 * s[4 + e]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float a = x.a[e], b = x.b[e];
-          x.a[e] = fmaf(a, c[e], -(b * s[e]));
-          x.b[e] = fmaf(b, c[e], a * s[e]);
-        }
+        float lo, hi;
+        f32x2_split(x.x[e], lo, hi);
+        partner = f32x2(__float_as_uint(hi), __float_as_uint(lo));
       }
+      y.x[e] = mul2(x.x[e], f.a[e]);
+      if (rotated) y.x[e] = fma_f32x2(partner, f.b[e], y.x[e]);
+      if (normed) y.x[e] = mul2(y.x[e], both(inv));
     }
+    return y;
   }
 };
 
-// Rows of one token: its queries and, where kKv, keys and values of a bf16 cache.
+// A step of one token: kRows queries a segment, or (kKv, of a bf16 cache) the keys of half as many heads and their values.
 template <int kLanes, bool kPairs, bool kKv>
-__device__ __forceinline__ void token_rows(const RopeAppendParams& p, int64_t item, int lane) {
-  constexpr int kSegs = 32 / kLanes, kStep = kSegs * kRows;  // rows of a token that a warp takes
+__device__ __forceinline__ void token_rows(const RopeAppendParams& p, int t, int step, int lane) {
+  constexpr int kSegs = 32 / kLanes, kTurned = kKv ? kRows / 2 : kRows;  // rows of a segment that are turned
   const Lane<kLanes, kPairs> me(p, lane);
-  const int Hkv = p.geom.num_kv_heads, heads = p.num_q_heads + (kKv ? 2 * Hkv : 0), steps = (heads + kStep - 1) / kStep;
-  const int64_t tok = item / steps;
-  if (tok >= p.n_tokens) return;
-  const int t = static_cast<int>(tok), row0 = static_cast<int>(item % steps) * kStep + lane / kLanes;
+  const int heads = kKv ? p.geom.num_kv_heads : p.num_q_heads, row0 = step * kSegs * kTurned + lane / kLanes;
+  const __nv_bfloat16* from = kKv ? p.k + t * p.k_token_stride : p.q + t * p.q_token_stride;
+  const __nv_bfloat16* from_v = p.v + t * p.v_token_stride;
+  const int head_stride = static_cast<int>(kKv ? p.k_head_stride : p.q_head_stride);
   uint4 ra[kRows], rb[kRows];
 #pragma unroll
   for (int k = 0; k < kRows; ++k) {
-    const int row = row0 + k * kSegs;
+    const bool is_v = k >= kTurned;
+    const int row = row0 + (is_v ? k - kTurned : k) * kSegs;
     ra[k] = rb[k] = make_uint4(0, 0, 0, 0);
     if (me.mine && row < heads) {
-      const __nv_bfloat16* at = row < p.num_q_heads ? p.q + t * p.q_token_stride + row * p.q_head_stride
-                                : row < p.num_q_heads + Hkv ? p.k + t * p.k_token_stride + (row - p.num_q_heads) * p.k_head_stride
-                                                            : p.v + t * p.v_token_stride + (row - p.num_q_heads - Hkv) * p.v_head_stride;
-      const uint4* src = reinterpret_cast<const uint4*>(at);
+      const uint4* src = reinterpret_cast<const uint4*>(is_v ? from_v + static_cast<int64_t>(row) * static_cast<int>(p.v_head_stride)
+                                                             : from + static_cast<int64_t>(row) * head_stride);
       ra[k] = src[me.ca];
       rb[k] = src[me.cb];
     }
@@ -170,45 +196,48 @@ __device__ __forceinline__ void token_rows(const RopeAppendParams& p, int64_t it
   int pos[4];
   const bool good = me.positions(p, t, pos);
   if (slot < 0) return;  // a padding entry
-  const bool in_cache = slot < static_cast<int64_t>(p.geom.num_pages) * kPageSize;
-  if (lane == 0 && row0 == 0 && !good) report(p.status, PDA_DEV_BAD_SEQ_LEN);
-  if (lane == 0 && row0 == 0 && !in_cache) report(p.status, PDA_DEV_BAD_PAGE);
+  if (kKv) {
+    if (!good) return;   // (reported with the token's queries)
+    if (slot >= static_cast<int64_t>(p.geom.num_pages) * kPageSize) return;
+  } else if (step == 0 && lane == 0) {
+    if (!good) report(p.status, PDA_DEV_BAD_SEQ_LEN);
+    if (slot >= static_cast<int64_t>(p.geom.num_pages) * kPageSize) report(p.status, PDA_DEV_BAD_PAGE);
+  }
   float cs[8], sn[8];
   me.angles(p, pos, good, cs, sn);
-  const int page = slot / kPageSize, in_page = slot % kPageSize;
-  const bool any_norm = p.q_norm != nullptr || p.k_norm != nullptr;
+  const __nv_bfloat16* weight = kKv ? p.k_norm : p.q_norm;
+  const auto f = me.factors(weight, cs, sn);
+  const int64_t cache_row = (slot / kPageSize) * p.geom.page_stride + (slot % kPageSize) * p.geom.slot_stride;
+  __nv_bfloat16* to = kKv ? static_cast<__nv_bfloat16*>(p.k_cache) + cache_row : p.q_out + t * p.qo_token_stride;
+  __nv_bfloat16* to_v = static_cast<__nv_bfloat16*>(p.v_cache) + cache_row;
+  const int to_stride = static_cast<int>(kKv ? p.geom.head_stride : p.qo_head_stride);
 #pragma unroll
   for (int k = 0; k < kRows; ++k) {
-    const int row = row0 + k * kSegs;
-    Row x;
-    unpack(ra[k], x.a);
-    unpack(rb[k], x.b);
-    const bool is_q = row < p.num_q_heads, is_v = row >= p.num_q_heads + Hkv;
-    me.turn(p, x, any_norm, is_q ? p.q_norm : is_v ? nullptr : p.k_norm, !is_v, cs, sn);
-    if (!me.mine || row >= heads) continue;
-    if (is_q) {
-      uint4* dst = reinterpret_cast<uint4*>(p.q_out + t * p.qo_token_stride + row * p.qo_head_stride);
-      const uint4 zero = make_uint4(0, 0, 0, 0);
-      dst[me.ca] = good ? pack(x.a) : zero;
-      dst[me.cb] = good ? pack(x.b) : zero;
-    } else if (kKv && in_cache && good) {
-      const int g = row - p.num_q_heads - (is_v ? Hkv : 0);
-      uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(is_v ? p.v_cache : p.k_cache) + page * p.geom.page_stride +
-                                            g * p.geom.head_stride + in_page * p.geom.slot_stride);
-      dst[me.ca] = pack(x.a);
-      dst[me.cb] = pack(x.b);
+    const bool is_v = k >= kTurned;
+    const int row = row0 + (is_v ? k - kTurned : k) * kSegs;
+    uint4 a = ra[k], b = rb[k];
+    if (!is_v) {
+      const Pairs y = me.turn(p, unpack(a, b), weight != nullptr, f);
+      a = make_uint4(to_bf16(y.x[0]), to_bf16(y.x[1]), to_bf16(y.x[2]), to_bf16(y.x[3]));
+      b = make_uint4(to_bf16(y.x[4]), to_bf16(y.x[5]), to_bf16(y.x[6]), to_bf16(y.x[7]));
+      if (!kKv && !good) a = b = make_uint4(0, 0, 0, 0);
+    }
+    if (me.mine && row < heads) {
+      uint4* dst = reinterpret_cast<uint4*>((is_v ? to_v : to) + static_cast<int64_t>(row) * to_stride);
+      dst[me.ca] = a;
+      dst[me.cb] = b;
     }
   }
 }
 
 // Keys, or values, of one head and kRows tokens a segment, into an e4m3 cache.
 template <int kLanes, bool kPairs>
-__device__ __forceinline__ void quantised_rows(const RopeAppendParams& p, int item, int lane) {
+__device__ __forceinline__ void quantised_rows(const RopeAppendParams& p, uint32_t item, int lane) {
   constexpr int kSegs = 32 / kLanes, kTokens = kSegs * kRows;
   const Lane<kLanes, kPairs> me(p, lane);
   const int Hkv = p.geom.num_kv_heads, seg = lane / kLanes;
   const bool is_v = item & 1;
-  const int g = (item >> 1) % Hkv, t0 = (item >> 1) / Hkv * kTokens;
+  const int g = static_cast<int>((item >> 1) % static_cast<uint32_t>(Hkv)), t0 = static_cast<int>((item >> 1) / static_cast<uint32_t>(Hkv)) * kTokens;
   const __nv_bfloat16* rows = is_v ? p.v + g * p.v_head_stride : p.k + g * p.k_head_stride;
   const int64_t stride = is_v ? p.v_token_stride : p.k_token_stride;
   float* scales = is_v ? p.v_scale : p.k_scale;
@@ -221,10 +250,24 @@ __device__ __forceinline__ void quantised_rows(const RopeAppendParams& p, int it
       b = src[me.cb];
     }
   };
-  auto largest = [&](const Row& x) {
+  // (values go through as they are)
+  auto turned = [&](int t, const uint4& a, const uint4& b, bool& good) {
+    int pos[4];
+    good = me.positions(p, t, pos);
+    const Pairs x = unpack(a, b);
+    if (is_v) return x;
+    float cs[8], sn[8];
+    me.angles(p, pos, good, cs, sn);
+    return me.turn(p, x, weight != nullptr, me.factors(weight, cs, sn));
+  };
+  auto largest = [&](const Pairs& x) {
     float top = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(x.a[e]), fabsf(x.b[e])));
+    for (int e = 0; e < 8; ++e) {
+      float lo, hi;
+      f32x2_split(x.x[e], lo, hi);
+      top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
+    }
 #pragma unroll
     for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     return top;
@@ -241,32 +284,18 @@ __device__ __forceinline__ void quantised_rows(const RopeAppendParams& p, int it
   const int slot0 = __ldg(p.slot_map + t0), back = slot0 >= 0 ? slot0 % kPageSize : 0;
   float top_before = -1.f;
   if (back > 0 && back <= t0 && __ldg(p.slot_map + t0 - back) == slot0 - back) {  // (uniform)
-    int pos[4];
-    const bool good = me.positions(p, t0 - back, pos);
-    Row x;
     uint4 a, b;
     load(t0 - back, true, a, b);
-    unpack(a, x.a);
-    unpack(b, x.b);
-    float cs[8], sn[8];
-    if (!is_v) me.angles(p, pos, good, cs, sn);
-    me.turn(p, x, weight != nullptr, weight, !is_v, cs, sn);
-    const float top = largest(x);
+    bool good;
+    const float top = largest(turned(t0 - back, a, b, good));
     if (good) top_before = top;
   }
-  Row x[kRows];
+  Pairs x[kRows];
   float top[kRows];  // of a page's first row; -1 of others
   bool good[kRows];
 #pragma unroll
   for (int k = 0; k < kRows; ++k) {
-    const int t = min(t0 + k * kSegs + seg, p.n_tokens - 1);
-    int pos[4];
-    good[k] = me.positions(p, t, pos);
-    unpack(ra[k], x[k].a);
-    unpack(rb[k], x[k].b);
-    float cs[8], sn[8];
-    if (!is_v) me.angles(p, pos, good[k], cs, sn);
-    me.turn(p, x[k], weight != nullptr, weight, !is_v, cs, sn);
+    x[k] = turned(min(t0 + k * kSegs + seg, p.n_tokens - 1), ra[k], rb[k], good[k]);
     top[k] = largest(x[k]);
     if (slot[k] < 0 || slot[k] % kPageSize != 0 || !good[k]) top[k] = -1.f;
   }
@@ -304,34 +333,42 @@ __device__ __forceinline__ void quantised_rows(const RopeAppendParams& p, int it
     if (!me.mine) continue;
     uint2* dst = reinterpret_cast<uint2*>(static_cast<uint8_t*>(is_v ? p.v_cache : p.k_cache) + page * p.geom.page_stride +
                                           g * p.geom.head_stride + in_page * p.geom.slot_stride);
-    dst[me.ca] = pack_e4m3(x[k].a, scale);
-    dst[me.cb] = pack_e4m3(x[k].b, scale);
+    dst[me.ca] = to_e4m3(&x[k].x[0], scale);
+    dst[me.cb] = to_e4m3(&x[k].x[4], scale);
   }
 }
 
+// quantised: items of e4m3 keys and values, before all others; q_steps, kv_steps: of a token.
 template <int kLanes, bool kPairs, bool kFp8>
-__global__ void __launch_bounds__(kRopeWarps * 32) rope_append_kernel(const __grid_constant__ RopeAppendParams p, int quantised) {
+__global__ void __launch_bounds__(kRopeWarps * 32, 5) rope_append_kernel(const __grid_constant__ RopeAppendParams p, uint32_t quantised, uint32_t q_steps,
+                                                                      uint32_t kv_steps) {
   const int lane = threadIdx.x & 31;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kRopeWarps + (threadIdx.x >> 5);
+  uint32_t item = blockIdx.x * kRopeWarps + (threadIdx.x >> 5);  // (rows are fewer than 2^31)
   if constexpr (kFp8) {  // (the longer items first)
-    if (item < quantised) quantised_rows<kLanes, kPairs>(p, static_cast<int>(item), lane);
-    else token_rows<kLanes, kPairs, false>(p, item - quantised, lane);
-  } else {
-    token_rows<kLanes, kPairs, true>(p, item, lane);
+    if (item < quantised) {
+      quantised_rows<kLanes, kPairs>(p, item, lane);
+      return;
+    }
+    item -= quantised;
   }
+  const uint32_t steps = q_steps + kv_steps, t = item / steps, step = item - t * steps;
+  if (t >= static_cast<uint32_t>(p.n_tokens)) return;
+  if (kFp8 || step < q_steps) token_rows<kLanes, kPairs, false>(p, static_cast<int>(t), static_cast<int>(step), lane);
+  else token_rows<kLanes, kPairs, true>(p, static_cast<int>(t), static_cast<int>(step - q_steps), lane);
 }
 
 template <int kLanes>
 cudaError_t launch(const RopeAppendParams& p, bool interleaved, cudaStream_t stream) {
   constexpr int kStep = 32 / kLanes * kRows;
   const bool fp8 = p.geom.dtype == PDA_FP8_E4M3;
-  const int Hkv = p.geom.num_kv_heads, heads = p.num_q_heads + (fp8 ? 0 : 2 * Hkv);
+  const int Hkv = p.geom.num_kv_heads;
+  const uint32_t q_steps = static_cast<uint32_t>((p.num_q_heads + kStep - 1) / kStep), kv_steps = fp8 ? 0 : static_cast<uint32_t>((Hkv + kStep / 2 - 1) / (kStep / 2));
   const int64_t quantised = fp8 ? 2ll * Hkv * ((static_cast<int64_t>(p.n_tokens) + kStep - 1) / kStep) : 0;
-  const int64_t items = quantised + static_cast<int64_t>(p.n_tokens) * ((heads + kStep - 1) / kStep);
+  const int64_t items = quantised + static_cast<int64_t>(p.n_tokens) * (q_steps + kv_steps);
   const unsigned blocks = static_cast<unsigned>((items + kRopeWarps - 1) / kRopeWarps);
   const auto kernel = interleaved ? (fp8 ? rope_append_kernel<kLanes, true, true> : rope_append_kernel<kLanes, true, false>)
                                   : (fp8 ? rope_append_kernel<kLanes, false, true> : rope_append_kernel<kLanes, false, false>);
-  kernel<<<blocks, kRopeWarps * 32, 0, stream>>>(p, static_cast<int>(quantised));
+  kernel<<<blocks, kRopeWarps * 32, 0, stream>>>(p, static_cast<uint32_t>(quantised), q_steps, kv_steps);
   return cudaGetLastError();
 }
 

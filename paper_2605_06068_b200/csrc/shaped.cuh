@@ -89,7 +89,7 @@ struct RopeAppendParams {
   int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride, qo_token_stride,
       qo_head_stride, positions_stride;
   CacheGeom geom;
-  float eps;
+  float eps, inv_dim;  // 1 / head_dim
   int32_t n_tokens, num_q_heads, table_len, rot_dim, num_axes, axes_used;  // axes_used: bit a for axis a
   alignas(4) uint8_t freq_axis[128];
 };
