@@ -651,20 +651,16 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
     return out
 
 
+# What the calls below take from shapes and strides alone is checked and worked out once for each layout.
+
 @functools.lru_cache(maxsize=64)
-def _kv_desc(page_stride, head_stride, slot_stride, num_pages, num_kv_heads, page_size, head_dim, dtype):
-    return CacheDesc(page_stride, head_stride, slot_stride, num_pages, page_size, num_kv_heads, head_dim, dtype)
-
-
-def _paged_caches(k_cache, v_cache, k_scale, v_scale):
-    """Descriptor of the two ``[num_pages, Hkv, 16, D]`` caches (not to be written to); e4m3 ones have a scale per page and
-    head."""
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or v_cache.dtype is not k_cache.dtype:
+def _kv_layout(shape, k_stride, v_shape, v_stride, dtype, v_dtype):
+    """Descriptor of two ``[num_pages, Hkv, 16, D]`` caches (not to be written to)."""
+    if len(shape) != 4 or v_shape != shape or v_dtype is not dtype:
         raise ValueError("k_cache and v_cache: expected two [pages, kv heads, page size, head_dim] tensors of one type")
-    n, heads, P, D = k_cache.shape
+    n, heads, P, D = shape
     strides = []
-    for cache in (k_cache, v_cache):
-        page, head, slot, last = cache.stride()
+    for page, head, slot, last in (k_stride, v_stride):
         if last != 1 and D > 1:
             raise ValueError("k_cache, v_cache: the last dimension must be contiguous")
         # (a dimension of extent 1 may carry any stride: a dense one is taken)
@@ -677,25 +673,38 @@ def _paged_caches(k_cache, v_cache, k_scale, v_scale):
         strides.append((page, head, slot))
     if strides[0] != strides[1]:
         raise ValueError("k_cache and v_cache: expected the same strides")
-    if k_cache.dtype is _BF16:
-        dtype = PDA_BF16
-    elif k_cache.dtype in (torch.uint8, torch.float8_e4m3fn):
-        dtype = PDA_FP8_E4M3
+    if dtype is not _BF16 and dtype not in (torch.uint8, torch.float8_e4m3fn):
+        raise TypeError(f"unsupported cache dtype {dtype}")
+    return CacheDesc(*strides[0], n, P, heads, D, PDA_BF16 if dtype is _BF16 else PDA_FP8_E4M3)
+
+
+def _paged_caches(k_cache, v_cache, k_scale, v_scale, head_dim):
+    """Descriptor of the two caches; e4m3 ones have a scale per page and head."""
+    desc = _kv_layout(k_cache.shape, k_cache.stride(), v_cache.shape, v_cache.stride(), k_cache.dtype, v_cache.dtype)
+    if desc.dtype == PDA_FP8_E4M3:
         for scale in (k_scale, v_scale):
-            if scale is None or scale.dtype is not torch.float32 or scale.shape != (n, heads) or not scale.is_contiguous():
+            if scale is None or scale.dtype is not torch.float32 or scale.shape != k_cache.shape[:2] or not scale.is_contiguous():
                 raise ValueError("k_scale and v_scale: expected contiguous float32 [pages, kv heads] for e4m3 caches")
-    else:
-        raise TypeError(f"unsupported cache dtype {k_cache.dtype}")
-    return _kv_desc(*strides[0], n, heads, P, D, dtype)
+    if desc.head_dim != head_dim:
+        raise ValueError("q and the caches differ in head_dim")
+    return desc
 
 
-def _head_rows(name, t, n, D):
-    """(token stride, head stride, heads) of bf16 rows ``[n, heads, D]``."""
-    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != D:
-        raise ValueError(f"{name}: expected [{n}, heads, {D}]")
-    token, head, _ = _bf16_rows(name, t)
-    heads = t.shape[1]
-    return (token if n > 1 else 0), (head if heads > 1 else 0), heads
+@functools.lru_cache(maxsize=256)
+def _row_layout(name, shape, stride, tokens, heads, head_dim):
+    """(token stride, head stride) of rows ``[tokens, heads, head_dim]``."""
+    if shape != (tokens, heads, head_dim):
+        raise ValueError(f"{name}: expected [{tokens}, {heads} heads, {head_dim}]")
+    if stride[2] != 1 and head_dim > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    # (a dimension of extent 1 may carry any stride)
+    return (stride[0] if tokens > 1 else 0), (stride[1] if heads > 1 else 0)
+
+
+def _rows_of(name, t, tokens, heads, head_dim):
+    if t.dtype is not _BF16:
+        raise TypeError(f"{name}: expected bfloat16, got {t.dtype}")
+    return _row_layout(name, t.shape, t.stride(), tokens, heads, head_dim)
 
 
 @functools.lru_cache(maxsize=64)
@@ -711,19 +720,17 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
 
     ``cos_sin`` float32 ``[positions, rot_dim]``: cosines, then sines, of each position's ``rot_dim / 2`` angles; None: no
     rotation. ``positions`` int32 ``[T]``, or ``[axes, T]`` with ``freq_axis``, the axis of each of the ``rot_dim / 2``
-    frequencies (a sequence of ints on the host). e4m3 caches take ``k_scale``/``v_scale`` ``[pages, Hkv]``, which are updated."""
+    frequencies (a sequence of ints on the host; a tuple or bytes is taken fastest). e4m3 caches take ``k_scale``/``v_scale``
+    ``[pages, Hkv]``, which are updated."""
     T, Hq, D = q.shape
-    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale)
-    if desc.head_dim != D:
-        raise ValueError("q and the caches differ in head_dim")
+    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale, D)
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
-    q_token, q_head, _ = _head_rows("q", q, T, D)
-    k_token, k_head, k_heads = _head_rows("k", k, T, D)
-    v_token, v_head, v_heads = _head_rows("v", v, T, D)
-    o_token, o_head, o_heads = _head_rows("out", out, T, D)
-    if k_heads != desc.num_kv_heads or v_heads != desc.num_kv_heads or o_heads != Hq:
-        raise ValueError("k, v or out: wrong number of heads")
+    Hkv = desc.num_kv_heads
+    q_token, q_head = _rows_of("q", q, T, Hq, D)
+    k_token, k_head = _rows_of("k", k, T, Hkv, D)
+    v_token, v_head = _rows_of("v", v, T, Hkv, D)
+    o_token, o_head = _rows_of("out", out, T, Hq, D)
     _int32(slot_map, status)
     if slot_map.numel() != T:
         raise ValueError("slot_map: expected one entry per token")
@@ -736,15 +743,16 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
         if cos_sin.dim() != 2 or cos_sin.dtype is not torch.float32 or not cos_sin.is_contiguous():
             raise ValueError("cos_sin: expected contiguous float32 [positions, rot_dim]")
         table, rot = cos_sin.shape
-        if positions.dtype is not _I32 or positions.dim() > 2 or positions.shape[-1] != T or (T > 1 and positions.stride(-1) != 1):
+        where = positions.shape
+        if positions.dtype is not _I32 or len(where) > 2 or where[-1] != T or (T > 1 and positions.stride(-1) != 1):
             raise ValueError("positions: expected int32 [T] or [axes, T]")
-        if positions.dim() == 2:
-            axes = positions.shape[0]
+        if len(where) == 2:
+            axes = where[0]
             pos_stride = positions.stride(0) if axes > 1 else T
             if freq_axis is None and axes > 1:
                 raise ValueError("freq_axis: needed for positions of several axes")
         if freq_axis is not None:
-            axis = _axis_bytes(tuple(freq_axis))
+            axis = freq_axis if type(freq_axis) is bytes else _axis_bytes(tuple(freq_axis))
             if len(axis) != rot // 2 or (len(axis) and max(axis) >= axes):
                 raise ValueError("freq_axis: expected an axis for each of the rot_dim / 2 frequencies")
     else:
@@ -753,8 +761,8 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
     with _device_call(dev):
         rc = lib().rope_kv_append(
             q.data_ptr(), q_token, q_head, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, _dp(positions), pos_stride,
-            axes, axis, _dp(cos_sin), table, rot, int(interleaved), _dp(q_norm), _dp(k_norm), eps, slot_map.data_ptr(), T, Hq,
-            out.data_ptr(), o_token, o_head, k_cache.data_ptr(), v_cache.data_ptr(), C.byref(desc), _dp(k_scale), _dp(v_scale),
+            axes, axis, _dp(cos_sin), table, rot, interleaved, _dp(q_norm), _dp(k_norm), eps, slot_map.data_ptr(), T, Hq,
+            out.data_ptr(), o_token, o_head, k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale),
             _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "rope_kv_append")
@@ -762,9 +770,16 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
 
 
 def _score_desc(scale, softcap, slopes, window, num_q_heads):
-    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.numel() != num_q_heads or not slopes.is_contiguous()):
+    if slopes is None:
+        return _plain_score(scale, softcap, window)
+    if slopes.dtype is not torch.float32 or slopes.numel() != num_q_heads or not slopes.is_contiguous():
         raise ValueError("slopes: expected contiguous float32 [query heads]")
-    return ScoreDesc(scale, softcap, _dp(slopes), window)
+    return ScoreDesc(scale, softcap, slopes.data_ptr(), window)
+
+
+@functools.lru_cache(maxsize=64)
+def _plain_score(scale, softcap, window):
+    return ScoreDesc(scale, softcap, None, window)
 
 
 def prefill_workspace(num_q_heads, head_dim, device="cuda", stream=None):
@@ -782,15 +797,11 @@ def paged_prefill_attention(q, k_cache, v_cache, block_table, seq_lens, cu_q, ma
     capped by ``softcap``, biased by ``slopes`` [Hq] times the distance and masked by ``window``, ``prefix_lens`` [B] and
     ``first_keys`` [Tq]. Without ``workspace`` one is allocated for the call."""
     Tq, Hq, D = q.shape
-    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale)
-    if desc.head_dim != D:
-        raise ValueError("q and the caches differ in head_dim")
+    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale, D)
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
-    q_token, q_head, _ = _head_rows("q", q, Tq, D)
-    o_token, o_head, o_heads = _head_rows("out", out, Tq, D)
-    if o_heads != Hq:
-        raise ValueError("out: expected the shape of q")
+    q_token, q_head = _rows_of("q", q, Tq, Hq, D)
+    o_token, o_head = _rows_of("out", out, Tq, Hq, D)
     _int32(seq_lens, cu_q, prefix_lens, first_keys, status)
     B = seq_lens.numel()
     if cu_q.numel() != B + 1:
@@ -809,8 +820,8 @@ def paged_prefill_attention(q, k_cache, v_cache, block_table, seq_lens, cu_q, ma
                        workspace, status)
     with _device_call(dev):
         rc = lib().paged_prefill_attention(
-            q.data_ptr(), q_token, q_head, k_cache.data_ptr(), v_cache.data_ptr(), C.byref(desc), _dp(k_scale), _dp(v_scale),
-            block_table.data_ptr(), stride, seq_lens.data_ptr(), cu_q.data_ptr(), B, Hq, min(int(max_q), Tq), Tq, C.byref(score),
+            q.data_ptr(), q_token, q_head, k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale),
+            block_table.data_ptr(), stride, seq_lens.data_ptr(), cu_q.data_ptr(), B, Hq, min(int(max_q), Tq), Tq, score,
             _dp(prefix_lens), _dp(first_keys), out.data_ptr(), o_token, o_head, workspace.data_ptr(), workspace.nbytes, flags,
             _dp(status), _raw(stream, dev))
     if rc:
@@ -825,9 +836,7 @@ def paged_biased_decode_attention(q, k_cache, v_cache, block_table, seq_lens, sc
     masked by ``window`` and ``first_keys`` [B]; ``q [B,Hq,D]``. ``chunk_tokens > 0`` splits the tokens (``part_o``, ``part_lse``
     as there; ``workspace`` as in ``paged_decode_step``). Always fills and returns ``out``."""
     B, Hq, D = q.shape
-    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale)
-    if desc.head_dim != D:
-        raise ValueError("q and the caches differ in head_dim")
+    desc = _paged_caches(k_cache, v_cache, k_scale, v_scale, D)
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
     for name, t in (("q", q), ("out", out)):
@@ -857,8 +866,8 @@ def paged_biased_decode_attention(q, k_cache, v_cache, block_table, seq_lens, sc
                        v_scale, status)
     with _device_call(dev):
         rc = lib().paged_biased_decode_attention(
-            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), C.byref(desc), _dp(k_scale), _dp(v_scale), block_table.data_ptr(),
-            stride, seq_lens.data_ptr(), B, Hq, C.byref(score), _dp(first_keys), chunk_tokens, out.data_ptr(), _dp(part_o),
+            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale), block_table.data_ptr(),
+            stride, seq_lens.data_ptr(), B, Hq, score, _dp(first_keys), chunk_tokens, out.data_ptr(), _dp(part_o),
             _dp(part_lse), mc, _dp(workspace), flags, _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "paged_biased_decode_attention")
