@@ -709,9 +709,9 @@ int64_t pda_prefill_workspace_bytes(int32_t num_q_heads, int32_t head_dim);
  * keys max(0, p - window + 1, first_keys[b]) <= j <= p.
  *   q, out       [batch, num_q_heads, head_dim] bf16, contiguous
  *   first_keys   int32[batch] or NULL
- *   chunk_tokens 0: one unit per (sequence, kv head); > 0 (a multiple of 16): split into chunks as in
- *                paged_decode_attention, with part_o, part_lse and max_chunks as there; they are scratch,
- *                and the merge runs inside this call
+ *   chunk_tokens 0: one unit per (sequence, kv head); > 0 (a multiple of 16): split into chunks of at most
+ *                so many tokens, with part_o, part_lse and max_chunks as in paged_decode_attention; they are
+ *                scratch, and the merge runs inside this call
  *   workspace    (chunk_tokens > 0) int32[pda_workspace_ints(batch, num_kv_heads * ceil(group / 8))] as in
  *                paged_decode_step: zeroed by the caller once, left zeroed, one per stream of overlapping
  *                calls. NULL: the merge is a launch of its own
