@@ -90,7 +90,7 @@ struct GCfg {
   static constexpr int kRing = 2 * kQBytes;
   static constexpr int kRawAt = kRing + kStages * (kKBytes + kVBytes);
   static constexpr int kBook = kRawAt + kRaw * 2 * kRawBytes;
-  static constexpr int kBars = 9 * kStages + 32 + 4 * kRaw + kGScaleSlots;
+  static constexpr int kBars = (9 * kStages + 32 + 4 * kRaw + kGScaleSlots + 1) / 2 * 2;
   static constexpr int kSmemBytes = kBook + kGBookBytes + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory");
 };
@@ -141,14 +141,19 @@ __device__ __forceinline__ float rescale(float from, float to, float c) { return
 // the later n1 tiles of the same head, and the first half's warps merge the two results.
 enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
 struct GUnit {
-  int b, row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace
+  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace
   __device__ int first_row(int w, int half_rows) const { return row0 + (dual ? 0 : half_rows * w); }
   __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
   __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
-  // The pair's i-th tile: whose half's (where that matters), and which 128 keys from tile0 on.
+  // The pair's i-th tile: whose half's (where that matters), and which 128 keys from tile0 on, the last ones first (down) or the
+  // first ones. Of a block of two halves both read the pair's tiles up to their own last one; down, from it on.
   __device__ int half_of(int i) const { return i & 1; }
-  __device__ int keys_of(int i) const { return dual ? key_tile(i & 1, i >> 1) : i; }
+  __device__ int keys_of(int i, bool down) const {
+    if (!dual) return down ? tiles() - 1 - i : i;
+    return key_tile(i & 1, down ? (i & 1 ? n1 : n0) - 1 - (i >> 1) : i >> 1);
+  }
   __device__ int key_tile(int w, int j) const { return dual == kSplitKeys && w ? n0 + j : j; }
+  __device__ int skipped(int w, bool down) const { return dual || !down ? 0 : tiles() - (w ? n1 : n0); }
 };
 constexpr uint32_t kGSmallBlock = 1u << 30;  // (in a list entry) fits one half
 __device__ __forceinline__ int units_of(uint32_t entry, int heads, bool by_two) {
@@ -175,13 +180,14 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   constexpr bool kZ = kShape != kShapeNone;        // scores are shaped before the softmax
   constexpr bool kCap = (kShape & kShapeCap) != 0, kBias = (kShape & kShapeBias) != 0;
   constexpr bool kFixed = kShape == kShapeCap;     // ... and lie within bounds: the reference is fixed
+  constexpr bool kDown = kBias;                    // a bias has the scores rise from tile to tile: the last tiles come first
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kBook);
-  GUnit* units = reinterpret_cast<GUnit*>(bars + C::kBars);         // [kGUnitSlots]
-  uint32_t* list = reinterpret_cast<uint32_t*>(units + kGUnitSlots);  // [kGMaxList] sequence and block, most work first
-  uint32_t* work = list + kGMaxList;                                // [kGMaxList] tiles, then units of the entries before
-  uint32_t* scan = work + kGMaxList;                                // [4] by warp
+  uint32_t* work = reinterpret_cast<uint32_t*>(bars + C::kBars);    // [kGMaxList] tiles, then units of the entries before
+  uint32_t* list = work + kGMaxList;                                // [kGMaxList] sequence and block, most work first
+  GUnit* units = reinterpret_cast<GUnit*>(list + kGMaxList);        // [kGUnitSlots]
+  uint32_t* scan = reinterpret_cast<uint32_t*>(units + kGUnitSlots);  // [4] by warp
   uint32_t* tmem_slot = scan + 5;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   uint32_t* target_sh = reinterpret_cast<uint32_t*>(cta_err + 1);   // tiles of a part
@@ -311,7 +317,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     if (tid < n_blocks) {
       my_work = work[tid];
       my_entry = list[tid];
-      for (int i = 0; i < n_blocks; ++i) place += work[i] > my_work || (work[i] == my_work && i < tid);
+      for (int i = 0; i < n_blocks; i += 4) {  // (behind the last: anything, which does not count)
+        const uint4 v = *reinterpret_cast<const uint4*>(work + i);
+        const uint32_t of[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) place += i + e < n_blocks && (of[e] > my_work || (of[e] == my_work && i + e < tid));
+      }
     }
     // Few units: the fewest tiles a part with which all parts find a pair each.
     if (plan.cut && warp == 0) {
@@ -406,21 +417,27 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       const int n = uniform(w == 0 ? un.n0 : un.n1), n_other = uniform(w == 0 ? un.n1 : un.n0);
       const int dual = uniform(un.dual);
       const int step = dual ? 2 : 1, own = dual ? w : 0;  // this half's tiles: t0 + step * j + own
-      const int set = dual ? 1 + w : 0, c0 = counts[dual ? 1 : 0];  // this unit's tiles on the set's barriers: c0 + j
+      const int skip = uniform(un.skipped(w, kDown));
+      const int set = dual ? 1 + w : 0, c0 = counts[dual ? 1 : 0] + skip;  // this unit's tiles on the set's barriers: c0 + j
       // Both halves give a tile of a block of two halves back. The one that does not read it does so as soon as it is
-      // there (see tile_bar) and goes on, to the next unit where this was the last tile.
+      // there (see tile_bar) and goes on. (j: counted from this half's first one)
       auto hand_on = [&](uint32_t full, uint32_t empty, int j) {
         wait(tile_bar(full, 0, c0 + j), (c0 + j) / kStages);
-        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty + 8 * ((t0 + j) % kStages), lane));
+        if (ok && lane < 2) arrive_cluster_tc(in_cta(empty + 8 * ((t0 + skip + j) % kStages), lane));
         __syncwarp();
       };
+      for (int j = -skip; ok && j < 0; ++j) {
+        hand_on(full_k, empty_k, j);
+        hand_on(v_ready, empty_v, j);
+      }
+      if (!ok) break;
       // (a tile of a dual block is given back twice by its half)
       auto give_back = [&](uint32_t bar) {
         commit2_if(leader, bar);
         if (dual) commit2_if(leader, bar);
       };
       if (n > 0) {  // S(0): its place is free, the tensor core works a thread's products off in order
-        const int t = t0 + own, sk = t % kStages;
+        const int t = t0 + skip + own, sk = t % kStages;
         wait(bar_q + 8 * w, done);
         wait(tile_bar(full_k, set, c0), c0 / kStages);
         if (!ok) break;
@@ -432,7 +449,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         give_back(uniform(u_ek + 8 * sk));
       }
       for (int j = 0; j < n; ++j) {
-        const int t = t0 + step * j + own, tn = t + step, sv = t % kStages, sk = tn % kStages;
+        const int t = t0 + skip + step * j + own, tn = t + step, sv = t % kStages, sk = tn % kStages;
         wait(tile_bar(v_ready, set, c0 + j), (c0 + j) / kStages);
         const uint64_t v0 = tc_desc(uniform(u_v + sv * C::kVBytes), 16, 1024);
         const uint32_t k_addr = uniform(u_k + sk * C::kKBytes), ev = uniform(u_ev + 8 * sv), ek = uniform(u_ek + 8 * sk);
@@ -462,7 +479,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         give_back(ev);
         if (j + 1 < n) give_back(ek);
       }
-      if (!dual)
+      if (!dual && !kDown)
         for (int j = n; ok && j < n_other; ++j) {
           hand_on(full_k, empty_k, j);
           hand_on(v_ready, empty_v, j);
@@ -528,7 +545,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           dual = kSplitKeys;
           n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last key)
         }
-        un = GUnit{b, row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0};
+        un = GUnit{row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0};
         b_now = b;
         lo_now = lo;
         hi_now = key_end;
@@ -617,11 +634,13 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           int id;
           float ks, vs;  // (e4m3) the page's scales
         };
+        // (lanes 8 j .. 8 j + 7: the j-th of four tiles, downwards or upwards)
         auto load_pages = [&](int first_tile, int head) {
-          const int64_t page = (static_cast<int64_t>(tile0) + first_tile) * 8 + lane;
+          const int tile = first_tile + (kDown ? -(lane >> 3) : lane >> 3);
+          const int64_t page = (static_cast<int64_t>(tile0) + tile) * 8 + (lane & 7);
           Pages r{p.geom.num_pages, 0.f, 0.f};
           bool bad = false;
-          if (page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now) {
+          if (tile >= 0 && page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now) {
             const int v = table[page];
             bad = v < 0 || v >= p.geom.num_pages;
             if (!bad) {
@@ -641,9 +660,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           return r;
         };
         // (of the second half where it has tiles of its own: other keys, or the same of the next head)
-        const int from1 = un.dual == kSplitKeys ? un.n0 : 0, head1 = un.head(1);
-        Pages now0 = load_pages(0, un.h), next0 = un.tiles() > 4 ? load_pages(4, un.h) : now0;
-        Pages now1 = un.dual ? load_pages(from1, head1) : now0, next1 = un.dual && un.n1 > 4 ? load_pages(from1 + 4, head1) : now0;
+        const int head1 = un.head(1), own0 = un.dual ? un.n0 : un.tiles();
+        auto tile_of = [&](int w, int j) { return un.key_tile(w, kDown ? (w ? un.n1 : own0) - 1 - j : j); };
+        Pages now0 = load_pages(tile_of(0, 0), un.h), next0 = un.tiles() > 4 ? load_pages(tile_of(0, 4), un.h) : now0;
+        Pages now1 = un.dual ? load_pages(tile_of(1, 0), head1) : now0, next1 = un.dual && un.n1 > 4 ? load_pages(tile_of(1, 4), head1) : now0;
         const int n_all = un.tiles();
         auto load_q = [&](int w) {
           if (ok && done[w] > 0) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_qfree + 8 * w, (done[w] - 1) & 1));
@@ -665,10 +685,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           if ((j & 3) == 0 && j > 0) {
             if (other) {
               now1 = next1;
-              if (j + 4 < un.n1) next1 = load_pages(from1 + j + 4, head1);
+              if (j + 4 < un.n1) next1 = load_pages(tile_of(1, j + 4), head1);
             } else {
               now0 = next0;
-              if (j + 4 < (un.dual ? un.n0 : n_all)) next0 = load_pages(j + 4, un.h);
+              if (j + 4 < own0) next0 = load_pages(tile_of(0, j + 4), un.h);
             }
           }
           const int ids = other ? now1.id : now0.id;
@@ -760,7 +780,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           const int set = un.dual ? 1 + (i & 1) : 0;
           const int count = set == 0 ? counts[0] : set == 1 ? counts[1] : counts[2];
           if (set == 0) ++counts[0]; else if (set == 1) ++counts[1]; else ++counts[2];
-          const int64_t valid = un.L - (static_cast<int64_t>(un.tile0) + un.keys_of(i)) * kGKeys;
+          const int64_t valid = un.L - (static_cast<int64_t>(un.tile0) + un.keys_of(i, kDown)) * kGKeys;
           const uint32_t raw = smem_u32(smem) + C::kRawAt + rs * 2 * C::kRawBytes;
 #pragma unroll 1
           for (int v = 0; v < 2; ++v) {  // K, then V
@@ -798,7 +818,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           const int st = t % kStages;
           ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_v + 8 * st, (t / kStages) & 1));
           if (!ok) break;
-          const int64_t valid = un.L - (static_cast<int64_t>(un.tile0) + un.keys_of(i)) * kGKeys;
+          const int64_t valid = un.L - (static_cast<int64_t>(un.tile0) + un.keys_of(i, kDown)) * kGKeys;
           const bool partly = valid > 0 && valid < kGKeys;  // (pages behind the end have been read as zeros)
           if (partly) {
             // (keys behind the end have weight 0, but what they hold may be anything)
@@ -854,7 +874,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         if (!next_unit(unit, un)) break;
         n = w == 0 ? un.n0 : un.n1;
         step = un.dual ? 2 : 1;
-        own = un.dual ? w : 0;
+        own = un.dual ? w : un.skipped(w, kDown);
         const int row = un.first_row(w, half_rows) + plan.tile_rows * rank + row_token, pos = un.L - un.nq + row;
         const bool exists = row_used && row < un.nq;
         lo = hi = 0;
@@ -872,51 +892,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         if constexpr (kBias) {
           slope = exists && p.score.slopes != nullptr ? p.score.slopes[un.head(w) * p.group + row_head] * kLog2e : 0.f;
           key0_pos = static_cast<int>(key0 - pos);
-          // A bias has the scores rise from tile to tile, up to the token's own key: its score, which no distance lowers, is
-          // taken here as the first reference. (The row's maximum is no lower, and rarely is it much higher.)
-          if (exists && n > 0 && pos >= 0 && lo <= -key0_pos) {
-            const int page = p.block_table[static_cast<int64_t>(un.b) * p.block_table_stride + pos / kPageSize];
-            if (page >= 0 && page < p.geom.num_pages) {
-              const uint4* q = reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(un.q0) + row) * p.q_token_stride + (un.head(w) * p.group + row_head) * p.q_head_stride);
-              const int64_t key_at = page * p.geom.page_stride + un.head(w) * p.geom.head_stride + (pos % kPageSize) * p.geom.slot_stride;
-              float dot = 0.f;
-              auto add = [&](uint32_t a, float b0, float b1) {
-                dot = fmaf(__uint_as_float(a << 16), b0, dot);
-                dot = fmaf(__uint_as_float(a & 0xffff0000u), b1, dot);
-              };
-              if constexpr (kFp8) {
-                const uint2* key = reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.k_cache) + key_at);
-#pragma unroll 8
-                for (int c = 0; c < D / 8; ++c) {
-                  const uint4 a = q[c];
-                  const uint2 b = key[c];
-                  const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[2] = {b.x, b.y};
-#pragma unroll
-                  for (int e = 0; e < 4; ++e)
-                    add(aw[e], e4m3_to_float(static_cast<uint8_t>(bw[e >> 1] >> (16 * (e & 1)))), e4m3_to_float(static_cast<uint8_t>(bw[e >> 1] >> (16 * (e & 1) + 8))));
-                }
-                dot *= p.k_scale[static_cast<int64_t>(page) * heads + un.head(w)];
-              } else {
-                const uint4* key = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.k_cache) + key_at);
-#pragma unroll 8
-                for (int c = 0; c < D / 8; ++c) {
-                  const uint4 a = q[c], b = key[c];
-                  const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) add(aw[e], __uint_as_float(bw[e] << 16), __uint_as_float(bw[e] & 0xffff0000u));
-                }
-              }
-              dot *= p.score.mul;
-              if constexpr (kCap) dot = fmaf(-2.f * p.score.cap, rcp_approx(ex2(dot) + 1.f), p.score.cap);
-              if (fabsf(dot) < 3.0e38f) m_ref = dot;
-            }
-          }
         }
       }
       c_ref = score_factor(m_ref, scale_log2);
       float l = 0.f;
       // One tile; masked: some row of the warp does not see all of it.
-      auto tile = [&](auto masked, int j) {
+      auto tile = [&](auto masked, int j, int j_key) {  // j_key: which of the half's tiles by its keys
         constexpr bool kMasked = decltype(masked)::value;
         // 64 keys at a time; the first run's products start while the second run is here. (Not unrolled: both runs' code, masked and
         // not, was more than the instruction caches held: a third of all stalls were for instructions.)
@@ -930,7 +911,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           tmem_ld32(my_s + 64 * k + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
           tmem_wait_ld();
           // keys of the run's columns: 32 k + e, from the 32nd on 32 k + 32 + e
-          const int first_lo = j * kGKeys + 32 * k, first_hi = first_lo + 32;
+          const int first_lo = j_key * kGKeys + 32 * k, first_hi = first_lo + 32;
           // (columns of the run that this row sees, a bit each)
           [[maybe_unused]] uint32_t seen[2];
           if (kMasked) {
@@ -1152,8 +1133,9 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         }
       };
       for (int j = 0; ok && j < n; ++j, ++t) {
-        if (full_from <= j * kGKeys && full_to >= (j + 1) * kGKeys) tile(std::false_type{}, j);
-        else tile(std::true_type{}, j);
+        const int j_key = kDown ? n - 1 - j : j;
+        if (full_from <= j_key * kGKeys && full_to >= (j_key + 1) * kGKeys) tile(std::false_type{}, j, j_key);
+        else tile(std::true_type{}, j, j_key);
       }
       // ---- output
       if constexpr (kFp8) pair_t += units[unit % kGUnitSlots].tiles();
