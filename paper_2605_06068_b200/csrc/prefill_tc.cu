@@ -26,9 +26,10 @@ bool encode_q(CUtensorMap* map, const PrefillParams& p, int tile_rows) {
 // of s could leave 32 bits' range, all go the other way.
 void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
   // tanh(x) by odd polynomials whose largest error over the range is least (linear programming over 4000 points):
-  // 5.3e-6 for |x| <= 1/2, 2.8e-6 for |x| <= 1
+  // 5.3e-6 for |x| <= 1/2, 2.4e-6 for |x| <= 5/4
   static const double c5[3] = {0.9999248385429382, -0.33085504174232483, 0.11254137754440308};
-  static const double c9[5] = {0.9999684691429138, -0.33265823125839233, 0.12922066450119019, -0.04329986125230789, 0.008365885354578495};
+  static const double c11[6] = {0.9999746680259705, -0.33283931016921997, 0.1305362582206726, -0.04692675918340683, 0.01253201998770237,
+                                -0.0016820720629766583};
   const double u = static_cast<double>(score.mul) / (2.0 * 1.4426950408889634);
   const auto twice = [](double v) {
     const float f = static_cast<float>(v);
@@ -36,14 +37,14 @@ void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
     memcpy(&bits, &f, 4);
     return static_cast<uint64_t>(bits) << 32 | bits;
   };
-  const bool usable = std::abs(u) >= 1.0 / 4096 && std::abs(u) <= 4096 && score.cap <= 4096.f && score.cap >= 1.f / 4096;
+  const bool usable = std::abs(u) >= 1.0 / 1024 && std::abs(u) <= 1024 && score.cap <= 4096.f && score.cap >= 1.f / 4096;
   plan->limit[0] = usable ? static_cast<float>(0.5 / std::abs(u)) : -1.f;
-  plan->limit[1] = usable ? static_cast<float>(1.0 / std::abs(u)) : -1.f;
+  plan->limit[1] = usable ? static_cast<float>(1.25 / std::abs(u)) : -1.f;
   plan->ref = shape == kShapeCap ? std::max(score.cap - kGFixedTop, 0.f) : 0.f;
   double power = u * score.cap;
-  for (int i = 0; i < 5; ++i, power *= u * u) {
+  for (int i = 0; i < 6; ++i, power *= u * u) {
     if (i < 3) plan->poly5[i] = twice(usable ? c5[i] * power : 0.0);
-    plan->poly9[i] = twice(usable ? c9[i] * power : 0.0);
+    plan->poly11[i] = twice(usable ? c11[i] * power : 0.0);
   }
 }
 
@@ -55,7 +56,7 @@ cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const Prefil
   if (e != cudaSuccess) return e;
   kernel<<<static_cast<unsigned>(2 * pairs), C::kThreads, C::kSmemBytes, stream>>>(maps, p, plan);
   if ((e = cudaGetLastError()) != cudaSuccess || !plan.cut) return e;
-  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone ? plan.scale_log2 : 1.f,
+  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone && !kFp8 ? plan.scale_log2 : 1.f,
                                                                                        kShape == kShapeCap ? 0.f : 5.4210109e-20f);
   return cudaGetLastError();
 }
@@ -86,6 +87,8 @@ bool encode_bytes(CUtensorMap* map, const void* base, const CacheGeom& g) {
 
 bool prefill_tc_supports(const PrefillParams& p) {
   if (p.geom.head_dim != 128 && (p.geom.head_dim != 64 || p.geom.dtype != PDA_BF16)) return false;
+  // (a bias of keys in a prefix is taken in the products' units)
+  if (p.score.slopes != nullptr && p.prefix_lens != nullptr && std::abs(p.score.mul) < 1e-18f) return false;
   if (p.group > 128 || p.geom.num_pages < 1 || p.geom.num_pages == INT32_MAX) return false;
   const auto fits = [](int64_t stride, int64_t extent) { return extent == 1 || (stride > 0 && stride < (1ll << 38)); };
   if (!fits(p.q_token_stride, p.total_q) || !fits(p.q_head_stride, p.num_q_heads)) return false;

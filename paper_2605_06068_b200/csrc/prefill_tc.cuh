@@ -31,9 +31,9 @@ struct PrefillPlan {
   int cut;        // few units: blocks are cut along the keys, so that every pair has a part
   float scale_log2;
   // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): of degree 5 for
-  // |s| <= limit[0], of degree 9 for |s| <= limit[1]; minus the fixed reference (capped only), or 0.
+  // |s| <= limit[0], of degree 11 for |s| <= limit[1]; ref: the fixed reference (capped only), or 0.
   float limit[2], ref;
-  uint64_t poly5[3], poly9[5];
+  uint64_t poly5[3], poly11[6];
 };
 struct PrefillMaps {
   CUtensorMap q, k, v;
@@ -126,7 +126,7 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
 // cancels in the quotient. c is the scale as long as |c r| < 2^28, where that is at most 2^8. Beyond, scores that differ at
 // all differ by 16 and more there, so that only the largest one weighs anything in 32 bits, and by any c that is large enough:
 // then c is a power of two with 2^31 <= |c r| < 2^32, c r is exact, and other scores are 2^7 and more away.
-// Biased scores are in the exponent's units already: c is 1 (far ones again a power of two).
+// References in the exponent's units have a factor of 1 (far ones again a power of two).
 __device__ __forceinline__ float score_factor(float r, float scale_log2) {
   if (fabsf(r * scale_log2) < 268435456.f) return scale_log2;
   const uint32_t exponent = (__float_as_uint(r) >> 23) & 255u;
@@ -177,9 +177,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                   const __grid_constant__ PrefillPlan plan) {
   using C = GCfg<D, kFp8>;
   constexpr int kStages = C::kStages;
-  constexpr bool kZ = kShape != kShapeNone;        // scores are shaped before the softmax
   constexpr bool kCap = (kShape & kShapeCap) != 0, kBias = (kShape & kShapeBias) != 0;
   constexpr bool kFixed = kShape == kShapeCap;     // ... and lie within bounds: the reference is fixed
+  // References in the exponent's units: of scores whose factor is not the same for all keys (a bias, e4m3's page scales).
+  constexpr bool kExp = kBias || (kFp8 && !kFixed);
   constexpr bool kDown = kBias;                    // a bias has the scores rise from tile to tile: the last tiles come first
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -852,7 +853,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     const int w = warp >> 2;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t my_s = tmem + 128 * w + lane_base, my_o = tmem + kGTmemO + 128 * w + lane_base;
-    const float scale_log2 = kZ ? 1.f : plan.scale_log2;
+    const float scale_log2 = kExp || kFixed ? 1.f : plan.scale_log2;
     const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
     const float neg_inf = -INFINITY;
     // this thread's row of a unit: query token row_token (from the half's first of this CTA), head row_head of the group
@@ -923,24 +924,28 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           auto two = [&](int e) { return f32x2(sv[2 * e], sv[2 * e + 1]); };
           uint32_t pk[32];
           float part = 0.f;
-          [[maybe_unused]] const float2* scales = nullptr;  // of the run's four pages
+          [[maybe_unused]] float2 page_scale[4];  // (e4m3) of keys and values of the run's four pages
           if constexpr (kFp8) {
             const int pt = pair_t + step * j + own;
             if (k == 0) {
               if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(scale_full + 8 * (pt % kGScaleSlots), (pt / kGScaleSlots) & 1));
               if (!ok) return;
             }
-            scales = reinterpret_cast<const float2*>(scales_sh) + (pt % kGScaleSlots) * 8 + 2 * k;
+            const float2* scales = reinterpret_cast<const float2*>(scales_sh) + (pt % kGScaleSlots) * 8 + 2 * k;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float s0, s1;
-              f32x2_split(mul_f32x2(two(e), both(scales[(e >> 4) * 4 + ((e >> 3) & 1)].x)), s0, s1);
-              sv[2 * e] = __float_as_uint(s0);
-              sv[2 * e + 1] = __float_as_uint(s1);
+            for (int g = 0; g < 4; ++g) page_scale[g] = scales[(g >> 1) * 4 + (g & 1)];
+            if constexpr (kShape != kShapeNone) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                float s0, s1;
+                f32x2_split(mul_f32x2(two(e), both(page_scale[e >> 3].x)), s0, s1);
+                sv[2 * e] = __float_as_uint(s0);
+                sv[2 * e + 1] = __float_as_uint(s1);
+              }
             }
           }
           auto pack = [&](int e, float w0, float w1) {  // (values' page scales go with the weights)
-            if constexpr (kFp8) f32x2_split(mul_f32x2(f32x2(__float_as_uint(w0), __float_as_uint(w1)), both(scales[(e >> 4) * 4 + ((e >> 3) & 1)].y)), w0, w1);
+            if constexpr (kFp8) f32x2_split(mul_f32x2(f32x2(__float_as_uint(w0), __float_as_uint(w1)), both(page_scale[e >> 3].y)), w0, w1);
             return pack2<false>(w0, w1);
           };
           if (kMasked && __all_sync(0xffffffffu, hi <= first_lo || lo >= first_hi + 64)) {  // no row of the warp sees any of these
@@ -949,9 +954,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           } else {
             if constexpr (kCap) {
               // The hyperbolic tangent of the cap goes by the row's largest product among the 64: small ones by a polynomial
-              // (|y| <= 1/2: degree 5; |y| <= 1: degree 9), of the form whose largest error is least (2^-17.5 and 2^-18.5, of
+              // (|y| <= 1/2: degree 5; |y| <= 5/4: degree 11), of the form whose largest error is least (2^-17.5 and 2^-18.7, of
               // 1), others, and infinities and NaN, by exponential and reciprocal: three results of the special-function unit a
-              // score with the weight's. Where the reference is fixed, the weights are taken right behind it.
+              // score with the weight's. A warp takes one of the polynomials, the longer one if any of its rows asks for it.
+              // Where the reference is fixed, the weights are taken right behind it.
               if (kMasked) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e) sv[e] = hidden(e) ? 0u : sv[e];
@@ -981,7 +987,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                   }
                 }
               };
-              if (!kMasked && far <= plan.limit[0]) {
+              const bool longer = kMasked || __any_sync(0xffffffffu, far > plan.limit[0] && far <= plan.limit[1] && hi > lo);
+              if (!longer && far <= plan.limit[0]) {
                 capped([&](uint64_t x) {
                   const uint64_t t2 = mul_f32x2(x, x);
                   const uint64_t y = fma_f32x2(t2, fma_f32x2(t2, plan.poly5[2], plan.poly5[1]), plan.poly5[0]);
@@ -990,10 +997,11 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               } else if (far <= plan.limit[1]) {
                 capped([&](uint64_t x) {
                   const uint64_t t2 = mul_f32x2(x, x);
-                  uint64_t y = fma_f32x2(t2, plan.poly9[4], plan.poly9[3]);
-                  y = fma_f32x2(t2, y, plan.poly9[2]);
-                  y = fma_f32x2(t2, y, plan.poly9[1]);
-                  y = fma_f32x2(t2, y, plan.poly9[0]);
+                  uint64_t y = fma_f32x2(t2, plan.poly11[5], plan.poly11[4]);
+                  y = fma_f32x2(t2, y, plan.poly11[3]);
+                  y = fma_f32x2(t2, y, plan.poly11[2]);
+                  y = fma_f32x2(t2, y, plan.poly11[1]);
+                  y = fma_f32x2(t2, y, plan.poly11[0]);
                   return kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y);
                 });
               } else {
@@ -1011,23 +1019,25 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               }
             }
             // What the weights' exponents are made of: of scores that are not biased x = c s - c r; of biased ones
-            // x = mul s + (slope (j - p) - r), a constant for the first of 16 keys and slope times 0 .. 15 (keys behind the token
-            // itself, of a prefix: less twice the bias).
+            // x = mul s + (slope (j - p) - r), a constant for the first of 16 keys and slope times 0 .. 15; e4m3's that are not
+            // shaped with the page's scale.
             const auto exponent = [&](int e, float minus_ref) {
               if constexpr (kBias) {
                 const int g = e >> 3, i = e & 7;
                 // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
-                const float base = fmaf(slope, static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g), minus_ref);
-                const uint64_t bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(base));
+                const float distance = static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g);
+                const uint64_t bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(fmaf(slope, distance, minus_ref)));
                 return kCap ? add_f32x2(two(e), bias2) : fma_f32x2(two(e), both(p.score.mul), bias2);
+              } else if constexpr (kExp) {
+                return fma_f32x2(two(e), both(p.score.mul * page_scale[e >> 3].x), both(minus_ref));
               } else {
                 return fma_f32x2(two(e), both(c_ref), both(minus_ref));
               }
             };
             if constexpr (kBias) {
-              if (kMasked && p.prefix_lens != nullptr) {
+              if (kMasked && p.prefix_lens != nullptr) {  // keys behind the token itself: their bias has the other sign
                 const int own_lo = -key0_pos - first_lo, own_hi = -key0_pos - first_hi;
-                const float twice = kCap ? -2.f * slope : p.score.mul != 0.f ? -2.f * slope / p.score.mul : 0.f;
+                const float twice = kCap ? -2.f * slope : -2.f * slope / p.score.mul;
 #pragma unroll
                 for (int e = 0; e < 64; ++e) {
                   const int behind = e - (e < 32 ? own_lo : own_hi);
@@ -1036,14 +1046,14 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               }
             }
             if constexpr (!kFixed) {
-              if (kMasked && !kBias) {
+              if (kMasked && !kExp) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e)
                   if (hidden(e)) sv[e] = 0xff800000u;  // -inf
               }
               const auto visible_exponent = [&](int e, float minus_ref) {
                 uint64_t x = exponent(e, minus_ref);
-                if (kMasked && kBias) {
+                if (kMasked && kExp) {
                   float x0, x1;
                   f32x2_split(x, x0, x1);
                   x = f32x2(hidden(2 * e) ? 0xff800000u : __float_as_uint(x0), hidden(2 * e + 1) ? 0xff800000u : __float_as_uint(x1));
@@ -1051,31 +1061,31 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 return x;
               };
               // The first reference, where there is none yet: the maximum of these 64 scores.
-              if (kBias ? __any_sync(0xffffffffu, m_ref == kGNoMax) : (k == 0 && j == 0)) {
+              if (kExp ? __any_sync(0xffffffffu, m_ref == kGNoMax) : (k == 0 && j == 0)) {
                 float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                   float z0, z1;
-                  f32x2_split(kBias ? visible_exponent(e, 0.f) : two(e), z0, z1);
+                  f32x2_split(kExp ? visible_exponent(e, 0.f) : two(e), z0, z1);
                   mx[e & 1] = max3(mx[e & 1], z0, z1);
                 }
                 const float first = fmaxf(mx[0], mx[1]);
-                if (kBias) m_ref = m_ref == kGNoMax && first > neg_inf ? first : m_ref;
+                if (kExp) m_ref = m_ref == kGNoMax && first > neg_inf ? first : m_ref;
                 else m_ref = fmaxf(m_ref, first);
-                if (!kBias) c_ref = score_factor(m_ref, scale_log2);
+                if (!kExp) c_ref = score_factor(m_ref, scale_log2);
               }
               // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
               // reference by so much that the reference is raised and the weights are taken again.
-              float top;  // of the scores; of biased ones, of the exponents
+              float top;  // of the scores, or of the exponents
               while (true) {
-                const float minus_ref = kBias ? -m_ref : -__fmul_rn(m_ref, c_ref);
+                const float minus_ref = kExp ? -m_ref : -__fmul_rn(m_ref, c_ref);
                 uint64_t sum2[2] = {0ull, 0ull};
                 float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                   const uint64_t x = visible_exponent(e, minus_ref);
                   float w0, w1;
-                  f32x2_split(kBias ? x : two(e), w0, w1);
+                  f32x2_split(kExp ? x : two(e), w0, w1);
                   mx[e & 1] = max3_nan(mx[e & 1], w0, w1);
                   if (!kMasked && e % kGPolyOf == kGPolyOf - 1) {  // (weights of hidden keys are exactly zero, the polynomial's are not)
                     exp2_two(x, w0, w1);
@@ -1092,12 +1102,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 part = s0 + s1;
                 top = max3_nan(mx[0], mx[0], mx[1]);
                 if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
-                const bool raise = kBias ? top > kGRescale : top * c_ref > m_ref * c_ref + kGRescale;
+                const bool raise = kExp ? top > kGRescale : top * c_ref > m_ref * c_ref + kGRescale;
                 if (!__any_sync(0xffffffffu, raise)) break;
                 // (only the rows that ask for it: a row's rounding does not depend on its neighbours' scores)
-                const float m_new = !raise ? m_ref : kBias ? m_ref + top : top;
+                const float m_new = !raise ? m_ref : kExp ? m_ref + top : top;
                 float a;
-                if (kBias) {
+                if (kExp) {
                   a = raise ? ex2(m_ref - m_new) : 1.f;
                 } else {
                   const float c_new = score_factor(m_new, scale_log2);

@@ -393,6 +393,13 @@ def test_prefill_layouts():
     run_prefill([200, 300], [0, 100], 8, 2, 128, seed=5, softcap=2.0, scale=3.0)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("kw", [dict(scale=0.0), dict(scale=1e-30), dict(scale=-0.1), dict(softcap=4.0), dict(scale=0.0, softcap=4.0)])
+def test_prefill_bias_within_a_prefix(fp8, kw):
+    """Keys behind the token itself, by their distance, whatever the products weigh; slopes of either sign."""
+    run_prefill([150, 40], [30, 200], 4, 2, 128, seed=9, fp8=fp8, prefix=[170, 240], slopes=[0.3, 0.0, -0.02, 0.05], **kw)
+
+
 def test_prefill_many_small_and_few_long():
     g = np.random.default_rng(5)
     run_prefill(list(g.integers(0, 40, size=300)), list(g.integers(0, 100, size=300)), 4, 2, 64, seed=6, softcap=10.0)
