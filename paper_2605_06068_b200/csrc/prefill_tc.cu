@@ -125,8 +125,10 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   const int64_t most = std::min(places, static_cast<int64_t>(p.batch) * q_blocks);
   const int listed = most <= kGMaxList ? 1 : 0;
   int64_t pairs = std::min(most * heads, static_cast<int64_t>(all_pairs));
-  // Blocks are cut along the keys where that gives each at least two pairs.
-  const int cut = listed && p.workspace != nullptr && 2 * most * heads <= std::min(all_pairs, kPreMaxPairs) ? 1 : 0;
+  // Blocks are cut along the keys where that gives each at least two pairs and the table has room for many keys: the merge is a
+  // launch of its own.
+  const int cut = listed && p.workspace != nullptr && 2 * most * heads <= std::min(all_pairs, kPreMaxPairs) &&
+                          static_cast<int64_t>(p.block_table_stride) * kPageSize >= kPreCutKeys ? 1 : 0;
   if (cut) pairs = std::min(all_pairs, kPreMaxPairs);
   // Scores that are only capped have a fixed reference, if the cap allows it; otherwise the bias's form takes them, with slopes of
   // 0, and so it does scores that are not shaped if their factor is not above 0 (they are scaled behind the maximum).

@@ -44,6 +44,7 @@ struct PrefillRecord {
 };
 constexpr int kPreMaxPairs = 74;       // a device with more SMs uses this many where blocks are cut
 constexpr int kPreRows = 512;
+constexpr int kPreCutKeys = 2048;      // keys that the block table has room for, below which nothing is cut
 __host__ __device__ constexpr int64_t prefill_part_bytes(int head_dim) { return static_cast<int64_t>(kPreRows) * head_dim * 4; }
 __host__ __device__ constexpr int64_t prefill_sums_at(int head_dim) { return kPreMaxPairs * prefill_part_bytes(head_dim); }
 __host__ __device__ constexpr int64_t prefill_records_at(int head_dim) { return prefill_sums_at(head_dim) + kPreMaxPairs * kPreRows * 8; }
@@ -54,10 +55,10 @@ constexpr int kGKeys = 128;  // keys per tile
 constexpr int kGQLine = 128 * 128, kGKLine = 64 * 128;
 constexpr int kGSoftWarps = 8, kGProducer = 8, kGMma = 9, kGRelay = 11, kGConvert = 12;
 constexpr int kGScaleSlots = 8;  // tiles whose page scales are kept (e4m3): more than both rings hold together
-constexpr int kGBookBytes = 6 * 1024;
+constexpr int kGBookBytes = 9 * 1024;
 constexpr uint32_t kGTmemCols = 512, kGTmemO = 256;
 constexpr int kGUnitSlots = 4;   // units the producer may be ahead
-constexpr int kGMaxList = 128;   // row blocks that are sorted by their work
+constexpr int kGMaxList = 256;   // row blocks that are sorted by their work
 constexpr float kGNoMax = -FLT_MAX;
 // A row's reference is raised once a score passes it by 2^32: weights and their sums are floating-point numbers of 8 exponent
 // bits, whose precision does not depend on their size, and 32 leaves values up to 2^64 room. With 2^8 (scores of +-15: a warp
@@ -189,13 +190,14 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   uint32_t* list = work + kGMaxList;                                // [kGMaxList] sequence and block, most work first
   GUnit* units = reinterpret_cast<GUnit*>(list + kGMaxList);        // [kGUnitSlots]
   uint32_t* scan = reinterpret_cast<uint32_t*>(units + kGUnitSlots);  // [4] by warp
-  uint32_t* tmem_slot = scan + 5;
+  uint32_t* tmem_slot = scan + kGMaxList / 32 + 1;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   uint32_t* target_sh = reinterpret_cast<uint32_t*>(cta_err + 1);   // tiles of a part
   float* merge_sh = reinterpret_cast<float*>(target_sh + 1);        // [128][2]
   float* scales_sh = merge_sh + 256;                                // (e4m3) [kGScaleSlots][8 pages][K, V]
   int4* spans = reinterpret_cast<int4*>(reinterpret_cast<uint8_t*>(bars) + kGBookBytes - kGMaxList * 16);  // listed sequences' q0, nq, L
-  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + 8 * 4 + 1024 + (kFp8 ? kGScaleSlots * 64 : 0) + kGMaxList * 16 <= kGBookBytes, "shared memory");
+  static_assert(kGMaxList == 256 && kGMaxList <= (kGSoftWarps + 4) * 32, "sequence numbers of 8 bits, a thread each");
+  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + (kGMaxList / 32 + 4) * 4 + 1024 + (kFp8 ? kGScaleSlots * 64 : 0) + kGMaxList * 16 <= kGBookBytes, "shared memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1;  // in the pair
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
@@ -306,18 +308,22 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     }
     // ... unless there is a pair of CTAs for each head of each block: half as many units are no gain then
     by_two = !plan.cut && static_cast<int64_t>(n_blocks) * heads > pairs;
-    for (int k = 0; k < my_blocks && before + k < kGMaxList; ++k) {
+    for (int k = 0; k < my_blocks && before + k < kGMaxList; ++k)
+      list[before + k] = tid | (k << 8) | (mine.nq - k * block_rows <= half_rows ? kGSmallBlock : 0u);
+    __syncthreads();
+    if (tid < n_blocks) {
+      my_entry = list[tid];
+      const int4 span = spans[my_entry & 255];
+      const int row0 = static_cast<int>((my_entry & (kGSmallBlock - 1)) >> 8) * block_rows;
       int lo, hi;
-      key_range(k * block_rows, min((k + 1) * block_rows, mine.nq) - 1, mine.nq, mine.L, my_prefix, lo, hi);
-      if (p.first_keys != nullptr) lo = max(lo, p.first_keys[mine.q0 + k * block_rows]);
-      work[before + k] = hi > lo ? (hi + kGKeys - 1) / kGKeys - lo / kGKeys : 0;
-      list[before + k] = tid | (k << 7) | (mine.nq - k * block_rows <= half_rows ? kGSmallBlock : 0u);
+      key_range(row0, min(row0 + block_rows, span.y) - 1, span.y, span.z, span.w, lo, hi);
+      if (p.first_keys != nullptr) lo = max(lo, p.first_keys[span.x + row0]);
+      my_work = hi > lo ? (hi + kGKeys - 1) / kGKeys - lo / kGKeys : 0;
+      work[tid] = my_work;
     }
     __syncthreads();
     int place = 0;
     if (tid < n_blocks) {
-      my_work = work[tid];
-      my_entry = list[tid];
       for (int i = 0; i < n_blocks; i += 4) {  // (behind the last: anything, which does not count)
         const uint4 v = *reinterpret_cast<const uint4*>(work + i);
         const uint32_t of[4] = {v.x, v.y, v.z, v.w};
@@ -359,8 +365,11 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     uint32_t units_before = units - my_units;
     for (int i = 0; i < kGMaxList / 32; ++i) units_before += i < warp ? scan[i] : 0;
     if (tid < n_blocks) work[tid] = units_before;
-    if (tid == 0) scan[4] = scan[0] + scan[1] + scan[2] + scan[3];
-    static_assert(kGMaxList == 128, "four warps' sums");
+    if (tid == 0) {
+      uint32_t all = 0;
+      for (int i = 0; i < kGMaxList / 32; ++i) all += scan[i];
+      scan[kGMaxList / 32] = all;
+    }
   }
   __syncthreads();
   cluster_sync();
@@ -507,7 +516,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       const uint32_t u_q = uniform(q_sm), u_k = uniform(k_sm), u_v = uniform(v_sm);
       const uint32_t to_q = uniform(in_cta(bar_q, 0));
       const int64_t n_units = !plan.listed ? plan.slots * heads
-                              : n_blocks == 0 ? 0 : static_cast<int64_t>(scan[4]);
+                              : n_blocks == 0 ? 0 : static_cast<int64_t>(scan[kGMaxList / 32]);
       int64_t round = 0;
       // b: the unit's sequence. part of parts: of the tiles.
       int b_now = 0, lo_now = 0, hi_now = 0;  // the unit's sequence and keys
@@ -567,7 +576,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
             const int in_entry = at - static_cast<int>(work[entry]);
             const int parts = plan.cut ? units / heads : 1;
             const int h = in_entry / parts;
-            make_unit(un, (e & (kGSmallBlock - 1)) >> 7, by_two && (e & kGSmallBlock) ? 2 * h : h, e & 127, spans[e & 127], in_entry % parts, parts, at);
+            make_unit(un, (e & (kGSmallBlock - 1)) >> 8, by_two && (e & kGSmallBlock) ? 2 * h : h, e & 255, spans[e & 255], in_entry % parts, parts, at);
             if (plan.cut && in_entry % parts == 0 && parts > 1) my_parts = parts;
             return true;
           }
