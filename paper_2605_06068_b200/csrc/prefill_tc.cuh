@@ -156,6 +156,7 @@ struct GUnit {
   __device__ int key_tile(int w, int j) const { return dual == kSplitKeys && w ? n0 + j : j; }
   __device__ int skipped(int w, bool down) const { return dual || !down ? 0 : tiles() - (w ? n1 : n0); }
 };
+constexpr int kGBuckets = 64;
 constexpr uint32_t kGSmallBlock = 1u << 30;  // (in a list entry) fits one half
 __device__ __forceinline__ int units_of(uint32_t entry, int heads, bool by_two) {
   return by_two && (entry & kGSmallBlock) ? (heads + 1) / 2 : heads;
@@ -193,11 +194,15 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   uint32_t* tmem_slot = scan + kGMaxList / 32 + 1;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   uint32_t* target_sh = reinterpret_cast<uint32_t*>(cta_err + 1);   // tiles of a part
-  float* merge_sh = reinterpret_cast<float*>(target_sh + 1);        // [128][2]
+  uint32_t* most_sh = target_sh + 1;                                // tiles of the block that has most
+  float* merge_sh = reinterpret_cast<float*>(most_sh + 2);          // [128][2]
+  static_assert(sizeof(GUnit) * kGUnitSlots % 8 == 0 && (kGMaxList / 32 + 1 + 5) % 2 == 0, "pairs of floats on 8 bytes");
   float* scales_sh = merge_sh + 256;                                // (e4m3) [kGScaleSlots][8 pages][K, V]
   int4* spans = reinterpret_cast<int4*>(reinterpret_cast<uint8_t*>(bars) + kGBookBytes - kGMaxList * 16);  // listed sequences' q0, nq, L
+  uint32_t* hist = reinterpret_cast<uint32_t*>(smem);               // [kGMaxList / 32][kGBuckets], in Q's place, before its first copy
+  uint32_t* bucket_sh = hist + kGMaxList / 32 * kGBuckets;          // [kGBuckets]
   static_assert(kGMaxList == 256 && kGMaxList <= (kGSoftWarps + 4) * 32, "sequence numbers of 8 bits, a thread each");
-  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + (kGMaxList / 32 + 4) * 4 + 1024 + (kFp8 ? kGScaleSlots * 64 : 0) + kGMaxList * 16 <= kGBookBytes, "shared memory");
+  static_assert(C::kBars * 8 + kGUnitSlots * sizeof(GUnit) + 2 * kGMaxList * 4 + (kGMaxList / 32 + 6) * 4 + 1024 + (kFp8 ? kGScaleSlots * 64 : 0) + kGMaxList * 16 <= kGBookBytes, "shared memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = blockIdx.x & 1;  // in the pair
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
@@ -251,6 +256,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     for (int i = 0; i < 4; ++i) mbar_init(bar_merge + 8 * i, 1);
     *cta_err = 0;
     *target_sh = 1u << 30;
+    *most_sh = 0;
     fence_mbar_init();
     fence_proxy_async();
   }
@@ -308,31 +314,60 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     }
     // ... unless there is a pair of CTAs for each head of each block: half as many units are no gain then
     by_two = !plan.cut && static_cast<int64_t>(n_blocks) * heads > pairs;
-    for (int k = 0; k < my_blocks && before + k < kGMaxList; ++k)
-      list[before + k] = tid | (k << 8) | (mine.nq - k * block_rows <= half_rows ? kGSmallBlock : 0u);
+    if (tid < kGMaxList) work[tid] = before;  // blocks of the sequences before
+    for (int i = tid; i < kGMaxList / 32 * kGBuckets; i += C::kThreads) hist[i] = 0;
     __syncthreads();
     if (tid < n_blocks) {
-      my_entry = list[tid];
-      const int4 span = spans[my_entry & 255];
-      const int row0 = static_cast<int>((my_entry & (kGSmallBlock - 1)) >> 8) * block_rows;
+      int seq = 0;  // the last sequence whose blocks start at or before this one
+#pragma unroll 1
+      for (int at = kGMaxList / 2; at > 0; at >>= 1)
+        if (seq + at < p.batch && work[seq + at] <= static_cast<uint32_t>(tid)) seq += at;
+      const int4 span = spans[seq];
+      const int k = tid - static_cast<int>(work[seq]), row0 = k * block_rows;
       int lo, hi;
       key_range(row0, min(row0 + block_rows, span.y) - 1, span.y, span.z, span.w, lo, hi);
       if (p.first_keys != nullptr) lo = max(lo, p.first_keys[span.x + row0]);
       my_work = hi > lo ? (hi + kGKeys - 1) / kGKeys - lo / kGKeys : 0;
+      my_entry = seq | (k << 8) | (span.y - row0 <= half_rows ? kGSmallBlock : 0u);
+    }
+    // Places by buckets of like work (the finest that hold the largest), by number within a bucket: a warp counts its 32 blocks by
+    // matching, one adds up. (Each block compared with all: 200 of them 4 us.)
+    const uint32_t most = __reduce_max_sync(0xffffffffu, my_work);
+    if (lane == 0) atomicMax(most_sh, most);
+    __syncthreads();  // (work has been read)
+    const int shift = max(32 - __clz(*most_sh) - 6, 0);
+    const uint32_t bucket = tid < n_blocks ? kGBuckets - 1 - (my_work >> shift) : kGBuckets + lane;
+    const uint32_t same = __match_any_sync(0xffffffffu, bucket);
+    const int in_bucket = __popc(same & ((1u << lane) - 1u));
+    if (tid < n_blocks) {
+      if (in_bucket == 0) hist[warp * kGBuckets + bucket] = __popc(same);
       work[tid] = my_work;
     }
     __syncthreads();
-    int place = 0;
-    if (tid < n_blocks) {
-      for (int i = 0; i < n_blocks; i += 4) {  // (behind the last: anything, which does not count)
-        const uint4 v = *reinterpret_cast<const uint4*>(work + i);
-        const uint32_t of[4] = {v.x, v.y, v.z, v.w};
+    if (warp == 0) {  // counts become counts before: of the blocks of earlier warps, and of all earlier buckets
+      uint32_t total[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) place += i + e < n_blocks && (of[e] > my_work || (of[e] == my_work && i + e < tid));
+      for (int h = 0; h < 2; ++h) {
+        uint32_t run = 0;
+#pragma unroll 1
+        for (int i = 0; i < kGMaxList / 32; ++i) {
+          const uint32_t x = hist[i * kGBuckets + lane + 32 * h];
+          hist[i * kGBuckets + lane + 32 * h] = run;
+          run += x;
+        }
+        total[h] = run;
       }
+      uint32_t low = total[0], high = total[1];
+#pragma unroll 1
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t a = __shfl_up_sync(0xffffffffu, low, o), b = __shfl_up_sync(0xffffffffu, high, o);
+        if (lane >= o) low += a, high += b;
+      }
+      bucket_sh[lane] = low - total[0];
+      bucket_sh[lane + 32] = __shfl_sync(0xffffffffu, low, 31) + high - total[1];
     }
     // Few units: the fewest tiles a part with which all parts find a pair each.
-    if (plan.cut && warp == 0) {
+    if (plan.cut && warp == 1) {
       uint32_t below = kGMinTiles - 1, t = work[0];  // (below: too small, or not wanted)
       for (int i = lane; i < n_blocks; i += 32) t = max(t, work[i]);
       t = max(__reduce_max_sync(0xffffffffu, t), static_cast<uint32_t>(kGMinTiles));
@@ -344,8 +379,9 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       }
       if (lane == 0) *target_sh = t;
     }
-    __syncthreads();
+    __syncthreads();  // (and `work` has been read)
     if (tid < n_blocks) {
+      const uint32_t place = bucket_sh[bucket] + hist[warp * kGBuckets + bucket] + in_bucket;
       list[place] = my_entry;
       work[place] = my_work;
     }
@@ -370,6 +406,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       for (int i = 0; i < kGMaxList / 32; ++i) all += scan[i];
       scan[kGMaxList / 32] = all;
     }
+    fence_proxy_async();  // (the counts lay where Q is copied to)
   }
   __syncthreads();
   cluster_sync();
