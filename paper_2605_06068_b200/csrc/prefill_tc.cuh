@@ -274,7 +274,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   auto key_range = [&](int row0, int last, int nq, int L, int prefix, int& lo, int& hi) {
     const int first_pos = L - nq + row0, last_pos = L - nq + last;
     hi = last_pos < 0 ? 0 : max(last_pos + 1, min(prefix, L));
-    lo = p.score.window > 0 ? max(first_pos - p.score.window + 1, 0) : 0;
+    lo = p.score.window > 0 ? max(max(first_pos, 0) - p.score.window + 1, 0) : 0;  // (rows before the sequence see nothing)
   };
   auto prefix_of = [&](int b) { return p.prefix_lens != nullptr ? p.prefix_lens[b] : 0; };
 

@@ -418,6 +418,9 @@ def test_prefill_more_query_tokens_than_keys():
                                               prefix_lens=None if prefix is None else ints(prefix))
             U.check(out, *U.reference(c, q, new, 0.1, prefix=prefix))
             assert (out[:30] == 0).all() and (out[50:60] == 0).all()
+        for window in (2 ** 31 - 1, 2 ** 31 - 30, 1):
+            out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, c.dev_table, ints([20, 0, 150]), cum(new), 200, 0.1, flags=flags, window=window)
+            U.check(out, *U.reference(c, q, new, 0.1, window=window))
 
 
 def test_prefill_rows_outside_the_sequences():
@@ -477,6 +480,159 @@ def test_prefill_nan_and_infinite_scores():
             assert torch.equal(out[0], before[0]) and torch.equal(out[1:, :50], before[1:, :50])     # (position 150 is not seen by rows before it)
             assert out[1, 50:].isnan().all() and out[3].isfinite().all()
             assert out[2, 50:].isfinite().all() if capped else out[2, 50:].isnan().all()
+
+
+# ---- few rows and many keys: blocks cut along the keys and joined -----------------------------------
+
+@pytest.mark.parametrize("kw", [dict(), dict(softcap=6.0), dict(slopes=[0.01, 0.2, 0.0, 0.05]), dict(softcap=30.0, slopes=[0.003] * 4, window=1500),
+                                dict(prefix=[2800, 100], window=900), dict(softcap=80.0)])
+@pytest.mark.parametrize("D,fp8", [(128, False), (128, True), (64, False)])
+def test_prefill_cut_along_the_keys(kw, D, fp8):
+    run_prefill([70, 3], [3000, 2600], 4, 1, D, seed=31, fp8=fp8, **kw)
+
+
+def test_prefill_cut_with_documents():
+    """Rows that see keys of some parts only, or of none."""
+    first = [3000 - 40 * i for i in range(60)] + [2 ** 31 - 1, 2500] + [0] * 8
+    run_prefill([70], [3000], 8, 2, 128, seed=32, first=first)
+    run_prefill([70], [3000], 8, 2, 128, seed=33, first=first, softcap=9.0, fp8=True)
+
+
+def test_prefill_cut_bad_pages_and_nan():
+    c = U.Cache([3000, 2900], 1, 128, seed=1)
+    new = [40, 30]
+    q = randn(2, 70, 8, 128).abs().cuda()
+    call = lambda **k: pda.paged_prefill_attention(q, c.k_cache, c.v_cache, c.dev_table, ints([3000, 2900]), cum(new), 40, 0.1, **k)
+    good = call()
+    U.check(good, *U.reference(c, q.cpu(), new, 0.1))
+    status = ints([0])
+    c.dev_table[0, 20] = -7
+    out = call(status=status)
+    assert int(status.item()) == 1 and (out[:40] == 0).all() and torch.equal(out[40:], good[40:])
+    c.dev_table[0, 20] = int(c.table[0, 20])
+    row = int(c.table[1, 2880 // 16]), 0, 0                          # token 2880 of the second sequence: seen from row 50 on
+    keep = c.k_cache[row].clone()
+    for value in (float("nan"), float("inf")):
+        c.k_cache[row] = value
+        out = call()
+        assert torch.equal(out[:50], good[:50]) and out[50:].isnan().all()
+        assert call(softcap=5.0)[50:].isnan().all() == (value != float("inf"))
+    c.k_cache[row] = keep
+    assert torch.equal(call(), good)
+
+
+def test_prefill_workspaces():
+    """A workspace that holds anything, none at all, and a call that is not cut behind one that is."""
+    c = U.Cache([3000], 2, 128, seed=1)
+    q = randn(2, 50, 8, 128).cuda()
+    args = q, c.k_cache, c.v_cache, c.dev_table, ints([3000]), ints([0, 50]), 50, 0.1
+    ws = pda.prefill_workspace(8, 128)
+    ws.fill_(0xFF)
+    a = pda.paged_prefill_attention(*args, workspace=ws)
+    ws.fill_(0x7F)
+    b = pda.paged_prefill_attention(*args, workspace=ws)
+    assert torch.equal(a, b)
+    ref, tol = U.reference(c, q.cpu(), [50], 0.1)
+    U.check(a, ref, tol)
+    out = torch.empty_like(q)
+    desc = pda._paged_caches(c.k_cache, c.v_cache, None, None, 128)
+    rc = pda.lib().paged_prefill_attention(q.data_ptr(), 1024, 128, c.k_cache.data_ptr(), c.v_cache.data_ptr(), desc, None, None,
+                                           c.dev_table.data_ptr(), c.dev_table.shape[1], args[4].data_ptr(), args[5].data_ptr(), 1, 8, 50, 50,
+                                           pda.ScoreDesc(0.1, 0.0, None, 0), None, None, out.data_ptr(), 1024, 128, None, 0, 0, None,
+                                           torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == 0
+    U.check(out, ref, tol)
+
+
+# ---- sizes at the ends ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("Hq,Hkv", [(128, 1), (100, 1), (130, 1), (66, 2), (12, 4)])
+def test_prefill_groups(Hq, Hkv):
+    """Groups that fill a tile's rows alone, that leave rows over, and one above what the tensor-core kernel takes."""
+    run_prefill([9, 1, 20], [0, 50, 130], Hq, Hkv, 64, seed=Hq, softcap=8.0)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(slopes=[0.1, 0.01]), dict(softcap=5.0)])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_prefill_many_blocks(kw, fp8):
+    """More row blocks than are listed, and just fewer, of sequences of very unequal lengths; empty ones among them."""
+    g = np.random.default_rng(7)
+    for n, hi in ((290, 30), (255, 5), (120, 2)):
+        new = [int(x) for x in g.integers(0, hi, size=n)]
+        new[3], new[7] = 600, 0
+        run_prefill(new, [int(x) for x in g.integers(0, 60, size=n)], 2, 1, 128, seed=n, fp8=fp8, **kw)
+
+
+def test_empty_calls_and_lengths_below_zero():
+    c = U.Cache([30], 2, 128, seed=1)
+    e = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+    cs = table_of(8, 128).cuda()
+    assert pda.rope_kv_append(e(0, 4, 128), e(0, 2, 128), e(0, 2, 128), ints([]), cs, c.k_cache, c.v_cache, ints([])).shape == (0, 4, 128)
+    assert pda.paged_prefill_attention(e(0, 4, 128), c.k_cache, c.v_cache, c.dev_table, ints([30]), ints([0, 0]), 0, 0.1).shape == (0, 4, 128)
+    none = torch.empty((0, 3), dtype=torch.int32, device="cuda")
+    assert pda.paged_biased_decode_attention(e(0, 4, 128), c.k_cache, c.v_cache, none, ints([]), 0.1).shape == (0, 4, 128)
+    q = randn(1, 5, 4, 128).cuda()
+    for flags in (0, GENERIC):
+        out = pda.paged_prefill_attention(q, c.k_cache, c.v_cache, c.dev_table, ints([-4]), ints([0, 5]), 5, 0.1, prefix_lens=ints([9]), flags=flags)
+        assert (out == 0).all()
+        assert (pda.paged_biased_decode_attention(q[:1], c.k_cache, c.v_cache, c.dev_table, ints([-4]), 0.1, flags=flags) == 0).all()
+
+
+def test_decode_cut_finer_than_asked_for():
+    """Sequences that are shorter than the partial buffers allow for are cut into as many chunks, of 2048 tokens at least."""
+    for kw in (dict(), dict(fp8=True, softcap=9.0, slopes=[0.001 * h for h in range(4)])):
+        run_decode([9000, 5000, 300, 0, 4097, 12288], 4, 1, 128, seed=40, chunk=4096, **kw)
+    run_decode([9000, 2500], 10, 1, 128, seed=41, chunk=6000 // 16 * 16, window=3000)
+
+
+def test_offsets_beyond_32_bits():
+    """Caches of more than 2^31 elements: the pages in use are the last ones."""
+    Hkv, D, n = 8, 128, 140000
+    caches = [torch.empty((n, Hkv, 16, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    assert caches[0].numel() > 2 ** 31
+    L = 200
+    pages = list(range(n - 13, n))
+    table = ints([pages])
+    slots = ints([pages[j // 16] * 16 + j % 16 for j in range(L)])
+    x = randn(3, L, 16 + 2 * Hkv, D).cuda()
+    q = pda.rope_kv_append(x[:, :16], x[:, 16:16 + Hkv], x[:, 16 + Hkv:], None, None, *caches, slots)
+    assert torch.equal(q, x[:, :16]) and torch.equal(caches[1][pages[3], :, 5], x[53, 16 + Hkv:])
+    c = U.Cache.__new__(U.Cache)
+    c.lens, c.fp8, c.byte = [L], False, 0.0
+    c.k, c.v = [x[:, 16:16 + Hkv].cpu().double()], [x[:, 16 + Hkv:].cpu().double()]
+    out = pda.paged_prefill_attention(q, *caches, table, ints([L]), ints([0, L]), L, 0.1, softcap=9.0)
+    U.check(out, *U.reference(c, q.cpu(), [L], 0.1, 9.0))
+    one = pda.paged_biased_decode_attention(q[-1:].contiguous(), *caches, table, ints([L]), 0.1, softcap=9.0)
+    U.check(one, *U.reference(c, q[-1:].cpu(), [1], 0.1, 9.0, decode=True))
+
+
+def test_calls_on_a_given_stream():
+    c = U.Cache([500], 2, 128, seed=1)
+    q = randn(2, 100, 8, 128).cuda()
+    args = q, c.k_cache, c.v_cache, c.dev_table, ints([500]), ints([0, 100]), 100, 0.1
+    want = pda.paged_prefill_attention(*args, softcap=7.0)
+    dec = pda.paged_biased_decode_attention(q[-1:].contiguous(), *args[1:5], 0.1, softcap=7.0)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    a = pda.paged_prefill_attention(*args, softcap=7.0, stream=side)      # (output and workspace belong to that stream)
+    b = pda.paged_biased_decode_attention(q[-1:].contiguous(), *args[1:5], 0.1, softcap=7.0, stream=side)
+    side.synchronize()
+    assert torch.equal(a, want) and torch.equal(b, dec)
+
+
+def test_results_do_not_depend_on_timing_or_on_other_sequences():
+    """The same bits call by call; and a sequence's bits whatever its neighbours' values are."""
+    lens, new = [700, 333, 90], [200, 333, 7]
+    for kw in (dict(), dict(softcap=10.0), dict(slopes=torch.tensor([0.02 * h for h in range(8)], device="cuda"))):
+        c = U.Cache(lens, 2, 128, seed=1)
+        q = randn(2, sum(new), 8, 128, scale=3.0).cuda()
+        call = lambda: pda.paged_prefill_attention(q, c.k_cache, c.v_cache, c.dev_table, ints(lens), cum(new), 333, 0.1, **kw)
+        a = call()
+        assert all(torch.equal(a, call()) for _ in range(5))
+        q[:200] *= 100
+        b = call()
+        assert torch.equal(a[200:], b[200:]) and not torch.equal(a[:200], b[:200])
 
 
 # ---- the operators together ------------------------------------------------------------------------

@@ -1,6 +1,9 @@
 """Host-side refusals of the rotating cache append and of attention with shaped scores: nothing is enqueued, no GPU needed."""
 import ctypes as C
+import os
+import re
 
+import numpy as np
 import pytest
 import torch
 
@@ -150,3 +153,32 @@ def test_append_binding_refusals(kw, text):
     args.update(kw)
     with pytest.raises(ValueError, match=text):
         pda.rope_kv_append(**args)
+
+
+def source(name):
+    return open(os.path.join(os.path.dirname(pda.__file__), "csrc", name)).read()
+
+
+@pytest.mark.parametrize("name,reach,bound", [("c5", 0.5, 2.0 ** -17.4), ("c11", 1.25, 2.0 ** -18.6)])
+def test_polynomials_of_the_cap_are_within_their_bounds(name, reach, bound):
+    """The odd polynomials of the hyperbolic tangent, as they stand in the source, in 64 and in 32 bits (a rounding for each of
+    their steps, of sums below 2)."""
+    text = re.search(r"static const double %s\[\d+\] = \{([^}]*)\}" % name, source("prefill_tc.cu")).group(1)
+    c = [float(x) for x in text.split(",")]
+    x = np.linspace(-reach, reach, 400001)
+    exact = np.tanh(x)
+    assert np.abs(x * np.polyval(c[::-1], x * x) - exact).max() < bound
+    f = x.astype(np.float32)
+    t = f * f
+    y = np.full(f.shape, c[-1], dtype=np.float32)
+    for a in c[-2::-1]:
+        y = y * t + np.float32(a)
+    assert np.abs((f * y).astype(np.float64) - np.tanh(f.astype(np.float64))).max() < bound + (2 * len(c) + 2) * 2.0 ** -24 * reach
+
+
+def test_polynomial_of_the_exponentials_is_within_its_bound():
+    body = source("prefill_tc.cuh").split("void exp2_two", 1)[1].split("\n}", 1)[0]
+    c = [float(x) for x in re.findall(r"both\((0\.\d+)f\)", body)]
+    assert len(c) == 4
+    f = np.linspace(-0.5, 0.5, 200001)
+    assert np.abs(np.polyval(c, f) / np.exp2(f) - 1).max() < 7.6e-5      # (of the 2^-12 that the GPU tests' bounds allow)
