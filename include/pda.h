@@ -682,7 +682,7 @@ int rope_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride,
  * Rows that see nothing (p < 0, lo >= hi) are zero. Rows of out outside all sequences are left as they
  * were, and rows of q outside all sequences may hold anything. Slots that hold no token < L, unused pages
  * and table entries of pages that no token sees may hold anything; the values of all tokens < L in
- * pages that are seen must be finite. A row with a NaN or +inf among the scores it sees is NaN;
+ * pages that are seen must be finite (and on the tensor-core kernel below 2^64 in size). A row with a NaN or +inf among the scores it sees is NaN;
  * one with none above -inf is NaN or zero. L < 0 counts as 0. A sequence whose query range does not
  * lie in the arrays, that has more than max_q query tokens or more than block_table_stride * 16 or
  * 2^30 tokens is zeroed (as far as its rows lie within the array and max_q) with PDA_DEV_BAD_SEQ_LEN; rows for

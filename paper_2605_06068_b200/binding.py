@@ -653,6 +653,20 @@ def latent_prefill_attention(q, k_nope, k_rope, v, cu_q, cu_k, max_q, scale, out
 
 # What the calls below take from shapes and strides alone is checked and worked out once for each layout.
 
+def _one_device(*tensors):
+    """``_same_device`` in fewer steps where all is well."""
+    devices = {t.get_device() for t in tensors if t is not None}
+    return devices.pop() if len(devices) == 1 and min(devices) >= 0 else _same_device(*tensors)
+
+
+def _on_device(dev, call, *args):
+    """The call with the device of its tensors current."""
+    if dev == torch.cuda.current_device():
+        return call(*args)
+    with torch.cuda.device(dev):
+        return call(*args)
+
+
 @functools.lru_cache(maxsize=64)
 def _kv_layout(shape, k_stride, v_shape, v_stride, dtype, v_dtype):
     """Descriptor of two ``[num_pages, Hkv, 16, D]`` caches (not to be written to)."""
@@ -757,13 +771,12 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
                 raise ValueError("freq_axis: expected an axis for each of the rot_dim / 2 frequencies")
     else:
         positions = None
-    dev = _same_device(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_norm, k_norm, out, k_scale, v_scale, status)
-    with _device_call(dev):
-        rc = lib().rope_kv_append(
-            q.data_ptr(), q_token, q_head, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, _dp(positions), pos_stride,
-            axes, axis, _dp(cos_sin), table, rot, interleaved, _dp(q_norm), _dp(k_norm), eps, slot_map.data_ptr(), T, Hq,
-            out.data_ptr(), o_token, o_head, k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale),
-            _dp(status), _raw(stream, dev))
+    dev = _one_device(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_norm, k_norm, out, k_scale, v_scale, status)
+    rc = _on_device(
+        dev, lib().rope_kv_append, q.data_ptr(), q_token, q_head, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, _dp(positions), pos_stride,
+        axes, axis, _dp(cos_sin), table, rot, interleaved, _dp(q_norm), _dp(k_norm), eps, slot_map.data_ptr(), T, Hq,
+        out.data_ptr(), o_token, o_head, k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale),
+        _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "rope_kv_append")
     return out
@@ -816,14 +829,13 @@ def paged_prefill_attention(q, k_cache, v_cache, block_table, seq_lens, cu_q, ma
         workspace = prefill_workspace(Hq, D, device=q.device, stream=stream)
     elif not workspace.is_contiguous():
         raise ValueError("workspace: must be contiguous")
-    dev = _same_device(q, k_cache, v_cache, block_table, seq_lens, cu_q, slopes, prefix_lens, first_keys, out, k_scale, v_scale,
+    dev = _one_device(q, k_cache, v_cache, block_table, seq_lens, cu_q, slopes, prefix_lens, first_keys, out, k_scale, v_scale,
                        workspace, status)
-    with _device_call(dev):
-        rc = lib().paged_prefill_attention(
-            q.data_ptr(), q_token, q_head, k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale),
-            block_table.data_ptr(), stride, seq_lens.data_ptr(), cu_q.data_ptr(), B, Hq, min(int(max_q), Tq), Tq, score,
-            _dp(prefix_lens), _dp(first_keys), out.data_ptr(), o_token, o_head, workspace.data_ptr(), workspace.nbytes, flags,
-            _dp(status), _raw(stream, dev))
+    rc = _on_device(
+        dev, lib().paged_prefill_attention, q.data_ptr(), q_token, q_head, k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale),
+        block_table.data_ptr(), stride, seq_lens.data_ptr(), cu_q.data_ptr(), B, Hq, min(int(max_q), Tq), Tq, score,
+        _dp(prefix_lens), _dp(first_keys), out.data_ptr(), o_token, o_head, workspace.data_ptr(), workspace.nbytes, flags,
+        _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "paged_prefill_attention")
     return out
@@ -862,13 +874,12 @@ def paged_biased_decode_attention(q, k_cache, v_cache, block_table, seq_lens, sc
             if workspace.numel() < workspace_ints(B, desc.num_kv_heads * parts):
                 raise ValueError("workspace: too small")
     score = _score_desc(scale, softcap, slopes, window, Hq)
-    dev = _same_device(q, k_cache, v_cache, block_table, seq_lens, slopes, first_keys, out, part_o, part_lse, workspace, k_scale,
+    dev = _one_device(q, k_cache, v_cache, block_table, seq_lens, slopes, first_keys, out, part_o, part_lse, workspace, k_scale,
                        v_scale, status)
-    with _device_call(dev):
-        rc = lib().paged_biased_decode_attention(
-            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale), block_table.data_ptr(),
-            stride, seq_lens.data_ptr(), B, Hq, score, _dp(first_keys), chunk_tokens, out.data_ptr(), _dp(part_o),
-            _dp(part_lse), mc, _dp(workspace), flags, _dp(status), _raw(stream, dev))
+    rc = _on_device(
+        dev, lib().paged_biased_decode_attention, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), desc, _dp(k_scale), _dp(v_scale), block_table.data_ptr(),
+        stride, seq_lens.data_ptr(), B, Hq, score, _dp(first_keys), chunk_tokens, out.data_ptr(), _dp(part_o),
+        _dp(part_lse), mc, _dp(workspace), flags, _dp(status), _raw(stream, dev))
     if rc:
         _check(rc, "paged_biased_decode_attention")
     return out

@@ -67,8 +67,8 @@ constexpr float kGRescale = 32.f;
 constexpr int kGPolyOf = 4;      // every fourth pair of exponentials by polynomial
 constexpr int kGMinTiles = 4;    // of a part
 // Capped scores that are not biased lie within [-C, C] (ScoreParams): they need no maximum. Their weights are taken relative
-// to a reference fixed at max(C - 60, 0), which keeps them and their sums within 2^-120 .. 2^60 for C <= 90 (a cap up to 62).
-constexpr float kGFixedTop = 60.f, kGFixedCap = 90.f;
+// to a reference fixed at max(C - 30, 0), which keeps them within 2^-120 .. 2^30 for C <= 75 (a cap up to 52).
+constexpr float kGFixedTop = 30.f, kGFixedCap = 75.f;
 
 // How scores are shaped (bits): capped; biased by distance.
 enum : int { kShapeNone = 0, kShapeCap = 1, kShapeBias = 2 };
