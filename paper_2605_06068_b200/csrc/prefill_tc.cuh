@@ -11,6 +11,9 @@
 // the row's maximum passes it by more than 2^32; row sums are kept by the row's thread, of the 32-bit weights.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the pair's first
 // CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are bounded.
+// Measured (B200, 32 query and 8 kv heads of 128): a prompt of 8192 tokens 449 us (1.22 PFLOP/s), capped 517, biased 493, e4m3 573;
+// 24 prompts of 1..700 tokens 100 us; 300 tokens behind 60000 in 72 parts 320 us (860 uncut). Tensor pipe 52 % of active
+// clocks, capped 44 %: the softmax's instructions and the products take turns.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>

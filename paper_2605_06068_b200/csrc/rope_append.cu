@@ -10,6 +10,8 @@
 // e4m3 caches: keys and values go another way, since a row's scale is that of its page's first row. A warp takes one head's
 // keys, or values, of kRows tokens a segment one behind the other; of them the first rows of pages give the others their
 // scale by shuffles, and only a page that begins before the warp's tokens has its first row read once more.
+// Measured: 16411 tokens of 32 + 16 heads with norm 70 us, 5.6 TB/s (0.85 of the copy rate); 5000 tokens of 28 + 8 heads, three
+// axes, e4m3 30 us; 64 tokens 4.3 us, which is the launch and the reads that wait for one another.
 #include "shaped.cuh"
 #include "tcgen05_ptx.cuh"
 #include "tma_ptx.cuh"
