@@ -1067,20 +1067,22 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 part = s0 + s1;
               }
             }
-            // What the weights' exponents are made of: of scores that are not biased x = c s - c r; of biased ones
-            // x = mul s + (slope (j - p) - r), a constant for the first of 16 keys and slope times 0 .. 15; e4m3's that are not
-            // shaped with the page's scale.
-            const auto exponent = [&](int e, float minus_ref) {
+            // Scores that references are taken of. Biased ones and e4m3's are in the exponent's units: mul s + slope (j - p), the slope's
+            // part a constant for the first of 16 keys and slope times 0 .. 15; e4m3's that are not biased with the page's scale. They
+            // are rounded before the reference is taken from them: so a reference is a score itself, none of those it was taken of
+            // passes it, and it is raised once at most for 64 keys. (Taken from the product in the same rounding, scores of 2^30 and
+            // more passed a reference that could not be raised by so little.)
+            const auto score = [&](int e) {
               if constexpr (kBias) {
                 const int g = e >> 3, i = e & 7;
                 // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
                 const float distance = static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g);
-                const uint64_t bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(fmaf(slope, distance, minus_ref)));
+                const uint64_t bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(slope * distance));
                 return kCap ? add_f32x2(two(e), bias2) : fma_f32x2(two(e), both(p.score.mul), bias2);
               } else if constexpr (kExp) {
-                return fma_f32x2(two(e), both(p.score.mul * page_scale[e >> 3].x), both(minus_ref));
+                return mul_f32x2(two(e), both(p.score.mul * page_scale[e >> 3].x));
               } else {
-                return fma_f32x2(two(e), both(c_ref), both(minus_ref));
+                return two(e);
               }
             };
             if constexpr (kBias) {
@@ -1100,14 +1102,14 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 for (int e = 0; e < 64; ++e)
                   if (hidden(e)) sv[e] = 0xff800000u;  // -inf
               }
-              const auto visible_exponent = [&](int e, float minus_ref) {
-                uint64_t x = exponent(e, minus_ref);
+              const auto visible = [&](int e) {
+                uint64_t z = score(e);
                 if (kMasked && kExp) {
-                  float x0, x1;
-                  f32x2_split(x, x0, x1);
-                  x = f32x2(hidden(2 * e) ? 0xff800000u : __float_as_uint(x0), hidden(2 * e + 1) ? 0xff800000u : __float_as_uint(x1));
+                  float z0, z1;
+                  f32x2_split(z, z0, z1);
+                  z = f32x2(hidden(2 * e) ? 0xff800000u : __float_as_uint(z0), hidden(2 * e + 1) ? 0xff800000u : __float_as_uint(z1));
                 }
-                return x;
+                return z;
               };
               // The first reference, where there is none yet: the maximum of these 64 scores.
               if (kExp ? __any_sync(0xffffffffu, m_ref == kGNoMax) : (k == 0 && j == 0)) {
@@ -1115,7 +1117,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                   float z0, z1;
-                  f32x2_split(kExp ? visible_exponent(e, 0.f) : two(e), z0, z1);
+                  f32x2_split(visible(e), z0, z1);
                   mx[e & 1] = max3(mx[e & 1], z0, z1);
                 }
                 const float first = fmaxf(mx[0], mx[1]);
@@ -1125,16 +1127,17 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               }
               // Weights relative to the reference as it stands, the maximum taken along the way: rarely does it pass the
               // reference by so much that the reference is raised and the weights are taken again.
-              float top;  // of the scores, or of the exponents
+              float top;
               while (true) {
                 const float minus_ref = kExp ? -m_ref : -__fmul_rn(m_ref, c_ref);
                 uint64_t sum2[2] = {0ull, 0ull};
                 float mx[2] = {neg_inf, neg_inf};
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
-                  const uint64_t x = visible_exponent(e, minus_ref);
+                  const uint64_t z = visible(e);
+                  const uint64_t x = kExp ? add_f32x2(z, both(minus_ref)) : fma_f32x2(z, both(c_ref), both(minus_ref));
                   float w0, w1;
-                  f32x2_split(kExp ? x : two(e), w0, w1);
+                  f32x2_split(z, w0, w1);
                   mx[e & 1] = max3_nan(mx[e & 1], w0, w1);
                   if (!kMasked && e % kGPolyOf == kGPolyOf - 1) {  // (weights of hidden keys are exactly zero, the polynomial's are not)
                     exp2_two(x, w0, w1);
@@ -1151,10 +1154,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 part = s0 + s1;
                 top = max3_nan(mx[0], mx[0], mx[1]);
                 if (!(top <= 3.4028235e38f)) part = __uint_as_float(0x7fc00000u);  // a NaN or +inf among the scores
-                const bool raise = kExp ? top > kGRescale : top * c_ref > m_ref * c_ref + kGRescale;
+                const bool raise = kExp ? top > m_ref + kGRescale : top * c_ref > m_ref * c_ref + kGRescale;
                 if (!__any_sync(0xffffffffu, raise)) break;
                 // (only the rows that ask for it: a row's rounding does not depend on its neighbours' scores)
-                const float m_new = !raise ? m_ref : kExp ? m_ref + top : top;
+                const float m_new = raise ? top : m_ref;
                 float a;
                 if (kExp) {
                   a = raise ? ex2(m_ref - m_new) : 1.f;

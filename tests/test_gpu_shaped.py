@@ -482,6 +482,79 @@ def test_prefill_nan_and_infinite_scores():
             assert out[2, 50:].isfinite().all() if capped else out[2, 50:].isnan().all()
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(slopes=[0.3, 0.01]), dict(softcap=3.0, slopes=[0.3, 0.01]), dict(slopes=[0.0, 0.0], prefix=[400, 0, 1900])])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("how", ["prompt", "generic", "decode"])
+def test_scores_whose_steps_pass_every_threshold(kw, fp8, how):
+    """Products up to 2^100: one step of such a score's 32-bit form is more than any weight's exponent may be off by. Each is
+    the product of one number of a query and one of a key: 80 keys a sequence have different ones of either sign, the others
+    zero. The numbers that count are so far apart that only the largest has a weight, or the same, and then their weights differ
+    by their biases alone; both whatever the product's rounding."""
+    if how == "decode" and "prefix" in kw:
+        kw = {k: v for k, v in kw.items() if k != "prefix"}
+    lens, new = ([400, 70, 2000], [300, 70, 20]) if how != "decode" else ([400, 70, 2000], [1, 1, 1])
+    D, scale = 128, 0.0883883
+    c = U.Cache(lens, 1, D, seed=71)
+    g = np.random.default_rng(72)
+    k0 = []
+    for L in lens:
+        x = torch.zeros(L, dtype=torch.float64)
+        at = torch.as_tensor(g.permutation(L)[:min(L, 80)])
+        x[at] = torch.as_tensor(np.concatenate([np.arange(8, 16) * 2.0 ** e for e in range(5)] + [-np.arange(8, 16) * 2.0 ** e for e in range(5)])[:len(at)])
+        k0.append(x)                                # (four bits each: 8-bit pages hold them too)
+    rows = torch.zeros(c.k_cache.shape, dtype=torch.bfloat16)
+    values = c.v_cache.cpu().float()
+    for b, L in enumerate(lens):
+        for j in range(L):
+            rows[int(c.table[b, j // 16]), 0, j % 16, 0] = k0[b][j]
+    k_cache, v_cache, scales = rows.cuda(), c.v_cache, {}
+    if fp8:
+        k_cache, v_cache = rows.float().to(U.E4M3).cuda(), torch.where(values.isnan(), 0.0, values).to(U.E4M3).cuda()
+        ones = torch.full((rows.shape[0], 1), 1.0, device="cuda")
+        scales = dict(k_scale=ones * 0.7, v_scale=ones)
+        values = v_cache.cpu().float()
+    T = sum(new)
+    q = torch.zeros((T, 2, D), dtype=torch.bfloat16)
+    powers = np.array([24, 27, 28, 30, 31, 33, 40, 64, 90])
+    if how == "decode" and fp8:                     # (queries are held in fp16 there: the rest is the scale's)
+        scale *= 2.0 ** 40
+        powers = np.minimum(powers - 40, 14)
+    q[:, :, 0] = torch.as_tensor(2.0 ** g.choice(powers, size=(T, 2)) * g.choice([-1.0, 1.0, 1.5, -1.25], size=(T, 2))).to(torch.bfloat16)
+    host = dict(kw, slopes=torch.tensor(kw.get("slopes", [0.0, 0.0]), dtype=torch.float32))
+    dev = dict(kw)
+    if "slopes" in kw:
+        dev["slopes"] = host["slopes"].cuda()
+    if "prefix" in kw:
+        dev["prefix_lens"] = ints(dev.pop("prefix"))
+    status = ints([0])
+    flags = GENERIC if how == "generic" else 0
+    if how == "decode":
+        out = pda.paged_biased_decode_attention(q.cuda(), k_cache, v_cache, c.dev_table, ints(lens), scale, status=status, **dev, **scales)
+    else:
+        out = pda.paged_prefill_attention(q.cuda(), k_cache, v_cache, c.dev_table, ints(lens), cum(new), max(new), scale, status=status, flags=flags, **dev, **scales)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    see = U.visible(lens, new, 0, kw.get("prefix"))
+    at = 0
+    for b, n in enumerate(new):
+        v = torch.stack([values[int(c.table[b, j // 16]), 0, j % 16] for j in range(lens[b])]).double()
+        j, pos = torch.arange(lens[b]), torch.arange(n) + (lens[b] - n)
+        live = (j[None, :] >= see[b][0][:, None]) & (j[None, :] < see[b][1][:, None])
+        for h in range(2):
+            s = q[at:at + n, h, :1].double() * (k0[b] * (0.7 if fp8 else 1.0))[None, :] * scale
+            if kw.get("softcap"):
+                s = kw["softcap"] * torch.tanh(s / kw["softcap"])
+            bias = float(host["slopes"][h]) * (pos[:, None] - j[None, :]).abs()
+            w = torch.softmax(torch.where(live, s - bias, float("-inf")), 1)
+            # 16-bit weights and result; exponents off by 2^-22 of a bias with a weight and 2^-17 of a cap; 32-bit sums
+            off = 2 * ((w * bias).max(1, keepdim=True).values * 2.0 ** -22 * lens[b] + kw.get("softcap", 0.0) * 2.0 ** -17)
+            # decode, 8 bits: weights times the value scale held in fp16, 2^-25 of a value each
+            small = 2.0 ** -25 * (live.double() @ v.abs()) if fp8 and how == "decode" else 0.0
+            tol = (3 * U.EPS + lens[b] * 2.0 ** -24 + 2.0 ** -12 + 2 * off) * (w @ v.abs()) * 1.01 + small
+            U.check(out[at:at + n, h], w @ v, tol, f"sequence {b} head {h}")
+        at += n
+
+
 # ---- few rows and many keys: blocks cut along the keys and joined -----------------------------------
 
 @pytest.mark.parametrize("kw", [dict(), dict(softcap=6.0), dict(slopes=[0.01, 0.2, 0.0, 0.05]), dict(softcap=30.0, slopes=[0.003] * 4, window=1500),
