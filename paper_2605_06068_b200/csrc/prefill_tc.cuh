@@ -11,7 +11,7 @@
 // the row's maximum passes it by more than 2^32; row sums are kept by the row's thread, of the 32-bit weights.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the pair's first
 // CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are bounded.
-// Measured (B200, 32 query and 8 kv heads of 128): a prompt of 8192 tokens 449 us (1.22 PFLOP/s), capped 517, biased 493, e4m3 573;
+// Measured (B200, 32 query and 8 kv heads of 128): a prompt of 8192 tokens 449 us (1.22 PFLOP/s), capped 517, biased 538, e4m3 617;
 // 24 prompts of 1..700 tokens 100 us; 300 tokens behind 60000 in 72 parts 320 us (860 uncut). Tensor pipe 52 % of active
 // clocks, capped 44 %: the softmax's instructions and the products take turns.
 #include <algorithm>
@@ -1071,7 +1071,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
             // part a constant for the first of 16 keys and slope times 0 .. 15; e4m3's that are not biased with the page's scale. They
             // are rounded before the reference is taken from them: so a reference is a score itself, none of those it was taken of
             // passes it, and it is raised once at most for 64 keys. (Taken from the product in the same rounding, scores of 2^30 and
-            // more passed a reference that could not be raised by so little.)
+            // more passed a reference that could not be raised by so little. Costs 7 %: 508 -> 538 us biased, 577 -> 617 e4m3. A pass of its own
+            // for rows with such scores, beside the hot one, gained nothing: 541 and 604, 543 and 613, or, in place, 528 and 664.)
             const auto score = [&](int e) {
               if constexpr (kBias) {
                 const int g = e >> 3, i = e & 7;
