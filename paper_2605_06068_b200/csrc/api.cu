@@ -287,7 +287,7 @@ int paged_prefix_decode_attention(const void* q, const void* k_cache, const void
                                block_table_stride, seq_lens, batch, num_q_heads, chunk_tokens,
                                out, part_o, part_lse, max_chunks, &p))
     return rc;
-  const int prefix_chunks = (prefix_tokens + prefix_chunk_tokens - 1) / prefix_chunk_tokens;
+  const int prefix_chunks = pda::chunk_count(prefix_tokens, prefix_chunk_tokens);
   if (prefix_chunks >= max_chunks) return PDA_ERR_INVALID_ARG;
   if (static_cast<int64_t>(prefix_tokens) > static_cast<int64_t>(block_table_stride) * pda::kPageSize)
     return PDA_ERR_INVALID_ARG;

@@ -32,9 +32,10 @@ __global__ void __launch_bounds__(32) attention_generic_kernel(AttnParams p) {
   const int L = max(p.seq_lens[b], 0);
   int t0 = p.first_token, t1 = L;
   if (split) {
-    t0 = p.first_token + c * p.chunk_tokens;
-    if (t0 >= L) return;  // no such chunk
-    t1 = min(t0 + p.chunk_tokens, L);
+    const int64_t start = chunk_start(p.first_token, c, p.chunk_tokens);
+    if (start >= L) return;  // no such chunk
+    t0 = static_cast<int>(start);
+    t1 = chunk_end(start, p.chunk_tokens, L);
   }
   // window: tokens before L - window are not attended; the unit may end up empty
   if (p.window > 0 && L - p.window > t0) t0 = min(L - p.window, t1);

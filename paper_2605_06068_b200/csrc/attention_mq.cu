@@ -66,9 +66,10 @@ attention_mq_kernel(const __grid_constant__ CUtensorMap k_map,
   const int L = mp.kv_len_fixed > 0 ? mp.kv_len_fixed : max(p.seq_lens[b], 0);
   int t0 = p.first_token, t1 = L;
   if (split) {
-    t0 = p.first_token + c * p.chunk_tokens;
-    if (t0 >= L) return;
-    t1 = min(t0 + p.chunk_tokens, L);
+    const int64_t start = chunk_start(p.first_token, c, p.chunk_tokens);
+    if (start >= L) return;
+    t0 = static_cast<int>(start);
+    t1 = chunk_end(start, p.chunk_tokens, L);
   }
   int err = 0;
   if (static_cast<int64_t>(L) > static_cast<int64_t>(p.block_table_stride) * kPageSize ||

@@ -153,7 +153,7 @@ attention_mq_tc_kernel(const __grid_constant__ CUtensorMap k_map,
   if (ranked && tid < p.batch) len_mine = max(p.seq_lens[tid], 0);
   if (split) {  // an empty chunk leaves before anything is allocated
     const int Lb = mp.kv_len_fixed > 0 ? mp.kv_len_fixed : max(p.seq_lens[b], 0);
-    if (p.first_token + c * p.chunk_tokens >= Lb) return;
+    if (chunk_start(p.first_token, c, p.chunk_tokens) >= Lb) return;
   }
   // once any CTA of this launch has reported a timed-out wait, the rest do not start
   if (status_now == PDA_DEV_TIMEOUT) return;
@@ -228,8 +228,9 @@ attention_mq_tc_kernel(const __grid_constant__ CUtensorMap k_map,
   const int L = mp.kv_len_fixed > 0 ? mp.kv_len_fixed : ranked ? rank_slot[1] : max(p.seq_lens[b], 0);
   int t0 = p.first_token, t1 = L;
   if (split) {
-    t0 = p.first_token + c * p.chunk_tokens;
-    t1 = min(t0 + p.chunk_tokens, L);
+    const int64_t start = chunk_start(p.first_token, c, p.chunk_tokens);  // (below L: see above)
+    t0 = static_cast<int>(start);
+    t1 = chunk_end(start, p.chunk_tokens, L);
   }
   int err = 0;
   if (static_cast<int64_t>(L) > static_cast<int64_t>(p.block_table_stride) * kPageSize ||

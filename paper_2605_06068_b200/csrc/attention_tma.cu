@@ -43,7 +43,7 @@ namespace {
 
 // ---- kernel ------------------------------------------------------------------------------
 
-constexpr int kMinChunk = 2048;    // tokens that a chunk cut finer than asked for has at least (512: 1024-token chunks 201 -> 216 us)
+constexpr unsigned kMinChunk = 2048;    // tokens that a chunk cut finer than asked for has at least (512: 1024-token chunks 201 -> 216 us)
 constexpr int kMaxLptBatch = 256;  // above this the O(batch^2 / threads) ranking costs more than it saves
 
 template <int D, bool kFp8, int kStages, int kWarps>
@@ -189,18 +189,19 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   if constexpr (Shape::kShaped) {
     // The partials are this launch's own: sequences shorter than the buffers allow for are cut finer, so that units come out alike
     // (8 sequences of 32k .. 131k, e4m3, in at most 10 chunks: 277 us with chunks of 13824 for all).
-    if (fuse && split) chunk_tokens = min(chunk_tokens, max((L / p.max_chunks + kPageSize) / kPageSize * kPageSize, kMinChunk));
+    if (fuse && split) chunk_tokens = static_cast<int>(min(static_cast<unsigned>(chunk_tokens), max((L / p.max_chunks / kPageSize + 1u) * kPageSize, kMinChunk)));
   }
   if (split) {
-    t0 = p.first_token + c * chunk_tokens;
-    if (t0 >= L) {
+    const int64_t start = chunk_start(p.first_token, c, chunk_tokens);
+    if (start >= L) {
       if (fuse && c == 0)  // empty sequence: its output rows are zero
         for (int i = tid; i < G * D; i += kWarps * 32) p.out[row0 * D + i] = __float2bfloat16_rn(0.f);
       return;
     }
-    t1 = min(t0 + chunk_tokens, L);
+    t0 = static_cast<int>(start);
+    t1 = chunk_end(start, chunk_tokens, L);
   }
-  const int nch = split ? min((L - p.first_token + chunk_tokens - 1) / chunk_tokens,
+  const int nch = split ? min(chunk_count(L - p.first_token, chunk_tokens),
                               p.max_chunks - p.chunk_slot0) : 1;
   // first attended token of this unit: the chunk start, raised by the sliding window
   int lo = (p.window > 0 && L - p.window > t0) ? L - p.window : t0;
@@ -215,7 +216,7 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
 
   if (tid == 0) { cta_err[0] = 0; cta_err[1] = 0; }
   const int page0 = lo / kPageSize;  // first page touched (lo need not be page-aligned)
-  const int n_tiles = (err || lo >= t1) ? 0 : (t1 + kPageSize - 1) / kPageSize - page0;
+  const int n_tiles = (err || lo >= t1) ? 0 : (t1 - 1) / kPageSize + 1 - page0;
   const int n_mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;  // tiles warp, warp+kWarps, ...
 
   const uint32_t ring = smem_u32(smem + warp * C::kWarpRing);

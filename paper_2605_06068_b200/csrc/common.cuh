@@ -51,6 +51,21 @@ struct StepParams {
   int32_t fuse_reduce; // 1: the launch writes `out` itself (needs workspace when split)
 };
 
+// Chunk c starts chunk_start(...) tokens into the sequence: its place may lie far beyond any sequence (chunks of 2^30 tokens in
+// buffers with room for many), so 64 bits.
+__host__ __device__ __forceinline__ int64_t chunk_start(int32_t first_token, int32_t c, int32_t chunk_tokens) {
+  return first_token + static_cast<int64_t>(c) * chunk_tokens;
+}
+// The token behind its last one, where start < L.
+__host__ __device__ __forceinline__ int32_t chunk_end(int64_t start, int32_t chunk_tokens, int32_t L) {
+  const int64_t end = start + chunk_tokens;
+  return end < L ? static_cast<int32_t>(end) : L;
+}
+// Chunks of `tokens` >= 0 tokens (the sum is below 2^32).
+__host__ __device__ __forceinline__ int32_t chunk_count(int32_t tokens, int32_t chunk_tokens) {
+  return static_cast<int32_t>((static_cast<uint32_t>(tokens) + static_cast<uint32_t>(chunk_tokens) - 1u) / static_cast<uint32_t>(chunk_tokens));
+}
+
 // Multi-query attention (attention_mq.cu): n_q query tokens per sequence.
 struct MqParams {
   AttnParams a;           // q is [B, n_q, Hq, D]; out / partials are indexed by (b*n_q + i)

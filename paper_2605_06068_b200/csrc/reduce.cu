@@ -24,7 +24,7 @@ reduce_kernel(const float* __restrict__ part_o, const float* __restrict__ part_l
   const int b = static_cast<int>(row / (static_cast<int64_t>(tokens_per_seq) * num_q_heads));  // row = (b, token, head)
   // first_chunks fixed slots (a shared prefix computed once), then the chunks of [first_token, L)
   const int L = max(seq_lens[b] - first_token, 0);
-  int n_chunks = first_chunks + (L + chunk_tokens - 1) / chunk_tokens;
+  int n_chunks = first_chunks + chunk_count(L, chunk_tokens);
   n_chunks = min(n_chunks, max_chunks);
   const float* lse = part_lse + row * max_chunks;
   float M = -INFINITY;
@@ -95,7 +95,7 @@ reduce_row_kernel(const float* __restrict__ part_o, const float* __restrict__ pa
   const int64_t row = blockIdx.x;
   const int b = static_cast<int>(row / (static_cast<int64_t>(tokens_per_seq) * num_q_heads));
   const int L = max(seq_lens[b] - first_token, 0);
-  int n_chunks = first_chunks + (L + chunk_tokens - 1) / chunk_tokens;
+  int n_chunks = first_chunks + chunk_count(L, chunk_tokens);
   n_chunks = min(n_chunks, max_chunks);
   const float* lse = part_lse + row * max_chunks;
   // every warp computes the row's maximum and weight sum the same way (same values in all four)
