@@ -1,5 +1,6 @@
 // C ABI of the rotating cache append and of attention with shaped scores: argument validation on the host, then dispatch.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -20,9 +21,14 @@ int check_score(const pda_score_desc* d, pda::ScoreParams* s) {
   if (!d || !std::isfinite(d->scale) || !std::isfinite(d->softcap) || d->softcap < 0.f || d->window < 0) return PDA_ERR_INVALID_ARG;
   if (!aligned4(d->slopes)) return PDA_ERR_MISALIGNED;
   const double log2e = 1.4426950408889634;
-  s->mul = static_cast<float>(d->softcap > 0.f ? 2.0 * log2e * d->scale / d->softcap : log2e * d->scale);
+  s->mul = static_cast<float>(log2e * d->scale);
   s->cap = static_cast<float>(log2e * d->softcap);
+  s->rate = 0.f;
   if (!std::isfinite(s->mul) || !std::isfinite(s->cap)) return PDA_ERR_INVALID_ARG;
+  if (d->softcap > 0.f) {
+    if (!std::isfinite(static_cast<float>(2.0 * log2e * d->scale / d->softcap))) return PDA_ERR_INVALID_ARG;
+    s->rate = static_cast<float>(std::min(2.0 / d->softcap, static_cast<double>(FLT_MAX)));
+  }
   s->slopes = d->slopes;
   s->window = d->window;
   return PDA_OK;

@@ -296,6 +296,7 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   if constexpr (Shape::kShaped) {
     scale_log2 = shape.score.mul;
     scores.cap = shape.score.cap;
+    scores.rate = shape.score.rate;
     const float* slopes = shape.score.slopes;
     const int head = g * p.group + 8 * part + 2 * tq;
     scores.slope0 = slopes != nullptr && 2 * tq < G ? slopes[head] * kLog2e : 0.f;

@@ -47,14 +47,14 @@ __device__ __forceinline__ void load_q_fragments(const __nv_bfloat16* q_rows, in
 struct PlainScores {
   static constexpr bool kShaped = false;
 };
-// Capped (cap = C > 0, see ScoreParams) and biased by the distance: token `row` of the tile is `dist - row` before the query;
+// Capped (cap = C > 0, rate: see ScoreParams) and biased by the distance: token `row` of the tile is `dist - row` before the query;
 // slopes times log2(e) of this thread's heads.
 struct ShapedScores {
   static constexpr bool kShaped = true;
-  float cap, slope0, slope1, dist;
-  __device__ __forceinline__ float operator()(float y, float slope, int row) const {
-    if (cap > 0.f) y = fmaf(-2.f * cap, rcp_approx(ex2(y) + 1.f), cap);
-    return fmaf(-slope, dist - static_cast<float>(row), y);
+  float cap, rate, slope0, slope1, dist;
+  __device__ __forceinline__ float operator()(float z, float slope, int row) const {
+    if (cap > 0.f) z = cap_score(z, cap, rate);
+    return fmaf(-slope, dist - static_cast<float>(row), z);
   }
 };
 

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(32) prefill_generic_kernel(const __grid_consta
       }
       if (kFp8) dot *= p.k_scale[static_cast<int64_t>(page) * p.geom.num_kv_heads + g];
       z = dot * p.score.mul;
-      if (p.score.cap > 0.f) z = fmaf(-2.f * p.score.cap, 1.f / (exp2f(z) + 1.f), p.score.cap);
+      if (p.score.cap > 0.f) z = cap_score(z, p.score.cap, p.score.rate);
       z = fmaf(-slope, static_cast<float>(abs(pos - j)), z);
     }
     float top = z;

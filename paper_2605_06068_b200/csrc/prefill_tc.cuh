@@ -33,9 +33,11 @@ struct PrefillPlan {
   int64_t slots;  // (not listed) row blocks are looked for at this many places
   int cut;        // few units: blocks are cut along the keys, so that every pair has a part
   float scale_log2;
-  // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): of degree 5 for
-  // |s| <= limit[0], of degree 11 for |s| <= limit[1]; ref: the fixed reference (capped only), or 0.
-  float limit[2], ref;
+  // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): for |s| <= limit[0] of degree 5 in s;
+  // for |s| <= limit[1] of degree 10 in u s, u = scale / softcap, times s. ref: the fixed reference (capped only), or 0. relative:
+  // the second polynomial's error goes with the score, and beyond it scores are taken one by one.
+  float limit[2], ref, u;
+  int relative;
   uint64_t poly5[3], poly11[6];
 };
 struct PrefillMaps {
@@ -1003,10 +1005,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           } else {
             if constexpr (kCap) {
               // The hyperbolic tangent of the cap goes by the row's largest product among the 64: small ones by a polynomial
-              // (|y| <= 1/2: degree 5; |y| <= 5/4: degree 11), of the form whose largest error is least (2^-17.5 and 2^-18.7, of
+              // (|x| <= 1/2: degree 5; |x| <= 5/4: degree 11), of the form whose largest error is least (2^-17.5 and 2^-18.7, of
               // 1), others, and infinities and NaN, by exponential and reciprocal: three results of the special-function unit a
               // score with the weight's. A warp takes one of the polynomials, the longer one if any of its rows asks for it.
               // Where the reference is fixed, the weights are taken right behind it.
+              // Caps above kAbsoluteCap take polynomials whose error goes with the score (cap_score), since scores may be far
+              // below the cap, and a row with larger products takes each of its scores the way that is its own.
               if (kMasked) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e) sv[e] = hidden(e) ? 0u : sv[e];
@@ -1036,6 +1040,14 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                   }
                 }
               };
+              auto poly11 = [&](uint64_t x) {  // (of x^2 before it is multiplied by x)
+                const uint64_t ux = mul_f32x2(x, both(plan.u)), t2 = mul_f32x2(ux, ux);
+                uint64_t y = fma_f32x2(t2, plan.poly11[5], plan.poly11[4]);
+                y = fma_f32x2(t2, y, plan.poly11[3]);
+                y = fma_f32x2(t2, y, plan.poly11[2]);
+                y = fma_f32x2(t2, y, plan.poly11[1]);
+                return fma_f32x2(t2, y, plan.poly11[0]);
+              };
               const bool longer = kMasked || __any_sync(0xffffffffu, far > plan.limit[0] && far <= plan.limit[1] && hi > lo);
               if (!longer && far <= plan.limit[0]) {
                 capped([&](uint64_t x) {
@@ -1045,18 +1057,23 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 });
               } else if (far <= plan.limit[1]) {
                 capped([&](uint64_t x) {
-                  const uint64_t t2 = mul_f32x2(x, x);
-                  uint64_t y = fma_f32x2(t2, plan.poly11[5], plan.poly11[4]);
-                  y = fma_f32x2(t2, y, plan.poly11[3]);
-                  y = fma_f32x2(t2, y, plan.poly11[2]);
-                  y = fma_f32x2(t2, y, plan.poly11[1]);
-                  y = fma_f32x2(t2, y, plan.poly11[0]);
+                  const uint64_t y = poly11(x);
                   return kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y);
+                });
+              } else if (!kFixed && plan.relative) {
+                capped([&](uint64_t x) {
+                  float x0, x1, z0, z1;
+                  f32x2_split(mul_f32x2(x, both(plan.u)), x0, x1);
+                  f32x2_split(mul_f32x2(x, poly11(x)), z0, z1);
+                  auto far_one = [&](float v) { return fmaf(-p.score.cap, 2.f * rcp_approx(ex2(2.f * kLog2e * v) + 1.f), p.score.cap); };
+                  if (!(fabsf(x0) <= kTanhReach)) z0 = far_one(x0);
+                  if (!(fabsf(x1) <= kTanhReach)) z1 = far_one(x1);
+                  return f32x2(__float_as_uint(z0), __float_as_uint(z1));
                 });
               } else {
                 capped([&](uint64_t x) {
                   float y0, y1;
-                  f32x2_split(mul_f32x2(x, both(p.score.mul)), y0, y1);
+                  f32x2_split(mul_f32x2(x, both(2.f * kLog2e * plan.u)), y0, y1);
                   const uint64_t r = f32x2(__float_as_uint(rcp_approx(ex2(y0) + 1.f)), __float_as_uint(rcp_approx(ex2(y1) + 1.f)));
                   return fma_f32x2(r, both(-2.f * p.score.cap), both(p.score.cap - plan.ref));
                 });

@@ -2,23 +2,53 @@
 #pragma once
 
 #include "common.cuh"
+#include "tma_ptx.cuh"
 
 namespace pda {
 
-// Scores are carried in the base-2 exponent: z = log2(e) * score. A cap is held as z = C - 2 C / (2^y + 1) with
-// C = log2(e) * softcap and y = 2 log2(e) / softcap * (scale * q.k): C * tanh, whose absolute error is a few 2^-23 C.
+// Scores are carried in the base-2 exponent: z = log2(e) * score. A cap C = log2(e) * softcap makes it C tanh(z / C).
 struct ScoreParams {
-  float mul;            // multiplies q.k: gives y (capped) or z (not capped)
+  float mul;            // log2(e) * scale: multiplies q.k and gives z, before any cap
   float cap;            // C, 0: no cap
+  float rate;           // 2 log2(e) / C, the largest 32-bit number if that is beyond it
   const float* slopes;  // nullptr: no bias
   int32_t window;       // 0: none
 };
 constexpr float kLog2e = 1.4426950408889634f;
 
+// tanh(x) / x for |x| <= 3/4 in powers of x^2, the polynomial of this degree whose largest relative error is least (2.9e-8, by
+// linear programming over 4000 points).
+constexpr float kTanhReach = 0.75f;
+#define PDA_TANH_COEFFICIENTS \
+  {0.9999999710136436f, -0.3333295887857063f, 0.13325406008671778f, -0.05334442977807218f, 0.019582907537387773f, -0.004716256828599296f}
+
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+
+// Polynomials and other forms of the cap whose error is relative to C are for C up to this one (a cap of 128): 5.3e-6 C is 2^-10 of an
+// exponent here, a quarter of a weight's rounding to bf16.
+constexpr float kAbsoluteCap = 184.f;
+
+// The cap on a score z: C - 2 C / (2^y + 1), y = 2 log2(e) z / C, whose error is a few 2^-23 C. Above kAbsoluteCap scores may be far below
+// the cap (which may be 10^8 times as large): there by the polynomial, whose error goes with the score, and only scores of 0.63 C and
+// more the first way. NaN stays, infinities give +-C. (All by the polynomial: 64 sequences of 512..4096, bf16 105 us instead of 103.)
+__device__ __forceinline__ float cap_score(float z, float cap, float rate) {
+  constexpr float c[6] = PDA_TANH_COEFFICIENTS;
+  const float y = z * rate;
+  if (cap > kAbsoluteCap) {
+    const float x = y * (0.5f / kLog2e);
+    if (fabsf(x) <= kTanhReach) {
+      const float t = x * x;
+      float r = fmaf(t, c[5], c[4]);
+#pragma unroll
+      for (int i = 3; i >= 0; --i) r = fmaf(t, r, c[i]);
+      return z * r;
+    }
+  }
+  return fmaf(-cap, 2.f * rcp_approx(ex2(y) + 1.f), cap);  // (2 C may be beyond 32 bits)
 }
 
 // Packed ragged queries (cu_q) or one query per sequence (cu_q == nullptr) over the paged cache.

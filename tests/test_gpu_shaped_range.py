@@ -72,3 +72,87 @@ def test_decode_lengths_up_to_the_last():
             kw = dict(chunk_tokens=1 << 30, part_o=nan(1, 2, 5, D), part_lse=nan(1, 2, 5), workspace=workspace)
             U.check(call(**kw)[:, h], ref, tol, "in chunks")
     assert int(status.item()) == 0
+
+
+# ---- caps of any size -------------------------------------------------------------------------------
+
+def capped(q, k, v, live, scale, cap, slope=0.0, dist=None, byte=None):
+    """(out, tol) of one head: rows q [n,D] over k, v [L,D], ``live`` [n,L]. Scores in 32 bits: the product is off by
+    (D + 3) 2^-24 scale sum |q_d k_d|, the cap by 2^-20 of the score (an odd polynomial whose error is relative, or exponential and
+    reciprocal where the tangent is not small: eight roundings of 2^-24 and two functions of 2^-22), and where a polynomial's error
+    is absolute by 2^-17 of the cap, for caps up to 128: 2^-10 at most. The rest as in shaped_util.attend. ``byte``: [n,L] bounds of
+    16-bit weights' steps."""
+    q, k, v = q.double(), k.double(), v.double()
+    s = (q @ k.T) * scale
+    e = (q.shape[1] + 3) * 2.0 ** -24 * abs(scale) * (q.abs() @ k.abs().T)
+    if cap > 0:
+        e = e * (1 - torch.tanh((s.abs() - e).clamp(min=0) / cap) ** 2)      # (the largest slope of the tangent on the way)
+        s = cap * torch.tanh(s / cap)
+        e = e + 2.0 ** -20 * s.abs() + (cap * 2.0 ** -17 if cap <= 128 else 0.0)
+    if dist is not None:
+        s = s - slope * dist
+        e = e + 2.0 ** -22 * (abs(slope) * dist + s.abs())
+    w = torch.softmax(torch.where(live, s, float("-inf")), 1)
+    o, A, we = w @ v, w @ v.abs(), w * e
+    tol = U.EPS * o.abs() + (2 * U.EPS + k.shape[0] * 2.0 ** -24 + 2.0 ** -12) * A + 2 * (we @ v.abs() + we.sum(1, keepdim=True) * o.abs())
+    if byte is not None:
+        tol = tol + byte
+    return o, 1.01 * tol
+
+
+def run_caps(how, D, fp8, cap, scale, seed, slopes=None, spread=4.0, near=None):
+    """Two sequences; ``near``: products q.k scale / cap spread over this range, by one number of a query and one of a key."""
+    lens, new, Hq, Hkv = [300, 70], ([300, 40] if how != "decode" else [1, 1]), 4, 2
+    c = U.Cache(lens, Hkv, D, fp8=fp8, seed=seed)
+    T = sum(new)
+    q = randn(seed + 1, T, Hq, D, scale=spread)
+    if near is not None:
+        g = np.random.default_rng(seed)
+        rows = torch.zeros(c.k_cache.shape)
+        for b, L in enumerate(lens):
+            x = torch.as_tensor(g.uniform(*near, size=(L, Hkv))).to(U.E4M3 if fp8 else torch.bfloat16)
+            for j in range(L):
+                rows[int(c.table[b, j // 16]), :, j % 16, 0] = x[j].float()
+            c.k[b] = torch.zeros((L, Hkv, D), dtype=torch.float64)
+            c.k[b][:, :, 0] = x.double()
+        c.k_cache = rows.to(c.k_cache.dtype).cuda()
+        if fp8:
+            c.k_scale = torch.ones_like(c.k_scale)
+        q = torch.zeros((T, Hq, D), dtype=torch.bfloat16)
+        q[:, :, 0] = 8.0
+        scale = float(np.float32(cap / 8.0))
+    dev_slopes = None if slopes is None else torch.tensor(slopes, device="cuda")
+    status = ints([0])
+    kw = dict(softcap=cap, slopes=dev_slopes, status=status, flags=GENERIC if how == "generic" else 0, **c.args())
+    if how == "decode":
+        out = pda.paged_biased_decode_attention(q.cuda(), c.k_cache, c.v_cache, c.dev_table, ints(lens), scale, **kw)
+    else:
+        out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, c.dev_table, ints(lens), cum(new), max(new), scale, **kw)
+    assert int(status.item()) == 0
+    at = 0
+    for b, n in enumerate(new):
+        pos, j = torch.arange(n) + lens[b] - n, torch.arange(lens[b])
+        live, dist = j[None, :] <= pos[:, None], (pos[:, None] - j[None, :]).abs().double()
+        for h in range(Hq):
+            k, v = c.k[b][:, h // 2], c.v[b][:, h // 2]
+            byte = 2.0 ** -25 * c.byte * live.sum(1, keepdim=True) if fp8 and how == "decode" else None
+            ref, tol = capped(q[at:at + n, h], k, v, live, float(np.float32(scale)), float(np.float32(cap)), 0.0 if slopes is None else float(np.float32(slopes[h])), dist, byte)
+            U.check(out[at:at + n, h], ref, tol, f"cap {cap} sequence {b} head {h}")
+        at += n
+
+
+WAYS = [("prompt", 128, False), ("prompt", 64, False), ("prompt", 128, True), ("generic", 96, False), ("generic", 64, True), ("decode", 128, False),
+        ("decode", 256, False), ("decode", 128, True)]
+
+
+@pytest.mark.parametrize("how,D,fp8", WAYS)
+@pytest.mark.parametrize("cap", [1.0, 30.0, 120.0, 135.0, 1000.0, 4100.0, 1e4, 1e6, 1e8, 1e20, 2e38])
+def test_scores_far_below_a_cap_are_left_alone(how, D, fp8, cap):
+    for slopes in (None, [0.3, 0.0, 0.05, -0.01]):
+        run_caps(how, D, fp8, cap, D ** -0.5, seed=50, slopes=slopes)
+
+
+@pytest.mark.parametrize("how,D,fp8", WAYS)
+@pytest.mark.parametrize("cap,near", [(20.0, (-1.5, 1.5)), (130.0, (2.0, 4.0)), (1000.0, (3.0, 6.0)), (1000.0, (0.6, 0.64)), (2000.0, (-0.001, 0.001)), (1e5, (5.0, 9.0)), (1e-30, (-2.0, 2.0))])
+def test_scores_about_a_cap(how, D, fp8, cap, near):
+    run_caps(how, D, fp8, cap, 0.0, seed=51, near=near)
