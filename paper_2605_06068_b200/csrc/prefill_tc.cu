@@ -44,7 +44,9 @@ void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
   const bool usable = std::abs(u) >= 1.0 / 1024 && std::abs(u) <= 1024 && !plan->relative && score.cap >= 1.f / 4096;
   plan->limit[0] = usable ? static_cast<float>(0.5 / std::abs(u)) : -1.f;
   plan->limit[1] = static_cast<float>((plan->relative ? static_cast<double>(kTanhReach) : 1.25) / std::abs(u));
-  plan->ref = shape == kShapeCap ? std::max(score.cap - kGFixedTop, 0.f) : 0.f;
+  plan->ref = shape & kShapeBias ? 0.f : std::max(score.cap - kGFixedTop, 0.f);
+  plan->ref_low = std::min(score.cap - kGFixedLow, plan->ref);
+  plan->low_limit = static_cast<float>(std::max(static_cast<double>(kGFixedFloor) - plan->ref, 0.0) / std::abs(static_cast<double>(score.mul)));  // (weights below 2^-60)
   double power = score.mul;
   for (int i = 0; i < 6; ++i, power *= u * u) {
     if (i < 3) plan->poly5[i] = twice(usable ? c5[i] * power : 0.0);
@@ -61,7 +63,7 @@ cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const Prefil
   kernel<<<static_cast<unsigned>(2 * pairs), C::kThreads, C::kSmemBytes, stream>>>(maps, p, plan);
   if ((e = cudaGetLastError()) != cudaSuccess || !plan.cut) return e;
   prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone && !kFp8 ? plan.scale_log2 : 1.f,
-                                                                                       kShape == kShapeCap ? 0.f : 5.4210109e-20f);
+                                                                                       (kShape & kShapeCap) && !(kShape & kShapeBias) ? 0.f : 5.4210109e-20f);
   return cudaGetLastError();
 }
 
@@ -69,6 +71,7 @@ template <int D, bool kFp8>
 cudaError_t launch_shape(const PrefillParams& p, const PrefillMaps& maps, const PrefillPlan& plan, int shape, int pairs, cudaStream_t stream) {
   if (shape == kShapeNone) return launch<D, kFp8, kShapeNone>(p, maps, plan, pairs, stream);
   if (shape == kShapeCap) return launch<D, kFp8, kShapeCap>(p, maps, plan, pairs, stream);
+  if (shape == (kShapeCap | kShapeLow)) return launch<D, kFp8, kShapeCap | kShapeLow>(p, maps, plan, pairs, stream);
   if (shape == kShapeBias) return launch<D, kFp8, kShapeBias>(p, maps, plan, pairs, stream);
   return launch<D, kFp8, kShapeCap | kShapeBias>(p, maps, plan, pairs, stream);
 }
@@ -137,8 +140,9 @@ cudaError_t launch_prefill_tc(const PrefillParams& p, cudaStream_t stream) {
   // Scores that are only capped have a fixed reference, if the cap allows it; otherwise the bias's form takes them, with slopes of
   // 0, and so it does scores that are not shaped if their factor is not above 0 (they are scaled behind the maximum).
   const float cap = p.score.cap;
-  const int shape = (cap > 0.f ? kShapeCap : 0) |
-                    (p.score.slopes != nullptr || cap > kGFixedCap || (cap == 0.f && !(p.score.mul > 0.f)) ? kShapeBias : 0);
+  int shape = (cap > 0.f ? kShapeCap : 0) |
+              (p.score.slopes != nullptr || cap > kGFixedCap || (cap == 0.f && !(p.score.mul > 0.f)) ? kShapeBias : 0);
+  if (shape == kShapeCap && cap + std::max(cap - kGFixedTop, 0.f) > kGFixedFloor) shape |= kShapeLow;
   PrefillPlan plan{q_blocks, tile_rows, listed, listed ? 0 : places, cut, p.score.mul};
   if (cap > 0.f) set_cap(p.score, shape, &plan);
   const int n = static_cast<int>(pairs);

@@ -34,9 +34,10 @@ struct PrefillPlan {
   int cut;        // few units: blocks are cut along the keys, so that every pair has a part
   float scale_log2;
   // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): for |s| <= limit[0] of degree 5 in s;
-  // for |s| <= limit[1] of degree 10 in u s, u = scale / softcap, times s. ref: the fixed reference (capped only), or 0. relative:
+  // for |s| <= limit[1] of degree 10 in u s, u = scale / softcap, times s. ref: the fixed reference (capped only), or 0; ref_low: that of rows with low scores,
+  // whose products are above low_limit in size. relative:
   // the second polynomial's error goes with the score, and beyond it scores are taken one by one.
-  float limit[2], ref, u;
+  float limit[2], ref, ref_low, low_limit, u;
   int relative;
   uint64_t poly5[3], poly11[6];
 };
@@ -72,11 +73,17 @@ constexpr float kGRescale = 32.f;
 constexpr int kGPolyOf = 4;      // every fourth pair of exponentials by polynomial
 constexpr int kGMinTiles = 4;    // of a part
 // Capped scores that are not biased lie within [-C, C] (ScoreParams): they need no maximum. Their weights are taken relative
-// to a reference fixed at max(C - 30, 0), which keeps them within 2^-120 .. 2^30 for C <= 75 (a cap up to 52).
-constexpr float kGFixedTop = 30.f, kGFixedCap = 75.f;
+// to a reference fixed at max(C - 30, 0), which keeps them within 2^-120 .. 2^30 for C <= 75 (a cap up to 52). A weight is multiplied
+// with values, and with their page's scale, that may be small too. So, where weights could be below 2^-60 (C > 45, a cap above 31: kShapeLow),
+// a row whose first 64 keys together weigh less than that (as the first tokens of a prompt may, or all, if their scores lie near -C) goes
+// on at C - 100, from where it returns once 64 keys weigh more than 2^36: its largest weight is never below 2^-60. Rows whose first
+// products are small are not looked at. The code for it costs 2 % of a prompt of 8192 tokens and 6 % of 24 of 1..700, although it
+// hardly runs (instruction caches: in front of the weights it cost 5 and 15 %, as a second copy of the loop 7 and 21 %).
+constexpr float kGFixedTop = 30.f, kGFixedCap = 75.f, kGFixedFloor = 60.f, kGFixedLow = 100.f;
+constexpr float kGFixedLeast = 8.6736174e-19f, kGFixedMost = 68719476736.f;  // 2^-60, 2^36
 
-// How scores are shaped (bits): capped; biased by distance.
-enum : int { kShapeNone = 0, kShapeCap = 1, kShapeBias = 2 };
+// How scores are shaped (bits): capped; biased by distance; capped alone, with a fixed reference that rows may lie far below.
+enum : int { kShapeNone = 0, kShapeCap = 1, kShapeBias = 2, kShapeLow = 4 };
 
 // e4m3 caches: tiles land in a ring of bytes and are converted to bf16 (exactly) by a warpgroup of their own; the page scales
 // go through the softmax.
@@ -141,6 +148,21 @@ __device__ __forceinline__ float score_factor(float r, float scale_log2) {
 // What weights and sums taken at reference `from` are multiplied by to be those at a reference `to` >= from whose factor is c.
 __device__ __forceinline__ float rescale(float from, float to, float c) { return ex2(__fmul_rn(from, c) - __fmul_rn(to, c)); }
 
+// O of a warp's rows in tensor memory, times `a` (each row its own). Out of line: it is rare, and the hot loop's code has to stay in the
+// instruction caches.
+template <int D>
+__device__ __noinline__ void rescale_columns(uint32_t my_o, float a) {
+#pragma unroll 1
+  for (int c = 0; c < D / 16; ++c) {
+    uint32_t ov[16];
+    tmem_ld16(my_o + 16 * c, ov);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
+    tmem_st16(my_o + 16 * c, ov);
+  }
+}
+
 // One row block of one kv head (or a part of its keys), as the producer hands it to the other warps of its CTA. row0 < 0: no
 // more. Rows are counted in query tokens of the sequence. dual: the block fits one half and both halves take the same
 // rows, with tiles of their own by turns: kTwoHeads: the second half's are the next head's; kSplitKeys: the second half's are
@@ -185,7 +207,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   using C = GCfg<D, kFp8>;
   constexpr int kStages = C::kStages;
   constexpr bool kCap = (kShape & kShapeCap) != 0, kBias = (kShape & kShapeBias) != 0;
-  constexpr bool kFixed = kShape == kShapeCap;     // ... and lie within bounds: the reference is fixed
+  constexpr bool kFixed = kCap && !kBias;          // ... and lie within bounds: the reference is fixed
+  constexpr bool kLow = (kShape & kShapeLow) != 0;
   // References in the exponent's units: of scores whose factor is not the same for all keys (a bias, e4m3's page scales).
   constexpr bool kExp = kBias || (kFp8 && !kFixed);
   constexpr bool kDown = kBias;                    // a bias has the scores rise from tile to tile: the last tiles come first
@@ -995,6 +1018,16 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               }
             }
           }
+          // (warp-collective) O so far, up to the last tile or to the first run of this one, times `a`; false: the wait for it ran out
+          auto rescale_output = [&](float a) {
+            if (j == 0 && k == 0) return true;
+            if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
+            if (!ok) return false;
+            __syncwarp();
+            tc_fence_after();
+            rescale_columns<D>(my_o, a);
+            return true;
+          };
           auto pack = [&](int e, float w0, float w1) {  // (values' page scales go with the weights)
             if constexpr (kFp8) f32x2_split(mul_f32x2(f32x2(__float_as_uint(w0), __float_as_uint(w1)), both(page_scale[e >> 3].y)), w0, w1);
             return pack2<false>(w0, w1);
@@ -1019,7 +1052,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
 #pragma unroll
               for (int e = 0; e < 32; ++e) mx[e & 3] = max3_nan(mx[e & 3], fabsf(__uint_as_float(sv[2 * e])), fabsf(__uint_as_float(sv[2 * e + 1])));
               const float far = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]);
-              const uint64_t minus_ref = both(-plan.ref);
+              const uint64_t minus_ref = both(-m_ref);
               [[maybe_unused]] uint64_t sum2[2] = {0ull, 0ull};
               auto capped = [&](auto shape) {  // (shape: of a pair of products)
 #pragma unroll
@@ -1048,6 +1081,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 y = fma_f32x2(t2, y, plan.poly11[1]);
                 return fma_f32x2(t2, y, plan.poly11[0]);
               };
+              [[maybe_unused]] const bool watch = kLow && __any_sync(0xffffffffu, (l == 0.f && far > plan.low_limit && hi > lo) || m_ref != plan.ref);
               const bool longer = kMasked || __any_sync(0xffffffffu, far > plan.limit[0] && far <= plan.limit[1] && hi > lo);
               if (!longer && far <= plan.limit[0]) {
                 capped([&](uint64_t x) {
@@ -1075,13 +1109,27 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                   float y0, y1;
                   f32x2_split(mul_f32x2(x, both(2.f * kLog2e * plan.u)), y0, y1);
                   const uint64_t r = f32x2(__float_as_uint(rcp_approx(ex2(y0) + 1.f)), __float_as_uint(rcp_approx(ex2(y1) + 1.f)));
-                  return fma_f32x2(r, both(-2.f * p.score.cap), both(p.score.cap - plan.ref));
+                  return fma_f32x2(r, both(-2.f * p.score.cap), both(kFixed ? p.score.cap - m_ref : p.score.cap));
                 });
               }
               if constexpr (kFixed) {
                 float s0, s1;
                 f32x2_split(add_f32x2(sum2[0], sum2[1]), s0, s1);
                 part = s0 + s1;
+                if constexpr (kLow) {
+                  // Where the reference is not the right one it is changed and the run begins again: its scores still stand in tensor memory.
+                  // (A row that has nothing yet has no O to be multiplied. A row goes down once and up once.)
+                  const bool lower = l == 0.f && part > 0.f && part < kGFixedLeast && m_ref > plan.ref_low && hi > lo;
+                  const bool raise = part > kGFixedMost && m_ref < plan.ref;
+                  if (__builtin_expect(watch && __any_sync(0xffffffffu, lower || raise), 0)) {
+                    const float a = raise ? ex2(m_ref - plan.ref) : 1.f;
+                    m_ref = raise ? plan.ref : lower ? plan.ref_low : m_ref;
+                    l *= a;
+                    if (__any_sync(0xffffffffu, raise) && !rescale_output(a)) return;
+                    --k;
+                    continue;
+                  }
+                }
               }
             }
             // Scores that references are taken of. Biased ones and e4m3's are in the exponent's units: mul s + slope (j - p), the slope's
@@ -1186,20 +1234,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 }
                 m_ref = m_new;
                 l *= a;
-                if (j > 0 || k > 0) {  // O so far: up to the last tile, or to the first run of this one
-                  if (ok) ok = __all_sync(0xffffffffu, mbar_spin_bounded(bar_pv + 16 * w + 8 * (k ^ 1), (k == 0 ? t - 1 : t) & 1));
-                  if (!ok) break;
-                  tc_fence_after();
-#pragma unroll 1
-                  for (int c = 0; c < D / 16; ++c) {
-                    uint32_t ov[16];
-                    tmem_ld16(my_o + 16 * c, ov);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * a);
-                    tmem_st16(my_o + 16 * c, ov);
-                  }
-                }
+                if (!rescale_output(a)) break;
               }
             }
           }
@@ -1231,7 +1266,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       const bool split = un.dual == kSplitKeys;
       float* sums = merge_sh + 2 * (tid & 127);  // the row's reference and sum from the second half
       if (split && w == 1) {  // the first half's warp of the same rows takes it from here
-        *reinterpret_cast<float2*>(sums) = make_float2(m_ref, l);
+        *reinterpret_cast<float2*>(sums) = make_float2(kFixed && l == 0.f ? kGNoMax : m_ref, l);  // (no keys of this half: no say in the reference)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_tc(bar_merge + 8 * (warp & 3));
@@ -1243,6 +1278,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         tc_fence_after();
         ++merges;
         const float2 other = *reinterpret_cast<const float2*>(sums);
+        if (kFixed && l == 0.f) m_ref = kGNoMax;
         const float m = fmaxf(m_ref, other.x);
         const float c_new = score_factor(m, scale_log2);
         const float mul = rescale(m_ref, m, c_new), mul_other = rescale(other.x, m, c_new);

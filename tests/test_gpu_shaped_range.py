@@ -156,3 +156,71 @@ def test_scores_far_below_a_cap_are_left_alone(how, D, fp8, cap):
 @pytest.mark.parametrize("cap,near", [(20.0, (-1.5, 1.5)), (130.0, (2.0, 4.0)), (1000.0, (3.0, 6.0)), (1000.0, (0.6, 0.64)), (2000.0, (-0.001, 0.001)), (1e5, (5.0, 9.0)), (1e-30, (-2.0, 2.0))])
 def test_scores_about_a_cap(how, D, fp8, cap, near):
     run_caps(how, D, fp8, cap, 0.0, seed=51, near=near)
+
+
+# ---- rows far below the cap -------------------------------------------------------------------------
+
+def signed_prompt(fp8, cap, vscale, signs, new, first=None, D=128, order=None, seed=5):
+    """A prompt whose scores are +-cap (or near zero) by ``signs`` [L] of its keys, values of the size ``vscale``: one kv head, two
+    query heads, of which the second sees the opposite scores. Returns (got, ref, tol)."""
+    L = len(signs)
+    c = U.Cache([L], 1, D, seed=seed)
+    rows = torch.zeros(c.k_cache.shape)
+    for j, s in enumerate(signs):
+        rows[int(c.table[0, j // 16]), 0, j % 16] = 8.0 * float(s)
+    values = torch.where(c.v_cache.cpu().isnan(), 0.0, c.v_cache.cpu().float())
+    kw = {}
+    if fp8:
+        k_cache, v_cache = rows.to(U.E4M3).cuda(), values.to(U.E4M3).cuda()
+        one = torch.ones((rows.shape[0], 1), device="cuda")
+        kw = dict(k_scale=one, v_scale=one * vscale)
+        values = v_cache.cpu().double() * vscale
+    else:
+        k_cache, v_cache = rows.to(torch.bfloat16).cuda(), (values * vscale).to(torch.bfloat16).cuda()
+        values = v_cache.cpu().double()
+    v = torch.stack([values[int(c.table[0, j // 16]), 0, j % 16] for j in range(L)])
+    q = torch.full((new, 2, D), 8.0, dtype=torch.bfloat16)
+    q[:, 1] = -8.0
+    status = ints([0])
+    got = pda.paged_prefill_attention(q.cuda(), k_cache, v_cache, c.dev_table, ints([L]), ints([0, new]), new, 1.0, softcap=cap, status=status,
+                                      first_keys=None if first is None else ints(first), **kw)
+    assert int(status.item()) == 0
+    pos, j = torch.arange(new) + L - new, torch.arange(L)
+    live = j[None, :] <= pos[:, None]
+    if first is not None:
+        live &= j[None, :] >= torch.tensor(first)[:, None]
+    ref, tol = torch.zeros((new, 2, D), dtype=torch.float64), torch.zeros((new, 2, D), dtype=torch.float64)
+    some = live.any(1)
+    for h, sign in enumerate((1.0, -1.0)):
+        s = cap * torch.tanh(sign * torch.tensor(signs, dtype=torch.float64) * 64 * D / cap)
+        # scores off by 2^-20 of the cap (and by 2^-17 of it where a polynomial takes them): the same for equal scores
+        e = cap * (2.0 ** -20 + 2.0 ** -17)
+        w = torch.softmax(torch.where(live, s[None, :], float("-inf"))[some], 1)
+        o, A = w @ v, w @ v.abs()
+        ref[some, h] = o
+        tol[some, h] = 1.01 * (U.EPS * o.abs() + (2 * U.EPS + L * 2.0 ** -24 + 2.0 ** -12 + 4 * e) * A)
+    return got, ref, tol
+
+
+SIZES = [(True, 2.0 ** -8), (True, 2.0 ** -14), (True, 2.0 ** -22), (True, 2.0 ** -40), (False, 1.0), (False, 2.0 ** -30), (False, 2.0 ** -45), (True, 2.0 ** 30), (False, 2.0 ** 40)]
+
+
+@pytest.mark.parametrize("cap", [5.0, 20.0, 40.0, 50.0, 51.9, 60.0])
+@pytest.mark.parametrize("fp8,vscale", SIZES)
+def test_rows_all_of_whose_scores_lie_at_the_negative_cap(cap, fp8, vscale):
+    g = np.random.default_rng(3)
+    U.check(*signed_prompt(fp8, cap, vscale, [-1.0], 1))
+    U.check(*signed_prompt(fp8, cap, vscale, [-1.0] * 300, 300))
+    # the first tokens see only the lowest scores, later ones higher and higher ones, 64 and more keys on
+    steps = [-1.0] * 100 + [0.0] * 30 + [1.0] + [-1.0] * 170
+    U.check(*signed_prompt(fp8, cap, vscale, steps, 300))
+    U.check(*signed_prompt(fp8, cap, vscale, list(g.choice([-1.0, -1.0, -1.0, 0.0, 1.0], size=700)), 700))
+
+
+@pytest.mark.parametrize("fp8,vscale", SIZES)
+def test_low_rows_whose_keys_are_split(fp8, vscale):
+    """Few rows: the tiles are shared by a block's halves, or cut along the keys; some rows see keys of one share only."""
+    U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 400, 5, first=[0, 390, 200, 0, INT_MAX]))
+    U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 150 + [1.0] + [-1.0] * 249, 5, first=[0, 390, 200, 120, 151]))
+    U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 3000, 60, first=[50 * i for i in range(59)] + [2999]))
+    U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 1000 + [0.0] + [-1.0] * 1000 + [1.0] + [-1.0] * 998, 60, first=[50 * i for i in range(59)] + [2999]))
