@@ -94,8 +94,6 @@ bool encode_bytes(CUtensorMap* map, const void* base, const CacheGeom& g) {
 
 bool prefill_tc_supports(const PrefillParams& p) {
   if (p.geom.head_dim != 128 && (p.geom.head_dim != 64 || p.geom.dtype != PDA_BF16)) return false;
-  // (a bias of keys in a prefix is taken in the products' units)
-  if (p.score.slopes != nullptr && p.prefix_lens != nullptr && std::abs(p.score.mul) < 1e-18f) return false;
   if (p.group > 128 || p.geom.num_pages < 1 || p.geom.num_pages == INT32_MAX) return false;
   const auto fits = [](int64_t stride, int64_t extent) { return extent == 1 || (stride > 0 && stride < (1ll << 38)); };
   if (!fits(p.q_token_stride, p.total_q) || !fits(p.q_head_stride, p.num_q_heads)) return false;

@@ -1133,7 +1133,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               }
             }
             // Scores that references are taken of. Biased ones and e4m3's are in the exponent's units: mul s + slope (j - p), the slope's
-            // part a constant for the first of 16 keys and slope times 0 .. 15; e4m3's that are not biased with the page's scale. They
+            // part a constant for the first of 16 keys and slope times 0 .. 15 (in masked tiles the distance of each key); e4m3's that are not biased with the page's scale. They
             // are rounded before the reference is taken from them: so a reference is a score itself, none of those it was taken of
             // passes it, and it is raised once at most for 64 keys. (Taken from the product in the same rounding, scores of 2^30 and
             // more passed a reference that could not be raised by so little. Costs 7 %: 508 -> 538 us biased, 577 -> 617 e4m3. A pass of its own
@@ -1143,7 +1143,12 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 const int g = e >> 3, i = e & 7;
                 // (the distance is taken in whole numbers: near keys' biases are off by little behind long contexts too)
                 const float distance = static_cast<float>(key0_pos + (g < 2 ? first_lo : first_hi) + 16 * g);
-                const uint64_t bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(slope * distance));
+                uint64_t bias2;
+                if constexpr (kMasked) {  // (keys behind the token itself may be among them, of a prefix: the bias goes down on that side too)
+                  bias2 = mul_f32x2(both(-slope), f32x2(__float_as_uint(fabsf(distance + 2.f * i)), __float_as_uint(fabsf(distance + (2.f * i + 1.f)))));
+                } else {
+                  bias2 = fma_f32x2(both(slope), f32x2(__float_as_uint(2.f * i), __float_as_uint(2.f * i + 1.f)), both(slope * distance));
+                }
                 return kCap ? add_f32x2(two(e), bias2) : fma_f32x2(two(e), both(p.score.mul), bias2);
               } else if constexpr (kExp) {
                 return mul_f32x2(two(e), both(p.score.mul * page_scale[e >> 3].x));
@@ -1151,17 +1156,6 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 return two(e);
               }
             };
-            if constexpr (kBias) {
-              if (kMasked && p.prefix_lens != nullptr) {  // keys behind the token itself: their bias has the other sign
-                const int own_lo = -key0_pos - first_lo, own_hi = -key0_pos - first_hi;
-                const float twice = kCap ? -2.f * slope : -2.f * slope / p.score.mul;
-#pragma unroll
-                for (int e = 0; e < 64; ++e) {
-                  const int behind = e - (e < 32 ? own_lo : own_hi);
-                  if (behind > 0) sv[e] = __float_as_uint(fmaf(twice, static_cast<float>(behind), __uint_as_float(sv[e])));
-                }
-              }
-            }
             if constexpr (!kFixed) {
               if (kMasked && !kExp) {
 #pragma unroll

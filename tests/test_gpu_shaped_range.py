@@ -224,3 +224,41 @@ def test_low_rows_whose_keys_are_split(fp8, vscale):
     U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 150 + [1.0] + [-1.0] * 249, 5, first=[0, 390, 200, 120, 151]))
     U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 3000, 60, first=[50 * i for i in range(59)] + [2999]))
     U.check(*signed_prompt(fp8, 50.0, vscale, [-1.0] * 1000 + [0.0] + [-1.0] * 1000 + [1.0] + [-1.0] * 998, 60, first=[50 * i for i in range(59)] + [2999]))
+
+
+# ---- a scale of zero --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("D,fp8", [(128, False), (128, True), (64, False), (64, True)])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-30, -0.2])
+def test_prefix_without_slopes_whatever_the_scale(D, fp8, scale):
+    lens, new, prefix = [170, 240, 60], [150, 40, 60], [170, 230, 33]
+    c = U.Cache(lens, 2, D, fp8=fp8, seed=8)
+    q = randn(9, sum(new), 4, D)
+    for flags in (0, GENERIC):
+        out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, c.dev_table, ints(lens), cum(new), 150, scale, prefix_lens=ints(prefix), flags=flags, **c.args())
+        U.check(out, *U.reference(c, q, new, scale, prefix=prefix))
+
+
+def test_prefix_and_slopes_that_a_small_scale_does_not_bear():
+    """Biases of 2^70 and more of keys behind the token itself: the nearest key's weight is all there is."""
+    lens, new, prefix = [200, 90], [150, 40], [170, 60]
+    c = U.Cache(lens, 2, 128, seed=8)
+    q = randn(9, sum(new), 4, 128)
+    first = [p + 3 if p + 3 < 170 else 0 for p in range(50, 200)] + [0] * 40      # (rows that see keys behind themselves alone)
+    status = ints([0])
+    for slope in (2.0 ** 70, 2.0 ** 100):
+        slopes = torch.tensor([slope, 0.0, slope, 0.1], device="cuda")
+        for scale in (1e-17, 1e-3):
+            for flags in (0, GENERIC):
+                out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, c.dev_table, ints(lens), cum(new), 150, scale, slopes=slopes,
+                                                  prefix_lens=ints(prefix), first_keys=ints(first), flags=flags, status=status)
+                U.check(out[:, [1, 3]], *(x[:, [1, 3]] for x in U.reference(c, q, new, scale, slopes=slopes.cpu().double(), prefix=prefix, first=first)))
+                at = 0
+                for b, (lo, hi) in enumerate(U.visible(lens, new, 0, prefix, first)):
+                    pos = torch.arange(new[b]) + lens[b] - new[b]
+                    near = torch.minimum(torch.maximum(pos, lo), hi - 1)
+                    for h in (0, 2):
+                        ref = c.v[b][near, h // 2]
+                        U.check(out[at:at + new[b], h], ref, 1.01 * 3 * U.EPS * ref.abs(), f"{slope} {scale} {flags}")
+                    at += new[b]
+    assert int(status.item()) == 0
