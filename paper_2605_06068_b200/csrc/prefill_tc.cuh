@@ -169,7 +169,7 @@ __device__ __noinline__ void rescale_columns(uint32_t my_o, float a) {
 // the later n1 tiles of the same head, and the first half's warps merge the two results.
 enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
 struct GUnit {
-  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace
+  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad, gaps;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace; gaps: there may be keys between that no row sees
   __device__ int first_row(int w, int half_rows) const { return row0 + (dual ? 0 : half_rows * w); }
   __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
   __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
@@ -297,8 +297,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kGTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  // The keys that the query tokens `row0` .. `last` of a sequence can see at most: none before `lo`, none from `hi` on.
-  // (lo by the first token and the window alone; documents that start later narrow it further)
+  // The keys that the query tokens `row0` .. `last` of a sequence see where nothing but position, window and prefix matters: none
+  // before `lo`, none from `hi` on, and each in between. (documents: the rows one by one, see make_unit)
   auto key_range = [&](int row0, int last, int nq, int L, int prefix, int& lo, int& hi) {
     const int first_pos = L - nq + row0, last_pos = L - nq + last;
     hi = last_pos < 0 ? 0 : max(last_pos + 1, min(prefix, L));
@@ -589,21 +589,45 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
       auto make_unit = [&](GUnit& un, int qb, int h, int b, int4 span, int part, int parts, int slot) {
         const int nq = span.y, L = span.z, row0 = qb * block_rows;
         const int rows = min(block_rows, nq - row0);
-        int lo, hi;
-        key_range(row0, row0 + rows - 1, nq, L, span.w, lo, hi);
-        if (p.first_keys != nullptr) {  // documents: the first key that any of the rows sees
-          int first_key = INT_MAX;
-          for (int i = lane; i < rows; i += 32) first_key = min(first_key, p.first_keys[span.x + row0 + i]);
-          lo = max(lo, __reduce_min_sync(0xffffffffu, first_key));
+        int lo, hi_w[2] = {0, 0};  // first key that any row sees; the last ones of the halves' rows
+        bool gaps = false;
+        if (p.first_keys == nullptr) {
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const int from = row0 + half_rows * w, last = min(from + half_rows, nq) - 1;
+            int lo_w;
+            if (from < nq) key_range(from, last, nq, L, span.w, lo_w, hi_w[w]);
+            if (w == 0) lo = lo_w;
+          }
+        } else {
+          // Rows that see nothing have no say: neither their pages nor the table's entries for them need be any good.
+          int lo_min = INT_MAX, first_row = INT_MAX, last_row = -1, own = 0;  // (own: rows that see the key they stand at)
+#pragma unroll 1
+          for (int i = lane; i < rows; i += 32) {
+            const int pos = L - nq + row0 + i;
+            int row_lo, row_hi;
+            visible_keys(pos, L, p.score.window, p.first_keys[span.x + row0 + i], span.w, row_lo, row_hi);
+            if (row_lo >= row_hi) continue;
+            lo_min = min(lo_min, row_lo);
+            hi_w[0] = i < half_rows ? max(hi_w[0], row_hi) : hi_w[0];
+            hi_w[1] = i < half_rows ? hi_w[1] : max(hi_w[1], row_hi);
+            first_row = min(first_row, i);
+            last_row = i;
+            own += row_lo <= pos;
+          }
+          lo = __reduce_min_sync(0xffffffffu, lo_min);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) hi_w[w] = __reduce_max_sync(0xffffffffu, hi_w[w]);
+          first_row = __reduce_min_sync(0xffffffffu, first_row);
+          last_row = __reduce_max_sync(0xffffffffu, last_row);
+          // (the keys of rows that see their own ones hang together, if there is no other row between them)
+          gaps = __reduce_add_sync(0xffffffffu, own) != last_row - first_row + 1;
+          if (last_row < 0) lo = 0, gaps = false;
         }
+        const int hi = max(hi_w[0], hi_w[1]);
         int n[2], tile0 = lo / kGKeys, key_end = hi;
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const int from = row0 + half_rows * w, last = min(from + half_rows, nq) - 1;
-          int lo_w, hi_w = 0;
-          if (from < nq) key_range(from, last, nq, L, span.w, lo_w, hi_w);
-          n[w] = hi_w > lo ? (hi_w + kGKeys - 1) / kGKeys - tile0 : 0;
-        }
+        for (int w = 0; w < 2; ++w) n[w] = hi_w[w] > lo ? (hi_w[w] + kGKeys - 1) / kGKeys - tile0 : 0;
         if (parts > 1) {  // (both halves' tiles within this part of the block's)
           const int all = max(n[0], n[1]);
           const int from = static_cast<int>(static_cast<int64_t>(all) * part / parts), to = static_cast<int>(static_cast<int64_t>(all) * (part + 1) / parts);
@@ -620,7 +644,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           dual = kSplitKeys;
           n[0] = n[1] = (n[0] + 1) / 2;  // (with an odd number the last tile lies behind the last key)
         }
-        un = GUnit{row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0};
+        un = GUnit{row0, h, span.x, nq, L, span.w, tile0, n[0], n[1], dual, parts > 1 ? slot : -1, key_end, 0, gaps};
         b_now = b;
         lo_now = lo;
         hi_now = key_end;
@@ -715,7 +739,18 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           const int64_t page = (static_cast<int64_t>(tile0) + tile) * 8 + (lane & 7);
           Pages r{p.geom.num_pages, 0.f, 0.f};
           bool bad = false;
-          if (tile >= 0 && page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now) {
+          bool wanted = tile >= 0 && page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now;
+          if (wanted && units[slot].gaps) {  // (the unit from shared memory: registers are short here)
+            const GUnit& un = units[slot];
+            wanted = false;
+#pragma unroll 1
+            for (int i = 0, rows = min(block_rows, un.nq - un.row0); i < rows && !wanted; ++i) {
+              int row_lo, row_hi;
+              visible_keys(un.L - un.nq + un.row0 + i, un.L, p.score.window, p.first_keys[un.q0 + un.row0 + i], un.prefix, row_lo, row_hi);
+              wanted = row_lo < row_hi && row_lo < (page + 1) * kPageSize && row_hi > page * kPageSize;
+            }
+          }
+          if (wanted) {
             const int v = table[page];
             bad = v < 0 || v >= p.geom.num_pages;
             if (!bad) {

@@ -262,3 +262,81 @@ def test_prefix_and_slopes_that_a_small_scale_does_not_bear():
                         U.check(out[at:at + new[b], h], ref, 1.01 * 3 * U.EPS * ref.abs(), f"{slope} {scale} {flags}")
                     at += new[b]
     assert int(status.item()) == 0
+
+
+# ---- rows that see nothing --------------------------------------------------------------------------
+
+def unseen(c, lens, new, window, prefix, first, how):
+    """Tables and caches in which nothing that no token sees can be used: ids outside the cache, or pages of NaN."""
+    see = U.visible(lens, new, window, prefix, first)
+    table = c.dev_table.clone()
+    for b, (lo, hi) in enumerate(see):
+        for i in range(-(-lens[b] // 16)):
+            if not ((lo < hi) & (lo < 16 * i + 16) & (hi > 16 * i)).any():
+                if how == "ids":
+                    table[b, i] = -1 if i % 2 else c.k_cache.shape[0] + i
+                else:
+                    for cache in (c.k_cache, c.v_cache):
+                        cache.view(torch.uint8)[int(c.table[b, i])] = 0xFF
+                    for scale in (c.k_scale, c.v_scale):
+                        if scale is not None:
+                            scale[int(c.table[b, i])] = float("nan")
+    return table
+
+
+CASES = [
+    # trailing rows that see nothing (padding), of a block, of a half and of whole blocks
+    ([128], [128], 0, None, [0] * 64 + [INT_MAX] * 64),
+    ([700], [700], 0, None, [0] * 10 + [INT_MAX] * 690),
+    # leading ones, with a window and without
+    ([300], [300], 40, None, [INT_MAX] * 150 + [0] * 150),
+    ([300, 90], [300, 60], 0, None, [250] * 250 + [255] * 20 + [270] * 30 + [INT_MAX] * 30 + [64] * 30),
+    # in the middle, in several places
+    ([400], [400], 30, None, [0] * 40 + [INT_MAX] * 100 + [0] * 10 + [390] * 240 + [0] * 10),
+    ([400], [400], 0, None, [16 * (i // 16) if i // 50 % 2 else INT_MAX for i in range(400)]),
+    # all of them
+    ([200, 33], [200, 20], 0, None, [INT_MAX] * 200 + [0] * 20),
+    # rows that see keys behind themselves alone, and none between
+    ([500], [300], 0, [450], [400] * 20 + [0] * 5 + [420] * 200 + [INT_MAX] * 60 + [499] * 15),
+    # rows before their sequence
+    ([100], [150], 5, None, [0] * 60 + [INT_MAX] * 30 + [0] * 60),
+    # many keys and few rows: blocks that are cut
+    ([4000, 2500], [60, 20], 0, None, [INT_MAX] * 10 + [3900 + i for i in range(20)] + [INT_MAX] * 10 + [3990] * 20 + [2490] * 10 + [INT_MAX] * 10),
+    ([4000], [40], 0, [1000], [0] * 10 + [3000] * 10 + [INT_MAX] * 20),
+]
+
+
+@pytest.mark.parametrize("how", ["ids", "pages"])
+@pytest.mark.parametrize("kw", [dict(), dict(softcap=9.0), dict(slopes=[0.1, 0.02, 0.0, 0.3])])
+@pytest.mark.parametrize("D,fp8", [(128, False), (128, True), (64, False)])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_pages_that_no_row_sees(case, D, fp8, kw, how):
+    lens, new, window, prefix, first = CASES[case]
+    Hq, Hkv = 4, 2
+    c = U.Cache(lens, Hkv, D, fp8=fp8, seed=case)
+    table = unseen(c, lens, new, window, prefix, first, how)
+    q = randn(case + 1, sum(new), Hq, D)
+    dev = dict(kw, slopes=torch.tensor(kw["slopes"], device="cuda")) if "slopes" in kw else kw
+    status = ints([0])
+    out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, table, ints(lens), cum(new), max(new), 0.1, window=window, first_keys=ints(first),
+                                      prefix_lens=None if prefix is None else ints(prefix), status=status, **c.args(), **dev)
+    assert int(status.item()) == 0
+    slopes = None if "slopes" not in kw else dev["slopes"].cpu().double()
+    U.check(out, *U.reference(c, q, new, 0.1, kw.get("softcap", 0.0), slopes, window, prefix, first))
+
+
+def test_pages_that_no_row_sees_in_many_sequences():
+    """More row blocks than are listed, half of them without a row that sees anything."""
+    g = np.random.default_rng(9)
+    new = [int(x) for x in g.integers(1, 40, size=400)]
+    lens = [n + int(x) for n, x in zip(new, g.integers(0, 60, size=400))]
+    first = []
+    for b, (L, n) in enumerate(zip(lens, new)):
+        first += [INT_MAX] * n if b % 2 else [int(g.integers(0, L - n + i + 2)) for i in range(n)]
+    c = U.Cache(lens, 2, 64, seed=9)
+    table = unseen(c, lens, new, 0, None, first, "ids")
+    q = randn(10, sum(new), 4, 64)
+    status = ints([0])
+    out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, table, ints(lens), cum(new), max(new), 0.1, first_keys=ints(first), status=status)
+    assert int(status.item()) == 0
+    U.check(out, *U.reference(c, q, new, 0.1, first=first))
