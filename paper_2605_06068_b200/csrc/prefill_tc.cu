@@ -62,7 +62,7 @@ cudaError_t launch(const PrefillParams& p, const PrefillMaps& maps, const Prefil
   if (e != cudaSuccess) return e;
   kernel<<<static_cast<unsigned>(2 * pairs), C::kThreads, C::kSmemBytes, stream>>>(maps, p, plan);
   if ((e = cudaGetLastError()) != cudaSuccess || !plan.cut) return e;
-  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone && !kFp8 ? plan.scale_log2 : 1.f,
+  prefill_merge_kernel<D><<<dim3(static_cast<unsigned>(pairs), 8), 256, 0, stream>>>(p, plan, kShape == kShapeNone && !kFp8 ? plan.scale_log2 : 0.f,
                                                                                        (kShape & kShapeCap) && !(kShape & kShapeBias) ? 0.f : 5.4210109e-20f);
   return cudaGetLastError();
 }

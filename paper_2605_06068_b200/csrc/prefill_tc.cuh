@@ -139,14 +139,20 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
 // cancels in the quotient. c is the scale as long as |c r| < 2^28, where that is at most 2^8. Beyond, scores that differ at
 // all differ by 16 and more there, so that only the largest one weighs anything in 32 bits, and by any c that is large enough:
 // then c is a power of two with 2^31 <= |c r| < 2^32, c r is exact, and other scores are 2^7 and more away.
-// References in the exponent's units have a factor of 1 (far ones again a power of two).
 __device__ __forceinline__ float score_factor(float r, float scale_log2) {
   if (fabsf(r * scale_log2) < 268435456.f) return scale_log2;
   const uint32_t exponent = (__float_as_uint(r) >> 23) & 255u;
   return __uint_as_float(min(127u + 31u + 127u - min(exponent, 254u), 254u) << 23);
 }
-// What weights and sums taken at reference `from` are multiplied by to be those at a reference `to` >= from whose factor is c.
-__device__ __forceinline__ float rescale(float from, float to, float c) { return ex2(__fmul_rn(from, c) - __fmul_rn(to, c)); }
+// What weights and sums taken at reference `from` are multiplied by to be those at a reference `to` >= from: with the factor that the
+// weights were taken with, so that a score of `to` among them, which weighed up to 2^32, comes out as 1, whichever factor `to` goes with.
+// scale_log2 = 0: references in the exponent's units, whose factor is always 1.
+__device__ __forceinline__ float rescale(float from, float to, float scale_log2) {
+  if (scale_log2 == 0.f) return ex2(from - to);
+  const float c = score_factor(from, scale_log2);
+  if (c == score_factor(to, scale_log2)) return ex2(__fmul_rn(from, c) - __fmul_rn(to, c));
+  return ex2(-fmaf(to, c, -__fmul_rn(from, c)));
+}
 
 // O of a warp's rows in tensor memory, times `a` (each row its own). Out of line: it is rare, and the hot loop's code has to stay in the
 // instruction caches.
@@ -962,7 +968,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
     const int w = warp >> 2;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t my_s = tmem + 128 * w + lane_base, my_o = tmem + kGTmemO + 128 * w + lane_base;
-    const float scale_log2 = kExp || kFixed ? 1.f : plan.scale_log2;
+    const float scale_log2 = kExp || kFixed ? 0.f : plan.scale_log2;  // (see rescale)
     const uint32_t to_p = in_cta(bar_p + 16 * w, 0), to_ofree = in_cta(bar_ofree + 8 * w, 0);
     const float neg_inf = -INFINITY;
     // this thread's row of a unit: query token row_token (from the half's first of this CTA), head row_head of the group
@@ -1004,7 +1010,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           key0_pos = static_cast<int>(key0 - pos);
         }
       }
-      c_ref = score_factor(m_ref, scale_log2);
+      c_ref = kExp || kFixed ? 1.f : score_factor(m_ref, scale_log2);
       float l = 0.f;
       // One tile; masked: some row of the warp does not see all of it.
       auto tile = [&](auto masked, int j, int j_key) {  // j_key: which of the half's tiles by its keys
@@ -1257,9 +1263,8 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 if (kExp) {
                   a = raise ? ex2(m_ref - m_new) : 1.f;
                 } else {
-                  const float c_new = score_factor(m_new, scale_log2);
-                  a = rescale(m_ref, m_new, c_new);
-                  c_ref = c_new;
+                  a = rescale(m_ref, m_new, scale_log2);
+                  c_ref = score_factor(m_new, scale_log2);
                 }
                 m_ref = m_new;
                 l *= a;
@@ -1309,8 +1314,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
         const float2 other = *reinterpret_cast<const float2*>(sums);
         if (kFixed && l == 0.f) m_ref = kGNoMax;
         const float m = fmaxf(m_ref, other.x);
-        const float c_new = score_factor(m, scale_log2);
-        const float mul = rescale(m_ref, m, c_new), mul_other = rescale(other.x, m, c_new);
+        const float mul = rescale(m_ref, m, scale_log2), mul_other = rescale(other.x, m, scale_log2);
         m_ref = m;
         l = l * mul + other.y * mul_other;
 #pragma unroll 1
@@ -1425,7 +1429,6 @@ __global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constan
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     bad = __any_sync(0xffffffffu, bad);
-    const float c = score_factor(m, scale_log2);
     float acc[kCols], l = 0.f;
 #pragma unroll
     for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
@@ -1433,7 +1436,7 @@ __global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constan
     for (int k = 0; k < rec.parts; ++k) {
       const float2 s = sums[static_cast<int64_t>(k) * kPreRows];
       if (bad || s.y == 0.f) continue;  // (nothing of this row in that part)
-      const float mul = rescale(s.x, m, c);
+      const float mul = rescale(s.x, m, scale_log2);
       const float* o = reinterpret_cast<const float*>(ws) + (at + static_cast<int64_t>(k) * kPreRows) * D + kCols * lane;
       l = fmaf(s.y, mul, l);
       if constexpr (kCols == 4) {

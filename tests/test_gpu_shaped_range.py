@@ -340,3 +340,43 @@ def test_pages_that_no_row_sees_in_many_sequences():
     out = pda.paged_prefill_attention(q.cuda(), c.k_cache, c.v_cache, table, ints(lens), cum(new), max(new), 0.1, first_keys=ints(first), status=status)
     assert int(status.item()) == 0
     U.check(out, *U.reference(c, q, new, 0.1, first=first))
+
+
+# ---- sums that are joined ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("shape", ["plain", "bias", "e4m3"])
+@pytest.mark.parametrize("L", [300, 4000])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_equal_scores_of_2_28_in_different_shares(shape, L, sign):
+    """The largest score stands twice, in shares of the keys that are joined afterwards (the halves of a block, or parts of it): both
+    weigh the same. In one of them a score that is less by one step came first, and the sums are relative to that one."""
+    D, fp8, hidden = 128, shape == "e4m3", -15 * 2 ** 25
+    # z = c s passes 2^28 from a score to the next one, 32 further on
+    for scale in np.arange(0.6925, 0.6929, 1e-7, dtype=np.float32):
+        factor = float(np.float32(1.4426950408889634 * float(scale)))
+        top = -(-int(2 ** 28 / factor) // 32) * 32
+        if 0 <= top * factor - 2 ** 28 < 4 and (top - 32) * factor < 2 ** 28 - 20:
+            break
+    else:
+        raise AssertionError("no such scale")
+    where = {10: top - 32, 100: top, L - 5: top} if sign > 0 else {10: -top, 100: 32 - top, L - 5: 32 - top}
+    # products that add up to a score exactly: digits to the base 16 of score / 32 as keys, their places' values as the query
+    c = U.Cache([L], 1, D, seed=2)
+    rows = torch.zeros(c.k_cache.shape)
+    for j in range(L):
+        s = abs(where.get(j, hidden)) // 32
+        for d in range(6):
+            rows[int(c.table[0, j // 16]), 0, j % 16, d] = (s >> 4 * d & 15) * (1 if where.get(j, hidden) > 0 else -1)
+    values = torch.where(c.v_cache.cpu().isnan(), 0.0, c.v_cache.cpu().float())
+    q = torch.zeros((3, 2, D), dtype=torch.bfloat16)
+    q[:, :, :6] = torch.tensor([32.0 * 16 ** d for d in range(6)])
+    dtype, kw = (U.E4M3, dict(k_scale=torch.ones((rows.shape[0], 1), device="cuda"), v_scale=torch.ones((rows.shape[0], 1), device="cuda"))) if fp8 else (torch.bfloat16, {})
+    if shape == "bias":
+        kw["slopes"] = torch.zeros(2, device="cuda")
+    k_cache, v_cache = rows.to(dtype).cuda(), values.to(dtype).cuda()
+    out = pda.paged_prefill_attention(q.cuda(), k_cache, v_cache, c.dev_table, ints([L]), ints([0, 3]), 3, float(scale), **kw)
+    host = v_cache.cpu().double()
+    a, b = (host[int(c.table[0, j // 16]), 0, j % 16] for j in (100, L - 5))
+    ref = ((a + b) / 2)[None, None].expand(3, 2, D)
+    # the third score weighs 2^-30 of the others at most
+    U.check(out, ref, 1.01 * (U.EPS * ref.abs() + (2 * U.EPS + L * 2.0 ** -24 + 2.0 ** -12) * ((a.abs() + b.abs()) / 2)[None, None]) + 2.0 ** -24, "joined")
