@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import functools
 import ctypes as C
+import operator
 import os
 
 import torch
@@ -721,11 +722,6 @@ def _rows_of(name, t, tokens, heads, head_dim):
     return _row_layout(name, t.shape, t.stride(), tokens, heads, head_dim)
 
 
-@functools.lru_cache(maxsize=64)
-def _axis_bytes(freq_axis):
-    return bytes(freq_axis)
-
-
 def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_norm=None, k_norm=None, eps=1e-6, interleaved=False,
                    freq_axis=None, out=None, k_scale=None, v_scale=None, status=None, stream=None):
     """A step's queries, keys and values ``[T, heads, D]`` as the projection leaves them: root-mean-square norm of each query
@@ -734,7 +730,7 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
 
     ``cos_sin`` float32 ``[positions, rot_dim]``: cosines, then sines, of each position's ``rot_dim / 2`` angles; None: no
     rotation. ``positions`` int32 ``[T]``, or ``[axes, T]`` with ``freq_axis``, the axis of each of the ``rot_dim / 2``
-    frequencies (a sequence of ints on the host; a tuple or bytes is taken fastest). e4m3 caches take ``k_scale``/``v_scale``
+    frequencies (a sequence of ints on the host; bytes are taken fastest). e4m3 caches take ``k_scale``/``v_scale``
     ``[pages, Hkv]``, which are updated."""
     T, Hq, D = q.shape
     desc = _paged_caches(k_cache, v_cache, k_scale, v_scale, D)
@@ -766,7 +762,7 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
             if freq_axis is None and axes > 1:
                 raise ValueError("freq_axis: needed for positions of several axes")
         if freq_axis is not None:
-            axis = freq_axis if type(freq_axis) is bytes else _axis_bytes(tuple(freq_axis))
+            axis = freq_axis if type(freq_axis) is bytes else bytes(tuple(freq_axis))
             if len(axis) != rot // 2 or (len(axis) and max(axis) >= axes):
                 raise ValueError("freq_axis: expected an axis for each of the rot_dim / 2 frequencies")
     else:
@@ -783,6 +779,8 @@ def rope_kv_append(q, k, v, positions, cos_sin, k_cache, v_cache, slot_map, q_no
 
 
 def _score_desc(scale, softcap, slopes, window, num_q_heads):
+    # (as plain numbers: a tensor of one element may hold another value at the next call)
+    scale, softcap, window = float(scale), float(softcap), operator.index(window)
     if slopes is None:
         return _plain_score(scale, softcap, window)
     if slopes.dtype is not torch.float32 or slopes.numel() != num_q_heads or not slopes.is_contiguous():
