@@ -297,6 +297,7 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
     scale_log2 = shape.score.mul;
     scores.cap = shape.score.cap;
     scores.rate = shape.score.rate;
+    scores.e0 = scores.e1 = kNoValue;
     const float* slopes = shape.score.slopes;
     const int head = g * p.group + 8 * part + 2 * tq;
     scores.slope0 = slopes != nullptr && 2 * tq < G ? slopes[head] * kLog2e : 0.f;
@@ -381,6 +382,11 @@ attention_tma_kernel(const __grid_constant__ CUtensorMap k_map,
   if constexpr (Shape::kShaped) {  // a NaN among the row's weights is above all of them, so that it gets through the merges
     if (l0 != l0) m0 = INFINITY;
     if (l1 != l1) m1 = INFINITY;
+    if constexpr (kFp8) {  // O in units of the largest weight from here on
+      const float a0 = ex2(scores.e0), a1 = ex2(scores.e1);
+#pragma unroll
+      for (int i = 0; i < C::kKSteps; ++i) { o[i][0] *= a0; o[i][1] *= a1; o[i][2] *= a0; o[i][3] *= a1; }
+    }
   }
   float* mo = reinterpret_cast<float*>(smem + warp * C::kWarpRing);
   float* mm = mo + 8 * C::kOStride;  // m[8] then l[8]

@@ -43,6 +43,8 @@ __device__ __forceinline__ void load_q_fragments(const __nv_bfloat16* q_rows, in
   }
 }
 
+constexpr float kNoValue = -1e30f;  // e0, e1 before any value
+
 // Shapes of the scores that a tile's products go through on their way to the softmax. PlainScores: none.
 struct PlainScores {
   static constexpr bool kShaped = false;
@@ -52,6 +54,9 @@ struct PlainScores {
 struct ShapedScores {
   static constexpr bool kShaped = true;
   float cap, rate, slope0, slope1, dist;
+  // e4m3: weights are held in fp16 together with their page's value scale, which may be of any size: relative to the largest such
+  // product of the head so far, which is 2^e of the head's largest weight. O is in these units.
+  float e0, e1;
   __device__ __forceinline__ float operator()(float z, float slope, int row) const {
     if (cap > 0.f) z = cap_score(z, cap, rate);
     return fmaf(-slope, dist - static_cast<float>(row), z);
@@ -62,11 +67,11 @@ struct ShapedScores {
 // swizzled lines); rows [n_skip, n_valid) of the tile are attended; sc = scale * log2(e)
 // (* k_scale for e4m3), vsc = v_scale (1 for bf16). (m, l) are this thread's running maxima and
 // partial sums for heads 2tq and 2tq+1; o is the O^T accumulator fragment. Warp-collective.
-template <int D, bool kFp8, class Scores = PlainScores>
+template <int D, bool kFp8, class Scores>
 __device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_valid, int n_skip, float sc,
                                             float vsc, const uint32_t (&qf)[D / 16][2], float& m0,
                                             float& m1, float& l0, float& l1, float (&o)[D / 16][4],
-                                            int lane, const Scores& shape = Scores{}) {
+                                            int lane, Scores& shape) {
   constexpr int kKSteps = D / 16;
   constexpr int kRowBytes = D * (kFp8 ? 1 : 2);
   constexpr int kPageSize = 16;
@@ -139,20 +144,37 @@ __device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_vali
       mn1 = mn1 == -INFINITY ? -FLT_MAX : mn1;
     }
     const float al0 = ex2(m0 - mn0), al1 = ex2(m1 - mn1);     // ex2(-inf) = 0 on the first tile
+    [[maybe_unused]] const float m0_before = m0, m1_before = m1;
     m0 = mn0; m1 = mn1;
     const float p0 = ex2(s0 - mn0), p1 = ex2(s1 - mn1), p2 = ex2(s2 - mn0), p3 = ex2(s3 - mn1);
     l0 = fmaf(l0, al0, p0 + p2);
     l1 = fmaf(l1, al1, p1 + p3);
-    const uint32_t pb0 = movmatrix_trans(pack2<kFp8>(p0 * vsc, p1 * vsc));   // P^T rows: tokens 0-7
-    const uint32_t pb1 = movmatrix_trans(pack2<kFp8>(p2 * vsc, p3 * vsc));   // tokens 8-15
+    float ao0 = al0, ao1 = al1;  // O's factors
+    uint32_t pb0, pb1;           // P^T rows: tokens 0-7, 8-15
+    if constexpr (Scores::kShaped && kFp8) {
+      // (differences are taken of scores first: they are exact however large the scores are)
+      const float lv = __log2f(fabsf(vsc));  // (0: -inf, and no weight)
+      const float was0 = shape.e0 + (m0_before - mn0), was1 = shape.e1 + (m1_before - mn1);
+      shape.e0 = fmaxf(fmaxf(was0, (mx0 - mn0) + lv), kNoValue);
+      shape.e1 = fmaxf(fmaxf(was1, (mx1 - mn1) + lv), kNoValue);
+      ao0 = ex2(was0 - shape.e0);
+      ao1 = ex2(was1 - shape.e1);
+      const float up0 = lv - shape.e0, up1 = lv - shape.e1;
+      const uint32_t sign = vsc < 0.f ? 0x80008000u : 0u;
+      pb0 = movmatrix_trans(pack2<true>(ex2((s0 - mn0) + up0), ex2((s1 - mn1) + up1)) ^ sign);
+      pb1 = movmatrix_trans(pack2<true>(ex2((s2 - mn0) + up0), ex2((s3 - mn1) + up1)) ^ sign);
+    } else {
+      pb0 = movmatrix_trans(pack2<kFp8>(p0 * vsc, p1 * vsc));
+      pb1 = movmatrix_trans(pack2<kFp8>(p2 * vsc, p3 * vsc));
+    }
 
     // ---- O^T = O^T * alpha + V^T . P^T
     // (after the first tiles of a unit the running maxima seldom move: alpha is exactly 1 then, and the
     // 4 D / 16 multiplications are skipped when it is for the whole warp)
-    if (__any_sync(0xffffffffu, (al0 != 1.f) | (al1 != 1.f))) {
+    if (__any_sync(0xffffffffu, (ao0 != 1.f) | (ao1 != 1.f))) {
 #pragma unroll
       for (int mt = 0; mt < kKSteps; ++mt) {
-        o[mt][0] *= al0; o[mt][1] *= al1; o[mt][2] *= al0; o[mt][3] *= al1;
+        o[mt][0] *= ao0; o[mt][1] *= ao1; o[mt][2] *= ao0; o[mt][3] *= ao1;
       }
     }
     if (!kFp8) {
@@ -180,6 +202,14 @@ __device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_vali
       }
     }
 
+}
+
+template <int D, bool kFp8>
+__device__ __forceinline__ void decode_tile(uint32_t kt, uint32_t vt, int n_valid, int n_skip, float sc,
+                                            float vsc, const uint32_t (&qf)[D / 16][2], float& m0,
+                                            float& m1, float& l0, float& l1, float (&o)[D / 16][4], int lane) {
+  PlainScores plain;
+  decode_tile<D, kFp8, PlainScores>(kt, vt, n_valid, n_skip, sc, vsc, qf, m0, m1, l0, l1, o, lane, plain);
 }
 
 }  // namespace pda

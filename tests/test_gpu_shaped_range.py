@@ -380,3 +380,45 @@ def test_equal_scores_of_2_28_in_different_shares(shape, L, sign):
     ref = ((a + b) / 2)[None, None].expand(3, 2, D)
     # the third score weighs 2^-30 of the others at most
     U.check(out, ref, 1.01 * (U.EPS * ref.abs() + (2 * U.EPS + L * 2.0 ** -24 + 2.0 ** -12) * ((a.abs() + b.abs()) / 2)[None, None]) + 2.0 ** -24, "joined")
+
+
+# ---- e4m3 decoding: value scales of any size --------------------------------------------------------
+
+@pytest.mark.parametrize("vscale", [2.0 ** -8, 2.0 ** -14, 2.0 ** -22, 2.0 ** -40, 2.0 ** -90, 2.0 ** 8, 2.0 ** 40, "pages"])
+@pytest.mark.parametrize("kw", [dict(), dict(softcap=20.0), dict(slopes=[0.02, 0.0, 0.3, 0.001])])
+def test_decode_value_scales_of_any_size(vscale, kw):
+    """Weights are held in 16 bits together with the value scale: relative to the largest of the products."""
+    lens, Hq, Hkv, D = [1, 17, 300, 3000], 4, 2, 128
+    c = U.Cache(lens, Hkv, D, fp8=True, seed=11)
+    g = np.random.default_rng(12)
+    per_page = torch.as_tensor(2.0 ** g.uniform(-60, 20, size=c.v_scale.shape) if vscale == "pages" else np.full(c.v_scale.shape, vscale)).float()
+    if vscale == "pages":
+        per_page[::3] = 0.0                        # (pages of zeros may have any scale)
+    stored = c.scales[1]
+    for b, L in enumerate(lens):
+        pages = torch.as_tensor(c.table[b].astype(np.int64))[torch.arange(L) // 16]
+        c.v[b] = c.v[b] / stored[pages].double()[:, :, None] * per_page[pages].double()[:, :, None]
+    c.v_scale = per_page.cuda()
+    q = randn(13, len(lens), Hq, D, scale=2.0)
+    scale = D ** -0.5
+    dev = dict(kw, slopes=torch.tensor(kw["slopes"], device="cuda")) if "slopes" in kw else kw
+    status = ints([0])
+    for chunk in (0, 64):
+        parts = dict(chunk_tokens=64, part_o=nan(4, Hq, 47, D), part_lse=nan(4, Hq, 47), workspace=pda.new_workspace(4, Hkv)) if chunk else {}
+        out = pda.paged_biased_decode_attention(q.cuda(), c.k_cache, c.v_cache, c.dev_table, ints(lens), scale, status=status, **c.args(), **dev, **parts)
+        assert int(status.item()) == 0
+        for b, L in enumerate(lens):
+            pages = torch.as_tensor(c.table[b].astype(np.int64))[torch.arange(L) // 16]
+            dist = (L - 1 - torch.arange(L)).double()
+            for h in range(Hq):
+                k, v = c.k[b][:, h // 2], c.v[b][:, h // 2]
+                ref, tol = U.attend(q[b:b + 1, h], k, v, torch.tensor([0]), torch.tensor([L]), torch.tensor([L - 1]), scale, kw.get("softcap", 0.0),
+                                    0.0 if "slopes" not in kw else float(dev["slopes"][h]))
+                # each product w_j scale_j off by half a step of 2^-24 of the largest such product, times the byte
+                s = (q[b, h].double() @ k.T) * scale
+                s = kw["softcap"] * torch.tanh(s / kw["softcap"]) if "softcap" in kw else s
+                w = torch.softmax(s - (0.0 if "slopes" not in kw else float(dev["slopes"][h])) * dist, 0)
+                product = w * per_page[pages, h // 2].double()
+                byte = torch.where(per_page[pages, h // 2][:, None] > 0, v / per_page[pages, h // 2].double()[:, None], 0.0).abs()
+                step = 2.0 ** -25 * product.max() * byte.sum(0, keepdim=True) * 1.01
+                U.check(out[b:b + 1, h], ref, tol + step + 1e-38, f"{vscale} sequence {b} head {h} chunk {chunk}")
