@@ -128,11 +128,6 @@ __device__ __forceinline__ void exp2_two(uint64_t x, float& w0, float& w1) {
   w1 = __uint_as_float(__float_as_uint(w1) + (__float_as_uint(t1) << 23));
 }
 __device__ __forceinline__ uint32_t bits_before(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 
 // Scores that are not shaped stay as they come from the product: weights are 2^(c s - c r), s the scores and r the
 // reference, by one fused multiply-add with c r rounded: off by half a step of c r, the same for all of the row, so it
@@ -224,7 +219,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
   uint32_t* work = reinterpret_cast<uint32_t*>(bars + C::kBars);    // [kGMaxList] tiles, then units of the entries before
   uint32_t* list = work + kGMaxList;                                // [kGMaxList] sequence and block, most work first
   GUnit* units = reinterpret_cast<GUnit*>(list + kGMaxList);        // [kGUnitSlots]
-  uint32_t* scan = reinterpret_cast<uint32_t*>(units + kGUnitSlots);  // [4] by warp
+  uint32_t* scan = reinterpret_cast<uint32_t*>(units + kGUnitSlots);  // [kGMaxList / 32] by warp, then the sum of all
   uint32_t* tmem_slot = scan + kGMaxList / 32 + 1;
   int* cta_err = reinterpret_cast<int*>(tmem_slot + 1);
   uint32_t* target_sh = reinterpret_cast<uint32_t*>(cta_err + 1);   // tiles of a part

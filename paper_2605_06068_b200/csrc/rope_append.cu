@@ -34,11 +34,6 @@ __device__ __forceinline__ Pairs unpack(const uint4& a, const uint4& b) {
   for (int e = 0; e < 8; ++e) r.x[e] = f32x2(w[e] << 16, w[e] & 0xffff0000u);
   return r;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ uint64_t both(float v) { return f32x2(__float_as_uint(v), __float_as_uint(v)); }
 __device__ __forceinline__ uint32_t to_bf16(uint64_t v) {
   float lo, hi;
@@ -129,14 +124,14 @@ struct Lane {
       if constexpr (kPairs) {
         float w0, w1;
         f32x2_split(w.x[e], w0, w1);
-        f.a[e] = mul2(w.x[e], both(c[e]));
+        f.a[e] = mul_f32x2(w.x[e], both(c[e]));
         f.b[e] = f32x2(__float_as_uint(-s[e] * w1), __float_as_uint(s[e] * w0));
       } else {
         const int k = 2 * (e & 3);
         const uint64_t c2 = f32x2(__float_as_uint(c[k]), __float_as_uint(c[k + 1]));
         const uint64_t s2 = f32x2(__float_as_uint(s[k]), __float_as_uint(s[k + 1])), minus_s2 = f32x2(__float_as_uint(-s[k]), __float_as_uint(-s[k + 1]));
-        f.a[e] = mul2(w.x[e], c2);
-        f.b[e] = mul2(w.x[e ^ 4], e < 4 ? minus_s2 : s2);
+        f.a[e] = mul_f32x2(w.x[e], c2);
+        f.b[e] = mul_f32x2(w.x[e ^ 4], e < 4 ? minus_s2 : s2);
       }
     }
     return f;
@@ -164,9 +159,9 @@ struct Lane {
         f32x2_split(x.x[e], lo, hi);
         partner = f32x2(__float_as_uint(hi), __float_as_uint(lo));
       }
-      y.x[e] = mul2(x.x[e], f.a[e]);
+      y.x[e] = mul_f32x2(x.x[e], f.a[e]);
       if (rotated) y.x[e] = fma_f32x2(partner, f.b[e], y.x[e]);
-      if (normed) y.x[e] = mul2(y.x[e], both(inv));
+      if (normed) y.x[e] = mul_f32x2(y.x[e], both(inv));
     }
     return y;
   }

@@ -120,7 +120,7 @@ struct RopeAppendParams {
       qo_head_stride, positions_stride;
   CacheGeom geom;
   float eps, inv_dim;  // 1 / head_dim
-  int32_t n_tokens, num_q_heads, table_len, rot_dim, num_axes, axes_used;  // axes_used: bit a for axis a
+  int32_t n_tokens, num_q_heads, table_len, rot_dim, axes_used;  // axes_used: bit a for axis a
   alignas(4) uint8_t freq_axis[128];
 };
 
