@@ -22,15 +22,15 @@ bool encode_q(CUtensorMap* map, const PrefillParams& p, int tile_rows) {
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The polynomials of the cap in the product s: C tanh(u s), u = scale / softcap. The first one's coefficients hold the powers of u:
-// where u is so far from 1 that they or the powers of s could leave 32 bits' range, all go to the second.
+// The polynomials of the cap in the product s: C tanh(u s), u = scale / softcap. Where u is so far from 1 that powers of u or
+// of s could leave 32 bits' range, all go the other way.
 void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
   // tanh(x) by odd polynomials whose largest error over the range is least (linear programming over 4000 points):
   // 5.3e-6 for |x| <= 1/2, 2.4e-6 for |x| <= 5/4
   static const double c5[3] = {0.9999248385429382, -0.33085504174232483, 0.11254137754440308};
   static const double c11[6] = {0.9999746680259705, -0.33283931016921997, 0.1305362582206726, -0.04692675918340683, 0.01253201998770237,
                                 -0.0016820720629766583};
-  // above kAbsoluteCap, for |x| <= 3/4: see cap_score
+  // above kAbsoluteCap: see cap_score
   static const float relative[6] = PDA_TANH_COEFFICIENTS;
   const double u = static_cast<double>(score.mul) / score.cap;
   const auto twice = [](double v) {
@@ -41,16 +41,16 @@ void set_cap(const ScoreParams& score, int shape, PrefillPlan* plan) {
   };
   plan->relative = score.cap > kAbsoluteCap;
   plan->u = static_cast<float>(u);
-  const bool usable = std::abs(u) >= 1.0 / 1024 && std::abs(u) <= 1024 && !plan->relative && score.cap >= 1.f / 4096;
+  const bool usable = std::abs(u) >= 1.0 / 2048 && std::abs(u) <= 1024 && !plan->relative && score.cap >= 1.f / 4096;
   plan->limit[0] = usable ? static_cast<float>(0.5 / std::abs(u)) : -1.f;
-  plan->limit[1] = static_cast<float>((plan->relative ? static_cast<double>(kTanhReach) : 1.25) / std::abs(u));
+  plan->limit[1] = usable ? static_cast<float>(1.25 / std::abs(u)) : -1.f;
   plan->ref = shape & kShapeBias ? 0.f : std::max(score.cap - kGFixedTop, 0.f);
   plan->ref_low = std::min(score.cap - kGFixedLow, plan->ref);
   plan->low_limit = static_cast<float>(std::max(static_cast<double>(kGFixedFloor) - plan->ref, 0.0) / std::abs(static_cast<double>(score.mul)));  // (weights below 2^-60)
   double power = score.mul;
   for (int i = 0; i < 6; ++i, power *= u * u) {
     if (i < 3) plan->poly5[i] = twice(usable ? c5[i] * power : 0.0);
-    plan->poly11[i] = twice((plan->relative ? relative[i] : c11[i]) * score.mul);
+    plan->poly11[i] = twice(plan->relative ? relative[i] * static_cast<double>(score.mul) : usable ? c11[i] * power : 0.0);
   }
 }
 

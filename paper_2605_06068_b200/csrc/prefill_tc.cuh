@@ -33,10 +33,10 @@ struct PrefillPlan {
   int64_t slots;  // (not listed) row blocks are looked for at this many places
   int cut;        // few units: blocks are cut along the keys, so that every pair has a part
   float scale_log2;
-  // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): for |s| <= limit[0] of degree 5 in s;
-  // for |s| <= limit[1] of degree 10 in u s, u = scale / softcap, times s. ref: the fixed reference (capped only), or 0; ref_low: that of rows with low scores,
+  // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): of degree 5 for
+  // |s| <= limit[0], of degree 11 for |s| <= limit[1]; u = scale / softcap. ref: the fixed reference (capped only), or 0; ref_low: that of rows with low scores,
   // whose products are above low_limit in size. relative:
-  // the second polynomial's error goes with the score, and beyond it scores are taken one by one.
+  // poly11 is that of cap_score, in u s, times s, and scores are taken one by one.
   float limit[2], ref, ref_low, low_limit, u;
   int relative;
   uint64_t poly5[3], poly11[6];
@@ -134,8 +134,9 @@ __device__ __forceinline__ uint32_t bits_before(int n) { return n >= 32 ? 0xffff
 // cancels in the quotient. c is the scale as long as |c r| < 2^28, where that is at most 2^8. Beyond, scores that differ at
 // all differ by 16 and more there, so that only the largest one weighs anything in 32 bits, and by any c that is large enough:
 // then c is a power of two with 2^31 <= |c r| < 2^32, c r is exact, and other scores are 2^7 and more away.
+constexpr float kGFar = 268435456.f;
 __device__ __forceinline__ float score_factor(float r, float scale_log2) {
-  if (fabsf(r * scale_log2) < 268435456.f) return scale_log2;
+  if (fabsf(r * scale_log2) < kGFar) return scale_log2;
   const uint32_t exponent = (__float_as_uint(r) >> 23) & 255u;
   return __uint_as_float(min(127u + 31u + 127u - min(exponent, 254u), 254u) << 23);
 }
@@ -144,6 +145,8 @@ __device__ __forceinline__ float score_factor(float r, float scale_log2) {
 // scale_log2 = 0: references in the exponent's units, whose factor is always 1.
 __device__ __forceinline__ float rescale(float from, float to, float scale_log2) {
   if (scale_log2 == 0.f) return ex2(from - to);
+  const float z_from = __fmul_rn(from, scale_log2), z_to = __fmul_rn(to, scale_log2);
+  if (fabsf(z_from) < kGFar && fabsf(z_to) < kGFar) return ex2(z_from - z_to);  // (nearly always)
   const float c = score_factor(from, scale_log2);
   if (c == score_factor(to, scale_log2)) return ex2(__fmul_rn(from, c) - __fmul_rn(to, c));
   return ex2(-fmaf(to, c, -__fmul_rn(from, c)));
@@ -1078,8 +1081,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               // 1), others, and infinities and NaN, by exponential and reciprocal: three results of the special-function unit a
               // score with the weight's. A warp takes one of the polynomials, the longer one if any of its rows asks for it.
               // Where the reference is fixed, the weights are taken right behind it.
-              // Caps above kAbsoluteCap take polynomials whose error goes with the score (cap_score), since scores may be far
-              // below the cap, and a row with larger products takes each of its scores the way that is its own.
+              // Above kAbsoluteCap each score is taken by itself as in cap_score, since scores may be far below the cap.
               if (kMasked) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e) sv[e] = hidden(e) ? 0u : sv[e];
@@ -1109,8 +1111,7 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                   }
                 }
               };
-              auto poly11 = [&](uint64_t x) {  // (of x^2 before it is multiplied by x)
-                const uint64_t ux = mul_f32x2(x, both(plan.u)), t2 = mul_f32x2(ux, ux);
+              auto poly11 = [&](uint64_t t2) {
                 uint64_t y = fma_f32x2(t2, plan.poly11[5], plan.poly11[4]);
                 y = fma_f32x2(t2, y, plan.poly11[3]);
                 y = fma_f32x2(t2, y, plan.poly11[2]);
@@ -1127,14 +1128,15 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
                 });
               } else if (far <= plan.limit[1]) {
                 capped([&](uint64_t x) {
-                  const uint64_t y = poly11(x);
+                  const uint64_t y = poly11(mul_f32x2(x, x));
                   return kFixed ? fma_f32x2(x, y, minus_ref) : mul_f32x2(x, y);
                 });
               } else if (!kFixed && plan.relative) {
                 capped([&](uint64_t x) {
                   float x0, x1, z0, z1;
-                  f32x2_split(mul_f32x2(x, both(plan.u)), x0, x1);
-                  f32x2_split(mul_f32x2(x, poly11(x)), z0, z1);
+                  const uint64_t ux = mul_f32x2(x, both(plan.u));
+                  f32x2_split(ux, x0, x1);
+                  f32x2_split(mul_f32x2(x, poly11(mul_f32x2(ux, ux))), z0, z1);
                   auto far_one = [&](float v) { return fmaf(-p.score.cap, 2.f * rcp_approx(ex2(2.f * kLog2e * v) + 1.f), p.score.cap); };
                   if (!(fabsf(x0) <= kTanhReach)) z0 = far_one(x0);
                   if (!(fabsf(x1) <= kTanhReach)) z1 = far_one(x1);
@@ -1414,32 +1416,45 @@ __global__ void __launch_bounds__(256) prefill_merge_kernel(const __grid_constan
     if (token >= plan.tile_rows || row >= rec.nq) continue;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kPreRows + r;
     const float2* sums = reinterpret_cast<const float2*>(ws + prefill_sums_at(D)) + at;
-    float m = kGNoMax;
+    // A lane takes every 32nd part's reference and sum (parts are kPreMaxPairs at most), and their factors.
+    constexpr int kRounds = (kPreMaxPairs + 31) / 32;
+    float2 sum[kRounds];
+    float m = kGNoMax, l = 0.f;
     bool bad = false;
-    for (int k = lane; k < rec.parts; k += 32) {
-      const float2 s = sums[static_cast<int64_t>(k) * kPreRows];
-      m = fmaxf(m, s.y != 0.f ? s.x : kGNoMax);
-      bad |= s.y < 0.f;
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      sum[i] = 32 * i + lane < rec.parts ? sums[static_cast<int64_t>(32 * i + lane) * kPreRows] : make_float2(kGNoMax, 0.f);
+      m = fmaxf(m, sum[i].y != 0.f ? sum[i].x : kGNoMax);
+      bad |= sum[i].y < 0.f;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     bad = __any_sync(0xffffffffu, bad);
-    float acc[kCols], l = 0.f;
+    float mul[kRounds], acc[kCols];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      mul[i] = bad || sum[i].y == 0.f ? 0.f : rescale(sum[i].x, m, scale_log2);  // (nothing of this row in that part)
+      l = fmaf(sum[i].y, mul[i], l);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
 #pragma unroll
     for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int n = min(rec.parts - 32 * i, 32);
 #pragma unroll 4
-    for (int k = 0; k < rec.parts; ++k) {
-      const float2 s = sums[static_cast<int64_t>(k) * kPreRows];
-      if (bad || s.y == 0.f) continue;  // (nothing of this row in that part)
-      const float mul = rescale(s.x, m, scale_log2);
-      const float* o = reinterpret_cast<const float*>(ws) + (at + static_cast<int64_t>(k) * kPreRows) * D + kCols * lane;
-      l = fmaf(s.y, mul, l);
-      if constexpr (kCols == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(o);
-        acc[0] = fmaf(v.x, mul, acc[0]), acc[1] = fmaf(v.y, mul, acc[1]), acc[2] = fmaf(v.z, mul, acc[2]), acc[3] = fmaf(v.w, mul, acc[3]);
-      } else {
-        const float2 v = *reinterpret_cast<const float2*>(o);
-        acc[0] = fmaf(v.x, mul, acc[0]), acc[1] = fmaf(v.y, mul, acc[1]);
+      for (int k = 0; k < n; ++k) {
+        const float a = __shfl_sync(0xffffffffu, mul[i], k);
+        if (a == 0.f) continue;  // (what stands there may be anything)
+        const float* o = reinterpret_cast<const float*>(ws) + (at + static_cast<int64_t>(32 * i + k) * kPreRows) * D + kCols * lane;
+        if constexpr (kCols == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(o);
+          acc[0] = fmaf(v.x, a, acc[0]), acc[1] = fmaf(v.y, a, acc[1]), acc[2] = fmaf(v.z, a, acc[2]), acc[3] = fmaf(v.w, a, acc[3]);
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(o);
+          acc[0] = fmaf(v.x, a, acc[0]), acc[1] = fmaf(v.y, a, acc[1]);
+        }
       }
     }
     const bool zero = bad || l == 0.f;
