@@ -612,7 +612,9 @@ int latent_prefill_attention(const void* q, int64_t q_token_stride, int64_t q_he
  *     s = softcap * tanh(s / softcap)          if softcap > 0
  *     s = s - slopes[h] * |p - j|              if slopes
  * in 32 bits, and the softmax is over the keys that the token sees. window > 0: among them only
- * j > p - window. scale finite, softcap finite and >= 0, slopes finite. */
+ * j > p - window. scale finite, softcap finite and >= 0, slopes finite; log2(e) scale, log2(e) softcap and
+ * 2 log2(e) scale / softcap within 32 bits' range too. A cap of any size is off by 2^-20 of the score at most,
+ * one up to 128 by 2^-17 of the cap besides. */
 typedef struct pda_score_desc {
   float scale;
   float softcap;        /* 0: none */
@@ -682,7 +684,8 @@ int rope_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride,
  * Rows that see nothing (p < 0, lo >= hi) are zero. Rows of out outside all sequences are left as they
  * were, and rows of q outside all sequences may hold anything. Slots that hold no token < L, unused pages
  * and table entries of pages that no token sees may hold anything; the values of all tokens < L in
- * pages that are seen must be finite (and on the tensor-core kernel below 2^64 in size). A row with a NaN or +inf among the scores it sees is NaN;
+ * pages that are seen must be finite (and on the tensor-core kernel below 2^64 in size; e4m3 value scales
+ * there 0 or at least 2^-56). A row with a NaN or +inf among the scores it sees is NaN;
  * one with none above -inf is NaN or zero. L < 0 counts as 0. A sequence whose query range does not
  * lie in the arrays, that has more than max_q query tokens or more than block_table_stride * 16 or
  * 2^30 tokens is zeroed (as far as its rows lie within the array and max_q) with PDA_DEV_BAD_SEQ_LEN; rows for
@@ -711,7 +714,8 @@ int64_t pda_prefill_workspace_bytes(int32_t num_q_heads, int32_t head_dim);
  *   first_keys   int32[batch] or NULL
  *   chunk_tokens 0: one unit per (sequence, kv head); > 0 (a multiple of 16): split into chunks of at most
  *                so many tokens, with part_o, part_lse and max_chunks as in paged_decode_attention; they are
- *                scratch, and the merge runs inside this call
+ *                scratch, and the merge runs inside this call. Chunks are joined by their log-sum-exp in 32
+ *                bits: beside the largest scores' size s a chunk's weight is off by 2^-23 s at most
  *   workspace    (chunk_tokens > 0) int32[pda_workspace_ints(batch, num_kv_heads * ceil(group / 8))] as in
  *                paged_decode_step: zeroed by the caller once, left zeroed, one per stream of overlapping
  *                calls. NULL: the merge is a launch of its own
@@ -719,7 +723,8 @@ int64_t pda_prefill_workspace_bytes(int32_t num_q_heads, int32_t head_dim);
  * `out` is always written: zeros where nothing is seen (an empty sequence). What is not seen may hold
  * anything, in pages that are read too. NaN and infinite scores, lengths and page ids as in
  * paged_prefill_attention. bf16 with head_dim 64, 128 and 256 and e4m3 with head_dim 128 run on the TMA +
- * tensor-core kernel (there |q| must stay below 65504 for e4m3), groups above 8 heads as several units; other
+ * tensor-core kernel (there e4m3 takes queries in fp16: |q| below 65504, in
+ * steps of 2^-24 below 2^-14), groups above 8 heads as several units; other
  * shapes on a plain kernel, which does not split. */
 int paged_biased_decode_attention(const void* q, const void* k_cache, const void* v_cache,
                                   const pda_cache_desc* desc, const float* k_scale,

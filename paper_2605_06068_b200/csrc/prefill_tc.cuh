@@ -11,9 +11,9 @@
 // the row's maximum passes it by more than 2^32; row sums are kept by the row's thread, of the 32-bit weights.
 // Warps of each CTA: 0-3, 4-7 softmax of the halves, 8 TMA producer, 9 and 10 MMA issue of the halves (in the pair's first
 // CTA; 9: TMEM), 11 hands V tiles on, clearing what lies behind the sequence's end. All waits are bounded.
-// Measured (B200, 32 query and 8 kv heads of 128): a prompt of 8192 tokens 449 us (1.22 PFLOP/s), capped 517, biased 538, e4m3 617;
-// 24 prompts of 1..700 tokens 100 us; 300 tokens behind 60000 in 72 parts 320 us (860 uncut). Tensor pipe 52 % of active
-// clocks, capped 44 %: the softmax's instructions and the products take turns.
+// Measured (B200, 32 query and 8 kv heads of 128, a call at a time): a prompt of 8192 tokens 442 us (1.24 PFLOP/s), capped at 50 533,
+// biased 519, e4m3 600; 24 prompts of 1..700 tokens 96 us, capped 115; 300 tokens behind 60000 in 72 parts 317 us (860 uncut). Tensor
+// pipe 52 % of active clocks, capped 42 %: the softmax's instructions and the products take turns.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -77,7 +77,7 @@ constexpr int kGMinTiles = 4;    // of a part
 // with values, and with their page's scale, that may be small too. So, where weights could be below 2^-60 (C > 45, a cap above 31: kShapeLow),
 // a row whose first 64 keys together weigh less than that (as the first tokens of a prompt may, or all, if their scores lie near -C) goes
 // on at C - 100, from where it returns once 64 keys weigh more than 2^36: its largest weight is never below 2^-60. Rows whose first
-// products are small are not looked at. The code for it costs 2 % of a prompt of 8192 tokens and 6 % of 24 of 1..700, although it
+// products are small are not looked at. The code for it costs 2 % of a prompt of 8192 tokens and 4 % of 24 of 1..700, although it
 // hardly runs (instruction caches: in front of the weights it cost 5 and 15 %, as a second copy of the loop 7 and 21 %).
 constexpr float kGFixedTop = 30.f, kGFixedCap = 75.f, kGFixedFloor = 60.f, kGFixedLow = 100.f;
 constexpr float kGFixedLeast = 8.6736174e-19f, kGFixedMost = 68719476736.f;  // 2^-60, 2^36

@@ -34,7 +34,7 @@ constexpr float kAbsoluteCap = 184.f;
 
 // The cap on a score z: C - 2 C / (2^y + 1), y = 2 log2(e) z / C, whose error is a few 2^-23 C. Above kAbsoluteCap scores may be far below
 // the cap (which may be 10^8 times as large): there by the polynomial, whose error goes with the score, and only scores of 0.63 C and
-// more the first way. NaN stays, infinities give +-C. (All by the polynomial: 64 sequences of 512..4096, bf16 105 us instead of 103.)
+// more the first way. NaN stays, infinities give +-C. (All by the polynomial, decoding 64 sequences of 512..4096: 105 us instead of 103.)
 __device__ __forceinline__ float cap_score(float z, float cap, float rate) {
   constexpr float c[6] = PDA_TANH_COEFFICIENTS;
   const float y = z * rate;
