@@ -422,3 +422,36 @@ def test_decode_value_scales_of_any_size(vscale, kw):
                 byte = torch.where(per_page[pages, h // 2][:, None] > 0, v / per_page[pages, h // 2].double()[:, None], 0.0).abs()
                 step = 2.0 ** -25 * product.max() * byte.sum(0, keepdim=True) * 1.01
                 U.check(out[b:b + 1, h], ref, tol + step + 1e-38, f"{vscale} sequence {b} head {h} chunk {chunk}")
+
+
+@pytest.mark.parametrize("vscale", [1.0, 2.0 ** -30])
+def test_low_rows_of_small_heads(vscale):
+    steps = [-1.0] * 100 + [0.0] * 30 + [1.0] + [-1.0] * 170
+    for cap in (30.0, 50.0):
+        U.check(*signed_prompt(False, cap, vscale, steps, 300, D=64))
+        U.check(*signed_prompt(False, cap, vscale, [-1.0] * 400, 5, first=[0, 390, 200, 0, INT_MAX], D=64))
+
+
+def test_captured_calls_with_low_rows_and_rows_that_see_nothing():
+    """Replayed as they were captured, and with other lengths, masks and queries in the same buffers."""
+    L, n = 900, 300
+    c = U.Cache([L], 2, 128, seed=21)
+    q, lens, cu = randn(22, n, 8, 128, scale=8.0).cuda(), ints([L]), ints([0, n])
+    first = ints([INT_MAX if i % 7 == 3 else i for i in range(n)])
+    ws, out = pda.prefill_workspace(8, 128), torch.empty((n, 8, 128), dtype=torch.bfloat16, device="cuda")
+    call = lambda o: pda.paged_prefill_attention(q, c.k_cache, c.v_cache, c.dev_table, lens, cu, n, 0.5, softcap=50.0, first_keys=first, workspace=ws, out=o)
+    call(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for step in range(3):
+        if step:
+            q.copy_(randn(23 + step, n, 8, 128, scale=8.0))
+            lens.fill_(L - 100 * step)
+            cu.copy_(ints([0, n - 50 * step]))
+        out.fill_(7.0)
+        graph.replay()
+        want = torch.full_like(out, 7.0)
+        call(want)
+        assert torch.equal(out, want)
