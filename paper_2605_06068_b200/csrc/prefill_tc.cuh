@@ -746,11 +746,15 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
           bool wanted = tile >= 0 && page * kPageSize < hi_now && (page + 1) * kPageSize > lo_now;
           if (wanted && units[slot].gaps) {  // (the unit from shared memory: registers are short here)
             const GUnit& un = units[slot];
-            wanted = false;
+            const int rows = min(block_rows, un.nq - un.row0), pos0 = un.L - un.nq + un.row0;
+            // Pages before the block's first position: what begins before their end reaches past them. Others: the rows one by one, from the
+            // one that stands at the page's first key on, as mostly that one sees it.
+            wanted = (page + 1) * kPageSize <= pos0;
+            int i = static_cast<int>(min(max(page * kPageSize - pos0, static_cast<int64_t>(0)), static_cast<int64_t>(rows - 1)));
 #pragma unroll 1
-            for (int i = 0, rows = min(block_rows, un.nq - un.row0); i < rows && !wanted; ++i) {
+            for (int k = 0; k < rows && !wanted; ++k, i = i + 1 < rows ? i + 1 : 0) {
               int row_lo, row_hi;
-              visible_keys(un.L - un.nq + un.row0 + i, un.L, p.score.window, p.first_keys[un.q0 + un.row0 + i], un.prefix, row_lo, row_hi);
+              visible_keys(pos0 + i, un.L, p.score.window, p.first_keys[un.q0 + un.row0 + i], un.prefix, row_lo, row_hi);
               wanted = row_lo < row_hi && row_lo < (page + 1) * kPageSize && row_hi > page * kPageSize;
             }
           }
