@@ -688,7 +688,8 @@ int rope_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride,
  * there 0 or at least 2^-56). A row with a NaN or +inf among the scores it sees is NaN;
  * one with none above -inf is NaN or zero. L < 0 counts as 0. A sequence whose query range does not
  * lie in the arrays, that has more than max_q query tokens or more than block_table_stride * 16 or
- * 2^30 tokens is zeroed (as far as its rows lie within the array and max_q) with PDA_DEV_BAD_SEQ_LEN; rows for
+ * 2^30 tokens is zeroed (as far as its rows lie within the array and max_q; one that starts below 0 is left
+ * out) with PDA_DEV_BAD_SEQ_LEN; rows for
  * which a page id outside the cache is read are zero, with PDA_DEV_BAD_PAGE.
  * batch and num_q_heads <= 65535; the smaller of max_q and total_q times num_q_heads < 2^31. Groups of up
  * to 128 query heads with head_dim 64 and 128 run on the tensor-core kernel (tcgen05; e4m3: head_dim 128);
