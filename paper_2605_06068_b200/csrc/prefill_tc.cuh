@@ -34,9 +34,9 @@ struct PrefillPlan {
   int cut;        // few units: blocks are cut along the keys, so that every pair has a part
   float scale_log2;
   // Capped scores as polynomials of the product s (each coefficient twice, for pairs of scores): of degree 5 for
-  // |s| <= limit[0], of degree 11 for |s| <= limit[1]; u = scale / softcap. ref: the fixed reference (capped only), or 0; ref_low: that of rows with low scores,
-  // whose products are above low_limit in size. relative:
-  // poly11 is that of cap_score, in u s, times s, and scores are taken one by one.
+  // |s| <= limit[0], of degree 11 for |s| <= limit[1]; u = scale / softcap. relative: poly11 is that of cap_score, in u s, times
+  // s, and scores are taken one by one. ref: the fixed reference (capped only), or 0; ref_low: that of rows with low scores, whose
+  // products are above low_limit in size.
   float limit[2], ref, ref_low, low_limit, u;
   int relative;
   uint64_t poly5[3], poly11[6];
@@ -173,7 +173,9 @@ __device__ __noinline__ void rescale_columns(uint32_t my_o, float a) {
 // the later n1 tiles of the same head, and the first half's warps merge the two results.
 enum : int { kOneHead = 0, kTwoHeads = 1, kSplitKeys = 2 };
 struct GUnit {
-  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad, gaps;  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace; gaps: there may be keys between that no row sees
+  // tile0: first 128 keys; slot >= 0: a part (keys before key_end), its place in the workspace; gaps: there may be keys between that
+  // no row sees
+  int row0, h, q0, nq, L, prefix, tile0, n0, n1, dual, slot, key_end, bad, gaps;
   __device__ int first_row(int w, int half_rows) const { return row0 + (dual ? 0 : half_rows * w); }
   __device__ int head(int w) const { return h + (dual == kTwoHeads ? w : 0); }
   __device__ int tiles() const { return dual ? n0 + n1 : max(n0, n1); }
@@ -1175,10 +1177,10 @@ prefill_tc_kernel(const __grid_constant__ PrefillMaps maps, const __grid_constan
               }
             }
             // Scores that references are taken of. Biased ones and e4m3's are in the exponent's units: mul s + slope (j - p), the slope's
-            // part a constant for the first of 16 keys and slope times 0 .. 15 (in masked tiles the distance of each key); e4m3's that are not biased with the page's scale. They
-            // are rounded before the reference is taken from them: so a reference is a score itself, none of those it was taken of
+            // part a constant for the first of 16 keys and slope times 0 .. 15 (in masked tiles the distance of each key); e4m3's that are
+            // not biased with the page's scale. They are rounded before the reference is taken from them: so a reference is a score itself, none of those it was taken of
             // passes it, and it is raised once at most for 64 keys. (Taken from the product in the same rounding, scores of 2^30 and
-            // more passed a reference that could not be raised by so little. Costs 7 %: 508 -> 538 us biased, 577 -> 617 e4m3. A pass of its own
+            // more passed a reference that could not be raised by so little. Cost 7 %: 508 -> 538 us biased, 577 -> 617 e4m3. A pass of its own
             // for rows with such scores, beside the hot one, gained nothing: 541 and 604, 543 and 613, or, in place, 528 and 664.)
             const auto score = [&](int e) {
               if constexpr (kBias) {
